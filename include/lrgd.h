@@ -24,6 +24,9 @@
  * argument validation fails.  A wait inside a kernel that exceeds its bound makes the kernel finish
  * early and set a device status word, read back with lr_last_device_status.
  *
+ * Besides the binary model there are the operators of a many-class gate over tokens (second half of this file): token
+ * rows (lr_embed), the choice of experts (lr_route), rows kept in 8 bits (lr_ckpt8_save) and the gradients of all three.
+ *
  * There is no CPU fallback: without a usable CUDA device lr_create fails with LR_ERR_CUDA.
  */
 #ifndef LRGD_H
@@ -374,15 +377,16 @@ int lr_profile_read(lr_ctx* ctx, int32_t* launches, double* total_ms);
 /* Number of kernels this context has launched since it was created. */
 int lr_launch_count(lr_ctx* ctx, int64_t* out);
 
-/* Synchronises the device and returns in *out the device status word: LR_OK or LR_ERR_TIMEOUT.  Clears it. */
+/* Synchronises the device and returns in *out the device status word: LR_OK, LR_ERR_TIMEOUT, or LR_ERR_VALUE after lr_embed /
+ * lr_embed_grad met a token outside the table.  Clears it. */
 int lr_last_device_status(lr_ctx* ctx, int32_t* out);
 
 /*
  * Bounds check of the library's own device workspaces (no counterpart in the paper).  Every array that the kernels index
  * by a computed offset -- the per-CTA partial rows, the gradient buffer of the stopping rule, the context's velocity and
  * the optimiser scratch -- is allocated between two 256-byte guard regions filled with a fixed pattern when the context
- * is created.  lr_check_guards synchronises the device, reads the guard regions back and returns in *corrupted how many of
- * them (0..8) no longer hold the pattern: anything but 0 means a kernel wrote outside its array.  It changes nothing, so it
+ * is created (the scratch of the token-gate calls: when a call makes it grow).  lr_check_guards synchronises the device, reads
+ * the guard regions back and returns in *corrupted how many of them (two per array) no longer hold the pattern: anything but 0 means a kernel wrote outside its array.  It changes nothing, so it
  * can be called at any point between calls; the tests call it after every batch of shapes.
  */
 int lr_check_guards(lr_ctx* ctx, int32_t* corrupted);
@@ -430,6 +434,108 @@ int lr_loss_grad_noalloc(int32_t device, const float* d_X, const float* d_y, int
 
 /* Static description of a status code. */
 const char* lr_status_string(int code);
+
+/*
+ * ---------------------------------------------------------------------------------------------------------------------
+ * A many-class gate over tokens.  (No counterpart in the paper, whose model is binary and whose rows are given; these are the
+ * operators that put a logistic layer to work inside a language model, where rows come from a token table, E classes are
+ * experts of which k are used, and the rows are kept between forward and backward.)  A training step strings them together:
+ *   X = lr_embed(tokens);  lr_ckpt8_save(X);  logits = X W^T (a library matrix product);  lr_route(logits);  ... loss ...
+ *   lr_route_grad -> dlogits;  lr_ckpt8_grad(dlogits) -> grad W, grad b;  dX = dlogits W;  lr_embed_grad(dX) -> grad table
+ * Sums, probabilities, weights and gradients of parameters are fp32 whatever the storage type; matrices of rows are fp32 or
+ * bfloat16 (the *_bf16 calls; uint16 patterns, rounded to nearest even where written).  A matrix is row-major with a leading
+ * dimension ("ld...", in elements, at least its row length), so a slice of columns can be passed as it is.  Any alignment to the
+ * element size works; rows that start on 16 bytes and hold whole 16-byte groups are fastest.  Results are bit-reproducible.
+ * T (rows, tokens) may be 0 and is at most 2^31 - 1.  The gradient calls of this section use a scratch owned by the context,
+ * allocated or grown on first use: make the first call of a size outside any stream capture.
+ * Errors as above: LR_ERR_NULL, LR_ERR_SHAPE (a size, ld, k, or group count out of range), LR_ERR_ALIGNMENT (a pointer is not
+ * aligned to its element size), LR_ERR_VALUE (a scale or factor that is not finite, an unknown score or id width), LR_ERR_NOMEM.
+ */
+
+/*
+ * Token rows: d_out[t,:] = scale * d_table[id_t,:], formed in fp32 and rounded once.  d_ids: T tokens of id_bytes = 4 (int32)
+ * or 8 (int64) bytes each; the table has V rows of n columns.  A token outside [0, V) gives a row of zeros and sets the device
+ * status word to LR_ERR_VALUE (lr_last_device_status); no memory outside the table is read.  d_out must not overlap the table.
+ */
+int lr_embed(lr_ctx* ctx, const float* d_table, int64_t ld_table, const void* d_ids, int32_t id_bytes, int64_t T, int64_t V,
+             int32_t n, float scale, float* d_out, int64_t ld_out, void* stream);
+int lr_embed_bf16(lr_ctx* ctx, const uint16_t* d_table, int64_t ld_table, const void* d_ids, int32_t id_bytes, int64_t T,
+                  int64_t V, int32_t n, float scale, uint16_t* d_out, int64_t ld_out, void* stream);
+
+/*
+ * Gradient of the table: d_grad[v,:] = scale * sum over { t : id_t = v } of d_dout[t,:] (fp32 [V*n], rows packed).  With
+ * accumulate == 0 all V rows are written (zeros where no token points), otherwise the sums are added to what d_grad holds
+ * and rows of other tokens are not touched.  Positions whose token is padding_id carry no gradient (a negative padding_id:
+ * none), nor do tokens outside [0, V), which set the status word as in lr_embed.
+ * The positions are sorted by token on the device (stable) and every row is summed in the order of its positions, long runs in
+ * pieces that are joined in order: no atomics on data, the same bits for the same ids.
+ */
+int lr_embed_grad(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const float* d_dout, int64_t ld_dout, int64_t T, int64_t V,
+                  int32_t n, float scale, int64_t padding_id, int32_t accumulate, float* d_grad, void* stream);
+int lr_embed_grad_bf16(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const uint16_t* d_dout, int64_t ld_dout, int64_t T,
+                       int64_t V, int32_t n, float scale, int64_t padding_id, int32_t accumulate, float* d_grad, void* stream);
+
+/*
+ * Routing: the k best of a row's `experts` logits l, with weights.
+ *   score LR_SCORE_SIGMOID: p = 1/(1+exp(-l)), chosen by c = p + bias;   LR_SCORE_SOFTMAX: p = softmax(l), chosen by c = l + bias
+ *   (the bias, NULL or [experts], balances the load: it enters the choice only, never the weights)
+ *   groups > 1: the experts stand in that many equal groups (expert e in group e / (experts/groups)); a group is worth the sum of
+ *   its two largest c (sigmoid) or its largest c (softmax), and only the top_groups best groups keep their experts
+ *   chosen are the k largest c, in descending order, ties to the lower index (for groups as well)
+ *   weight_i = factor * p_i / (sum of the chosen p) with renorm != 0, else factor * p_i
+ * d_ids int32 [T][k], d_weights fp32 [T][k]; d_counts is NULL or int32 [experts] and receives how many tokens chose each expert.
+ * An expert whose l or c is -inf is never chosen (a mask); where fewer than k are left the slots hold id -1 and weight 0.  (The
+ * c are compared as fp32 numbers; the renormalised weights keep their ratios even where every chosen p underflows.)  A row with a NaN logit (softmax: or +inf) gets ids -1 and NaN weights.
+ * Limits: experts <= 1024, k <= 32, groups <= 32 and a divisor of experts, k <= top_groups * experts/groups.
+ */
+enum { LR_SCORE_SIGMOID = 0, LR_SCORE_SOFTMAX = 1 };
+typedef struct lr_route_opt {
+    int32_t k;
+    int32_t groups;
+    int32_t top_groups;
+    int32_t score;
+    int32_t renorm;
+    float factor;
+} lr_route_opt;
+int lr_route(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+             const float* d_bias, int32_t* d_ids, float* d_weights, int32_t* d_counts, void* stream);
+int lr_route_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+                  const float* d_bias, int32_t* d_ids, float* d_weights, int32_t* d_counts, void* stream);
+
+/*
+ * Gradient of the weights of lr_route back to the logits: d_dlogits [T][ld_d] = dL/dl from d_dweights [T][k] = dL/dweight, with
+ * the d_ids that lr_route chose and the same options (the choice itself has no gradient).  All `experts` columns are written.
+ * Ids outside [0, experts) carry none; the ids of a row are taken to be different.  d_dlogits must not overlap d_logits.
+ */
+int lr_route_grad(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+                  const int32_t* d_ids, const float* d_dweights, float* d_dlogits, int64_t ld_d, void* stream);
+int lr_route_grad_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+                       const int32_t* d_ids, const float* d_dweights, uint16_t* d_dlogits, int64_t ld_d, void* stream);
+
+/*
+ * Rows kept in 8 bits between forward and backward.  Each row is cut into groups of 128 columns (the last one may be shorter) with
+ * one scale each: a = max |x|, s = a / 127, q = rint(x * (127 / a)) in [-127, 127]; read back as q * s, so an element is off by
+ * at most a / 254 (and two roundings).  d_q int8 [T][ld_q], d_s fp32 [T][ceil(n/128)] packed.  A group whose a is below 1e-36 is
+ * kept as zeros; one with a NaN or an infinity gets the scale NaN and is read back as NaN.  n <= 2^24.
+ * Fastest where n, ld_q are multiples of 8 and d_q is 8-byte aligned (16 for lr_ckpt8_grad).
+ */
+int lr_ckpt8_save(lr_ctx* ctx, const float* d_X, int64_t ld, int64_t T, int32_t n, int8_t* d_q, int64_t ld_q, float* d_s, void* stream);
+int lr_ckpt8_save_bf16(lr_ctx* ctx, const uint16_t* d_X, int64_t ld, int64_t T, int32_t n, int8_t* d_q, int64_t ld_q, float* d_s,
+                       void* stream);
+int lr_ckpt8_load(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, float* d_X, int64_t ld,
+                  void* stream);
+int lr_ckpt8_load_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, uint16_t* d_X,
+                       int64_t ld, void* stream);
+
+/*
+ * Gradient of a C-class logistic layer z = X W^T + b from the kept rows and d_dz [T][ld_dz] = dL/dz (C columns):
+ *   d_grad_w[c*n + j] = sum_t dz[t,c] * q[t,j] * s[t,j/128],   d_grad_b[c] = sum_t dz[t,c]   (d_grad_b may be NULL)
+ * written, or with accumulate != 0 added to what they hold.  C = 1 is X^T err of the binary model.  C <= 65536.
+ */
+int lr_ckpt8_grad(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const float* d_dz,
+                  int64_t ld_dz, int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream);
+int lr_ckpt8_grad_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const uint16_t* d_dz,
+                       int64_t ld_dz, int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream);
 
 #ifdef __cplusplus
 }

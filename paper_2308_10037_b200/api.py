@@ -25,7 +25,12 @@ EXPORTS = ["lr_plan_query", "lr_create", "lr_destroy", "lr_loss_grad", "lr_fit",
            "lr_convert_bf16", "lr_loss_grad_bf16", "lr_fit_bf16", "lr_predict_bf16", "lr_plan_query_bf16",
            "lr_fit_tol_bf16", "lr_fit_opt_bf16", "lr_fit_sgd_bf16", "lr_shard_sums_bf16", "lr_set_overlap",
            "lr_fit_host_bf16", "lr_predict_host_bf16", "lr_exchange_bytes", "lr_fit_sharded", "lr_fit_sharded_bf16", "lr_fit_sharded_local", "lr_set_sm_limit",
-           "lr_set_cluster", "lr_cluster_ctas", "lr_f1_counts", "lr_check_guards"]
+           "lr_set_cluster", "lr_cluster_ctas", "lr_f1_counts", "lr_check_guards",
+           "lr_embed", "lr_embed_bf16", "lr_embed_grad", "lr_embed_grad_bf16", "lr_route", "lr_route_bf16", "lr_route_grad",
+           "lr_route_grad_bf16", "lr_ckpt8_save", "lr_ckpt8_save_bf16", "lr_ckpt8_load", "lr_ckpt8_load_bf16", "lr_ckpt8_grad",
+           "lr_ckpt8_grad_bf16"]
+
+CKPT8_GROUP = 128                                   # columns of a row that share a scale in the 8-bit form
 
 
 class LrPlan(ctypes.Structure):
@@ -38,6 +43,14 @@ class LrPlan(ctypes.Structure):
 
 class LrOpt(ctypes.Structure):
     _fields_ = [("l2", ctypes.c_float), ("momentum", ctypes.c_float), ("nesterov", ctypes.c_int32)]
+
+
+class LrRouteOpt(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_int32), ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("score", ctypes.c_int32),
+                ("renorm", ctypes.c_int32), ("factor", ctypes.c_float)]
+
+
+_SCORES = {"sigmoid": 0, "softmax": 1}              # LR_SCORE_SIGMOID, LR_SCORE_SOFTMAX
 
 
 class LrError(RuntimeError):
@@ -106,6 +119,16 @@ def lib() -> ctypes.CDLL:
         L.lr_last_cuda_error.argtypes = [P]
         L.lr_status_string.argtypes = [ctypes.c_int]
         L.lr_status_string.restype = ctypes.c_char_p
+        PO = ctypes.POINTER(LrRouteOpt)
+        L.lr_embed.argtypes = [P, P, I64, P, I32, I64, I64, I32, F, P, I64, P]
+        L.lr_embed_grad.argtypes = [P, P, I32, P, I64, I64, I64, I32, F, I64, I32, P, P]
+        L.lr_route.argtypes = [P, P, I64, I64, I32, PO, P, P, P, P, P]
+        L.lr_route_grad.argtypes = [P, P, I64, I64, I32, PO, P, P, P, I64, P]
+        L.lr_ckpt8_save.argtypes = [P, P, I64, I64, I32, P, I64, P, P]
+        L.lr_ckpt8_load.argtypes = [P, P, I64, P, I64, I32, P, I64, P]
+        L.lr_ckpt8_grad.argtypes = [P, P, I64, P, I64, I32, P, I64, I32, I32, P, P, P]
+        for name in ("lr_embed", "lr_embed_grad", "lr_route", "lr_route_grad", "lr_ckpt8_save", "lr_ckpt8_load", "lr_ckpt8_grad"):
+            getattr(L, name + "_bf16").argtypes = getattr(L, name).argtypes
         for name in EXPORTS:
             if name != "lr_status_string":
                 getattr(L, name).restype = ctypes.c_int
@@ -323,6 +346,140 @@ class Context:
         tp, fp, fn = (int(v) for v in counts.tolist())
         return (2.0 * tp / (2.0 * tp + fp + fn) if tp > 0 else 0.0), tp, fp, fn
 
+    # ---- a many-class gate over tokens -------------------------------------------------------------
+    # Matrices of rows may be slices of wider ones (any row stride, unit column stride), float32 or bfloat16.
+    def _rows(self, t, dtypes, name, shape=None):
+        """(address, rows, columns, leading dimension, entry-point suffix) of a 2-D CUDA tensor with unit column stride."""
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes):
+            raise TypeError(f"{name}: expected a CUDA tensor of dtype {' or '.join(str(d) for d in dtypes)}")
+        if t.dim() != 2 or t.shape[1] < 1:
+            raise ValueError(f"{name}: expected a 2-D tensor with at least one column")
+        rows, cols = t.shape
+        if shape is not None and (rows, cols) != shape:
+            raise ValueError(f"{name}: shape {(rows, cols)}, the call needs {shape}")
+        ld = t.stride(0) if rows > 1 else cols
+        if (cols > 1 and t.stride(1) != 1) or ld < cols:
+            raise ValueError(f"{name}: rows must be contiguous and must not overlap")
+        if t.device.index != self.device:
+            raise ValueError(f"{name}: lives on cuda:{t.device.index}, the call runs on cuda:{self.device}")
+        return t.data_ptr(), rows, cols, ld, "_bf16" if t.dtype == torch.bfloat16 else ""
+
+    def _tokens(self, ids):
+        if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dtype in (torch.int32, torch.int64) and ids.is_contiguous()):
+            raise TypeError("ids: expected a contiguous CUDA tensor of dtype torch.int32 or torch.int64")
+        if ids.device.index != self.device:
+            raise ValueError(f"ids: lives on cuda:{ids.device.index}, the call runs on cuda:{self.device}")
+        return ids.data_ptr(), 8 if ids.dtype == torch.int64 else 4, ids.numel()
+
+    def embed(self, table, ids, scale=1.0, out=None):
+        """``scale * table[ids]``: rows of a token table [V, n] (float32 or bfloat16) for int32 or int64 ``ids`` of any shape;
+        returns ``ids.shape + (n,)`` in the table's type, or writes the rows to ``out`` [T, n].  A token outside [0, V) gives zeros
+        and a device status of LR_ERR_VALUE."""
+        pt, V, n, ld, sfx = self._rows(table, (torch.float32, torch.bfloat16), "table")
+        pi, ib, T = self._tokens(ids)
+        flat = torch.empty((T, n), dtype=table.dtype, device=table.device) if out is None else out
+        po, _, _, ldo, _ = self._rows(flat, (table.dtype,), "out", (T, n))
+        rc = getattr(lib(), "lr_embed" + sfx)(self._h, pt, ld, pi, ib, T, V, n, float(scale), po, ldo, self._stream())
+        self._check(rc, "lr_embed" + sfx)
+        return flat.view(*ids.shape, n) if out is None else out
+
+    def embed_grad(self, ids, dout, rows, scale=1.0, padding_id=-1, out=None, accumulate=False):
+        """Gradient [rows, n] (float32) of the table of ``embed``: ``scale *`` the sum of ``dout`` [T, n] over the places of each
+        token, none for ``padding_id``.  With ``accumulate`` it is added to ``out``."""
+        pi, ib, T = self._tokens(ids)
+        pd, _, n, ld, sfx = self._rows(dout, (torch.float32, torch.bfloat16), "dout", (T, dout.shape[-1] if isinstance(dout, torch.Tensor) and dout.dim() else 0))
+        if out is None:
+            if accumulate:
+                raise ValueError("accumulate needs the gradient to add to as out")
+            out = torch.empty((int(rows), n), dtype=torch.float32, device=dout.device)
+        elif not isinstance(out, torch.Tensor) or out.shape != (int(rows), n):
+            raise ValueError(f"out: expected a float32 CUDA tensor of shape {(int(rows), n)}")
+        rc = getattr(lib(), "lr_embed_grad" + sfx)(self._h, pi, ib, pd, ld, T, int(rows), n, float(scale), int(padding_id),
+                                                   int(bool(accumulate)), self._p(out, torch.float32, "out"), self._stream())
+        self._check(rc, "lr_embed_grad" + sfx)
+        return out
+
+    @staticmethod
+    def _route_opt(k, groups, top_groups, score, renorm, factor):
+        if score not in _SCORES:
+            raise ValueError(f"score: expected one of {sorted(_SCORES)}")
+        return LrRouteOpt(int(k), int(groups), int(groups if top_groups is None else top_groups), _SCORES[score], int(bool(renorm)),
+                          float(factor))
+
+    def route(self, logits, k, bias=None, groups=1, top_groups=None, score="sigmoid", renorm=True, factor=1.0):
+        """The ``k`` best experts of every row of ``logits`` [T, E] (float32 or bfloat16): (ids int32 [T, k], weights float32
+        [T, k], counts int32 [E]).  ``score`` "sigmoid" or "softmax"; ``bias`` float32 [E] enters the choice only; with ``groups``
+        only the experts of the ``top_groups`` best groups (default: all) can be chosen; ``renorm`` divides by the sum of the chosen;
+        ``factor`` multiplies the weights.  See ``lr_route`` in the header for the exact rules."""
+        pl, T, E, ld, sfx = self._rows(logits, (torch.float32, torch.bfloat16), "logits")
+        opt = self._route_opt(k, groups, top_groups, score, renorm, factor)
+        pb = self._p(bias, torch.float32, "bias", E)
+        width, dev = max(opt.k, 0), logits.device
+        ids = torch.empty((T, width), dtype=torch.int32, device=dev)
+        weights = torch.empty((T, width), dtype=torch.float32, device=dev)
+        counts = torch.empty(E, dtype=torch.int32, device=dev)
+        rc = getattr(lib(), "lr_route" + sfx)(self._h, pl, ld, T, E, ctypes.byref(opt), pb, ids.data_ptr(), weights.data_ptr(),
+                                              counts.data_ptr(), self._stream())
+        self._check(rc, "lr_route" + sfx)
+        return ids, weights, counts
+
+    def route_grad(self, logits, ids, dweights, score="sigmoid", renorm=True, factor=1.0, out=None):
+        """Gradient of ``route``'s weights back to the logits: [T, E] in the logits' type from ``ids`` int32 [T, k] and ``dweights``
+        float32 [T, k]."""
+        pl, T, E, ld, sfx = self._rows(logits, (torch.float32, torch.bfloat16), "logits")
+        if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or ids.shape[0] != T or not isinstance(dweights, torch.Tensor) or dweights.shape != ids.shape:
+            raise ValueError("ids, dweights: expected two tensors [T, k]")
+        opt = self._route_opt(ids.shape[1], 1, 1, score, renorm, factor)
+        pi, pw = self._p(ids, torch.int32, "ids"), self._p(dweights, torch.float32, "dweights")
+        res = torch.empty((T, E), dtype=logits.dtype, device=logits.device) if out is None else out
+        po, _, _, ldo, _ = self._rows(res, (logits.dtype,), "out", (T, E))
+        rc = getattr(lib(), "lr_route_grad" + sfx)(self._h, pl, ld, T, E, ctypes.byref(opt), pi, pw, po, ldo, self._stream())
+        self._check(rc, "lr_route_grad" + sfx)
+        return res
+
+    def ckpt8_save(self, X):
+        """Rows ``X`` [T, n] (float32 or bfloat16) in 8 bits: (q int8 [T, n], s float32 [T, ceil(n/128)]).  The rows of ``q`` start
+        16 bytes apart or a multiple of that."""
+        px, T, n, ld, sfx = self._rows(X, (torch.float32, torch.bfloat16), "X")
+        pitch = (n + 15) // 16 * 16
+        q = torch.empty((T, pitch), dtype=torch.int8, device=X.device)
+        if pitch != n:
+            q = q[:, :n]
+        s = torch.empty((T, (n + CKPT8_GROUP - 1) // CKPT8_GROUP), dtype=torch.float32, device=X.device)
+        rc = getattr(lib(), "lr_ckpt8_save" + sfx)(self._h, px, ld, T, n, q.data_ptr(), pitch, s.data_ptr(), self._stream())
+        self._check(rc, "lr_ckpt8_save" + sfx)
+        return q, s
+
+    def _ckpt8(self, q, s):
+        pq, T, n, ld, _ = self._rows(q, (torch.int8,), "q")
+        return pq, ld, self._p(s, torch.float32, "s", T * ((n + CKPT8_GROUP - 1) // CKPT8_GROUP)), T, n
+
+    def ckpt8_load(self, q, s, dtype=torch.float32, out=None):
+        """The rows that ``ckpt8_save`` kept, in ``dtype`` (float32 or bfloat16)."""
+        pq, ldq, ps, T, n = self._ckpt8(q, s)
+        res = torch.empty((T, n), dtype=dtype, device=q.device) if out is None else out
+        po, _, _, ld, sfx = self._rows(res, (torch.float32, torch.bfloat16), "out", (T, n))
+        rc = getattr(lib(), "lr_ckpt8_load" + sfx)(self._h, pq, ldq, ps, T, n, po, ld, self._stream())
+        self._check(rc, "lr_ckpt8_load" + sfx)
+        return res
+
+    def ckpt8_grad(self, q, s, dz, grad_w=None, grad_b=None, accumulate=False):
+        """(grad_w [C, n], grad_b [C]) of a logistic layer with C outputs from the kept rows and ``dz`` [T, C] (float32 or
+        bfloat16); with ``accumulate`` added to the given ``grad_w`` and ``grad_b``."""
+        pq, ldq, ps, T, n = self._ckpt8(q, s)
+        pz, rows, C, ldz, sfx = self._rows(dz, (torch.float32, torch.bfloat16), "dz")
+        if rows != T:
+            raise ValueError(f"dz: {rows} rows, q has {T}")
+        if accumulate and (grad_w is None or grad_b is None):
+            raise ValueError("accumulate needs grad_w and grad_b to add to")
+        grad_w = torch.empty((C, n), dtype=torch.float32, device=q.device) if grad_w is None else grad_w
+        grad_b = torch.empty(C, dtype=torch.float32, device=q.device) if grad_b is None else grad_b
+        rc = getattr(lib(), "lr_ckpt8_grad" + sfx)(self._h, pq, ldq, ps, T, n, pz, ldz, C, int(bool(accumulate)),
+                                                   self._p(grad_w, torch.float32, "grad_w", C * n),
+                                                   self._p(grad_b, torch.float32, "grad_b", C), self._stream())
+        self._check(rc, "lr_ckpt8_grad" + sfx)
+        return grad_w, grad_b
+
     def shard_sums(self, X, y, w, b, sums):
         """Unnormalised fp64 sums [n+2] of the local rows into ``sums`` (float64 CUDA tensor)."""
         m, n = _shape2(X)
@@ -516,6 +673,51 @@ def lr_fit(X, y, lr, iters, w0=None, b0=None, return_history=False, ctx: Context
 def lr_predict(X, w, b, thr, ctx: Context | None = None):
     """uint8 CUDA tensor [m]: 1 where sigmoid(x.w + b) >= thr."""
     return _ctx_for(X, ctx).predict(X, w, _as_b(b, X.device), thr)
+
+
+def _ctx_of(t, ctx: Context | None) -> Context:
+    """The default context of the tensor's device, for calls whose workspace does not depend on a number of columns."""
+    if ctx is not None:
+        return ctx
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise TypeError("expected a CUDA tensor")
+    c = _default_ctx.get(t.device.index)
+    return c if c is not None else _default_ctx.setdefault(t.device.index, Context(device=t.device.index))
+
+
+def lr_embed(table, ids, scale=1.0, out=None, ctx: Context | None = None):
+    """Scaled rows of a token table (see ``Context.embed``)."""
+    return _ctx_of(table, ctx).embed(table, ids, scale, out)
+
+
+def lr_embed_grad(ids, dout, rows, scale=1.0, padding_id=-1, out=None, accumulate=False, ctx: Context | None = None):
+    """Gradient of the token table (see ``Context.embed_grad``)."""
+    return _ctx_of(dout, ctx).embed_grad(ids, dout, rows, scale, padding_id, out, accumulate)
+
+
+def lr_route(logits, k, bias=None, groups=1, top_groups=None, score="sigmoid", renorm=True, factor=1.0, ctx: Context | None = None):
+    """The k best experts of every token with their weights (see ``Context.route``)."""
+    return _ctx_of(logits, ctx).route(logits, k, bias, groups, top_groups, score, renorm, factor)
+
+
+def lr_route_grad(logits, ids, dweights, score="sigmoid", renorm=True, factor=1.0, out=None, ctx: Context | None = None):
+    """Gradient of the routing weights back to the logits (see ``Context.route_grad``)."""
+    return _ctx_of(logits, ctx).route_grad(logits, ids, dweights, score, renorm, factor, out)
+
+
+def lr_ckpt8_save(X, ctx: Context | None = None):
+    """Rows in 8 bits (see ``Context.ckpt8_save``)."""
+    return _ctx_of(X, ctx).ckpt8_save(X)
+
+
+def lr_ckpt8_load(q, s, dtype=torch.float32, out=None, ctx: Context | None = None):
+    """The rows that ``lr_ckpt8_save`` kept (see ``Context.ckpt8_load``)."""
+    return _ctx_of(q, ctx).ckpt8_load(q, s, dtype, out)
+
+
+def lr_ckpt8_grad(q, s, dz, grad_w=None, grad_b=None, accumulate=False, ctx: Context | None = None):
+    """Gradient of a C-class logistic layer from rows kept in 8 bits (see ``Context.ckpt8_grad``)."""
+    return _ctx_of(q, ctx).ckpt8_grad(q, s, dz, grad_w, grad_b, accumulate)
 
 
 LR_NOALLOC_MAX_N = 1022

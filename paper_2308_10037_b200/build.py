@@ -8,9 +8,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblrgd.so")
-SOURCES = ["lrgd_api.cu"]
+SOURCES = ["lrgd_api.cu", "lrgd_gate_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared", "-Xptxas", "-v"]
+              "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 
 
 def _newest_source_mtime() -> float:
@@ -25,12 +25,26 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     nvcc = os.environ.get("NVCC", "nvcc")
     tmp = LIB + f".tmp{os.getpid()}"
-    cmd = [nvcc, *NVCC_FLAGS, "-o", tmp, *[os.path.join(CSRC, s) for s in SOURCES]]
-    proc = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or proc.returncode != 0:
-        sys.stderr.write(proc.stdout + proc.stderr)
-    if proc.returncode != 0:
-        raise RuntimeError("nvcc failed: " + " ".join(cmd))
+    objects = [f"{tmp}.{i}.o" for i in range(len(SOURCES))]
+    compiles = [[nvcc, *NVCC_FLAGS, "-c", "-o", obj, os.path.join(CSRC, src)] for obj, src in zip(objects, SOURCES)]
+    try:
+        # the sources are compiled side by side, then linked
+        procs = [subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True) for cmd in compiles]
+        outs = [p.communicate()[0] for p in procs]
+        for cmd, proc, out in zip(compiles, procs, outs):
+            if verbose or proc.returncode != 0:
+                sys.stderr.write(out)
+            if proc.returncode != 0:
+                raise RuntimeError("nvcc failed: " + " ".join(cmd))
+        link = [nvcc, *NVCC_FLAGS, "-shared", "-o", tmp, *objects]
+        proc = subprocess.run(link, capture_output=True, text=True)
+        if proc.returncode != 0:
+            sys.stderr.write(proc.stdout + proc.stderr)
+            raise RuntimeError("nvcc failed: " + " ".join(link))
+    finally:
+        for obj in objects:
+            if os.path.exists(obj):
+                os.remove(obj)
     os.replace(tmp, LIB)
     return LIB
 

@@ -91,7 +91,7 @@ __device__ __forceinline__ bool mbar_wait_drain(uint64_t* bar, uint32_t parity) 
 
 // One warp waits on an mbarrier that is completed up front (arm != 0) or never (arm == 0), with the given limit; on
 // expiry it sets the status word exactly as the streaming kernels do.  Used to exercise the give-up path on purpose.
-__global__ void k_wait_probe(int* status, unsigned long long limit_ns, int arm) {
+static __global__ void k_wait_probe(int* status, unsigned long long limit_ns, int arm) {
     __shared__ uint64_t bar;
     __shared__ int abort_flag;
     if (threadIdx.x == 0) {

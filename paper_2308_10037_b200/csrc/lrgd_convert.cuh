@@ -19,7 +19,7 @@ __device__ __forceinline__ unsigned short bf16_bits_rne(float x) {
 
 // vec != 0: src is 16-byte aligned and dst 8-byte aligned, so four elements move per load/store; the tail of a count
 // that is not a multiple of four is done element by element by the thread that owns it.
-__global__ void __launch_bounds__(kConvertThreads) k_convert_bf16(const float* __restrict__ src, long long count,
+static __global__ void __launch_bounds__(kConvertThreads) k_convert_bf16(const float* __restrict__ src, long long count,
                                                                   unsigned short* __restrict__ dst, int vec) {
     const long long tid = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x;
     const long long nthreads = static_cast<long long>(gridDim.x) * blockDim.x;

@@ -1,0 +1,379 @@
+// C-ABI layer of the token-gate operators: routing, token rows, rows kept in 8 bits, and their gradients.
+// The declarations and their contracts are in include/lrgd.h.
+#include "../../include/lrgd.h"
+
+#include <cmath>
+#include <new>
+#include <type_traits>
+
+#include "lrgd_ckpt8.cuh"
+#include "lrgd_ctx.cuh"
+#include "lrgd_embed.cuh"
+#include "lrgd_route.cuh"
+
+using namespace lrgd;
+
+namespace {
+
+constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;   // positions are sorted as 32-bit numbers
+constexpr int64_t kMaxLd = int64_t(1) << 40;
+
+// The context's scratch for these calls, between guard regions, grown when a call needs more than any before it.  What it
+// outgrew is kept until lr_destroy: a captured graph may still point there.  Growing by half at least bounds the sum.
+int gate_scratch(lr_ctx* ctx, size_t need) {
+    if (ctx->scratch_bytes >= need) return LR_OK;
+    need = std::max(need, ctx->scratch_bytes + ctx->scratch_bytes / 2);
+    need = (need + (size_t(1) << 20) - 1) >> 20 << 20;
+    try {
+        ctx->guard_bases.reserve(ctx->guard_bases.size() + 1);
+        ctx->guard_sizes.reserve(ctx->guard_sizes.size() + 1);
+    } catch (const std::bad_alloc&) {
+        return LR_ERR_NOMEM;
+    }
+    unsigned char* fresh = nullptr;
+    const cudaError_t e = guarded_alloc(ctx, &fresh, need);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        ctx->last_cuda = int(e);
+        return e == cudaErrorMemoryAllocation ? LR_ERR_NOMEM : LR_ERR_CUDA;
+    }
+    ctx->d_scratch = fresh;
+    ctx->scratch_bytes = need;
+    return LR_OK;
+}
+
+template <class K>
+int launched(lr_ctx* ctx, K&& launch) {
+    launch();
+    LR_CK(ctx, cudaGetLastError());
+    ctx->launches += 1;
+    return LR_OK;
+}
+
+int grid_for(const lr_ctx* ctx, int64_t units, int64_t per_cta, int per_sm) {
+    return int(std::max<int64_t>(1, std::min<int64_t>((units + per_cta - 1) / per_cta, int64_t(plan_sms(ctx)) * per_sm)));
+}
+
+int check_route(int64_t T, int32_t E, int64_t ld, const lr_route_opt* o) {
+    if (!o) return LR_ERR_NULL;
+    if (T < 0 || T > kMaxTokens || E < 1 || E > kRouteMaxExperts || ld < E || ld > kMaxLd) return LR_ERR_SHAPE;
+    if (o->k < 1 || o->k > kRouteMaxK) return LR_ERR_SHAPE;
+    if (o->score != LR_SCORE_SIGMOID && o->score != LR_SCORE_SOFTMAX) return LR_ERR_VALUE;
+    if (!std::isfinite(o->factor)) return LR_ERR_VALUE;
+    if (o->groups < 1 || o->groups > kRouteMaxGroups || E % o->groups || o->top_groups < 1 || o->top_groups > o->groups) return LR_ERR_SHAPE;
+    if (int64_t(o->k) > int64_t(E / o->groups) * o->top_groups) return LR_ERR_SHAPE;
+    return LR_OK;
+}
+
+// f(std::integral_constant<int, VPL>) for the number of experts a lane holds
+template <class F>
+void for_vpl(int E, F&& f) {
+    if (E <= 64) f(std::integral_constant<int, 2>{});
+    else if (E <= 128) f(std::integral_constant<int, 4>{});
+    else if (E <= 256) f(std::integral_constant<int, 8>{});
+    else if (E <= 512) f(std::integral_constant<int, 16>{});
+    else f(std::integral_constant<int, 32>{});
+}
+
+template <class E>
+int route_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt, const float* d_bias,
+               int32_t* d_ids, float* d_weights, int32_t* d_counts, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_route(T, experts, ld, opt);
+    if (rc != LR_OK) return rc;
+    if (T > 0 && (!d_logits || !d_ids || !d_weights)) return LR_ERR_NULL;
+    if (!aligned(d_logits, sizeof(E)) || !aligned(d_bias, 4) || !aligned(d_ids, 4) || !aligned(d_weights, 4) || !aligned(d_counts, 4))
+        return LR_ERR_ALIGNMENT;
+    NvtxRange range("lr_route");
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        if (d_counts) LR_CK(ctx, cudaMemsetAsync(d_counts, 0, size_t(experts) * 4, st));
+        return LR_OK;
+    }
+    const RouteParams p{d_logits, ld, T, experts, opt->k, opt->groups, opt->top_groups, opt->renorm != 0, opt->factor,
+                        d_bias, d_ids, d_weights, d_counts, ctx->d_gate_words};
+    const int grid = grid_for(ctx, T, kRouteWarps, 8);
+    return launched(ctx, [&] {
+        for_vpl(experts, [&](auto vpl) {
+            constexpr int VPL = decltype(vpl)::value;
+            const bool grouped = opt->top_groups < opt->groups;    // all groups kept: no need to look at them
+            if (opt->score == LR_SCORE_SOFTMAX) {
+                if (grouped) k_route<E, VPL, true, true><<<grid, kRouteThreads, 0, st>>>(p);
+                else k_route<E, VPL, true, false><<<grid, kRouteThreads, 0, st>>>(p);
+            } else {
+                if (grouped) k_route<E, VPL, false, true><<<grid, kRouteThreads, 0, st>>>(p);
+                else k_route<E, VPL, false, false><<<grid, kRouteThreads, 0, st>>>(p);
+            }
+        });
+    });
+}
+
+template <class E>
+int route_grad_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+                    const int32_t* d_ids, const float* d_dweights, E* d_dlogits, int64_t ld_d, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_route(T, experts, ld, opt);
+    if (rc != LR_OK) return rc;
+    if (ld_d < experts || ld_d > kMaxLd) return LR_ERR_SHAPE;
+    if (T == 0) return LR_OK;
+    if (!d_logits || !d_ids || !d_dweights || !d_dlogits) return LR_ERR_NULL;
+    if (!aligned(d_logits, sizeof(E)) || !aligned(d_ids, 4) || !aligned(d_dweights, 4) || !aligned(d_dlogits, sizeof(E))) return LR_ERR_ALIGNMENT;
+    NvtxRange range("lr_route_grad");
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const RouteGradParams p{d_logits, ld, T, experts, opt->k, opt->renorm != 0, opt->factor, d_ids, d_dweights, d_dlogits, ld_d};
+    const int grid = grid_for(ctx, T, kRouteWarps, 8);
+    return launched(ctx, [&] {
+        for_vpl(experts, [&](auto vpl) {
+            constexpr int VPL = decltype(vpl)::value;
+            if (opt->score == LR_SCORE_SOFTMAX) k_route_grad<E, VPL, true><<<grid, kRouteThreads, 0, st>>>(p);
+            else k_route_grad<E, VPL, false><<<grid, kRouteThreads, 0, st>>>(p);
+        });
+    });
+}
+
+int check_tokens(int64_t T, int64_t V, int32_t n, int32_t id_bytes) {
+    if (T < 0 || T > kMaxTokens || V < 1 || V >= kMaxTokens || n < 1) return LR_ERR_SHAPE;
+    if (id_bytes != 4 && id_bytes != 8) return LR_ERR_VALUE;
+    return LR_OK;
+}
+
+template <class E>
+int embed_impl(lr_ctx* ctx, const E* d_table, int64_t ld_table, const void* d_ids, int32_t id_bytes, int64_t T, int64_t V, int32_t n,
+               float scale, E* d_out, int64_t ld_out, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_tokens(T, V, n, id_bytes);
+    if (rc != LR_OK) return rc;
+    if (ld_table < n || ld_table > kMaxLd || ld_out < n || ld_out > kMaxLd) return LR_ERR_SHAPE;
+    if (!std::isfinite(scale)) return LR_ERR_VALUE;
+    if (T == 0) return LR_OK;
+    if (!d_table || !d_ids || !d_out) return LR_ERR_NULL;
+    if (!aligned(d_table, sizeof(E)) || !aligned(d_out, sizeof(E)) || !aligned(d_ids, id_bytes)) return LR_ERR_ALIGNMENT;
+    NvtxRange range("lr_embed");
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const EmbedParams p{d_table, ld_table, d_ids, T, V, n, scale, d_out, ld_out, ctx->d_status};
+    auto fits = [&](int64_t vec) {     // vectors of `vec` elements: every row of both matrices starts on one and holds whole ones
+        const size_t b = size_t(vec) * sizeof(E);
+        return n % vec == 0 && ld_table % vec == 0 && ld_out % vec == 0 && aligned(d_table, b) && aligned(d_out, b);
+    };
+    auto go = [&](auto vec) {
+        constexpr int VEC = decltype(vec)::value;
+        const int64_t pieces = (int64_t(n) + 128 * VEC - 1) / (128 * VEC);
+        if (pieces > 65535) return int(LR_ERR_SHAPE);
+        const dim3 grid(unsigned(grid_for(ctx, T, kEmbedThreads / 32, std::max<int>(1, int(32 / pieces)))), unsigned(pieces));
+        return launched(ctx, [&] {
+            if (id_bytes == 8) k_embed<E, VEC, long long><<<grid, kEmbedThreads, 0, st>>>(p);
+            else k_embed<E, VEC, int><<<grid, kEmbedThreads, 0, st>>>(p);
+        });
+    };
+    if (fits(16 / int(sizeof(E)))) return go(std::integral_constant<int, 16 / int(sizeof(E))>{});
+    if (sizeof(E) == 2 && fits(2)) return go(std::integral_constant<int, 2>{});
+    return go(std::integral_constant<int, 1>{});
+}
+
+template <class E>
+int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d_dout, int64_t ld_dout, int64_t T, int64_t V, int32_t n,
+                    float scale, int64_t padding_id, int32_t accumulate, float* d_grad, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_tokens(T, V, n, id_bytes);
+    if (rc != LR_OK) return rc;
+    if (ld_dout < n || ld_dout > kMaxLd) return LR_ERR_SHAPE;
+    if (!std::isfinite(scale)) return LR_ERR_VALUE;
+    if (!d_grad || (T > 0 && (!d_ids || !d_dout))) return LR_ERR_NULL;
+    if (!aligned(d_grad, 4) || !aligned(d_dout, sizeof(E)) || !aligned(d_ids, id_bytes)) return LR_ERR_ALIGNMENT;
+    NvtxRange range("lr_embed_grad");
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        if (!accumulate) LR_CK(ctx, cudaMemsetAsync(d_grad, 0, size_t(V) * n * 4, st));
+        return LR_OK;
+    }
+    const int R = T >= 8192 ? 64 : T >= 1024 ? 32 : 16;
+    const int64_t chunks = (T + R - 1) / R;
+    auto up = [](size_t b) { return (b + 255) / 256 * 256; };
+    const size_t list = up(size_t(T) * 4), split = up(size_t(chunks) * 4), piece = size_t(2) * chunks * n * 4;
+    const int rs = gate_scratch(ctx, 4 * list + split + piece);
+    if (rs != LR_OK) return rs;
+    unsigned char* w = ctx->d_scratch;
+    SortParams sp{};
+    sp.ids = d_ids;
+    sp.T = unsigned(T);
+    sp.V = V;
+    sp.padding = padding_id;
+    for (int i = 0; i < 2; ++i) {
+        sp.key[i] = reinterpret_cast<unsigned int*>(w + 2 * i * list);
+        sp.pos[i] = reinterpret_cast<unsigned int*>(w + (2 * i + 1) * list);
+    }
+    sp.passes = V < (int64_t(1) << 8) ? 1 : V < (int64_t(1) << 16) ? 2 : V < (int64_t(1) << 24) ? 3 : 4;   // keys 0..V
+    sp.status = ctx->d_status;
+    sp.zero = accumulate ? nullptr : d_grad;
+    sp.zero_count = accumulate ? 0 : V * n;
+    int clusters = 1;
+    if (!accumulate) {
+        const int64_t want = (sp.zero_count / 4 + kSortThreads * kSortCtas * 4 - 1) / (kSortThreads * kSortCtas * 4);
+        clusters += int(std::max<int64_t>(1, std::min<int64_t>(want, plan_sms(ctx) * 2 / kSortCtas)));
+    }
+    int r = launched(ctx, [&] {
+        if (id_bytes == 8) k_token_sort<long long><<<clusters * kSortCtas, kSortThreads, 0, st>>>(sp);
+        else k_token_sort<int><<<clusters * kSortCtas, kSortThreads, 0, st>>>(sp);
+    });
+    if (r != LR_OK) return r;
+    const int last = (sp.passes - 1) & 1;
+    RunParams rp{sp.key[last], sp.pos[last], unsigned(T), unsigned(V), R, d_dout, ld_dout, n, scale, accumulate != 0, d_grad,
+                 reinterpret_cast<float*>(w + 4 * list + split), reinterpret_cast<unsigned int*>(w + 4 * list)};
+    auto go = [&](auto vec) {
+        constexpr int VEC = decltype(vec)::value;
+        const int64_t slices = (int64_t(n) + RunCols<E, VEC>::kSlice - 1) / RunCols<E, VEC>::kSlice;
+        if (slices > 65535) return int(LR_ERR_SHAPE);
+        const dim3 grid{unsigned(chunks), unsigned(slices), 1u};
+        r = launched(ctx, [&] { k_run_sum<E, VEC><<<grid, kRunThreads, 0, st>>>(rp); });
+        if (r != LR_OK) return r;
+        return launched(ctx, [&] { k_run_join<E, VEC><<<grid, kRunThreads, 0, st>>>(rp); });
+    };
+    constexpr int kVec = 16 / int(sizeof(E));
+    if (n % kVec == 0 && ld_dout % kVec == 0 && aligned(d_dout, 16) && aligned(d_grad, 16)) return go(std::integral_constant<int, kVec>{});
+    return go(std::integral_constant<int, 1>{});
+}
+
+int check_ckpt(int64_t T, int32_t n, int64_t ld_q) {
+    if (T < 0 || T > kMaxTokens || n < 1 || n > (1 << 24) || ld_q < n || ld_q > kMaxLd) return LR_ERR_SHAPE;
+    return LR_OK;
+}
+
+template <class E>
+int ckpt8_move(lr_ctx* ctx, bool save, const E* x, E* back, int64_t ld, int64_t T, int32_t n, int8_t* q, int64_t ld_q, float* s, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_ckpt(T, n, ld_q);
+    if (rc != LR_OK) return rc;
+    if (ld < n || ld > kMaxLd) return LR_ERR_SHAPE;
+    if (T == 0) return LR_OK;
+    const E* rows = save ? x : back;
+    if (!rows || !q || !s) return LR_ERR_NULL;
+    if (!aligned(rows, sizeof(E)) || !aligned(s, 4)) return LR_ERR_ALIGNMENT;
+    NvtxRange range(save ? "lr_ckpt8_save" : "lr_ckpt8_load");
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int groups = (n + kCkptGroup - 1) / kCkptGroup;
+    const CkptParams p{x, back, ld, q, ld_q, s, T, n, groups};
+    const bool vec = n % 8 == 0 && ld % (16 / int(sizeof(E))) == 0 && ld_q % 8 == 0 && aligned(rows, 16) && aligned(q, 8);
+    const int grid = grid_for(ctx, T * groups, kCkptThreads / 16, 16);
+    return launched(ctx, [&] {
+        if (save) {
+            if (vec) k_ckpt8_save<E, true><<<grid, kCkptThreads, 0, st>>>(p);
+            else k_ckpt8_save<E, false><<<grid, kCkptThreads, 0, st>>>(p);
+        } else {
+            if (vec) k_ckpt8_load<E, true><<<grid, kCkptThreads, 0, st>>>(p);
+            else k_ckpt8_load<E, false><<<grid, kCkptThreads, 0, st>>>(p);
+        }
+    });
+}
+
+template <class E>
+int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const E* d_dz, int64_t ld_dz,
+                    int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_ckpt(T, n, ld_q);
+    if (rc != LR_OK) return rc;
+    if (C < 1 || C > 65536 || ld_dz < C || ld_dz > kMaxLd) return LR_ERR_SHAPE;
+    if (!d_grad_w || (T > 0 && (!d_q || !d_s || !d_dz))) return LR_ERR_NULL;
+    if (!aligned(d_s, 4) || !aligned(d_dz, sizeof(E)) || !aligned(d_grad_w, 4) || !aligned(d_grad_b, 4)) return LR_ERR_ALIGNMENT;
+    NvtxRange range("lr_ckpt8_grad");
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        if (!accumulate) {
+            LR_CK(ctx, cudaMemsetAsync(d_grad_w, 0, size_t(C) * n * 4, st));
+            if (d_grad_b) LR_CK(ctx, cudaMemsetAsync(d_grad_b, 0, size_t(C) * 4, st));
+        }
+        return LR_OK;
+    }
+    const int groups = (n + kCkptGroup - 1) / kCkptGroup;
+    const int cblocks = (C + kGradClasses - 1) / kGradClasses;
+    int64_t chunks = std::max<int64_t>(1, int64_t(plan_sms(ctx)) * 8 / (int64_t(groups) * cblocks));
+    int64_t rows = std::max<int64_t>((T + chunks - 1) / chunks, kGradTile);
+    chunks = (T + rows - 1) / rows;
+    const size_t part_w = (size_t(chunks) * C * n * 4 + 255) / 256 * 256, part_b = size_t(chunks) * C * 4;
+    const int rs = gate_scratch(ctx, part_w + part_b);
+    if (rs != LR_OK) return rs;
+    const CkptGradParams p{d_q, ld_q, d_s, T, n, groups, d_dz, ld_dz, C, int(chunks), rows, accumulate != 0,
+                           reinterpret_cast<float*>(ctx->d_scratch), reinterpret_cast<float*>(ctx->d_scratch + part_w), d_grad_w, d_grad_b};
+    int r = launched(ctx, [&] { k_ckpt8_grad<E><<<dim3(unsigned(groups), unsigned(cblocks), unsigned(chunks)), kCkptGroup, 0, st>>>(p); });
+    if (r != LR_OK) return r;
+    return launched(ctx, [&] { k_ckpt8_join<<<grid_for(ctx, int64_t(C) * n + C, kCkptThreads, 8), kCkptThreads, 0, st>>>(p); });
+}
+
+// bfloat16 is the unsigned 16-bit pattern of the interface
+using u16 = unsigned short;
+const u16* bf(const uint16_t* p) { return reinterpret_cast<const u16*>(p); }
+u16* bf(uint16_t* p) { return reinterpret_cast<u16*>(p); }
+
+}  // namespace
+
+extern "C" {
+
+int lr_embed(lr_ctx* ctx, const float* d_table, int64_t ld_table, const void* d_ids, int32_t id_bytes, int64_t T, int64_t V, int32_t n,
+             float scale, float* d_out, int64_t ld_out, void* stream) {
+    return embed_impl<float>(ctx, d_table, ld_table, d_ids, id_bytes, T, V, n, scale, d_out, ld_out, stream);
+}
+int lr_embed_bf16(lr_ctx* ctx, const uint16_t* d_table, int64_t ld_table, const void* d_ids, int32_t id_bytes, int64_t T, int64_t V,
+                  int32_t n, float scale, uint16_t* d_out, int64_t ld_out, void* stream) {
+    return embed_impl<u16>(ctx, bf(d_table), ld_table, d_ids, id_bytes, T, V, n, scale, bf(d_out), ld_out, stream);
+}
+int lr_embed_grad(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const float* d_dout, int64_t ld_dout, int64_t T, int64_t V, int32_t n,
+                  float scale, int64_t padding_id, int32_t accumulate, float* d_grad, void* stream) {
+    return embed_grad_impl<float>(ctx, d_ids, id_bytes, d_dout, ld_dout, T, V, n, scale, padding_id, accumulate, d_grad, stream);
+}
+int lr_embed_grad_bf16(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const uint16_t* d_dout, int64_t ld_dout, int64_t T, int64_t V,
+                       int32_t n, float scale, int64_t padding_id, int32_t accumulate, float* d_grad, void* stream) {
+    return embed_grad_impl<u16>(ctx, d_ids, id_bytes, bf(d_dout), ld_dout, T, V, n, scale, padding_id, accumulate, d_grad, stream);
+}
+
+int lr_route(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt, const float* d_bias,
+             int32_t* d_ids, float* d_weights, int32_t* d_counts, void* stream) {
+    return route_impl<float>(ctx, d_logits, ld, T, experts, opt, d_bias, d_ids, d_weights, d_counts, stream);
+}
+int lr_route_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+                  const float* d_bias, int32_t* d_ids, float* d_weights, int32_t* d_counts, void* stream) {
+    return route_impl<u16>(ctx, bf(d_logits), ld, T, experts, opt, d_bias, d_ids, d_weights, d_counts, stream);
+}
+int lr_route_grad(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+                  const int32_t* d_ids, const float* d_dweights, float* d_dlogits, int64_t ld_d, void* stream) {
+    return route_grad_impl<float>(ctx, d_logits, ld, T, experts, opt, d_ids, d_dweights, d_dlogits, ld_d, stream);
+}
+int lr_route_grad_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t experts, const lr_route_opt* opt,
+                       const int32_t* d_ids, const float* d_dweights, uint16_t* d_dlogits, int64_t ld_d, void* stream) {
+    return route_grad_impl<u16>(ctx, bf(d_logits), ld, T, experts, opt, d_ids, d_dweights, bf(d_dlogits), ld_d, stream);
+}
+
+int lr_ckpt8_save(lr_ctx* ctx, const float* d_X, int64_t ld, int64_t T, int32_t n, int8_t* d_q, int64_t ld_q, float* d_s, void* stream) {
+    return ckpt8_move<float>(ctx, true, d_X, nullptr, ld, T, n, d_q, ld_q, d_s, stream);
+}
+int lr_ckpt8_save_bf16(lr_ctx* ctx, const uint16_t* d_X, int64_t ld, int64_t T, int32_t n, int8_t* d_q, int64_t ld_q, float* d_s,
+                       void* stream) {
+    return ckpt8_move<u16>(ctx, true, bf(d_X), nullptr, ld, T, n, d_q, ld_q, d_s, stream);
+}
+int lr_ckpt8_load(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, float* d_X, int64_t ld, void* stream) {
+    return ckpt8_move<float>(ctx, false, nullptr, d_X, ld, T, n, const_cast<int8_t*>(d_q), ld_q, const_cast<float*>(d_s), stream);
+}
+int lr_ckpt8_load_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, uint16_t* d_X, int64_t ld,
+                       void* stream) {
+    return ckpt8_move<u16>(ctx, false, nullptr, bf(d_X), ld, T, n, const_cast<int8_t*>(d_q), ld_q, const_cast<float*>(d_s), stream);
+}
+int lr_ckpt8_grad(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const float* d_dz, int64_t ld_dz,
+                  int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream) {
+    return ckpt8_grad_impl<float>(ctx, d_q, ld_q, d_s, T, n, d_dz, ld_dz, C, accumulate, d_grad_w, d_grad_b, stream);
+}
+int lr_ckpt8_grad_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const uint16_t* d_dz,
+                       int64_t ld_dz, int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream) {
+    return ckpt8_grad_impl<u16>(ctx, d_q, ld_q, d_s, T, n, bf(d_dz), ld_dz, C, accumulate, d_grad_w, d_grad_b, stream);
+}
+
+}  // extern "C"

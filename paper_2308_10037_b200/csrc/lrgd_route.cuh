@@ -1,0 +1,300 @@
+// Routing of tokens to experts: the k best of a gate's E logits per token, with weights, and the gradient of the weights.
+//
+//   sigmoid:  p_e = 1/(1+exp(-l_e)),                 chosen by  c_e = p_e + bias_e
+//   softmax:  p_e = exp(l_e)/sum_j exp(l_j),         chosen by  c_e = l_e + bias_e   (the order of p, without its rounding)
+//   groups:   the experts stand in `groups` equal groups; a group is worth the sum of its two largest c (sigmoid) or its largest
+//             c (softmax); the `top_groups` best groups keep their experts
+//   the k largest c among the kept ones, ties to the lower index; w_i = factor * p_i / sum of the chosen p  (or factor * p_i)
+//
+// An expert whose logit or choice value is -inf is never chosen; where fewer than k remain, the slots hold id -1 and weight 0.
+// A row with a NaN (softmax: or +inf) has ids -1 and NaN weights.
+//
+// The comparisons are on integers (a float's bits mapped so that their unsigned order is the float order), so the
+// choice is exact given the c values.  One warp per token, expert e in lane e % 32: a row is read once, coalesced, at any alignment.
+#pragma once
+#include "lrgd_convert.cuh"
+
+namespace lrgd {
+
+constexpr int kRouteThreads = 256;
+constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr int kRouteMaxExperts = 1024;
+constexpr int kRouteMaxK = 32;
+constexpr int kRouteMaxGroups = 32;
+
+struct RouteParams {
+    const void* logits;
+    long long ld;
+    long long T;
+    int E;
+    int k;
+    int groups;
+    int top_groups;
+    int renorm;
+    float factor;
+    const float* bias;         // nullable
+    int* ids;
+    float* weights;
+    int* counts;               // nullable
+    unsigned int* words;       // [kRouteMaxExperts + 1] zero on entry and on exit: running counts, then the ticket
+};
+
+struct RouteGradParams {
+    const void* logits;
+    long long ld;
+    long long T;
+    int E;
+    int k;
+    int renorm;
+    float factor;
+    const int* ids;
+    const float* dweights;
+    void* dlogits;
+    long long ld_d;
+};
+
+__device__ __forceinline__ float load_as_float(const float* p) { return __ldg(p); }
+__device__ __forceinline__ float load_as_float(const unsigned short* p) { return __uint_as_float(static_cast<uint32_t>(__ldg(p)) << 16); }
+__device__ __forceinline__ void store_from_float(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_from_float(unsigned short* p, float v) { *p = bf16_bits_rne(v); }
+
+__device__ __forceinline__ uint32_t order_key(float v) {
+    const uint32_t u = __float_as_uint(v);
+    return u ^ ((u >> 31) ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
+    return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+    return v;
+}
+// The sigmoid as it is written: the choice compares these values, so their rounding is part of the definition.
+__device__ __forceinline__ float plain_sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+
+// Sigmoids that are only needed relative to one another: sigmoid(x) * exp(-m) = 1 / (exp(m) + exp(m - x)) with m the largest
+// chosen logit, at most 0.  With m = 0 it is the sigmoid itself; where all chosen ones would underflow, their ratio is kept.
+// x = -inf (no expert) gives 0.
+__device__ __forceinline__ float sigmoid_shift(float x) { return fminf(warp_max(x), 0.0f); }
+__device__ __forceinline__ float relative_sigmoid(float x, float m) {
+    return x > -INFINITY ? 1.0f / (expf(m) + expf(m - x)) : 0.0f;
+}
+
+// keys of order_key are above 0, which stands for "not to be chosen"
+
+// VPL: experts per lane (E <= 32 * VPL).
+template <class E, int VPL, bool SOFTMAX, bool GROUPED>
+__global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__ RouteParams p) {
+    __shared__ int hist[VPL * 32];
+    __shared__ float row_choice[GROUPED ? kRouteWarps : 1][GROUPED ? VPL * 32 : 1];
+    __shared__ unsigned int last_cta;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    constexpr uint32_t kAll = 0xffffffffu;
+    if (p.counts) {
+        for (int e = threadIdx.x; e < p.E; e += kRouteThreads) hist[e] = 0;
+        __syncthreads();
+    }
+    const int group_size = p.E / p.groups;
+    for (long long t = static_cast<long long>(blockIdx.x) * kRouteWarps + warp; t < p.T; t += static_cast<long long>(gridDim.x) * kRouteWarps) {
+        const E* row = static_cast<const E*>(p.logits) + t * p.ld;
+        uint32_t key[VPL];
+        float row_max = -INFINITY;
+        bool bad = false;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int e = j * 32 + lane;
+            key[j] = 0;
+            float c = -INFINITY;
+            if (e < p.E) {
+                const float x = load_as_float(row + e);
+                bad |= SOFTMAX ? !(x < INFINITY) : x != x;
+                if constexpr (SOFTMAX) row_max = fmaxf(row_max, x);
+                c = (SOFTMAX ? x : plain_sigmoid(x)) + (p.bias ? __ldg(p.bias + e) : 0.0f);
+                if (!(x > -INFINITY) || !(c > -INFINITY)) c = -INFINITY;
+                else key[j] = order_key(c);
+            }
+            if constexpr (GROUPED) row_choice[warp][e] = c;
+        }
+        bad = __any_sync(kAll, bad);
+        if constexpr (GROUPED) {
+            __syncwarp();
+            // 32 / groups lanes per group find its two largest values, then the first of them collects the others' pairs
+            const int per = 32 / p.groups, g = lane / per, sub = lane - g * per;
+            float v1 = -INFINITY, v2 = -INFINITY;
+            if (g < p.groups)
+                for (int i = sub; i < group_size; i += per) {
+                    const float c = row_choice[warp][g * group_size + i];
+                    v2 = fmaxf(v2, fminf(v1, c));
+                    v1 = fmaxf(v1, c);
+                }
+            float a1 = v1, a2 = v2;
+            for (int i = 1; i < per; ++i) {
+                const float o1 = __shfl_sync(kAll, v1, (lane + i) & 31), o2 = __shfl_sync(kAll, v2, (lane + i) & 31);
+                a2 = fmaxf(fmaxf(fminf(a1, o1), a2), o2);
+                a1 = fmaxf(a1, o1);
+            }
+            // what lane h < groups holds now: the worth of group h, 0 if it has no expert to choose
+            a1 = __shfl_sync(kAll, a1, (lane * per) & 31);
+            a2 = __shfl_sync(kAll, a2, (lane * per) & 31);
+            const float worth = SOFTMAX || !(a2 > -INFINITY) ? a1 : a1 + a2;
+            const uint32_t wkey = lane < p.groups && a1 > -INFINITY ? order_key(worth + 0.0f) : 0u;
+            int better = 0;
+            for (int h = 0; h < p.groups; ++h) {
+                const uint32_t o = __shfl_sync(kAll, wkey, h);
+                better += o > wkey || (o == wkey && h < lane);
+            }
+            const uint32_t kept = __ballot_sync(kAll, lane < p.groups && better < p.top_groups);
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) {
+                const int e = j * 32 + lane;
+                if (e < p.E && !((kept >> (e / group_size)) & 1u)) key[j] = 0;
+            }
+            __syncwarp();                           // the next token's values go to the same place
+        }
+        uint32_t best = 0;
+        int slot = 0;
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+            if (key[j] > best) { best = key[j]; slot = j; }
+        int my_id = -1;
+        for (int r = 0; r < p.k; ++r) {
+            const uint32_t top = __reduce_max_sync(kAll, best);
+            if (top == 0) break;
+            const unsigned int e = __reduce_min_sync(kAll, best == top ? unsigned(slot * 32 + lane) : 0xffffffffu);
+            if (lane == r) my_id = int(e);
+            if (lane == int(e & 31u)) {
+                best = 0;
+                const int gone = slot;
+#pragma unroll
+                for (int j = 0; j < VPL; ++j) {
+                    if (j == gone) key[j] = 0;
+                    if (key[j] > best) { best = key[j]; slot = j; }
+                }
+            }
+        }
+        // lane r < k holds the r-th expert: its probability again from the logit
+        if (bad) my_id = -1;
+        float w = 0.0f;
+        if constexpr (SOFTMAX) {
+            float total = 1.0f, shift = 0.0f;
+            if (p.renorm) {                         // the sum over the row cancels: exp relative to the largest chosen logit
+                const float x = my_id >= 0 ? load_as_float(row + my_id) : -INFINITY;
+                shift = warp_max(x);
+                w = my_id >= 0 ? expf(x - shift) : 0.0f;
+                total = warp_sum(w);
+            } else {
+                shift = warp_max(row_max);
+                float s = 0.0f;
+#pragma unroll
+                for (int j = 0; j < VPL; ++j) {
+                    const int e = j * 32 + lane;
+                    if (e < p.E) s += expf(load_as_float(row + e) - shift);
+                }
+                total = warp_sum(s);
+                w = my_id >= 0 ? expf(load_as_float(row + my_id) - shift) : 0.0f;
+            }
+            w = my_id >= 0 ? w / total : 0.0f;
+        } else {
+            const float x = my_id >= 0 ? load_as_float(row + my_id) : -INFINITY;
+            w = p.renorm ? relative_sigmoid(x, sigmoid_shift(x)) : plain_sigmoid(x);
+            if (p.renorm) {
+                const float total = warp_sum(w);
+                w = total > 0.0f ? w / total : 0.0f;   // no expert chosen: 0
+            }
+        }
+        if (lane < p.k) {
+            p.ids[t * p.k + lane] = my_id;
+            p.weights[t * p.k + lane] = bad ? __int_as_float(0x7fc00000) : w * p.factor;
+            if (p.counts && my_id >= 0) atomicAdd(hist + my_id, 1);
+        }
+    }
+    if (!p.counts) return;
+    __syncthreads();
+    if (gridDim.x == 1) {
+        for (int e = threadIdx.x; e < p.E; e += kRouteThreads) p.counts[e] = hist[e];
+        return;
+    }
+    // integer sums: their order does not matter.  The CTA that finishes last hands the totals over and leaves the words at zero.
+    for (int e = threadIdx.x; e < p.E; e += kRouteThreads)
+        if (hist[e]) atomicAdd(p.words + e, static_cast<unsigned int>(hist[e]));
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) last_cta = atomicAdd(p.words + kRouteMaxExperts, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (last_cta) {
+        __threadfence();
+        for (int e = threadIdx.x; e < p.E; e += kRouteThreads) p.counts[e] = static_cast<int>(atomicExch(p.words + e, 0u));
+        if (threadIdx.x == 0) p.words[kRouteMaxExperts] = 0u;
+    }
+}
+
+// Gradient of the weights back to the logits.  With g_i the gradient of weight i and S the sum of the chosen p:
+//   sigmoid:            dl_i = factor g_i p_i (1 - p_i);                                        0 for the others
+//   sigmoid, renorm:    dl_i = factor (g_i - sum_j g_j w_j) w_i (1 - p_i),  w_i = p_i / S;      0 for the others
+//   softmax, renorm:    dl_i = factor (g_i - sum_j g_j w_j) w_i;                                0 for the others
+//   softmax:            dl_e = p_e (dp_e - sum_i dp_i p_i) for every expert,  dp_i = factor g_i for the chosen, else 0
+// Ids outside [0, E) (a slot that found no expert) carry no gradient.  One warp per token; lane r < k holds chosen expert r.
+template <class E, int VPL, bool SOFTMAX>
+__global__ void __launch_bounds__(kRouteThreads) k_route_grad(const __grid_constant__ RouteGradParams p) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (long long t = static_cast<long long>(blockIdx.x) * kRouteWarps + warp; t < p.T; t += static_cast<long long>(gridDim.x) * kRouteWarps) {
+        const E* row = static_cast<const E*>(p.logits) + t * p.ld;
+        E* out = static_cast<E*>(p.dlogits) + t * p.ld_d;
+        int id = lane < p.k ? __ldg(p.ids + t * p.k + lane) : -1;
+        if (id >= p.E) id = -1;
+        const float g = id >= 0 ? p.factor * __ldg(p.dweights + t * p.k + lane) : 0.0f;
+        const float x = id >= 0 ? load_as_float(row + id) : -INFINITY;
+        float d = 0.0f;                             // gradient of this lane's chosen logit
+        float rest = 0.0f;                          // softmax without renormalisation: minus the common term of all experts
+        float shift = 0.0f, total = 1.0f;
+        float v[VPL];
+        if (!SOFTMAX) {
+            const float q = id >= 0 ? plain_sigmoid(x) : 0.0f;
+            if (p.renorm) {
+                const float r = relative_sigmoid(x, sigmoid_shift(x)), S = warp_sum(r);
+                const float w = S > 0.0f ? r / S : 0.0f;
+                d = (g - warp_sum(g * w)) * w * (1.0f - q);
+            } else {
+                d = g * q * (1.0f - q);
+            }
+        } else if (p.renorm) {
+            shift = warp_max(x);
+            const float w0 = id >= 0 ? expf(x - shift) : 0.0f;
+            const float w = w0 / fmaxf(warp_sum(w0), 1.0f);    // the largest term is 1; no chosen expert at all: 0
+            d = w * (g - warp_sum(g * w));
+        } else {
+            float m = -INFINITY, s = 0.0f;
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) {
+                const int e = j * 32 + lane;
+                v[j] = e < p.E ? load_as_float(row + e) : -INFINITY;
+                m = fmaxf(m, v[j]);
+            }
+            shift = warp_max(m);
+#pragma unroll
+            for (int j = 0; j < VPL; ++j) {
+                v[j] = shift > -INFINITY ? expf(v[j] - shift) : 0.0f;
+                s += v[j];
+            }
+            total = warp_sum(s);
+            const float q = id >= 0 ? expf(x - shift) / total : 0.0f;
+            rest = warp_sum(g * q);
+            d = q * (g - rest);
+        }
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int e = j * 32 + lane;
+            float o = 0.0f;
+            if constexpr (SOFTMAX)
+                if (!p.renorm && rest != 0.0f) o = -(v[j] / total) * rest;
+            if (e < p.E) store_from_float(out + e, o);
+        }
+        __syncwarp();                               // the chosen ones replace what was just written
+        if (id >= 0) store_from_float(out + id, d);
+    }
+}
+
+}  // namespace lrgd
