@@ -287,27 +287,12 @@ cudaError_t launch_rows(const lr_plan& P, const StreamParams& sp, cudaStream_t s
 // Tensor map of X for the wide-row kernel: [m][n] row-major, box = cw 16-byte groups by rb rows, zero fill outside.
 // The copy moves bytes untouched, and a box may span at most 256 elements per dimension, so a bfloat16 matrix is
 // described as 32-bit words (n/2 per row): the widest slice, 64 groups, is then 256 elements for either storage type.
-// The encoder is a driver entry point, resolved at run time so that the library links against the runtime only.
 bool split_words64(bool /*bf16*/, int cw) { return cw > 64; }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 cudaError_t make_x_tensor_map(const void* X, bool bf16, int64_t m, int32_t n, int cw, int rb, CUtensorMap* out) {
-    // resolved once per process; the initialisation of a function-local static is thread-safe
-    struct Resolved { EncodeTiledFn fn = nullptr; cudaError_t err = cudaSuccess; };
-    static const Resolved resolved = [] {
-        Resolved r;
-        void* fn = nullptr;
-        cudaDriverEntryPointQueryResult q;
-        r.err = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
-        if (r.err == cudaSuccess && (q != cudaDriverEntryPointSuccess || !fn)) r.err = cudaErrorNotSupported;
-        if (r.err == cudaSuccess) r.fn = reinterpret_cast<EncodeTiledFn>(fn);
-        return r;
-    }();
-    if (resolved.err != cudaSuccess) return resolved.err;
-    const EncodeTiledFn encode = resolved.fn;
+    EncodeTiledFn encode = nullptr;
+    const cudaError_t found = tensor_map_encoder(&encode);
+    if (found != cudaSuccess) return found;
     // (fp32 slices of more than 64 groups -- rows of more than 4096 columns -- are described as 64-bit words for the same reason)
     const bool wide64 = split_words64(bf16, cw);
     const cuuint64_t row_bytes = cuuint64_t(n) * (bf16 ? 2 : 4);

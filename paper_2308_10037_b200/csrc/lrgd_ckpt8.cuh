@@ -1,8 +1,7 @@
-// Rows kept between forward and backward in 8 bits, and the gradient of a C-class logistic layer taken from them.
+// Rows kept between forward and backward in 8 bits.
 //
 //   save:      128 columns of a row share a scale:  a = max |x|,  s = a / 127,  q = rint(x * (127 / a))   (ties to even)
 //   load:      x' = q * s
-//   gradient:  grad_w[c,j] (+)= sum_t dz[t,c] * s[t,j/128] * q[t,j],   grad_b[c] (+)= sum_t dz[t,c]
 //
 // |x' - x| <= a/254 within a group (plus the rounding of the two products).  A group whose a is below 1e-36 (127 / a would
 // overflow) is kept as zeros; one with a NaN or an infinity gets the scale NaN, so that what is read back shows it.
@@ -132,75 +131,6 @@ __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_load(const __grid_consta
             for (int i = 0; i < 8; ++i)
                 if (c0 + 16 * i < p.n) store_from_float(dst + 16 * i, static_cast<float>(src[16 * i]) * s);
         }
-    }
-}
-
-// ---- gradient ------------------------------------------------------------------------------------------
-// The rows are cut into `chunks` parts; a CTA takes one part, one group of 128 columns (a column per thread) and kGradClasses
-// classes, and leaves its sums in the scratch; k_ckpt8_join adds the parts in order.
-constexpr int kGradClasses = 8;
-constexpr int kGradTile = 32;
-
-struct CkptGradParams {
-    const signed char* q;
-    long long ld_q;
-    const float* s;
-    long long T;
-    int n;
-    int groups;
-    const void* dz;
-    long long ld_dz;
-    int C;
-    int chunks;
-    long long rows;            // rows per chunk
-    int accumulate;
-    float* part_w;             // [chunks][C][n]
-    float* part_b;             // [chunks][C]
-    float* grad_w;             // [C][n]
-    float* grad_b;             // [C], nullable
-};
-
-template <class E>
-__global__ void __launch_bounds__(kCkptGroup) k_ckpt8_grad(const __grid_constant__ CkptGradParams p) {
-    __shared__ float dz[kGradTile][kGradClasses], sc[kGradTile];
-    const int tid = threadIdx.x, g = blockIdx.x, c0 = blockIdx.y * kGradClasses, col = g * kCkptGroup + tid;
-    const long long lo = blockIdx.z * p.rows, hi = min(p.T, lo + p.rows);
-    float acc[kGradClasses] = {}, accb = 0.0f;
-    for (long long t0 = lo; t0 < hi; t0 += kGradTile) {
-        const int rows = static_cast<int>(min(static_cast<long long>(kGradTile), hi - t0));
-        __syncthreads();
-        for (int i = tid; i < kGradTile * kGradClasses; i += kCkptGroup) {
-            const int r = i / kGradClasses, c = i % kGradClasses;
-            dz[r][c] = r < rows && c0 + c < p.C ? load_as_float(static_cast<const E*>(p.dz) + (t0 + r) * p.ld_dz + c0 + c) : 0.0f;
-        }
-        if (tid < rows) sc[tid] = __ldg(p.s + (t0 + tid) * p.groups + g);
-        __syncthreads();
-        if (col < p.n)
-            for (int r = 0; r < rows; ++r) {
-                const float x = static_cast<float>(__ldg(p.q + (t0 + r) * p.ld_q + col)) * sc[r];
-#pragma unroll
-                for (int c = 0; c < kGradClasses; ++c) acc[c] += x * dz[r][c];
-            }
-        if (g == 0 && tid < kGradClasses)
-            for (int r = 0; r < rows; ++r) accb += dz[r][tid];
-    }
-#pragma unroll
-    for (int c = 0; c < kGradClasses; ++c)
-        if (c0 + c < p.C && col < p.n) p.part_w[(static_cast<long long>(blockIdx.z) * p.C + c0 + c) * p.n + col] = acc[c];
-    if (g == 0 && tid < kGradClasses && c0 + tid < p.C) p.part_b[static_cast<long long>(blockIdx.z) * p.C + c0 + tid] = accb;
-}
-
-static __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_join(const __grid_constant__ CkptGradParams p) {
-    const long long count = static_cast<long long>(p.C) * p.n;
-    for (long long i = static_cast<long long>(blockIdx.x) * kCkptThreads + threadIdx.x; i < count + p.C; i += static_cast<long long>(gridDim.x) * kCkptThreads) {
-        const bool w = i < count;
-        if (!w && !p.grad_b) break;
-        const float* part = w ? p.part_w + i : p.part_b + (i - count);
-        const long long step = w ? count : p.C;
-        float* out = w ? p.grad_w + i : p.grad_b + (i - count);
-        float sum = 0.0f;
-        for (int c = 0; c < p.chunks; ++c) sum += part[c * step];
-        *out = p.accumulate ? *out + sum : sum;
     }
 }
 

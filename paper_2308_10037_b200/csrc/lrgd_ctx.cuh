@@ -3,6 +3,7 @@
 #pragma once
 #include "../../include/lrgd.h"
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <nvtx3/nvToolsExt.h>
 
@@ -156,6 +157,27 @@ cudaError_t ensure_dynamic_smem(const void* kern, int smem) {
     if (e == cudaSuccess && dev >= 0 && dev < kDevices) have[dev] = smem;
     return e;
 }
+// The tensor-map encoder is a driver entry point, resolved at run time so that the library links against the runtime only.
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+cudaError_t tensor_map_encoder(EncodeTiledFn* out) {
+    // resolved once per process; the initialisation of a function-local static is thread-safe
+    struct Resolved { EncodeTiledFn fn = nullptr; cudaError_t err = cudaSuccess; };
+    static const Resolved resolved = [] {
+        Resolved r;
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        r.err = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
+        if (r.err == cudaSuccess && (q != cudaDriverEntryPointSuccess || !fn)) r.err = cudaErrorNotSupported;
+        if (r.err == cudaSuccess) r.fn = reinterpret_cast<EncodeTiledFn>(fn);
+        return r;
+    }();
+    *out = resolved.fn;
+    return resolved.err;
+}
+
 int grow(lr_ctx* ctx, void** buf, size_t* have, size_t need) {
     if (*have >= need) return LR_OK;
     if (*buf) { LR_CK(ctx, cudaFree(*buf)); *buf = nullptr; *have = 0; }

@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "lrgd_ckpt8.cuh"
+#include "lrgd_ckpt8_grad.cuh"
 #include "lrgd_ctx.cuh"
 #include "lrgd_embed.cuh"
 #include "lrgd_route.cuh"
@@ -275,6 +276,9 @@ int ckpt8_move(lr_ctx* ctx, bool save, const E* x, E* back, int64_t ld, int64_t 
     });
 }
 
+template <class E, bool TMA>
+struct CkptGradTag {};
+
 template <class E>
 int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const E* d_dz, int64_t ld_dz,
                     int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream) {
@@ -295,19 +299,60 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
         }
         return LR_OK;
     }
-    const int groups = (n + kCkptGroup - 1) / kCkptGroup;
-    const int cblocks = (C + kGradClasses - 1) / kGradClasses;
-    int64_t chunks = std::max<int64_t>(1, int64_t(plan_sms(ctx)) * 8 / (int64_t(groups) * cblocks));
-    int64_t rows = std::max<int64_t>((T + chunks - 1) / chunks, kGradTile);
-    chunks = (T + rows - 1) / rows;
-    const size_t part_w = (size_t(chunks) * C * n * 4 + 255) / 256 * 256, part_b = size_t(chunks) * C * 4;
-    const int rs = gate_scratch(ctx, part_w + part_b);
-    if (rs != LR_OK) return rs;
-    const CkptGradParams p{d_q, ld_q, d_s, T, n, groups, d_dz, ld_dz, C, int(chunks), rows, accumulate != 0,
-                           reinterpret_cast<float*>(ctx->d_scratch), reinterpret_cast<float*>(ctx->d_scratch + part_w), d_grad_w, d_grad_b};
-    int r = launched(ctx, [&] { k_ckpt8_grad<E><<<dim3(unsigned(groups), unsigned(cblocks), unsigned(chunks)), kCkptGroup, 0, st>>>(p); });
-    if (r != LR_OK) return r;
-    return launched(ctx, [&] { k_ckpt8_join<<<grid_for(ctx, int64_t(C) * n + C, kCkptThreads, 8), kCkptThreads, 0, st>>>(p); });
+    // CTAs take two groups of columns, a block of classes and a range of rows; as many ranges as fill the SMs once
+    const int groups = (n + kCkptGroup - 1) / kCkptGroup, pairs = (groups + 1) / 2;
+    const int cblocks = (C + kTcMaxClasses - 1) / kTcMaxClasses, cblock = (C + cblocks - 1) / cblocks, cp = (cblock + 15) / 16 * 16;
+    const int64_t stages = (T + kTcRows - 1) / kTcRows;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(stages, plan_sms(ctx) / (int64_t(pairs) * cblocks)));
+    const int64_t rows = (stages + want - 1) / want * kTcRows, chunks = (T + rows - 1) / rows;
+    float *part_w = nullptr, *part_b = nullptr;
+    if (chunks > 1) {
+        const size_t wb = (size_t(chunks) * C * n * 4 + 255) / 256 * 256;
+        const int rs = gate_scratch(ctx, wb + size_t(chunks) * C * 4);
+        if (rs != LR_OK) return rs;
+        part_w = reinterpret_cast<float*>(ctx->d_scratch);
+        part_b = reinterpret_cast<float*>(ctx->d_scratch + wb);
+    }
+    TcGradParams p{};
+    p.g = CkptGradParams{d_q, ld_q, d_s, T, n, groups, d_dz, ld_dz, C, int(chunks), rows, accumulate != 0, part_w, part_b, d_grad_w, d_grad_b};
+    p.cp = cp;
+    p.cblock = cblock;
+    p.status = ctx->d_status;
+    const bool tma = aligned(d_q, 16) && ld_q % 16 == 0;
+    CUtensorMap map{};
+    if (tma) {
+        EncodeTiledFn encode = nullptr;
+        LR_CK(ctx, tensor_map_encoder(&encode));
+        const cuuint64_t dims[2] = {cuuint64_t(n), cuuint64_t(T)}, strides[1] = {cuuint64_t(ld_q)};
+        const cuuint32_t box[2] = {kCkptGroup, kTcRows}, unit[2] = {1, 1};
+        if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(d_q), dims, strides, box, unit, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+            ctx->last_cuda = int(cudaErrorInvalidValue);
+            return LR_ERR_CUDA;
+        }
+    }
+    const dim3 grid{unsigned(pairs), unsigned(chunks), unsigned(cblocks)};
+    const int smem = tc_smem_bytes(cp, tma);
+    int r = LR_OK;
+    if (tma) {
+        LR_CK(ctx, (ensure_dynamic_smem<CkptGradTag<E, true>>(reinterpret_cast<const void*>(k_ckpt8_grad_tc<E, true>), smem)));
+        r = launched(ctx, [&] { k_ckpt8_grad_tc<E, true><<<grid, kTcThreads, smem, st>>>(map, p); });
+    } else {
+        LR_CK(ctx, (ensure_dynamic_smem<CkptGradTag<E, false>>(reinterpret_cast<const void*>(k_ckpt8_grad_tc<E, false>), smem)));
+        r = launched(ctx, [&] { k_ckpt8_grad_tc<E, false><<<grid, kTcThreads, smem, st>>>(map, p); });
+    }
+    if (r != LR_OK || chunks == 1) return r;
+    const int64_t values = int64_t(C) * n;
+    const bool vec = values % 4 == 0 && aligned(d_grad_w, 16);
+    // sixteen parts and fewer are added by one thread each; more leave too few loads in flight
+    auto join = [&](auto kern, int64_t units, int per_cta) -> int {
+        LR_CK(ctx, launch_kernel(kern, dim3(grid_for(ctx, units + C, per_cta, 16)), dim3(kJoinThreads), 0, st, ctx->overlap, p.g));
+        ctx->launches += 1;
+        return LR_OK;
+    };
+    if (chunks > 16) return join(k_ckpt8_join<1, 8>, values, kJoinThreads / 8);
+    if (vec) return join(k_ckpt8_join<4, 1>, values / 4, kJoinThreads);
+    return join(k_ckpt8_join<1, 1>, values, kJoinThreads);
 }
 
 // bfloat16 is the unsigned 16-bit pattern of the interface

@@ -490,6 +490,25 @@ def test_ckpt8_grad(ctx, dt, T, n, C):
     close(ob, wb, rel * mb)
 
 
+@pytest.mark.parametrize("shift", [0, 3])
+@pytest.mark.parametrize("T", [32, 33, 64, 65, 96, 511, 512, 513, 544, 545, 577, 1024, 1025, 1057, 1537, 5000])
+def test_ckpt8_grad_many_rows_per_cta(ctx, T, shift):
+    # one CTA for all rows: every number of stages, of buffer turns and of flushes of the accumulators
+    n, C = 300, 50
+    q, s = ctx.ckpt8_save(rnd(T, n, seed=n))
+    dz = rnd(T, C, seed=C)
+    x = (padded_groups(q) * s.double()[:, :, None]).flatten(1)[:, :n]
+    want, mag = dz.double().t() @ x, dz.double().abs().t() @ x.abs()
+    rel = (8 + math.sqrt(T)) * U
+    ctx.set_sm_limit(1)
+    try:
+        gw, gb = ctx.ckpt8_grad(strided(q, 5, shift) if shift else q, s, dz)
+    finally:
+        ctx.set_sm_limit(0)
+    close(gw, want, rel * mag)
+    close(gb, dz.double().sum(0), rel * dz.double().abs().sum(0))
+
+
 def test_ckpt8_grad_wide_range_of_dz(ctx):
     # rows whose gradient differs by many orders of magnitude: the small ones must not be lost where they stand alone
     T, n, C = 300, 256, 20
