@@ -7,6 +7,7 @@ library has not been built; there is no fallback of any kind.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -206,6 +207,18 @@ def _host_ptr(a, dtype, name: str, count: int | None = None):
     return ctypes.c_void_p(a.ctypes.data)
 
 
+# The current stream's address without building a Stream object around it (a tenth of the time, on every call).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
+def _new(rows: int, cols: int, dtype, device) -> torch.Tensor:
+    """An uninitialised [rows, cols] tensor; the call that says the strides is the quickest of torch's allocations."""
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+
+
+_ROW_TYPES = (torch.float32, torch.bfloat16)
+
+
 class Context:
     """Owns one ``lr_ctx``: workspace for problems of up to ``n_max`` columns on one device."""
 
@@ -235,7 +248,8 @@ class Context:
             raise LrError(rc, where, detail)
 
     def _stream(self):
-        return ctypes.c_void_p(torch.cuda.current_stream(self.device).cuda_stream)
+        """Address of the current stream of the context's device (0 is the legacy default stream)."""
+        return _raw_stream(self.device)
 
     # ---- device-pointer entry points -------------------------------------------------------------
     # X may be a float32 tensor (lr_loss_grad / lr_fit / lr_predict) or a bfloat16 tensor (the *_bf16 entry points).
@@ -352,17 +366,20 @@ class Context:
         """(address, rows, columns, leading dimension, entry-point suffix) of a 2-D CUDA tensor with unit column stride."""
         if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype in dtypes):
             raise TypeError(f"{name}: expected a CUDA tensor of dtype {' or '.join(str(d) for d in dtypes)}")
-        if t.dim() != 2 or t.shape[1] < 1:
+        size = t.shape
+        if len(size) != 2 or size[1] < 1:
             raise ValueError(f"{name}: expected a 2-D tensor with at least one column")
-        rows, cols = t.shape
-        if shape is not None and (rows, cols) != shape:
-            raise ValueError(f"{name}: shape {(rows, cols)}, the call needs {shape}")
-        ld = t.stride(0) if rows > 1 else cols
-        if (cols > 1 and t.stride(1) != 1) or ld < cols:
+        if shape is not None and size != shape:
+            raise ValueError(f"{name}: shape {tuple(size)}, the call needs {shape}")
+        rows, cols = size
+        ld, step = t.stride()
+        if rows <= 1:
+            ld = cols
+        if (step != 1 and cols > 1) or ld < cols:
             raise ValueError(f"{name}: rows must be contiguous and must not overlap")
         if t.device.index != self.device:
             raise ValueError(f"{name}: lives on cuda:{t.device.index}, the call runs on cuda:{self.device}")
-        return t.data_ptr(), rows, cols, ld, "_bf16" if t.dtype == torch.bfloat16 else ""
+        return t.data_ptr(), rows, cols, ld, "_bf16" if t.dtype is torch.bfloat16 else ""
 
     def _tokens(self, ids):
         if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dtype in (torch.int32, torch.int64) and ids.is_contiguous()):
@@ -375,31 +392,41 @@ class Context:
         """``scale * table[ids]``: rows of a token table [V, n] (float32 or bfloat16) for int32 or int64 ``ids`` of any shape;
         returns ``ids.shape + (n,)`` in the table's type, or writes the rows to ``out`` [T, n].  A token outside [0, V) gives zeros
         and a device status of LR_ERR_VALUE."""
-        pt, V, n, ld, sfx = self._rows(table, (torch.float32, torch.bfloat16), "table")
+        pt, V, n, ld, sfx = self._rows(table, _ROW_TYPES, "table")
         pi, ib, T = self._tokens(ids)
-        flat = torch.empty((T, n), dtype=table.dtype, device=table.device) if out is None else out
-        po, _, _, ldo, _ = self._rows(flat, (table.dtype,), "out", (T, n))
+        if out is None:
+            flat = _new(T, n, table.dtype, table.device)
+            po, ldo = flat.data_ptr(), n
+        else:
+            po, _, _, ldo, _ = self._rows(out, (table.dtype,), "out", (T, n))
         rc = getattr(lib(), "lr_embed" + sfx)(self._h, pt, ld, pi, ib, T, V, n, float(scale), po, ldo, self._stream())
-        self._check(rc, "lr_embed" + sfx)
-        return flat.view(*ids.shape, n) if out is None else out
+        if rc:
+            self._check(rc, "lr_embed" + sfx)
+        if out is not None:
+            return out
+        return flat if ids.dim() == 1 else flat.view(*ids.shape, n)
 
     def embed_grad(self, ids, dout, rows, scale=1.0, padding_id=-1, out=None, accumulate=False):
         """Gradient [rows, n] (float32) of the table of ``embed``: ``scale *`` the sum of ``dout`` [T, n] over the places of each
         token, none for ``padding_id``.  With ``accumulate`` it is added to ``out``."""
         pi, ib, T = self._tokens(ids)
-        pd, _, n, ld, sfx = self._rows(dout, (torch.float32, torch.bfloat16), "dout", (T, dout.shape[-1] if isinstance(dout, torch.Tensor) and dout.dim() else 0))
+        pd, d_rows, n, ld, sfx = self._rows(dout, _ROW_TYPES, "dout")
+        if d_rows != T:
+            raise ValueError(f"dout: {d_rows} rows for {T} tokens")
         if out is None:
             if accumulate:
                 raise ValueError("accumulate needs the gradient to add to as out")
-            out = torch.empty((int(rows), n), dtype=torch.float32, device=dout.device)
+            out = _new(int(rows), n, torch.float32, dout.device)
         elif not isinstance(out, torch.Tensor) or out.shape != (int(rows), n):
             raise ValueError(f"out: expected a float32 CUDA tensor of shape {(int(rows), n)}")
         rc = getattr(lib(), "lr_embed_grad" + sfx)(self._h, pi, ib, pd, ld, T, int(rows), n, float(scale), int(padding_id),
                                                    int(bool(accumulate)), self._p(out, torch.float32, "out"), self._stream())
-        self._check(rc, "lr_embed_grad" + sfx)
+        if rc:
+            self._check(rc, "lr_embed_grad" + sfx)
         return out
 
     @staticmethod
+    @functools.lru_cache(maxsize=64)
     def _route_opt(k, groups, top_groups, score, renorm, factor):
         if score not in _SCORES:
             raise ValueError(f"score: expected one of {sorted(_SCORES)}")
@@ -411,43 +438,46 @@ class Context:
         [T, k], counts int32 [E]).  ``score`` "sigmoid" or "softmax"; ``bias`` float32 [E] enters the choice only; with ``groups``
         only the experts of the ``top_groups`` best groups (default: all) can be chosen; ``renorm`` divides by the sum of the chosen;
         ``factor`` multiplies the weights.  See ``lr_route`` in the header for the exact rules."""
-        pl, T, E, ld, sfx = self._rows(logits, (torch.float32, torch.bfloat16), "logits")
+        pl, T, E, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
         opt = self._route_opt(k, groups, top_groups, score, renorm, factor)
         pb = self._p(bias, torch.float32, "bias", E)
         width, dev = max(opt.k, 0), logits.device
-        ids = torch.empty((T, width), dtype=torch.int32, device=dev)
-        weights = torch.empty((T, width), dtype=torch.float32, device=dev)
-        counts = torch.empty(E, dtype=torch.int32, device=dev)
+        ids = _new(T, width, torch.int32, dev)
+        weights = _new(T, width, torch.float32, dev)
+        counts = torch.empty_strided((E,), (1,), dtype=torch.int32, device=dev)
         rc = getattr(lib(), "lr_route" + sfx)(self._h, pl, ld, T, E, ctypes.byref(opt), pb, ids.data_ptr(), weights.data_ptr(),
                                               counts.data_ptr(), self._stream())
-        self._check(rc, "lr_route" + sfx)
+        if rc:
+            self._check(rc, "lr_route" + sfx)
         return ids, weights, counts
 
     def route_grad(self, logits, ids, dweights, score="sigmoid", renorm=True, factor=1.0, out=None):
         """Gradient of ``route``'s weights back to the logits: [T, E] in the logits' type from ``ids`` int32 [T, k] and ``dweights``
         float32 [T, k]."""
-        pl, T, E, ld, sfx = self._rows(logits, (torch.float32, torch.bfloat16), "logits")
+        pl, T, E, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
         if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or ids.shape[0] != T or not isinstance(dweights, torch.Tensor) or dweights.shape != ids.shape:
             raise ValueError("ids, dweights: expected two tensors [T, k]")
         opt = self._route_opt(ids.shape[1], 1, 1, score, renorm, factor)
         pi, pw = self._p(ids, torch.int32, "ids"), self._p(dweights, torch.float32, "dweights")
-        res = torch.empty((T, E), dtype=logits.dtype, device=logits.device) if out is None else out
-        po, _, _, ldo, _ = self._rows(res, (logits.dtype,), "out", (T, E))
+        res = _new(T, E, logits.dtype, logits.device) if out is None else out
+        po, ldo = (res.data_ptr(), E) if out is None else self._rows(res, (logits.dtype,), "out", (T, E))[0:4:3]
         rc = getattr(lib(), "lr_route_grad" + sfx)(self._h, pl, ld, T, E, ctypes.byref(opt), pi, pw, po, ldo, self._stream())
-        self._check(rc, "lr_route_grad" + sfx)
+        if rc:
+            self._check(rc, "lr_route_grad" + sfx)
         return res
 
     def ckpt8_save(self, X):
         """Rows ``X`` [T, n] (float32 or bfloat16) in 8 bits: (q int8 [T, n], s float32 [T, ceil(n/128)]).  The rows of ``q`` start
         16 bytes apart or a multiple of that."""
-        px, T, n, ld, sfx = self._rows(X, (torch.float32, torch.bfloat16), "X")
-        pitch = (n + 15) // 16 * 16
-        q = torch.empty((T, pitch), dtype=torch.int8, device=X.device)
+        px, T, n, ld, sfx = self._rows(X, _ROW_TYPES, "X")
+        pitch, dev = (n + 15) // 16 * 16, X.device
+        q = _new(T, pitch, torch.int8, dev)
         if pitch != n:
             q = q[:, :n]
-        s = torch.empty((T, (n + CKPT8_GROUP - 1) // CKPT8_GROUP), dtype=torch.float32, device=X.device)
+        s = _new(T, (n + CKPT8_GROUP - 1) // CKPT8_GROUP, torch.float32, dev)
         rc = getattr(lib(), "lr_ckpt8_save" + sfx)(self._h, px, ld, T, n, q.data_ptr(), pitch, s.data_ptr(), self._stream())
-        self._check(rc, "lr_ckpt8_save" + sfx)
+        if rc:
+            self._check(rc, "lr_ckpt8_save" + sfx)
         return q, s
 
     def _ckpt8(self, q, s):
@@ -457,27 +487,29 @@ class Context:
     def ckpt8_load(self, q, s, dtype=torch.float32, out=None):
         """The rows that ``ckpt8_save`` kept, in ``dtype`` (float32 or bfloat16)."""
         pq, ldq, ps, T, n = self._ckpt8(q, s)
-        res = torch.empty((T, n), dtype=dtype, device=q.device) if out is None else out
-        po, _, _, ld, sfx = self._rows(res, (torch.float32, torch.bfloat16), "out", (T, n))
+        res = _new(T, n, dtype, q.device) if out is None else out
+        po, _, _, ld, sfx = self._rows(res, _ROW_TYPES, "out", (T, n))
         rc = getattr(lib(), "lr_ckpt8_load" + sfx)(self._h, pq, ldq, ps, T, n, po, ld, self._stream())
-        self._check(rc, "lr_ckpt8_load" + sfx)
+        if rc:
+            self._check(rc, "lr_ckpt8_load" + sfx)
         return res
 
     def ckpt8_grad(self, q, s, dz, grad_w=None, grad_b=None, accumulate=False):
         """(grad_w [C, n], grad_b [C]) of a logistic layer with C outputs from the kept rows and ``dz`` [T, C] (float32 or
         bfloat16); with ``accumulate`` added to the given ``grad_w`` and ``grad_b``."""
         pq, ldq, ps, T, n = self._ckpt8(q, s)
-        pz, rows, C, ldz, sfx = self._rows(dz, (torch.float32, torch.bfloat16), "dz")
+        pz, rows, C, ldz, sfx = self._rows(dz, _ROW_TYPES, "dz")
         if rows != T:
             raise ValueError(f"dz: {rows} rows, q has {T}")
         if accumulate and (grad_w is None or grad_b is None):
             raise ValueError("accumulate needs grad_w and grad_b to add to")
-        grad_w = torch.empty((C, n), dtype=torch.float32, device=q.device) if grad_w is None else grad_w
-        grad_b = torch.empty(C, dtype=torch.float32, device=q.device) if grad_b is None else grad_b
+        grad_w = _new(C, n, torch.float32, q.device) if grad_w is None else grad_w
+        grad_b = torch.empty_strided((C,), (1,), dtype=torch.float32, device=q.device) if grad_b is None else grad_b
         rc = getattr(lib(), "lr_ckpt8_grad" + sfx)(self._h, pq, ldq, ps, T, n, pz, ldz, C, int(bool(accumulate)),
                                                    self._p(grad_w, torch.float32, "grad_w", C * n),
                                                    self._p(grad_b, torch.float32, "grad_b", C), self._stream())
-        self._check(rc, "lr_ckpt8_grad" + sfx)
+        if rc:
+            self._check(rc, "lr_ckpt8_grad" + sfx)
         return grad_w, grad_b
 
     def shard_sums(self, X, y, w, b, sums):

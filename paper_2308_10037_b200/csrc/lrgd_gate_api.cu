@@ -195,11 +195,12 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
         if (!accumulate) LR_CK(ctx, cudaMemsetAsync(d_grad, 0, size_t(V) * n * 4, st));
         return LR_OK;
     }
-    const int R = T >= 8192 ? 64 : T >= 1024 ? 32 : 16;
+    const int R = T >= 4096 ? 32 : 16;             // fewer rows per chunk where there are few chunks
     const int64_t chunks = (T + R - 1) / R;
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-    const size_t list = up(size_t(T) * 4), split = up(size_t(chunks) * 4), piece = size_t(2) * chunks * n * 4;
-    const int rs = gate_scratch(ctx, 4 * list + split + piece);
+    const size_t list = up(size_t(T) * 8), runs = up(size_t(chunks / 2 + 2) * 4), bits = up((size_t(V) + 31) / 32 * 4),
+                 piece = size_t(2) * chunks * n * 4;
+    const int rs = gate_scratch(ctx, 2 * list + runs + bits + piece);
     if (rs != LR_OK) return rs;
     unsigned char* w = ctx->d_scratch;
     SortParams sp{};
@@ -207,16 +208,21 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
     sp.T = unsigned(T);
     sp.V = V;
     sp.padding = padding_id;
-    for (int i = 0; i < 2; ++i) {
-        sp.key[i] = reinterpret_cast<unsigned int*>(w + 2 * i * list);
-        sp.pos[i] = reinterpret_cast<unsigned int*>(w + (2 * i + 1) * list);
-    }
-    sp.passes = V < (int64_t(1) << 8) ? 1 : V < (int64_t(1) << 16) ? 2 : V < (int64_t(1) << 24) ? 3 : 4;   // keys 0..V
+    for (int i = 0; i < 2; ++i) sp.place[i] = reinterpret_cast<uint2*>(w + i * list);
+    for (sp.passes = 1; V >> (kSortBits * sp.passes); ++sp.passes) {}               // keys 0..V
     sp.status = ctx->d_status;
-    sp.zero = accumulate ? nullptr : d_grad;
-    sp.zero_count = accumulate ? 0 : V * n;
+    sp.long_runs = reinterpret_cast<unsigned int*>(w + 2 * list);
+    sp.present = accumulate ? nullptr : reinterpret_cast<unsigned int*>(w + 2 * list + runs);
+    // Rows cleared while the sort runs, whether a token points there or not; the others are cleared after it, where none does.
+    // A pass over few positions takes about 5 us, in which the memory takes kClearPerPass bytes; kClearPerToken is what it takes in the
+    // time of each further position (32768 positions, two passes: 25 us).  The join takes about 8 us: kClearLate.
+    constexpr int64_t kClearPerPass = 28 << 20, kClearPerToken = 1100, kClearLate = 40 << 20;
+    const int64_t row_bytes = int64_t(n) * 4;
+    const int64_t early = accumulate ? 0 : std::min<int64_t>(V, (sp.passes * (kClearPerPass + T * kClearPerToken)) / row_bytes);
+    sp.zero = d_grad;
+    sp.zero_count = early * n;
     int clusters = 1;
-    if (!accumulate) {
+    if (early > 0) {
         const int64_t want = (sp.zero_count / 4 + kSortThreads * kSortCtas * 4 - 1) / (kSortThreads * kSortCtas * 4);
         clusters += int(std::max<int64_t>(1, std::min<int64_t>(want, plan_sms(ctx) * 2 / kSortCtas)));
     }
@@ -226,20 +232,37 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
     });
     if (r != LR_OK) return r;
     const int last = (sp.passes - 1) & 1;
-    RunParams rp{sp.key[last], sp.pos[last], unsigned(T), unsigned(V), R, d_dout, ld_dout, n, scale, accumulate != 0, d_grad,
-                 reinterpret_cast<float*>(w + 4 * list + split), reinterpret_cast<unsigned int*>(w + 4 * list)};
-    auto go = [&](auto vec) {
+    RunParams rp{sp.place[last], unsigned(T), unsigned(V), R, int(chunks), 0, d_dout, ld_dout, n, scale, d_grad,
+                 reinterpret_cast<float*>(w + 2 * list + runs + bits), sp.long_runs, sp.present, {0, 0}, 1, 0};
+    auto go = [&](auto vec, auto add) -> int {
         constexpr int VEC = decltype(vec)::value;
+        constexpr bool ADD = decltype(add)::value;
         const int64_t slices = (int64_t(n) + RunCols<E, VEC>::kSlice - 1) / RunCols<E, VEC>::kSlice;
-        if (slices > 65535) return int(LR_ERR_SHAPE);
-        const dim3 grid{unsigned(chunks), unsigned(slices), 1u};
-        r = launched(ctx, [&] { k_run_sum<E, VEC><<<grid, kRunThreads, 0, st>>>(rp); });
-        if (r != LR_OK) return r;
-        return launched(ctx, [&] { k_run_join<E, VEC><<<grid, kRunThreads, 0, st>>>(rp); });
+        rp.slices = int(slices);
+        // long runs have more than one chunk to themselves
+        rp.joiners = chunks < 3 ? 0 : int(std::min<int64_t>(chunks / 2, std::max<int64_t>(1, plan_sms(ctx) / slices)));
+        rp.clear[0] = rp.clear[1] = V;
+        rp.clear_rows = int(std::max<int64_t>(1, (64 << 10) / row_bytes));              // about 64 KB per clearing CTA
+        if (!accumulate) {
+            rp.clear[0] = early;
+            if (rp.joiners > 0) rp.clear[1] = std::max(early, V - kClearLate / row_bytes);
+        }
+        const int64_t mid = (rp.clear[1] - rp.clear[0] + rp.clear_rows - 1) / rp.clear_rows, late = (V - rp.clear[1] + rp.clear_rows - 1) / rp.clear_rows;
+        if (slices > 65535 || chunks * slices + mid > INT32_MAX || late > INT32_MAX / 2) return LR_ERR_SHAPE;
+        LR_CK(ctx, launch_kernel(k_run_sum<E, VEC, ADD>, dim3(unsigned(chunks * slices + mid)), dim3(kRunThreads), 0, st, ctx->overlap, rp));
+        ctx->launches += 1;
+        if (rp.joiners == 0) return LR_OK;
+        LR_CK(ctx, launch_kernel(k_run_join<E, VEC, ADD>, dim3(unsigned(rp.joiners * slices + late)), dim3(kRunThreads * kJoinGroups), 0, st,
+                                 ctx->overlap, rp));
+        ctx->launches += 1;
+        return LR_OK;
     };
     constexpr int kVec = 16 / int(sizeof(E));
-    if (n % kVec == 0 && ld_dout % kVec == 0 && aligned(d_dout, 16) && aligned(d_grad, 16)) return go(std::integral_constant<int, kVec>{});
-    return go(std::integral_constant<int, 1>{});
+    using Vector = std::integral_constant<int, kVec>;
+    using Single = std::integral_constant<int, 1>;
+    const bool vec = n % kVec == 0 && ld_dout % kVec == 0 && aligned(d_dout, 16) && aligned(d_grad, 16);
+    if (accumulate) return vec ? go(Vector{}, std::true_type{}) : go(Single{}, std::true_type{});
+    return vec ? go(Vector{}, std::false_type{}) : go(Single{}, std::false_type{});
 }
 
 int check_ckpt(int64_t T, int32_t n, int64_t ld_q) {
@@ -285,7 +308,7 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     if (!ctx) return LR_ERR_NULL;
     const int rc = check_ckpt(T, n, ld_q);
     if (rc != LR_OK) return rc;
-    if (C < 1 || C > 65536 || ld_dz < C || ld_dz > kMaxLd) return LR_ERR_SHAPE;
+    if (C < 1 || C > 65536 || ld_dz < C || ld_dz > (int64_t(1) << 28)) return LR_ERR_SHAPE;
     if (!d_grad_w || (T > 0 && (!d_q || !d_s || !d_dz))) return LR_ERR_NULL;
     if (!aligned(d_s, 4) || !aligned(d_dz, sizeof(E)) || !aligned(d_grad_w, 4) || !aligned(d_grad_b, 4)) return LR_ERR_ALIGNMENT;
     NvtxRange range("lr_ckpt8_grad");

@@ -20,8 +20,8 @@ def ctx(monkeypatch):
     rec = Recorder()
     monkeypatch.setattr(api, "lib", lambda: rec)
     monkeypatch.setattr(api.Context, "_stream", lambda self: 0)
-    empty = torch.empty
-    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **k: FakeCuda(empty(*a, **k)))
+    empty = torch.empty_strided
+    monkeypatch.setattr(torch, "empty_strided", lambda *a, device=None, **k: FakeCuda(empty(*a, **k)))
     c = api.Context.__new__(api.Context)
     c._h, c.device, c.n_max = ctypes.c_void_p(1), 0, 4096
     c.rec = rec

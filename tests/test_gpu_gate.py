@@ -173,7 +173,7 @@ def test_embed_grad_padding_and_tokens_outside(ctx):
     assert none.shape == (V, n) and bool((none == 0).all())
 
 
-@pytest.mark.parametrize("V", [255, 256, 65535, 65536, (1 << 24) - 1, 1 << 24])
+@pytest.mark.parametrize("V", [255, 256, 511, 512, 65535, 65536, (1 << 18) - 1, 1 << 18, (1 << 24) - 1, 1 << 24])
 def test_embed_grad_around_the_passes_of_the_sort(ctx, V):
     ids = torch.randint(0, V, (20000,), generator=gen(5), device="cuda")
     ids[:4] = torch.tensor([0, V - 1, V - 1, V // 2], device="cuda")
