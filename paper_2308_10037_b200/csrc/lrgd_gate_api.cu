@@ -55,6 +55,12 @@ int grid_for(const lr_ctx* ctx, int64_t units, int64_t per_cta, int per_sm) {
     return int(std::max<int64_t>(1, std::min<int64_t>((units + per_cta - 1) / per_cta, int64_t(plan_sms(ctx)) * per_sm)));
 }
 
+// The same with every CTA taking equally many turns, so that the last turn is not that of a few
+int even_grid(const lr_ctx* ctx, int64_t units, int64_t per_cta, int per_sm) {
+    const int64_t ctas = (units + per_cta - 1) / per_cta, most = int64_t(plan_sms(ctx)) * per_sm, turns = (ctas + most - 1) / most;
+    return int((ctas + turns - 1) / turns);
+}
+
 int check_route(int64_t T, int32_t E, int64_t ld, const lr_route_opt* o) {
     if (!o) return LR_ERR_NULL;
     if (T < 0 || T > kMaxTokens || E < 1 || E > kRouteMaxExperts || ld < E || ld > kMaxLd) return LR_ERR_SHAPE;
@@ -95,7 +101,7 @@ int route_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t ex
     }
     const RouteParams p{d_logits, ld, T, experts, opt->k, opt->groups, opt->top_groups, opt->renorm != 0, opt->factor,
                         d_bias, d_ids, d_weights, d_counts, ctx->d_gate_words};
-    const int grid = grid_for(ctx, T, kRouteWarps, 8);
+    const int grid = even_grid(ctx, T, kRouteWarps, 8);
     return launched(ctx, [&] {
         for_vpl(experts, [&](auto vpl) {
             constexpr int VPL = decltype(vpl)::value;
@@ -126,7 +132,7 @@ int route_grad_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const RouteGradParams p{d_logits, ld, T, experts, opt->k, opt->renorm != 0, opt->factor, d_ids, d_dweights, d_dlogits, ld_d};
-    const int grid = grid_for(ctx, T, kRouteWarps, 8);
+    const int grid = even_grid(ctx, T, kRouteWarps, 8);
     return launched(ctx, [&] {
         for_vpl(experts, [&](auto vpl) {
             constexpr int VPL = decltype(vpl)::value;

@@ -11,6 +11,9 @@
 //
 // The comparisons are on integers (a float's bits mapped so that their unsigned order is the float order), so the
 // choice is exact given the c values.  One warp per token, expert e in lane e % 32: a row is read once, coalesced, at any alignment.
+// The choice: k rounds of a warp-wide maximum over the lanes' largest values give a bound that at least k experts reach; those that
+// reach it (k and a few more) move to one lane each, where every lane counts how many of the others are better than its own.  That
+// leaves no round in which a lane has to search its values again.  Issue-bound: per token about 20 instructions per lane and expert.
 #pragma once
 #include "lrgd_convert.cuh"
 
@@ -72,8 +75,8 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int m = 16; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
     return v;
 }
-// The sigmoid as it is written: the choice compares these values, so their rounding is part of the definition.
-__device__ __forceinline__ float plain_sigmoid(float x) { return 1.0f / (1.0f + expf(-x)); }
+// The sigmoid as it is written, 1 / (1 + exp(-x)): the choice compares these values, so their rounding is part of the definition.
+__device__ __forceinline__ float plain_sigmoid(float x) { return __frcp_rn(1.0f + expf(-x)); }
 
 // Sigmoids that are only needed relative to one another: sigmoid(x) * exp(-m) = 1 / (exp(m) + exp(m - x)) with m the largest
 // chosen logit, at most 0.  With m = 0 it is the sigmoid itself; where all chosen ones would underflow, their ratio is kept.
@@ -83,13 +86,14 @@ __device__ __forceinline__ float relative_sigmoid(float x, float m) {
     return x > -INFINITY ? 1.0f / (expf(m) + expf(m - x)) : 0.0f;
 }
 
-// keys of order_key are above 0, which stands for "not to be chosen"
+constexpr uint32_t kKeyLowest = 0x00800000u;        // order_key of the lowest number; -inf and what is not to be chosen are below
 
 // VPL: experts per lane (E <= 32 * VPL).
 template <class E, int VPL, bool SOFTMAX, bool GROUPED>
 __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__ RouteParams p) {
     __shared__ int hist[VPL * 32];
     __shared__ float row_choice[GROUPED ? kRouteWarps : 1][GROUPED ? VPL * 32 : 1];
+    __shared__ unsigned long long candidate[kRouteWarps][32];       // key, then ~expert: the larger is the better one
     __shared__ unsigned int last_cta;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     constexpr uint32_t kAll = 0xffffffffu;
@@ -98,25 +102,26 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__
         __syncthreads();
     }
     const int group_size = p.E / p.groups;
+    const uint32_t group_inverse = ((1u << 20) + group_size - 1) / group_size;   // e / group_size = e * this >> 20 for e < 1024
+    float bias[VPL];
+#pragma unroll
+    for (int j = 0; j < VPL; ++j) bias[j] = p.bias && j * 32 + lane < p.E ? __ldg(p.bias + j * 32 + lane) : 0.0f;
     for (long long t = static_cast<long long>(blockIdx.x) * kRouteWarps + warp; t < p.T; t += static_cast<long long>(gridDim.x) * kRouteWarps) {
         const E* row = static_cast<const E*>(p.logits) + t * p.ld;
         uint32_t key[VPL];
+        float x[VPL];
         float row_max = -INFINITY;
         bool bad = false;
 #pragma unroll
+        for (int j = 0; j < VPL; ++j) x[j] = j * 32 + lane < p.E ? load_as_float(row + j * 32 + lane) : -INFINITY;
+#pragma unroll
         for (int j = 0; j < VPL; ++j) {
-            const int e = j * 32 + lane;
-            key[j] = 0;
-            float c = -INFINITY;
-            if (e < p.E) {
-                const float x = load_as_float(row + e);
-                bad |= SOFTMAX ? !(x < INFINITY) : x != x;
-                if constexpr (SOFTMAX) row_max = fmaxf(row_max, x);
-                c = (SOFTMAX ? x : plain_sigmoid(x)) + (p.bias ? __ldg(p.bias + e) : 0.0f);
-                if (!(x > -INFINITY) || !(c > -INFINITY)) c = -INFINITY;
-                else key[j] = order_key(c);
-            }
-            if constexpr (GROUPED) row_choice[warp][e] = c;
+            bad |= SOFTMAX ? !(x[j] < INFINITY) : x[j] != x[j];
+            if constexpr (SOFTMAX) row_max = fmaxf(row_max, x[j]);
+            float c = fmaxf((SOFTMAX ? x[j] : plain_sigmoid(x[j])) + bias[j], -INFINITY);      // (a NaN of the bias: -inf)
+            if (!SOFTMAX && x[j] == -INFINITY) c = -INFINITY;
+            key[j] = order_key(c + 0.0f);                           // (-0 as +0: they are equal)
+            if constexpr (GROUPED) row_choice[warp][j * 32 + lane] = c;
         }
         bad = __any_sync(kAll, bad);
         if constexpr (GROUPED) {
@@ -124,23 +129,26 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__
             // 32 / groups lanes per group find its two largest values, then the first of them collects the others' pairs
             const int per = 32 / p.groups, g = lane / per, sub = lane - g * per;
             float v1 = -INFINITY, v2 = -INFINITY;
-            if (g < p.groups)
+            if (g < p.groups) {
+                const float* mine = row_choice[warp] + g * group_size;
+#pragma unroll 4
                 for (int i = sub; i < group_size; i += per) {
-                    const float c = row_choice[warp][g * group_size + i];
+                    const float c = mine[i];
                     v2 = fmaxf(v2, fminf(v1, c));
                     v1 = fmaxf(v1, c);
                 }
+            }
             float a1 = v1, a2 = v2;
             for (int i = 1; i < per; ++i) {
                 const float o1 = __shfl_sync(kAll, v1, (lane + i) & 31), o2 = __shfl_sync(kAll, v2, (lane + i) & 31);
                 a2 = fmaxf(fmaxf(fminf(a1, o1), a2), o2);
                 a1 = fmaxf(a1, o1);
             }
-            // what lane h < groups holds now: the worth of group h, 0 if it has no expert to choose
+            // what lane h < groups holds now: the worth of group h, below kKeyLowest if it has no expert to choose
             a1 = __shfl_sync(kAll, a1, (lane * per) & 31);
             a2 = __shfl_sync(kAll, a2, (lane * per) & 31);
             const float worth = SOFTMAX || !(a2 > -INFINITY) ? a1 : a1 + a2;
-            const uint32_t wkey = lane < p.groups && a1 > -INFINITY ? order_key(worth + 0.0f) : 0u;
+            const uint32_t wkey = lane < p.groups ? order_key(worth + 0.0f) : 0u;
             int better = 0;
             for (int h = 0; h < p.groups; ++h) {
                 const uint32_t o = __shfl_sync(kAll, wkey, h);
@@ -148,35 +156,60 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__
             }
             const uint32_t kept = __ballot_sync(kAll, lane < p.groups && better < p.top_groups);
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const int e = j * 32 + lane;
-                if (e < p.E && !((kept >> (e / group_size)) & 1u)) key[j] = 0;
-            }
-            __syncwarp();                           // the next token's values go to the same place
+            for (int j = 0; j < VPL; ++j)
+                if (!((kept >> ((j * 32 + lane) * group_inverse >> 20)) & 1u)) key[j] = 0;
         }
+        // a bound that at least k experts reach, if there are k: the k-th largest of the lanes' maxima (equal ones count as one)
         uint32_t best = 0;
-        int slot = 0;
 #pragma unroll
-        for (int j = 0; j < VPL; ++j)
-            if (key[j] > best) { best = key[j]; slot = j; }
-        int my_id = -1;
+        for (int j = 0; j < VPL; ++j) best = max(best, key[j]);
+        uint32_t bound = 0, left = best;
         for (int r = 0; r < p.k; ++r) {
-            const uint32_t top = __reduce_max_sync(kAll, best);
-            if (top == 0) break;
-            const unsigned int e = __reduce_min_sync(kAll, best == top ? unsigned(slot * 32 + lane) : 0xffffffffu);
-            if (lane == r) my_id = int(e);
-            if (lane == int(e & 31u)) {
-                best = 0;
-                const int gone = slot;
+            bound = __reduce_max_sync(kAll, left);
+            if (left == bound) left = 0;
+        }
+        bound = max(bound, kKeyLowest);
+        int found = 0;
 #pragma unroll
-                for (int j = 0; j < VPL; ++j) {
-                    if (j == gone) key[j] = 0;
-                    if (key[j] > best) { best = key[j]; slot = j; }
-                }
+        for (int j = 0; j < VPL; ++j) {
+            const bool in = key[j] >= bound;
+            const uint32_t who = __ballot_sync(kAll, in);
+            if (who) {
+                const int at = found + __popc(who & ((1u << lane) - 1u));
+                if (in && at < 32) candidate[warp][at] = static_cast<unsigned long long>(key[j]) << 32 | ~unsigned(j * 32 + lane);
+                found += __popc(who);
             }
         }
-        // lane r < k holds the r-th expert: its probability again from the logit
-        if (bad) my_id = -1;
+        __syncwarp();
+        int my_id = -1, place = lane;               // this lane's expert and where it comes in the order
+        if (found <= 32) {
+            const unsigned long long own = lane < found ? candidate[warp][lane] : 0ull;
+            int better = 0;
+            for (int i = 0; i < found; ++i) better += candidate[warp][i] > own;
+            if (lane < found && better < p.k) {
+                my_id = static_cast<int>(~static_cast<unsigned int>(own));
+                place = better;
+            }
+            found = min(found, p.k);
+        } else {                                    // many equal values: one expert after the other, the lowest index first
+            found = p.k;
+            for (int r = 0; r < p.k; ++r) {
+                int slot = 0;
+                best = 0;
+#pragma unroll
+                for (int j = 0; j < VPL; ++j)
+                    if (key[j] > best) { best = key[j]; slot = j; }
+                const uint32_t top = __reduce_max_sync(kAll, best);
+                const unsigned int e = __reduce_min_sync(kAll, best == top ? unsigned(slot * 32 + lane) : 0xffffffffu);
+                if (lane == r) my_id = int(e);
+#pragma unroll
+                for (int j = 0; j < VPL; ++j)
+                    if (j * 32 + lane == int(e)) key[j] = 0;
+            }
+        }
+        __syncwarp();                               // the next token's values go to the same places
+        // the chosen experts stand in lanes of their own: their probabilities again from the logits
+        if (bad) { my_id = -1; found = 0; }
         float w = 0.0f;
         if constexpr (SOFTMAX) {
             float total = 1.0f, shift = 0.0f;
@@ -189,10 +222,7 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__
                 shift = warp_max(row_max);
                 float s = 0.0f;
 #pragma unroll
-                for (int j = 0; j < VPL; ++j) {
-                    const int e = j * 32 + lane;
-                    if (e < p.E) s += expf(load_as_float(row + e) - shift);
-                }
+                for (int j = 0; j < VPL; ++j) s += x[j] > -INFINITY ? expf(x[j] - shift) : 0.0f;
                 total = warp_sum(s);
                 w = my_id >= 0 ? expf(load_as_float(row + my_id) - shift) : 0.0f;
             }
@@ -205,10 +235,16 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__
                 w = total > 0.0f ? w / total : 0.0f;   // no expert chosen: 0
             }
         }
-        if (lane < p.k) {
-            p.ids[t * p.k + lane] = my_id;
-            p.weights[t * p.k + lane] = bad ? __int_as_float(0x7fc00000) : w * p.factor;
-            if (p.counts && my_id >= 0) atomicAdd(hist + my_id, 1);
+        int* out_ids = p.ids + t * p.k;
+        float* out_weights = p.weights + t * p.k;
+        if (my_id >= 0) {
+            out_ids[place] = my_id;
+            out_weights[place] = w * p.factor;
+            if (p.counts) atomicAdd(hist + my_id, 1);
+        }
+        if (lane >= found && lane < p.k) {          // places that no expert fills
+            out_ids[lane] = -1;
+            out_weights[lane] = bad ? __int_as_float(0x7fc00000) : 0.0f;
         }
     }
     if (!p.counts) return;
