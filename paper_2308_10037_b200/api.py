@@ -471,9 +471,7 @@ class Context:
         16 bytes apart or a multiple of that."""
         px, T, n, ld, sfx = self._rows(X, _ROW_TYPES, "X")
         pitch, dev = (n + 15) // 16 * 16, X.device
-        q = _new(T, pitch, torch.int8, dev)
-        if pitch != n:
-            q = q[:, :n]
+        q = torch.empty_strided((T, n), (pitch, 1), dtype=torch.int8, device=dev)
         s = _new(T, (n + CKPT8_GROUP - 1) // CKPT8_GROUP, torch.float32, dev)
         rc = getattr(lib(), "lr_ckpt8_save" + sfx)(self._h, px, ld, T, n, q.data_ptr(), pitch, s.data_ptr(), self._stream())
         if rc:

@@ -25,111 +25,167 @@ struct CkptParams {
     int groups;
 };
 
-__device__ __forceinline__ uint32_t half_warp_max_u32(uint32_t v) {
-#pragma unroll
-    for (int m = 8; m >= 1; m >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, m));
-    return v;
+// A warp takes 1024 columns of one row, all loaded before the first group is worked on (one group at a time left too few bytes in
+// flight).  VEC: 16-byte loads and 8-byte accesses to q; otherwise element by element, neighbouring lanes on neighbouring columns.
+// HBM-bound as long as a value costs few instructions: when saving, eight lanes share a group, so that its two divisions and the
+// exchange of the maximum are spread over sixteen values a lane; maxima of bfloat16 pairs are taken packed; rounding and widening go
+// through the mantissa of a float instead of the conversion unit.
+constexpr int kCkptSteps = 4;                               // when loading: pairs of groups, sixteen lanes each
+constexpr int kSaveSteps = 2;                               // when saving: fours of groups, eight lanes each
+constexpr int kCkptCols = kCkptSteps * 2 * kCkptGroup;      // columns of a row per warp
+static_assert(kCkptCols == kSaveSteps * 4 * kCkptGroup, "both kernels cut a row the same way");
+
+// fp32 pair -> packed bfloat16, to nearest even
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// rint(v), |v| <= 127, as the low byte: adding 1.5 * 2^23 leaves the integer (ties to even) in the mantissa's low bits
+__device__ __forceinline__ uint32_t rint_byte(float v) { return __float_as_uint(v + 12582912.0f); }
+__device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+// byte I of w (signed) as a float: with the sign bit flipped it is q + 128, which is read as the mantissa of 2^23 + q + 128
+template <int I>
+__device__ __forceinline__ float byte_to_float(uint32_t flipped) {
+    return __uint_as_float(__byte_perm(flipped, 0x4b000000u, 0x7540 | I)) - 8388736.0f;
 }
 
-// Sixteen lanes hold a group, eight values each.  VEC: eight neighbouring columns by 16-byte loads and one 8-byte store;
-// otherwise columns sixteen apart, element by element.
+// Eight values of a row: columns c0 .. c0 + 7 (VEC) or c0, c0 + 8, ..., c0 + 56
 template <class E, bool VEC>
-__global__ void __launch_bounds__(kCkptThreads) k_ckpt8_save(const __grid_constant__ CkptParams p) {
-    const int lane = threadIdx.x & 31, sub = lane & 15;
-    const long long units = p.T * p.groups;
-    const long long step = static_cast<long long>(gridDim.x) * (kCkptThreads / 16);
-    for (long long u0 = static_cast<long long>(blockIdx.x) * (kCkptThreads / 16) + (threadIdx.x >> 5) * 2; u0 < units; u0 += step) {
-        const long long u = u0 + (lane >> 4);
-        const bool on = u < units;
-        const long long t = on ? u / p.groups : 0;
-        const int g = on ? static_cast<int>(u - t * p.groups) : 0;
-        const int c0 = g * kCkptGroup + (VEC ? sub * 8 : sub);
-        const E* src = static_cast<const E*>(p.x) + t * p.ld + c0;
-        float v[8];
+struct CkptLane {
+    static constexpr int kWords = sizeof(E) == 4 ? 8 : 4;      // raw 32-bit words
+    uint32_t w[kWords];
+    __device__ __forceinline__ void load(const E* row, int c0, int n) {      // zeros past the end
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        for (int i = 0; i < kWords; ++i) w[i] = 0u;
         if constexpr (VEC) {
-            if (on && c0 < p.n) {
-                if constexpr (sizeof(E) == 4) {
-                    const float4 a = __ldcs(reinterpret_cast<const float4*>(src)), b = __ldcs(reinterpret_cast<const float4*>(src) + 1);
-                    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-                } else {
-                    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(src));
-                    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+            if (c0 < n) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[2 * i] = __uint_as_float(w[i] << 16);
-                        v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-                    }
+                for (int i = 0; i < kWords; i += 4) {
+                    const uint4 a = __ldcs(reinterpret_cast<const uint4*>(row + c0) + i / 4);
+                    w[i] = a.x; w[i + 1] = a.y; w[i + 2] = a.z; w[i + 3] = a.w;
                 }
             }
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (on && c0 + 16 * i < p.n) v[i] = load_as_float(src + 16 * i);
+                if (c0 + 8 * i < n) {
+                    if constexpr (sizeof(E) == 4) w[i] = __float_as_uint(__ldg(row + c0 + 8 * i));
+                    else w[i / 2] |= static_cast<uint32_t>(__ldg(row + c0 + 8 * i)) << (16 * (i & 1));
+                }
         }
-        // the largest magnitude as bits: a NaN is above an infinity, which is above every number
-        uint32_t top = 0;
+    }
+    __device__ __forceinline__ float value(int i) const {
+        if constexpr (sizeof(E) == 4) return __uint_as_float(w[i]);
+        else return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+    }
+    // bits of the largest magnitude: a NaN is above an infinity, which is above every number
+    __device__ __forceinline__ uint32_t top() const {
+        uint32_t t = 0;
+        if constexpr (sizeof(E) == 4) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
-        top = half_warp_max_u32(top);
-        const float a = __uint_as_float(top);
-        const bool lost = top >= 0x7f800000u, none = a < 1e-36f;
-        const float inv = lost || none ? 0.0f : 127.0f / a;
-        int q[8];
+            for (int i = 0; i < 8; ++i) t = max(t, w[i] & 0x7fffffffu);
+            return t;
+        } else {                                               // two 16-bit maxima
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = lost ? 0 : __float2int_rn(v[i] * inv);
-        signed char* dst = p.q + t * p.ld_q + c0;
+            for (int i = 0; i < 4; ++i) t = __vmaxu2(t, w[i] & 0x7fff7fffu);
+            return max(t & 0xffff0000u, t << 16);
+        }
+    }
+    __device__ __forceinline__ void store(signed char* out, int c0, int n, float inv, bool lost) const {
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = rint_byte(value(i) * inv);
         if constexpr (VEC) {
-            if (on && c0 < p.n) {
-                uint2 o;
-                o.x = (q[0] & 255) | (q[1] & 255) << 8 | (q[2] & 255) << 16 | static_cast<uint32_t>(q[3]) << 24;
-                o.y = (q[4] & 255) | (q[5] & 255) << 8 | (q[6] & 255) << 16 | static_cast<uint32_t>(q[7]) << 24;
-                *reinterpret_cast<uint2*>(dst) = o;
-            }
+            const uint32_t a = pack_bytes(q[0], q[1], q[2], q[3]), b = pack_bytes(q[4], q[5], q[6], q[7]);
+            if (c0 < n) *reinterpret_cast<uint2*>(out + c0) = lost ? make_uint2(0u, 0u) : make_uint2(a, b);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (on && c0 + 16 * i < p.n) dst[16 * i] = static_cast<signed char>(q[i]);
+                if (c0 + 8 * i < n) out[c0 + 8 * i] = lost ? 0 : static_cast<signed char>(q[i]);
         }
-        // (the cap matters for the largest finite values alone: 127 times a scale that was rounded up would be infinite)
-        if (on && sub == 0) p.s[u] = lost ? __int_as_float(0x7fc00000) : none ? 0.0f : fminf(a / 127.0f, __fdiv_rz(3.402823466e38f, 127.0f));
+    }
+};
+
+template <class E, bool VEC>
+__global__ void __launch_bounds__(kCkptThreads) k_ckpt8_save(const __grid_constant__ CkptParams p) {
+    const int lane = threadIdx.x & 31, sub = lane & 7;
+    const int first = blockIdx.y * (4 * kSaveSteps), mine = lane >> 3;       // groups first + 4 * k + mine
+    const long long warps = static_cast<long long>(gridDim.x) * (kCkptThreads / 32);
+    for (long long t = static_cast<long long>(blockIdx.x) * (kCkptThreads / 32) + (threadIdx.x >> 5); t < p.T; t += warps) {
+        const E* row = static_cast<const E*>(p.x) + t * p.ld;
+        signed char* out = p.q + t * p.ld_q;
+        float* scales = p.s + t * p.groups;
+        CkptLane<E, VEC> x[kSaveSteps][2];                     // the two halves of the group
+        const int c0 = (first + mine) * kCkptGroup + (VEC ? sub * 8 : sub);
+#pragma unroll
+        for (int k = 0; k < kSaveSteps; ++k) {
+            x[k][0].load(row, c0 + 4 * k * kCkptGroup, p.n);
+            x[k][1].load(row, c0 + 4 * k * kCkptGroup + kCkptGroup / 2, p.n);
+        }
+#pragma unroll
+        for (int k = 0; k < kSaveSteps; ++k) {
+            const int g = first + 4 * k + mine, c = c0 + 4 * k * kCkptGroup;
+            if (first + 4 * k >= p.groups) break;              // the same for the whole warp
+            uint32_t top = max(x[k][0].top(), x[k][1].top());
+#pragma unroll
+            for (int m = 4; m >= 1; m >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
+            const float a = __uint_as_float(top);
+            const bool lost = top >= 0x7f800000u, none = a < 1e-36f;
+            const float inv = none ? 0.0f : 127.0f / a;
+            x[k][0].store(out, c, p.n, inv, lost);
+            x[k][1].store(out, c + kCkptGroup / 2, p.n, inv, lost);
+            // (the cap matters for the largest finite values alone: 127 times a scale that was rounded up would be infinite)
+            if (sub == 0 && g < p.groups) scales[g] = lost ? __int_as_float(0x7fc00000) : none ? 0.0f : fminf(a / 127.0f, __fdiv_rz(3.402823466e38f, 127.0f));
+        }
     }
 }
 
 template <class E, bool VEC>
 __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_load(const __grid_constant__ CkptParams p) {
     const int lane = threadIdx.x & 31, sub = lane & 15;
-    const long long units = p.T * p.groups;
-    const long long step = static_cast<long long>(gridDim.x) * (kCkptThreads / 16);
-    for (long long u = static_cast<long long>(blockIdx.x) * (kCkptThreads / 16) + (threadIdx.x >> 4); u < units; u += step) {
-        const long long t = u / p.groups;
-        const int g = static_cast<int>(u - t * p.groups);
-        const int c0 = g * kCkptGroup + (VEC ? sub * 8 : sub);
-        const signed char* src = p.q + t * p.ld_q + c0;
-        E* dst = static_cast<E*>(p.back) + t * p.ld + c0;
-        const float s = __ldg(p.s + u);
-        if constexpr (VEC) {
-            if (c0 < p.n) {
-                const uint2 w = __ldcs(reinterpret_cast<const uint2*>(src));
-                E o[8];
+    const int first = blockIdx.y * (2 * kCkptSteps) + (lane >> 4);
+    const long long warps = static_cast<long long>(gridDim.x) * (kCkptThreads / 32);
+    for (long long t = static_cast<long long>(blockIdx.x) * (kCkptThreads / 32) + (threadIdx.x >> 5); t < p.T; t += warps) {
+        const signed char* row = p.q + t * p.ld_q;
+        E* out = static_cast<E*>(p.back) + t * p.ld;
+        uint2 w[kCkptSteps];
+        float s[kCkptSteps];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    store_from_float(&o[i], static_cast<float>(static_cast<signed char>(w.x >> (8 * i))) * s);
-                    store_from_float(&o[4 + i], static_cast<float>(static_cast<signed char>(w.y >> (8 * i))) * s);
-                }
-                if constexpr (sizeof(E) == 4) {
-                    reinterpret_cast<float4*>(dst)[0] = make_float4(o[0], o[1], o[2], o[3]);
-                    reinterpret_cast<float4*>(dst)[1] = make_float4(o[4], o[5], o[6], o[7]);
-                } else {
-                    *reinterpret_cast<uint4*>(dst) = make_uint4(o[0] | uint32_t(o[1]) << 16, o[2] | uint32_t(o[3]) << 16,
-                                                                o[4] | uint32_t(o[5]) << 16, o[6] | uint32_t(o[7]) << 16);
-                }
+        for (int k = 0; k < kCkptSteps; ++k) {
+            const int g = first + 2 * k, c0 = g * kCkptGroup + (VEC ? sub * 8 : sub);
+            w[k] = make_uint2(0u, 0u);
+            s[k] = g < p.groups ? __ldg(p.s + t * p.groups + g) : 0.0f;
+            if constexpr (VEC) {
+                if (c0 < p.n) w[k] = __ldcs(reinterpret_cast<const uint2*>(row + c0));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c0 + 16 * i < p.n) (i < 4 ? w[k].x : w[k].y) |= static_cast<uint32_t>(static_cast<unsigned char>(__ldg(row + c0 + 16 * i))) << (8 * (i & 3));
             }
-        } else {
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c0 + 16 * i < p.n) store_from_float(dst + 16 * i, static_cast<float>(src[16 * i]) * s);
+        for (int k = 0; k < kCkptSteps; ++k) {
+            const int c0 = (first + 2 * k) * kCkptGroup + (VEC ? sub * 8 : sub);
+            const uint32_t a = w[k].x ^ 0x80808080u, b = w[k].y ^ 0x80808080u;
+            const float v[8] = {byte_to_float<0>(a) * s[k], byte_to_float<1>(a) * s[k], byte_to_float<2>(a) * s[k], byte_to_float<3>(a) * s[k],
+                                byte_to_float<0>(b) * s[k], byte_to_float<1>(b) * s[k], byte_to_float<2>(b) * s[k], byte_to_float<3>(b) * s[k]};
+            if constexpr (VEC) {
+                if (c0 < p.n) {
+                    if constexpr (sizeof(E) == 4) {
+                        reinterpret_cast<float4*>(out + c0)[0] = make_float4(v[0], v[1], v[2], v[3]);
+                        reinterpret_cast<float4*>(out + c0)[1] = make_float4(v[4], v[5], v[6], v[7]);
+                    } else {
+                        *reinterpret_cast<uint4*>(out + c0) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (c0 + 16 * i < p.n) store_from_float(out + c0 + 16 * i, v[i]);
+            }
         }
     }
 }

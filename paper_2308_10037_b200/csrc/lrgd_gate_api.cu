@@ -293,7 +293,8 @@ int ckpt8_move(lr_ctx* ctx, bool save, const E* x, E* back, int64_t ld, int64_t 
     const int groups = (n + kCkptGroup - 1) / kCkptGroup;
     const CkptParams p{x, back, ld, q, ld_q, s, T, n, groups};
     const bool vec = n % 8 == 0 && ld % (16 / int(sizeof(E))) == 0 && ld_q % 8 == 0 && aligned(rows, 16) && aligned(q, 8);
-    const int grid = grid_for(ctx, T * groups, kCkptThreads / 16, 16);
+    const int blocks = (n + kCkptCols - 1) / kCkptCols;      // of columns, at most 2^24 / 1024
+    const dim3 grid(unsigned(grid_for(ctx, T, kCkptThreads / 32, std::max(1, 32 / blocks))), unsigned(blocks));
     return launched(ctx, [&] {
         if (save) {
             if (vec) k_ckpt8_save<E, true><<<grid, kCkptThreads, 0, st>>>(p);
