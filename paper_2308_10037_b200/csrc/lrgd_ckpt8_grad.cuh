@@ -412,8 +412,116 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
     if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
+// One class, X^T err of the binary model: bound by reading q, the pipeline above would only add its start and its conversions.
+// Sixteen lanes take 256 columns of a row, sixteen neighbouring ones per lane (VEC: one 16-byte load), a warp two rows at a time,
+// the CTA's warps take turns; kUnitAhead rows are loaded before the first is added.  Scale and dz are one factor per lane and row.
+// The sums of the lanes and warps that share a column meet in shared memory in a fixed order.
+constexpr int kUnitWarps = 16;
+constexpr int kUnitAhead = 4;
+constexpr int kUnitRows = 2 * kUnitWarps * kUnitAhead;               // rows of a turn of the CTA
+
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
+template <class E, bool VEC>
+__global__ void __launch_bounds__(kUnitWarps * 32) k_ckpt8_grad_unit(const __grid_constant__ CkptGradParams p) {
+    __shared__ float sums[kUnitWarps][256];
+    __shared__ float bias_sums[kUnitWarps];
+    grid_dependency_release();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane & 15;
+    const int c0 = blockIdx.x * 256 + (VEC ? sub * 16 : sub);        // columns c0 .. c0 + 15, or c0, c0 + 16, ...
+    const int g0 = blockIdx.x * 2;
+    const long long lo = blockIdx.y * p.rows, hi = min(p.T, lo + p.rows);
+    uint64_t acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0ull;
+    float zsum = 0.0f;
+    const long long first = lo + warp * 2 + (lane >> 4);
+    const signed char* row = p.q + first * p.ld_q + c0;
+    const float* scale = p.s + first * p.groups + g0 + (VEC ? sub >> 3 : 0);
+    const E* dz = static_cast<const E*>(p.dz) + first * p.ld_dz;
+    const bool in = c0 < p.n, two = g0 + 1 < p.groups;
+    for (long long t = first; t < hi; t += kUnitRows) {
+        uint4 w[kUnitAhead];
+        float f0[kUnitAhead], f1[kUnitAhead], z[kUnitAhead];
+#pragma unroll
+        for (int u = 0; u < kUnitAhead; ++u) {
+            w[u] = make_uint4(0u, 0u, 0u, 0u);
+            f0[u] = f1[u] = z[u] = 0.0f;
+            if (t + u * 2 * kUnitWarps < hi) {
+                if constexpr (VEC) {
+                    if (in) {
+                        w[u] = __ldcs(reinterpret_cast<const uint4*>(row));
+                        f0[u] = __ldg(scale);
+                    }
+                } else {
+                    uint32_t b[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (c0 + 16 * i < p.n) b[i / 4] |= static_cast<uint32_t>(static_cast<unsigned char>(__ldg(row + 16 * i))) << (8 * (i & 3));
+                    w[u] = make_uint4(b[0], b[1], b[2], b[3]);
+                    f0[u] = __ldg(scale);
+                    if (two) f1[u] = __ldg(scale + 1);
+                }
+                z[u] = load_as_float(dz);
+            }
+            row += 2 * kUnitWarps * p.ld_q;
+            scale += 2 * kUnitWarps * static_cast<long long>(p.groups);
+            dz += 2 * kUnitWarps * p.ld_dz;
+        }
+#pragma unroll
+        for (int u = 0; u < kUnitAhead; ++u) {
+            zsum += z[u];
+            const float a = z[u] * f0[u], b = VEC ? a : z[u] * f1[u];
+            const uint64_t fa = f32x2_pack(a, a), fb = f32x2_pack(b, b), bias = f32x2_pack(-8388736.0f, -8388736.0f);
+            const uint32_t q[4] = {w[u].x ^ 0x80808080u, w[u].y ^ 0x80808080u, w[u].z ^ 0x80808080u, w[u].w ^ 0x80808080u};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                // q + 128 as the mantissa of 2^23 + q + 128
+                const uint64_t x0 = f32x2_pack(__uint_as_float(__byte_perm(q[i], 0x4b000000u, 0x7540)), __uint_as_float(__byte_perm(q[i], 0x4b000000u, 0x7541)));
+                const uint64_t x1 = f32x2_pack(__uint_as_float(__byte_perm(q[i], 0x4b000000u, 0x7542)), __uint_as_float(__byte_perm(q[i], 0x4b000000u, 0x7543)));
+                acc[2 * i] = f32x2_fma(f32x2_add(x0, bias), i < 2 ? fa : fb, acc[2 * i]);
+                acc[2 * i + 1] = f32x2_fma(f32x2_add(x1, bias), i < 2 ? fa : fb, acc[2 * i + 1]);
+            }
+        }
+    }
+    // the two half-warps' rows, then the warps'
+    zsum += __shfl_xor_sync(0xffffffffu, zsum, 16);
+    if (lane == 0) bias_sums[warp] = zsum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        float even, odd;
+        f32x2_unpack(acc[i], even, odd);
+        even += __shfl_xor_sync(0xffffffffu, even, 16);
+        odd += __shfl_xor_sync(0xffffffffu, odd, 16);
+        if (lane < 16) {
+            sums[warp][VEC ? sub * 16 + 2 * i : sub + 32 * i] = even;
+            sums[warp][VEC ? sub * 16 + 2 * i + 1 : sub + 32 * i + 16] = odd;
+        }
+    }
+    __syncthreads();
+    const bool direct = p.chunks == 1;
+    const int col = blockIdx.x * 256 + threadIdx.x;
+    if (threadIdx.x < 256 && col < p.n) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kUnitWarps; ++w) sum += sums[w][threadIdx.x];
+        float* o = (direct ? p.grad_w : p.part_w + static_cast<long long>(blockIdx.y) * p.n) + col;
+        *o = direct && p.accumulate ? *o + sum : sum;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 256) {
+        float sum = 0.0f;
+        for (int w = 0; w < kUnitWarps; ++w) sum += bias_sums[w];
+        if (!direct) p.part_b[blockIdx.y] = sum;
+        else if (p.grad_b) *p.grad_b = p.accumulate ? *p.grad_b + sum : sum;
+    }
+}
+
 // Adds the parts in a fixed order.  Few parts (SLICES == 1): a thread adds those of four neighbouring values (VEC) in turn.  Many
-// parts: slice y of a value takes parts y, y + 8, ..., and the eight slices are added in turn.
+// parts: slice y of a value takes parts y, y + SLICES, ..., and the slices are added in turn.
 constexpr int kJoinThreads = 256;
 
 template <int VEC, int SLICES>

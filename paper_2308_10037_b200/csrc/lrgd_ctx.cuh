@@ -95,6 +95,7 @@ struct DeviceGuard {
     bool ok = true;
     explicit DeviceGuard(lr_ctx* c) {
         if (cudaGetDevice(&prev) != cudaSuccess) { prev = -1; }
+        if (prev == c->device) { prev = -1; return; }        // nothing to switch, nothing to switch back
         cudaError_t e = cudaSetDevice(c->device);
         if (e != cudaSuccess) { c->last_cuda = int(e); ok = false; }
     }

@@ -331,10 +331,11 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     }
     // CTAs take two groups of columns, a block of classes and a range of rows; as many ranges as fill the SMs once
     const int groups = (n + kCkptGroup - 1) / kCkptGroup, pairs = (groups + 1) / 2;
+    const bool one = C == 1;
     const int cblocks = (C + kTcMaxClasses - 1) / kTcMaxClasses, cblock = (C + cblocks - 1) / cblocks, cp = (cblock + 15) / 16 * 16;
-    const int64_t stages = (T + kTcRows - 1) / kTcRows;
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(stages, plan_sms(ctx) / (int64_t(pairs) * cblocks)));
-    const int64_t rows = (stages + want - 1) / want * kTcRows, chunks = (T + rows - 1) / rows;
+    const int64_t unit = one ? kUnitRows : kTcRows, units = (T + unit - 1) / unit;
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(units, plan_sms(ctx) * (one ? 2 : 1) / (int64_t(pairs) * cblocks)));
+    const int64_t rows = (units + want - 1) / want * unit, chunks = (T + rows - 1) / rows;
     float *part_w = nullptr, *part_b = nullptr;
     if (chunks > 1) {
         const size_t wb = (size_t(chunks) * C * n * 4 + 255) / 256 * 256;
@@ -348,7 +349,7 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     p.cp = cp;
     p.cblock = cblock;
     p.status = ctx->d_status;
-    const bool tma = aligned(d_q, 16) && ld_q % 16 == 0;
+    const bool tma = !one && aligned(d_q, 16) && ld_q % 16 == 0;
     CUtensorMap map{};
     if (tma) {
         EncodeTiledFn encode = nullptr;
@@ -364,7 +365,12 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     const dim3 grid{unsigned(pairs), unsigned(chunks), unsigned(cblocks)};
     const int smem = tc_smem_bytes(cp, tma);
     int r = LR_OK;
-    if (tma) {
+    if (one) {
+        r = launched(ctx, [&] {
+            if (ld_q % 16 == 0 && n % 16 == 0 && aligned(d_q, 16)) k_ckpt8_grad_unit<E, true><<<grid, kUnitWarps * 32, 0, st>>>(p.g);
+            else k_ckpt8_grad_unit<E, false><<<grid, kUnitWarps * 32, 0, st>>>(p.g);
+        });
+    } else if (tma) {
         LR_CK(ctx, (ensure_dynamic_smem<CkptGradTag<E, true>>(reinterpret_cast<const void*>(k_ckpt8_grad_tc<E, true>), smem)));
         r = launched(ctx, [&] { k_ckpt8_grad_tc<E, true><<<grid, kTcThreads, smem, st>>>(map, p); });
     } else {
@@ -380,7 +386,7 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
         ctx->launches += 1;
         return LR_OK;
     };
-    if (chunks > 16) return join(k_ckpt8_join<1, 8>, values, kJoinThreads / 8);
+    if (chunks > 16) return join(k_ckpt8_join<1, 32>, values, kJoinThreads / 32);
     if (vec) return join(k_ckpt8_join<4, 1>, values / 4, kJoinThreads);
     return join(k_ckpt8_join<1, 1>, values, kJoinThreads);
 }
