@@ -3,8 +3,8 @@
 //   grad_w[c,j] (+)= sum_t (dz[t,c] * s[t,g]) * q[t,j]   for the columns j of group g,      grad_b[c] (+)= sum_t dz[t,c]
 //
 // As a matrix product, D[j,(c)] = sum over t of A[j,t] B[t,c] with A = q^T, B = dz * s: the sum index is the row t, and the scale
-// differs from one group of 128 columns to the next, so B is formed per group.  q is an int8 operand as it is: a TMA copy puts
-// it where the tensor cores read it and nothing converts it.  For B the fp32 factor x = dz * s becomes a 31-bit integer
+// differs from one group of 128 columns to the next, so B is formed per group.  q is an int8 operand as it is: asynchronous copies
+// put it where the tensor cores read it and nothing converts it.  For B the fp32 factor x = dz * s becomes a 31-bit integer
 // I = rint(x * 2^k), cut into four signed bytes, I = d3 * 2^24 + d2 * 2^16 + d1 * 2^8 + d0, which stand side by side as 4 * CP
 // columns of B.  The products are summed in 32-bit integers, exactly, and the four sums of a class are put together in fp64 when
 // they are read back; the one rounding to fp32 is the last.  2^k belongs to a class, a group and a range of rows: it brings the
@@ -13,32 +13,40 @@
 // Measured against three bfloat16 terms with fp32 sums (24 bits, but q converted and every operand twice as wide): 16384 x 4096,
 // 64 classes, TCOLD us there, TCNEW us here.
 //
-// A CTA takes two groups (256 columns), one block of up to 64 classes and a range of rows, 32 rows per stage, kTcSlots stages in
-// flight.  A slot goes round: one warp copies q (TMA) and the scales in; four of sixteen warps write the bytes of dz * s beside
-// them, K-major (16 consecutive t of one byte and class are 16 bytes); one thread issues the tcgen05.mma of the stage, whose
-// completion frees the slot.  The parties meet on mbarriers alone.  Where q is not 16-byte aligned the four warps also place its
-// bytes.  The rows are split over CTAs to fill the GPU; k_ckpt8_join adds the parts in order.
+// A CTA takes two groups (256 columns), one block of up to 64 classes and a range of rows, 32 rows per stage.  Four warps copy q
+// and the scales into the slots of q, eleven to sixteen stages ahead, 16 bytes per lane and copy (tensor copies of 128-byte rows,
+// all that the operand's layout leaves them, ran at 4.2 TB/s at most); a set of one to four warps (16 classes each) writes the
+// bytes of dz * s into a slot of B, K-major (16 consecutive t of one byte and class are 16 bytes), the sets taking the stages in
+// turn; one thread issues the tcgen05.mma of the stage, whose completion frees both slots.  The parties meet on mbarriers alone.
+// Where q is not 16-byte aligned the set places its bytes.  The rows are split over CTAs to fill the GPU; k_ckpt8_join adds the parts in order.
 #pragma once
-#include <cuda.h>
-
 #include "lrgd_ckpt8.cuh"
 
 namespace lrgd {
 
-constexpr int kTcWarps = 16;                       // converting warps; one more issues the products, another one the copies
-constexpr int kTcThreads = (kTcWarps + 2) * 32;
-constexpr int kTcSets = 4;                         // sets of four converting warps: stage i is set i % 4's
+constexpr int kTcWarps = 16;                       // converting warps
+constexpr int kTcCopyWarps = 4;                    // copying warps, after them; the last two issue the products, one group each
+constexpr int kTcThreads = (kTcWarps + kTcCopyWarps + 2) * 32;
 constexpr int kTcRows = 32;                        // rows per stage: K of one tcgen05.mma on bytes
 constexpr int kTcMaxClasses = 64;
-constexpr int kTcSlots = 8;
-constexpr int kTcHeader = 4096;                    // barriers, flags and exponents (1 KB), then the scales of the slots
+constexpr int kTcMaxSlots = 16;
+constexpr int kTcHeader = 5120;                    // barriers, flags and exponents (1 KB), then the scales of the slots
 constexpr int kTcTileA = kTcRows * kCkptGroup;     // bytes of q per group and slot
 constexpr int64_t kTcMaxRows = 1 << 16;            // rows per CTA: 2^16 products of two bytes stay below 2^31
 constexpr int kTcMaxSub = 32;
-constexpr int tc_smem_bytes(int cp) {
-    const int need = kTcHeader + kTcSlots * 2 * (kTcTileA + 4 * cp * kTcRows) + 1024;
-    return need > 120 * 1024 ? need : 120 * 1024;  // more than half an SM's: one CTA per SM, which takes all of its tensor memory
+constexpr int kTcMaxSmem = 232448;                 // dynamic shared memory a CTA may ask for
+// Slots: those of dz * s first, then what is left for q (eleven for 64 classes, sixteen for 32 and fewer; always more than those
+// of dz * s, so that a slot of q comes round later than the slot of dz * s it was multiplied with).
+constexpr int tc_slots_b(int cp) { return cp <= 16 ? 14 : 8; }
+constexpr int tc_fixed_bytes(int cp) { return kTcHeader + tc_slots_b(cp) * 2 * 4 * cp * kTcRows + 1024; }
+constexpr int tc_slots_a(int cp) {
+    const int fit = (kTcMaxSmem - tc_fixed_bytes(cp)) / (2 * kTcTileA);
+    return fit < kTcMaxSlots ? fit : kTcMaxSlots;
 }
+// (always more than half an SM's: one CTA per SM, which takes all of its tensor memory)
+constexpr int tc_smem_bytes(int cp) { return tc_fixed_bytes(cp) + tc_slots_a(cp) * 2 * kTcTileA; }
+static_assert(tc_slots_a(64) > tc_slots_b(64) && tc_slots_a(48) > tc_slots_b(48) && tc_slots_a(16) > tc_slots_b(16), "see above");
+static_assert(tc_smem_bytes(16) > 120 * 1024, "one CTA per SM");
 
 struct CkptGradParams {
     const signed char* q;
@@ -62,6 +70,7 @@ struct CkptGradParams {
 struct TcGradParams {
     CkptGradParams g;
     int cp;                    // classes per block: a multiple of 16
+    int slots_a, slots_b;      // stages in flight, of q and of dz * s
     int sub;                   // parts of a chunk that k_ckpt8_ranges looks at one by one
     unsigned int* ranges;      // [chunks][sub][C + groups]: bits of the largest |dz| of a class and the largest |s| of a group
     int* status;
@@ -130,9 +139,13 @@ __device__ __forceinline__ void tmem_load8(uint32_t addr, int (&r)[8]) {
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-// Four bytes global -> shared, zeros where !real, and the arrival on `bar` of this thread when its copies so far have landed.
-__device__ __forceinline__ void async_copy4(float* dst, const float* src, bool real) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real ? 4 : 0) : "memory");
+// Asynchronous copies global -> shared of 4 or 16 bytes, of which the first `real` are read and the others zeros; then the arrival
+// on `bar` of this thread when its copies so far have landed.
+__device__ __forceinline__ void async_copy4(void* dst, const void* src, int real) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real) : "memory");
+}
+__device__ __forceinline__ void async_copy16(void* dst, const void* src, int real) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real) : "memory");
 }
 __device__ __forceinline__ void async_copy_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
@@ -168,23 +181,26 @@ __device__ __forceinline__ int factor_exponent(unsigned int dz, unsigned int s) 
     return min(28 - e, 126);
 }
 
-template <class E, bool TMA>
-__global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_constant__ CUtensorMap map, const __grid_constant__ TcGradParams tp) {
+template <class E, bool ALIGNED>
+__global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_constant__ TcGradParams tp) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     const CkptGradParams& p = tp.g;
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem);              // [kTcSlots] q and the scales of a stage have landed
-    uint64_t* ready = full + kTcSlots;                               // [kTcSlots] both operands are in place
-    uint64_t* done = ready + kTcSlots;                               // [kTcSlots] the products that read the slot are complete
-    uint32_t* tmem_at = reinterpret_cast<uint32_t*>(done + kTcSlots);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem);              // [slots_a] q and the scales of a stage have landed
+    uint64_t* done = full + kTcMaxSlots;                             // [slots_a] the products of the stage are complete
+    uint64_t* ready = done + kTcMaxSlots;                            // [slots_b] both operands are in place
+    uint64_t* last = ready + kTcMaxSlots;                            // [2 groups] all products are complete
+    uint32_t* tmem_at = reinterpret_cast<uint32_t*>(last + 2);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_at + 1);
-    volatile int* issued_at = abort_flag + 1;
     int* exponent = reinterpret_cast<int*>(smem + 512);              // [2 groups][kTcMaxClasses]
-    float* scales = reinterpret_cast<float*>(smem + 1024);           // [kTcSlots][2 groups][kTcRows]
+    float* scales = reinterpret_cast<float*>(smem + 1024);           // [slots_a][2 groups][kTcRows]
     const int cp = tp.cp, ncols = 4 * cp;
     const int tile_b = ncols * kTcRows;                              // bytes per group and slot
-    unsigned char* opa = smem + kTcHeader;                           // [kTcSlots][2 groups]
-    unsigned char* opb = opa + kTcSlots * 2 * kTcTileA;              // [kTcSlots][2 groups]
+    const int slots_a = tp.slots_a, slots_b = tp.slots_b;
+    // sets of converting warps; at most one per slot of B, so that none is more than a turn of a ring ahead of another
+    const int set_warps = cp / 16, sets = min(kTcWarps / set_warps, slots_b);
+    unsigned char* opa = smem + kTcHeader;                           // [slots_a][2 groups]
+    unsigned char* opb = opa + slots_a * 2 * kTcTileA;               // [slots_b][2 groups]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g0 = blockIdx.x * 2, groups = min(2, p.groups - g0);
     const int c0 = blockIdx.z * cp, classes = min(cp, p.C - c0);
@@ -193,13 +209,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
 
     grid_dependency_release();                                       // k_ckpt8_join may be launched; it waits for this kernel's end
     if (tid == 0) {
-        for (int i = 0; i < kTcSlots; ++i) {
-            mbar_init(full + i, 32 + (TMA ? 1 : 0));                 // the lanes that copy scales, and the copy of q
-            mbar_init(ready + i, kTcWarps / kTcSets);
-            mbar_init(done + i, 1);
+        for (int i = 0; i < slots_a; ++i) {
+            mbar_init(full + i, kTcCopyWarps * 32);                  // every copying lane, when its copies have landed
+            mbar_init(done + i, groups);
         }
+        for (int i = 0; i < slots_b; ++i) mbar_init(ready + i, set_warps);
         *abort_flag = 0;
-        *issued_at = 0;
+        for (int i = 0; i < 2; ++i) mbar_init(last + i, 1);
         fence_mbar_init();
     }
     if (warp == 0) tmem_alloc(tmem_at, 512);
@@ -210,48 +226,67 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
     bool ok = true;
     float zsum = 0.0f;
 
-    if (warp == kTcWarps) {
-        if (lane == 0) {
+    if (warp >= kTcWarps + kTcCopyWarps) {
+        const int gi = warp - kTcWarps - kTcCopyWarps;
+        if (lane == 0 && gi < groups) {
             // D int32, A and B int8, A with M contiguous
             const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (uint32_t(ncols / 8) << 17) | (uint32_t(kCkptGroup / 16) << 24);
-            const uint64_t a0 = desc_a(smem_u32(opa)), b0 = desc_b(smem_u32(opb), ncols * 16);
-            int stage = 0;
-            for (; stage < stages; ++stage) {
-                const int slot = stage % kTcSlots;
-                if (!mbar_wait_bounded(ready + slot, (stage / kTcSlots) & 1, abort_flag)) { ok = false; break; }
+            const uint64_t a0 = desc_a(smem_u32(opa + gi * kTcTileA)), b0 = desc_b(smem_u32(opb + gi * tile_b), ncols * 16);
+            const uint32_t d = tmem + gi * ncols, step_b = 2 * tile_b >> 4;         // (descriptors count in 16 bytes)
+            uint64_t a = a0, b = b0;
+            int slot = 0, slot_b = 0, parity = 0;
+#pragma unroll 1
+            for (int stage = 0; stage < stages; ++stage) {
+                if (!mbar_wait_bounded(ready + slot_b, parity, abort_flag)) { ok = false; break; }
                 tmem_fence_after();
-                for (int gi = 0; gi < groups; ++gi)                  // (descriptors count in 16 bytes)
-                    mma_int8(tmem + gi * ncols, a0 + ((slot * 2 + gi) * kTcTileA >> 4), b0 + ((slot * 2 + gi) * tile_b >> 4), idesc, stage > 0);
+                mma_int8(d, a, b, idesc, stage > 0);
                 mma_commit(done + slot);
+                a += 2 * kTcTileA >> 4;
+                b += step_b;
+                if (++slot == slots_a) { slot = 0; a = a0; }
+                if (++slot_b == slots_b) { slot_b = 0; b = b0; parity ^= 1; }
             }
-            *issued_at = stage;
+            mma_commit(last + gi);                                   // all products of this thread, also after giving up
+            if (!mbar_wait_drain(last + gi, 0)) ok = false;
         }
-    } else if (warp == kTcWarps + 1) {
-        const uint64_t policy = l2_policy_evict_first();
-        int stage = 0;
+    } else if (warp >= kTcWarps) {
+        // this warp: eight rows of every stage; a copy takes two rows, sixteen bytes per lane (rows and columns past the end: zeros)
+        const int row0 = (warp - kTcWarps) * 8, half = lane >> 4, piece = lane & 15;
+        const int bytes = ALIGNED ? max(0, min(16, p.n - g0 * kCkptGroup - piece * 16)) : 0;
+        const signed char* qp = p.q + (lo + row0 + half) * p.ld_q + g0 * kCkptGroup + (bytes > 0 ? piece * 16 : 0);
+        unsigned char* to = opa + (piece >> 3) * kTcTileA + (row0 + half) * 128;
+        const int sg = (lane >> 3) & 1;                              // lanes below 16: a scale each
+        const bool scales_too = lane < 16 && sg < groups;
+        const float* sp = p.s + (lo + row0 + (lane & 7)) * p.groups + g0 + (sg < groups ? sg : 0);
+        long long t = lo + row0;
+        int stage = 0, slot = 0, turn = 0;
         for (; stage < stages; ++stage) {
-            const int slot = stage % kTcSlots;
-            if (stage >= kTcSlots) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(done + slot, (stage / kTcSlots - 1) & 1, abort_flag));
+            if (turn > 0) {
+                ok = __all_sync(0xffffffffu, mbar_wait_bounded(done + slot, (turn - 1) & 1, abort_flag));
                 if (!ok) break;
             }
-            if (TMA && lane == 0) {
-                mbar_arrive_expect_tx(full + slot, uint32_t(groups * kTcTileA));
-                for (int gi = 0; gi < groups; ++gi)
-                    bulk_tensor_2d_g2s(opa + (slot * 2 + gi) * kTcTileA, &map, (g0 + gi) * kCkptGroup, int(lo) + stage * kTcRows, full + slot, policy);
+            if (ALIGNED) {
+                const signed char* src = qp;
+#pragma unroll
+                for (int k = 0; k < 4; ++k, src += 2 * p.ld_q) {
+                    const bool in = t + 2 * k + half < hi;
+                    async_copy16(to + slot * 2 * kTcTileA + 2 * k * 128 + (((piece & 7) ^ (2 * k + half)) << 4), in ? src : p.q, in ? bytes : 0);
+                }
+                qp += kTcRows * p.ld_q;
             }
-            // lane: one row of the stage, both groups' scales (rows past the end: zeros)
-            const long long t = lo + static_cast<long long>(stage) * kTcRows + lane;
-            const float* sp = p.s + min(t, hi - 1) * p.groups + g0;
-            float* dst = scales + slot * 2 * kTcRows + lane;
-            async_copy4(dst, sp, t < hi);
-            if (groups > 1) async_copy4(dst + kTcRows, sp + 1, t < hi);
+            if (scales_too) {
+                const bool in = t + (lane & 7) < hi;
+                async_copy4(scales + (slot * 2 + sg) * kTcRows + row0 + (lane & 7), in ? sp : p.s, in ? 4 : 0);
+            }
             async_copy_arrive(full + slot);
+            sp += static_cast<long long>(kTcRows) * p.groups;
+            t += kTcRows;
+            if (++slot == slots_a) { slot = 0; ++turn; }
         }
         // every copy lands before the CTA ends, also after giving up
-        for (int i = max(0, stage - kTcSlots); i < stage; ++i) mbar_wait_drain(full + i % kTcSlots, (i / kTcSlots) & 1);
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
-        const int set = warp >> 2, stid = tid & 127;
+        const int set = warp / set_warps, stid = tid - set * set_warps * 32;
         const int zk = stid / cp, zc = stid - zk * cp;               // this thread's part of dz: class c0 + zc, rows 16 * zk .. + 15
         const bool z_on = zk < kTcRows / 16, z_real = z_on && zc < classes;
         long long zt = lo + set * kTcRows + zk * 16;
@@ -266,8 +301,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
 #pragma unroll
                 for (int r = 0; r < 16; ++r, q += p.ld_dz) z[r] = z_real && zt + r < hi ? load_as_float(q) : 0.0f;
             }
-            zp += kTcSets * kTcRows * p.ld_dz;
-            zt += kTcSets * kTcRows;
+            zp += sets * kTcRows * p.ld_dz;
+            zt += sets * kTcRows;
         };
         load_dz();
         // exponents of the classes and groups of this CTA's rows
@@ -287,17 +322,22 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
             }
             exponent[gi * kTcMaxClasses + c] = e;
         }
-        asm volatile("bar.sync 1, 512;" ::: "memory");               // the converting warps
+        asm volatile("bar.sync 1, %0;" ::"n"(kTcWarps * 32) : "memory");               // the converting warps
         float factor[2];
 #pragma unroll
         for (int gi = 0; gi < 2; ++gi) {
             const int e = exponent[gi * kTcMaxClasses + (z_on ? zc : 0)];
             factor[gi] = e == kNotFinite ? 0.0f : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
         }
-        for (int stage = set; stage < stages; stage += kTcSets) {
-            const int slot = stage % kTcSlots;
-            // q and scales are there, and whatever read the slot before is done
-            ok = __all_sync(0xffffffffu, mbar_wait_bounded(full + slot, (stage / kTcSlots) & 1, abort_flag));
+        // the stage's slot of q, and that of the stage which had its slot of B before
+        int slot = set % slots_a, turn = set / slots_a, slot_b = set % slots_b;
+        int before = set - slots_b, before_turn = 0;
+        auto move = [](int& at, int& turn, int by, int ring) {
+            for (at += by; at >= ring; at -= ring) ++turn;
+        };
+        for (int stage = set < sets ? set : stages; stage < stages; stage += sets) {
+            const bool in_time = before < 0 || mbar_wait_bounded(done + before, before_turn & 1, abort_flag);
+            ok = __all_sync(0xffffffffu, in_time && mbar_wait_bounded(full + slot, turn & 1, abort_flag));
             if (!ok) break;
             if (z_on) {
                 zsum += (((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]))) + (((z[8] + z[9]) + (z[10] + z[11])) + ((z[12] + z[13]) + (z[14] + z[15])));
@@ -313,17 +353,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
                                               __float2int_rn(z[4 * r + 2] * s.z * factor[gi]), __float2int_rn(z[4 * r + 3] * s.w * factor[gi])};
                             bytes_of_four(v, word[r]);
                         }
-                        uint4* dst = reinterpret_cast<uint4*>(opb + (slot * 2 + gi) * tile_b + zk * (ncols * 16)) + zc;
+                        uint4* dst = reinterpret_cast<uint4*>(opb + (slot_b * 2 + gi) * tile_b + zk * (ncols * 16)) + zc;
 #pragma unroll
                         for (int d = 0; d < 4; ++d) dst[d * cp] = make_uint4(word[0][d], word[1][d], word[2][d], word[3][d]);
                     }
                 }
             }
-            if (stage + kTcSets < stages) load_dz();
-            if (!TMA) {
+            if (!ALIGNED) {
                 // sixteen bytes at a time from the words that hold them, to where the copy would have put them
 #pragma unroll 1
-                for (int u = stid; u < kTcRows * 2 * 8; u += 128) {
+                for (int u = stid; u < kTcRows * 2 * 8; u += set_warps * 32) {
                     const int row = u >> 4, gi = (u >> 3) & 1, piece = u & 7;
                     const long long t = lo + static_cast<long long>(stage) * kTcRows + row;
                     const int col = (g0 + gi) * kCkptGroup + piece * 16, left = min(16, p.n - col);
@@ -349,18 +388,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
             }
             fence_proxy_async_smem();                                // what was just stored is read by the tensor cores
             __syncwarp();
-            if (lane == 0) mbar_arrive(ready + slot);
+            if (lane == 0) mbar_arrive(ready + slot_b);
+            int none = 0;
+            move(slot, turn, sets, slots_a);
+            move(before, before_turn, sets, slots_a);
+            move(slot_b, none, sets, slots_b);
+            if (stage + sets < stages) load_dz();
         }
     }
-    // all warps get here: every wait above is bounded.  Then the products still in flight, before their memory is used again.
-    ok = __syncthreads_and(ok);
-    const int issued = *issued_at;
-    if (issued > 0 && !mbar_wait_drain(done + (issued - 1) % kTcSlots, ((issued - 1) / kTcSlots) & 1)) ok = false;
+    // all warps get here: every wait above is bounded, and the products are complete
     ok = __syncthreads_and(ok);
     tmem_fence_after();
     if (ok) {
         const bool direct = p.chunks == 1;
-        float* bsum = reinterpret_cast<float*>(opb);                 // [kTcSets][128]
+        float* bsum = reinterpret_cast<float*>(opb);                 // [kTcWarps][32]
         if (warp < kTcWarps) {
             bsum[tid] = zsum;
             // this warp: 32 columns of one group, classes 16 * i + 8 * half ..
@@ -392,8 +433,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
         __syncthreads();
         if (blockIdx.x == 0 && tid < classes) {
             float sum = 0.0f;
-            for (int k = 0; k < kTcSets; ++k)
-                for (int b = 0; b < kTcRows / 16; ++b) sum += bsum[k * 128 + b * cp + tid];
+            for (int k = 0; k < sets; ++k)
+                for (int b = 0; b < kTcRows / 16; ++b) sum += bsum[k * set_warps * 32 + b * cp + tid];
             if (!direct) p.part_b[static_cast<long long>(blockIdx.y) * p.C + c0 + tid] = sum;
             else if (p.grad_b) p.grad_b[c0 + tid] = p.accumulate ? p.grad_b[c0 + tid] + sum : sum;
         }

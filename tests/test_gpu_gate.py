@@ -490,11 +490,12 @@ def test_ckpt8_grad(ctx, dt, T, n, C):
     close(ob, wb, rel * mb)
 
 
+@pytest.mark.parametrize("C", [2, 16, 17, 40, 50])
 @pytest.mark.parametrize("shift", [0, 3])
 @pytest.mark.parametrize("T", [32, 33, 64, 65, 96, 511, 512, 513, 544, 545, 577, 1024, 1025, 1057, 1537, 5000])
-def test_ckpt8_grad_many_rows_per_cta(ctx, T, shift):
-    # one CTA for all rows: every number of stages, of buffer turns and of flushes of the accumulators
-    n, C = 300, 50
+def test_ckpt8_grad_many_rows_per_cta(ctx, T, shift, C):
+    # one CTA per block of columns for all rows: every number of stages, turns of the rings and sets of warps
+    n = 300
     q, s = ctx.ckpt8_save(rnd(T, n, seed=n))
     dz = rnd(T, C, seed=C)
     x = (padded_groups(q) * s.double()[:, :, None]).flatten(1)[:, :n]
