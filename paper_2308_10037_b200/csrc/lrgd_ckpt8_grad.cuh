@@ -3,8 +3,8 @@
 //   grad_w[c,j] (+)= sum_t (dz[t,c] * s[t,g]) * q[t,j]   for the columns j of group g,      grad_b[c] (+)= sum_t dz[t,c]
 //
 // As a matrix product, D[j,(c)] = sum over t of A[j,t] B[t,c] with A = q^T, B = dz * s: the sum index is the row t, and the scale
-// differs from one group of 128 columns to the next, so B is formed per group.  q is an int8 operand as it is: asynchronous copies
-// put it where the tensor cores read it and nothing converts it.  For B the fp32 factor x = dz * s becomes a 31-bit integer
+// differs from one group of 128 columns to the next, so B is formed per group.  q is an int8 operand as it is: a TMA copy puts
+// it where the tensor cores read it and nothing converts it.  For B the fp32 factor x = dz * s becomes a 31-bit integer
 // I = rint(x * 2^k), cut into four signed bytes, I = d3 * 2^24 + d2 * 2^16 + d1 * 2^8 + d0, which stand side by side as 4 * CP
 // columns of B.  The products are summed in 32-bit integers, exactly, and the four sums of a class are put together in fp64 when
 // they are read back; the one rounding to fp32 is the last.  2^k belongs to a class, a group and a range of rows: it brings the
@@ -13,20 +13,24 @@
 // Measured against three bfloat16 terms with fp32 sums (24 bits, but q converted and every operand twice as wide): 16384 x 4096,
 // 64 classes, TCOLD us there, TCNEW us here.
 //
-// A CTA takes two groups (256 columns), one block of up to 64 classes and a range of rows, 32 rows per stage.  Four warps copy q
-// and the scales into the slots of q, eleven to sixteen stages ahead, 16 bytes per lane and copy (tensor copies of 128-byte rows,
-// all that the operand's layout leaves them, ran at 4.2 TB/s at most); a set of one to four warps (16 classes each) writes the
+// A CTA takes two groups (256 columns), one block of up to 64 classes and a range of rows, 32 rows per stage.  One warp copies q
+// (TMA) and the scales into the slots of q, eleven to sixteen stages ahead; a set of one to four warps (16 classes each) writes the
 // bytes of dz * s into a slot of B, K-major (16 consecutive t of one byte and class are 16 bytes), the sets taking the stages in
-// turn; one thread issues the tcgen05.mma of the stage, whose completion frees both slots.  The parties meet on mbarriers alone.
-// Where q is not 16-byte aligned the set places its bytes.  The rows are split over CTAs to fill the GPU; k_ckpt8_join adds the parts in order.
+// turn; one thread per group issues the tcgen05.mma of the stage, whose completion frees both slots.  The parties meet on mbarriers
+// alone.  Where q is not 16-byte aligned the set places its bytes.  The rows are split over CTAs to fill the GPU; k_ckpt8_join adds
+// the parts in order.
+// What bounds it (clock readings of one CTA): with 64 classes the converting warps, 1900 clocks for the 16 rows x 32 classes x 2
+// groups of a warp and stage, four stages at a time; with few classes the issuing threads, about 500 clocks a stage: alone in
+// its warp, every instruction of such a thread costs its latency (one thread for both groups took 670 to 900).
 #pragma once
+#include <cuda.h>
+
 #include "lrgd_ckpt8.cuh"
 
 namespace lrgd {
 
 constexpr int kTcWarps = 16;                       // converting warps
-constexpr int kTcCopyWarps = 4;                    // copying warps, after them; the last two issue the products, one group each
-constexpr int kTcThreads = (kTcWarps + kTcCopyWarps + 2) * 32;
+constexpr int kTcThreads = (kTcWarps + 3) * 32;    // then a copying warp and two that issue the products, one group each
 constexpr int kTcRows = 32;                        // rows per stage: K of one tcgen05.mma on bytes
 constexpr int kTcMaxClasses = 64;
 constexpr int kTcMaxSlots = 16;
@@ -139,13 +143,9 @@ __device__ __forceinline__ void tmem_load8(uint32_t addr, int (&r)[8]) {
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-// Asynchronous copies global -> shared of 4 or 16 bytes, of which the first `real` are read and the others zeros; then the arrival
-// on `bar` of this thread when its copies so far have landed.
-__device__ __forceinline__ void async_copy4(void* dst, const void* src, int real) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real) : "memory");
-}
-__device__ __forceinline__ void async_copy16(void* dst, const void* src, int real) {
-    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real) : "memory");
+// Four bytes global -> shared, zeros where !real, and the arrival on `bar` of this thread when its copies so far have landed.
+__device__ __forceinline__ void async_copy4(float* dst, const float* src, bool real) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void async_copy_arrive(uint64_t* bar) {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
@@ -181,8 +181,8 @@ __device__ __forceinline__ int factor_exponent(unsigned int dz, unsigned int s) 
     return min(28 - e, 126);
 }
 
-template <class E, bool ALIGNED>
-__global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_constant__ TcGradParams tp) {
+template <class E, bool TMA>
+__global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_constant__ CUtensorMap map, const __grid_constant__ TcGradParams tp) {
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     const CkptGradParams& p = tp.g;
@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
     grid_dependency_release();                                       // k_ckpt8_join may be launched; it waits for this kernel's end
     if (tid == 0) {
         for (int i = 0; i < slots_a; ++i) {
-            mbar_init(full + i, kTcCopyWarps * 32);                  // every copying lane, when its copies have landed
+            mbar_init(full + i, 32 + (TMA ? 1 : 0));                 // the lanes that copy scales, and the copy of q
             mbar_init(done + i, groups);
         }
         for (int i = 0; i < slots_b; ++i) mbar_init(ready + i, set_warps);
@@ -226,8 +226,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
     bool ok = true;
     float zsum = 0.0f;
 
-    if (warp >= kTcWarps + kTcCopyWarps) {
-        const int gi = warp - kTcWarps - kTcCopyWarps;
+    if (warp > kTcWarps) {
+        const int gi = warp - kTcWarps - 1;
         if (lane == 0 && gi < groups) {
             // D int32, A and B int8, A with M contiguous
             const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (uint32_t(ncols / 8) << 17) | (uint32_t(kCkptGroup / 16) << 24);
@@ -249,57 +249,51 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
             mma_commit(last + gi);                                   // all products of this thread, also after giving up
             if (!mbar_wait_drain(last + gi, 0)) ok = false;
         }
-    } else if (warp >= kTcWarps) {
-        // this warp: eight rows of every stage; a copy takes two rows, sixteen bytes per lane (rows and columns past the end: zeros)
-        const int row0 = (warp - kTcWarps) * 8, half = lane >> 4, piece = lane & 15;
-        const int bytes = ALIGNED ? max(0, min(16, p.n - g0 * kCkptGroup - piece * 16)) : 0;
-        const signed char* qp = p.q + (lo + row0 + half) * p.ld_q + g0 * kCkptGroup + (bytes > 0 ? piece * 16 : 0);
-        unsigned char* to = opa + (piece >> 3) * kTcTileA + (row0 + half) * 128;
-        const int sg = (lane >> 3) & 1;                              // lanes below 16: a scale each
-        const bool scales_too = lane < 16 && sg < groups;
-        const float* sp = p.s + (lo + row0 + (lane & 7)) * p.groups + g0 + (sg < groups ? sg : 0);
-        long long t = lo + row0;
+    } else if (warp == kTcWarps) {
+        const uint64_t policy = l2_policy_evict_first();
+        // lane: one row of a stage, both groups' scales (rows past the end: zeros)
+        long long t = lo + lane;
+        const float* sp = p.s + min(t, hi - 1) * p.groups + g0;
         int stage = 0, slot = 0, turn = 0;
         for (; stage < stages; ++stage) {
             if (turn > 0) {
                 ok = __all_sync(0xffffffffu, mbar_wait_bounded(done + slot, (turn - 1) & 1, abort_flag));
                 if (!ok) break;
             }
-            if (ALIGNED) {
-                const signed char* src = qp;
-#pragma unroll
-                for (int k = 0; k < 4; ++k, src += 2 * p.ld_q) {
-                    const bool in = t + 2 * k + half < hi;
-                    async_copy16(to + slot * 2 * kTcTileA + 2 * k * 128 + (((piece & 7) ^ (2 * k + half)) << 4), in ? src : p.q, in ? bytes : 0);
-                }
-                qp += kTcRows * p.ld_q;
+            if (TMA && lane == 0) {
+                mbar_arrive_expect_tx(full + slot, uint32_t(groups * kTcTileA));
+                for (int gi = 0; gi < groups; ++gi)
+                    bulk_tensor_2d_g2s(opa + (slot * 2 + gi) * kTcTileA, &map, (g0 + gi) * kCkptGroup, int(lo) + stage * kTcRows, full + slot, policy);
             }
-            if (scales_too) {
-                const bool in = t + (lane & 7) < hi;
-                async_copy4(scales + (slot * 2 + sg) * kTcRows + row0 + (lane & 7), in ? sp : p.s, in ? 4 : 0);
-            }
+            float* dst = scales + slot * 2 * kTcRows + lane;
+            const bool in = t < hi;
+            async_copy4(dst, in ? sp : p.s, in);
+            if (groups > 1) async_copy4(dst + kTcRows, in ? sp + 1 : p.s, in);
             async_copy_arrive(full + slot);
-            sp += static_cast<long long>(kTcRows) * p.groups;
             t += kTcRows;
+            sp += static_cast<long long>(kTcRows) * p.groups;
             if (++slot == slots_a) { slot = 0; ++turn; }
         }
         // every copy lands before the CTA ends, also after giving up
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        for (int i = max(0, stage - slots_a); i < stage; ++i) mbar_wait_drain(full + i % slots_a, (i / slots_a) & 1);
     } else {
         const int set = warp / set_warps, stid = tid - set * set_warps * 32;
         const int zk = stid / cp, zc = stid - zk * cp;               // this thread's part of dz: class c0 + zc, rows 16 * zk .. + 15
         const bool z_on = zk < kTcRows / 16, z_real = z_on && zc < classes;
         long long zt = lo + set * kTcRows + zk * 16;
         const E* zp = static_cast<const E*>(p.dz) + c0 + zc + zt * p.ld_dz;
+        const uint32_t row_bytes = static_cast<uint32_t>(p.ld_dz) * sizeof(E);
         float z[16];
         auto load_dz = [&] {                                         // and on to this set's next stage
-            const E* q = zp;
+            // (a 32-bit factor: one multiply-add per address; ld_dz is at most 2^28)
+            const char* q = reinterpret_cast<const char*>(zp);
             if (z_real && zt + 16 <= hi) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r, q += p.ld_dz) z[r] = load_as_float(q);
+                for (unsigned int r = 0; r < 16; ++r) z[r] = load_as_float(reinterpret_cast<const E*>(q + static_cast<uint64_t>(row_bytes) * r));
             } else {
 #pragma unroll
-                for (int r = 0; r < 16; ++r, q += p.ld_dz) z[r] = z_real && zt + r < hi ? load_as_float(q) : 0.0f;
+                for (unsigned int r = 0; r < 16; ++r)
+                    z[r] = z_real && zt + r < hi ? load_as_float(reinterpret_cast<const E*>(q + static_cast<uint64_t>(row_bytes) * r)) : 0.0f;
             }
             zp += sets * kTcRows * p.ld_dz;
             zt += sets * kTcRows;
@@ -330,11 +324,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
             factor[gi] = e == kNotFinite ? 0.0f : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
         }
         // the stage's slot of q, and that of the stage which had its slot of B before
-        int slot = set % slots_a, turn = set / slots_a, slot_b = set % slots_b;
+        int slot = set, turn = 0, slot_b = set;
         int before = set - slots_b, before_turn = 0;
-        auto move = [](int& at, int& turn, int by, int ring) {
-            for (at += by; at >= ring; at -= ring) ++turn;
-        };
         for (int stage = set < sets ? set : stages; stage < stages; stage += sets) {
             const bool in_time = before < 0 || mbar_wait_bounded(done + before, before_turn & 1, abort_flag);
             ok = __all_sync(0xffffffffu, in_time && mbar_wait_bounded(full + slot, turn & 1, abort_flag));
@@ -359,7 +350,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
                     }
                 }
             }
-            if (!ALIGNED) {
+            if (!TMA) {
                 // sixteen bytes at a time from the words that hold them, to where the copy would have put them
 #pragma unroll 1
                 for (int u = stid; u < kTcRows * 2 * 8; u += set_warps * 32) {
@@ -389,11 +380,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
             fence_proxy_async_smem();                                // what was just stored is read by the tensor cores
             __syncwarp();
             if (lane == 0) mbar_arrive(ready + slot_b);
-            int none = 0;
-            move(slot, turn, sets, slots_a);
-            move(before, before_turn, sets, slots_a);
-            move(slot_b, none, sets, slots_b);
             if (stage + sets < stages) load_dz();
+            // (sets <= slots_b < slots_a)
+            slot += sets;
+            if (slot >= slots_a) { slot -= slots_a; ++turn; }
+            before += sets;
+            if (before >= slots_a) { before -= slots_a; ++before_turn; }
+            slot_b += sets;
+            if (slot_b >= slots_b) slot_b -= slots_b;
         }
     }
     // all warps get here: every wait above is bounded, and the products are complete

@@ -306,7 +306,7 @@ int ckpt8_move(lr_ctx* ctx, bool save, const E* x, E* back, int64_t ld, int64_t 
     });
 }
 
-template <class E, bool ALIGNED>
+template <class E, bool TMA>
 struct CkptGradTag {};
 
 template <class E>
@@ -365,16 +365,29 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
             else k_ckpt8_grad_unit<E, false><<<grid, kUnitWarps * 32, 0, st>>>(p.g);
         });
     } else {
+        const bool tma = aligned(d_q, 16) && ld_q % 16 == 0;
+        CUtensorMap map{};
+        if (tma) {
+            EncodeTiledFn encode = nullptr;
+            LR_CK(ctx, tensor_map_encoder(&encode));
+            const cuuint64_t dims[2] = {cuuint64_t(n), cuuint64_t(T)}, strides[1] = {cuuint64_t(ld_q)};
+            const cuuint32_t box[2] = {kCkptGroup, kTcRows}, step[2] = {1, 1};
+            if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(d_q), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+                ctx->last_cuda = int(cudaErrorInvalidValue);
+                return LR_ERR_CUDA;
+            }
+        }
         r = launched(ctx, [&] { k_ckpt8_ranges<E><<<dim3(unsigned(range_blocks), unsigned(chunks * sub)), kRangeThreads, 0, st>>>(p); });
         if (r != LR_OK) return r;
         const int smem = tc_smem_bytes(cp);
         auto go = [&](auto kern, auto tag) -> int {
             LR_CK(ctx, ensure_dynamic_smem<decltype(tag)>(reinterpret_cast<const void*>(kern), smem));
-            LR_CK(ctx, launch_kernel(kern, grid, dim3(kTcThreads), size_t(smem), st, ctx->overlap, p));
+            LR_CK(ctx, launch_kernel(kern, grid, dim3(kTcThreads), size_t(smem), st, ctx->overlap, map, p));
             ctx->launches += 1;
             return LR_OK;
         };
-        r = aligned(d_q, 16) && ld_q % 16 == 0 ? go(k_ckpt8_grad_tc<E, true>, CkptGradTag<E, true>{}) : go(k_ckpt8_grad_tc<E, false>, CkptGradTag<E, false>{});
+        r = tma ? go(k_ckpt8_grad_tc<E, true>, CkptGradTag<E, true>{}) : go(k_ckpt8_grad_tc<E, false>, CkptGradTag<E, false>{});
     }
     if (r != LR_OK || chunks == 1) return r;
     const int64_t values = int64_t(C) * n;
