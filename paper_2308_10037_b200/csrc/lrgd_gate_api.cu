@@ -334,7 +334,7 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     const bool one = C == 1;
     const int cblocks = (C + kTcMaxClasses - 1) / kTcMaxClasses, cp = ((C + cblocks - 1) / cblocks + 15) / 16 * 16;
     const int64_t unit = one ? kUnitRows : kTcRows, units = (T + unit - 1) / unit;
-    const int64_t fill = std::max<int64_t>(1, plan_sms(ctx) * (one ? 2 : 1) / (int64_t(pairs) * cblocks));
+    const int64_t fill = std::max<int64_t>(1, plan_sms(ctx) * (one ? kUnitCtas : 1) / (int64_t(pairs) * cblocks));
     const int64_t want = std::min<int64_t>(units, std::max<int64_t>(fill, (T + kTcMaxRows - 1) / kTcMaxRows));
     const int64_t rows = (units + want - 1) / want * unit, chunks = (T + rows - 1) / rows;
     if (chunks > 65535 || cblocks > 65535) return LR_ERR_SHAPE;
