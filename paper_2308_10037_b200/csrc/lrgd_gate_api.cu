@@ -132,13 +132,20 @@ int route_grad_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const RouteGradParams p{d_logits, ld, T, experts, opt->k, opt->renorm != 0, opt->factor, d_ids, d_dweights, d_dlogits, ld_d};
-    const int grid = even_grid(ctx, T, kRouteWarps, 8);
-    return launched(ctx, [&] {
-        for_vpl(experts, [&](auto vpl) {
-            constexpr int VPL = decltype(vpl)::value;
-            if (opt->score == LR_SCORE_SOFTMAX) k_route_grad<E, VPL, true><<<grid, kRouteThreads, 0, st>>>(p);
-            else k_route_grad<E, VPL, false><<<grid, kRouteThreads, 0, st>>>(p);
+    if (opt->score == LR_SCORE_SOFTMAX && !opt->renorm) {
+        const int grid = even_grid(ctx, T, kRouteWarps, 8);
+        return launched(ctx, [&] {
+            for_vpl(experts, [&](auto vpl) { k_route_grad_all<E, decltype(vpl)::value><<<grid, kRouteThreads, 0, st>>>(p); });
         });
+    }
+    int lanes = 1;
+    while (lanes < opt->k) lanes *= 2;
+    constexpr int kVec = 16 / int(sizeof(E));
+    const int vec = experts % kVec == 0 && ld_d % kVec == 0 && aligned(d_dlogits, 16);
+    const int grid = even_grid(ctx, T, kRouteWarps * (32 / lanes), 8);
+    return launched(ctx, [&] {
+        if (opt->score == LR_SCORE_SOFTMAX) k_route_grad_chosen<E, true><<<grid, kRouteThreads, 0, st>>>(p, lanes, vec);
+        else k_route_grad_chosen<E, false><<<grid, kRouteThreads, 0, st>>>(p, lanes, vec);
     });
 }
 

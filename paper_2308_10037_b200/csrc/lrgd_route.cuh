@@ -272,9 +272,67 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__
 //   sigmoid, renorm:    dl_i = factor (g_i - sum_j g_j w_j) w_i (1 - p_i),  w_i = p_i / S;      0 for the others
 //   softmax, renorm:    dl_i = factor (g_i - sum_j g_j w_j) w_i;                                0 for the others
 //   softmax:            dl_e = p_e (dp_e - sum_i dp_i p_i) for every expert,  dp_i = factor g_i for the chosen, else 0
-// Ids outside [0, E) (a slot that found no expert) carry no gradient.  One warp per token; lane r < k holds chosen expert r.
-template <class E, int VPL, bool SOFTMAX>
-__global__ void __launch_bounds__(kRouteThreads) k_route_grad(const __grid_constant__ RouteGradParams p) {
+// Ids outside [0, E) (a slot that found no expert) carry no gradient.
+//
+// Where only the chosen experts have a gradient, a warp takes 32 / L tokens, L lanes each (L: k rounded up to a power of two): the few
+// steps per token would leave most lanes of a warp idle.  It clears the tokens' rows (16 bytes at a time where they allow it), then
+// the lanes store their experts' values.  HBM-bound by the rows written.
+template <class E, bool SOFTMAX>
+__global__ void __launch_bounds__(kRouteThreads) k_route_grad_chosen(const __grid_constant__ RouteGradParams p, int lanes, int vec) {
+    const int lane = threadIdx.x & 31, sub = lane & (lanes - 1), tokens = 32 / lanes;
+    const long long step = static_cast<long long>(gridDim.x) * kRouteWarps * tokens;
+    auto group_sum = [&](float v) {
+        for (int m = lanes >> 1; m >= 1; m >>= 1) v += __shfl_xor_sync(0xffffffffu, v, m);
+        return v;
+    };
+    auto group_max = [&](float v) {
+        for (int m = lanes >> 1; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
+        return v;
+    };
+    for (long long t0 = (static_cast<long long>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5)) * tokens; t0 < p.T; t0 += step) {
+        const long long t = t0 + lane / lanes;
+        const bool mine = t < p.T && sub < p.k;
+        int id = mine ? __ldg(p.ids + t * p.k + sub) : -1;
+        if (id >= p.E) id = -1;
+        const float g = id >= 0 ? __ldg(p.dweights + t * p.k + sub) : 0.0f;
+        const float x = id >= 0 ? load_as_float(static_cast<const E*>(p.logits) + t * p.ld + id) : -INFINITY;
+        // the rows of this warp's tokens
+        const int rows = static_cast<int>(min(static_cast<long long>(tokens), p.T - t0));
+        E* out = static_cast<E*>(p.dlogits) + t0 * p.ld_d;
+        if (vec) {
+            const int per_row = p.E * static_cast<int>(sizeof(E)) / 16;
+            for (int r = 0; r < rows; ++r) {
+                uint4* q = reinterpret_cast<uint4*>(out + r * p.ld_d);
+                for (int i = lane; i < per_row; i += 32) q[i] = make_uint4(0u, 0u, 0u, 0u);
+            }
+        } else {
+            for (int r = 0; r < rows; ++r)
+                for (int i = lane; i < p.E; i += 32) store_from_float(out + r * p.ld_d + i, 0.0f);
+        }
+        float d;
+        if (SOFTMAX) {
+            const float top = group_max(x);
+            const float w0 = id >= 0 ? expf(x - top) : 0.0f;
+            const float w = w0 / fmaxf(group_sum(w0), 1.0f);     // the largest term is 1; no chosen expert at all: 0
+            d = w * (g - group_sum(g * w));
+        } else {
+            const float q = id >= 0 ? plain_sigmoid(x) : 0.0f;
+            if (p.renorm) {
+                const float r = relative_sigmoid(x, fminf(group_max(x), 0.0f)), S = group_sum(r);
+                const float w = S > 0.0f ? r / S : 0.0f;
+                d = (g - group_sum(g * w)) * w * (1.0f - q);
+            } else {
+                d = g * q * (1.0f - q);
+            }
+        }
+        __syncwarp();                               // the chosen ones replace the zeros
+        if (id >= 0) store_from_float(static_cast<E*>(p.dlogits) + t * p.ld_d + id, d * p.factor);
+    }
+}
+
+// Softmax without renormalisation: every expert has a gradient.  One warp per token; lane r < k holds chosen expert r.
+template <class E, int VPL>
+__global__ void __launch_bounds__(kRouteThreads) k_route_grad_all(const __grid_constant__ RouteGradParams p) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (long long t = static_cast<long long>(blockIdx.x) * kRouteWarps + warp; t < p.T; t += static_cast<long long>(gridDim.x) * kRouteWarps) {
         const E* row = static_cast<const E*>(p.logits) + t * p.ld;
@@ -283,53 +341,30 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_grad(const __grid_const
         if (id >= p.E) id = -1;
         const float g = id >= 0 ? p.factor * __ldg(p.dweights + t * p.k + lane) : 0.0f;
         const float x = id >= 0 ? load_as_float(row + id) : -INFINITY;
-        float d = 0.0f;                             // gradient of this lane's chosen logit
-        float rest = 0.0f;                          // softmax without renormalisation: minus the common term of all experts
-        float shift = 0.0f, total = 1.0f;
-        float v[VPL];
-        if (!SOFTMAX) {
-            const float q = id >= 0 ? plain_sigmoid(x) : 0.0f;
-            if (p.renorm) {
-                const float r = relative_sigmoid(x, sigmoid_shift(x)), S = warp_sum(r);
-                const float w = S > 0.0f ? r / S : 0.0f;
-                d = (g - warp_sum(g * w)) * w * (1.0f - q);
-            } else {
-                d = g * q * (1.0f - q);
-            }
-        } else if (p.renorm) {
-            shift = warp_max(x);
-            const float w0 = id >= 0 ? expf(x - shift) : 0.0f;
-            const float w = w0 / fmaxf(warp_sum(w0), 1.0f);    // the largest term is 1; no chosen expert at all: 0
-            d = w * (g - warp_sum(g * w));
-        } else {
-            float m = -INFINITY, s = 0.0f;
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                const int e = j * 32 + lane;
-                v[j] = e < p.E ? load_as_float(row + e) : -INFINITY;
-                m = fmaxf(m, v[j]);
-            }
-            shift = warp_max(m);
-#pragma unroll
-            for (int j = 0; j < VPL; ++j) {
-                v[j] = shift > -INFINITY ? expf(v[j] - shift) : 0.0f;
-                s += v[j];
-            }
-            total = warp_sum(s);
-            const float q = id >= 0 ? expf(x - shift) / total : 0.0f;
-            rest = warp_sum(g * q);
-            d = q * (g - rest);
-        }
+        float v[VPL], m = -INFINITY, s = 0.0f;
 #pragma unroll
         for (int j = 0; j < VPL; ++j) {
             const int e = j * 32 + lane;
-            float o = 0.0f;
-            if constexpr (SOFTMAX)
-                if (!p.renorm && rest != 0.0f) o = -(v[j] / total) * rest;
-            if (e < p.E) store_from_float(out + e, o);
+            v[j] = e < p.E ? load_as_float(row + e) : -INFINITY;
+            m = fmaxf(m, v[j]);
+        }
+        const float shift = warp_max(m);
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            v[j] = shift > -INFINITY ? expf(v[j] - shift) : 0.0f;
+            s += v[j];
+        }
+        const float total = warp_sum(s);
+        const float q = id >= 0 ? expf(x - shift) / total : 0.0f;
+        const float common = warp_sum(g * q);
+        const float scale = common != 0.0f ? -common / total : 0.0f;       // (an empty row: total is 0)
+#pragma unroll
+        for (int j = 0; j < VPL; ++j) {
+            const int e = j * 32 + lane;
+            if (e < p.E) store_from_float(out + e, v[j] * scale);
         }
         __syncwarp();                               // the chosen ones replace what was just written
-        if (id >= 0) store_from_float(out + id, d);
+        if (id >= 0) store_from_float(out + id, q * (g - common));
     }
 }
 
