@@ -576,3 +576,31 @@ def test_calls_can_be_captured(ctx):
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((grad, gw, gb), want))
+
+
+# ---- the operators together ------------------------------------------------------------------------------
+
+def test_token_gate_step_matches_automatic_differentiation(ctx):
+    from paper_2308_10037_b200.examples import token_gate
+    m = token_gate.TokenGate(vocab=300, n=48, experts=12, k=3, ctx=ctx, seed=3)
+    tokens = torch.randint(0, 300, (700,), generator=gen(9), device="cuda")
+    y = (torch.rand(700, generator=gen(10), device="cuda") < 0.5).float()
+    X, logits, ids, *_ = m.forward(tokens)
+    loss, _, (dtable, dW, db, da) = m.step(tokens, y)
+    p = [t.double().clone().requires_grad_(True) for t in (m.table, m.W, m.b, m.a)]
+    z64 = (p[0] * m.scale)[tokens] @ p[1].t() + p[2]
+    c = torch.sigmoid(z64).gather(1, ids.long())
+    ref = torch.nn.functional.binary_cross_entropy_with_logits(((c / c.sum(1, keepdim=True)) * p[3][ids.long()]).sum(1), y.double())
+    ref.backward()
+    # rows of about 1 in fp32, sums over 48 columns and 700 tokens: 1e-5 covers the roundings; the gate's own gradient sees rows that are
+    # off by half a step of 8 bits, a/254 with a about 2.5 times the rows' size, independently from row to row: 1 % of its norm
+    assert abs(loss.item() - ref.item()) <= 1e-5
+    for got, want, bound in ((dtable, p[0].grad, 1e-5), (dW, p[1].grad, 1e-2), (db, p[2].grad, 1e-5), (da, p[3].grad, 1e-5)):
+        assert (got.double() - want).norm() <= bound * want.norm()
+
+
+def test_token_gate_learns(ctx):
+    from paper_2308_10037_b200.examples import token_gate
+    _, losses, counts, _ = token_gate.train(120, ctx=ctx)
+    assert losses[-10:].mean() < 0.5 < losses[:5].mean()     # 0.69 at the start, 0.33 is the planted noise's
+    assert counts.sum().item() == 4096 * 2
