@@ -115,6 +115,12 @@ __device__ __forceinline__ void clear_floats(float* z, long long count, long lon
     if (me < count - head - quads * 4) z[head + quads * 4 + me] = 0.f;
 }
 
+// What another CTA of the cluster has placed: from L2, and not before the barrier that this follows.
+__device__ __forceinline__ uint2 load_placed(const uint2* p) {
+    uint2 v;
+    asm volatile("ld.global.cg.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
 // Lanes whose digit is the same (all 32 lanes call it; `digit` has kSortBits + 1 bits): one ballot per bit.
 __device__ __forceinline__ unsigned int lanes_alike(unsigned int digit) {
     unsigned int same = 0xffffffffu;
@@ -165,7 +171,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
         const int shift = kSortBits * pass;
         const uint2* from = p.place[(pass + 1) & 1];
         uint2* to = p.place[pass & 1];
-        auto place_at = [&](unsigned int i) -> uint2 { return pass > 0 ? __ldcg(from + i) : make_uint2(token_key(i), i); };
+        auto place_at = [&](unsigned int i) -> uint2 { return pass > 0 ? load_placed(from + i) : make_uint2(token_key(i), i); };
         auto digit_of = [&](unsigned int key) { return (key >> shift) & (kSortBins - 1u); };
         // first place of this CTA's elements of digit `tid` (threads below kSortBins): all smaller digits, then the same digit of
         // the CTAs before this one.  Every thread calls it.
@@ -352,17 +358,34 @@ struct RunCols {
     }
 };
 
-// CTA `index` of those that clear rows [from, to): its clear_rows of them, where no token points there
+// CTA `index` of those that clear rows [from, to): its clear_rows of them, where no token points there.  The bits of 32 rows are
+// taken into a register at once, so that the stores of one row do not wait for the look at the next.
 __device__ __forceinline__ void clear_absent_rows(const RunParams& p, long long from, long long to, long long index) {
     const long long r0 = from + index * p.clear_rows, r1 = min(to, r0 + p.clear_rows);
-    auto absent = [&](long long v) { return !((p.present[v >> 5] >> (v & 31)) & 1u); };
     if (p.n >= kRunThreads) {
-        for (long long v = r0 + threadIdx.x / kRunThreads; v < r1; v += blockDim.x / kRunThreads)
-            if (absent(v)) clear_floats(p.grad + v * p.n, p.n, threadIdx.x % kRunThreads, kRunThreads);
+        const int group = threadIdx.x / kRunThreads, groups = blockDim.x / kRunThreads, t = threadIdx.x % kRunThreads;
+        const bool whole = p.n % 4 == 0 && (reinterpret_cast<uintptr_t>(p.grad) & 15) == 0;
+        const int quads = p.n / 4;
+        for (long long v0 = r0 & ~31ll; v0 < r1; v0 += 32) {
+            const uint32_t here = p.present[v0 >> 5];
+#pragma unroll 4
+            for (int k = group; k < 32; k += groups) {
+                const long long v = v0 + k;
+                if (v < r0 || v >= r1 || ((here >> k) & 1u)) continue;
+                float* row = p.grad + v * p.n;
+                if (whole) {
+                    for (int i = t; i < quads; i += kRunThreads) reinterpret_cast<float4*>(row)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                } else {
+                    for (int i = t; i < p.n; i += kRunThreads) row[i] = 0.f;
+                }
+            }
+        }
     } else if (r1 > r0) {                                // narrow rows: several at a time
         const int count = static_cast<int>(r1 - r0) * p.n;
-        for (int i = threadIdx.x; i < count; i += blockDim.x)
-            if (absent(r0 + i / p.n)) p.grad[r0 * p.n + i] = 0.f;
+        for (int i = threadIdx.x; i < count; i += blockDim.x) {
+            const long long v = r0 + i / p.n;
+            if (!((p.present[v >> 5] >> (v & 31)) & 1u)) p.grad[r0 * p.n + i] = 0.f;
+        }
     }
 }
 
@@ -480,9 +503,9 @@ __global__ void __launch_bounds__(kRunThreads* kJoinGroups) k_run_join(const __g
         return;
     }
     const Cols cols(blockIdx.x % p.slices, p.n, tid);
-    const unsigned int runs = __ldcg(p.long_runs);
+    const unsigned int runs = *p.long_runs;
     for (unsigned int r = blockIdx.x / p.slices; r < runs; r += p.joiners) {
-        const int chunk = static_cast<int>(__ldcg(p.long_runs + 1 + r));
+        const int chunk = static_cast<int>(p.long_runs[1 + r]);
         const unsigned int v = p.place[static_cast<long long>(chunk + 1) * p.R].x;      // the run covers the chunk after its first
         // how far it goes: the first chunk whose first position holds another token
         if (threadIdx.x == 0) last_chunk = p.chunks;

@@ -232,6 +232,7 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
     constexpr int64_t kClearPerPass = 28 << 20, kClearPerToken = 1100, kClearLate = 40 << 20;
     const int64_t row_bytes = int64_t(n) * 4;
     const int64_t early = accumulate ? 0 : std::min<int64_t>(V, (sp.passes * (kClearPerPass + T * kClearPerToken)) / row_bytes);
+    if (early == V) sp.present = nullptr;          // all rows are cleared beside the sort: nobody asks which tokens occur
     sp.zero = d_grad;
     sp.zero_count = early * n;
     int clusters = 1;
