@@ -484,7 +484,7 @@ int lr_embed_grad_bf16(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const u
  *   chosen are the k largest c, in descending order, ties to the lower index (for groups as well)
  *   weight_i = factor * p_i / (sum of the chosen p) with renorm != 0, else factor * p_i
  * d_ids int32 [T][k], d_weights fp32 [T][k]; d_counts is NULL or int32 [experts] and receives how many tokens chose each expert.
- * An expert whose l or c is -inf is never chosen (a mask); where fewer than k are left the slots hold id -1 and weight 0.  (The
+ * An expert whose l or c is -inf is never chosen (a mask; a bias that is NaN counts as -inf); where fewer than k are left the slots hold id -1 and weight 0.  (The
  * c are compared as fp32 numbers; the renormalised weights keep their ratios even where every chosen p underflows.)  A row with a NaN logit (softmax: or +inf) gets ids -1 and NaN weights.
  * Limits: experts <= 1024, k <= 32, groups <= 32 and a divisor of experts, k <= top_groups * experts/groups.
  */
@@ -514,8 +514,8 @@ int lr_route_grad_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_
 
 /*
  * Rows kept in 8 bits between forward and backward.  Each row is cut into groups of 128 columns (the last one may be shorter) with
- * one scale each: a = max |x|, s = a / 127, q = rint(x * (127 / a)) in [-127, 127]; read back as q * s, so an element is off by
- * at most a / 254 (and two roundings).  d_q int8 [T][ld_q], d_s fp32 [T][ceil(n/128)] packed.  A group whose a is below 1e-36 is
+ * one scale each: a = max |x|, s = a / 127, q = rint(x * (127 / a)) in [-127, 127] (the quotients are rounded to fp32, the
+ * product once, to the integer, ties to even); read back as q * s, so an element is off by at most a / 254 (and two roundings).  d_q int8 [T][ld_q], d_s fp32 [T][ceil(n/128)] packed.  A group whose a is below 1e-36 is
  * kept as zeros; one with a NaN or an infinity gets the scale NaN and is read back as NaN.  n <= 2^24.
  * Fastest where n, ld_q are multiples of 8 and d_q is 8-byte aligned (16 for lr_ckpt8_grad).
  */

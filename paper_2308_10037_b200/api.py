@@ -430,8 +430,7 @@ class Context:
     def _route_opt(k, groups, top_groups, score, renorm, factor):
         if score not in _SCORES:
             raise ValueError(f"score: expected one of {sorted(_SCORES)}")
-        return LrRouteOpt(int(k), int(groups), int(groups if top_groups is None else top_groups), _SCORES[score], int(bool(renorm)),
-                          float(factor))
+        return LrRouteOpt(k, groups, top_groups, _SCORES[score], int(renorm), factor)
 
     def route(self, logits, k, bias=None, groups=1, top_groups=None, score="sigmoid", renorm=True, factor=1.0):
         """The ``k`` best experts of every row of ``logits`` [T, E] (float32 or bfloat16): (ids int32 [T, k], weights float32
@@ -439,7 +438,8 @@ class Context:
         only the experts of the ``top_groups`` best groups (default: all) can be chosen; ``renorm`` divides by the sum of the chosen;
         ``factor`` multiplies the weights.  See ``lr_route`` in the header for the exact rules."""
         pl, T, E, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
-        opt = self._route_opt(k, groups, top_groups, score, renorm, factor)
+        groups = int(groups)
+        opt = self._route_opt(int(k), groups, groups if top_groups is None else int(top_groups), score, bool(renorm), float(factor))
         pb = self._p(bias, torch.float32, "bias", E)
         width, dev = max(opt.k, 0), logits.device
         ids = _new(T, width, torch.int32, dev)
@@ -457,7 +457,7 @@ class Context:
         pl, T, E, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
         if not isinstance(ids, torch.Tensor) or ids.dim() != 2 or ids.shape[0] != T or not isinstance(dweights, torch.Tensor) or dweights.shape != ids.shape:
             raise ValueError("ids, dweights: expected two tensors [T, k]")
-        opt = self._route_opt(ids.shape[1], 1, 1, score, renorm, factor)
+        opt = self._route_opt(ids.shape[1], 1, 1, score, bool(renorm), float(factor))
         pi, pw = self._p(ids, torch.int32, "ids"), self._p(dweights, torch.float32, "dweights")
         res = _new(T, E, logits.dtype, logits.device) if out is None else out
         po, ldo = (res.data_ptr(), E) if out is None else self._rows(res, (logits.dtype,), "out", (T, E))[0:4:3]
@@ -705,14 +705,28 @@ def lr_predict(X, w, b, thr, ctx: Context | None = None):
     return _ctx_for(X, ctx).predict(X, w, _as_b(b, X.device), thr)
 
 
+_gate_ctx: dict[tuple[int, int], Context] = {}
+_gate_latest: dict[int, Context] = {}
+
+
 def _ctx_of(t, ctx: Context | None) -> Context:
-    """The default context of the tensor's device, for calls whose workspace does not depend on a number of columns."""
+    """The default context of the token-gate calls: one per device and stream, because a context's scratch serves one stream at a
+    time, and kept for good, because a captured graph may hold its address.  A stream that is being captured and has none yet
+    borrows the one used last on the device (the warm-up's: nothing can be allocated then); replays of such a graph must not overlap
+    with calls on the stream of the warm-up."""
     if ctx is not None:
         return ctx
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
         raise TypeError("expected a CUDA tensor")
-    c = _default_ctx.get(t.device.index)
-    return c if c is not None else _default_ctx.setdefault(t.device.index, Context(device=t.device.index))
+    dev = t.device.index
+    at = (dev, _raw_stream(dev))
+    c = _gate_ctx.get(at)
+    if c is None:
+        if dev in _gate_latest and torch.cuda.is_current_stream_capturing():
+            return _gate_latest[dev]
+        c = _gate_ctx[at] = Context(n_max=1, device=dev)
+    _gate_latest[dev] = c
+    return c
 
 
 def lr_embed(table, ids, scale=1.0, out=None, ctx: Context | None = None):

@@ -1,6 +1,7 @@
 // Rows kept between forward and backward in 8 bits.
 //
-//   save:      128 columns of a row share a scale:  a = max |x|,  s = a / 127,  q = rint(x * (127 / a))   (ties to even)
+//   save:      128 columns of a row share a scale:  a = max |x|,  s = a / 127,  q = rint(x * r), r = 127 / a   (s and r are
+//              rounded to fp32; the product is rounded once, to the integer, ties to even)
 //   load:      x' = q * s
 //
 // |x' - x| <= a/254 within a group (plus the rounding of the two products).  A group whose a is below 1e-36 (127 / a would
@@ -41,8 +42,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// rint(v), |v| <= 127, as the low byte: adding 1.5 * 2^23 leaves the integer (ties to even) in the mantissa's low bits
-__device__ __forceinline__ uint32_t rint_byte(float v) { return __float_as_uint(v + 12582912.0f); }
+// rint(v * r), at most 127, as the low byte: adding 1.5 * 2^23 leaves the integer (ties to even) in the mantissa's low bits
+__device__ __forceinline__ uint32_t rint_byte(float v, float r) { return __float_as_uint(__fmaf_rn(v, r, 12582912.0f)); }
 __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
@@ -97,7 +98,7 @@ struct CkptLane {
     __device__ __forceinline__ void store(signed char* out, int c0, int n, float inv, bool lost) const {
         uint32_t q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = rint_byte(value(i) * inv);
+        for (int i = 0; i < 8; ++i) q[i] = rint_byte(value(i), inv);
         if constexpr (VEC) {
             const uint32_t a = pack_bytes(q[0], q[1], q[2], q[3]), b = pack_bytes(q[4], q[5], q[6], q[7]);
             if (c0 < n) *reinterpret_cast<uint2*>(out + c0) = lost ? make_uint2(0u, 0u) : make_uint2(a, b);

@@ -558,6 +558,26 @@ def test_calls_run_on_the_current_stream(ctx):
     assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
+def test_default_contexts_of_two_streams_do_not_share_scratch(ctx):
+    # the module's functions keep a context per stream: calls that overlap on the GPU must not meet in one scratch
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    work = []
+    for i, st in enumerate(streams):
+        ids, dout, x = skewed(20000, 3000, i), rnd(20000, 128, seed=i + 2), rnd(20000, 96, seed=i + 4)
+        q, s = ctx.ckpt8_save(dout)
+        want = (ctx.embed_grad(ids, dout, 3000), ctx.route(x, 4)[2], *ctx.ckpt8_grad(q, s, x))
+        work.append((st, ids, dout, x, q, s, want))
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(5):
+        for i, (st, ids, dout, x, q, s, _) in enumerate(work):
+            with torch.cuda.stream(st):
+                got[i].append((api.lr_embed_grad(ids, dout, 3000), api.lr_route(x, 4)[2], *api.lr_ckpt8_grad(q, s, x)))
+    torch.cuda.synchronize()
+    for g, w in zip(got, work):
+        assert all(torch.equal(a, b) for one in g for a, b in zip(one, w[-1]))
+
+
 def test_calls_can_be_captured(ctx):
     ids, dout, x = skewed(5000, 500, 1), rnd(5000, 64, seed=2), rnd(5000, 64, seed=3)
     grad, dz = torch.empty(500, 64, device="cuda"), rnd(5000, 40, seed=4)
@@ -576,6 +596,15 @@ def test_calls_can_be_captured(ctx):
     graph.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip((grad, gw, gb), want))
+    # the module's functions: the capture borrows the context of the warm-up
+    api.lr_embed_grad(ids, dout, 500, out=grad)
+    graph2 = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph2):
+        api.lr_embed_grad(ids, dout, 500, out=grad)
+    grad.zero_()
+    graph2.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(grad, want[0])
 
 
 # ---- the operators together ------------------------------------------------------------------------------
