@@ -31,6 +31,7 @@ struct CkptParams {
 // HBM-bound as long as a value costs few instructions: when saving, eight lanes share a group, so that its two divisions and the
 // exchange of the maximum are spread over sixteen values a lane; maxima of bfloat16 pairs are taken packed; rounding and widening go
 // through the mantissa of a float instead of the conversion unit.
+// 16384 x 4096 bfloat16: save 33 us, load 30 us (203 MB each, 6.2 to 6.7 TB/s); with sixteen lanes a group when saving 46 us.
 constexpr int kCkptSteps = 4;                               // when loading: pairs of groups, sixteen lanes each
 constexpr int kSaveSteps = 2;                               // when saving: fours of groups, eight lanes each
 constexpr int kCkptCols = kCkptSteps * 2 * kCkptGroup;      // columns of a row per warp
