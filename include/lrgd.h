@@ -514,8 +514,8 @@ int lr_route_grad_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_
 
 /*
  * Rows kept in 8 bits between forward and backward.  Each row is cut into groups of 128 columns (the last one may be shorter) with
- * one scale each: a = max |x|, s = a / 127, q = rint(x * (127 / a)) in [-127, 127] (the quotients are rounded to fp32, the
- * product once, to the integer, ties to even); read back as q * s, so an element is off by at most a / 254 (and two roundings).  d_q int8 [T][ld_q], d_s fp32 [T][ceil(n/128)] packed.  A group whose a is below 1e-36 is
+ * one scale each: a = max |x|, s = a / 127, q = rint(x * (127 * (1 / a))) in [-127, 127] (each operation rounded to fp32,
+ * ties to even); read back as q * s, so an element is off by at most a / 254 (and two roundings).  d_q int8 [T][ld_q], d_s fp32 [T][ceil(n/128)] packed.  A group whose a is below 1e-36 is
  * kept as zeros; one with a NaN or an infinity gets the scale NaN and is read back as NaN.  n <= 2^24.
  * Fastest where n, ld_q are multiples of 8 and d_q is 8-byte aligned (16 for lr_ckpt8_grad).
  */

@@ -1,7 +1,7 @@
 // Rows kept between forward and backward in 8 bits.
 //
-//   save:      128 columns of a row share a scale:  a = max |x|,  s = a / 127,  q = rint(x * r), r = 127 / a   (s and r are
-//              rounded to fp32; the product is rounded once, to the integer, ties to even)
+//   save:      128 columns of a row share a scale:  a = max |x|,  s = a / 127,  q = rint(x * r), r = 127 * (1 / a)   (every
+//              operation rounded to fp32; ties to even)
 //   load:      x' = q * s
 //
 // |x' - x| <= a/254 within a group (plus the rounding of the two products).  A group whose a is below 1e-36 (127 / a would
@@ -43,8 +43,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// rint(v * r), at most 127, as the low byte: adding 1.5 * 2^23 leaves the integer (ties to even) in the mantissa's low bits
-__device__ __forceinline__ uint32_t rint_byte(float v, float r) { return __float_as_uint(__fmaf_rn(v, r, 12582912.0f)); }
+// rint(v * r), at most 127, as the low byte: adding 1.5 * 2^23 leaves the integer (ties to even) in the mantissa's low bits.  The
+// product is rounded first, as the definition has it: fused, one value in a million went to the other neighbour.
+__device__ __forceinline__ uint32_t rint_byte(float v, float r) { return __float_as_uint(__fadd_rn(__fmul_rn(v, r), 12582912.0f)); }
 __device__ __forceinline__ uint32_t pack_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
@@ -136,7 +137,7 @@ __global__ void __launch_bounds__(kCkptThreads) k_ckpt8_save(const __grid_consta
             for (int m = 4; m >= 1; m >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
             const float a = __uint_as_float(top);
             const bool lost = top >= 0x7f800000u, none = a < 1e-36f;
-            const float inv = none ? 0.0f : 127.0f / a;
+            const float inv = none ? 0.0f : __fmul_rn(__frcp_rn(a), 127.0f);
             x[k][0].store(out, c, p.n, inv, lost);
             x[k][1].store(out, c + kCkptGroup / 2, p.n, inv, lost);
             // (the cap matters for the largest finite values alone: 127 times a scale that was rounded up would be infinite)

@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kRouteThreads) k_route(const __grid_constant__
             const uint32_t kept = __ballot_sync(kAll, lane < p.groups && better < p.top_groups);
 #pragma unroll
             for (int j = 0; j < VPL; ++j)
-                if (!((kept >> (((j * 32 + lane) * group_inverse >> 20) & 31u)) & 1u)) key[j] = 0;    // (lanes past E: -inf anyway)
+                if (!(__funnelshift_rc(kept, 0u, (j * 32 + lane) * group_inverse >> 20) & 1u)) key[j] = 0;    // (past E: 0, -inf before)
         }
         // a bound that at least k experts reach, if there are k: the k-th largest of the lanes' maxima (equal ones count as one)
         uint32_t best = 0;
