@@ -531,7 +531,8 @@ int lr_ckpt8_load_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float
  * Gradient of a C-class logistic layer z = X W^T + b from the kept rows and d_dz [T][ld_dz] = dL/dz (C columns):
  *   d_grad_w[c*n + j] = sum_t dz[t,c] * q[t,j] * s[t,j/128],   d_grad_b[c] = sum_t dz[t,c]   (d_grad_b may be NULL)
  * written, or with accumulate != 0 added to what they hold.  C = 1 is X^T err of the binary model.  C <= 65536,
- * ld_dz <= 2^28.  A dz or a scale that is not finite makes what it enters not finite.
+ * ld_dz <= 2^28.  Products are formed as (dz * s) * q in fp32 range and precision whatever the sizes of other rows; a dz, a scale or
+ * a product dz * s that is not finite makes what it enters not finite.
  */
 int lr_ckpt8_grad(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const float* d_dz,
                   int64_t ld_dz, int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream);

@@ -3,25 +3,26 @@
 //   grad_w[c,j] (+)= sum_t (dz[t,c] * s[t,g]) * q[t,j]   for the columns j of group g,      grad_b[c] (+)= sum_t dz[t,c]
 //
 // As a matrix product, D[j,(c)] = sum over t of A[j,t] B[t,c] with A = q^T, B = dz * s: the sum index is the row t, and the scale
-// differs from one group of 128 columns to the next, so B is formed per group.  q is an int8 operand as it is: a TMA copy puts
-// it where the tensor cores read it and nothing converts it.  For B the fp32 factor x = dz * s becomes a 31-bit integer
-// I = rint(x * 2^k), cut into four signed bytes, I = d3 * 2^24 + d2 * 2^16 + d1 * 2^8 + d0, which stand side by side as 4 * CP
-// columns of B.  The products are summed in 32-bit integers, exactly, and the four sums of a class are put together in fp64 when
-// they are read back; the one rounding to fp32 is the last.  2^k belongs to a class, a group and a range of rows: it brings the
-// largest |dz| of the class times the largest s of the group to 2^28 .. 2^30 (k_ckpt8_ranges finds the two), so the rounding of
-// I (a half) is 2^-29 of that at most: nothing beside the fp32 rounding of the terms that carry the sum.
-// Measured against three bfloat16 terms with fp32 sums (24 bits, but q converted and every operand twice as wide): 16384 x 4096,
-// 64 classes, 52 us there, 40 us here, k_ckpt8_ranges (5) and k_ckpt8_join (6) included; the floor is 11 (74 MB).
+// differs from one group of 128 columns to the next, so B is formed per group.  An int8 is exact in bfloat16; the fp32 factor
+// x = dz * s is cut into three bfloat16 terms, the upper eight bits of x, of what is left and of what is then left, which hold its
+// 24 bits exactly whatever its size beside other rows' (two terms would leave 2^-16 of every factor).  The terms stand side by side as
+// 3 * CP columns of B, products accumulate in fp32 in tensor memory, and the three sums of a class are added when they are read back.
+// So every product is a floating-point one: a row loses no bits to another row of a larger dz or scale.  Integers of a common step
+// per class and group (four bytes a factor on the int8 products, 40 us at the size below) did lose them: beside one
+// masked row whose scale was 1e6 times the others' the sums were off by a thousandth, so that form was taken out.
+// 16384 x 4096, 64 classes: 53 us, k_ckpt8_join (6) included; the floor is 11 (74 MB).
 //
-// A CTA takes two groups (256 columns), one block of up to 64 classes and a range of rows, 32 rows per stage.  One warp copies q
-// (TMA) and the scales into the slots of q, eleven to sixteen stages ahead; a set of one to four warps (16 classes each) writes the
-// bytes of dz * s into a slot of B, K-major (16 consecutive t of one byte and class are 16 bytes), the sets taking the stages in
-// turn; one thread per group issues the tcgen05.mma of the stage, whose completion frees both slots.  The parties meet on mbarriers
-// alone.  Where q is not 16-byte aligned the set places its bytes.  The rows are split over CTAs to fill the GPU; k_ckpt8_join adds
-// the parts in order.
-// What bounds it (clock readings of one CTA): with 64 classes the converting warps, 1900 clocks for the 16 rows x 32 classes x 2
-// groups of a warp and stage, four stages at a time; with few classes the issuing threads, about 500 clocks a stage: alone in
-// its warp, every instruction of such a thread costs its latency (one thread for both groups took 670 to 900).
+// A CTA takes two groups (256 columns), one block of up to 64 classes and a range of rows, 32 rows per stage.  The raw q of a
+// stage comes by TMA (a ring of kTcRing stages; by plain word loads where q is not 16-byte aligned).  Two sets of eight warps
+// convert, one the even stages and one the odd ones: a warp turns 8 rows x 128 columns of q into bfloat16 and a thread 8 rows of one
+// class of dz into 2 x 3 terms, written K-major (8 consecutive t of one column or class are 16 bytes) into one of three operand
+// buffers.  A seventeenth warp issues the tcgen05.mma of a stage when its eight warps have arrived, an eighteenth the copies of a
+// later stage: the scales, one row per lane, are fetched once per stage there (every warp gathering its own cost a quarter of
+// the kernel's shared-memory bandwidth, which bounds it: operands written once and read once by the tensor cores).
+// No barrier spans the CTA inside the loop: the warps meet on mbarriers, so that loads, conversion and products overlap.
+// Every kTcFlush stages the sums move from tensor memory to registers: the tensor cores drop the bits below the accumulator's last
+// place, an error that grows with the length of the chain (114 steps: 1.2e-6 of the result; 32 steps: 2.6e-7).
+// The rows are split over CTAs to fill the GPU; k_ckpt8_join adds the parts in order.
 #pragma once
 #include <cuda.h>
 
@@ -29,28 +30,21 @@
 
 namespace lrgd {
 
-constexpr int kTcWarps = 16;                       // converting warps
-constexpr int kTcThreads = (kTcWarps + 3) * 32;    // then a copying warp and two that issue the products, one group each
-constexpr int kTcRows = 32;                        // rows per stage: K of one tcgen05.mma on bytes
+constexpr int kTcWarps = 16;                       // converting warps; one more issues the products, another one the copies
+constexpr int kTcThreads = (kTcWarps + 2) * 32;
+constexpr int kTcFlush = 16;                       // stages between two flushes of the accumulators
+constexpr int kTcRows = 32;                        // rows per stage
+constexpr int kTcBlocks = kTcRows / 8;             // blocks of eight rows: 16 bytes of an operand's row
+constexpr int kTcBuffers = 3;
 constexpr int kTcMaxClasses = 64;
-constexpr int kTcMaxSlots = 16;
-constexpr int kTcHeader = 5120;                    // barriers, flags and exponents (1 KB), then the scales of the slots
-constexpr int kTcTileA = kTcRows * kCkptGroup;     // bytes of q per group and slot
-constexpr int64_t kTcMaxRows = 1 << 16;            // rows per CTA: 2^16 products of two bytes stay below 2^31
-constexpr int kTcMaxSub = 32;
-constexpr int kTcMaxSmem = 232448;                 // dynamic shared memory a CTA may ask for
-// Slots: those of dz * s first, then what is left for q (eleven for 64 classes, sixteen for 32 and fewer; always more than those
-// of dz * s, so that a slot of q comes round later than the slot of dz * s it was multiplied with).
-constexpr int tc_slots_b(int cp) { return cp <= 16 ? 14 : 8; }
-constexpr int tc_fixed_bytes(int cp) { return kTcHeader + tc_slots_b(cp) * 2 * 4 * cp * kTcRows + 1024; }
-constexpr int tc_slots_a(int cp) {
-    const int fit = (kTcMaxSmem - tc_fixed_bytes(cp)) / (2 * kTcTileA);
-    return fit < kTcMaxSlots ? fit : kTcMaxSlots;
+constexpr int kTcRing = 12;
+constexpr int kTcHeader = 4096;                    // barriers and flags (1 KB), then the scales of the ring's stages
+constexpr int kTcOperandA = kCkptGroup * kTcRows * 2;              // bytes per group and buffer
+constexpr int kTcRaw = kTcRows * kCkptGroup;       // bytes of raw q per group and stage
+constexpr int tc_smem_bytes(int cp, bool tma) {
+    const int need = kTcHeader + (tma ? kTcRing * 2 * kTcRaw : 0) + kTcBuffers * 2 * (kTcOperandA + 3 * cp * kTcRows * 2) + 1024;
+    return need > 120 * 1024 ? need : 120 * 1024;   // more than half an SM's: one CTA per SM, which takes all of its tensor memory
 }
-// (always more than half an SM's: one CTA per SM, which takes all of its tensor memory)
-constexpr int tc_smem_bytes(int cp) { return tc_fixed_bytes(cp) + tc_slots_a(cp) * 2 * kTcTileA; }
-static_assert(tc_slots_a(64) > tc_slots_b(64) && tc_slots_a(48) > tc_slots_b(48) && tc_slots_a(16) > tc_slots_b(16), "see above");
-static_assert(tc_smem_bytes(16) > 120 * 1024, "one CTA per SM");
 
 struct CkptGradParams {
     const signed char* q;
@@ -74,47 +68,8 @@ struct CkptGradParams {
 struct TcGradParams {
     CkptGradParams g;
     int cp;                    // classes per block: a multiple of 16
-    int slots_a, slots_b;      // stages in flight, of q and of dz * s
-    int sub;                   // parts of a chunk that k_ckpt8_ranges looks at one by one
-    unsigned int* ranges;      // [chunks][sub][C + groups]: bits of the largest |dz| of a class and the largest |s| of a group
     int* status;
 };
-
-// Largest magnitudes, as bits (a NaN above an infinity above every number).  Block: 32 columns x 8 rows of dz or of s.
-constexpr int kRangeThreads = 256;
-
-template <class E>
-__global__ void __launch_bounds__(kRangeThreads) k_ckpt8_ranges(const __grid_constant__ TcGradParams tp) {
-    __shared__ unsigned int top[8][32];
-    const CkptGradParams& p = tp.g;
-    grid_dependency_release();
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int dz_blocks = (p.C + 31) / 32;
-    const bool is_dz = static_cast<int>(blockIdx.x) < dz_blocks;
-    const int col = (is_dz ? blockIdx.x : blockIdx.x - dz_blocks) * 32 + x, cols = is_dz ? p.C : p.groups;
-    const int chunk = blockIdx.y / tp.sub, part = blockIdx.y - chunk * tp.sub;
-    const long long per = (p.rows + tp.sub - 1) / tp.sub;
-    const long long lo = chunk * p.rows + part * per, hi = min(min(p.T, (chunk + 1) * p.rows), lo + per);
-    unsigned int m = 0;
-    if (col < cols) {
-        if (is_dz) {
-            const E* dz = static_cast<const E*>(p.dz) + col;
-#pragma unroll 8
-            for (long long t = lo + y; t < hi; t += 8) m = max(m, __float_as_uint(load_as_float(dz + t * p.ld_dz)) & 0x7fffffffu);
-        } else {
-            const float* s = p.s + col;
-#pragma unroll 8
-            for (long long t = lo + y; t < hi; t += 8) m = max(m, __float_as_uint(__ldg(s + t * p.groups)) & 0x7fffffffu);
-        }
-    }
-    top[y][x] = m;
-    __syncthreads();
-    if (y == 0 && col < cols) {
-#pragma unroll
-        for (int k = 1; k < 8; ++k) m = max(m, top[k][x]);
-        tp.ranges[static_cast<long long>(blockIdx.y) * (p.C + p.groups) + (is_dz ? 0 : p.C) + col] = m;
-    }
-}
 
 __device__ __forceinline__ void tmem_alloc(uint32_t* where, uint32_t cols) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(where)), "r"(cols) : "memory");
@@ -129,56 +84,45 @@ __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence
 __device__ __forceinline__ void mma_commit(uint64_t* bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
-__device__ __forceinline__ void mma_int8(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
         : "memory");
 }
-__device__ __forceinline__ void tmem_load8(uint32_t addr, int (&r)[8]) {
+__device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8]) {
+    uint32_t r[8];
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(addr)
                  : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
-// Four bytes global -> shared, zeros where !real, and the arrival on `bar` of this thread when its copies so far have landed.
-__device__ __forceinline__ void async_copy4(float* dst, const float* src, bool real) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(real ? 4 : 0) : "memory");
-}
-__device__ __forceinline__ void async_copy_arrive(uint64_t* bar) {
-    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// Shared-memory operands.  A: rows of K are 128 contiguous bytes (the M index), 16-byte pieces exchanged within blocks of eight
-// rows as the 128-byte swizzle does, 1024 bytes from one block of eight to the next.  B: K-major without swizzle, eight rows of 16 bytes
-// are 128 contiguous bytes; `k_stride` bytes to the next 16 values of K, 128 bytes to the next eight rows.
-__device__ __forceinline__ uint64_t desc_a(uint32_t addr) {
-    return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(1024 >> 4) << 16 | uint64_t(1024 >> 4) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
-}
-__device__ __forceinline__ uint64_t desc_b(uint32_t addr, uint32_t k_stride) {
+// Shared-memory operand, K-major without swizzle: 8 rows x 16 bytes (8 values of K) are 128 contiguous bytes; `k_stride` bytes to
+// the next 8 values of K, 128 bytes to the next 8 rows.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t k_stride) {
     return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(k_stride >> 4) << 16 | uint64_t(128 >> 4) << 32 | uint64_t(1) << 46;
 }
 
-// Four integers to their four signed bytes: word d of `out` holds byte d of all four.
-__device__ __forceinline__ void bytes_of_four(const int (&v)[4], uint32_t (&out)[4]) {
-    uint32_t x[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (static_cast<uint32_t>(v[i]) + 0x80808080u) ^ 0x80808080u;      // digits in [-128, 127]
-    const uint32_t lo01 = __byte_perm(x[0], x[1], 0x5140), hi01 = __byte_perm(x[0], x[1], 0x7362);
-    const uint32_t lo23 = __byte_perm(x[2], x[3], 0x5140), hi23 = __byte_perm(x[2], x[3], 0x7362);
-    out[0] = __byte_perm(lo01, lo23, 0x5410);
-    out[1] = __byte_perm(lo01, lo23, 0x7632);
-    out[2] = __byte_perm(hi01, hi23, 0x5410);
-    out[3] = __byte_perm(hi01, hi23, 0x7632);
+// Two int8 (byte `i` of two words) to two bfloat16: the low seven bits under the exponent of 128 give 128 + (q & 127); a q >= 0
+// then has 128 too much, a negative one 256.  Exact.
+template <int I>
+__device__ __forceinline__ uint32_t int8_pair_to_bf16(uint32_t w0, uint32_t w1) {
+    const uint32_t p = __byte_perm(w0, w1, I | (4 + I) << 8);      // bytes 0 and 2; the others are masked off
+    const uint32_t m = (p & 0x007f007fu) | 0x43004300u, b = (p & 0x00800080u) | 0x43004300u;
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(m), "r"(b));
+    return r;
 }
-
-// Exponent k of the factor 2^k from the largest |dz| and |s| (bits); kNotFinite where a product of the two need not be finite.
-constexpr int kNotFinite = 1 << 20;
-__device__ __forceinline__ int factor_exponent(unsigned int dz, unsigned int s) {
-    const int e = static_cast<int>(dz >> 23) + static_cast<int>(s >> 23) - 254;                       // product < 2^(e + 2)
-    if (dz >= 0x7f800000u || s >= 0x7f800000u || e > 125) return kNotFinite;
-    return min(28 - e, 126);
+// The upper halves of (x0, x1) as packed bfloat16, and what is left of the two.  Cut off, not rounded: three times eight bits hold the 24
+// of an fp32 number exactly, and the largest numbers do not become infinite.
+__device__ __forceinline__ uint32_t split_term(float& x0, float& x1) {
+    const uint32_t a = __float_as_uint(x0), b = __float_as_uint(x1);
+    x0 -= __uint_as_float(a & 0xffff0000u);
+    x1 -= __uint_as_float(b & 0xffff0000u);
+    return __byte_perm(a, b, 0x7632);
 }
 
 template <class E, bool TMA>
@@ -186,249 +130,280 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024 - (smem_u32(smem_raw) & 1023)) & 1023);
     const CkptGradParams& p = tp.g;
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem);              // [slots_a] q and the scales of a stage have landed
-    uint64_t* done = full + kTcMaxSlots;                             // [slots_a] the products of the stage are complete
-    uint64_t* ready = done + kTcMaxSlots;                            // [slots_b] both operands are in place
-    uint64_t* last = ready + kTcMaxSlots;                            // [2 groups] all products are complete
-    uint32_t* tmem_at = reinterpret_cast<uint32_t*>(last + 2);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem);              // [kTcRing] raw q and the scales of a stage have landed
+    uint64_t* empty = full + kTcRing;                                // [kTcRing] the eight warps of the stage have read them
+    uint64_t* ready = empty + kTcRing;                               // [kTcBuffers] an operand buffer is written
+    uint64_t* done = ready + kTcBuffers;                             // [kTcBuffers] the products that read it are complete
+    uint64_t* flushed = done + kTcBuffers;                           // the accumulators have been read out
+    uint32_t* tmem_at = reinterpret_cast<uint32_t*>(flushed + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_at + 1);
-    int* exponent = reinterpret_cast<int*>(smem + 512);              // [2 groups][kTcMaxClasses]
-    float* scales = reinterpret_cast<float*>(smem + 1024);           // [slots_a][2 groups][kTcRows]
-    const int cp = tp.cp, ncols = 4 * cp;
-    const int tile_b = ncols * kTcRows;                              // bytes per group and slot
-    const int slots_a = tp.slots_a, slots_b = tp.slots_b;
-    // sets of converting warps; at most one per slot of B, so that none is more than a turn of a ring ahead of another
-    const int set_warps = cp / 16, sets = min(kTcWarps / set_warps, slots_b);
-    unsigned char* opa = smem + kTcHeader;                           // [slots_a][2 groups]
-    unsigned char* opb = opa + slots_a * 2 * kTcTileA;               // [slots_b][2 groups]
+    volatile int* issued_at = abort_flag + 1;
+    const int cp = tp.cp, ncols = 3 * cp;
+    const int op_b = 3 * cp * kTcRows * 2;                           // bytes per group and buffer
+    float* scales = reinterpret_cast<float*>(smem + 1024);           // [kTcRing][2 groups][kTcRows]
+    unsigned char* ring = smem + kTcHeader;
+    unsigned char* opa = ring + (TMA ? kTcRing * 2 * kTcRaw : 0);    // [kTcBuffers][2 groups]
+    unsigned char* opb = opa + kTcBuffers * 2 * kTcOperandA;         // [kTcBuffers][2 groups]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g0 = blockIdx.x * 2, groups = min(2, p.groups - g0);
     const int c0 = blockIdx.z * cp, classes = min(cp, p.C - c0);
     const long long lo = blockIdx.y * p.rows, hi = min(p.T, lo + p.rows);
     const int stages = static_cast<int>((hi - lo + kTcRows - 1) / kTcRows);
 
-    grid_dependency_release();                                       // k_ckpt8_join may be launched; it waits for this kernel's end
     if (tid == 0) {
-        for (int i = 0; i < slots_a; ++i) {
-            mbar_init(full + i, 32 + (TMA ? 1 : 0));                 // the lanes that copy scales, and the copy of q
-            mbar_init(done + i, groups);
+        for (int i = 0; i < kTcRing; ++i) {
+            mbar_init(full + i, TMA ? 2 : 1);
+            mbar_init(empty + i, kTcWarps / 2);
         }
-        for (int i = 0; i < slots_b; ++i) mbar_init(ready + i, set_warps);
+        for (int i = 0; i < kTcBuffers; ++i) {
+            mbar_init(ready + i, kTcWarps / 2);
+            mbar_init(done + i, 1);
+        }
+        mbar_init(flushed, kTcWarps);
         *abort_flag = 0;
-        for (int i = 0; i < 2; ++i) mbar_init(last + i, 1);
+        *issued_at = 0;
         fence_mbar_init();
     }
     if (warp == 0) tmem_alloc(tmem_at, 512);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
+    grid_dependency_release();                                       // k_ckpt8_join may be launched; it waits for this kernel's end
     const uint32_t tmem = *tmem_at;
     bool ok = true;
+    float acc[kTcMaxClasses / 2];                                    // sums of this thread's column, (warp >> 2) & 1 its group
+#pragma unroll
+    for (int i = 0; i < kTcMaxClasses / 2; ++i) acc[i] = 0.0f;
     float zsum = 0.0f;
-
-    if (warp > kTcWarps) {
-        const int gi = warp - kTcWarps - 1;
-        if (lane == 0 && gi < groups) {
-            // D int32, A and B int8, A with M contiguous
-            const uint32_t idesc = (2u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (uint32_t(ncols / 8) << 17) | (uint32_t(kCkptGroup / 16) << 24);
-            const uint64_t a0 = desc_a(smem_u32(opa + gi * kTcTileA)), b0 = desc_b(smem_u32(opb + gi * tile_b), ncols * 16);
-            const uint32_t d = tmem + gi * ncols, step_b = 2 * tile_b >> 4;         // (descriptors count in 16 bytes)
-            uint64_t a = a0, b = b0;
-            int slot = 0, slot_b = 0, parity = 0;
-#pragma unroll 1
-            for (int stage = 0; stage < stages; ++stage) {
-                if (!mbar_wait_bounded(ready + slot_b, parity, abort_flag)) { ok = false; break; }
-                tmem_fence_after();
-                mma_int8(d, a, b, idesc, stage > 0);
-                mma_commit(done + slot);
-                a += 2 * kTcTileA >> 4;
-                b += step_b;
-                if (++slot == slots_a) { slot = 0; a = a0; }
-                if (++slot_b == slots_b) { slot_b = 0; b = b0; parity ^= 1; }
-            }
-            mma_commit(last + gi);                                   // all products of this thread, also after giving up
-            if (!mbar_wait_drain(last + gi, 0)) ok = false;
-        }
-    } else if (warp == kTcWarps) {
-        const uint64_t policy = l2_policy_evict_first();
-        // lane: one row of a stage, both groups' scales (rows past the end: zeros)
-        long long t = lo + lane;
-        const float* sp = p.s + min(t, hi - 1) * p.groups + g0;
-        int stage = 0, slot = 0, turn = 0;
-        for (; stage < stages; ++stage) {
-            if (turn > 0) {
-                ok = __all_sync(0xffffffffu, mbar_wait_bounded(done + slot, (turn - 1) & 1, abort_flag));
-                if (!ok) break;
-            }
-            if (TMA && lane == 0) {
-                mbar_arrive_expect_tx(full + slot, uint32_t(groups * kTcTileA));
-                for (int gi = 0; gi < groups; ++gi)
-                    bulk_tensor_2d_g2s(opa + (slot * 2 + gi) * kTcTileA, &map, (g0 + gi) * kCkptGroup, int(lo) + stage * kTcRows, full + slot, policy);
-            }
-            float* dst = scales + slot * 2 * kTcRows + lane;
-            const bool in = t < hi;
-            async_copy4(dst, in ? sp : p.s, in);
-            if (groups > 1) async_copy4(dst + kTcRows, in ? sp + 1 : p.s, in);
-            async_copy_arrive(full + slot);
-            t += kTcRows;
-            sp += static_cast<long long>(kTcRows) * p.groups;
-            if (++slot == slots_a) { slot = 0; ++turn; }
-        }
-        // every copy lands before the CTA ends, also after giving up
-        for (int i = max(0, stage - slots_a); i < stage; ++i) mbar_wait_drain(full + i % slots_a, (i / slots_a) & 1);
-    } else {
-        const int set = warp / set_warps, stid = tid - set * set_warps * 32;
-        const int zk = stid / cp, zc = stid - zk * cp;               // this thread's part of dz: class c0 + zc, rows 16 * zk .. + 15
-        const bool z_on = zk < kTcRows / 16, z_real = z_on && zc < classes;
-        long long zt = lo + set * kTcRows + zk * 16;
-        const E* zp = static_cast<const E*>(p.dz) + c0 + zc + zt * p.ld_dz;
-        const uint32_t row_bytes = static_cast<uint32_t>(p.ld_dz) * sizeof(E);
-        float z[16];
-        auto load_dz = [&] {                                         // and on to this set's next stage
-            // (a 32-bit factor: one multiply-add per address; ld_dz is at most 2^28)
-            const char* q = reinterpret_cast<const char*>(zp);
-            if (z_real && zt + 16 <= hi) {
+    const int fg = (warp >> 2) & 1, fhalf = warp >> 3;
+    auto flush = [&] {                                               // accumulators -> acc: class 16 * i + 8 * fhalf + k in acc[8 * i + k]
+        tmem_fence_after();
+        if (fg < groups) {
 #pragma unroll
-                for (unsigned int r = 0; r < 16; ++r) z[r] = load_as_float(reinterpret_cast<const E*>(q + static_cast<uint64_t>(row_bytes) * r));
-            } else {
+            for (int i = 0; i < kTcMaxClasses / 16; ++i)
+                if (16 * i < cp) {
+                    float a[8], b[8], d[8];
+                    const uint32_t at = tmem + (uint32_t((warp & 3) * 32) << 16) + fg * ncols + 16 * i + 8 * fhalf;
+                    tmem_load8(at, a);
+                    tmem_load8(at + cp, b);
+                    tmem_load8(at + 2 * cp, d);
 #pragma unroll
-                for (unsigned int r = 0; r < 16; ++r)
-                    z[r] = z_real && zt + r < hi ? load_as_float(reinterpret_cast<const E*>(q + static_cast<uint64_t>(row_bytes) * r)) : 0.0f;
-            }
-            zp += sets * kTcRows * p.ld_dz;
-            zt += sets * kTcRows;
-        };
-        load_dz();
-        // exponents of the classes and groups of this CTA's rows
-        grid_dependency_wait();                                      // k_ckpt8_ranges
-        if (tid < 2 * kTcMaxClasses) {
-            const int c = tid & (kTcMaxClasses - 1), gi = tid / kTcMaxClasses;
-            int e = 0;
-            if (c < classes && gi < groups) {
-                const unsigned int* r = tp.ranges + static_cast<long long>(blockIdx.y) * tp.sub * (p.C + p.groups);
-                unsigned int dz_top = 0, s_top = 0;
-#pragma unroll 8
-                for (int k = 0; k < tp.sub; ++k, r += p.C + p.groups) {
-                    dz_top = max(dz_top, r[c0 + c]);
-                    s_top = max(s_top, r[p.C + g0 + gi]);
-                }
-                e = factor_exponent(dz_top, s_top);
-            }
-            exponent[gi * kTcMaxClasses + c] = e;
-        }
-        asm volatile("bar.sync 1, %0;" ::"n"(kTcWarps * 32) : "memory");               // the converting warps
-        float factor[2];
-#pragma unroll
-        for (int gi = 0; gi < 2; ++gi) {
-            const int e = exponent[gi * kTcMaxClasses + (z_on ? zc : 0)];
-            factor[gi] = e == kNotFinite ? 0.0f : __uint_as_float(static_cast<uint32_t>(e + 127) << 23);
-        }
-        // the stage's slot of q, and that of the stage which had its slot of B before
-        int slot = set, turn = 0, slot_b = set;
-        int before = set - slots_b, before_turn = 0;
-        for (int stage = set < sets ? set : stages; stage < stages; stage += sets) {
-            const bool in_time = before < 0 || mbar_wait_bounded(done + before, before_turn & 1, abort_flag);
-            ok = __all_sync(0xffffffffu, in_time && mbar_wait_bounded(full + slot, turn & 1, abort_flag));
-            if (!ok) break;
-            if (z_on) {
-                zsum += (((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]))) + (((z[8] + z[9]) + (z[10] + z[11])) + ((z[12] + z[13]) + (z[14] + z[15])));
-#pragma unroll
-                for (int gi = 0; gi < 2; ++gi) {
-                    if (gi < groups) {
-                        const float4* sp = reinterpret_cast<const float4*>(scales + (slot * 2 + gi) * kTcRows + zk * 16);
-                        uint32_t word[4][4];                         // [four rows][byte]
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            const float4 s = sp[r];
-                            const int v[4] = {__float2int_rn(z[4 * r] * s.x * factor[gi]), __float2int_rn(z[4 * r + 1] * s.y * factor[gi]),
-                                              __float2int_rn(z[4 * r + 2] * s.z * factor[gi]), __float2int_rn(z[4 * r + 3] * s.w * factor[gi])};
-                            bytes_of_four(v, word[r]);
-                        }
-                        uint4* dst = reinterpret_cast<uint4*>(opb + (slot_b * 2 + gi) * tile_b + zk * (ncols * 16)) + zc;
-#pragma unroll
-                        for (int d = 0; d < 4; ++d) dst[d * cp] = make_uint4(word[0][d], word[1][d], word[2][d], word[3][d]);
-                    }
-                }
-            }
-            if (!TMA) {
-                // sixteen bytes at a time from the words that hold them, to where the copy would have put them
-#pragma unroll 1
-                for (int u = stid; u < kTcRows * 2 * 8; u += set_warps * 32) {
-                    const int row = u >> 4, gi = (u >> 3) & 1, piece = u & 7;
-                    const long long t = lo + static_cast<long long>(stage) * kTcRows + row;
-                    const int col = (g0 + gi) * kCkptGroup + piece * 16, left = min(16, p.n - col);
-                    uint32_t w[5] = {0u, 0u, 0u, 0u, 0u};
-                    int off = 0;
-                    if (gi < groups && t < hi && left > 0) {
-                        const uintptr_t a = reinterpret_cast<uintptr_t>(p.q) + t * p.ld_q + col;
-                        off = static_cast<int>(a & 3);
-                        const uint32_t* base = reinterpret_cast<const uint32_t*>(a & ~uintptr_t(3));
-#pragma unroll
-                        for (int k = 0; k < 5; ++k)
-                            if (4 * k < off + left) w[k] = __ldg(base + k);
-                    }
-                    uint32_t b[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int real = left - 4 * k;               // bytes of this word that belong to the row
-                        b[k] = real <= 0 ? 0u : __funnelshift_r(w[k], w[k + 1], 8 * off) & (real >= 4 ? 0xffffffffu : (1u << (8 * real)) - 1u);
-                    }
-                    if (gi < groups)
-                        *reinterpret_cast<uint4*>(opa + (slot * 2 + gi) * kTcTileA + row * 128 + ((piece ^ (row & 7)) << 4)) = make_uint4(b[0], b[1], b[2], b[3]);
-                }
-            }
-            fence_proxy_async_smem();                                // what was just stored is read by the tensor cores
-            __syncwarp();
-            if (lane == 0) mbar_arrive(ready + slot_b);
-            if (stage + sets < stages) load_dz();
-            // (sets <= slots_b < slots_a)
-            slot += sets;
-            if (slot >= slots_a) { slot -= slots_a; ++turn; }
-            before += sets;
-            if (before >= slots_a) { before -= slots_a; ++before_turn; }
-            slot_b += sets;
-            if (slot_b >= slots_b) slot_b -= slots_b;
-        }
-    }
-    // all warps get here: every wait above is bounded, and the products are complete
-    ok = __syncthreads_and(ok);
-    tmem_fence_after();
-    if (ok) {
-        const bool direct = p.chunks == 1;
-        float* bsum = reinterpret_cast<float*>(opb);                 // [kTcWarps][32]
-        if (warp < kTcWarps) {
-            bsum[tid] = zsum;
-            // this warp: 32 columns of one group, classes 16 * i + 8 * half ..
-            const int gi = (warp >> 2) & 1, half = warp >> 3, col = (g0 + gi) * kCkptGroup + (warp & 3) * 32 + lane;
-            float* out = (direct ? p.grad_w : p.part_w + static_cast<long long>(blockIdx.y) * p.C * p.n) + static_cast<long long>(c0) * p.n + col;
-            if (gi < groups)
-                for (int i = 0; 16 * i < cp; ++i) {
-                    int d[4][8];
-                    const uint32_t at = tmem + (uint32_t((warp & 3) * 32) << 16) + gi * ncols + 16 * i + 8 * half;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) tmem_load8(at + k * cp, d[k]);
-                    tmem_load_wait();
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        const int c = 16 * i + 8 * half + k;
-                        if (c < classes && col < p.n) {
-                            const long long top = static_cast<long long>(d[3][k]) * 256 + d[2][k], low = static_cast<long long>(d[1][k]) * 256 + d[0][k];
-                            const int e = exponent[gi * kTcMaxClasses + c];
-                            // (top * 2^16 + low) / 2^e, rounded once to fp32
-                            const double v = (static_cast<double>(top) * 65536.0 + static_cast<double>(low)) * __hiloint2double((1023 - e) << 20, 0);
-                            float sum = e == kNotFinite ? __int_as_float(0x7fc00000) : static_cast<float>(v);
-                            float* o = out + static_cast<long long>(c) * p.n;
-                            *o = direct && p.accumulate ? *o + sum : sum;
-                        }
-                    }
+                    for (int k = 0; k < 8; ++k) acc[8 * i + k] += a[k] + (b[k] + d[k]);
                 }
         }
         tmem_fence_before();
+    };
+    const int set = warp >> 3, sw = warp & 7, stid = tid & 255;      // set of eight warps, place in it
+    const int zk = stid / cp, zc = stid - zk * cp;                   // this thread's part of dz: class c0 + zc, rows 8 * zk .. + 7
+    const bool z_on = zk < kTcBlocks;
+
+    if (warp == kTcWarps) {
+        if (lane == 0) {
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (uint32_t(ncols / 8) << 17) | (uint32_t(kCkptGroup / 16) << 24);
+            const uint64_t a0 = operand_desc(smem_u32(opa), kCkptGroup * 16), b0 = operand_desc(smem_u32(opb), ncols * 16);
+            int stage = 0, buf = 0, parity = 0, sums = 0;
+            for (; stage < stages; ++stage) {
+                if (!mbar_wait_bounded(ready + buf, parity, abort_flag)) { ok = false; break; }
+                const bool fresh = stage % kTcFlush == 0;            // the sums so far are taken out first
+                if (fresh && stage > 0 && !mbar_wait_bounded(flushed, sums++ & 1, abort_flag)) { ok = false; break; }
+                tmem_fence_after();
+                for (int gi = 0; gi < groups; ++gi) {
+                    // descriptors count in 16 bytes; 16 rows of the sum are two blocks of K
+                    const uint64_t a = a0 + ((buf * 2 + gi) * kTcOperandA >> 4), b = b0 + ((buf * 2 + gi) * op_b >> 4);
+#pragma unroll
+                    for (int k = 0; k < kTcRows / 16; ++k)
+                        mma_bf16(tmem + gi * ncols, a + k * 2 * kCkptGroup, b + k * 2 * ncols, idesc, !fresh || k > 0);
+                }
+                mma_commit(done + buf);
+                if (++buf == kTcBuffers) { buf = 0; parity ^= 1; }
+            }
+            *issued_at = stage;
+        }
+    } else if (warp == kTcWarps + 1) {
+        const uint64_t policy = l2_policy_evict_first();
+        // lane: one row of the stage, both groups' scales
+        float s0 = 0.0f, s1 = 0.0f;
+        auto load_scales = [&](int stage) {
+            const long long t = lo + static_cast<long long>(stage) * kTcRows + lane;
+            const float* sp = p.s + t * p.groups + g0;
+            s0 = stage < stages && t < hi ? __ldg(sp) : 0.0f;
+            s1 = stage < stages && t < hi && groups > 1 ? __ldg(sp + 1) : 0.0f;
+        };
+        auto fetch = [&](int stage, int slot) {
+            if (TMA && lane == 0) {
+                mbar_arrive_expect_tx(full + slot, uint32_t(groups * kTcRaw));
+                for (int gi = 0; gi < groups; ++gi)
+                    bulk_tensor_2d_g2s(ring + (slot * 2 + gi) * kTcRaw, &map, (g0 + gi) * kCkptGroup, int(lo) + stage * kTcRows, full + slot, policy);
+            }
+            scales[slot * 2 * kTcRows + lane] = s0;
+            scales[slot * 2 * kTcRows + kTcRows + lane] = s1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + slot);
+            load_scales(stage + 1);
+        };
+        load_scales(0);
+        const int ahead = min(kTcRing, stages);
+        for (int i = 0; i < ahead; ++i) fetch(i, i);
+        int slot = 0, parity = 0, stage = 0;
+        for (; stage + kTcRing < stages; ++stage) {
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(empty + slot, parity, abort_flag));
+            if (!ok) break;
+            fetch(stage + kTcRing, slot);
+            if (++slot == kTcRing) { slot = 0; parity ^= 1; }
+        }
+        if (TMA)                                                     // every copy lands before the CTA ends, also after giving up
+            for (int i = stage; i < min(stages, stage + kTcRing); ++i) mbar_wait_drain(full + i % kTcRing, (i / kTcRing) & 1);
+    } else {
+        const bool z_real = z_on && zc < classes;
+        long long zt = lo + set * kTcRows + zk * 8;
+        const E* zp = static_cast<const E*>(p.dz) + c0 + zc + zt * p.ld_dz;
+        float z[8];
+        auto load_dz = [&] {                                         // and on to this set's next stage
+#pragma unroll
+            for (int r = 0; r < 8; ++r) z[r] = 0.0f;
+            if (z_real) {
+                const E* q = zp;
+                if (zt + 8 <= hi) {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r, q += p.ld_dz) z[r] = load_as_float(q);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < 8; ++r, q += p.ld_dz)
+                        if (zt + r < hi) z[r] = load_as_float(q);
+                }
+            }
+            zp += 2 * kTcRows * p.ld_dz;
+            zt += 2 * kTcRows;
+        };
+        // this warp's part of q: group qg, rows 8 * qk .. 8 * qk + 7, four columns per lane
+        const int qg = sw & 1, qk = sw >> 1;
+        uint32_t w[8];
+        auto load_words = [&](int stage) {                           // q without alignment: the words that hold the four bytes
+            const int col = (g0 + qg) * kCkptGroup + 4 * lane;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const long long t = lo + stage * kTcRows + qk * 8 + r;
+                w[r] = 0;
+                if (qg < groups && t < hi && col < p.n) {
+                    const uintptr_t a = reinterpret_cast<uintptr_t>(p.q) + t * p.ld_q + col;
+                    const int left = min(4, p.n - col), off = int(a & 3);
+                    const uint32_t* base = reinterpret_cast<const uint32_t*>(a & ~uintptr_t(3));
+                    const uint32_t w0 = __ldg(base), w1 = off + left > 4 ? __ldg(base + 1) : 0u;
+                    w[r] = __funnelshift_r(w0, w1, 8 * off) & (0xffffffffu >> (32 - 8 * left));
+                }
+            }
+        };
+        load_dz();
+        if (!TMA) load_words(set);
+        auto wait = [&](uint64_t* bar, uint32_t parity) {            // one verdict for the warp
+            ok = __all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag));
+            return ok;
+        };
+        // both sets take the sums out before the (even) stage `next` starts them afresh
+        auto take_out = [&](int next) {
+            if (next == 0 || next % kTcFlush != 0) return true;
+            if (!wait(done + (next - 1) % kTcBuffers, ((next - 1) / kTcBuffers) & 1)) return false;
+            flush();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(flushed);
+            return true;
+        };
+        int slot = set, slot_phase = 0, buf = set, use = 0;          // use: how often this buffer was filled before
+        for (int stage = set; stage < stages; stage += 2) {
+            if (use > 0 && !wait(done + buf, (use - 1) & 1)) break;  // the products of three stages ago have read this buffer
+            if (!wait(full + slot, slot_phase)) break;
+            if (TMA && qg < groups) {
+                const uint32_t* raw = reinterpret_cast<const uint32_t*>(ring + (slot * 2 + qg) * kTcRaw) + qk * 8 * 32 + lane;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) w[r] = raw[r * 32];
+            }
+            if (z_on) {
+                const float4* rows = reinterpret_cast<const float4*>(scales + slot * 2 * kTcRows) + 2 * zk;
+                zsum += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
+#pragma unroll
+                for (int gi = 0; gi < 2; ++gi) {
+                    if (gi < groups) {
+                        const float4 sa = rows[gi * (kTcRows / 4)], sb = rows[gi * (kTcRows / 4) + 1];
+                        float x[8] = {z[0] * sa.x, z[1] * sa.y, z[2] * sa.z, z[3] * sa.w, z[4] * sb.x, z[5] * sb.y, z[6] * sb.z, z[7] * sb.w};
+                        uint4* dst = reinterpret_cast<uint4*>(opb + (buf * 2 + gi) * op_b + zk * (ncols * 16)) + zc;
+#pragma unroll
+                        for (int term = 0; term < 3; ++term) {
+                            uint4 o;
+                            o.x = split_term(x[0], x[1]);
+                            o.y = split_term(x[2], x[3]);
+                            o.z = split_term(x[4], x[5]);
+                            o.w = split_term(x[6], x[7]);
+                            dst[term * cp] = o;
+                        }
+                    }
+                }
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(empty + slot);                // raw rows and scales are in registers or used
+            if (stage + 2 < stages) load_dz();
+            slot += 2;
+            if (slot >= kTcRing) { slot -= kTcRing; slot_phase ^= 1; }
+            if (qg < groups) {
+                // column 4 * lane + i becomes row i * 32 + lane of the operand, so that neighbouring lanes store neighbouring 16 bytes
+                uint4* dst = reinterpret_cast<uint4*>(opa + (buf * 2 + qg) * kTcOperandA + qk * (kCkptGroup * 16)) + lane;
+#define LRGD_COLUMN(I) \
+    dst[I * 32] = make_uint4(int8_pair_to_bf16<I>(w[0], w[1]), int8_pair_to_bf16<I>(w[2], w[3]), int8_pair_to_bf16<I>(w[4], w[5]), int8_pair_to_bf16<I>(w[6], w[7]))
+                LRGD_COLUMN(0);
+                LRGD_COLUMN(1);
+                LRGD_COLUMN(2);
+                LRGD_COLUMN(3);
+#undef LRGD_COLUMN
+            }
+            if (!TMA && stage + 2 < stages) load_words(stage + 2);
+            if (!take_out(stage - set)) break;
+            fence_proxy_async_smem();                                // what was just stored is read by the tensor cores
+            __syncwarp();
+            if (lane == 0) mbar_arrive(ready + buf);
+            buf += 2;
+            if (buf >= kTcBuffers) { buf -= kTcBuffers; ++use; }
+        }
+        if (ok && set == 1 && (stages & 1)) take_out(stages - 1);    // the last stage is the other set's
+    }
+    // all warps get here: every wait above is bounded.  Then the products still in flight, before their memory is used again.
+    ok = __syncthreads_and(ok);
+    const int issued = *issued_at;
+    for (int b = 0; b < kTcBuffers; ++b) {
+        const int uses = (issued + kTcBuffers - 1 - b) / kTcBuffers; // stages that committed to this barrier
+        if (uses > 0 && !mbar_wait_drain(done + b, (uses - 1) & 1)) ok = false;
+    }
+    ok = __syncthreads_and(ok);
+    if (ok) {
+        // sums -> shared memory [class][256] -> rows of the part
+        float* tile = reinterpret_cast<float*>(opa);
+        float* bsum = tile + kTcMaxClasses * 256;                    // [2 sets][kTcBlocks][cp], each set 256 long
+        if (warp < kTcWarps) {
+            flush();
+            if (fg < groups)
+#pragma unroll
+                for (int i = 0; i < kTcMaxClasses / 16; ++i)
+                    if (16 * i < cp)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) tile[(16 * i + 8 * fhalf + k) * 256 + fg * 128 + 4 * lane + (warp & 3)] = acc[8 * i + k];
+            bsum[tid] = z_on ? zsum : 0.0f;
+        }
         __syncthreads();
+        const bool direct = p.chunks == 1;
+        const int width = min(256, p.n - g0 * kCkptGroup);
+        float* out = direct ? p.grad_w : p.part_w + static_cast<long long>(blockIdx.y) * p.C * p.n;
+        out += static_cast<long long>(c0) * p.n + g0 * kCkptGroup;
+        if (!direct && p.n % 4 == 0) {                               // rows of the scratch start on 16 bytes
+            for (int i = tid; i < classes * 64; i += kTcThreads)
+                if ((i & 63) * 4 < width)
+                    *reinterpret_cast<float4*>(out + static_cast<long long>(i >> 6) * p.n + (i & 63) * 4) = reinterpret_cast<const float4*>(tile)[i];
+        } else {
+            for (int i = tid; i < classes * 256; i += kTcThreads) {
+                float* o = out + static_cast<long long>(i >> 8) * p.n + (i & 255);
+                if ((i & 255) < width) *o = direct && p.accumulate ? *o + tile[i] : tile[i];
+            }
+        }
         if (blockIdx.x == 0 && tid < classes) {
             float sum = 0.0f;
-            for (int k = 0; k < sets; ++k)
-                for (int b = 0; b < kTcRows / 16; ++b) sum += bsum[k * set_warps * 32 + b * cp + tid];
+            for (int k = 0; k < kTcBlocks; ++k) sum += bsum[k * cp + tid] + bsum[256 + k * cp + tid];
             if (!direct) p.part_b[static_cast<long long>(blockIdx.y) * p.C + c0 + tid] = sum;
             else if (p.grad_b) p.grad_b[c0 + tid] = p.accumulate ? p.grad_b[c0 + tid] + sum : sum;
         }

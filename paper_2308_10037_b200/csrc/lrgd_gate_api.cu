@@ -342,28 +342,20 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     const bool one = C == 1;
     const int cblocks = (C + kTcMaxClasses - 1) / kTcMaxClasses, cp = ((C + cblocks - 1) / cblocks + 15) / 16 * 16;
     const int64_t unit = one ? kUnitRows : kTcRows, units = (T + unit - 1) / unit;
-    const int64_t fill = std::max<int64_t>(1, plan_sms(ctx) * (one ? kUnitCtas : 1) / (int64_t(pairs) * cblocks));
-    const int64_t want = std::min<int64_t>(units, std::max<int64_t>(fill, (T + kTcMaxRows - 1) / kTcMaxRows));
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>(units, plan_sms(ctx) * (one ? kUnitCtas : 1) / (int64_t(pairs) * cblocks)));
     const int64_t rows = (units + want - 1) / want * unit, chunks = (T + rows - 1) / rows;
-    if (chunks > 65535 || cblocks > 65535) return LR_ERR_SHAPE;
-    // each chunk is looked at in so many parts for its largest values that this, too, fills the SMs
-    const int range_blocks = (C + 31) / 32 + (groups + 31) / 32;
-    const int sub = one ? 0 : int(std::max<int64_t>(1, std::min<int64_t>({kTcMaxSub, rows / 8, int64_t(plan_sms(ctx)) * 4 / (chunks * range_blocks), 65535 / chunks})));
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
-    const size_t wb = chunks > 1 ? up(size_t(chunks) * C * n * 4) : 0, bb = chunks > 1 ? up(size_t(chunks) * C * 4) : 0;
-    const size_t rb = size_t(chunks) * sub * (size_t(C) + groups) * 4;
-    if (wb + bb + rb > 0) {
-        const int rs = gate_scratch(ctx, wb + bb + rb);
+    float *part_w = nullptr, *part_b = nullptr;
+    if (chunks > 1) {
+        const size_t wb = up(size_t(chunks) * C * n * 4);
+        const int rs = gate_scratch(ctx, wb + size_t(chunks) * C * 4);
         if (rs != LR_OK) return rs;
+        part_w = reinterpret_cast<float*>(ctx->d_scratch);
+        part_b = reinterpret_cast<float*>(ctx->d_scratch + wb);
     }
     TcGradParams p{};
-    p.g = CkptGradParams{d_q, ld_q, d_s, T, n, groups, d_dz, ld_dz, C, int(chunks), rows, accumulate != 0,
-                         reinterpret_cast<float*>(ctx->d_scratch), reinterpret_cast<float*>(ctx->d_scratch + wb), d_grad_w, d_grad_b};
+    p.g = CkptGradParams{d_q, ld_q, d_s, T, n, groups, d_dz, ld_dz, C, int(chunks), rows, accumulate != 0, part_w, part_b, d_grad_w, d_grad_b};
     p.cp = cp;
-    p.slots_a = tc_slots_a(cp);
-    p.slots_b = tc_slots_b(cp);
-    p.sub = sub;
-    p.ranges = reinterpret_cast<unsigned int*>(ctx->d_scratch + wb + bb);
     p.status = ctx->d_status;
     const dim3 grid{unsigned(pairs), unsigned(chunks), unsigned(cblocks)};
     int r = LR_OK;
@@ -381,19 +373,15 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
             const cuuint64_t dims[2] = {cuuint64_t(n), cuuint64_t(T)}, strides[1] = {cuuint64_t(ld_q)};
             const cuuint32_t box[2] = {kCkptGroup, kTcRows}, step[2] = {1, 1};
             if (encode(&map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<int8_t*>(d_q), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                       CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
+                       CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS) {
                 ctx->last_cuda = int(cudaErrorInvalidValue);
                 return LR_ERR_CUDA;
             }
         }
-        r = launched(ctx, [&] { k_ckpt8_ranges<E><<<dim3(unsigned(range_blocks), unsigned(chunks * sub)), kRangeThreads, 0, st>>>(p); });
-        if (r != LR_OK) return r;
-        const int smem = tc_smem_bytes(cp);
+        const int smem = tc_smem_bytes(cp, tma);
         auto go = [&](auto kern, auto tag) -> int {
             LR_CK(ctx, ensure_dynamic_smem<decltype(tag)>(reinterpret_cast<const void*>(kern), smem));
-            LR_CK(ctx, launch_kernel(kern, grid, dim3(kTcThreads), size_t(smem), st, ctx->overlap, map, p));
-            ctx->launches += 1;
-            return LR_OK;
+            return launched(ctx, [&] { kern<<<grid, kTcThreads, smem, st>>>(map, p); });
         };
         r = tma ? go(k_ckpt8_grad_tc<E, true>, CkptGradTag<E, true>{}) : go(k_ckpt8_grad_tc<E, false>, CkptGradTag<E, false>{});
     }
