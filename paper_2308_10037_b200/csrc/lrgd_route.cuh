@@ -317,13 +317,14 @@ __global__ void __launch_bounds__(kRouteThreads) k_route_grad_chosen(const __gri
             const float w = w0 / fmaxf(group_sum(w0), 1.0f);     // the largest term is 1; no chosen expert at all: 0
             d = w * (g - group_sum(g * w));
         } else {
-            const float q = id >= 0 ? plain_sigmoid(x) : 0.0f;
+            // 1 - p is the sigmoid of -x: taken from a p that is rounded near 1 it would lose its bits (all of them from x = 17 on)
+            const float rest = plain_sigmoid(-x);
             if (p.renorm) {
                 const float r = relative_sigmoid(x, fminf(group_max(x), 0.0f)), S = group_sum(r);
                 const float w = S > 0.0f ? r / S : 0.0f;
-                d = (g - group_sum(g * w)) * w * (1.0f - q);
+                d = (g - group_sum(g * w)) * w * rest;
             } else {
-                d = g * q * (1.0f - q);
+                d = g * plain_sigmoid(x) * rest;
             }
         }
         __syncwarp();                               // the chosen ones replace the zeros

@@ -1,0 +1,33 @@
+"""Edges of the token-gate calls: saturated scores, tokens outside the table, refusals, status words, new contexts."""
+import pytest
+import torch
+
+from test_gpu_gate import DT, U, close, ctx, gen, rnd   # noqa: F401 (ctx is a fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("renorm", [False, True])
+def test_route_grad_of_saturated_sigmoids(ctx, dt, renorm):
+    # relative to the derivative itself, not to the largest one: both sigmoids take an exp (2 ulp) and a quotient, the weights a sum more
+    x = (torch.arange(-80, 81, device="cuda").float() / 2)[:, None] + torch.tensor([0.0, 0.25, -0.5], device="cuda")
+    x = torch.cat([x, 2 * x]).to(DT[dt])
+    T = x.shape[0]
+    ids = torch.tensor([[2, 0]], dtype=torch.int32, device="cuda").repeat(T, 1)
+    g = rnd(T, 2, seed=1)
+    z = x.double().gather(1, ids.long())
+    p, rest = torch.sigmoid(z), torch.sigmoid(-z)
+    lg = torch.nn.functional.logsigmoid(z)
+    w = torch.softmax(lg, 1)
+    G = g.double()
+    if renorm:
+        d = 2.5 * (G - (G * w).sum(1, keepdim=True)) * w * rest
+        bound = 160 * U * 2.5 * G.abs().sum(1, keepdim=True) * w * rest
+    else:
+        d = 2.5 * G * p * rest
+        bound = 40 * U * d.abs()
+    want = torch.zeros_like(x, dtype=torch.float64).scatter_(1, ids.long(), d)
+    room = torch.zeros_like(want).scatter_(1, ids.long(), bound)
+    got = ctx.route_grad(x, ids, g, score="sigmoid", renorm=renorm, factor=2.5)
+    close(got, want, room + (2.0 ** -8 * want.abs() if dt == "bf16" else 0.0) + 2.0 ** -126)
