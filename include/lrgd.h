@@ -466,7 +466,7 @@ int lr_embed_bf16(lr_ctx* ctx, const uint16_t* d_table, int64_t ld_table, const 
  * Gradient of the table: d_grad[v,:] = scale * sum over { t : id_t = v } of d_dout[t,:] (fp32 [V*n], rows packed).  With
  * accumulate == 0 all V rows are written (zeros where no token points), otherwise the sums are added to what d_grad holds
  * and rows of other tokens are not touched.  Positions whose token is padding_id carry no gradient (a negative padding_id:
- * none), nor do tokens outside [0, V), which set the status word as in lr_embed.
+ * none), nor do tokens outside [0, V), which set the status word as in lr_embed (whatever padding_id is).
  * The positions are sorted by token on the device (stable) and every row is summed in the order of its positions, long runs in
  * pieces that are joined in order: no atomics on data, the same bits for the same ids.
  */

@@ -164,7 +164,7 @@ __global__ void __cluster_dims__(kSortCtas, 1, 1) __launch_bounds__(kSortThreads
     };
     for (unsigned int i = lo + tid; i < hi; i += kSortThreads) {
         const long long id = load_id<Id>(p.ids, i);
-        if ((id < 0 || id >= p.V) && id != p.padding) atomicExch(p.status, -4);             // LR_ERR_VALUE
+        if (id < 0 || id >= p.V) atomicExch(p.status, -4);      // LR_ERR_VALUE, also where padding_id (then no row of the table) says the same
         const unsigned int k = token_key(i);
         if (p.present && k < p.V) atomicOr(p.present + (k >> 5), 1u << (k & 31));
     }

@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2308_10037_b200 import api
 from test_gpu_gate import DT, U, close, ctx, gen, rnd   # noqa: F401 (ctx is a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -31,3 +32,18 @@ def test_route_grad_of_saturated_sigmoids(ctx, dt, renorm):
     room = torch.zeros_like(want).scatter_(1, ids.long(), bound)
     got = ctx.route_grad(x, ids, g, score="sigmoid", renorm=renorm, factor=2.5)
     close(got, want, room + (2.0 ** -8 * want.abs() if dt == "bf16" else 0.0) + 2.0 ** -126)
+
+
+@pytest.mark.parametrize("T", [3, 3000])
+def test_tokens_outside_the_table_are_reported_whatever_the_padding(ctx, T):
+    V, n = 20, 12
+    dout = rnd(T, n)
+    assert ctx.device_status() == 0
+    for token, padding, status in ((-1, -1, api.LR_ERR_VALUE), (V + 5, V + 5, api.LR_ERR_VALUE), (-4, -1, api.LR_ERR_VALUE), (7, 7, 0)):
+        ids = torch.full((T,), 3, device="cuda")
+        ids[T // 2] = token
+        got = ctx.embed_grad(ids, dout, V, padding_id=padding)
+        assert ctx.device_status() == status, token
+        want = dout.double().sum(0) - dout[T // 2].double()
+        close(got[3], want, (T + 3) * U * dout.double().abs().sum(0))
+        assert int((got != 0).any(dim=1).sum()) == 1
