@@ -446,7 +446,9 @@ const char* lr_status_string(int code);
  * bfloat16 (the *_bf16 calls; uint16 patterns, rounded to nearest even where written).  A matrix is row-major with a leading
  * dimension ("ld...", in elements, at least its row length), so a slice of columns can be passed as it is.  Any alignment to the
  * element size works; rows that start on 16 bytes and hold whole 16-byte groups are fastest.  Results are bit-reproducible.
- * T (rows, tokens) may be 0 and is at most 2^31 - 1.  The gradient calls of this section use a scratch owned by the context,
+ * T (rows, tokens) may be 0 and is at most 2^31 - 1; a table has at most 2^31 - 2 rows.  Rows of tokens have up to 8,388,480
+ * columns (more only where they hold whole 16-byte groups), and lr_embed_grad takes T * n up to 2^42: what passes that is
+ * LR_ERR_SHAPE like any other size, before anything is launched.  The gradient calls of this section use a scratch owned by the context,
  * allocated or grown on first use: make the first call of a size outside any stream capture.
  * Errors as above: LR_ERR_NULL, LR_ERR_SHAPE (a size, ld, k, or group count out of range), LR_ERR_ALIGNMENT (a pointer is not
  * aligned to its element size), LR_ERR_VALUE (a scale or factor that is not finite, an unknown score or id width), LR_ERR_NOMEM.

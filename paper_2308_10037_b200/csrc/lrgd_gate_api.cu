@@ -166,27 +166,29 @@ int embed_impl(lr_ctx* ctx, const E* d_table, int64_t ld_table, const void* d_id
     if (T == 0) return LR_OK;
     if (!d_table || !d_ids || !d_out) return LR_ERR_NULL;
     if (!aligned(d_table, sizeof(E)) || !aligned(d_out, sizeof(E)) || !aligned(d_ids, id_bytes)) return LR_ERR_ALIGNMENT;
+    auto fits = [&](int64_t vec) {     // vectors of `vec` elements: every row of both matrices starts on one and holds whole ones
+        const size_t b = size_t(vec) * sizeof(E);
+        return n % vec == 0 && ld_table % vec == 0 && ld_out % vec == 0 && aligned(d_table, b) && aligned(d_out, b);
+    };
+    constexpr int kVec = 16 / int(sizeof(E));
+    const int width = fits(kVec) ? kVec : sizeof(E) == 2 && fits(2) ? 2 : 1;
+    const int64_t pieces = (int64_t(n) + 128 * width - 1) / (128 * width);
+    if (pieces > 65535) return LR_ERR_SHAPE;
     NvtxRange range("lr_embed");
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const EmbedParams p{d_table, ld_table, d_ids, T, V, n, scale, d_out, ld_out, ctx->d_status};
-    auto fits = [&](int64_t vec) {     // vectors of `vec` elements: every row of both matrices starts on one and holds whole ones
-        const size_t b = size_t(vec) * sizeof(E);
-        return n % vec == 0 && ld_table % vec == 0 && ld_out % vec == 0 && aligned(d_table, b) && aligned(d_out, b);
-    };
+    const dim3 grid(unsigned(grid_for(ctx, T, kEmbedThreads / 32, std::max<int>(1, int(32 / pieces)))), unsigned(pieces));
     auto go = [&](auto vec) {
         constexpr int VEC = decltype(vec)::value;
-        const int64_t pieces = (int64_t(n) + 128 * VEC - 1) / (128 * VEC);
-        if (pieces > 65535) return int(LR_ERR_SHAPE);
-        const dim3 grid(unsigned(grid_for(ctx, T, kEmbedThreads / 32, std::max<int>(1, int(32 / pieces)))), unsigned(pieces));
         return launched(ctx, [&] {
             if (id_bytes == 8) k_embed<E, VEC, long long><<<grid, kEmbedThreads, 0, st>>>(p);
             else k_embed<E, VEC, int><<<grid, kEmbedThreads, 0, st>>>(p);
         });
     };
-    if (fits(16 / int(sizeof(E)))) return go(std::integral_constant<int, 16 / int(sizeof(E))>{});
-    if (sizeof(E) == 2 && fits(2)) return go(std::integral_constant<int, 2>{});
+    if (width == kVec) return go(std::integral_constant<int, kVec>{});
+    if (sizeof(E) == 2 && width == 2) return go(std::integral_constant<int, 2>{});
     return go(std::integral_constant<int, 1>{});
 }
 
@@ -200,6 +202,30 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
     if (!std::isfinite(scale)) return LR_ERR_VALUE;
     if (!d_grad || (T > 0 && (!d_ids || !d_dout))) return LR_ERR_NULL;
     if (!aligned(d_grad, 4) || !aligned(d_dout, sizeof(E)) || !aligned(d_ids, id_bytes)) return LR_ERR_ALIGNMENT;
+    const int R = T >= 4096 ? 32 : 16;             // fewer rows per chunk where there are few chunks
+    const int64_t chunks = (T + R - 1) / R;
+    SortParams sp{};
+    for (sp.passes = 1; V >> (kSortBits * sp.passes); ++sp.passes) {}               // keys 0..V
+    // Rows cleared while the sort runs, whether a token points there or not; the others are cleared after it, where none does.
+    // A pass over few positions takes about 5 us, in which the memory takes kClearPerPass bytes; kClearPerToken is what it takes in the
+    // time of each further position (32768 positions, two passes: 25 us).  The join takes about 8 us: kClearLate.
+    constexpr int64_t kClearPerPass = 28 << 20, kClearPerToken = 1100, kClearLate = 40 << 20;
+    const int64_t row_bytes = int64_t(n) * 4;
+    const int64_t early = accumulate ? 0 : std::min<int64_t>(V, (sp.passes * (kClearPerPass + T * kClearPerToken)) / row_bytes);
+    constexpr int kVec = 16 / int(sizeof(E));
+    const bool vec = n % kVec == 0 && ld_dout % kVec == 0 && aligned(d_dout, 16) && aligned(d_grad, 16);
+    const int64_t width = vec ? RunCols<E, kVec>::kSlice : RunCols<E, 1>::kSlice, slices = (int64_t(n) + width - 1) / width;
+    RunParams rp{};
+    // long runs have more than one chunk to themselves
+    rp.joiners = chunks < 3 ? 0 : int(std::min<int64_t>(chunks / 2, std::max<int64_t>(1, plan_sms(ctx) / slices)));
+    rp.clear[0] = rp.clear[1] = V;
+    rp.clear_rows = int(std::max<int64_t>(1, (64 << 10) / row_bytes));                  // about 64 KB per clearing CTA
+    if (!accumulate) {
+        rp.clear[0] = early;
+        if (rp.joiners > 0) rp.clear[1] = std::max(early, V - kClearLate / row_bytes);
+    }
+    const int64_t mid = (rp.clear[1] - rp.clear[0] + rp.clear_rows - 1) / rp.clear_rows, late = (V - rp.clear[1] + rp.clear_rows - 1) / rp.clear_rows;
+    if (slices > 65535 || chunks * slices + mid > INT32_MAX || late > INT32_MAX / 2) return LR_ERR_SHAPE;
     NvtxRange range("lr_embed_grad");
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
@@ -208,30 +234,20 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
         if (!accumulate) LR_CK(ctx, cudaMemsetAsync(d_grad, 0, size_t(V) * n * 4, st));
         return LR_OK;
     }
-    const int R = T >= 4096 ? 32 : 16;             // fewer rows per chunk where there are few chunks
-    const int64_t chunks = (T + R - 1) / R;
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     const size_t list = up(size_t(T) * 8), runs = up(size_t(chunks / 2 + 2) * 4), bits = up((size_t(V) + 31) / 32 * 4),
                  piece = size_t(2) * chunks * n * 4;
     const int rs = gate_scratch(ctx, 2 * list + runs + bits + piece);
     if (rs != LR_OK) return rs;
     unsigned char* w = ctx->d_scratch;
-    SortParams sp{};
     sp.ids = d_ids;
     sp.T = unsigned(T);
     sp.V = V;
     sp.padding = padding_id;
     for (int i = 0; i < 2; ++i) sp.place[i] = reinterpret_cast<uint2*>(w + i * list);
-    for (sp.passes = 1; V >> (kSortBits * sp.passes); ++sp.passes) {}               // keys 0..V
     sp.status = ctx->d_status;
     sp.long_runs = reinterpret_cast<unsigned int*>(w + 2 * list);
     sp.present = accumulate ? nullptr : reinterpret_cast<unsigned int*>(w + 2 * list + runs);
-    // Rows cleared while the sort runs, whether a token points there or not; the others are cleared after it, where none does.
-    // A pass over few positions takes about 5 us, in which the memory takes kClearPerPass bytes; kClearPerToken is what it takes in the
-    // time of each further position (32768 positions, two passes: 25 us).  The join takes about 8 us: kClearLate.
-    constexpr int64_t kClearPerPass = 28 << 20, kClearPerToken = 1100, kClearLate = 40 << 20;
-    const int64_t row_bytes = int64_t(n) * 4;
-    const int64_t early = accumulate ? 0 : std::min<int64_t>(V, (sp.passes * (kClearPerPass + T * kClearPerToken)) / row_bytes);
     if (early == V) sp.present = nullptr;          // all rows are cleared beside the sort: nobody asks which tokens occur
     sp.zero = d_grad;
     sp.zero_count = early * n;
@@ -245,24 +261,23 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
         else k_token_sort<int><<<clusters * kSortCtas, kSortThreads, 0, st>>>(sp);
     });
     if (r != LR_OK) return r;
-    const int last = (sp.passes - 1) & 1;
-    RunParams rp{sp.place[last], unsigned(T), unsigned(V), R, int(chunks), 0, d_dout, ld_dout, n, scale, d_grad,
-                 reinterpret_cast<float*>(w + 2 * list + runs + bits), sp.long_runs, sp.present, {0, 0}, 1, 0};
-    auto go = [&](auto vec, auto add) -> int {
-        constexpr int VEC = decltype(vec)::value;
+    rp.place = sp.place[(sp.passes - 1) & 1];
+    rp.T = unsigned(T);
+    rp.V = unsigned(V);
+    rp.R = R;
+    rp.chunks = int(chunks);
+    rp.slices = int(slices);
+    rp.dout = d_dout;
+    rp.ld = ld_dout;
+    rp.n = n;
+    rp.scale = scale;
+    rp.grad = d_grad;
+    rp.piece = reinterpret_cast<float*>(w + 2 * list + runs + bits);
+    rp.long_runs = sp.long_runs;
+    rp.present = sp.present;
+    auto go = [&](auto vector, auto add) -> int {
+        constexpr int VEC = decltype(vector)::value;
         constexpr bool ADD = decltype(add)::value;
-        const int64_t slices = (int64_t(n) + RunCols<E, VEC>::kSlice - 1) / RunCols<E, VEC>::kSlice;
-        rp.slices = int(slices);
-        // long runs have more than one chunk to themselves
-        rp.joiners = chunks < 3 ? 0 : int(std::min<int64_t>(chunks / 2, std::max<int64_t>(1, plan_sms(ctx) / slices)));
-        rp.clear[0] = rp.clear[1] = V;
-        rp.clear_rows = int(std::max<int64_t>(1, (64 << 10) / row_bytes));              // about 64 KB per clearing CTA
-        if (!accumulate) {
-            rp.clear[0] = early;
-            if (rp.joiners > 0) rp.clear[1] = std::max(early, V - kClearLate / row_bytes);
-        }
-        const int64_t mid = (rp.clear[1] - rp.clear[0] + rp.clear_rows - 1) / rp.clear_rows, late = (V - rp.clear[1] + rp.clear_rows - 1) / rp.clear_rows;
-        if (slices > 65535 || chunks * slices + mid > INT32_MAX || late > INT32_MAX / 2) return LR_ERR_SHAPE;
         LR_CK(ctx, launch_kernel(k_run_sum<E, VEC, ADD>, dim3(unsigned(chunks * slices + mid)), dim3(kRunThreads), 0, st, ctx->overlap, rp));
         ctx->launches += 1;
         if (rp.joiners == 0) return LR_OK;
@@ -271,10 +286,8 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
         ctx->launches += 1;
         return LR_OK;
     };
-    constexpr int kVec = 16 / int(sizeof(E));
     using Vector = std::integral_constant<int, kVec>;
     using Single = std::integral_constant<int, 1>;
-    const bool vec = n % kVec == 0 && ld_dout % kVec == 0 && aligned(d_dout, 16) && aligned(d_grad, 16);
     if (accumulate) return vec ? go(Vector{}, std::true_type{}) : go(Single{}, std::true_type{});
     return vec ? go(Vector{}, std::false_type{}) : go(Single{}, std::false_type{});
 }

@@ -47,3 +47,13 @@ def test_tokens_outside_the_table_are_reported_whatever_the_padding(ctx, T):
         want = dout.double().sum(0) - dout[T // 2].double()
         close(got[3], want, (T + 3) * U * dout.double().abs().sum(0))
         assert int((got != 0).any(dim=1).sum()) == 1
+
+
+def test_a_refused_embed_grad_launches_nothing(ctx):
+    n = 65535 * 256 + 1
+    out, dout = torch.full((1, n), 7.0, device="cuda"), torch.ones(1, n, device="cuda")
+    before = ctx.launch_count()
+    with pytest.raises(api.LrError) as e:
+        ctx.embed_grad(torch.zeros(1, dtype=torch.int64, device="cuda"), dout, 1, out=out)
+    assert e.value.code == api.LR_ERR_SHAPE
+    assert ctx.launch_count() == before and bool((out == 7.0).all())
