@@ -377,8 +377,9 @@ int lr_profile_read(lr_ctx* ctx, int32_t* launches, double* total_ms);
 /* Number of kernels this context has launched since it was created. */
 int lr_launch_count(lr_ctx* ctx, int64_t* out);
 
-/* Synchronises the device and returns in *out the device status word: LR_OK, LR_ERR_TIMEOUT, or LR_ERR_VALUE after lr_embed /
- * lr_embed_grad met a token outside the table.  Clears it. */
+/* Synchronises the device and returns in *out what its kernels have reported: LR_OK, LR_ERR_TIMEOUT, or LR_ERR_VALUE after lr_embed /
+ * lr_embed_grad met a token outside the table.  Clears what it returns; where both were reported, the first call returns
+ * LR_ERR_TIMEOUT and the next one LR_ERR_VALUE. */
 int lr_last_device_status(lr_ctx* ctx, int32_t* out);
 
 /*

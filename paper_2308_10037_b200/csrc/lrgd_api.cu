@@ -689,8 +689,8 @@ int lr_create(lr_ctx** out, int32_t device, int32_t n_max) {
         e = guarded_alloc(c, &c->d_partial, bytes);
         if (e == cudaErrorMemoryAllocation) rc = LR_ERR_NOMEM;
     }
-    if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_status), sizeof(int));
-    if (e == cudaSuccess) e = cudaMemset(c->d_status, 0, sizeof(int));
+    if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_status), 2 * sizeof(int));
+    if (e == cudaSuccess) e = cudaMemset(c->d_status, 0, 2 * sizeof(int));
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_tol), sizeof(TolState));
     if (e == cudaSuccess) e = cudaMemset(c->d_tol, 0, sizeof(TolState));
     if (e == cudaSuccess) e = guarded_alloc(c, &c->d_gbuf, (size_t(n_max) + 1) * sizeof(double));
@@ -1301,10 +1301,11 @@ int lr_last_device_status(lr_ctx* ctx, int32_t* out) {
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     LR_CK(ctx, cudaDeviceSynchronize());
-    int v = 0;
-    LR_CK(ctx, cudaMemcpy(&v, ctx->d_status, sizeof(int), cudaMemcpyDeviceToHost));
-    LR_CK(ctx, cudaMemset(ctx->d_status, 0, sizeof(int)));
-    *out = v;
+    int v[2] = {0, 0};
+    LR_CK(ctx, cudaMemcpy(v, ctx->d_status, sizeof(v), cudaMemcpyDeviceToHost));
+    const int which = v[0] != 0 ? 0 : 1;                              // the other one stays for the next call
+    LR_CK(ctx, cudaMemset(ctx->d_status + which, 0, sizeof(int)));
+    *out = v[which];
     return LR_OK;
 }
 

@@ -23,7 +23,7 @@ struct lr_ctx {
     int sm_count = 0;
     int n_max = 0;
     double* d_partial = nullptr;
-    int* d_status = nullptr;
+    int* d_status = nullptr;                        // [0] a wait that ran out, [1] a token outside its table: neither hides the other
     lrgd::TolState* d_tol = nullptr;                // stopping-rule state of lr_fit_tol
     double* d_gbuf = nullptr;                       // [n_max+1] gradient entries for the norm
     lrgd::TolState* h_tol = nullptr;                // pinned host mirror

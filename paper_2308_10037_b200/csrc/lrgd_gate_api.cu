@@ -178,7 +178,7 @@ int embed_impl(lr_ctx* ctx, const E* d_table, int64_t ld_table, const void* d_id
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const EmbedParams p{d_table, ld_table, d_ids, T, V, n, scale, d_out, ld_out, ctx->d_status};
+    const EmbedParams p{d_table, ld_table, d_ids, T, V, n, scale, d_out, ld_out, ctx->d_status + 1};
     const dim3 grid(unsigned(grid_for(ctx, T, kEmbedThreads / 32, std::max<int>(1, int(32 / pieces)))), unsigned(pieces));
     auto go = [&](auto vec) {
         constexpr int VEC = decltype(vec)::value;
@@ -245,7 +245,7 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
     sp.V = V;
     sp.padding = padding_id;
     for (int i = 0; i < 2; ++i) sp.place[i] = reinterpret_cast<uint2*>(w + i * list);
-    sp.status = ctx->d_status;
+    sp.status = ctx->d_status + 1;
     sp.long_runs = reinterpret_cast<unsigned int*>(w + 2 * list);
     sp.present = accumulate ? nullptr : reinterpret_cast<unsigned int*>(w + 2 * list + runs);
     if (early == V) sp.present = nullptr;          // all rows are cleared beside the sort: nobody asks which tokens occur

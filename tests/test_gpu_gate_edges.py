@@ -57,3 +57,15 @@ def test_a_refused_embed_grad_launches_nothing(ctx):
         ctx.embed_grad(torch.zeros(1, dtype=torch.int64, device="cuda"), dout, 1, out=out)
     assert e.value.code == api.LR_ERR_SHAPE
     assert ctx.launch_count() == before and bool((out == 7.0).all())
+
+
+def test_a_token_outside_the_table_does_not_hide_a_wait_that_ran_out(ctx):
+    table, outside = rnd(4, 8), torch.tensor([9], device="cuda")
+    assert ctx.device_status() == 0
+    for first in (True, False):                     # whichever was reported first
+        if first:
+            ctx.embed(table, outside)
+        ctx.selftest_wait(arm=False, limit_ms=20)
+        if not first:
+            ctx.embed_grad(outside, rnd(1, 8), 4)
+        assert [ctx.device_status() for _ in range(3)] == [api.LR_ERR_TIMEOUT, api.LR_ERR_VALUE, 0]
