@@ -176,7 +176,12 @@ cudaError_t tensor_map_encoder(EncodeTiledFn* out) {
         return r;
     }();
     *out = resolved.fn;
-    return resolved.err;
+    if (resolved.err != cudaSuccess) return resolved.err;
+    // The encoder needs a current context, which a host thread has only after a runtime call that needs one too: setting the
+    // device that is current anyway (0 by default) is such a call.
+    int device = 0;
+    const cudaError_t e = cudaGetDevice(&device);
+    return e == cudaSuccess ? cudaSetDevice(device) : e;
 }
 
 int grow(lr_ctx* ctx, void** buf, size_t* have, size_t need) {
