@@ -683,6 +683,9 @@ int lr_create(lr_ctx** out, int32_t device, int32_t n_max) {
     cudaGetDevice(&prev);
     int rc = LR_OK;
     cudaError_t e = cudaSetDevice(device);
+    // Everything below is cleared on a stream of the context's own, which is waited for at the end: the default stream may be busy, and
+    // the stream of the first call need not wait for it.
+    if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&c->hstream, cudaStreamNonBlocking);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&c->sm_count, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) {
         const size_t bytes = size_t(c->sm_count) * kMaxGridPerSm * (size_t(n_max) + 2) * sizeof(double);
@@ -690,20 +693,20 @@ int lr_create(lr_ctx** out, int32_t device, int32_t n_max) {
         if (e == cudaErrorMemoryAllocation) rc = LR_ERR_NOMEM;
     }
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_status), 2 * sizeof(int));
-    if (e == cudaSuccess) e = cudaMemset(c->d_status, 0, 2 * sizeof(int));
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->d_status, 0, 2 * sizeof(int), c->hstream);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_tol), sizeof(TolState));
-    if (e == cudaSuccess) e = cudaMemset(c->d_tol, 0, sizeof(TolState));
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->d_tol, 0, sizeof(TolState), c->hstream);
     if (e == cudaSuccess) e = guarded_alloc(c, &c->d_gbuf, (size_t(n_max) + 1) * sizeof(double));
     if (e == cudaSuccess) e = cudaMallocHost(reinterpret_cast<void**>(&c->h_tol), sizeof(TolState));
     if (e == cudaSuccess) e = cudaMallocHost(reinterpret_cast<void**>(&c->h_words), 4 * sizeof(int));
     if (e == cudaSuccess) e = guarded_alloc(c, &c->d_vel, (size_t(n_max) + 1) * sizeof(float));
     if (e == cudaSuccess) e = guarded_alloc(c, &c->d_oscr, (size_t(n_max) + 2) * sizeof(double));
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_oticket), sizeof(unsigned int));
-    if (e == cudaSuccess) e = cudaMemset(c->d_oticket, 0, sizeof(unsigned int));
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->d_oticket, 0, sizeof(unsigned int), c->hstream);
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_gbar), 2 * kMaxWorld * sizeof(unsigned int));
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_rank_params), kMaxWorld * sizeof(FitParams));
     if (e == cudaSuccess) e = cudaMalloc(reinterpret_cast<void**>(&c->d_gate_words), kGateWords * sizeof(unsigned int));
-    if (e == cudaSuccess) e = cudaMemset(c->d_gate_words, 0, kGateWords * sizeof(unsigned int));
+    if (e == cudaSuccess) e = cudaMemsetAsync(c->d_gate_words, 0, kGateWords * sizeof(unsigned int), c->hstream);
     if (e == cudaSuccess) {
         int l2 = 0;
         e = cudaDeviceGetAttribute(&l2, cudaDevAttrL2CacheSize, device);
@@ -714,7 +717,7 @@ int lr_create(lr_ctx** out, int32_t device, int32_t n_max) {
         e = cudaDeviceGetAttribute(&coop, cudaDevAttrCooperativeLaunch, device);
         c->coop = coop != 0;
     }
-    if (e == cudaSuccess) e = cudaStreamCreateWithFlags(&c->hstream, cudaStreamNonBlocking);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(c->hstream);
     if (prev >= 0) cudaSetDevice(prev);
     if (e != cudaSuccess) {
         for (unsigned char* base : c->guard_bases) cudaFree(base);     // d_partial, d_gbuf, d_vel, d_oscr
@@ -726,6 +729,7 @@ int lr_create(lr_ctx** out, int32_t device, int32_t n_max) {
         if (c->d_gbar) cudaFree(c->d_gbar);
         if (c->d_rank_params) cudaFree(c->d_rank_params);
         if (c->d_gate_words) cudaFree(c->d_gate_words);
+        if (c->hstream) cudaStreamDestroy(c->hstream);
         delete c;
         return rc != LR_OK ? rc : LR_ERR_CUDA;
     }
@@ -1304,7 +1308,8 @@ int lr_last_device_status(lr_ctx* ctx, int32_t* out) {
     int v[2] = {0, 0};
     LR_CK(ctx, cudaMemcpy(v, ctx->d_status, sizeof(v), cudaMemcpyDeviceToHost));
     const int which = v[0] != 0 ? 0 : 1;                              // the other one stays for the next call
-    LR_CK(ctx, cudaMemset(ctx->d_status + which, 0, sizeof(int)));
+    LR_CK(ctx, cudaMemsetAsync(ctx->d_status + which, 0, sizeof(int), ctx->hstream));
+    LR_CK(ctx, cudaStreamSynchronize(ctx->hstream));                  // a report of a later call is not cleared
     *out = v[which];
     return LR_OK;
 }

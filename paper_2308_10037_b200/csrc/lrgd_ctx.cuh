@@ -78,8 +78,8 @@ cudaError_t guarded_alloc(lr_ctx* c, T** user, size_t bytes) {
     if (e != cudaSuccess) return e;
     c->guard_bases.push_back(base);
     c->guard_sizes.push_back(body);
-    e = cudaMemset(base, kGuardPattern, kGuardBytes);
-    if (e == cudaSuccess) e = cudaMemset(base + kGuardBytes + body, kGuardPattern, kGuardBytes);
+    e = cudaMemsetAsync(base, kGuardPattern, kGuardBytes, c->hstream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(base + kGuardBytes + body, kGuardPattern, kGuardBytes, c->hstream);
     *user = reinterpret_cast<T*>(base + kGuardBytes);
     return e;
 }

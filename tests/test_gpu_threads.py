@@ -1,4 +1,5 @@
 """Calls from host threads: the first CUDA call of a thread, and threads that share a stream."""
+import ctypes
 import threading
 
 import pytest
@@ -46,4 +47,28 @@ def test_a_tensor_map_is_made_in_a_thread_that_has_made_no_cuda_call():
     got = in_a_new_thread(lambda: c.loss_grad(X, y, w, b))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+    c.close()
+
+
+def test_a_new_context_is_ready_when_it_is_there(ctx):
+    # its words are cleared when the call returns, not when the default stream gets to it: that one is busy here, and the stream in use
+    # does not wait for it.  Memory of that size that was freed with other contents makes the difference visible.
+    rt = ctypes.CDLL(next(p for p in map(str.strip, open("/proc/self/maps").read().split()) if "libcudart.so" in p))
+    blocks = [ctypes.c_void_p() for _ in range(512)]
+    for p in blocks:
+        assert rt.cudaMalloc(ctypes.byref(p), ctypes.c_size_t(8192)) == 0
+        assert rt.cudaMemset(p, 0xFF, ctypes.c_size_t(8192)) == 0
+    torch.cuda.synchronize()
+    for p in blocks:
+        assert rt.cudaFree(p) == 0
+    x = rnd(30001, 64, seed=5)
+    want = ctx.route(x, 4)[2]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(600_000_000)                  # the default stream, a third of a second
+    c = api.Context(n_max=1, device=0)
+    with torch.cuda.stream(side):
+        got = [c.route(x, 4)[2] for _ in range(2)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want) for g in got)
     c.close()
