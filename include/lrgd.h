@@ -18,7 +18,8 @@
  *
  * Streams: every device-pointer call enqueues its kernels on `stream` (a cudaStream_t passed as
  * void*, NULL = the legacy default stream) and returns without synchronising; outputs are valid once
- * the caller has synchronised that stream.  One lr_ctx must not be used from two streams at once.
+ * the caller has synchronised that stream.  One lr_ctx must not be used from two streams at once, nor by two host threads at
+ * once; only the calls of the token-gate section may come from several threads that share the context's stream.
  *
  * Errors: every call returns LR_OK (0) or a negative LR_ERR_* code; nothing is launched when
  * argument validation fails.  A wait inside a kernel that exceeds its bound makes the kernel finish

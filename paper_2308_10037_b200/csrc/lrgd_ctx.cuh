@@ -48,6 +48,9 @@ struct lr_ctx {
     void* d_hl = nullptr; size_t hl_bytes = 0;      // labels
     void* d_hXh = nullptr; size_t hXh_bytes = 0;    // bfloat16 copy of X (lr_fit_host_bf16, lr_predict_host_bf16)
     cudaStream_t hstream = nullptr;
+    // One token-gate call at a time, from the look at the scratch to the call's last launch: the kernels of one call hand data to each
+    // other through the scratch, so those of another host thread on the same stream must come before or after all of them.
+    std::mutex gate_mu;
     // scratch of the token-gate entry points (grown on demand, between guard regions) and their zero-initialised counters
     unsigned char* d_scratch = nullptr; size_t scratch_bytes = 0;
     unsigned int* d_gate_words = nullptr;           // [kGateWords] zero between calls

@@ -92,6 +92,7 @@ int route_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t ex
     if (!aligned(d_logits, sizeof(E)) || !aligned(d_bias, 4) || !aligned(d_ids, 4) || !aligned(d_weights, 4) || !aligned(d_counts, 4))
         return LR_ERR_ALIGNMENT;
     NvtxRange range("lr_route");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -128,6 +129,7 @@ int route_grad_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32
     if (!d_logits || !d_ids || !d_dweights || !d_dlogits) return LR_ERR_NULL;
     if (!aligned(d_logits, sizeof(E)) || !aligned(d_ids, 4) || !aligned(d_dweights, 4) || !aligned(d_dlogits, sizeof(E))) return LR_ERR_ALIGNMENT;
     NvtxRange range("lr_route_grad");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -175,6 +177,7 @@ int embed_impl(lr_ctx* ctx, const E* d_table, int64_t ld_table, const void* d_id
     const int64_t pieces = (int64_t(n) + 128 * width - 1) / (128 * width);
     if (pieces > 65535) return LR_ERR_SHAPE;
     NvtxRange range("lr_embed");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -227,6 +230,7 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
     const int64_t mid = (rp.clear[1] - rp.clear[0] + rp.clear_rows - 1) / rp.clear_rows, late = (V - rp.clear[1] + rp.clear_rows - 1) / rp.clear_rows;
     if (slices > 65535 || chunks * slices + mid > INT32_MAX || late > INT32_MAX / 2) return LR_ERR_SHAPE;
     NvtxRange range("lr_embed_grad");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -308,6 +312,7 @@ int ckpt8_move(lr_ctx* ctx, bool save, const E* x, E* back, int64_t ld, int64_t 
     if (!rows || !q || !s) return LR_ERR_NULL;
     if (!aligned(rows, sizeof(E)) || !aligned(s, 4)) return LR_ERR_ALIGNMENT;
     NvtxRange range(save ? "lr_ckpt8_save" : "lr_ckpt8_load");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -340,6 +345,7 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     if (!d_grad_w || (T > 0 && (!d_q || !d_s || !d_dz))) return LR_ERR_NULL;
     if (!aligned(d_s, 4) || !aligned(d_dz, sizeof(E)) || !aligned(d_grad_w, 4) || !aligned(d_grad_b, 4)) return LR_ERR_ALIGNMENT;
     NvtxRange range("lr_ckpt8_grad");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
     DeviceGuard g(ctx);
     if (!g.ok) return LR_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

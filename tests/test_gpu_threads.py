@@ -72,3 +72,29 @@ def test_a_new_context_is_ready_when_it_is_there(ctx):
     torch.cuda.synchronize()
     assert all(torch.equal(g, want) for g in got)
     c.close()
+
+
+def test_two_threads_on_one_stream(ctx):
+    # calls of several kernels that hand data on through one scratch: each thread's results are those of its calls alone
+    work = []
+    for i, (T, V, n, C) in enumerate([(20000, 3000, 128, 40), (700, 50, 96, 5)]):
+        ids, dout = torch.randint(0, V, (T,), generator=gen(i), device="cuda"), rnd(T, n, seed=i + 2)
+        dz = rnd(T, C, seed=i + 4)
+        q, s = ctx.ckpt8_save(dout)
+        work.append((ids, dout, V, q, s, dz, (ctx.embed_grad(ids, dout, V), *ctx.ckpt8_grad(q, s, dz), ctx.route(dz, 2)[2])))
+    torch.cuda.synchronize()
+    start, wrong = threading.Barrier(2), [None, None]
+
+    def run(i):
+        ids, dout, V, q, s, dz, want = work[i]
+        start.wait()
+        got = [(api.lr_embed_grad(ids, dout, V), *api.lr_ckpt8_grad(q, s, dz), api.lr_route(dz, 2)[2]) for _ in range(150)]
+        torch.cuda.synchronize()
+        wrong[i] = sum(not torch.equal(a, b) for one in got for a, b in zip(one, want))
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert wrong == [0, 0]
