@@ -387,7 +387,7 @@ int lr_last_device_status(lr_ctx* ctx, int32_t* out);
  * Bounds check of the library's own device workspaces (no counterpart in the paper).  Every array that the kernels index
  * by a computed offset -- the per-CTA partial rows, the gradient buffer of the stopping rule, the context's velocity and
  * the optimiser scratch -- is allocated between two 256-byte guard regions filled with a fixed pattern when the context
- * is created (the scratch of the token-gate calls: when a call makes it grow).  lr_check_guards synchronises the device, reads
+ * is created (the scratch of the token-gate calls: when a call makes it grow or a graph gets its own).  lr_check_guards synchronises the device, reads
  * the guard regions back and returns in *corrupted how many of them (two per array) no longer hold the pattern: anything but 0 means a kernel wrote outside its array.  It changes nothing, so it
  * can be called at any point between calls; the tests call it after every batch of shapes.
  */
@@ -451,7 +451,9 @@ const char* lr_status_string(int code);
  * T (rows, tokens) may be 0 and is at most 2^31 - 1; a table has at most 2^31 - 2 rows.  Rows of tokens have up to 8,388,480
  * columns (more only where they hold whole 16-byte groups), and lr_embed_grad takes T * n up to 2^42: what passes that is
  * LR_ERR_SHAPE like any other size, before anything is launched.  The gradient calls of this section use a scratch owned by the context,
- * allocated or grown on first use: make the first call of a size outside any stream capture.
+ * allocated or grown on first use (what it outgrew is freed, which waits for the device).  Calls that are captured into a graph
+ * work in scratch of the graph's own, which lives as long as the graph and what is instantiated from it: graphs may be replayed on
+ * several streams, beside one another and beside calls on the context's stream.  The context has to outlive them.
  * Errors as above: LR_ERR_NULL, LR_ERR_SHAPE (a size, ld, k, or group count out of range), LR_ERR_ALIGNMENT (a pointer is not
  * aligned to its element size), LR_ERR_VALUE (a scale or factor that is not finite, an unknown score or id width), LR_ERR_NOMEM.
  */

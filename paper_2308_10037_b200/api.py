@@ -707,16 +707,13 @@ def lr_predict(X, w, b, thr, ctx: Context | None = None):
 
 
 _gate_ctx: dict[tuple[int, int], Context] = {}
-_gate_latest: dict[int, Context] = {}
 _gate_lock = threading.Lock()
 
 
 def _ctx_of(t, ctx: Context | None) -> Context:
     """The default context of the token-gate calls: one per device and stream, because a context's scratch serves one stream at a
-    time (threads on one stream share it: the library takes their calls one after the other), and kept for good, because a captured
-    graph may hold its address.  A stream that is being captured and has none yet
-    borrows the one used last on the device (the warm-up's: nothing can be allocated then); replays of such a graph must not overlap
-    with calls on the stream of the warm-up."""
+    time (threads on one stream share it: the library takes their calls one after the other).  Calls that are captured work in scratch of
+    the graph's own."""
     if ctx is not None:
         return ctx
     if not (isinstance(t, torch.Tensor) and t.is_cuda):
@@ -728,10 +725,7 @@ def _ctx_of(t, ctx: Context | None) -> Context:
         with _gate_lock:                            # two threads on one stream share one context, also when both are its first
             c = _gate_ctx.get(at)
             if c is None:
-                if dev in _gate_latest and torch.cuda.is_current_stream_capturing():
-                    return _gate_latest[dev]
                 c = _gate_ctx[at] = Context(n_max=1, device=dev)
-    _gate_latest[dev] = c
     return c
 
 

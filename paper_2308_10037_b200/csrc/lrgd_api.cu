@@ -682,6 +682,7 @@ int lr_create(lr_ctx** out, int32_t device, int32_t n_max) {
     int prev = -1;
     cudaGetDevice(&prev);
     int rc = LR_OK;
+    const RelaxedCapture relaxed;
     cudaError_t e = cudaSetDevice(device);
     // Everything below is cleared on a stream of the context's own, which is waited for at the end: the default stream may be busy, and
     // the stream of the first call need not wait for it.
@@ -742,6 +743,14 @@ int lr_destroy(lr_ctx* ctx) {
     {
         DeviceGuard g(ctx);
         cudaDeviceSynchronize();
+        {
+            // what graphs hold stays with them
+            GraphScratches& captured = graph_scratches();
+            const std::lock_guard<std::mutex> hold(captured.mu);
+            for (GraphScratch* b : captured.all)
+                if (b->owner == ctx) b->owner = nullptr;
+        }
+        free_dead_scratch();
         for (cudaEvent_t e : ctx->ev) cudaEventDestroy(e);
         if (ctx->hstream) cudaStreamDestroy(ctx->hstream);
         for (unsigned char* base : ctx->guard_bases) cudaFree(base);   // d_partial, d_gbuf, d_vel, d_oscr, the scratch of the token-gate calls
@@ -1320,15 +1329,26 @@ int lr_check_guards(lr_ctx* ctx, int32_t* corrupted) {
     if (!g.ok) return LR_ERR_CUDA;
     LR_CK(ctx, cudaDeviceSynchronize());
     int bad = 0;
-    unsigned char host[kGuardBytes];
-    for (size_t i = 0; i < ctx->guard_bases.size(); ++i) {
+    auto look = [&](const unsigned char* base, size_t body) -> int {
+        unsigned char host[kGuardBytes];
         for (int side = 0; side < 2; ++side) {
-            const unsigned char* src = ctx->guard_bases[i] + (side ? kGuardBytes + ctx->guard_sizes[i] : 0);
-            LR_CK(ctx, cudaMemcpy(host, src, kGuardBytes, cudaMemcpyDeviceToHost));
+            LR_CK(ctx, cudaMemcpy(host, base + (side ? kGuardBytes + body : 0), kGuardBytes, cudaMemcpyDeviceToHost));
             bool clean = true;
             for (size_t k = 0; k < kGuardBytes; ++k) clean = clean && host[k] == static_cast<unsigned char>(kGuardPattern);
             if (!clean) ++bad;
         }
+        return LR_OK;
+    };
+    for (size_t i = 0; i < ctx->guard_bases.size(); ++i) {
+        const int rc = look(ctx->guard_bases[i], ctx->guard_sizes[i]);
+        if (rc != LR_OK) return rc;
+    }
+    GraphScratches& captured = graph_scratches();
+    const std::lock_guard<std::mutex> hold(captured.mu);
+    for (const GraphScratch* b : captured.all) {
+        if (b->owner != ctx) continue;
+        const int rc = look(b->base, b->body);
+        if (rc != LR_OK) return rc;
     }
     *corrupted = bad;
     return LR_OK;

@@ -8,7 +8,9 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>
+#include <atomic>
 #include <mutex>
+#include <new>
 #include <vector>
 
 namespace lrgd {
@@ -65,6 +67,50 @@ struct lr_ctx {
     std::vector<size_t> guard_sizes;                // user bytes, rounded up to kGuardBytes
 };
 
+namespace lrgd {
+
+// Scratch that belongs to a captured graph: calls captured on one stream use it one after the other, whenever and wherever the graph is
+// replayed, and nobody else does.  The graph and what is instantiated from it hold it through a user object, whose end marks it
+// dead (no CUDA call may be made there); the memory is given back by a later call.
+struct GraphScratch {
+    const lr_ctx* owner;                            // the context it was made through, NULL once that is gone
+    int device;
+    unsigned long long capture;                     // id of the capture, and the stream in it
+    cudaStream_t stream;
+    unsigned char* base;                            // guard region, counters, scratch, guard region
+    size_t body;
+    std::atomic<bool> dead{false};
+};
+struct GraphScratches {
+    std::mutex mu;
+    std::vector<GraphScratch*> all;
+    std::atomic<int> dead{0};
+};
+inline GraphScratches& graph_scratches() {
+    static GraphScratches* const them = new GraphScratches();      // (never destroyed: graphs may end after the library's statics)
+    return *them;
+}
+inline void end_of_graph(void* scratch) {
+    static_cast<GraphScratch*>(scratch)->dead.store(true);
+    graph_scratches().dead.fetch_add(1);
+}
+// Gives back what ended graphs held (cudaFree waits for what still runs).
+inline void free_dead_scratch() {
+    GraphScratches& g = graph_scratches();
+    const std::lock_guard<std::mutex> hold(g.mu);
+    for (size_t i = 0; i < g.all.size();) {
+        GraphScratch* b = g.all[i];
+        if (!b->dead.load()) { ++i; continue; }
+        cudaFree(b->base);
+        delete b;
+        g.all[i] = g.all.back();
+        g.all.pop_back();
+        g.dead.fetch_sub(1);
+    }
+}
+
+}  // namespace lrgd
+
 namespace {
 
 // Guard regions around the context's device workspaces (per-CTA partial rows, gradient buffer, velocity, optimiser scratch):
@@ -73,19 +119,35 @@ namespace {
 constexpr size_t kGuardBytes = 256;
 constexpr int kGuardPattern = 0xA5;
 
+// `bytes` of device memory (rounded up to *body) that start kGuardBytes into *base, between two guard regions
+cudaError_t guarded_block(const lr_ctx* c, size_t bytes, unsigned char** base, size_t* body) {
+    *body = (bytes + kGuardBytes - 1) / kGuardBytes * kGuardBytes;
+    *base = nullptr;
+    cudaError_t e = cudaMalloc(reinterpret_cast<void**>(base), *body + 2 * kGuardBytes);
+    if (e != cudaSuccess) return e;
+    e = cudaMemsetAsync(*base, kGuardPattern, kGuardBytes, c->hstream);
+    if (e == cudaSuccess) e = cudaMemsetAsync(*base + kGuardBytes + *body, kGuardPattern, kGuardBytes, c->hstream);
+    return e;
+}
+
 template <class T>
 cudaError_t guarded_alloc(lr_ctx* c, T** user, size_t bytes) {
-    const size_t body = (bytes + kGuardBytes - 1) / kGuardBytes * kGuardBytes;
     unsigned char* base = nullptr;
-    cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&base), body + 2 * kGuardBytes);
-    if (e != cudaSuccess) return e;
+    size_t body = 0;
+    const cudaError_t e = guarded_block(c, bytes, &base, &body);
+    if (!base) return e;
     c->guard_bases.push_back(base);
     c->guard_sizes.push_back(body);
-    e = cudaMemsetAsync(base, kGuardPattern, kGuardBytes, c->hstream);
-    if (e == cudaSuccess) e = cudaMemsetAsync(base + kGuardBytes + body, kGuardPattern, kGuardBytes, c->hstream);
     *user = reinterpret_cast<T*>(base + kGuardBytes);
     return e;
 }
+
+// While one of these lives, this host thread may allocate and free though a stream is being captured (here or in another thread).
+struct RelaxedCapture {
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+    ~RelaxedCapture() { cudaThreadExchangeStreamCaptureMode(&mode); }
+};
 
 // A named range around a whole library call, visible on a profiler's timeline (costs nothing when no tool is attached).
 struct NvtxRange {

@@ -19,27 +19,102 @@ namespace {
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - 1;   // positions are sorted as 32-bit numbers
 constexpr int64_t kMaxLd = int64_t(1) << 40;
 
-// The context's scratch for these calls, between guard regions, grown when a call needs more than any before it.  What it
-// outgrew is kept until lr_destroy: a captured graph may still point there.  Growing by half at least bounds the sum.
-int gate_scratch(lr_ctx* ctx, size_t need) {
-    if (ctx->scratch_bytes >= need) return LR_OK;
-    need = std::max(need, ctx->scratch_bytes + ctx->scratch_bytes / 2);
-    need = (need + (size_t(1) << 20) - 1) >> 20 << 20;
+// What a call works in: `words` are kGateWords counters that are zero between calls, `data` is at least what it asked for.
+struct Scratch {
+    unsigned char* data;
+    unsigned int* words;
+};
+
+int alloc_failed(lr_ctx* ctx, cudaError_t e) {
+    cudaGetLastError();
+    ctx->last_cuda = int(e);
+    return e == cudaErrorMemoryAllocation ? LR_ERR_NOMEM : LR_ERR_CUDA;
+}
+
+// A capture: the scratch of this graph and stream, made now if there is none that is large enough (see GraphScratch).
+int captured_scratch(lr_ctx* ctx, size_t need, cudaStream_t st, unsigned long long id, cudaGraph_t graph, Scratch* out) {
+    constexpr size_t kWordBytes = kGateWords * sizeof(unsigned int);
+    auto use = [&](const GraphScratch* b) {
+        out->words = reinterpret_cast<unsigned int*>(b->base + kGuardBytes);
+        out->data = b->base + kGuardBytes + kWordBytes;
+        return LR_OK;
+    };
+    GraphScratches& g = graph_scratches();
+    const std::lock_guard<std::mutex> hold(g.mu);
+    for (const GraphScratch* b : g.all)
+        if (!b->dead.load() && b->owner == ctx && b->capture == id && b->stream == st && b->body >= kWordBytes + need) return use(b);
     try {
-        ctx->guard_bases.reserve(ctx->guard_bases.size() + 1);
-        ctx->guard_sizes.reserve(ctx->guard_sizes.size() + 1);
+        g.all.reserve(g.all.size() + 1);
     } catch (const std::bad_alloc&) {
         return LR_ERR_NOMEM;
     }
-    unsigned char* fresh = nullptr;
-    const cudaError_t e = guarded_alloc(ctx, &fresh, need);
+    GraphScratch* b = new (std::nothrow) GraphScratch{ctx, ctx->device, id, st, nullptr, 0};
+    if (!b) return LR_ERR_NOMEM;
+    cudaError_t e = guarded_block(ctx, kWordBytes + need, &b->base, &b->body);
+    if (e == cudaSuccess) e = cudaMemsetAsync(b->base + kGuardBytes, 0, kWordBytes, ctx->hstream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(ctx->hstream);
+    cudaUserObject_t object = nullptr;
+    if (e == cudaSuccess) e = cudaUserObjectCreate(&object, b, end_of_graph, 1, cudaUserObjectNoDestructorSync);
     if (e != cudaSuccess) {
-        cudaGetLastError();
-        ctx->last_cuda = int(e);
-        return e == cudaErrorMemoryAllocation ? LR_ERR_NOMEM : LR_ERR_CUDA;
+        if (b->base) cudaFree(b->base);
+        delete b;
+        return alloc_failed(ctx, e);
     }
-    ctx->d_scratch = fresh;
-    ctx->scratch_bytes = need;
+    g.all.push_back(b);
+    e = cudaGraphRetainUserObject(graph, object, 1, cudaGraphUserObjectMove);
+    if (e != cudaSuccess) {
+        cudaUserObjectRelease(object, 1);           // marks it dead
+        return alloc_failed(ctx, e);
+    }
+    return use(b);
+}
+
+// The scratch of a call on `st`.  Outside a capture it is the context's, between guard regions, grown (by half at least) when a call needs
+// more than any before it; what it outgrew is freed.  A capture gets scratch of the graph's own.
+int gate_scratch(lr_ctx* ctx, size_t need, cudaStream_t st, Scratch* out) {
+    if (st != nullptr && st != cudaStreamLegacy) {              // (the legacy stream cannot be captured)
+        cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+        unsigned long long id = 0;
+        cudaGraph_t graph = nullptr;
+        LR_CK(ctx, cudaStreamGetCaptureInfo(st, &capturing, &id, &graph));
+        if (capturing == cudaStreamCaptureStatusActive) {
+            const RelaxedCapture relaxed;
+            return captured_scratch(ctx, need, st, id, graph, out);
+        }
+    }
+    if (graph_scratches().dead.load() > 0) {
+        const RelaxedCapture relaxed;
+        free_dead_scratch();
+    }
+    if (ctx->scratch_bytes < need) {
+        need = std::max(need, ctx->scratch_bytes + ctx->scratch_bytes / 2);
+        need = (need + (size_t(1) << 20) - 1) >> 20 << 20;
+        const RelaxedCapture relaxed;
+        if (ctx->scratch_bytes > 0) {
+            for (size_t i = 0; i < ctx->guard_bases.size(); ++i) {
+                if (ctx->guard_bases[i] + kGuardBytes != ctx->d_scratch) continue;
+                cudaFree(ctx->guard_bases[i]);      // waits for the calls that use it
+                ctx->guard_bases.erase(ctx->guard_bases.begin() + i);
+                ctx->guard_sizes.erase(ctx->guard_sizes.begin() + i);
+                break;
+            }
+            ctx->d_scratch = nullptr;
+            ctx->scratch_bytes = 0;
+        }
+        try {
+            ctx->guard_bases.reserve(ctx->guard_bases.size() + 1);
+            ctx->guard_sizes.reserve(ctx->guard_sizes.size() + 1);
+        } catch (const std::bad_alloc&) {
+            return LR_ERR_NOMEM;
+        }
+        unsigned char* fresh = nullptr;
+        const cudaError_t e = guarded_alloc(ctx, &fresh, need);
+        if (e != cudaSuccess) return alloc_failed(ctx, e);
+        ctx->d_scratch = fresh;
+        ctx->scratch_bytes = need;
+    }
+    out->data = ctx->d_scratch;
+    out->words = ctx->d_gate_words;
     return LR_OK;
 }
 
@@ -100,9 +175,14 @@ int route_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t ex
         if (d_counts) LR_CK(ctx, cudaMemsetAsync(d_counts, 0, size_t(experts) * 4, st));
         return LR_OK;
     }
-    const RouteParams p{d_logits, ld, T, experts, opt->k, opt->groups, opt->top_groups, opt->renorm != 0, opt->factor,
-                        d_bias, d_ids, d_weights, d_counts, ctx->d_gate_words};
     const int grid = even_grid(ctx, T, kRouteWarps, 8);
+    Scratch scratch{};
+    if (d_counts && grid > 1) {                    // the CTAs add their counts up in words of the scratch
+        const int rs = gate_scratch(ctx, 0, st, &scratch);
+        if (rs != LR_OK) return rs;
+    }
+    const RouteParams p{d_logits, ld, T, experts, opt->k, opt->groups, opt->top_groups, opt->renorm != 0, opt->factor,
+                        d_bias, d_ids, d_weights, d_counts, scratch.words};
     return launched(ctx, [&] {
         for_vpl(experts, [&](auto vpl) {
             constexpr int VPL = decltype(vpl)::value;
@@ -241,9 +321,10 @@ int embed_grad_impl(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const E* d
     auto up = [](size_t b) { return (b + 255) / 256 * 256; };
     const size_t list = up(size_t(T) * 8), runs = up(size_t(chunks / 2 + 2) * 4), bits = up((size_t(V) + 31) / 32 * 4),
                  piece = size_t(2) * chunks * n * 4;
-    const int rs = gate_scratch(ctx, 2 * list + runs + bits + piece);
+    Scratch scratch{};
+    const int rs = gate_scratch(ctx, 2 * list + runs + bits + piece, st, &scratch);
     if (rs != LR_OK) return rs;
-    unsigned char* w = ctx->d_scratch;
+    unsigned char* w = scratch.data;
     sp.ids = d_ids;
     sp.T = unsigned(T);
     sp.V = V;
@@ -367,10 +448,11 @@ int ckpt8_grad_impl(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d
     float *part_w = nullptr, *part_b = nullptr;
     if (chunks > 1) {
         const size_t wb = up(size_t(chunks) * C * n * 4);
-        const int rs = gate_scratch(ctx, wb + size_t(chunks) * C * 4);
+        Scratch scratch{};
+        const int rs = gate_scratch(ctx, wb + size_t(chunks) * C * 4, st, &scratch);
         if (rs != LR_OK) return rs;
-        part_w = reinterpret_cast<float*>(ctx->d_scratch);
-        part_b = reinterpret_cast<float*>(ctx->d_scratch + wb);
+        part_w = reinterpret_cast<float*>(scratch.data);
+        part_b = reinterpret_cast<float*>(scratch.data + wb);
     }
     TcGradParams p{};
     p.g = CkptGradParams{d_q, ld_q, d_s, T, n, groups, d_dz, ld_dz, C, int(chunks), rows, accumulate != 0, part_w, part_b, d_grad_w, d_grad_b};

@@ -3,7 +3,6 @@ import threading
 import time
 
 import pytest
-import torch
 
 from paper_2308_10037_b200 import api
 from test_gate_validation import fake
@@ -22,9 +21,7 @@ def made(monkeypatch):
 
     monkeypatch.setattr(api, "Context", Slow)
     monkeypatch.setattr(api, "_gate_ctx", {})
-    monkeypatch.setattr(api, "_gate_latest", {})
     monkeypatch.setattr(api, "_raw_stream", lambda device: 7)
-    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
     return got
 
 
