@@ -729,6 +729,18 @@ def _ctx_of(t, ctx: Context | None) -> Context:
     return c
 
 
+def release_contexts() -> None:
+    """Closes the contexts that the module's functions have made (one per device for the binary model, one per device and stream for the
+    token-gate calls) and gives their memory back; later calls make new ones.  Waits for the devices.  No other thread may be in a call of
+    the module, and a graph captured through one of these contexts must not be replayed any more."""
+    with _gate_lock:
+        closing = [*_default_ctx.values(), *_gate_ctx.values()]
+        _default_ctx.clear()
+        _gate_ctx.clear()
+    for c in closing:
+        c.close()
+
+
 def lr_embed(table, ids, scale=1.0, out=None, ctx: Context | None = None):
     """Scaled rows of a token table (see ``Context.embed``)."""
     return _ctx_of(table, ctx).embed(table, ids, scale, out)

@@ -16,11 +16,15 @@ def made(monkeypatch):
     class Slow:
         def __init__(self, n_max, device):
             time.sleep(0.05)
-            self.device = device
+            self.device, self.open = device, True
             got.append(self)
+
+        def close(self):
+            self.open = False
 
     monkeypatch.setattr(api, "Context", Slow)
     monkeypatch.setattr(api, "_gate_ctx", {})
+    monkeypatch.setattr(api, "_default_ctx", {})
     monkeypatch.setattr(api, "_raw_stream", lambda device: 7)
     return got
 
@@ -38,3 +42,13 @@ def test_threads_that_come_first_together_share_one_context(made):
     for t in threads:
         t.join()
     assert len(made) == 1 and len(seen) == 8 and all(c is made[0] for c in seen)
+
+
+def test_contexts_can_be_released(made, monkeypatch):
+    x = fake((2, 2))
+    first = api._ctx_of(x, None)
+    monkeypatch.setattr(api, "_raw_stream", lambda device: 8)
+    assert api._ctx_of(x, None) is not first and api._ctx_of(x, None) is made[1] and len(made) == 2
+    api.release_contexts()
+    assert not any(c.open for c in made)
+    assert api._ctx_of(x, None) is made[2] and made[2].open

@@ -98,3 +98,16 @@ def test_two_threads_on_one_stream(ctx):
     for t in threads:
         t.join()
     assert wrong == [0, 0]
+
+
+def test_released_contexts_give_their_memory_back_and_come_again():
+    x, y = rnd(2000, 64, seed=6), (rnd(2000, seed=7) < 0).float()
+    ids = torch.randint(0, 50, (200_000,), generator=gen(8), device="cuda")
+    dout = rnd(200_000, 256, seed=9)
+    want = [t.clone() for t in (api.lr_fit(x, y, 0.5, 3)[0], api.lr_embed_grad(ids, dout, 50))]
+    torch.cuda.synchronize()
+    held = torch.cuda.mem_get_info()[0]
+    api.release_contexts()
+    assert torch.cuda.mem_get_info()[0] > held
+    got = (api.lr_fit(x, y, 0.5, 3)[0], api.lr_embed_grad(ids, dout, 50))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
