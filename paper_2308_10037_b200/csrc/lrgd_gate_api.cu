@@ -271,7 +271,9 @@ int embed_impl(lr_ctx* ctx, const E* d_table, int64_t ld_table, const void* d_id
         });
     };
     if (width == kVec) return go(std::integral_constant<int, kVec>{});
-    if (sizeof(E) == 2 && width == 2) return go(std::integral_constant<int, 2>{});
+    if constexpr (sizeof(E) == 2) {
+        if (width == 2) return go(std::integral_constant<int, 2>{});
+    }
     return go(std::integral_constant<int, 1>{});
 }
 
