@@ -484,7 +484,8 @@ int lr_embed_grad_bf16(lr_ctx* ctx, const void* d_ids, int32_t id_bytes, const u
 /*
  * Routing: the k best of a row's `experts` logits l, with weights.
  *   score LR_SCORE_SIGMOID: p = 1/(1+exp(-l)), chosen by c = p + bias;   LR_SCORE_SOFTMAX: p = softmax(l), chosen by c = l + bias
- *   (the bias, NULL or [experts], balances the load: it enters the choice only, never the weights)
+ *   (the bias, NULL or [experts], balances the load: it enters the choice only, never the weights.  With softmax it is added to the
+ *   logit, not to the probability: a gate that was trained with a bias on the probabilities chooses differently)
  *   groups > 1: the experts stand in that many equal groups (expert e in group e / (experts/groups)); a group is worth the sum of
  *   its two largest c (sigmoid) or its largest c (softmax), and only the top_groups best groups keep their experts
  *   chosen are the k largest c, in descending order, ties to the lower index (for groups as well)

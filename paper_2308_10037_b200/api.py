@@ -435,9 +435,10 @@ class Context:
 
     def route(self, logits, k, bias=None, groups=1, top_groups=None, score="sigmoid", renorm=True, factor=1.0):
         """The ``k`` best experts of every row of ``logits`` [T, E] (float32 or bfloat16): (ids int32 [T, k], weights float32
-        [T, k], counts int32 [E]).  ``score`` "sigmoid" or "softmax"; ``bias`` float32 [E] enters the choice only; with ``groups``
-        only the experts of the ``top_groups`` best groups (default: all) can be chosen; ``renorm`` divides by the sum of the chosen;
-        ``factor`` multiplies the weights.  See ``lr_route`` in the header for the exact rules."""
+        [T, k], counts int32 [E]).  ``score`` "sigmoid" or "softmax"; ``bias`` float32 [E] enters the choice only (added to the
+        sigmoid, or to the logit where the score is softmax); with ``groups`` only the experts of the ``top_groups`` best groups (default:
+        all) can be chosen; ``renorm`` divides by the sum of the chosen; ``factor`` multiplies the weights.  See ``lr_route`` in the header
+        for the exact rules."""
         pl, T, E, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
         groups = int(groups)
         opt = self._route_opt(int(k), groups, groups if top_groups is None else int(top_groups), score, bool(renorm), float(factor))

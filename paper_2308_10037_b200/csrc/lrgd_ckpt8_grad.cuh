@@ -10,7 +10,7 @@
 // So every product is a floating-point one: a row loses no bits to another row of a larger dz or scale.  Integers of a common step
 // per class and group (four bytes a factor on the int8 products, 40 us at the size below) did lose them: beside one
 // masked row whose scale was 1e6 times the others' the sums were off by a thousandth, so that form was taken out.
-// 16384 x 4096, 64 classes: 53 us, k_ckpt8_join (6) included; the floor is 11 (74 MB).
+// 16384 x 4096, 64 classes: 53 us, k_ckpt8_join (6) included; two classes 41 us; the floor is 11 (74 MB).
 //
 // A CTA takes two groups (256 columns), one block of up to 64 classes and a range of rows, 32 rows per stage.  The raw q of a
 // stage comes by TMA (a ring of kTcRing stages; by plain word loads where q is not 16-byte aligned).  Two sets of eight warps
@@ -18,10 +18,13 @@
 // class of dz into 2 x 3 terms, written K-major (8 consecutive t of one column or class are 16 bytes) into one of three operand
 // buffers.  A seventeenth warp issues the tcgen05.mma of a stage when its eight warps have arrived, an eighteenth the copies of a
 // later stage: the scales, one row per lane, are fetched once per stage there (every warp gathering its own cost a quarter of
-// the kernel's shared-memory bandwidth, which bounds it: operands written once and read once by the tensor cores).
+// the kernel's shared-memory bandwidth).
+// What bounds it: the latency of the converting warps, of which the registers leave room for four per scheduler.  With 64 classes a warp
+// takes 3,100 clocks per stage of its own: 830 to form and cut dz * s, 590 to widen q, 300 to fetch its next dz, 230 in the flushes, the
+// rest waiting and publishing; issue slots are 64 % busy.  Stages of 64 rows (fewer of them, but spilled registers) took 59 us.
 // No barrier spans the CTA inside the loop: the warps meet on mbarriers, so that loads, conversion and products overlap.
 // Every kTcFlush stages the sums move from tensor memory to registers: the tensor cores drop the bits below the accumulator's last
-// place, an error that grows with the length of the chain (114 steps: 1.2e-6 of the result; 32 steps: 2.6e-7).
+// place, an error that grows with the length of the chain (114 steps: 1.2e-6 of the result; 32 steps: 2.3e-7).
 // The rows are split over CTAs to fill the GPU; k_ckpt8_join adds the parts in order.
 #pragma once
 #include <cuda.h>
@@ -418,7 +421,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
 // One class, X^T err of the binary model: bound by reading q, the pipeline above would only add its start and its conversions.
 // Sixteen lanes take 256 columns of a row, sixteen neighbouring ones per lane (VEC: one 16-byte load), a warp two rows at a time,
 // the CTA's warps take turns.  Scale and dz are one factor per lane and row.  The sums of the lanes and warps that share a column
-// meet in shared memory in a fixed order.  Two CTAs of 16 warps with 64 registers a thread, no rows fetched ahead by hand:
+// meet in shared memory in a fixed order.  The sums are fp32 in short chains (a lane adds every 32nd row of its CTA's, seven at
+// 65536 x 256; then 32 lanes and warps, then the CTAs in 32 slices): 2e-7 of the result there, 3e-7 for a matrix product in fp32.
+// Two CTAs of 16 warps with 64 registers a thread, no rows fetched ahead by hand:
 // 16384 x 4096 17 us (3.9 TB/s), 65536 x 256 8.5 us; with two rows ahead 27 and 9.0 us, with four and one CTA per SM 52 and 12.
 constexpr int kUnitWarps = 16;
 constexpr int kUnitCtas = 2;                                         // per SM
