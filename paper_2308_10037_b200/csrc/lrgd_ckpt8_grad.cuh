@@ -422,7 +422,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) k_ckpt8_grad_tc(const __grid_co
 // Sixteen lanes take 256 columns of a row, sixteen neighbouring ones per lane (VEC: one 16-byte load), a warp two rows at a time,
 // the CTA's warps take turns.  Scale and dz are one factor per lane and row.  The sums of the lanes and warps that share a column
 // meet in shared memory in a fixed order.  The sums are fp32 in short chains (a lane adds every 32nd row of its CTA's, seven at
-// 65536 x 256; then 32 lanes and warps, then the CTAs in 32 slices): 2e-7 of the result there, 3e-7 for a matrix product in fp32.
+// 65536 x 256; then 32 lanes and warps, then the CTAs in 32 slices): 2 to 4e-7 of the result there (dz has both signs and the sums
+// cancel), like a matrix product in fp32.
 // Two CTAs of 16 warps with 64 registers a thread, no rows fetched ahead by hand:
 // 16384 x 4096 17 us (3.9 TB/s), 65536 x 256 8.5 us; with two rows ahead 27 and 9.0 us, with four and one CTA per SM 52 and 12.
 constexpr int kUnitWarps = 16;
