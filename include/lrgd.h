@@ -379,7 +379,7 @@ int lr_profile_read(lr_ctx* ctx, int32_t* launches, double* total_ms);
 int lr_launch_count(lr_ctx* ctx, int64_t* out);
 
 /* Synchronises the device and returns in *out what its kernels have reported: LR_OK, LR_ERR_TIMEOUT, or LR_ERR_VALUE after lr_embed /
- * lr_embed_grad met a token outside the table.  Clears what it returns; where both were reported, the first call returns
+ * lr_embed_grad met a token outside the table or a class loss a target outside the classes.  Clears what it returns; where both were reported, the first call returns
  * LR_ERR_TIMEOUT and the next one LR_ERR_VALUE. */
 int lr_last_device_status(lr_ctx* ctx, int32_t* out);
 
@@ -545,6 +545,117 @@ int lr_ckpt8_grad(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s
                   int64_t ld_dz, int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream);
 int lr_ckpt8_grad_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float* d_s, int64_t T, int32_t n, const uint16_t* d_dz,
                        int64_t ld_dz, int32_t C, int32_t accumulate, float* d_grad_w, float* d_grad_b, void* stream);
+
+/*
+ * ---------------------------------------------------------------------------------------------------------------------
+ * Losses over a vocabulary's classes.  (No counterpart in the paper: its model has two classes.  These are the log-likelihood of a
+ * many-class logistic model and what is learned through it from preferences -- the logistic loss again --, from rewards and from a
+ * teacher.)  A row holds the logits of V classes; with l = scale * row, lse = log sum_v exp(l_v), p = exp(l - lse) and a target y its
+ * log-probability is lp = l_y - lse.  scale (finite, > 0) is the inverse of a temperature.
+ * Logits are fp32 or bfloat16 (the *_bf16 calls), row-major with a leading dimension, of any alignment to the element size; gradients have
+ * their type, are formed in fp32 and rounded once.  They are fastest where rows of the gradient start at the same offset from a 16-byte
+ * boundary as those of the logits.  d_dlogits may be the logits themselves (the same address and ld: the gradient replaces them); any other
+ * overlap is LR_ERR_VALUE.  All T rows of a gradient are written.
+ * Targets and classes are int32 or int64 (id_bytes 4, 8).  A row whose target is ignore_id does not count: its logits are not read (they may
+ * hold anything), its log-probability and its gradient are 0.  A target outside [0, V) that is not ignore_id is treated the same way and sets
+ * the device status word to LR_ERR_VALUE (lr_last_device_status).  The same goes for a row whose weight is 0.
+ * A row of logits may hold -inf (a class that is masked); a NaN, a +inf or nothing but -inf makes what the row enters NaN.
+ * A loss is factor * sum of weight * (row's or pair's loss) / norm; norm = 0 stands for the sum of the weights that count (their number without
+ * weights), and where that is 0 the loss and the gradient are 0.  factor carries a gradient from further up, or a share of a larger batch.
+ * Sums of a row are fp32, what is left of it and sums over rows fp64; results are bit-reproducible.
+ * T is at most 2^31 - 1 and may be 0, V at most 2^24.  Scratch, streams, threads and graphs as in the section above.
+ * Errors: LR_ERR_NULL, LR_ERR_SHAPE (a size, ld or K out of range), LR_ERR_ALIGNMENT, LR_ERR_VALUE (an option out of range or not
+ * finite, an id width, an overlap), LR_ERR_NOMEM.
+ */
+
+/* d_logp [T] = lp, d_lse (NULL or [T]) = lse of every row; both 0 for rows that do not count. */
+int lr_logp(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+            int64_t ignore_id, float scale, float* d_logp, float* d_lse, void* stream);
+int lr_logp_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                 int64_t ignore_id, float scale, float* d_logp, float* d_lse, void* stream);
+
+/*
+ * Gradient of sum_t d_dlogp[t] * lp_t:  d_dlogits[t,v] = scale * d_dlogp[t] * ([v = y_t] - exp(l_tv - d_lse[t])), with the d_lse of
+ * lr_logp.  A row whose d_dlogp is 0 does not count.
+ */
+int lr_logp_grad(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                 int64_t ignore_id, float scale, const float* d_lse, const float* d_dlogp, float* d_dlogits, int64_t ld_d, void* stream);
+int lr_logp_grad_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                      int64_t ignore_id, float scale, const float* d_lse, const float* d_dlogp, uint16_t* d_dlogits, int64_t ld_d,
+                      void* stream);
+
+/*
+ * Clipped policy loss of rows with an advantage A, the log-probability `old` of the policy that acted and `ref` of a reference:
+ *   r = exp(lp - old)  (d_old_logp NULL: 1, the policy itself acted; its gradient is that of lp),  r' = r held in [1 - clip_low, 1 + clip_high]
+ *   row's loss = -min(r A, r' A) + kl_coef * kl,   kl = exp(ref - lp) - (ref - lp) - 1  (d_ref_logp NULL: 0)
+ * d_stats [4] = loss, and of the rows that count the weighted means (divided by norm) of -min(r A, r' A), of kl and of [r A > r' A]
+ * (rows that the clip holds: no gradient from the first term).  d_logp NULL or [T] = lp.  d_dlogits NULL: no gradient.
+ * d_weights NULL or [T] (a mask, or 1 / length).  clip_low, clip_high >= 0 (infinity: no clip), kl_coef finite.
+ */
+typedef struct lr_policy_opt {
+    int64_t ignore_id;
+    float scale;
+    float clip_low;
+    float clip_high;
+    float kl_coef;
+    float norm;
+    float factor;
+} lr_policy_opt;
+int lr_policy_loss(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                   const lr_policy_opt* opt, const float* d_advantages, const float* d_old_logp, const float* d_ref_logp,
+                   const float* d_weights, float* d_stats, float* d_logp, float* d_dlogits, int64_t ld_d, void* stream);
+int lr_policy_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                        const lr_policy_opt* opt, const float* d_advantages, const float* d_old_logp, const float* d_ref_logp,
+                        const float* d_weights, float* d_stats, float* d_logp, uint16_t* d_dlogits, int64_t ld_d, void* stream);
+
+/*
+ * Preference loss of `pairs` pairs of sequences: sequence i holds rows offsets[i] .. offsets[i+1] - 1 (d_offsets [2 * pairs + 1], int32 or
+ * int64 by offset_bytes, rising); sequence i < pairs is preferred to sequence i + pairs.  With S_i the sum of lp over the rows of the
+ * sequence that count (their mean with average != 0; 0 where none counts) and R = d_ref_logp [2 * pairs] the same of a reference (NULL: 0)
+ *   h_i = beta * ((S_i - R_i) - (S_(i+pairs) - R_(i+pairs))) - margin
+ *   pair's loss = -(1 - smoothing) * log sigmoid(h_i) - smoothing * log sigmoid(-h_i),   0 <= smoothing <= 1
+ * d_loss [1], d_margins [pairs] = h, d_seq_logp NULL or [2 * pairs] = S.  Weights (NULL or [pairs]) and norm are those of pairs.  Rows
+ * outside all sequences do not count.  A sequence whose offsets fall or leave [0, T] is taken as empty and sets the status word.
+ */
+typedef struct lr_pref_opt {
+    int64_t ignore_id;
+    float scale;
+    float beta;
+    float margin;
+    float smoothing;
+    int32_t average;
+    float norm;
+    float factor;
+} lr_pref_opt;
+int lr_pref_loss(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                 const void* d_offsets, int32_t offset_bytes, int64_t pairs, const lr_pref_opt* opt, const float* d_ref_logp,
+                 const float* d_weights, float* d_loss, float* d_margins, float* d_seq_logp, float* d_dlogits, int64_t ld_d, void* stream);
+int lr_pref_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                      const void* d_offsets, int32_t offset_bytes, int64_t pairs, const lr_pref_opt* opt, const float* d_ref_logp,
+                      const float* d_weights, float* d_loss, float* d_margins, float* d_seq_logp, uint16_t* d_dlogits, int64_t ld_d,
+                      void* stream);
+
+/*
+ * Distillation from the K logits of a teacher that are known of every row: d_ids [T][K] names their classes, d_teacher [T][K] holds them (fp32
+ * or bfloat16 by teacher_bytes 4, 2).  With t = scale * teacher
+ *   q_k = exp(t_k) / sum_j exp(t_j), or with d_teacher_lse [T] (the log-sum-exp of all of the teacher's t) q_k = exp(t_k - lse): the known part
+ *   row's loss = sum_k q_k (log q_k - lp_k),  lp over all V classes of the student;   gradient scale * ((sum_k q_k) p_v - q_v)
+ * d_loss [1], d_row_kl NULL or [T] = the rows' losses.  Weights NULL or [T]; all rows of a weight other than 0 count in norm.  A class equal
+ * to ignore_id, or whose teacher logit is -inf, is absent; one outside [0, V) is absent and sets the status word.  A row of which
+ * all are absent has loss and gradient 0.  A class that is named twice has both weights.  K <= 1024.
+ */
+typedef struct lr_distill_opt {
+    int64_t ignore_id;
+    float scale;
+    float norm;
+    float factor;
+} lr_distill_opt;
+int lr_distill_loss(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_ids, int32_t id_bytes, int32_t K,
+                    const void* d_teacher, int32_t teacher_bytes, const lr_distill_opt* opt, const float* d_teacher_lse,
+                    const float* d_weights, float* d_loss, float* d_row_kl, float* d_dlogits, int64_t ld_d, void* stream);
+int lr_distill_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_ids, int32_t id_bytes,
+                         int32_t K, const void* d_teacher, int32_t teacher_bytes, const lr_distill_opt* opt, const float* d_teacher_lse,
+                         const float* d_weights, float* d_loss, float* d_row_kl, uint16_t* d_dlogits, int64_t ld_d, void* stream);
 
 #ifdef __cplusplus
 }

@@ -30,7 +30,8 @@ EXPORTS = ["lr_plan_query", "lr_create", "lr_destroy", "lr_loss_grad", "lr_fit",
            "lr_set_cluster", "lr_cluster_ctas", "lr_f1_counts", "lr_check_guards",
            "lr_embed", "lr_embed_bf16", "lr_embed_grad", "lr_embed_grad_bf16", "lr_route", "lr_route_bf16", "lr_route_grad",
            "lr_route_grad_bf16", "lr_ckpt8_save", "lr_ckpt8_save_bf16", "lr_ckpt8_load", "lr_ckpt8_load_bf16", "lr_ckpt8_grad",
-           "lr_ckpt8_grad_bf16"]
+           "lr_ckpt8_grad_bf16", "lr_logp", "lr_logp_bf16", "lr_logp_grad", "lr_logp_grad_bf16", "lr_policy_loss", "lr_policy_loss_bf16",
+           "lr_pref_loss", "lr_pref_loss_bf16", "lr_distill_loss", "lr_distill_loss_bf16"]
 
 CKPT8_GROUP = 128                                   # columns of a row that share a scale in the 8-bit form
 
@@ -50,6 +51,19 @@ class LrOpt(ctypes.Structure):
 class LrRouteOpt(ctypes.Structure):
     _fields_ = [("k", ctypes.c_int32), ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("score", ctypes.c_int32),
                 ("renorm", ctypes.c_int32), ("factor", ctypes.c_float)]
+
+
+class LrPolicyOpt(ctypes.Structure):
+    _fields_ = [("ignore_id", ctypes.c_int64)] + [(k, ctypes.c_float) for k in ("scale", "clip_low", "clip_high", "kl_coef", "norm", "factor")]
+
+
+class LrPrefOpt(ctypes.Structure):
+    _fields_ = [("ignore_id", ctypes.c_int64), ("scale", ctypes.c_float), ("beta", ctypes.c_float), ("margin", ctypes.c_float),
+                ("smoothing", ctypes.c_float), ("average", ctypes.c_int32), ("norm", ctypes.c_float), ("factor", ctypes.c_float)]
+
+
+class LrDistillOpt(ctypes.Structure):
+    _fields_ = [("ignore_id", ctypes.c_int64), ("scale", ctypes.c_float), ("norm", ctypes.c_float), ("factor", ctypes.c_float)]
 
 
 _SCORES = {"sigmoid": 0, "softmax": 1}              # LR_SCORE_SIGMOID, LR_SCORE_SOFTMAX
@@ -129,7 +143,13 @@ def lib() -> ctypes.CDLL:
         L.lr_ckpt8_save.argtypes = [P, P, I64, I64, I32, P, I64, P, P]
         L.lr_ckpt8_load.argtypes = [P, P, I64, P, I64, I32, P, I64, P]
         L.lr_ckpt8_grad.argtypes = [P, P, I64, P, I64, I32, P, I64, I32, I32, P, P, P]
-        for name in ("lr_embed", "lr_embed_grad", "lr_route", "lr_route_grad", "lr_ckpt8_save", "lr_ckpt8_load", "lr_ckpt8_grad"):
+        L.lr_logp.argtypes = [P, P, I64, I64, I32, P, I32, I64, F, P, P, P]
+        L.lr_logp_grad.argtypes = [P, P, I64, I64, I32, P, I32, I64, F, P, P, P, I64, P]
+        L.lr_policy_loss.argtypes = [P, P, I64, I64, I32, P, I32, ctypes.POINTER(LrPolicyOpt), P, P, P, P, P, P, P, I64, P]
+        L.lr_pref_loss.argtypes = [P, P, I64, I64, I32, P, I32, P, I32, I64, ctypes.POINTER(LrPrefOpt), P, P, P, P, P, P, I64, P]
+        L.lr_distill_loss.argtypes = [P, P, I64, I64, I32, P, I32, I32, P, I32, ctypes.POINTER(LrDistillOpt), P, P, P, P, P, I64, P]
+        for name in ("lr_embed", "lr_embed_grad", "lr_route", "lr_route_grad", "lr_ckpt8_save", "lr_ckpt8_load", "lr_ckpt8_grad", "lr_logp",
+                     "lr_logp_grad", "lr_policy_loss", "lr_pref_loss", "lr_distill_loss"):
             getattr(L, name + "_bf16").argtypes = getattr(L, name).argtypes
         for name in EXPORTS:
             if name != "lr_status_string":
@@ -382,11 +402,11 @@ class Context:
             raise ValueError(f"{name}: lives on cuda:{t.device.index}, the call runs on cuda:{self.device}")
         return t.data_ptr(), rows, cols, ld, "_bf16" if t.dtype is torch.bfloat16 else ""
 
-    def _tokens(self, ids):
+    def _tokens(self, ids, name="ids"):
         if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dtype in (torch.int32, torch.int64) and ids.is_contiguous()):
-            raise TypeError("ids: expected a contiguous CUDA tensor of dtype torch.int32 or torch.int64")
+            raise TypeError(f"{name}: expected a contiguous CUDA tensor of dtype torch.int32 or torch.int64")
         if ids.device.index != self.device:
-            raise ValueError(f"ids: lives on cuda:{ids.device.index}, the call runs on cuda:{self.device}")
+            raise ValueError(f"{name}: lives on cuda:{ids.device.index}, the call runs on cuda:{self.device}")
         return ids.data_ptr(), 8 if ids.dtype == torch.int64 else 4, ids.numel()
 
     def embed(self, table, ids, scale=1.0, out=None):
@@ -511,6 +531,140 @@ class Context:
         if rc:
             self._check(rc, "lr_ckpt8_grad" + sfx)
         return grad_w, grad_b
+
+    # ---- losses over a vocabulary's classes --------------------------------------------------------
+    def _targets(self, targets, T, name="targets"):
+        pi, ib, count = self._tokens(targets, name)
+        if targets.dim() != 1 or count != T:
+            raise ValueError(f"{name}: shape {tuple(targets.shape)} for {T} rows of logits")
+        return pi, ib
+
+    def _per_row(self, t, T, name):
+        """Address of an optional float32 [T]."""
+        if t is not None and (not isinstance(t, torch.Tensor) or t.shape != (T,)):
+            raise ValueError(f"{name}: expected a float32 CUDA tensor of shape {(T,)}")
+        return self._p(t, torch.float32, name)
+
+    def _dlogits(self, logits, out):
+        """(gradient, its address, its leading dimension): ``out``, or a new one whose rows start as far from a 16-byte boundary as those
+        of the logits."""
+        T, V = logits.shape
+        if out is None:
+            per = 16 // logits.element_size()
+            pitch = V + (logits.stride(0) - V) % per if T > 1 else V
+            first = logits.data_ptr() % 16 // logits.element_size()
+            out = torch.empty_strided((T * pitch + first,), (1,), dtype=logits.dtype, device=logits.device)[first:].as_strided((T, V), (pitch, 1)) \
+                if pitch != V or first else _new(T, V, logits.dtype, logits.device)
+            return out, out.data_ptr(), pitch
+        return (out, *self._rows(out, (logits.dtype,), "out", (T, V))[0:4:3])
+
+    @staticmethod
+    @functools.lru_cache(maxsize=64)
+    def _loss_opt(kind, *fields):
+        return kind(*fields)
+
+    @staticmethod
+    def _norm(norm):
+        """The C side's 0 is the sum of the weights that count."""
+        if norm is None:
+            return 0.0
+        if not float(norm) > 0.0:
+            raise ValueError("norm: expected a positive number, or None for the sum of the weights that count")
+        return float(norm)
+
+    def logp(self, logits, targets, scale=1.0, ignore_id=-100):
+        """(logp, lse) of the rows of ``logits`` [T, V] (float32 or bfloat16): the log-probability of ``targets`` [T] (int32 or int64) under
+        softmax(scale * logits) and the log-sum-exp, float32 [T].  Both are 0 for rows whose target is ``ignore_id``."""
+        pl, T, V, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
+        pt, ib = self._targets(targets, T)
+        both = _new(2, T, torch.float32, logits.device)
+        at = both.data_ptr()
+        rc = getattr(lib(), "lr_logp" + sfx)(self._h, pl, ld, T, V, pt, ib, int(ignore_id), float(scale), at, at + 4 * T, self._stream())
+        if rc:
+            self._check(rc, "lr_logp" + sfx)
+        return both[0], both[1]
+
+    def logp_grad(self, logits, targets, lse, dlogp, scale=1.0, ignore_id=-100, out=None):
+        """Gradient [T, V] of sum(dlogp * logp) back to the logits, in their type, from ``logp``'s ``lse`` and ``dlogp`` (float32 [T]).
+        ``out`` may be ``logits``."""
+        pl, T, V, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
+        pt, ib = self._targets(targets, T)
+        if lse is None or dlogp is None:
+            raise ValueError("lse, dlogp: expected float32 CUDA tensors")
+        ps, pg = self._per_row(lse, T, "lse"), self._per_row(dlogp, T, "dlogp")
+        out, po, ldo = self._dlogits(logits, out)
+        rc = getattr(lib(), "lr_logp_grad" + sfx)(self._h, pl, ld, T, V, pt, ib, int(ignore_id), float(scale), ps, pg, po, ldo, self._stream())
+        if rc:
+            self._check(rc, "lr_logp_grad" + sfx)
+        return out
+
+    def policy_loss(self, logits, targets, advantages, old_logp=None, ref_logp=None, weights=None, scale=1.0, clip_low=0.2, clip_high=0.2,
+                    kl_coef=0.0, norm=None, factor=1.0, ignore_id=-100, grad=True, out=None):
+        """Clipped policy loss of rows with ``advantages`` [T] and its gradient: (stats, logp, dlogits).  ``old_logp``, ``ref_logp``,
+        ``weights``: float32 [T] or None.  ``stats`` [4]: the loss, and the means of its first term, of the divergence from the reference
+        and of the share of clipped rows.  ``norm`` is what the weighted sum over rows is divided by (None: the sum of the weights that count).
+        ``grad`` False: no gradient (None).  ``out`` may be ``logits``.  See ``lr_policy_loss`` in the header for the exact rules."""
+        pl, T, V, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
+        pt, ib = self._targets(targets, T)
+        opt = self._loss_opt(LrPolicyOpt, int(ignore_id), float(scale), float(clip_low), float(clip_high), float(kl_coef), self._norm(norm), float(factor))
+        if advantages is None:
+            raise ValueError("advantages: expected a float32 CUDA tensor")
+        rows = [self._per_row(t, T, n) for t, n in ((advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights"))]
+        buf = torch.empty_strided((4 + T,), (1,), dtype=torch.float32, device=logits.device)
+        out, po, ldo = self._dlogits(logits, out) if grad else (None, None, V)
+        at = buf.data_ptr()
+        rc = getattr(lib(), "lr_policy_loss" + sfx)(self._h, pl, ld, T, V, pt, ib, ctypes.byref(opt), *rows, at, at + 16, po, ldo, self._stream())
+        if rc:
+            self._check(rc, "lr_policy_loss" + sfx)
+        return buf[:4], buf[4:], out
+
+    def pref_loss(self, logits, targets, offsets, ref_logp=None, weights=None, beta=0.1, margin=0.0, smoothing=0.0, average=False, scale=1.0,
+                  norm=None, factor=1.0, ignore_id=-100, grad=True, out=None):
+        """Preference loss of pairs of sequences and its gradient: (loss [1], margins [P], seq_logp [2P], dlogits).  ``offsets`` [2P + 1]
+        (int32 or int64) cuts the rows of ``logits`` into sequences; sequence i is preferred to sequence i + P.  ``ref_logp`` float32
+        [2P] or None: a reference's ``seq_logp``; ``weights`` float32 [P] or None.  ``average``: means instead of sums over a sequence.
+        See ``lr_pref_loss`` in the header for the exact rules."""
+        pl, T, V, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
+        pt, ib = self._targets(targets, T)
+        pf, ob, count = self._tokens(offsets, "offsets")
+        if offsets.dim() != 1 or count % 2 == 0:
+            raise ValueError("offsets: expected 2 * pairs + 1 of them")
+        P = count // 2
+        opt = self._loss_opt(LrPrefOpt, int(ignore_id), float(scale), float(beta), float(margin), float(smoothing), int(bool(average)),
+                             self._norm(norm), float(factor))
+        pr, pw = self._per_row(ref_logp, 2 * P, "ref_logp"), self._per_row(weights, P, "weights")
+        buf = torch.empty_strided((1 + 3 * P,), (1,), dtype=torch.float32, device=logits.device)
+        out, po, ldo = self._dlogits(logits, out) if grad else (None, None, V)
+        at = buf.data_ptr()
+        rc = getattr(lib(), "lr_pref_loss" + sfx)(self._h, pl, ld, T, V, pt, ib, pf, ob, P, ctypes.byref(opt), pr, pw, at, at + 4,
+                                                  at + 4 + 4 * P, po, ldo, self._stream())
+        if rc:
+            self._check(rc, "lr_pref_loss" + sfx)
+        return buf[:1], buf[1:1 + P], buf[1 + P:], out
+
+    def distill_loss(self, logits, ids, teacher, teacher_lse=None, weights=None, scale=1.0, norm=None, factor=1.0, ignore_id=-1, grad=True,
+                     out=None):
+        """Divergence from a teacher whose logits ``teacher`` [T, K] (float32 or bfloat16) of the classes ``ids`` [T, K] (int32 or int64)
+        are known, and its gradient: (loss [1], row_kl [T], dlogits).  ``teacher_lse`` float32 [T]: the log-sum-exp of all of the teacher's
+        scaled logits, where the known ones are not to be normalised among themselves.  A usual ``factor`` is 1 / scale**2.  See
+        ``lr_distill_loss`` in the header for the exact rules."""
+        pl, T, V, ld, sfx = self._rows(logits, _ROW_TYPES, "logits")
+        pi, ib, _ = self._tokens(ids)
+        if ids.dim() != 2 or ids.shape[0] != T or not isinstance(teacher, torch.Tensor) or teacher.shape != ids.shape:
+            raise ValueError("ids, teacher: expected two tensors [T, K]")
+        if teacher.dtype not in _ROW_TYPES:
+            raise TypeError("teacher: expected a CUDA tensor of dtype torch.float32 or torch.bfloat16")
+        pv = self._p(teacher, teacher.dtype, "teacher")
+        opt = self._loss_opt(LrDistillOpt, int(ignore_id), float(scale), self._norm(norm), float(factor))
+        ps, pw = self._per_row(teacher_lse, T, "teacher_lse"), self._per_row(weights, T, "weights")
+        buf = torch.empty_strided((1 + T,), (1,), dtype=torch.float32, device=logits.device)
+        out, po, ldo = self._dlogits(logits, out) if grad else (None, None, V)
+        at = buf.data_ptr()
+        rc = getattr(lib(), "lr_distill_loss" + sfx)(self._h, pl, ld, T, V, pi, ib, ids.shape[1], pv, teacher.element_size(), ctypes.byref(opt),
+                                                     ps, pw, at, at + 4, po, ldo, self._stream())
+        if rc:
+            self._check(rc, "lr_distill_loss" + sfx)
+        return buf[:1], buf[1:], out
 
     def shard_sums(self, X, y, w, b, sums):
         """Unnormalised fp64 sums [n+2] of the local rows into ``sums`` (float64 CUDA tensor)."""
@@ -775,6 +929,36 @@ def lr_ckpt8_load(q, s, dtype=torch.float32, out=None, ctx: Context | None = Non
 def lr_ckpt8_grad(q, s, dz, grad_w=None, grad_b=None, accumulate=False, ctx: Context | None = None):
     """Gradient of a C-class logistic layer from rows kept in 8 bits (see ``Context.ckpt8_grad``)."""
     return _ctx_of(q, ctx).ckpt8_grad(q, s, dz, grad_w, grad_b, accumulate)
+
+
+def lr_logp(logits, targets, scale=1.0, ignore_id=-100, ctx: Context | None = None):
+    """Log-probabilities of targets (see ``Context.logp``)."""
+    return _ctx_of(logits, ctx).logp(logits, targets, scale, ignore_id)
+
+
+def lr_logp_grad(logits, targets, lse, dlogp, scale=1.0, ignore_id=-100, out=None, ctx: Context | None = None):
+    """Gradient of log-probabilities back to the logits (see ``Context.logp_grad``)."""
+    return _ctx_of(logits, ctx).logp_grad(logits, targets, lse, dlogp, scale, ignore_id, out)
+
+
+def lr_policy_loss(logits, targets, advantages, old_logp=None, ref_logp=None, weights=None, scale=1.0, clip_low=0.2, clip_high=0.2, kl_coef=0.0,
+                   norm=None, factor=1.0, ignore_id=-100, grad=True, out=None, ctx: Context | None = None):
+    """Clipped policy loss with its gradient (see ``Context.policy_loss``)."""
+    return _ctx_of(logits, ctx).policy_loss(logits, targets, advantages, old_logp, ref_logp, weights, scale, clip_low, clip_high, kl_coef, norm,
+                                            factor, ignore_id, grad, out)
+
+
+def lr_pref_loss(logits, targets, offsets, ref_logp=None, weights=None, beta=0.1, margin=0.0, smoothing=0.0, average=False, scale=1.0, norm=None,
+                 factor=1.0, ignore_id=-100, grad=True, out=None, ctx: Context | None = None):
+    """Preference loss of pairs of sequences with its gradient (see ``Context.pref_loss``)."""
+    return _ctx_of(logits, ctx).pref_loss(logits, targets, offsets, ref_logp, weights, beta, margin, smoothing, average, scale, norm, factor,
+                                          ignore_id, grad, out)
+
+
+def lr_distill_loss(logits, ids, teacher, teacher_lse=None, weights=None, scale=1.0, norm=None, factor=1.0, ignore_id=-1, grad=True, out=None,
+                    ctx: Context | None = None):
+    """Divergence from a teacher's top logits with its gradient (see ``Context.distill_loss``)."""
+    return _ctx_of(logits, ctx).distill_loss(logits, ids, teacher, teacher_lse, weights, scale, norm, factor, ignore_id, grad, out)
 
 
 LR_NOALLOC_MAX_N = 1022

@@ -8,7 +8,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "liblrgd.so")
-SOURCES = ["lrgd_api.cu", "lrgd_gate_api.cu"]
+SOURCES = ["lrgd_api.cu", "lrgd_gate_api.cu", "lrgd_class_api.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

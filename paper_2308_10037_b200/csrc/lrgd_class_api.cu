@@ -1,0 +1,405 @@
+// C-ABI layer of the losses over a vocabulary's classes: log-probabilities and their gradient, the clipped policy loss, the preference
+// loss and distillation from a teacher's top logits.  The declarations and their contracts are in include/lrgd.h.
+#include "../../include/lrgd.h"
+
+#include <cmath>
+
+#include "lrgd_class.cuh"
+#include "lrgd_scratch.cuh"
+
+using namespace lrgd;
+
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
+constexpr int64_t kMaxClasses = int64_t(1) << 24;
+constexpr int64_t kMaxPitch = int64_t(1) << 40;
+constexpr int64_t kMaxPairs = int64_t(1) << 24;
+
+size_t up256(size_t b) { return (b + 255) / 256 * 256; }
+
+int check_rows(int64_t T, int32_t V, int64_t ld, int32_t id_bytes, float scale) {
+    if (T < 0 || T > kMaxRows || V < 1 || V > kMaxClasses || ld < V || ld > kMaxPitch) return LR_ERR_SHAPE;
+    if (id_bytes != 4 && id_bytes != 8) return LR_ERR_VALUE;
+    if (!std::isfinite(scale) || !(scale > 0.0f)) return LR_ERR_VALUE;
+    return LR_OK;
+}
+bool norm_ok(float norm, float factor) { return std::isfinite(norm) && norm >= 0.0f && std::isfinite(factor); }
+
+// Gradient rows either are the logits' own (the same address and ld) or share no element with them.
+template <class E>
+bool apart(const E* x, int64_t ld, const E* dx, int64_t ld_d, int64_t T, int64_t V) {
+    if (T == 0) return true;
+    if (x == dx) return ld == ld_d || T == 1;
+    const intptr_t a = reinterpret_cast<intptr_t>(x), b = reinterpret_cast<intptr_t>(dx), es = sizeof(E);
+    const intptr_t a_end = a + ((T - 1) * ld + V) * es, b_end = b + ((T - 1) * ld_d + V) * es;
+    if (a_end <= b || b_end <= a) return true;
+    if (ld != ld_d) return false;
+    const intptr_t pitch = ld * es, off = ((b - a) % pitch + pitch) % pitch;                // columns of one wider matrix
+    return off >= V * es && off + V * es <= pitch;
+}
+
+int class_threads(int V, size_t es) {
+    const int64_t groups = int64_t(V) * int64_t(es) / 16;
+    return 32 * int(std::max<int64_t>(2, std::min<int64_t>(kClassThreads / 32, (groups + 127) / 128)));
+}
+
+template <int MODE>
+int norm_parts(lr_ctx* ctx, ClassParams& p, double* part, cudaStream_t st) {
+    if (p.norm != 0.0) return LR_OK;
+    p.norm_part = part;
+    p.norm_parts = int((p.T + kNormRows - 1) / kNormRows);
+    return launched(ctx, [&] { k_class_norm<MODE><<<p.norm_parts, kNormThreads, 0, st>>>(p, part); });
+}
+
+// Rows in chunks of at least about 64 KB, each with sums of its own
+template <class E>
+void cut_rows(ClassParams& p) {
+    const int64_t row = int64_t(p.V) * int64_t(sizeof(E));
+    p.chunk_rows = std::max<int64_t>(1, std::max<int64_t>((64 << 10) / row, (p.T + kClassChunks - 1) / kClassChunks));
+    p.chunks = int((p.T + p.chunk_rows - 1) / p.chunk_rows);
+}
+
+template <class E, int MODE>
+int launch_rows(lr_ctx* ctx, ClassParams& p, bool grad, bool dependent, cudaStream_t st) {
+    const int threads = class_threads(p.V, sizeof(E));
+    const size_t smem = MODE == kClassDistill ? sizeof(ClassTop) : 0;
+    const dim3 grid(grid_for(ctx, p.chunks, 1, 2048 / threads));
+    auto go = [&](auto kern) -> int {
+        LR_CK(ctx, launch_kernel(kern, grid, dim3(threads), smem, st, dependent && ctx->overlap, p));
+        ctx->launches += 1;
+        return LR_OK;
+    };
+    if constexpr (MODE != kClassLogp) {
+        if (grad) return go(k_class_rows<E, MODE, true>);
+    }
+    return go(k_class_rows<E, MODE, false>);
+}
+
+template <class E>
+ClassParams row_params(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_ids, int32_t id_bytes, int64_t ignore,
+                       float scale) {
+    ClassParams p{};
+    p.x = d_logits;
+    p.ld = ld;
+    p.T = T;
+    p.V = V;
+    p.ids = d_ids;
+    p.wide_ids = id_bytes == 8;
+    p.ignore = ignore;
+    p.scale = scale;
+    p.c = float(double(scale) * 1.4426950408889634074);
+    p.status = ctx->d_status + 1;
+    cut_rows<E>(p);
+    return p;
+}
+
+template <class E>
+int launch_grad(lr_ctx* ctx, ClassGradParams& p, bool dependent, cudaStream_t st) {
+    const int64_t groups = int64_t(p.V) * int64_t(sizeof(E)) / 16 + 1;
+    p.slice_groups = kClassGradThreads * 8;
+    p.slices = int((groups + p.slice_groups - 1) / p.slice_groups);
+    const int threads = int(std::max<int64_t>(32, std::min<int64_t>(kClassGradThreads, (groups + 31) / 32 * 32)));
+    LR_CK(ctx, launch_kernel(k_class_grad<E>, dim3(grid_for(ctx, p.T * p.slices, 1, 2048 / threads)), dim3(threads), 0, st, dependent && ctx->overlap, p));
+    ctx->launches += 1;
+    return LR_OK;
+}
+
+template <class E>
+int logp_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes, int64_t ignore_id,
+              float scale, float* d_logp, float* d_lse, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_rows(T, V, ld, id_bytes, scale);
+    if (rc != LR_OK) return rc;
+    if (T == 0) return LR_OK;
+    if (!d_logits || !d_targets || !d_logp) return LR_ERR_NULL;
+    if (!aligned(d_logits, sizeof(E)) || !aligned(d_targets, id_bytes) || !aligned(d_logp, 4) || !aligned(d_lse, 4)) return LR_ERR_ALIGNMENT;
+    NvtxRange range("lr_logp");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    ClassParams p = row_params(ctx, d_logits, ld, T, V, d_targets, id_bytes, ignore_id, scale);
+    p.logp = d_logp;
+    p.lse = d_lse;
+    return launch_rows<E, kClassLogp>(ctx, p, false, false, static_cast<cudaStream_t>(stream));
+}
+
+template <class E>
+int logp_grad_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes, int64_t ignore_id,
+                   float scale, const float* d_lse, const float* d_dlogp, E* d_dlogits, int64_t ld_d, void* stream) {
+    if (!ctx) return LR_ERR_NULL;
+    const int rc = check_rows(T, V, ld, id_bytes, scale);
+    if (rc != LR_OK) return rc;
+    if (ld_d < V || ld_d > kMaxPitch) return LR_ERR_SHAPE;
+    if (T == 0) return LR_OK;
+    if (!d_logits || !d_targets || !d_lse || !d_dlogp || !d_dlogits) return LR_ERR_NULL;
+    if (!aligned(d_logits, sizeof(E)) || !aligned(d_targets, id_bytes) || !aligned(d_lse, 4) || !aligned(d_dlogp, 4) || !aligned(d_dlogits, sizeof(E)))
+        return LR_ERR_ALIGNMENT;
+    if (!apart(d_logits, ld, d_dlogits, ld_d, T, V)) return LR_ERR_VALUE;
+    NvtxRange range("lr_logp_grad");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    ClassGradParams p{};
+    p.x = d_logits;
+    p.ld = ld;
+    p.T = T;
+    p.V = V;
+    p.ids = d_targets;
+    p.wide_ids = id_bytes == 8;
+    p.ignore = ignore_id;
+    p.scale = scale;
+    p.c = float(double(scale) * 1.4426950408889634074);
+    p.lse = d_lse;
+    p.g = d_dlogp;
+    p.dx = d_dlogits;
+    p.ld_d = ld_d;
+    p.status = ctx->d_status + 1;
+    return launch_grad<E>(ctx, p, false, static_cast<cudaStream_t>(stream));
+}
+
+template <class E>
+int policy_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                const lr_policy_opt* opt, const float* d_advantages, const float* d_old_logp, const float* d_ref_logp, const float* d_weights,
+                float* d_stats, float* d_logp, E* d_dlogits, int64_t ld_d, void* stream) {
+    if (!ctx || !opt) return LR_ERR_NULL;
+    const int rc = check_rows(T, V, ld, id_bytes, opt->scale);
+    if (rc != LR_OK) return rc;
+    if (d_dlogits && (ld_d < V || ld_d > kMaxPitch)) return LR_ERR_SHAPE;
+    if (!(opt->clip_low >= 0.0f) || !(opt->clip_high >= 0.0f) || !std::isfinite(opt->kl_coef) || !norm_ok(opt->norm, opt->factor)) return LR_ERR_VALUE;
+    if (!d_stats || (T > 0 && (!d_logits || !d_targets || !d_advantages))) return LR_ERR_NULL;
+    if (!aligned(d_logits, sizeof(E)) || !aligned(d_targets, id_bytes) || !aligned(d_advantages, 4) || !aligned(d_old_logp, 4) ||
+        !aligned(d_ref_logp, 4) || !aligned(d_weights, 4) || !aligned(d_stats, 4) || !aligned(d_logp, 4) || !aligned(d_dlogits, sizeof(E)))
+        return LR_ERR_ALIGNMENT;
+    if (d_dlogits && !apart(d_logits, ld, d_dlogits, ld_d, T, V)) return LR_ERR_VALUE;
+    NvtxRange range("lr_policy_loss");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        LR_CK(ctx, cudaMemsetAsync(d_stats, 0, 4 * sizeof(float), st));
+        return LR_OK;
+    }
+    ClassParams p = row_params(ctx, d_logits, ld, T, V, d_targets, id_bytes, opt->ignore_id, opt->scale);
+    p.weights = d_weights;
+    p.dx = d_dlogits;
+    p.ld_d = ld_d;
+    p.logp = d_logp;
+    p.adv = d_advantages;
+    p.old_logp = d_old_logp;
+    p.ref_logp = d_ref_logp;
+    p.ratio_low = 1.0 - double(opt->clip_low);
+    p.ratio_high = 1.0 + double(opt->clip_high);
+    p.kl_coef = opt->kl_coef;
+    p.norm = opt->norm;
+    p.factor = opt->factor;
+    p.out = d_stats;
+    const size_t sums = up256(size_t(p.chunks) * 3 * sizeof(double)), parts = up256(size_t(T / kNormRows + 1) * sizeof(double));
+    Scratch scratch{};
+    const int rs = gate_scratch(ctx, sums + parts, st, &scratch);
+    if (rs != LR_OK) return rs;
+    p.chunk_sum = reinterpret_cast<double*>(scratch.data);
+    p.words = scratch.words;
+    const int rn = norm_parts<kClassPolicy>(ctx, p, reinterpret_cast<double*>(scratch.data + sums), st);
+    if (rn != LR_OK) return rn;
+    return launch_rows<E, kClassPolicy>(ctx, p, d_dlogits != nullptr, p.norm == 0.0, st);
+}
+
+template <class E>
+int distill_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_ids, int32_t id_bytes, int32_t K,
+                 const void* d_teacher, int32_t teacher_bytes, const lr_distill_opt* opt, const float* d_teacher_lse, const float* d_weights,
+                 float* d_loss, float* d_row_kl, E* d_dlogits, int64_t ld_d, void* stream) {
+    if (!ctx || !opt) return LR_ERR_NULL;
+    const int rc = check_rows(T, V, ld, id_bytes, opt->scale);
+    if (rc != LR_OK) return rc;
+    if (K < 1 || K > kClassMaxTop || (d_dlogits && (ld_d < V || ld_d > kMaxPitch))) return LR_ERR_SHAPE;
+    if ((teacher_bytes != 2 && teacher_bytes != 4) || !norm_ok(opt->norm, opt->factor)) return LR_ERR_VALUE;
+    if (!d_loss || (T > 0 && (!d_logits || !d_ids || !d_teacher))) return LR_ERR_NULL;
+    if (!aligned(d_logits, sizeof(E)) || !aligned(d_ids, id_bytes) || !aligned(d_teacher, teacher_bytes) || !aligned(d_teacher_lse, 4) ||
+        !aligned(d_weights, 4) || !aligned(d_loss, 4) || !aligned(d_row_kl, 4) || !aligned(d_dlogits, sizeof(E)))
+        return LR_ERR_ALIGNMENT;
+    if (d_dlogits && !apart(d_logits, ld, d_dlogits, ld_d, T, V)) return LR_ERR_VALUE;
+    NvtxRange range("lr_distill_loss");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        LR_CK(ctx, cudaMemsetAsync(d_loss, 0, sizeof(float), st));
+        return LR_OK;
+    }
+    ClassParams p = row_params(ctx, d_logits, ld, T, V, d_ids, id_bytes, opt->ignore_id, opt->scale);
+    p.weights = d_weights;
+    p.dx = d_dlogits;
+    p.ld_d = ld_d;
+    p.teacher = d_teacher;
+    p.teacher_half = teacher_bytes == 2;
+    p.K = K;
+    p.teacher_lse = d_teacher_lse;
+    p.row_kl = d_row_kl;
+    p.norm = opt->norm;
+    p.factor = opt->factor;
+    p.out = d_loss;
+    if (p.norm == 0.0 && !d_weights) p.norm = double(T);
+    const size_t sums = up256(size_t(p.chunks) * 3 * sizeof(double)), parts = up256(size_t(T / kNormRows + 1) * sizeof(double));
+    Scratch scratch{};
+    const int rs = gate_scratch(ctx, sums + parts, st, &scratch);
+    if (rs != LR_OK) return rs;
+    p.chunk_sum = reinterpret_cast<double*>(scratch.data);
+    p.words = scratch.words;
+    const int rn = norm_parts<kClassDistill>(ctx, p, reinterpret_cast<double*>(scratch.data + sums), st);
+    if (rn != LR_OK) return rn;
+    return launch_rows<E, kClassDistill>(ctx, p, d_dlogits != nullptr, p.norm == 0.0, st);
+}
+
+template <class E>
+int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes, const void* d_offsets,
+              int32_t offset_bytes, int64_t pairs, const lr_pref_opt* opt, const float* d_ref_logp, const float* d_weights, float* d_loss,
+              float* d_margins, float* d_seq_logp, E* d_dlogits, int64_t ld_d, void* stream) {
+    if (!ctx || !opt) return LR_ERR_NULL;
+    const int rc = check_rows(T, V, ld, id_bytes, opt->scale);
+    if (rc != LR_OK) return rc;
+    if (pairs < 0 || pairs > kMaxPairs || (d_dlogits && (ld_d < V || ld_d > kMaxPitch))) return LR_ERR_SHAPE;
+    if ((offset_bytes != 4 && offset_bytes != 8) || !std::isfinite(opt->beta) || !std::isfinite(opt->margin) ||
+        !(opt->smoothing >= 0.0f && opt->smoothing <= 1.0f) || !norm_ok(opt->norm, opt->factor))
+        return LR_ERR_VALUE;
+    if (!d_loss || (T > 0 && (!d_logits || !d_targets)) || (pairs > 0 && (!d_offsets || !d_margins))) return LR_ERR_NULL;
+    if (!aligned(d_logits, sizeof(E)) || !aligned(d_targets, id_bytes) || !aligned(d_offsets, offset_bytes) || !aligned(d_ref_logp, 4) ||
+        !aligned(d_weights, 4) || !aligned(d_loss, 4) || !aligned(d_margins, 4) || !aligned(d_seq_logp, 4) || !aligned(d_dlogits, sizeof(E)))
+        return LR_ERR_ALIGNMENT;
+    if (d_dlogits && !apart(d_logits, ld, d_dlogits, ld_d, T, V)) return LR_ERR_VALUE;
+    NvtxRange range("lr_pref_loss");
+    const std::lock_guard<std::mutex> one_call(ctx->gate_mu);
+    DeviceGuard g(ctx);
+    if (!g.ok) return LR_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (pairs == 0) {                               // no pair: nothing counts
+        LR_CK(ctx, cudaMemsetAsync(d_loss, 0, sizeof(float), st));
+        if (d_dlogits && T > 0) LR_CK(ctx, cudaMemset2DAsync(d_dlogits, size_t(ld_d) * sizeof(E), 0, size_t(V) * sizeof(E), size_t(T), st));
+        return LR_OK;
+    }
+    const size_t stat = up256(size_t(T) * sizeof(float2)), lp = up256(size_t(T) * 8), coef = up256(size_t(T) * 4), loss = up256(size_t(pairs) * 8);
+    Scratch scratch{};
+    const int rs = gate_scratch(ctx, stat + lp + coef + loss, st, &scratch);
+    if (rs != LR_OK) return rs;
+    ClassPairParams q{};
+    if (T > 0) {
+        ClassParams p = row_params(ctx, d_logits, ld, T, V, d_targets, id_bytes, opt->ignore_id, opt->scale);
+        p.stat = reinterpret_cast<float2*>(scratch.data);
+        p.logp64 = reinterpret_cast<double*>(scratch.data + stat);
+        p.coef = reinterpret_cast<float*>(scratch.data + stat + lp);
+        p.offsets = d_offsets;
+        p.wide_offsets = offset_bytes == 8;
+        p.offset_count = 2 * pairs;
+        const int r = launch_rows<E, kClassLogp>(ctx, p, false, false, st);
+        if (r != LR_OK) return r;
+    }
+    q.ids = d_targets;
+    q.wide_ids = id_bytes == 8;
+    q.ignore = opt->ignore_id;
+    q.V = V;
+    q.T = T;
+    q.offsets = d_offsets;
+    q.wide_offsets = offset_bytes == 8;
+    q.P = pairs;
+    q.ref = d_ref_logp;
+    q.weights = d_weights;
+    q.beta = opt->beta;
+    q.margin = opt->margin;
+    q.smoothing = opt->smoothing;
+    q.norm = opt->norm;
+    q.factor = opt->factor;
+    q.average = opt->average != 0;
+    q.logp64 = reinterpret_cast<const double*>(scratch.data + stat);
+    q.coef = reinterpret_cast<float*>(scratch.data + stat + lp);
+    q.loss = d_loss;
+    q.h = d_margins;
+    q.seq_logp = d_seq_logp;
+    q.pair_loss = reinterpret_cast<double*>(scratch.data + stat + lp + coef);
+    q.words = scratch.words;
+    q.status = ctx->d_status + 1;
+    LR_CK(ctx, launch_kernel(k_class_pair, dim3(grid_for(ctx, pairs, 1, 8)), dim3(kPairThreads), 0, st, ctx->overlap && T > 0, q));
+    ctx->launches += 1;
+    if (!d_dlogits || T == 0) return LR_OK;
+    ClassGradParams d{};
+    d.x = d_logits;
+    d.ld = ld;
+    d.T = T;
+    d.V = V;
+    d.ids = d_targets;
+    d.wide_ids = id_bytes == 8;
+    d.ignore = opt->ignore_id;
+    d.scale = opt->scale;
+    d.c = float(double(opt->scale) * 1.4426950408889634074);
+    d.stat = reinterpret_cast<const float2*>(scratch.data);
+    d.g = q.coef;
+    d.dx = d_dlogits;
+    d.ld_d = ld_d;
+    d.backwards = 1;
+    return launch_grad<E>(ctx, d, true, st);
+}
+
+// bfloat16 is the unsigned 16-bit pattern of the interface
+using u16 = unsigned short;
+const u16* bf(const uint16_t* p) { return reinterpret_cast<const u16*>(p); }
+u16* bf(uint16_t* p) { return reinterpret_cast<u16*>(p); }
+
+}  // namespace
+
+extern "C" {
+
+int lr_logp(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes, int64_t ignore_id,
+            float scale, float* d_logp, float* d_lse, void* stream) {
+    return logp_impl<float>(ctx, d_logits, ld, T, V, d_targets, id_bytes, ignore_id, scale, d_logp, d_lse, stream);
+}
+int lr_logp_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                 int64_t ignore_id, float scale, float* d_logp, float* d_lse, void* stream) {
+    return logp_impl<u16>(ctx, bf(d_logits), ld, T, V, d_targets, id_bytes, ignore_id, scale, d_logp, d_lse, stream);
+}
+int lr_logp_grad(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                 int64_t ignore_id, float scale, const float* d_lse, const float* d_dlogp, float* d_dlogits, int64_t ld_d, void* stream) {
+    return logp_grad_impl<float>(ctx, d_logits, ld, T, V, d_targets, id_bytes, ignore_id, scale, d_lse, d_dlogp, d_dlogits, ld_d, stream);
+}
+int lr_logp_grad_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                      int64_t ignore_id, float scale, const float* d_lse, const float* d_dlogp, uint16_t* d_dlogits, int64_t ld_d, void* stream) {
+    return logp_grad_impl<u16>(ctx, bf(d_logits), ld, T, V, d_targets, id_bytes, ignore_id, scale, d_lse, d_dlogp, bf(d_dlogits), ld_d, stream);
+}
+int lr_policy_loss(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                   const lr_policy_opt* opt, const float* d_advantages, const float* d_old_logp, const float* d_ref_logp,
+                   const float* d_weights, float* d_stats, float* d_logp, float* d_dlogits, int64_t ld_d, void* stream) {
+    return policy_impl<float>(ctx, d_logits, ld, T, V, d_targets, id_bytes, opt, d_advantages, d_old_logp, d_ref_logp, d_weights, d_stats, d_logp,
+                              d_dlogits, ld_d, stream);
+}
+int lr_policy_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                        const lr_policy_opt* opt, const float* d_advantages, const float* d_old_logp, const float* d_ref_logp,
+                        const float* d_weights, float* d_stats, float* d_logp, uint16_t* d_dlogits, int64_t ld_d, void* stream) {
+    return policy_impl<u16>(ctx, bf(d_logits), ld, T, V, d_targets, id_bytes, opt, d_advantages, d_old_logp, d_ref_logp, d_weights, d_stats, d_logp,
+                            bf(d_dlogits), ld_d, stream);
+}
+int lr_pref_loss(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                 const void* d_offsets, int32_t offset_bytes, int64_t pairs, const lr_pref_opt* opt, const float* d_ref_logp,
+                 const float* d_weights, float* d_loss, float* d_margins, float* d_seq_logp, float* d_dlogits, int64_t ld_d, void* stream) {
+    return pref_impl<float>(ctx, d_logits, ld, T, V, d_targets, id_bytes, d_offsets, offset_bytes, pairs, opt, d_ref_logp, d_weights, d_loss,
+                            d_margins, d_seq_logp, d_dlogits, ld_d, stream);
+}
+int lr_pref_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_targets, int32_t id_bytes,
+                      const void* d_offsets, int32_t offset_bytes, int64_t pairs, const lr_pref_opt* opt, const float* d_ref_logp,
+                      const float* d_weights, float* d_loss, float* d_margins, float* d_seq_logp, uint16_t* d_dlogits, int64_t ld_d, void* stream) {
+    return pref_impl<u16>(ctx, bf(d_logits), ld, T, V, d_targets, id_bytes, d_offsets, offset_bytes, pairs, opt, d_ref_logp, d_weights, d_loss,
+                          d_margins, d_seq_logp, bf(d_dlogits), ld_d, stream);
+}
+int lr_distill_loss(lr_ctx* ctx, const float* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_ids, int32_t id_bytes, int32_t K,
+                    const void* d_teacher, int32_t teacher_bytes, const lr_distill_opt* opt, const float* d_teacher_lse, const float* d_weights,
+                    float* d_loss, float* d_row_kl, float* d_dlogits, int64_t ld_d, void* stream) {
+    return distill_impl<float>(ctx, d_logits, ld, T, V, d_ids, id_bytes, K, d_teacher, teacher_bytes, opt, d_teacher_lse, d_weights, d_loss,
+                               d_row_kl, d_dlogits, ld_d, stream);
+}
+int lr_distill_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t T, int32_t V, const void* d_ids, int32_t id_bytes, int32_t K,
+                         const void* d_teacher, int32_t teacher_bytes, const lr_distill_opt* opt, const float* d_teacher_lse,
+                         const float* d_weights, float* d_loss, float* d_row_kl, uint16_t* d_dlogits, int64_t ld_d, void* stream) {
+    return distill_impl<u16>(ctx, bf(d_logits), ld, T, V, d_ids, id_bytes, K, d_teacher, teacher_bytes, opt, d_teacher_lse, d_weights, d_loss,
+                             d_row_kl, bf(d_dlogits), ld_d, stream);
+}
+
+}  // extern "C"
