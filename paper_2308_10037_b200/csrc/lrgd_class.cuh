@@ -17,9 +17,7 @@
 
 namespace lrgd {
 
-constexpr int kClassThreads = 512;
 constexpr int kClassMaxTop = 1024;                  // classes of a teacher per row, at most
-constexpr int kClassChunks = 8192;                  // pieces of work with a sum of their own, at most
 constexpr double kLn2 = 0.693147180559945309417232121458;
 
 enum ClassMode { kClassLogp = 0, kClassPolicy = 1, kClassDistill = 2 };
@@ -44,7 +42,7 @@ struct ClassParams {
     // what the preference loss keeps of a row: m and s, lp in fp64; rows outside [offsets[0], offsets[count]) do not count
     float2* stat;
     double* logp64;
-    float* coef;
+    float* coef;                 // set to 0
     const void* offsets;
     int wide_offsets;
     long long offset_count;
@@ -60,13 +58,15 @@ struct ClassParams {
     const float* teacher_lse;
     float* row_kl;
     // sums
-    double norm;                 // 0: the sum of the weights of the rows that count, from norm_part
+    double norm;                 // 0: the sum of the weights of the rows that count
     double factor;
-    const double* norm_part;
-    int norm_parts;
-    long long chunk_rows;
-    int chunks;
-    double* chunk_sum;           // [chunks][3]
+    // rows and their CTAs
+    const int* order;            // the rows that count, then the others (k_class_prep); NULL: all rows, looked at one by one
+    const struct ClassPrep* prep;
+    int cluster;                 // CTAs per row
+    int depth;                   // stages in a warp's ring
+    double* cta_sum;             // [CTAs][3]
+    int* timeout;                // status word of waits
     unsigned int* words;         // [0] CTAs that are done
     float* out;                  // [4] policy, [1] distillation
 };
@@ -80,32 +80,70 @@ __device__ __forceinline__ float exp2_fast(float v) {               // 2^v, rela
     return r;
 }
 
+// Two fp32 values in one 64-bit register (see f32x2_fma)
+__device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t f32x2_mul(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+// 2^(x * c - m) of both halves
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x, uint64_t c, uint64_t minus_m) {
+    float lo, hi;
+    f32x2_unpack(f32x2_fma(x, c, minus_m), lo, hi);
+    return f32x2_pack(exp2_fast(lo), exp2_fast(hi));
+}
+
 // 16 bytes of a row
 template <class E>
 struct ClassGroup {
     static constexpr int N = 16 / int(sizeof(E));
-    static __device__ __forceinline__ void widen(const uint4& w, float (&v)[N]) {
-        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(E) == 4) {
-                v[i] = __uint_as_float(u[i]);
-            } else {
-                v[2 * i] = __uint_as_float(u[i] << 16);
-                v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-            }
-        }
+    static constexpr int P = N / 2;
+    static __device__ __forceinline__ uint32_t word(const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
+    // elements 2 i and 2 i + 1
+    static __device__ __forceinline__ uint64_t pair(const uint4& w, int i) {
+        if constexpr (sizeof(E) == 4) return f32x2_pack(__uint_as_float(word(w, 2 * i)), __uint_as_float(word(w, 2 * i + 1)));
+        else return f32x2_pack(__uint_as_float(word(w, i) << 16), __uint_as_float(word(w, i) & 0xffff0000u));
     }
-    static __device__ __forceinline__ uint4 narrow(const float (&v)[N]) {
+    static __device__ __forceinline__ uint4 narrow(const uint64_t (&v)[P]) {
         uint32_t u[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(E) == 4) u[i] = __float_as_uint(v[i]);
-            else asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
+        for (int i = 0; i < P; ++i) {
+            float lo, hi;
+            f32x2_unpack(v[i], lo, hi);
+            if constexpr (sizeof(E) == 4) {
+                u[2 * i] = __float_as_uint(lo);
+                u[2 * i + 1] = __float_as_uint(hi);
+            } else {
+                asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u[i]) : "f"(hi), "f"(lo));
+            }
         }
         return make_uint4(u[0], u[1], u[2], u[3]);
     }
+    // the largest of J groups, NaN left out
+    template <int J>
+    static __device__ __forceinline__ float largest(const uint4 (&raw)[J]) {
+        if constexpr (sizeof(E) == 4) {
+            float t = __uint_as_float(raw[0].x);
+#pragma unroll
+            for (int i = 1; i < 4 * J; ++i) t = fmaxf(t, __uint_as_float(word(raw[i / 4], i % 4)));
+            return t;
+        } else {
+            uint32_t t = raw[0].x;
+#pragma unroll
+            for (int i = 1; i < 4 * J; ++i) asm("max.bf16x2 %0, %1, %2;" : "=r"(t) : "r"(t), "r"(word(raw[i / 4], i % 4)));
+            return fmaxf(__uint_as_float(t << 16), __uint_as_float(t & 0xffff0000u));
+        }
+    }
 };
+
+__device__ __forceinline__ void store_streaming(void* at, const uint4& v) {
+    asm volatile("st.global.cs.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 
 // A row as `head` elements, `groups` groups of 16 bytes that start on 16 bytes, and a tail
 template <class E>
@@ -127,14 +165,19 @@ struct ClassRow {
     // element e of those outside the groups
     __device__ __forceinline__ int edge(int e) const { return e < head ? e : e + groups * ClassGroup<E>::N; }
     __device__ __forceinline__ uint4 load(int g) const { return *reinterpret_cast<const uint4*>(x + head + g * ClassGroup<E>::N); }
-    __device__ __forceinline__ void store(int g, const float (&v)[ClassGroup<E>::N]) const {
+    __device__ __forceinline__ void store(int g, const uint64_t (&v)[ClassGroup<E>::P]) const {
         constexpr int N = ClassGroup<E>::N;
         E* at = dx + head + g * N;
         if (wide_store) {
-            *reinterpret_cast<uint4*>(at) = ClassGroup<E>::narrow(v);
+            store_streaming(at, ClassGroup<E>::narrow(v));
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) store_from_float(at + i, v[i]);
+            for (int i = 0; i < N / 2; ++i) {
+                float lo, hi;
+                f32x2_unpack(v[i], lo, hi);
+                store_from_float(at + 2 * i, lo);
+                store_from_float(at + 2 * i + 1, hi);
+            }
         }
     }
 };
@@ -142,31 +185,43 @@ struct ClassRow {
 // The running maximum and sum of a part of a row: s = sum of 2^(fma(x, c, -m)), m = fl(c * largest), m = -inf before the first finite x
 struct ClassSum {
     float top = -INFINITY, m = -INFINITY, s = 0.0f;
-    template <int N>
-    __device__ __forceinline__ void add(const float (&v)[N], float c) {
-        float t = top;
-#pragma unroll
-        for (int i = 0; i < N; ++i) t = fmaxf(t, v[i]);
+    // room for terms up to t; false where nothing finite has come yet
+    __device__ __forceinline__ bool raise(float t, float c) {
         if (t > top) {
             const float next = t * c;
             s *= exp2_fast(m - next);
             top = t;
             m = next;
         }
-        if (t == -INFINITY) {                       // nothing finite yet; a NaN has to be seen all the same
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (v[i] != v[i]) s = v[i];
-            return;
-        }
-        float part = 0.0f;
-#pragma unroll
-        for (int i = 0; i < N; ++i) part += exp2_fast(fmaf(v[i], c, -m));
-        s += part;
+        return top != -INFINITY;
     }
     __device__ __forceinline__ void add(float v, float c) {
-        const float one[1] = {v};
-        add(one, c);
+        if (raise(v, c)) s += exp2_fast(fmaf(v, c, -m));
+        else if (v != v) s = v;
+    }
+    template <class E, int J>
+    __device__ __forceinline__ void add_groups(const uint4 (&raw)[J], float c) {
+        using G = ClassGroup<E>;
+        if (!raise(G::template largest<J>(raw), c)) {               // a NaN has to be seen all the same
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < G::P; ++i) {
+                    float lo, hi;
+                    f32x2_unpack(G::pair(raw[j], i), lo, hi);
+                    if (lo != lo || hi != hi) s = NAN;
+                }
+            return;
+        }
+        const uint64_t c2 = f32x2_pack(c, c), m2 = f32x2_pack(-m, -m);
+        uint64_t part = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int i = 0; i < G::P; ++i) part = f32x2_add(part, exp2_pair(G::pair(raw[j], i), c2, m2));
+        float lo, hi;
+        f32x2_unpack(part, lo, hi);
+        s += lo + hi;
     }
     __device__ __forceinline__ void join(float top2, float m2, float s2) {
         if (top2 > top) {
@@ -196,7 +251,6 @@ __device__ __forceinline__ void class_sum_cta(ClassSum& a, float (*slot)[3]) {
     __syncthreads();
     a = ClassSum{};
     for (int w = 0; w < warps; ++w) a.join(slot[w][0], slot[w][1], slot[w][2]);
-    if (a.top == -INFINITY) a.m = 0.0f;             // no finite logit: s is 0 (or NaN)
 }
 
 // Whether a row counts, with its target and weight
@@ -215,43 +269,10 @@ __device__ __forceinline__ bool class_counts(const ClassParams& p, long long t, 
     return live;
 }
 
-constexpr int kNormThreads = 256;
-constexpr int kNormRows = 4096;                     // rows of a part
-
 __device__ __forceinline__ double warp_sum64(double v) {
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
-}
-
-// norm_part[b] = sum of the weights of rows that count among rows b * kNormRows ...
-template <int MODE>
-__global__ void __launch_bounds__(kNormThreads) k_class_norm(const __grid_constant__ ClassParams p, double* part) {
-    __shared__ double warp_part[kNormThreads / 32];
-    grid_dependency_release();
-    const long long first = static_cast<long long>(blockIdx.x) * kNormRows, last = min(first + kNormRows, p.T);
-    double sum = 0.0;
-    for (long long t = first + threadIdx.x; t < last; t += kNormThreads) {
-        long long target;
-        float w;
-        if (class_counts(p, t, MODE, &target, &w)) sum += w;
-    }
-    sum = warp_sum64(sum);
-    if ((threadIdx.x & 31) == 0) warp_part[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        sum = 0.0;
-        for (int w = 0; w < kNormThreads / 32; ++w) sum += warp_part[w];
-        part[blockIdx.x] = sum;
-    }
-}
-
-// 1 / norm, 0 where nothing counts
-__device__ __forceinline__ double class_inv_norm(const ClassParams& p) {
-    double n = p.norm;
-    if (n == 0.0)
-        for (int i = 0; i < p.norm_parts; ++i) n += __ldcg(p.norm_part + i);
-    return n == 0.0 ? 0.0 : 1.0 / n;
 }
 
 // A row's numbers, from its statistics: lp and, for the gradient, k (what the terms 2^(..) are multiplied by) and at (the value at the target)
@@ -259,7 +280,13 @@ struct ClassNumbers {
     float k, at;
     double sums[3];
 };
-__device__ __forceinline__ double class_lse2(float m, float s) { return static_cast<double>(m) + log2(static_cast<double>(s)); }
+// log2 of the sum.  exp2_fast drops the bits of its argument below 2^-23 or so: terms below 1/2 come out 4.9e-8 too small in the mean
+// (measured over 4 M random arguments; 2.2e-8 between 1/2 and 1, the largest term is exact).  One row's lp does not show that, the sum over a
+// long sequence does; in the gradient it cancels, whose numerator has the same terms.
+__device__ __forceinline__ double class_lse2(float m, float s) {
+    const double sum = s;
+    return static_cast<double>(m) + log2(sum + 4.9e-8 * (sum - 1.0));
+}
 
 // lp of the target whose logit is xy; above 0 it is rounding
 __device__ __forceinline__ double class_logp(const ClassParams& p, float xy, float m, float s) {
@@ -267,10 +294,10 @@ __device__ __forceinline__ double class_logp(const ClassParams& p, float xy, flo
     return lp > 0.0 ? 0.0 : lp;
 }
 
-__device__ __forceinline__ ClassNumbers class_policy_row(const ClassParams& p, long long t, float w, float xy, float m, float s, double inv) {
+__device__ __forceinline__ ClassNumbers class_policy_row(const ClassParams& p, long long t, float w, float xy, float m, float s, double inv, bool write) {
     ClassNumbers r;
     const double lp = class_logp(p, xy, m, s);
-    if (p.logp) p.logp[t] = static_cast<float>(lp);
+    if (p.logp && write) p.logp[t] = static_cast<float>(lp);
     const double a = __ldg(p.adv + t), ratio = p.old_logp ? exp(lp - __ldg(p.old_logp + t)) : 1.0;
     const double held = fmin(fmax(ratio, p.ratio_low), p.ratio_high);
     const bool clipped = ratio * a > held * a;
@@ -289,136 +316,426 @@ __device__ __forceinline__ ClassNumbers class_policy_row(const ClassParams& p, l
     return r;
 }
 
-// The teacher's side of a row, by one warp: top.q (weights of its classes, those of equal classes not yet added up), top.x (the student's
-// logits there), top.id (-1: absent).  Returns Q = sum of q and, per lane, the part of sum q * log2(q) - q * c * x that is its own.
-struct ClassTop {
-    float q[kClassMaxTop];
-    float x[kClassMaxTop];
-    int id[kClassMaxTop];
+// ---- which rows count ----------------------------------------------------------------------------------
+// One CTA writes the numbers of the rows that count into `order`, in their order, those of the others behind them, and sums the weights.
+// Rows that do not count get their zeros here (all but their gradient).  T = 8192: 3 us, beside the start of k_class_rows.
+constexpr int kPrepThreads = 1024;
+constexpr int kPrepItems = 8;
+
+struct ClassPrep {
+    double norm;
+    int live;
 };
-template <class E>
-__device__ __forceinline__ void class_top_load(const ClassParams& p, long long t, const E* row, ClassTop& top, float& largest) {
-    const int lane = threadIdx.x & 31;
-    largest = -INFINITY;
-    for (int k = lane; k < p.K; k += 32) {
-        const long long at = t * p.K + k;
-        long long id = load_any_id(p.ids, p.wide_ids, at);
-        const float v = p.teacher_half ? load_local(static_cast<const unsigned short*>(p.teacher) + at) : static_cast<const float*>(p.teacher)[at];
-        if (id < 0 || id >= p.V) {
-            if (id != p.ignore) atomicExch(p.status, -4);
-            id = -1;
+
+template <int MODE>
+__device__ __forceinline__ void class_dead_row(const ClassParams& p, long long t) {
+    if (MODE == kClassDistill) {
+        if (p.row_kl) p.row_kl[t] = 0.0f;
+    } else {
+        if (p.logp) p.logp[t] = 0.0f;
+        if (MODE == kClassLogp && p.lse) p.lse[t] = 0.0f;
+        if (MODE == kClassLogp && p.logp64) {
+            p.logp64[t] = 0.0;
+            p.coef[t] = 0.0f;
         }
-        if (v == -INFINITY) id = -1;
-        top.id[k] = static_cast<int>(id);
-        top.q[k] = v;
-        top.x[k] = id >= 0 ? load_local(row + id) : 0.0f;
-        if (id >= 0) largest = fmaxf(largest, v);
     }
-    largest = warp_max(largest);
-}
-// After it: top.q holds q
-__device__ __forceinline__ double class_top_weights(const ClassParams& p, long long t, ClassTop& top, float largest, double& cross) {
-    const int lane = threadIdx.x & 31;
-    const double base = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) * (static_cast<double>(p.c) / p.scale)
-                                      : (largest == -INFINITY ? 0.0 : static_cast<double>(largest) * p.c);
-    double sum = 0.0;
-    cross = 0.0;                                    // sum of 2^a (a - c x), a = c v - base
-    for (int k = lane; k < p.K; k += 32) {
-        const bool here = top.id[k] >= 0;
-        const double a = static_cast<double>(top.q[k]) * p.c - base;
-        const double e = here ? exp2(a) : 0.0;
-        sum += e;
-        if (e != 0.0) cross += e * (a - static_cast<double>(top.x[k]) * p.c);
-        top.q[k] = static_cast<float>(e);
-    }
-    sum = warp_sum64(sum);
-    cross = warp_sum64(cross);
-    return sum;
 }
 
-// ---- one CTA per row -----------------------------------------------------------------------------------
-// Bound by HBM: a row is read once for its statistics and, while it is still in L2, once more for the gradient.
-template <class E, int MODE, bool GRAD>
-__global__ void __launch_bounds__(kClassThreads) k_class_rows(const __grid_constant__ ClassParams p) {
-    constexpr int N = ClassGroup<E>::N;
-    __shared__ float slot[2][kClassThreads / 32][3];
-    __shared__ float now[2];
-    __shared__ float top_sum, top_scale;
-    __shared__ bool last_cta;
-    __shared__ double warp_part[kClassThreads / 32][3];
-    extern __shared__ __align__(16) unsigned char class_smem[];
-    ClassTop& top = *reinterpret_cast<ClassTop*>(class_smem);
-    const int tid = threadIdx.x, threads = blockDim.x;
-    grid_dependency_wait();
+template <int MODE>
+__global__ void __launch_bounds__(kPrepThreads) k_class_prep(const __grid_constant__ ClassParams p, int* order, ClassPrep* prep) {
+    __shared__ double warp_norm[kPrepThreads / 32];
+    __shared__ int warp_live[kPrepThreads / 32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    grid_dependency_release();
     long long from = 0, to = p.T;
     if (MODE == kClassLogp && p.offsets) {
         from = load_any_id(p.offsets, p.wide_offsets, 0);
         to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
     }
-    double inv = 0.0;
-    if (MODE != kClassLogp && tid == 0) inv = class_inv_norm(p);
-    int turn = 0;
-    for (int chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
-        double sums[3] = {0.0, 0.0, 0.0};
-        const long long first = chunk * p.chunk_rows, end = min(first + p.chunk_rows, p.T);
-        for (long long t = first; t < end; ++t) {
-            const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
-            long long target;
-            float w;
-            bool live = class_counts(p, t, MODE, &target, &w);
-            if (MODE == kClassLogp) live = live && t >= from && t < to;
-            if (!live) {
-                if (GRAD) {
-                    const float zero[N] = {};
-                    for (int g = tid; g < row.groups; g += threads) row.store(g, zero);
-                    if (tid < row.edges) store_from_float(row.dx + row.edge(tid), 0.0f);
-                }
-                if (tid == 0) {
-                    if (MODE == kClassDistill) {
-                        if (p.row_kl) p.row_kl[t] = 0.0f;
-                    } else if (p.logp) {
-                        p.logp[t] = 0.0f;
-                    }
-                    if (MODE == kClassLogp && p.lse) p.lse[t] = 0.0f;
-                    if (MODE == kClassLogp && p.stat) {
-                        p.stat[t] = make_float2(0.0f, 1.0f);
-                        p.logp64[t] = 0.0;
-                        p.coef[t] = 0.0f;
-                    }
+    double norm = 0.0;
+    int before = 0;                                 // rows that count so far
+    for (long long base = 0; base < p.T; base += kPrepThreads * kPrepItems) {
+        const long long first = base + warp * (32 * kPrepItems) + lane;
+        unsigned int mask[kPrepItems];
+        int mine = 0;
+#pragma unroll
+        for (int j = 0; j < kPrepItems; ++j) {
+            const long long t = first + 32 * j;
+            bool live = false;
+            if (t < p.T) {
+                long long target;
+                float w;
+                live = class_counts(p, t, MODE, &target, &w);
+                if (MODE == kClassLogp) live = live && t >= from && t < to;
+                if (live) norm += w;
+                else class_dead_row<MODE>(p, t);
+            }
+            mask[j] = __ballot_sync(0xffffffffu, live);
+            mine += __popc(mask[j]);
+        }
+        __syncthreads();                            // the last turn's counts have been read
+        if (lane == 0) warp_live[warp] = mine;
+        __syncthreads();
+        int at = before, all = 0;
+        for (int w = 0; w < kPrepThreads / 32; ++w) {
+            const int n = warp_live[w];
+            if (w < warp) at += n;
+            all += n;
+        }
+        before += all;
+#pragma unroll
+        for (int j = 0; j < kPrepItems; ++j) {
+            const long long t = first + 32 * j;
+            const int ahead = at + __popc(mask[j] & ((1u << lane) - 1));
+            // of the rows up to t, t - ahead do not count: they fill `order` from its end
+            if (t < p.T) order[(mask[j] >> lane & 1) ? ahead : p.T - 1 - (t - ahead)] = static_cast<int>(t);
+            at += __popc(mask[j]);
+        }
+    }
+    norm = warp_sum64(norm);
+    if (lane == 0) warp_norm[warp] = norm;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        norm = 0.0;
+        for (int w = 0; w < kPrepThreads / 32; ++w) norm += warp_norm[w];
+        prep->norm = norm;
+        prep->live = before;
+    }
+}
+
+// ---- a teacher's classes -------------------------------------------------------------------------------
+// Entry j of a row belongs to thread j mod (threads of the CTA).  q is 2^(c * v - base of the entry's warp); `part` turns it into the weight.
+struct ClassTop {
+    int* id;                     // [K], -1: absent
+    float* q;                    // [K]
+    float* x;                    // [K] the student's logits
+    int* table;                  // [size] the classes seen so far, -1: free
+    int size;                    // a power of two, at least 2 K
+    double (*warp)[3];           // [warps] base, sum of q, sum of q * (c * v - base - c * x)
+    float* part;                 // [warps]
+    int* twice;                  // [2] some class is named twice
+};
+__host__ __device__ inline int class_table_size(int K) {
+    int n = 64;
+    while (n < 2 * K) n *= 2;
+    return n;
+}
+__host__ __device__ inline size_t class_top_bytes(int K, int warps) {
+    return size_t(K) * 12 + size_t(class_table_size(K)) * 4 + size_t(warps) * 32 + 64;
+}
+__device__ __forceinline__ ClassTop class_top_at(unsigned char* at, int K, int warps) {
+    ClassTop top;
+    top.warp = reinterpret_cast<double(*)[3]>(at);
+    at += warps * 24;
+    top.part = reinterpret_cast<float*>(at);
+    at += warps * 4;
+    top.twice = reinterpret_cast<int*>(at);
+    at += 8;
+    top.size = class_table_size(K);
+    top.table = reinterpret_cast<int*>(at);
+    at += top.size * 4;
+    top.id = reinterpret_cast<int*>(at);
+    top.q = reinterpret_cast<float*>(at + 4 * K);
+    top.x = reinterpret_cast<float*>(at + 8 * K);
+    return top;
+}
+struct ClassEntry {
+    long long id;
+    float v;
+};
+__device__ __forceinline__ ClassEntry class_entry(const ClassParams& p, long long t, int j) {
+    ClassEntry e{0, -INFINITY};
+    if (j < p.K) {
+        const long long at = t * p.K + j;
+        e.id = load_any_id(p.ids, p.wide_ids, at);
+        e.v = p.teacher_half ? __uint_as_float(static_cast<uint32_t>(__ldg(static_cast<const unsigned short*>(p.teacher) + at)) << 16)
+                             : __ldg(static_cast<const float*>(p.teacher) + at);
+    }
+    return e;
+}
+// id in [0, V), or -1 where the entry is absent
+__device__ __forceinline__ int class_entry_id(const ClassParams& p, const ClassEntry& e) {
+    if (e.id < 0 || e.id >= p.V) {
+        if (e.id != p.ignore) atomicExch(p.status, -4);
+        return -1;
+    }
+    return e.v == -INFINITY ? -1 : static_cast<int>(e.id);
+}
+// Writes an entry down; true where its class has been seen in this row
+__device__ __forceinline__ bool class_entry_put(const ClassTop& top, int j, int id, float v, float x) {
+    top.id[j] = id;
+    top.q[j] = v;
+    top.x[j] = x;
+    if (id < 0) return false;
+    unsigned int at = static_cast<unsigned int>(id) * 2654435761u;
+    for (at = (at >> 12) & (top.size - 1);; at = (at + 1) & (top.size - 1)) {       // ends: at most K of 2 K places are taken
+        const int was = atomicCAS(top.table + at, -1, id);
+        if (was == -1) return false;
+        if (was == id) return true;
+    }
+}
+// A warp's share of the row: its entries' q, their sums
+__device__ __forceinline__ void class_top_warp(const ClassParams& p, long long t, const ClassTop& top, float largest) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    largest = warp_max(largest);
+    const double base = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) * (static_cast<double>(p.c) / p.scale)
+                                      : (largest == -INFINITY ? 0.0 : static_cast<double>(largest) * p.c);
+    double sum = 0.0, cross = 0.0;
+    for (int j = threadIdx.x; j < p.K; j += blockDim.x) {
+        const double a = static_cast<double>(top.q[j]) * p.c - base;
+        const double e = top.id[j] >= 0 ? exp2(a) : 0.0;
+        sum += e;
+        if (e != 0.0) cross += e * (a - static_cast<double>(top.x[j]) * p.c);
+        top.q[j] = static_cast<float>(e);
+    }
+    sum = warp_sum64(sum);
+    cross = warp_sum64(cross);
+    if (lane == 0) {
+        top.warp[warp][0] = sum == 0.0 && !p.teacher_lse ? -INFINITY : base;
+        top.warp[warp][1] = sum;
+        top.warp[warp][2] = cross;
+    }
+}
+
+// ---- rows ----------------------------------------------------------------------------------------------
+// One CTA per row, or a cluster of C where there are fewer rows than SMs.  A row's 16-byte groups are dealt out to the warps in stages of
+// 2 KB; every warp brings its own stages into its own ring of shared memory with bulk copies, as far ahead as the ring allows, over the ends of
+// rows too.  First pass: running maximum and sum; one barrier joins the warps (one more the CTAs).  Second pass: the gradient, from the
+// stages that are still in the ring, then from those that were overwritten, which come from L2 again.  A stage is given back when it has been
+// read for the last time, always in the order of the copies, so the ring needs no bookkeeping beyond two counters.
+constexpr int kRingThreads = 512;
+constexpr int kStageGroups = 128;
+constexpr int kStageBytes = kStageGroups * 16;
+constexpr int kMaxCluster = 8;
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_store_f32(const float* local, uint32_t rank, float v) {
+    uint32_t addr;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(local)), "r"(rank));
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+// A warp's stages of a row
+template <class E>
+struct WarpRow {
+    const E* x;                  // first group
+    int groups;
+    int stages;
+    __device__ __forceinline__ void set(const ClassParams& p, long long t, int gw, int tw) {
+        const ClassRow<E> row(p.x, p.ld, nullptr, 0, t, p.V);
+        x = row.x + row.head;
+        groups = row.groups;
+        const int all = (groups + kStageGroups - 1) / kStageGroups;
+        stages = all > gw ? (all - gw + tw - 1) / tw : 0;
+    }
+};
+
+template <class E, int MODE, bool GRAD>
+__global__ void __launch_bounds__(kRingThreads, 2) k_class_rows(const __grid_constant__ ClassParams p) {
+    using G = ClassGroup<E>;
+    constexpr int N = G::N;
+    constexpr int J = kStageGroups / 32;            // groups of a stage per lane
+    __shared__ float slot[2][kRingThreads / 32][3];
+    __shared__ float cta_slot[2][kMaxCluster][4];
+    __shared__ float now[2];
+    __shared__ int abort_word;
+    __shared__ bool last_cta;
+    extern __shared__ __align__(128) unsigned char class_smem[];
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5, depth = p.depth;
+    const int C = p.cluster, rank = C > 1 ? int(cluster_rank()) : 0, q = blockIdx.x / C, Q = gridDim.x / C;
+    const int gw = rank * warps + warp, tw = C * warps;
+    unsigned char* ring = class_smem + size_t(warp) * depth * kStageBytes;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(class_smem + size_t(warps) * depth * kStageBytes) + warp * depth;
+    ClassTop top{};
+    if (MODE == kClassDistill) {
+        top = class_top_at(class_smem + size_t(warps) * depth * (kStageBytes + 8), p.K, warps);
+        for (int i = tid; i < top.size; i += threads) top.table[i] = -1;
+        if (tid < 2) top.twice[tid] = 0;
+    }
+    volatile int* abort_flag = &abort_word;
+    if (tid == 0) abort_word = 0;
+    if (lane == 0) {
+        for (int i = 0; i < depth; ++i) mbar_init(bars + i, 1);
+        fence_mbar_init();
+    }
+    if (C > 1) cluster_barrier();                   // (a CTA that writes into another's shared memory has to find it started)
+    else __syncthreads();
+    grid_dependency_wait();
+    const uint64_t first_use = l2_policy_evict_first();
+    const int live = p.order ? p.prep->live : int(p.T);
+    const int mine = live > q ? (live - q + Q - 1) / Q : 0;
+    // rows of this CTA, 64 of them known ahead: lane i holds the numbers of rows 32 * block + i and 32 * (block + 1) + i
+    int block = 0, order0 = 0, order1 = 0;
+    auto fetch = [&](int b) { const int k = 32 * b + lane; return p.order && k < mine ? __ldg(p.order + q + static_cast<long long>(k) * Q) : 0; };
+    order0 = fetch(0);
+    order1 = fetch(1);
+    auto row_of = [&](int k) -> int {
+        if (!p.order) return q + k * Q;
+        return __shfl_sync(0xffffffffu, (k >> 5) == block ? order0 : order1, k & 31);
+    };
+    // copies: row and stage that come next, the ring's place and how many places are taken
+    WarpRow<E> next{};
+    int next_row = 0, next_stage = 0, next_uses = 0, in_slot = 0, taken = 0;
+    if (mine > 0) {
+        next.set(p, row_of(0), gw, tw);
+        next_uses = next.stages + (GRAD ? max(0, next.stages - depth) : 0);
+    }
+    auto copy_ahead = [&](int row_now) {
+        while (taken < depth && next_row < mine) {
+            if (next_stage == next_uses) {
+                if (next_row - row_now >= 30) return;
+                ++next_row;
+                next_stage = 0;
+                if (next_row < mine) {
+                    next.set(p, row_of(next_row), gw, tw);
+                    next_uses = next.stages + (GRAD ? max(0, next.stages - depth) : 0);
                 }
                 continue;
             }
-            float largest = 0.0f, xy = 0.0f;
-            if (MODE == kClassDistill) {
-                if (tid < 32) class_top_load(p, t, row.x, top, largest);
-            } else if (tid == 0) {
-                xy = load_local(row.x + target);
+            const int stage = next_stage < next.stages ? next_stage : next_stage - next.stages;
+            const int first = (stage * tw + gw) * kStageGroups, bytes = min(kStageGroups, next.groups - first) * 16;
+            if (lane == 0) {
+                fence_proxy_async_smem();
+                mbar_arrive_expect_tx(bars + in_slot, bytes);
+                bulk_copy_g2s(ring + in_slot * kStageBytes, next.x + static_cast<long long>(first) * N, bytes, bars + in_slot, first_use);
             }
-            ClassSum sum;
-            int g = tid;
-            for (; g + 3 * threads < row.groups; g += 4 * threads) {
-                uint4 raw[4];
+            ++next_stage;
+            ++taken;
+            if (++in_slot == depth) in_slot = 0;
+        }
+    };
+    int out_slot = 0, out_parity = 0, wait_slot = 0, wait_parity = 0;   // the place that is given back next; the copy that is waited for next
+    bool gone = false;                              // a wait ran out: nothing is copied any more
+    auto give_back = [&](int row_now) {             // what is in registers now may be overwritten
+        __syncwarp();
+        if (gone) return;
+        --taken;
+        if (++out_slot == depth) {
+            out_slot = 0;
+            out_parity ^= 1;
+        }
+        copy_ahead(row_now);
+    };
+    auto wait_copy = [&]() -> const unsigned char* {
+        if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + wait_slot, wait_parity, abort_flag))) gone = true;
+        const unsigned char* at = ring + wait_slot * kStageBytes;
+        if (++wait_slot == depth) {
+            wait_slot = 0;
+            wait_parity ^= 1;
+        }
+        return at;
+    };
+    copy_ahead(0);
+
+    double inv = 0.0;                               // warp 0: 1 / norm, 0 where nothing counts
+    if (MODE != kClassLogp && warp == 0) {
+        double n = p.norm;
+        if (n == 0.0 && p.order) n = p.prep->norm;
+        if (n == 0.0 && !p.order) {                 // few rows: every CTA adds their weights up
+            for (long long t = lane; t < p.T; t += 32) {
+                long long target;
+                float w;
+                if (class_counts(p, t, MODE, &target, &w)) n += w;
+            }
+            n = warp_sum64(n);
+        }
+        inv = n == 0.0 ? 0.0 : 1.0 / n;
+    }
+    long long from = 0, to = p.T;
+    if (MODE == kClassLogp && !p.order && p.offsets) {
+        from = load_any_id(p.offsets, p.wide_offsets, 0);
+        to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+    }
+    double sums[3] = {0.0, 0.0, 0.0};
+    int turn = 0;
+    for (int k = 0; k < mine; ++k) {
+        if ((k >> 5) != block) {
+            ++block;
+            order0 = order1;
+            order1 = fetch(block + 1);
+        }
+        copy_ahead(k);                              // (a warp without a stage of the rows before gives nothing back)
+        const long long t = row_of(k);
+        const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
+        WarpRow<E> own;
+        own.set(p, t, gw, tw);
+        long long target = 0;
+        float w = 1.0f;
+        bool counts = true;
+        if (p.order) {
+            if (p.weights) w = __ldg(p.weights + t);
+            if (MODE != kClassDistill) target = load_any_id(p.ids, p.wide_ids, t);
+        } else {
+            counts = class_counts(p, t, MODE, &target, &w);
+            if (MODE == kClassLogp) counts = counts && t >= from && t < to;
+        }
+        const bool edges = gw == 0 && lane < row.edges;
+        float xy = 0.0f, edge = 0.0f;
+        if (counts) {
+            if (MODE != kClassDistill && tid == 0) xy = load_local(row.x + target);
+            if (edges) edge = load_local(row.x + row.edge(lane));
+        }
+        float largest = -INFINITY;
+        if (MODE == kClassDistill && counts) {
+            bool twice = false;
+            for (int j = tid; j < p.K; j += threads) {
+                const ClassEntry e = class_entry(p, t, j);
+                const int id = class_entry_id(p, e);
+                if (id >= 0) largest = fmaxf(largest, e.v);
+                twice |= class_entry_put(top, j, id, e.v, id >= 0 ? load_local(row.x + id) : 0.0f);
+            }
+            if (twice) top.twice[turn] = 1;
+            class_top_warp(p, t, top, largest);
+        }
+        ClassSum sum;
+        const int dropped = GRAD ? max(0, own.stages - depth) : own.stages;
+        for (int i = 0; i < own.stages; ++i) {
+            const int left = min(kStageGroups, own.groups - (i * tw + gw) * kStageGroups) - lane;
+            const unsigned char* at = wait_copy();
+            uint4 raw[J];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) raw[j] = row.load(g + j * threads);
-                float v[4 * N];
+            for (int j = 0; j < J; ++j) raw[j] = *reinterpret_cast<const uint4*>(at + (lane + 32 * j) * 16);
+            if (i < dropped) give_back(k);
+            if (left > 32 * (J - 1)) {
+                sum.add_groups<E, J>(raw, p.c);
+            } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) ClassGroup<E>::widen(raw[j], reinterpret_cast<float(&)[N]>(v[j * N]));
-                sum.add(v, p.c);
+                for (int j = 0; j < J; ++j) {
+                    const uint4 one[1] = {raw[j]};
+                    if (32 * j < left) sum.add_groups<E, 1>(one, p.c);
+                }
             }
-            for (; g < row.groups; g += threads) {
-                float v[N];
-                ClassGroup<E>::widen(row.load(g), v);
-                sum.add(v, p.c);
+        }
+        if (edges) sum.add(edge, p.c);
+        class_sum_cta(sum, slot[turn]);
+        bool stop = *abort_flag != 0;
+        if (C > 1) {
+            if (tid < C) {
+                cluster_store_f32(&cta_slot[turn][rank][0], tid, sum.top);
+                cluster_store_f32(&cta_slot[turn][rank][1], tid, sum.m);
+                cluster_store_f32(&cta_slot[turn][rank][2], tid, sum.s);
+                cluster_store_f32(&cta_slot[turn][rank][3], tid, stop ? 1.0f : 0.0f);
             }
-            float edge = 0.0f;
-            if (tid < row.edges) {
-                edge = load_local(row.x + row.edge(tid));
-                sum.add(edge, p.c);
+            cluster_barrier();
+            sum = ClassSum{};
+            stop = false;
+            for (int r = 0; r < C; ++r) {
+                sum.join(cta_slot[turn][r][0], cta_slot[turn][r][1], cta_slot[turn][r][2]);
+                stop = stop || cta_slot[turn][r][3] != 0.0f;
             }
-            class_sum_cta(sum, slot[turn]);
-            turn ^= 1;
-            if (MODE == kClassLogp) {
-                if (tid == 0) {
+        }
+        if (stop) {
+            gone = true;
+            break;
+        }
+        if (sum.top == -INFINITY) sum.m = 0.0f;     // no finite logit: s is 0 (or NaN)
+        if (MODE == kClassLogp) {
+            if (gw == 0 && lane == 0) {
+                if (counts) {
                     const double lse2 = class_lse2(sum.m, sum.s), lp = class_logp(p, xy, sum.m, sum.s);
                     if (p.logp) p.logp[t] = static_cast<float>(lp);
                     if (p.lse) p.lse[t] = static_cast<float>(kLn2 * lse2);
@@ -427,93 +744,138 @@ __global__ void __launch_bounds__(kClassThreads) k_class_rows(const __grid_const
                         p.logp64[t] = lp;
                         p.coef[t] = 0.0f;
                     }
+                } else {
+                    class_dead_row<MODE>(p, t);
                 }
-                continue;
             }
-            if (MODE == kClassPolicy && tid == 0) {
-                const ClassNumbers r = class_policy_row(p, t, w, xy, sum.m, sum.s, inv);
+            turn ^= 1;
+            continue;
+        }
+        if (MODE == kClassPolicy && tid == 0) {
+            if (counts) {
+                const ClassNumbers r = class_policy_row(p, t, w, xy, sum.m, sum.s, inv, rank == 0);
                 now[0] = r.k;
                 now[1] = r.at;
 #pragma unroll
                 for (int i = 0; i < 3; ++i) sums[i] += r.sums[i];
+            } else if (rank == 0) {
+                class_dead_row<MODE>(p, t);
             }
-            if (MODE == kClassDistill && tid < 32) {
-                double cross;
-                const double part = class_top_weights(p, t, top, largest, cross);
-                const double one = p.teacher_lse || part == 0.0 ? 1.0 : 1.0 / part, q = part * one;      // q: the sum of the weights
-                if (tid == 0) {
-                    // sum q (log2 q - c x + lse2): with the teacher's own normalisation log2 q is smaller by log2(part)
+        }
+        bool twice = false;
+        if (MODE == kClassDistill) {
+            twice = top.twice[turn] != 0;
+            if (counts && warp == 0) {
+                const bool here = lane < warps;
+                double base = here ? top.warp[lane][0] : -INFINITY, all = here ? top.warp[lane][1] : 0.0, cross = here ? top.warp[lane][2] : 0.0;
+                double most = base;
+#pragma unroll
+                for (int d = 16; d >= 1; d >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, d));
+                const double f = all == 0.0 ? 0.0 : exp2(base - most);
+                cross = warp_sum64(all == 0.0 ? 0.0 : f * (cross + (base - most) * all));
+                all = warp_sum64(f * all);
+                // with the teacher's own normalisation log2 q is smaller by log2(all)
+                const double one = p.teacher_lse || all == 0.0 ? 1.0 : 1.0 / all, mass = all * one;
+                if (here) top.part[lane] = static_cast<float>(f * one);
+                if (lane == 0) {
                     double kl = 0.0;
-                    if (part != 0.0) kl = kLn2 * (cross * one + q * (class_lse2(sum.m, sum.s) + log2(one)));
-                    if (p.row_kl) p.row_kl[t] = static_cast<float>(kl);
+                    if (all != 0.0) kl = kLn2 * (cross * one + mass * (class_lse2(sum.m, sum.s) + log2(one)));
+                    if (p.row_kl && rank == 0) p.row_kl[t] = static_cast<float>(kl);
                     sums[0] += w * kl;
                     const double gain = w * inv * p.factor * p.scale;
-                    now[0] = static_cast<float>(q == 0.0 ? 0.0 : gain * q / sum.s);
+                    now[0] = static_cast<float>(mass == 0.0 ? 0.0 : gain * mass / sum.s);
                     now[1] = static_cast<float>(gain);
-                    top_sum = static_cast<float>(q);
-                    top_scale = static_cast<float>(one);
                 }
+            } else if (!counts && rank == 0 && tid == 0) {
+                class_dead_row<MODE>(p, t);
             }
-            if (!GRAD) continue;
-            __syncthreads();
-            const float k = now[0], m = -sum.m;
-            const int where = MODE == kClassPolicy ? static_cast<int>(target) - row.head : -1;
-            for (g = tid; g < row.groups; g += threads) {
-                float v[N];
-                ClassGroup<E>::widen(row.load(g), v);
+            // the table is empty again before the next row's classes come
+            for (int i = tid; i < top.size; i += threads) top.table[i] = -1;
+            if (tid == 0) top.twice[turn ^ 1] = 0;
+        }
+        turn ^= 1;
+        if (MODE == kClassDistill || GRAD) __syncthreads();
+        if (!GRAD) continue;
+        const float factor = counts ? now[0] : 0.0f, m = -sum.m;
+        const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), factor2 = f32x2_pack(factor, factor);
+        auto second = [&](int i, const unsigned char* at) {
+            const int first = (i * tw + gw) * kStageGroups, left = min(kStageGroups, own.groups - first) - lane;
+            uint4 raw[J];
 #pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = exp2_fast(fmaf(v[i], p.c, m)) * k;
-                if (MODE == kClassPolicy && where >= g * N && where < g * N + N) {
+            for (int j = 0; j < J; ++j) raw[j] = *reinterpret_cast<const uint4*>(at + (lane + 32 * j) * 16);
+            give_back(k);
 #pragma unroll
-                    for (int i = 0; i < N; ++i)
-                        if (where == g * N + i) v[i] = now[1];
-                }
-                row.store(g, v);
+            for (int j = 0; j < J; ++j) {
+                if (32 * j >= left) break;
+                uint64_t v[G::P];
+#pragma unroll
+                for (int e = 0; e < G::P; ++e) v[e] = counts ? f32x2_mul(exp2_pair(G::pair(raw[j], e), c2, m2), factor2) : 0;
+                row.store(first + lane + 32 * j, v);
             }
-            if (tid < row.edges) {
-                const bool hit = MODE == kClassPolicy && row.edge(tid) == static_cast<int>(target);
-                store_from_float(row.dx + row.edge(tid), hit ? now[1] : exp2_fast(fmaf(edge, p.c, m)) * k);
-            }
-            if (MODE == kClassDistill) {
-                __syncthreads();                    // the classes' values replace what was just written
-                const float gain = now[1], one = top_scale;
-                for (int j = tid; j < p.K; j += threads) {
-                    const int id = top.id[j];
-                    if (id < 0) continue;
-                    float q = 0.0f;                 // a class that the teacher names twice has both weights
+        };
+        for (int i = dropped; i < own.stages; ++i) second(i, ring + out_slot * kStageBytes);
+        for (int i = 0; i < dropped; ++i) second(i, wait_copy());
+        if (edges) store_from_float(row.dx + row.edge(lane), counts ? exp2_fast(fmaf(edge, p.c, m)) * factor : 0.0f);
+        if (!counts) continue;
+        __syncwarp();                               // the targets' values replace what was just written, by the warp that wrote it
+        auto owner = [&](int column) {
+            const int g = column - row.head;
+            return g < 0 || g >= row.groups * N ? 0 : (g / (N * kStageGroups)) % tw;
+        };
+        if (MODE == kClassPolicy) {
+            if (lane == 0 && owner(int(target)) == gw) store_from_float(row.dx + target, now[1]);
+        } else {
+            const float gain = now[1];
+            for (int j = lane; j < p.K; j += 32) {
+                const int id = top.id[j];
+                if (id < 0 || owner(id) != gw) continue;
+                float weight = top.q[j] * top.part[(j % threads) >> 5];
+                if (twice) {                        // a class that the teacher names twice has both weights
+                    weight = 0.0f;
                     for (int i = 0; i < p.K; ++i)
-                        if (top.id[i] == id) q += top.q[i];
-                    store_from_float(row.dx + id, fmaf(exp2_fast(fmaf(top.x[j], p.c, m)), k, -gain * (q * one)));
+                        if (top.id[i] == id) weight += top.q[i] * top.part[(i % threads) >> 5];
                 }
-                __syncthreads();
+                store_from_float(row.dx + id, fmaf(exp2_fast(fmaf(top.x[j], p.c, m)), factor, -gain * weight));
+            }
+            __syncthreads();                        // the next row's classes replace these
+        }
+    }
+    if (gone) {
+        // the copies in flight have to land before the shared memory is given up
+        for (; taken > 0; --taken) {
+            mbar_wait_drain(bars + out_slot, out_parity);
+            if (++out_slot == depth) {
+                out_slot = 0;
+                out_parity ^= 1;
             }
         }
-        if (MODE != kClassLogp && tid == 0)
-            for (int i = 0; i < 3; ++i) p.chunk_sum[3 * static_cast<long long>(chunk) + i] = sums[i];
+        if (tid == 0) atomicExch(p.timeout, kStatusTimeout);
     }
-    if (MODE == kClassLogp) return;
-    // the CTA that is done last adds the chunks up, in a fixed order
-    if (tid == 0) {
-        __threadfence();
-        last_cta = atomicAdd(p.words, 1u) == gridDim.x - 1;
-    }
-    __syncthreads();
-    if (!last_cta) return;
-    __threadfence();
-    double sums[3] = {0.0, 0.0, 0.0};
-    for (int chunk = tid; chunk < p.chunks; chunk += threads)
-        for (int i = 0; i < 3; ++i) sums[i] += __ldcg(p.chunk_sum + 3 * static_cast<long long>(chunk) + i);
-    for (int i = 0; i < 3; ++i) {
-        sums[i] = warp_sum64(sums[i]);
-        if ((tid & 31) == 0) warp_part[tid >> 5][i] = sums[i];
-    }
-    __syncthreads();
-    if (tid == 0) {
-        for (int i = 0; i < 3; ++i) {
-            sums[i] = 0.0;
-            for (int w = 0; w < threads / 32; ++w) sums[i] += warp_part[w][i];
-            sums[i] *= inv;
+    // gradients of rows that do not count
+    if (GRAD && p.order) {
+        for (long long k = live + q; k < p.T; k += Q) {
+            const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, __ldg(p.order + k), p.V);
+            const uint64_t zero[G::P] = {};
+            for (int g = rank * threads + tid; g < row.groups; g += C * threads) row.store(g, zero);
+            if (gw == 0 && lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
         }
+    }
+    if (MODE == kClassLogp || rank != 0) return;
+    // the CTA that is done last adds the CTAs' sums up, in a fixed order
+    if (tid == 0) {
+        for (int i = 0; i < 3; ++i) p.cta_sum[3 * q + i] = sums[i];
+        __threadfence();
+        last_cta = atomicAdd(p.words, 1u) == unsigned(Q) - 1;
+    }
+    __syncthreads();
+    if (!last_cta || warp != 0) return;
+    __threadfence();
+    for (int i = 0; i < 3; ++i) {
+        sums[i] = 0.0;
+        for (int r = lane; r < Q; r += 32) sums[i] += __ldcg(p.cta_sum + 3 * r + i);
+        sums[i] = warp_sum64(sums[i]) * inv;
+    }
+    if (lane == 0) {
         if (MODE == kClassPolicy) {
             p.out[0] = static_cast<float>(p.factor * (sums[0] + p.kl_coef * sums[1]));
             for (int i = 0; i < 3; ++i) p.out[1 + i] = static_cast<float>(sums[i]);
@@ -551,7 +913,8 @@ constexpr int kClassGradThreads = 256;
 
 template <class E>
 __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_constant__ ClassGradParams p) {
-    constexpr int N = ClassGroup<E>::N;
+    using G = ClassGroup<E>;
+    constexpr int N = G::N;
     const int tid = threadIdx.x, threads = blockDim.x;
     grid_dependency_wait();
     const long long items = p.T * p.slices;
@@ -570,7 +933,7 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
         int g = slice * p.slice_groups + tid;
         const bool edges = slice == 0 && tid < row.edges;
         if (!live) {
-            const float zero[N] = {};
+            const uint64_t zero[G::P] = {};
             for (; g < end; g += threads) row.store(g, zero);
             if (edges) store_from_float(row.dx + row.edge(tid), 0.0f);
             continue;
@@ -586,16 +949,18 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
             k = -gt * exp2_fast(static_cast<float>(-static_cast<double>(m) - l2));
         }
         const int where = static_cast<int>(target) - row.head;
+        const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), k2 = f32x2_pack(k, k);
         for (; g < end; g += threads) {
-            float v[N];
-            ClassGroup<E>::widen(row.load(g), v);
-            const bool hit = where >= g * N && where < g * N + N;
+            const uint4 raw = row.load(g);
+            uint64_t v[G::P];
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = exp2_fast(fmaf(v[j], p.c, m)) * k;
-            if (hit) {
+            for (int j = 0; j < G::P; ++j) v[j] = f32x2_mul(exp2_pair(G::pair(raw, j), c2, m2), k2);
+            if (where >= g * N && where < g * N + N) {
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (where == g * N + j) v[j] += gt;
+                for (int j = 0; j < G::P; ++j) {
+                    const int at = where - g * N - 2 * j;
+                    v[j] = f32x2_add(v[j], f32x2_pack(at == 0 ? gt : 0.0f, at == 1 ? gt : 0.0f));
+                }
             }
             row.store(g, v);
         }

@@ -11,6 +11,9 @@ using namespace lrgd;
 
 namespace {
 
+template <class E, int MODE, bool GRAD>
+struct ClassRowsTag {};
+
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxClasses = int64_t(1) << 24;
 constexpr int64_t kMaxPitch = int64_t(1) << 40;
@@ -39,41 +42,82 @@ bool apart(const E* x, int64_t ld, const E* dx, int64_t ld_d, int64_t T, int64_t
     return off >= V * es && off + V * es <= pitch;
 }
 
-int class_threads(int V, size_t es) {
-    const int64_t groups = int64_t(V) * int64_t(es) / 16;
-    return 32 * int(std::max<int64_t>(2, std::min<int64_t>(kClassThreads / 32, (groups + 127) / 128)));
+constexpr int kRingStages = 96;                     // of an SM's shared memory (192 KB), shared by its CTAs
+
+// CTAs for the rows: `warps` each, `cluster` to a row, `ctas` in all.  Rows that fill the SMs have one CTA each of as many warps as there are
+// pairs of stages in a row, up to 32 warps an SM; fewer rows are split over clusters until every stage has a warp of its own.
+struct RowPlan {
+    int warps, cluster, ctas, depth;
+};
+RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es) {
+    const int64_t stages = std::max<int64_t>(1, (V * es / 16 + kStageGroups - 1) / kStageGroups);
+    const int sms = plan_sms(ctx);
+    RowPlan r{};
+    r.cluster = 1;
+    while (r.cluster < kMaxCluster && r.cluster * 2 * T <= sms && r.cluster * 2 <= stages) r.cluster *= 2;
+    const int64_t want = r.cluster > 1 ? (stages + r.cluster - 1) / r.cluster : (stages + 1) / 2;
+    r.warps = 1;
+    while (r.warps < kRingThreads / 32 && r.warps < want) r.warps *= 2;
+    const int per_sm = 32 / r.warps;
+    r.depth = kRingStages / 32;
+    r.ctas = int(std::max<int64_t>(1, std::min<int64_t>(T, int64_t(sms) * per_sm / r.cluster))) * r.cluster;
+    return r;
 }
 
-template <int MODE>
-int norm_parts(lr_ctx* ctx, ClassParams& p, double* part, cudaStream_t st) {
-    if (p.norm != 0.0) return LR_OK;
-    p.norm_part = part;
-    p.norm_parts = int((p.T + kNormRows - 1) / kNormRows);
-    return launched(ctx, [&] { k_class_norm<MODE><<<p.norm_parts, kNormThreads, 0, st>>>(p, part); });
-}
-
-// Rows in chunks of at least about 64 KB, each with sums of its own
-template <class E>
-void cut_rows(ClassParams& p) {
-    const int64_t row = int64_t(p.V) * int64_t(sizeof(E));
-    p.chunk_rows = std::max<int64_t>(1, std::max<int64_t>((64 << 10) / row, (p.T + kClassChunks - 1) / kClassChunks));
-    p.chunks = int((p.T + p.chunk_rows - 1) / p.chunk_rows);
+// Scratch of k_class_rows and k_class_prep: sums of the CTAs, the order of the rows
+struct RowScratch {
+    size_t sums, prep, order;
+    size_t bytes() const { return sums + prep + order; }
+};
+RowScratch row_scratch(const RowPlan& plan, int64_t T) {
+    return {up256(size_t(plan.ctas / plan.cluster) * 3 * sizeof(double)), up256(sizeof(ClassPrep)), up256(size_t(T) * sizeof(int))};
 }
 
 template <class E, int MODE>
-int launch_rows(lr_ctx* ctx, ClassParams& p, bool grad, bool dependent, cudaStream_t st) {
-    const int threads = class_threads(p.V, sizeof(E));
-    const size_t smem = MODE == kClassDistill ? sizeof(ClassTop) : 0;
-    const dim3 grid(grid_for(ctx, p.chunks, 1, 2048 / threads));
-    auto go = [&](auto kern) -> int {
-        LR_CK(ctx, launch_kernel(kern, grid, dim3(threads), smem, st, dependent && ctx->overlap, p));
+int launch_rows(lr_ctx* ctx, ClassParams& p, const RowPlan& plan, const RowScratch& at, const Scratch& scratch, bool grad, cudaStream_t st) {
+    p.cluster = plan.cluster;
+    p.depth = plan.depth;
+    p.cta_sum = reinterpret_cast<double*>(scratch.data);
+    p.words = scratch.words;
+    p.timeout = ctx->d_status;
+    // with a row for every CTA the rows are looked at on the way
+    const bool prep = p.T > plan.ctas / plan.cluster && (MODE != kClassDistill || p.weights);
+    if (prep) {
+        ClassPrep* out = reinterpret_cast<ClassPrep*>(scratch.data + at.sums);
+        int* order = reinterpret_cast<int*>(scratch.data + at.sums + at.prep);
+        const int r = launched(ctx, [&] { k_class_prep<MODE><<<1, kPrepThreads, 0, st>>>(p, order, out); });
+        if (r != LR_OK) return r;
+        p.prep = out;
+        p.order = order;
+    }
+    const size_t smem = size_t(plan.warps) * plan.depth * (kStageBytes + 8) + (MODE == kClassDistill ? class_top_bytes(p.K, plan.warps) : 0);
+    auto go = [&](auto kern, auto tag) -> int {
+        LR_CK(ctx, ensure_dynamic_smem<decltype(tag)>(reinterpret_cast<const void*>(kern), int(smem)));
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(plan.ctas);
+        cfg.blockDim = dim3(plan.warps * 32);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[2];
+        if (plan.cluster > 1) {
+            attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+            attr[cfg.numAttrs].val.clusterDim.x = unsigned(plan.cluster);
+            attr[cfg.numAttrs].val.clusterDim.y = 1;
+            attr[cfg.numAttrs++].val.clusterDim.z = 1;
+        }
+        if (prep && ctx->overlap) {
+            attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
+        }
+        cfg.attrs = attr;
+        LR_CK(ctx, cudaLaunchKernelEx(&cfg, kern, p));
         ctx->launches += 1;
         return LR_OK;
     };
     if constexpr (MODE != kClassLogp) {
-        if (grad) return go(k_class_rows<E, MODE, true>);
+        if (grad) return go(k_class_rows<E, MODE, true>, ClassRowsTag<E, MODE, true>{});
     }
-    return go(k_class_rows<E, MODE, false>);
+    return go(k_class_rows<E, MODE, false>, ClassRowsTag<E, MODE, false>{});
 }
 
 template <class E>
@@ -90,7 +134,6 @@ ClassParams row_params(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, in
     p.scale = scale;
     p.c = float(double(scale) * 1.4426950408889634074);
     p.status = ctx->d_status + 1;
-    cut_rows<E>(p);
     return p;
 }
 
@@ -121,7 +164,13 @@ int logp_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
     ClassParams p = row_params(ctx, d_logits, ld, T, V, d_targets, id_bytes, ignore_id, scale);
     p.logp = d_logp;
     p.lse = d_lse;
-    return launch_rows<E, kClassLogp>(ctx, p, false, false, static_cast<cudaStream_t>(stream));
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const RowPlan plan = plan_rows(ctx, T, V, sizeof(E));
+    const RowScratch at = row_scratch(plan, T);
+    Scratch scratch{};
+    const int rs = gate_scratch(ctx, at.bytes(), st, &scratch);
+    if (rs != LR_OK) return rs;
+    return launch_rows<E, kClassLogp>(ctx, p, plan, at, scratch, false, st);
 }
 
 template <class E>
@@ -195,15 +244,12 @@ int policy_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V
     p.norm = opt->norm;
     p.factor = opt->factor;
     p.out = d_stats;
-    const size_t sums = up256(size_t(p.chunks) * 3 * sizeof(double)), parts = up256(size_t(T / kNormRows + 1) * sizeof(double));
+    const RowPlan plan = plan_rows(ctx, T, V, sizeof(E));
+    const RowScratch at = row_scratch(plan, T);
     Scratch scratch{};
-    const int rs = gate_scratch(ctx, sums + parts, st, &scratch);
+    const int rs = gate_scratch(ctx, at.bytes(), st, &scratch);
     if (rs != LR_OK) return rs;
-    p.chunk_sum = reinterpret_cast<double*>(scratch.data);
-    p.words = scratch.words;
-    const int rn = norm_parts<kClassPolicy>(ctx, p, reinterpret_cast<double*>(scratch.data + sums), st);
-    if (rn != LR_OK) return rn;
-    return launch_rows<E, kClassPolicy>(ctx, p, d_dlogits != nullptr, p.norm == 0.0, st);
+    return launch_rows<E, kClassPolicy>(ctx, p, plan, at, scratch, d_dlogits != nullptr, st);
 }
 
 template <class E>
@@ -242,15 +288,12 @@ int distill_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t 
     p.factor = opt->factor;
     p.out = d_loss;
     if (p.norm == 0.0 && !d_weights) p.norm = double(T);
-    const size_t sums = up256(size_t(p.chunks) * 3 * sizeof(double)), parts = up256(size_t(T / kNormRows + 1) * sizeof(double));
+    const RowPlan plan = plan_rows(ctx, T, V, sizeof(E));
+    const RowScratch at = row_scratch(plan, T);
     Scratch scratch{};
-    const int rs = gate_scratch(ctx, sums + parts, st, &scratch);
+    const int rs = gate_scratch(ctx, at.bytes(), st, &scratch);
     if (rs != LR_OK) return rs;
-    p.chunk_sum = reinterpret_cast<double*>(scratch.data);
-    p.words = scratch.words;
-    const int rn = norm_parts<kClassDistill>(ctx, p, reinterpret_cast<double*>(scratch.data + sums), st);
-    if (rn != LR_OK) return rn;
-    return launch_rows<E, kClassDistill>(ctx, p, d_dlogits != nullptr, p.norm == 0.0, st);
+    return launch_rows<E, kClassDistill>(ctx, p, plan, at, scratch, d_dlogits != nullptr, st);
 }
 
 template <class E>
@@ -279,20 +322,23 @@ int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
         if (d_dlogits && T > 0) LR_CK(ctx, cudaMemset2DAsync(d_dlogits, size_t(ld_d) * sizeof(E), 0, size_t(V) * sizeof(E), size_t(T), st));
         return LR_OK;
     }
-    const size_t stat = up256(size_t(T) * sizeof(float2)), lp = up256(size_t(T) * 8), coef = up256(size_t(T) * 4), loss = up256(size_t(pairs) * 8);
+    const RowPlan plan = plan_rows(ctx, std::max<int64_t>(T, 1), V, sizeof(E));
+    const RowScratch at = row_scratch(plan, T);
+    const size_t rows = at.bytes(), stat = rows + up256(size_t(T) * sizeof(float2)), lp = up256(size_t(T) * 8), coef = up256(size_t(T) * 4),
+                 loss = up256(size_t(pairs) * 8);
     Scratch scratch{};
     const int rs = gate_scratch(ctx, stat + lp + coef + loss, st, &scratch);
     if (rs != LR_OK) return rs;
     ClassPairParams q{};
     if (T > 0) {
         ClassParams p = row_params(ctx, d_logits, ld, T, V, d_targets, id_bytes, opt->ignore_id, opt->scale);
-        p.stat = reinterpret_cast<float2*>(scratch.data);
+        p.stat = reinterpret_cast<float2*>(scratch.data + rows);
         p.logp64 = reinterpret_cast<double*>(scratch.data + stat);
         p.coef = reinterpret_cast<float*>(scratch.data + stat + lp);
         p.offsets = d_offsets;
         p.wide_offsets = offset_bytes == 8;
         p.offset_count = 2 * pairs;
-        const int r = launch_rows<E, kClassLogp>(ctx, p, false, false, st);
+        const int r = launch_rows<E, kClassLogp>(ctx, p, plan, at, scratch, false, st);
         if (r != LR_OK) return r;
     }
     q.ids = d_targets;
@@ -332,7 +378,7 @@ int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
     d.ignore = opt->ignore_id;
     d.scale = opt->scale;
     d.c = float(double(opt->scale) * 1.4426950408889634074);
-    d.stat = reinterpret_cast<const float2*>(scratch.data);
+    d.stat = reinterpret_cast<const float2*>(scratch.data + rows);
     d.g = q.coef;
     d.dx = d_dlogits;
     d.ld_d = ld_d;
