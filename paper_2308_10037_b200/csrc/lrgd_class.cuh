@@ -63,8 +63,10 @@ struct ClassParams {
     // rows and their CTAs
     const int* order;            // the rows that count, then the others (k_class_prep); NULL: all rows, looked at one by one
     const struct ClassPrep* prep;
-    int cluster;                 // CTAs per row
-    int depth;                   // stages in a warp's ring
+    int cluster;                 // long rows: CTAs per row (a power of two), stages in a ring, rows between the passes (see k_class_ring)
+    int depth, lag;
+    const double* norm_part;     // short rows: the sum of the weights in parts (k_class_norm), or none
+    int norm_parts;
     double* cta_sum;             // [CTAs][3]
     int* timeout;                // status word of waits
     unsigned int* words;         // [0] CTAs that are done
@@ -109,6 +111,8 @@ struct ClassGroup {
         if constexpr (sizeof(E) == 4) return f32x2_pack(__uint_as_float(word(w, 2 * i)), __uint_as_float(word(w, 2 * i + 1)));
         else return f32x2_pack(__uint_as_float(word(w, i) << 16), __uint_as_float(word(w, i) & 0xffff0000u));
     }
+    // 2^(x * c - m) of pair i
+    static __device__ __forceinline__ uint64_t power(const uint4& w, int i, uint64_t c, uint64_t minus_m) { return exp2_pair(pair(w, i), c, minus_m); }
     static __device__ __forceinline__ uint4 narrow(const uint64_t (&v)[P]) {
         uint32_t u[4];
 #pragma unroll
@@ -128,21 +132,33 @@ struct ClassGroup {
     template <int J>
     static __device__ __forceinline__ float largest(const uint4 (&raw)[J]) {
         if constexpr (sizeof(E) == 4) {
-            float t = __uint_as_float(raw[0].x);
+            float t[J];
 #pragma unroll
-            for (int i = 1; i < 4 * J; ++i) t = fmaxf(t, __uint_as_float(word(raw[i / 4], i % 4)));
-            return t;
+            for (int j = 0; j < J; ++j)
+                t[j] = fmaxf(fmaxf(__uint_as_float(raw[j].x), __uint_as_float(raw[j].y)), fmaxf(__uint_as_float(raw[j].z), __uint_as_float(raw[j].w)));
+#pragma unroll
+            for (int j = 1; j < J; ++j) t[0] = fmaxf(t[0], t[j]);
+            return t[0];
         } else {
-            uint32_t t = raw[0].x;
+            uint32_t t[J];
 #pragma unroll
-            for (int i = 1; i < 4 * J; ++i) asm("max.bf16x2 %0, %1, %2;" : "=r"(t) : "r"(t), "r"(word(raw[i / 4], i % 4)));
-            return fmaxf(__uint_as_float(t << 16), __uint_as_float(t & 0xffff0000u));
+            for (int j = 0; j < J; ++j) t[j] = max2(max2(raw[j].x, raw[j].y), max2(raw[j].z, raw[j].w));
+#pragma unroll
+            for (int d = 1; d < J; d *= 2)
+#pragma unroll
+                for (int j = 0; j + d < J; j += 2 * d) t[j] = max2(t[j], t[j + d]);
+            return fmaxf(__uint_as_float(t[0] << 16), __uint_as_float(t[0] & 0xffff0000u));
         }
+    }
+    static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
     }
 };
 
-__device__ __forceinline__ void store_streaming(void* at, const uint4& v) {
-    asm volatile("st.global.cs.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+__device__ __forceinline__ void store_group(void* at, const uint4& v) {
+    *reinterpret_cast<uint4*>(at) = v;
 }
 
 // A row as `head` elements, `groups` groups of 16 bytes that start on 16 bytes, and a tail
@@ -169,7 +185,7 @@ struct ClassRow {
         constexpr int N = ClassGroup<E>::N;
         E* at = dx + head + g * N;
         if (wide_store) {
-            store_streaming(at, ClassGroup<E>::narrow(v));
+            store_group(at, ClassGroup<E>::narrow(v));
         } else {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
@@ -188,7 +204,7 @@ struct ClassSum {
     // room for terms up to t; false where nothing finite has come yet
     __device__ __forceinline__ bool raise(float t, float c) {
         if (t > top) {
-            const float next = t * c;
+            const float next = __fmul_rn(t, c);     // (rounded before anything is taken from it, here and wherever m is formed)
             s *= exp2_fast(m - next);
             top = t;
             m = next;
@@ -214,44 +230,35 @@ struct ClassSum {
             return;
         }
         const uint64_t c2 = f32x2_pack(c, c), m2 = f32x2_pack(-m, -m);
-        uint64_t part = 0;
+        uint64_t part[2] = {0, 0};
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int i = 0; i < G::P; ++i) part = f32x2_add(part, exp2_pair(G::pair(raw[j], i), c2, m2));
+            for (int i = 0; i < G::P; ++i) part[i & 1] = f32x2_add(part[i & 1], G::power(raw[j], i, c2, m2));
         float lo, hi;
-        f32x2_unpack(part, lo, hi);
+        f32x2_unpack(f32x2_add(part[0], part[1]), lo, hi);
         s += lo + hi;
     }
-    __device__ __forceinline__ void join(float top2, float m2, float s2) {
-        if (top2 > top) {
-            s = (s == 0.0f ? 0.0f : s * exp2_fast(m - m2)) + s2;
-            top = top2;
-            m = m2;
-        } else if (s2 != 0.0f) {
-            s += top2 == top ? s2 : s2 * exp2_fast(m2 - m);
-        }
+    // the sum over the lanes of a warp, the same bits in all of them
+    __device__ __forceinline__ void over_warp(float c) {
+        const uint32_t key = __reduce_max_sync(0xffffffffu, order_key(top));
+        top = __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
+        const float next = __fmul_rn(top, c);
+        s = s == 0.0f ? 0.0f : s * exp2_fast(m - next);             // (a NaN stays one)
+        m = next;
+#pragma unroll
+        for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    }
+    __device__ __forceinline__ void set(float top2, float s2, float c) {
+        top = top2;
+        m = __fmul_rn(top2, c);
+        s = s2;
+    }
+    // where no logit is finite s is 0 (or NaN), and m is not used
+    __device__ __forceinline__ void settle() {
+        if (top == -INFINITY) m = 0.0f;
     }
 };
-
-// The sum over a warp, then over the CTA: every thread gets the same bits.  One barrier; `slot` is not used again before the next one.
-__device__ __forceinline__ void class_sum_cta(ClassSum& a, float (*slot)[3]) {
-#pragma unroll
-    for (int d = 16; d >= 1; d >>= 1) {
-        const float t = __shfl_down_sync(0xffffffffu, a.top, d), m = __shfl_down_sync(0xffffffffu, a.m, d),
-                    s = __shfl_down_sync(0xffffffffu, a.s, d);
-        a.join(t, m, s);
-    }
-    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if ((threadIdx.x & 31) == 0) {
-        slot[warp][0] = a.top;
-        slot[warp][1] = a.m;
-        slot[warp][2] = a.s;
-    }
-    __syncthreads();
-    a = ClassSum{};
-    for (int w = 0; w < warps; ++w) a.join(slot[w][0], slot[w][1], slot[w][2]);
-}
 
 // Whether a row counts, with its target and weight
 __device__ __forceinline__ bool class_counts(const ClassParams& p, long long t, int mode, long long* target, float* weight) {
@@ -275,11 +282,6 @@ __device__ __forceinline__ double warp_sum64(double v) {
     return v;
 }
 
-// A row's numbers, from its statistics: lp and, for the gradient, k (what the terms 2^(..) are multiplied by) and at (the value at the target)
-struct ClassNumbers {
-    float k, at;
-    double sums[3];
-};
 // log2 of the sum.  exp2_fast drops the bits of its argument below 2^-23 or so: terms below 1/2 come out 4.9e-8 too small in the mean
 // (measured over 4 M random arguments; 2.2e-8 between 1/2 and 1, the largest term is exact).  One row's lp does not show that, the sum over a
 // long sequence does; in the gradient it cancels, whose numerator has the same terms.
@@ -288,37 +290,9 @@ __device__ __forceinline__ double class_lse2(float m, float s) {
     return static_cast<double>(m) + log2(sum + 4.9e-8 * (sum - 1.0));
 }
 
-// lp of the target whose logit is xy; above 0 it is rounding
-__device__ __forceinline__ double class_logp(const ClassParams& p, float xy, float m, float s) {
-    const double lp = kLn2 * (static_cast<double>(xy) * p.c - class_lse2(m, s));
-    return lp > 0.0 ? 0.0 : lp;
-}
-
-__device__ __forceinline__ ClassNumbers class_policy_row(const ClassParams& p, long long t, float w, float xy, float m, float s, double inv, bool write) {
-    ClassNumbers r;
-    const double lp = class_logp(p, xy, m, s);
-    if (p.logp && write) p.logp[t] = static_cast<float>(lp);
-    const double a = __ldg(p.adv + t), ratio = p.old_logp ? exp(lp - __ldg(p.old_logp + t)) : 1.0;
-    const double held = fmin(fmax(ratio, p.ratio_low), p.ratio_high);
-    const bool clipped = ratio * a > held * a;
-    double g = clipped ? 0.0 : -ratio * a, kl = 0.0;
-    if (p.ref_logp) {
-        const double d = __ldg(p.ref_logp + t) - lp, e = expm1(d);
-        kl = e - d;
-        g -= p.kl_coef * e;
-    }
-    r.sums[0] = -w * (clipped ? held : ratio) * a;
-    r.sums[1] = w * kl;
-    r.sums[2] = clipped ? w : 0.0;
-    g *= w * inv * p.factor * p.scale;
-    r.k = static_cast<float>(-g / s);
-    r.at = static_cast<float>(-g * expm1(lp));
-    return r;
-}
-
 // ---- which rows count ----------------------------------------------------------------------------------
 // One CTA writes the numbers of the rows that count into `order`, in their order, those of the others behind them, and sums the weights.
-// Rows that do not count get their zeros here (all but their gradient).  T = 8192: 3 us, beside the start of k_class_rows.
+// Rows that do not count get their zeros here (all but their gradient).  T = 8192: 3 us, beside the start of k_class_ring.
 constexpr int kPrepThreads = 1024;
 constexpr int kPrepItems = 8;
 
@@ -404,40 +378,27 @@ __global__ void __launch_bounds__(kPrepThreads) k_class_prep(const __grid_consta
 }
 
 // ---- a teacher's classes -------------------------------------------------------------------------------
-// Entry j of a row belongs to thread j mod (threads of the CTA).  q is 2^(c * v - base of the entry's warp); `part` turns it into the weight.
+// One warp has them: entry j belongs to lane j mod 32.  q is 2^(c * v - base), times `part` it is the weight.
 struct ClassTop {
     int* id;                     // [K], -1: absent
     float* q;                    // [K]
     float* x;                    // [K] the student's logits
-    int* table;                  // [size] the classes seen so far, -1: free
-    int size;                    // a power of two, at least 2 K
-    double (*warp)[3];           // [warps] base, sum of q, sum of q * (c * v - base - c * x)
-    float* part;                 // [warps]
-    int* twice;                  // [2] some class is named twice
+    uint32_t* marks;             // [kMarkBits / 32] a bitmap of classes
 };
-__host__ __device__ inline int class_table_size(int K) {
-    int n = 64;
-    while (n < 2 * K) n *= 2;
-    return n;
-}
-__host__ __device__ inline size_t class_top_bytes(int K, int warps) {
-    return size_t(K) * 12 + size_t(class_table_size(K)) * 4 + size_t(warps) * 32 + 64;
-}
-__device__ __forceinline__ ClassTop class_top_at(unsigned char* at, int K, int warps) {
+constexpr int kMarkBits = 1 << 14;
+__host__ __device__ inline size_t class_top_bytes(int K) { return (size_t(K) * 12 + kMarkBits / 8 + 15) / 16 * 16; }
+__device__ __forceinline__ ClassTop class_top_at(unsigned char* at, int K) {
     ClassTop top;
-    top.warp = reinterpret_cast<double(*)[3]>(at);
-    at += warps * 24;
-    top.part = reinterpret_cast<float*>(at);
-    at += warps * 4;
-    top.twice = reinterpret_cast<int*>(at);
-    at += 8;
-    top.size = class_table_size(K);
-    top.table = reinterpret_cast<int*>(at);
-    at += top.size * 4;
+    top.marks = reinterpret_cast<uint32_t*>(at);
+    at += kMarkBits / 8;
     top.id = reinterpret_cast<int*>(at);
     top.q = reinterpret_cast<float*>(at + 4 * K);
     top.x = reinterpret_cast<float*>(at + 8 * K);
     return top;
+}
+__device__ __forceinline__ void class_clear_marks(const ClassTop& top) {
+    for (int i = threadIdx.x & 31; i < kMarkBits / 128; i += 32) reinterpret_cast<uint4*>(top.marks)[i] = make_uint4(0, 0, 0, 0);
+    __syncwarp();
 }
 struct ClassEntry {
     long long id;
@@ -461,418 +422,189 @@ __device__ __forceinline__ int class_entry_id(const ClassParams& p, const ClassE
     }
     return e.v == -INFINITY ? -1 : static_cast<int>(e.id);
 }
-// Writes an entry down; true where its class has been seen in this row
-__device__ __forceinline__ bool class_entry_put(const ClassTop& top, int j, int id, float v, float x) {
-    top.id[j] = id;
-    top.q[j] = v;
-    top.x[j] = x;
-    if (id < 0) return false;
-    unsigned int at = static_cast<unsigned int>(id) * 2654435761u;
-    for (at = (at >> 12) & (top.size - 1);; at = (at + 1) & (top.size - 1)) {       // ends: at most K of 2 K places are taken
-        const int was = atomicCAS(top.table + at, -1, id);
-        if (was == -1) return false;
-        if (was == id) return true;
-    }
+// Marks the class; true where this place of the bitmap is taken, by the same class or by another one
+__device__ __forceinline__ bool class_mark(const ClassTop& top, int id) {
+    uint32_t h = static_cast<uint32_t>(id) * 2654435761u;
+    h ^= h >> 15;
+    h = h * 2246822519u >> 18;                      // kMarkBits places
+    const uint32_t bit = 1u << (h & 31);
+    return (atomicOr(top.marks + (h >> 5), bit) & bit) != 0;
 }
-// A warp's share of the row: its entries' q, their sums
-__device__ __forceinline__ void class_top_warp(const ClassParams& p, long long t, const ClassTop& top, float largest) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+
+// What the entries add up to
+struct ClassTopSum {
+    double all, cross;           // sum of q, sum of q * (c * v - base - c * x)
+    bool twice;                  // some class is named twice
+};
+// Reads a row's classes; the bitmap is empty before and after.  Eight entries of a lane are on their way together.
+template <class E>
+__device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long long t, const E* row, const ClassTop& top) {
+    constexpr int U = 8;
+    const int lane = threadIdx.x & 31;
+    ClassTopSum r{0.0, 0.0, false};
+    float largest = -INFINITY;
+    for (int j0 = 0; j0 < p.K; j0 += 32 * U) {
+        ClassEntry e[U];
+        int id[U];
+        float x[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) e[i] = class_entry(p, t, j0 + 32 * i + lane);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            id[i] = j0 + 32 * i + lane < p.K ? class_entry_id(p, e[i]) : -1;
+            x[i] = id[i] >= 0 ? load_local(row + id[i]) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int j = j0 + 32 * i + lane;
+            if (j < p.K) {
+                top.id[j] = id[i];
+                top.q[j] = e[i].v;
+                top.x[j] = x[i];
+            }
+            if (id[i] >= 0) largest = fmaxf(largest, e[i].v);
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < U; ++i) {               // a place of the bitmap that was taken: is it the same class?
+            if (j0 + 32 * i >= p.K) break;
+            uint32_t taken = __ballot_sync(0xffffffffu, id[i] >= 0 && class_mark(top, id[i]));
+            for (; taken && !r.twice; taken &= taken - 1) {
+                const int from = __ffs(taken) - 1, which = __shfl_sync(0xffffffffu, id[i], from);
+                int same = 0;
+                for (int j = lane; j < min(p.K, j0 + 32 * U); j += 32) same += top.id[j] == which;
+                r.twice = __reduce_add_sync(0xffffffffu, same) > 1;
+            }
+        }
+    }
     largest = warp_max(largest);
     const double base = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) * (static_cast<double>(p.c) / p.scale)
                                       : (largest == -INFINITY ? 0.0 : static_cast<double>(largest) * p.c);
-    double sum = 0.0, cross = 0.0;
-    for (int j = threadIdx.x; j < p.K; j += blockDim.x) {
+    for (int j = lane; j < p.K; j += 32) {
         const double a = static_cast<double>(top.q[j]) * p.c - base;
-        const double e = top.id[j] >= 0 ? exp2(a) : 0.0;
-        sum += e;
-        if (e != 0.0) cross += e * (a - static_cast<double>(top.x[j]) * p.c);
-        top.q[j] = static_cast<float>(e);
+        const float e = top.id[j] >= 0 ? exp2f(static_cast<float>(a)) : 0.0f;
+        r.all += e;
+        if (e != 0.0f) r.cross += e * (a - static_cast<double>(top.x[j]) * p.c);
+        top.q[j] = e;
     }
-    sum = warp_sum64(sum);
-    cross = warp_sum64(cross);
-    if (lane == 0) {
-        top.warp[warp][0] = sum == 0.0 && !p.teacher_lse ? -INFINITY : base;
-        top.warp[warp][1] = sum;
-        top.warp[warp][2] = cross;
-    }
-}
-
-// ---- rows ----------------------------------------------------------------------------------------------
-// One CTA per row, or a cluster of C where there are fewer rows than SMs.  A row's 16-byte groups are dealt out to the warps in stages of
-// 2 KB; every warp brings its own stages into its own ring of shared memory with bulk copies, as far ahead as the ring allows, over the ends of
-// rows too.  First pass: running maximum and sum; one barrier joins the warps (one more the CTAs).  Second pass: the gradient, from the
-// stages that are still in the ring, then from those that were overwritten, which come from L2 again.  A stage is given back when it has been
-// read for the last time, always in the order of the copies, so the ring needs no bookkeeping beyond two counters.
-constexpr int kRingThreads = 512;
-constexpr int kStageGroups = 128;
-constexpr int kStageBytes = kStageGroups * 16;
-constexpr int kMaxCluster = 8;
-
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    r.all = warp_sum64(r.all);
+    r.cross = warp_sum64(r.cross);
+    class_clear_marks(top);
     return r;
 }
-__device__ __forceinline__ void cluster_store_f32(const float* local, uint32_t rank, float v) {
-    uint32_t addr;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"(smem_u32(local)), "r"(rank));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
-}
 
-// A warp's stages of a row
-template <class E>
-struct WarpRow {
-    const E* x;                  // first group
-    int groups;
-    int stages;
-    __device__ __forceinline__ void set(const ClassParams& p, long long t, int gw, int tw) {
-        const ClassRow<E> row(p.x, p.ld, nullptr, 0, t, p.V);
-        x = row.x + row.head;
-        groups = row.groups;
-        const int all = (groups + kStageGroups - 1) / kStageGroups;
-        stages = all > gw ? (all - gw + tw - 1) / tw : 0;
-    }
+// ---- a row's last numbers ------------------------------------------------------------------------------
+// What the statistics of a row that counts give, by one warp: outputs of the row (with `write`), its part of the sums, and for the gradient
+// factor (what the terms 2^(..) are multiplied by) and at (policy: the value at the target; distillation: what q is multiplied by).
+struct ClassNumbers {
+    float factor, at;
 };
-
-template <class E, int MODE, bool GRAD>
-__global__ void __launch_bounds__(kRingThreads, 2) k_class_rows(const __grid_constant__ ClassParams p) {
-    using G = ClassGroup<E>;
-    constexpr int N = G::N;
-    constexpr int J = kStageGroups / 32;            // groups of a stage per lane
-    __shared__ float slot[2][kRingThreads / 32][3];
-    __shared__ float cta_slot[2][kMaxCluster][4];
-    __shared__ float now[2];
-    __shared__ int abort_word;
-    __shared__ bool last_cta;
-    extern __shared__ __align__(128) unsigned char class_smem[];
-    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5, depth = p.depth;
-    const int C = p.cluster, rank = C > 1 ? int(cluster_rank()) : 0, q = blockIdx.x / C, Q = gridDim.x / C;
-    const int gw = rank * warps + warp, tw = C * warps;
-    unsigned char* ring = class_smem + size_t(warp) * depth * kStageBytes;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(class_smem + size_t(warps) * depth * kStageBytes) + warp * depth;
-    ClassTop top{};
+// What a row has beside its logits, fetched before its statistics are known
+struct ClassInputs {
+    long long target;
+    float w, xy, adv, old_logp, ref_logp;
+    ClassTopSum top;
+};
+template <int MODE, class E>
+__device__ __forceinline__ void class_inputs(const ClassParams& p, long long t, const E* row, const ClassTop& top, ClassInputs& in) {
     if (MODE == kClassDistill) {
-        top = class_top_at(class_smem + size_t(warps) * depth * (kStageBytes + 8), p.K, warps);
-        for (int i = tid; i < top.size; i += threads) top.table[i] = -1;
-        if (tid < 2) top.twice[tid] = 0;
+        in.top = class_top_read(p, t, row, top);
+        return;
     }
-    volatile int* abort_flag = &abort_word;
-    if (tid == 0) abort_word = 0;
+    in.xy = load_local(row + in.target);
+    if (MODE == kClassPolicy) {
+        in.adv = __ldg(p.adv + t);
+        in.old_logp = p.old_logp ? __ldg(p.old_logp + t) : 0.0f;
+        in.ref_logp = p.ref_logp ? __ldg(p.ref_logp + t) : 0.0f;
+    }
+}
+template <int MODE>
+__device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, long long t, const ClassInputs& in, const ClassSum& sum, double inv, bool write,
+                                                      double (&sums)[3]) {
+    const int lane = threadIdx.x & 31;
+    const double lse2 = class_lse2(sum.m, sum.s);
+    ClassNumbers r{};
+    write = write && lane == 0;
+    if (MODE == kClassDistill) {
+        // with the teacher's own normalisation log2 q is smaller by log2(all)
+        const double all = in.top.all, one = p.teacher_lse || all == 0.0 ? 1.0 : 1.0 / all, mass = all * one;
+        const double kl = all == 0.0 ? 0.0 : kLn2 * (in.top.cross * one + mass * (lse2 + log2(one)));
+        if (p.row_kl && write) p.row_kl[t] = static_cast<float>(kl);
+        sums[0] += in.w * kl;
+        const double gain = in.w * inv * p.factor * p.scale;
+        r.factor = static_cast<float>(mass == 0.0 ? 0.0 : gain * mass / sum.s);
+        r.at = static_cast<float>(gain * one);
+        return r;
+    }
+    double lp = kLn2 * (static_cast<double>(in.xy) * p.c - lse2);
+    if (lp > 0.0) lp = 0.0;                         // rounding
+    if (p.logp && write) p.logp[t] = static_cast<float>(lp);
+    if (MODE == kClassLogp) {
+        if (p.lse && write) p.lse[t] = static_cast<float>(kLn2 * lse2);
+        if (p.stat && write) {
+            p.stat[t] = make_float2(sum.m, sum.s);
+            p.logp64[t] = lp;
+            p.coef[t] = 0.0f;
+        }
+    } else {
+        // exp(lp - old) - 1, exp(ref - lp) - 1 and exp(lp) - 1: one lane each
+        const double d = in.ref_logp - lp;
+        const double e = expm1(lane == 0 ? lp - in.old_logp : lane == 1 ? d : lp);
+        const double ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0) + 1.0 : 1.0, away = __shfl_sync(0xffffffffu, e, 1),
+                     rest = __shfl_sync(0xffffffffu, e, 2);
+        const double a = in.adv, held = fmin(fmax(ratio, p.ratio_low), p.ratio_high);
+        const bool clipped = ratio * a > held * a;
+        double g = clipped ? 0.0 : -ratio * a, kl = 0.0;
+        if (p.ref_logp) {
+            kl = away - d;
+            g -= p.kl_coef * away;
+        }
+        sums[0] -= in.w * (clipped ? held : ratio) * a;
+        sums[1] += in.w * kl;
+        sums[2] += clipped ? in.w : 0.0;
+        g *= in.w * inv * p.factor * p.scale;
+        r.factor = static_cast<float>(-g / sum.s);
+        r.at = static_cast<float>(-g * rest);
+    }
+    return r;
+}
+// What the gradient is at entry j of the teacher's classes
+__device__ __forceinline__ float class_top_value(const ClassParams& p, const ClassTop& top, int j, bool twice, float m, const ClassNumbers& r) {
+    const int id = top.id[j];
+    float q = top.q[j];
+    if (twice) {                                    // a class that the teacher names twice has both weights
+        q = 0.0f;
+        for (int i = 0; i < p.K; ++i)
+            if (top.id[i] == id) q += top.q[i];
+    }
+    return fmaf(exp2_fast(fmaf(top.x[j], p.c, -m)), r.factor, -r.at * q);
+}
+// Sum of the weights of all rows that count, by one warp
+template <int MODE>
+__device__ __forceinline__ double class_norm_warp(const ClassParams& p) {
+    double n = 0.0;
+    for (long long t = threadIdx.x & 31; t < p.T; t += 32) {
+        long long target;
+        float w;
+        if (class_counts(p, t, MODE, &target, &w)) n += w;
+    }
+    return warp_sum64(n);
+}
+// The warp that is done last adds the sums of all `ctas` warps that call this up, in a fixed order
+template <int MODE>
+__device__ __forceinline__ void class_finish(const ClassParams& p, int me, int ctas, double inv, double (&sums)[3]) {
+    const int lane = threadIdx.x & 31;
+    int last = 0;
     if (lane == 0) {
-        for (int i = 0; i < depth; ++i) mbar_init(bars + i, 1);
-        fence_mbar_init();
-    }
-    if (C > 1) cluster_barrier();                   // (a CTA that writes into another's shared memory has to find it started)
-    else __syncthreads();
-    grid_dependency_wait();
-    const uint64_t first_use = l2_policy_evict_first();
-    const int live = p.order ? p.prep->live : int(p.T);
-    const int mine = live > q ? (live - q + Q - 1) / Q : 0;
-    // rows of this CTA, 64 of them known ahead: lane i holds the numbers of rows 32 * block + i and 32 * (block + 1) + i
-    int block = 0, order0 = 0, order1 = 0;
-    auto fetch = [&](int b) { const int k = 32 * b + lane; return p.order && k < mine ? __ldg(p.order + q + static_cast<long long>(k) * Q) : 0; };
-    order0 = fetch(0);
-    order1 = fetch(1);
-    auto row_of = [&](int k) -> int {
-        if (!p.order) return q + k * Q;
-        return __shfl_sync(0xffffffffu, (k >> 5) == block ? order0 : order1, k & 31);
-    };
-    // copies: row and stage that come next, the ring's place and how many places are taken
-    WarpRow<E> next{};
-    int next_row = 0, next_stage = 0, next_uses = 0, in_slot = 0, taken = 0;
-    if (mine > 0) {
-        next.set(p, row_of(0), gw, tw);
-        next_uses = next.stages + (GRAD ? max(0, next.stages - depth) : 0);
-    }
-    auto copy_ahead = [&](int row_now) {
-        while (taken < depth && next_row < mine) {
-            if (next_stage == next_uses) {
-                if (next_row - row_now >= 30) return;
-                ++next_row;
-                next_stage = 0;
-                if (next_row < mine) {
-                    next.set(p, row_of(next_row), gw, tw);
-                    next_uses = next.stages + (GRAD ? max(0, next.stages - depth) : 0);
-                }
-                continue;
-            }
-            const int stage = next_stage < next.stages ? next_stage : next_stage - next.stages;
-            const int first = (stage * tw + gw) * kStageGroups, bytes = min(kStageGroups, next.groups - first) * 16;
-            if (lane == 0) {
-                fence_proxy_async_smem();
-                mbar_arrive_expect_tx(bars + in_slot, bytes);
-                bulk_copy_g2s(ring + in_slot * kStageBytes, next.x + static_cast<long long>(first) * N, bytes, bars + in_slot, first_use);
-            }
-            ++next_stage;
-            ++taken;
-            if (++in_slot == depth) in_slot = 0;
-        }
-    };
-    int out_slot = 0, out_parity = 0, wait_slot = 0, wait_parity = 0;   // the place that is given back next; the copy that is waited for next
-    bool gone = false;                              // a wait ran out: nothing is copied any more
-    auto give_back = [&](int row_now) {             // what is in registers now may be overwritten
-        __syncwarp();
-        if (gone) return;
-        --taken;
-        if (++out_slot == depth) {
-            out_slot = 0;
-            out_parity ^= 1;
-        }
-        copy_ahead(row_now);
-    };
-    auto wait_copy = [&]() -> const unsigned char* {
-        if (!__all_sync(0xffffffffu, mbar_wait_bounded(bars + wait_slot, wait_parity, abort_flag))) gone = true;
-        const unsigned char* at = ring + wait_slot * kStageBytes;
-        if (++wait_slot == depth) {
-            wait_slot = 0;
-            wait_parity ^= 1;
-        }
-        return at;
-    };
-    copy_ahead(0);
-
-    double inv = 0.0;                               // warp 0: 1 / norm, 0 where nothing counts
-    if (MODE != kClassLogp && warp == 0) {
-        double n = p.norm;
-        if (n == 0.0 && p.order) n = p.prep->norm;
-        if (n == 0.0 && !p.order) {                 // few rows: every CTA adds their weights up
-            for (long long t = lane; t < p.T; t += 32) {
-                long long target;
-                float w;
-                if (class_counts(p, t, MODE, &target, &w)) n += w;
-            }
-            n = warp_sum64(n);
-        }
-        inv = n == 0.0 ? 0.0 : 1.0 / n;
-    }
-    long long from = 0, to = p.T;
-    if (MODE == kClassLogp && !p.order && p.offsets) {
-        from = load_any_id(p.offsets, p.wide_offsets, 0);
-        to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
-    }
-    double sums[3] = {0.0, 0.0, 0.0};
-    int turn = 0;
-    for (int k = 0; k < mine; ++k) {
-        if ((k >> 5) != block) {
-            ++block;
-            order0 = order1;
-            order1 = fetch(block + 1);
-        }
-        copy_ahead(k);                              // (a warp without a stage of the rows before gives nothing back)
-        const long long t = row_of(k);
-        const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
-        WarpRow<E> own;
-        own.set(p, t, gw, tw);
-        long long target = 0;
-        float w = 1.0f;
-        bool counts = true;
-        if (p.order) {
-            if (p.weights) w = __ldg(p.weights + t);
-            if (MODE != kClassDistill) target = load_any_id(p.ids, p.wide_ids, t);
-        } else {
-            counts = class_counts(p, t, MODE, &target, &w);
-            if (MODE == kClassLogp) counts = counts && t >= from && t < to;
-        }
-        const bool edges = gw == 0 && lane < row.edges;
-        float xy = 0.0f, edge = 0.0f;
-        if (counts) {
-            if (MODE != kClassDistill && tid == 0) xy = load_local(row.x + target);
-            if (edges) edge = load_local(row.x + row.edge(lane));
-        }
-        float largest = -INFINITY;
-        if (MODE == kClassDistill && counts) {
-            bool twice = false;
-            for (int j = tid; j < p.K; j += threads) {
-                const ClassEntry e = class_entry(p, t, j);
-                const int id = class_entry_id(p, e);
-                if (id >= 0) largest = fmaxf(largest, e.v);
-                twice |= class_entry_put(top, j, id, e.v, id >= 0 ? load_local(row.x + id) : 0.0f);
-            }
-            if (twice) top.twice[turn] = 1;
-            class_top_warp(p, t, top, largest);
-        }
-        ClassSum sum;
-        const int dropped = GRAD ? max(0, own.stages - depth) : own.stages;
-        for (int i = 0; i < own.stages; ++i) {
-            const int left = min(kStageGroups, own.groups - (i * tw + gw) * kStageGroups) - lane;
-            const unsigned char* at = wait_copy();
-            uint4 raw[J];
-#pragma unroll
-            for (int j = 0; j < J; ++j) raw[j] = *reinterpret_cast<const uint4*>(at + (lane + 32 * j) * 16);
-            if (i < dropped) give_back(k);
-            if (left > 32 * (J - 1)) {
-                sum.add_groups<E, J>(raw, p.c);
-            } else {
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    const uint4 one[1] = {raw[j]};
-                    if (32 * j < left) sum.add_groups<E, 1>(one, p.c);
-                }
-            }
-        }
-        if (edges) sum.add(edge, p.c);
-        class_sum_cta(sum, slot[turn]);
-        bool stop = *abort_flag != 0;
-        if (C > 1) {
-            if (tid < C) {
-                cluster_store_f32(&cta_slot[turn][rank][0], tid, sum.top);
-                cluster_store_f32(&cta_slot[turn][rank][1], tid, sum.m);
-                cluster_store_f32(&cta_slot[turn][rank][2], tid, sum.s);
-                cluster_store_f32(&cta_slot[turn][rank][3], tid, stop ? 1.0f : 0.0f);
-            }
-            cluster_barrier();
-            sum = ClassSum{};
-            stop = false;
-            for (int r = 0; r < C; ++r) {
-                sum.join(cta_slot[turn][r][0], cta_slot[turn][r][1], cta_slot[turn][r][2]);
-                stop = stop || cta_slot[turn][r][3] != 0.0f;
-            }
-        }
-        if (stop) {
-            gone = true;
-            break;
-        }
-        if (sum.top == -INFINITY) sum.m = 0.0f;     // no finite logit: s is 0 (or NaN)
-        if (MODE == kClassLogp) {
-            if (gw == 0 && lane == 0) {
-                if (counts) {
-                    const double lse2 = class_lse2(sum.m, sum.s), lp = class_logp(p, xy, sum.m, sum.s);
-                    if (p.logp) p.logp[t] = static_cast<float>(lp);
-                    if (p.lse) p.lse[t] = static_cast<float>(kLn2 * lse2);
-                    if (p.stat) {
-                        p.stat[t] = make_float2(sum.m, sum.s);
-                        p.logp64[t] = lp;
-                        p.coef[t] = 0.0f;
-                    }
-                } else {
-                    class_dead_row<MODE>(p, t);
-                }
-            }
-            turn ^= 1;
-            continue;
-        }
-        if (MODE == kClassPolicy && tid == 0) {
-            if (counts) {
-                const ClassNumbers r = class_policy_row(p, t, w, xy, sum.m, sum.s, inv, rank == 0);
-                now[0] = r.k;
-                now[1] = r.at;
-#pragma unroll
-                for (int i = 0; i < 3; ++i) sums[i] += r.sums[i];
-            } else if (rank == 0) {
-                class_dead_row<MODE>(p, t);
-            }
-        }
-        bool twice = false;
-        if (MODE == kClassDistill) {
-            twice = top.twice[turn] != 0;
-            if (counts && warp == 0) {
-                const bool here = lane < warps;
-                double base = here ? top.warp[lane][0] : -INFINITY, all = here ? top.warp[lane][1] : 0.0, cross = here ? top.warp[lane][2] : 0.0;
-                double most = base;
-#pragma unroll
-                for (int d = 16; d >= 1; d >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, d));
-                const double f = all == 0.0 ? 0.0 : exp2(base - most);
-                cross = warp_sum64(all == 0.0 ? 0.0 : f * (cross + (base - most) * all));
-                all = warp_sum64(f * all);
-                // with the teacher's own normalisation log2 q is smaller by log2(all)
-                const double one = p.teacher_lse || all == 0.0 ? 1.0 : 1.0 / all, mass = all * one;
-                if (here) top.part[lane] = static_cast<float>(f * one);
-                if (lane == 0) {
-                    double kl = 0.0;
-                    if (all != 0.0) kl = kLn2 * (cross * one + mass * (class_lse2(sum.m, sum.s) + log2(one)));
-                    if (p.row_kl && rank == 0) p.row_kl[t] = static_cast<float>(kl);
-                    sums[0] += w * kl;
-                    const double gain = w * inv * p.factor * p.scale;
-                    now[0] = static_cast<float>(mass == 0.0 ? 0.0 : gain * mass / sum.s);
-                    now[1] = static_cast<float>(gain);
-                }
-            } else if (!counts && rank == 0 && tid == 0) {
-                class_dead_row<MODE>(p, t);
-            }
-            // the table is empty again before the next row's classes come
-            for (int i = tid; i < top.size; i += threads) top.table[i] = -1;
-            if (tid == 0) top.twice[turn ^ 1] = 0;
-        }
-        turn ^= 1;
-        if (MODE == kClassDistill || GRAD) __syncthreads();
-        if (!GRAD) continue;
-        const float factor = counts ? now[0] : 0.0f, m = -sum.m;
-        const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), factor2 = f32x2_pack(factor, factor);
-        auto second = [&](int i, const unsigned char* at) {
-            const int first = (i * tw + gw) * kStageGroups, left = min(kStageGroups, own.groups - first) - lane;
-            uint4 raw[J];
-#pragma unroll
-            for (int j = 0; j < J; ++j) raw[j] = *reinterpret_cast<const uint4*>(at + (lane + 32 * j) * 16);
-            give_back(k);
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                if (32 * j >= left) break;
-                uint64_t v[G::P];
-#pragma unroll
-                for (int e = 0; e < G::P; ++e) v[e] = counts ? f32x2_mul(exp2_pair(G::pair(raw[j], e), c2, m2), factor2) : 0;
-                row.store(first + lane + 32 * j, v);
-            }
-        };
-        for (int i = dropped; i < own.stages; ++i) second(i, ring + out_slot * kStageBytes);
-        for (int i = 0; i < dropped; ++i) second(i, wait_copy());
-        if (edges) store_from_float(row.dx + row.edge(lane), counts ? exp2_fast(fmaf(edge, p.c, m)) * factor : 0.0f);
-        if (!counts) continue;
-        __syncwarp();                               // the targets' values replace what was just written, by the warp that wrote it
-        auto owner = [&](int column) {
-            const int g = column - row.head;
-            return g < 0 || g >= row.groups * N ? 0 : (g / (N * kStageGroups)) % tw;
-        };
-        if (MODE == kClassPolicy) {
-            if (lane == 0 && owner(int(target)) == gw) store_from_float(row.dx + target, now[1]);
-        } else {
-            const float gain = now[1];
-            for (int j = lane; j < p.K; j += 32) {
-                const int id = top.id[j];
-                if (id < 0 || owner(id) != gw) continue;
-                float weight = top.q[j] * top.part[(j % threads) >> 5];
-                if (twice) {                        // a class that the teacher names twice has both weights
-                    weight = 0.0f;
-                    for (int i = 0; i < p.K; ++i)
-                        if (top.id[i] == id) weight += top.q[i] * top.part[(i % threads) >> 5];
-                }
-                store_from_float(row.dx + id, fmaf(exp2_fast(fmaf(top.x[j], p.c, m)), factor, -gain * weight));
-            }
-            __syncthreads();                        // the next row's classes replace these
-        }
-    }
-    if (gone) {
-        // the copies in flight have to land before the shared memory is given up
-        for (; taken > 0; --taken) {
-            mbar_wait_drain(bars + out_slot, out_parity);
-            if (++out_slot == depth) {
-                out_slot = 0;
-                out_parity ^= 1;
-            }
-        }
-        if (tid == 0) atomicExch(p.timeout, kStatusTimeout);
-    }
-    // gradients of rows that do not count
-    if (GRAD && p.order) {
-        for (long long k = live + q; k < p.T; k += Q) {
-            const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, __ldg(p.order + k), p.V);
-            const uint64_t zero[G::P] = {};
-            for (int g = rank * threads + tid; g < row.groups; g += C * threads) row.store(g, zero);
-            if (gw == 0 && lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
-        }
-    }
-    if (MODE == kClassLogp || rank != 0) return;
-    // the CTA that is done last adds the CTAs' sums up, in a fixed order
-    if (tid == 0) {
-        for (int i = 0; i < 3; ++i) p.cta_sum[3 * q + i] = sums[i];
+        for (int i = 0; i < 3; ++i) p.cta_sum[3 * me + i] = sums[i];
         __threadfence();
-        last_cta = atomicAdd(p.words, 1u) == unsigned(Q) - 1;
+        last = atomicAdd(p.words, 1u) == unsigned(ctas) - 1;
     }
-    __syncthreads();
-    if (!last_cta || warp != 0) return;
+    if (!__shfl_sync(0xffffffffu, last, 0)) return;
     __threadfence();
     for (int i = 0; i < 3; ++i) {
         sums[i] = 0.0;
-        for (int r = lane; r < Q; r += 32) sums[i] += __ldcg(p.cta_sum + 3 * r + i);
+        for (int r = lane; r < ctas; r += 32) sums[i] += __ldcg(p.cta_sum + 3 * r + i);
         sums[i] = warp_sum64(sums[i]) * inv;
     }
     if (lane == 0) {
@@ -886,8 +618,428 @@ __global__ void __launch_bounds__(kRingThreads, 2) k_class_rows(const __grid_con
     }
 }
 
+// ---- long rows -----------------------------------------------------------------------------------------
+// A CTA per row, or a cluster of C.  Its warps have different work, and hand rows to each other through mbarriers:
+//   one warp copies a row's 16-byte groups, in stages of 32 KB, into a ring of shared memory, as far ahead as the ring allows, over the ends of
+//     rows too;
+//   sixteen warps go through the stages: first pass (running maximum and sum) of row k, then second pass (the gradient) of row k - lag, so
+//     that they do not wait for a row's numbers;
+//   kNumberWarps warps take turns at the rows: they fetch what a row has beside its logits, join the sums of the sixteen warps (and of the
+//     cluster's CTAs, by 16-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
+// The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that (lag + 1) rows fit, lag >= 1.
+// For the longest rows lag is 0, and stages that the ring could not hold are copied once more (`dropped`).  Stages are given back in the order
+// of the copies.
+constexpr int kPassWarps = 16;
+constexpr int kNumberWarps = 4;
+constexpr int kRingThreads = 32 * (kPassWarps + 1 + kNumberWarps);
+constexpr int kLaneGroups = 4;                      // of a stage
+constexpr int kWarpGroups = 32 * kLaneGroups;
+constexpr int kStageGroups = kPassWarps * kWarpGroups;
+constexpr int kStageBytes = kStageGroups * 16;
+constexpr int kRingDepth = 6;
+constexpr int kMaxCluster = 8;
+constexpr int kRows = 4;                            // rows under way between the warps; a multiple of kNumberWarps, above the largest lag
+constexpr int kMaxLag = kRows - 1;
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// Two floats into the same place of another CTA's shared memory; 8 bytes are counted on its barrier
+__device__ __forceinline__ void send_f32x2(const float2* local, const uint64_t* bar, uint32_t rank, float a, float b) {
+    uint32_t to, to_bar;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_u32(local)), "r"(rank));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to_bar) : "r"(smem_u32(bar)), "r"(rank));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];"
+                 ::"r"(to), "f"(a), "f"(b), "r"(to_bar)
+                 : "memory");
+}
+
+struct alignas(16) RingShared {
+    uint64_t full[kRingDepth], free[kRingDepth];
+    // of row k, at k mod kRows: the sixteen warps' sums are there; the row's numbers are there; its gradient is written
+    uint64_t summed[kRows], ready[kRows], written[kRows];
+    // the cluster's sums, twice as many rows: a CTA that is ahead sends row k + kRows before this one has looked at row k, but not row
+    // k + 2 kRows, for which it needs this CTA's row k + kRows, which the warp that looks at row k sends later
+    uint64_t joined[2 * kRows];
+    float2 cta_sum[2 * kRows][kMaxCluster];
+    float2 warp_sum[kRows][kPassWarps];             // largest logit, sum
+    float4 row[kRows];                              // factor, m, 1 where the row counts
+    int abort_word;
+};
+
+template <class E, int MODE, bool GRAD>
+__global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_constant__ ClassParams p) {
+    using G = ClassGroup<E>;
+    constexpr int N = G::N, J = kLaneGroups;
+    __shared__ RingShared sh;
+    extern __shared__ __align__(128) unsigned char class_smem[];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, depth = p.depth, lag = p.lag;
+    const int C = p.cluster, rank = C > 1 ? int(cluster_rank()) : 0, q = blockIdx.x / C, Q = gridDim.x / C;
+    volatile int* abort_flag = &sh.abort_word;
+    if (tid == 0) {
+        sh.abort_word = 0;
+        for (int i = 0; i < kRingDepth; ++i) {
+            mbar_init(sh.full + i, 1);
+            mbar_init(sh.free + i, kPassWarps);
+        }
+        for (int i = 0; i < kRows; ++i) {
+            mbar_init(sh.summed + i, kPassWarps);
+            mbar_init(sh.ready + i, 1);
+            mbar_init(sh.written + i, kPassWarps);
+        }
+        for (int i = 0; i < 2 * kRows; ++i) mbar_init(sh.joined + i, 1);
+        fence_mbar_init();
+    }
+    __syncthreads();
+    if (C > 1) cluster_barrier();                   // who writes into another CTA's shared memory has to find it started
+    grid_dependency_wait();
+    const int live = p.order ? p.prep->live : int(p.T);
+    const int mine = live > q ? (live - q + Q - 1) / Q : 0;
+    auto row_of = [&](int k) -> int {
+        const long long at = q + static_cast<long long>(k) * Q;
+        return k < mine ? (p.order ? __ldg(p.order + at) : static_cast<int>(at)) : 0;
+    };
+    auto stages_of = [&](int groups) {              // of this CTA: every C-th
+        const int all = (groups + kStageGroups - 1) / kStageGroups;
+        return all > rank ? (all - rank + C - 1) / C : 0;
+    };
+    if (warp == kPassWarps) {
+        if (lane == 0) {
+            const uint64_t once = l2_policy_evict_first();
+            int slot = 0, parity = 0, copies = 0;
+            bool ok = true;
+            int t = row_of(0);
+            for (int k = 0; k < mine && ok; ++k) {
+                const ClassRow<E> row(p.x, p.ld, nullptr, 0, t, p.V);
+                t = row_of(k + 1);
+                const int stages = stages_of(row.groups), again = GRAD ? max(0, stages - depth) : 0;
+                for (int i = 0; i < stages + again; ++i) {
+                    const int first = ((i < stages ? i : i - stages) * C + rank) * kStageGroups;
+                    const uint32_t bytes = min(kStageGroups, row.groups - first) * 16;
+                    if (copies >= depth && !mbar_wait_bounded(sh.free + slot, parity ^ 1, abort_flag)) {
+                        ok = false;
+                        break;
+                    }
+                    fence_proxy_async_smem();
+                    mbar_arrive_expect_tx(sh.full + slot, bytes);
+                    bulk_copy_g2s(class_smem + slot * kStageBytes, row.x + row.head + static_cast<long long>(first) * N, bytes, sh.full + slot, once);
+                    if (copies < depth) ++copies;
+                    if (++slot == depth) {
+                        slot = 0;
+                        parity ^= 1;
+                    }
+                }
+            }
+            // whatever happened, the copies have to land before the shared memory is given up
+            for (; copies > 0; --copies) {
+                if (slot == 0) {
+                    slot = depth;
+                    parity ^= 1;
+                }
+                mbar_wait_drain(sh.full + --slot, parity);
+            }
+        }
+    } else if (warp < kPassWarps) {
+        int out_slot = 0, wait_slot = 0, wait_parity = 0;
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, int parity) {
+            if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag))) ok = false;
+        };
+        auto read_stage = [&](int at, uint4 (&raw)[J]) {
+            const unsigned char* from = class_smem + at * kStageBytes + (warp * kWarpGroups + lane) * 16;
+#pragma unroll
+            for (int j = 0; j < J; ++j) raw[j] = *reinterpret_cast<const uint4*>(from + j * 512);
+        };
+        auto wait_copy = [&]() {
+            wait(sh.full + wait_slot, wait_parity);
+            const int at = wait_slot;
+            if (++wait_slot == depth) {
+                wait_slot = 0;
+                wait_parity ^= 1;
+            }
+            return at;
+        };
+        auto give_back = [&]() {                    // what is in registers now may be overwritten
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.free + out_slot);
+            if (++out_slot == depth) out_slot = 0;
+        };
+        int t_first = row_of(0), t_second = t_first;
+        for (int step = 0; step < mine + lag && ok; ++step) {
+            if (step < mine) {
+                const ClassRow<E> row(p.x, p.ld, nullptr, 0, t_first, p.V);
+                t_first = row_of(step + 1);
+                const int stages = stages_of(row.groups), dropped = GRAD ? max(0, stages - depth) : stages;
+                ClassSum sum;
+                for (int i = 0; i < stages; ++i) {
+                    const int left = row.groups - (i * C + rank) * kStageGroups - warp * kWarpGroups;
+                    uint4 raw[J];
+                    read_stage(wait_copy(), raw);
+                    if (i < dropped) give_back();
+                    if (left >= kWarpGroups) {
+                        sum.add_groups<E, J>(raw, p.c);
+                    } else if (left > 0) {
+#pragma unroll
+                        for (int j = 0; j < J; ++j) {
+                            const uint4 one[1] = {raw[j]};
+                            if (32 * j + lane < left) sum.add_groups<E, 1>(one, p.c);
+                        }
+                    }
+                }
+                sum.over_warp(p.c);
+                if (lane == 0) {
+                    sh.warp_sum[step % kRows][warp] = make_float2(sum.top, sum.s);
+                    mbar_arrive(sh.summed + step % kRows);
+                }
+            }
+            const int k = step - lag;
+            if (k < 0 || !ok) continue;
+            wait(sh.ready + k % kRows, (k / kRows) & 1);
+            if (!GRAD || !ok) continue;
+            const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t_second, p.V);
+            t_second = row_of(k + 1);
+            const int stages = stages_of(row.groups), dropped = max(0, stages - depth);
+            const float4 numbers = sh.row[k % kRows];
+            const bool counts = numbers.z != 0.0f;
+            const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(-numbers.y, -numbers.y), factor2 = f32x2_pack(numbers.x, numbers.x);
+            auto second = [&](int i, int at) {
+                const int first = (i * C + rank) * kStageGroups + warp * kWarpGroups, left = row.groups - first;
+                uint4 raw[J];
+                read_stage(at, raw);
+                give_back();
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    if (32 * j + lane < left) {
+                        uint64_t v[G::P];
+#pragma unroll
+                        for (int e = 0; e < G::P; ++e) v[e] = counts ? f32x2_mul(G::power(raw[j], e, c2, m2), factor2) : 0;
+                        row.store(first + lane + 32 * j, v);
+                    }
+                }
+            };
+            for (int i = dropped; i < stages; ++i) second(i, out_slot);
+            for (int i = 0; i < dropped; ++i) second(i, wait_copy());
+            __syncwarp();
+            if (lane == 0) mbar_arrive(sh.written + k % kRows);
+        }
+        // gradients of rows that do not count
+        if (GRAD && p.order) {
+            for (long long k = live + q; k < p.T; k += Q) {
+                const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, __ldg(p.order + k), p.V);
+                const uint64_t zero[G::P] = {};
+                for (int g = rank * (32 * kPassWarps) + tid; g < row.groups; g += C * (32 * kPassWarps)) row.store(g, zero);
+                if (rank == 0 && tid < row.edges) store_from_float(row.dx + row.edge(tid), 0.0f);
+            }
+        }
+    } else {
+        const int h = warp - kPassWarps - 1;
+        ClassTop top{};
+        if (MODE == kClassDistill) {
+            top = class_top_at(class_smem + depth * kStageBytes + h * class_top_bytes(p.K), p.K);
+            class_clear_marks(top);
+        }
+        double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
+        if (MODE != kClassLogp) {
+            double n = p.norm;
+            if (n == 0.0) n = p.order ? p.prep->norm : class_norm_warp<MODE>(p);
+            inv = n == 0.0 ? 0.0 : 1.0 / n;
+        }
+        long long from = 0, to = p.T;
+        if (MODE == kClassLogp && !p.order && p.offsets) {
+            from = load_any_id(p.offsets, p.wide_offsets, 0);
+            to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+        }
+        bool ok = true;
+        auto wait = [&](uint64_t* bar, int parity) {
+            if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag))) ok = false;
+            return ok;
+        };
+        for (int k = h; k < mine; k += kNumberWarps) {
+            const long long t = row_of(k);
+            const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
+            ClassInputs in{};
+            bool counts = class_counts(p, t, MODE, &in.target, &in.w);
+            if (MODE == kClassLogp) counts = counts && t >= from && t < to;
+            const bool edges = rank == 0 && lane < row.edges;
+            const float edge = counts && edges ? load_local(row.x + row.edge(lane)) : 0.0f;
+            if (counts) class_inputs<MODE>(p, t, row.x, top, in);
+            const int at = k % kRows, parity = (k / kRows) & 1;
+            if (!wait(sh.summed + at, parity)) break;
+            ClassSum sum;
+            if (lane < kPassWarps) sum.set(sh.warp_sum[at][lane].x, sh.warp_sum[at][lane].y, p.c);
+            if (edges) sum.add(edge, p.c);
+            sum.over_warp(p.c);
+            if (C > 1) {
+                const int at2 = k % (2 * kRows);
+                if (lane == 0) mbar_arrive_expect_tx(sh.joined + at2, 8 * C);
+                __syncwarp();
+                if (lane < C) send_f32x2(&sh.cta_sum[at2][rank], sh.joined + at2, lane, sum.top, sum.s);
+                if (!wait(sh.joined + at2, (k / (2 * kRows)) & 1)) break;
+                sum = ClassSum{};
+                if (lane < C) sum.set(sh.cta_sum[at2][lane].x, sh.cta_sum[at2][lane].y, p.c);
+                sum.over_warp(p.c);
+            }
+            sum.settle();
+            ClassNumbers now{};
+            if (counts) now = class_numbers<MODE>(p, t, in, sum, inv, rank == 0, sums);
+            else if (rank == 0 && lane == 0) class_dead_row<MODE>(p, t);
+            if (lane == 0) {
+                if (GRAD) sh.row[at] = make_float4(now.factor, sum.m, counts ? 1.0f : 0.0f, 0.0f);
+                mbar_arrive(sh.ready + at);
+            }
+            if (!GRAD) continue;
+            if (edges) store_from_float(row.dx + row.edge(lane), counts ? exp2_fast(fmaf(edge, p.c, -sum.m)) * now.factor : 0.0f);
+            // the values at the targets replace what the passes have written, in this CTA's stages
+            if (!wait(sh.written + at, parity)) break;
+            if (!counts) continue;
+            auto here = [&](int column) {
+                const int g = (column - row.head) / N;
+                return column < row.head || g >= row.groups ? rank == 0 : (g / kStageGroups & (C - 1)) == rank;
+            };
+            if (MODE == kClassPolicy) {
+                __syncwarp();
+                if (lane == 0 && here(int(in.target))) store_from_float(row.dx + in.target, now.at);
+            } else {
+                __syncwarp();
+                for (int j = lane; j < p.K; j += 32)
+                    if (top.id[j] >= 0 && here(top.id[j])) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, in.top.twice, sum.m, now));
+                __syncwarp();
+            }
+        }
+        if (MODE != kClassLogp && rank == 0) class_finish<MODE>(p, q * kNumberWarps + h, Q * kNumberWarps, inv, sums);
+    }
+    __syncwarp();
+    if (C > 1) cluster_barrier();                   // what was sent has arrived before a CTA's shared memory is given up
+    if (tid == 0 && *abort_flag) atomicExch(p.timeout, kStatusTimeout);
+}
+
+// ---- short rows ----------------------------------------------------------------------------------------
+// A warp per row, the row in its registers between the passes: no barrier, no shared memory but for a teacher's classes.
+constexpr int kShortWarps = 8;
+
+template <class E, int MODE, bool GRAD, int J>
+__global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_constant__ ClassParams p) {
+    using G = ClassGroup<E>;
+    __shared__ double cta_part[kShortWarps][3];
+    extern __shared__ __align__(128) unsigned char class_smem[];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    ClassTop top{};
+    if (MODE == kClassDistill) {
+        top = class_top_at(class_smem + warp * class_top_bytes(p.K), p.K);
+        class_clear_marks(top);
+    }
+    grid_dependency_wait();
+    long long from = 0, to = p.T;
+    if (MODE == kClassLogp && p.offsets) {
+        from = load_any_id(p.offsets, p.wide_offsets, 0);
+        to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+    }
+    double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
+    if (MODE != kClassLogp) {
+        double n = p.norm;
+        if (n == 0.0 && p.norm_parts > 0)
+            for (int i = 0; i < p.norm_parts; ++i) n += __ldcg(p.norm_part + i);
+        else if (n == 0.0) n = class_norm_warp<MODE>(p);
+        inv = n == 0.0 ? 0.0 : 1.0 / n;
+    }
+    for (long long t = static_cast<long long>(blockIdx.x) * kShortWarps + warp; t < p.T; t += static_cast<long long>(gridDim.x) * kShortWarps) {
+        const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
+        ClassInputs in{};
+        bool counts = class_counts(p, t, MODE, &in.target, &in.w);
+        if (MODE == kClassLogp) counts = counts && t >= from && t < to;
+        if (!counts) {
+            if (GRAD) {
+                const uint64_t zero[G::P] = {};
+                for (int g = lane; g < row.groups; g += 32) row.store(g, zero);
+                if (lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
+            }
+            if (lane == 0) class_dead_row<MODE>(p, t);
+            continue;
+        }
+        uint4 raw[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (32 * j + lane < row.groups) raw[j] = row.load(32 * j + lane);
+        float edge = 0.0f;
+        if (lane < row.edges) edge = load_local(row.x + row.edge(lane));
+        class_inputs<MODE>(p, t, row.x, top, in);
+        ClassSum sum;
+        if (row.groups >= 32 * J) {
+            sum.add_groups<E, J>(raw, p.c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const uint4 one[1] = {raw[j]};
+                if (32 * j + lane < row.groups) sum.add_groups<E, 1>(one, p.c);
+            }
+        }
+        if (lane < row.edges) sum.add(edge, p.c);
+        sum.over_warp(p.c);
+        sum.settle();
+        const ClassNumbers now = class_numbers<MODE>(p, t, in, sum, inv, true, sums);
+        if (!GRAD) continue;
+        const float m = -sum.m;
+        const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), factor2 = f32x2_pack(now.factor, now.factor);
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (32 * j + lane < row.groups) {
+                uint64_t v[G::P];
+#pragma unroll
+                for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(G::power(raw[j], e, c2, m2), factor2);
+                row.store(32 * j + lane, v);
+            }
+        }
+        if (lane < row.edges) store_from_float(row.dx + row.edge(lane), exp2_fast(fmaf(edge, p.c, m)) * now.factor);
+        __syncwarp();                               // the targets' values replace what was just written
+        if (MODE == kClassPolicy) {
+            if (lane == 0) store_from_float(row.dx + in.target, now.at);
+        } else {
+            for (int j = lane; j < p.K; j += 32)
+                if (top.id[j] >= 0) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, in.top.twice, sum.m, now));
+            __syncwarp();
+        }
+    }
+    if (MODE == kClassLogp) return;
+    if (lane == 0)
+        for (int i = 0; i < 3; ++i) cta_part[warp][i] = sums[i];
+    __syncthreads();
+    if (warp != 0) return;
+    for (int i = 0; i < 3; ++i) {
+        sums[i] = 0.0;
+        for (int w = 0; w < kShortWarps; ++w) sums[i] += cta_part[w][i];
+    }
+    class_finish<MODE>(p, blockIdx.x, gridDim.x, inv, sums);
+}
+
+// norm_part[b] = sum of the weights of the rows that count among rows b * kNormRows ...
+constexpr int kNormThreads = 256;
+constexpr int kNormRows = 4096;
+
+template <int MODE>
+__global__ void __launch_bounds__(kNormThreads) k_class_norm(const __grid_constant__ ClassParams p, double* part) {
+    __shared__ double warp_part[kNormThreads / 32];
+    grid_dependency_release();
+    const long long first = static_cast<long long>(blockIdx.x) * kNormRows, last = min(first + kNormRows, p.T);
+    double sum = 0.0;
+    for (long long t = first + threadIdx.x; t < last; t += kNormThreads) {
+        long long target;
+        float w;
+        if (class_counts(p, t, MODE, &target, &w)) sum += w;
+    }
+    sum = warp_sum64(sum);
+    if ((threadIdx.x & 31) == 0) warp_part[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sum = 0.0;
+        for (int w = 0; w < kNormThreads / 32; ++w) sum += warp_part[w];
+        part[blockIdx.x] = sum;
+    }
+}
+
 // ---- gradient of log-probabilities ---------------------------------------------------------------------
-// Rows whose statistics are known: from the caller (lse, fp32) or from k_class_rows (m and s).  One read, one write.
+// Rows whose statistics are known: from the caller (lse, fp32) or from an earlier pass (m and s).  One read, one write.
 struct ClassGradParams {
     const void* x;
     long long ld;
@@ -905,56 +1057,83 @@ struct ClassGradParams {
     long long ld_d;
     int* status;                 // NULL: targets outside the classes have been reported
     int slices;                  // of a row
-    int slice_groups;
     int backwards;               // from the last row on: what was read last may still be in L2
 };
 
 constexpr int kClassGradThreads = 256;
+#ifndef GU
+#define GU 4
+#endif
+constexpr int kClassGradGroups = GU;                // per thread, all on their way before the first is worked on
 
 template <class E>
 __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_constant__ ClassGradParams p) {
     using G = ClassGroup<E>;
-    constexpr int N = G::N;
+    constexpr int N = G::N, U = kClassGradGroups;
     const int tid = threadIdx.x, threads = blockDim.x;
     grid_dependency_wait();
     const long long items = p.T * p.slices;
+    struct Numbers {             // of a row
+        long long target;
+        float g;
+        float2 stat;
+    };
+    auto row_of = [&](long long item) { return (p.backwards ? items - 1 - item : item) / p.slices; };
+    auto fetch = [&](long long item) {
+        Numbers n{};
+        if (item < items) {
+            const long long t = row_of(item);
+            n.target = load_any_id(p.ids, p.wide_ids, t);
+            n.g = p.g[t];
+            n.stat = p.stat ? p.stat[t] : make_float2(p.lse[t], 0.0f);
+        }
+        return n;
+    };
+    Numbers next = fetch(blockIdx.x);
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
-        const long long i = p.backwards ? items - 1 - item : item, t = i / p.slices;
-        const int slice = static_cast<int>(i - t * p.slices);
+        const Numbers now = next;
+        next = fetch(item + gridDim.x);
+        const long long t = row_of(item);
+        const int slice = static_cast<int>((p.backwards ? items - 1 - item : item) - t * p.slices);
         const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
-        const long long target = load_any_id(p.ids, p.wide_ids, t);
-        const float gt = p.g[t] * p.scale;
-        bool live = target != p.ignore && gt != 0.0f;
-        if (target != p.ignore && (target < 0 || target >= p.V)) {
+        const float gt = now.g * p.scale;
+        bool live = now.target != p.ignore && gt != 0.0f;
+        if (now.target != p.ignore && (now.target < 0 || now.target >= p.V)) {
             live = false;
             if (p.status && tid == 0) atomicExch(p.status, -4);
         }
-        const int end = min((slice + 1) * p.slice_groups, row.groups);
-        int g = slice * p.slice_groups + tid;
+        const int first = slice * threads * U + tid;
         const bool edges = slice == 0 && tid < row.edges;
         if (!live) {
             const uint64_t zero[G::P] = {};
-            for (; g < end; g += threads) row.store(g, zero);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (first + u * threads < row.groups) row.store(first + u * threads, zero);
             if (edges) store_from_float(row.dx + row.edge(tid), 0.0f);
             continue;
         }
+        uint4 raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (first + u * threads < row.groups) raw[u] = row.load(first + u * threads);
         float m, k;
         if (p.stat) {
-            const float2 st = p.stat[t];
-            m = -st.x;
-            k = -gt / st.y;
+            m = -now.stat.x;
+            k = -gt / now.stat.y;
         } else {                                    // lse in the units of c, the part below fp32 put into the factor
-            const double l2 = static_cast<double>(p.lse[t]) * (static_cast<double>(p.c) / p.scale);
+            const double l2 = static_cast<double>(now.stat.x) * (static_cast<double>(p.c) / p.scale);
             m = -static_cast<float>(l2);
             k = -gt * exp2_fast(static_cast<float>(-static_cast<double>(m) - l2));
         }
-        const int where = static_cast<int>(target) - row.head;
+        const int where = static_cast<int>(now.target) - row.head;
         const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), k2 = f32x2_pack(k, k);
-        for (; g < end; g += threads) {
-            const uint4 raw = row.load(g);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int g = first + u * threads;
+            if (g >= row.groups) break;
             uint64_t v[G::P];
 #pragma unroll
-            for (int j = 0; j < G::P; ++j) v[j] = f32x2_mul(exp2_pair(G::pair(raw, j), c2, m2), k2);
+            for (int j = 0; j < G::P; ++j) v[j] = f32x2_mul(exp2_pair(G::pair(raw[u], j), c2, m2), k2);
             if (where >= g * N && where < g * N + N) {
 #pragma unroll
                 for (int j = 0; j < G::P; ++j) {
@@ -967,7 +1146,7 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
         if (edges) {
             const int at = row.edge(tid);
             const float v = exp2_fast(fmaf(load_local(row.x + at), p.c, m)) * k;
-            store_from_float(row.dx + at, at == target ? v + gt : v);
+            store_from_float(row.dx + at, at == now.target ? v + gt : v);
         }
     }
 }

@@ -3,6 +3,7 @@
 #include "../../include/lrgd.h"
 
 #include <cmath>
+#include <type_traits>
 
 #include "lrgd_class.cuh"
 #include "lrgd_scratch.cuh"
@@ -13,6 +14,8 @@ namespace {
 
 template <class E, int MODE, bool GRAD>
 struct ClassRowsTag {};
+template <class E, int MODE, bool GRAD, int J>
+struct ClassShortTag {};
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
 constexpr int64_t kMaxClasses = int64_t(1) << 24;
@@ -42,46 +45,93 @@ bool apart(const E* x, int64_t ld, const E* dx, int64_t ld_d, int64_t T, int64_t
     return off >= V * es && off + V * es <= pitch;
 }
 
-constexpr int kRingStages = 96;                     // of an SM's shared memory (192 KB), shared by its CTAs
+constexpr int kShortGroups = 16;                    // 16-byte groups per lane of the short rows, at most
+constexpr int kNormInline = 512;                    // rows whose weights every warp adds up for itself
 
-// CTAs for the rows: `warps` each, `cluster` to a row, `ctas` in all.  Rows that fill the SMs have one CTA each of as many warps as there are
-// pairs of stages in a row, up to 32 warps an SM; fewer rows are split over clusters until every stage has a warp of its own.
+// How rows are worked on: a warp each (groups per lane: 1, 2, 4, 8 or 16), or by CTAs with rings, `cluster` to a row.
 struct RowPlan {
-    int warps, cluster, ctas, depth;
+    int lane_groups;             // 0: rings
+    int cluster, lag;            // (see k_class_ring)
 };
-RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es) {
-    const int64_t stages = std::max<int64_t>(1, (V * es / 16 + kStageGroups - 1) / kStageGroups);
-    const int sms = plan_sms(ctx);
-    RowPlan r{};
-    r.cluster = 1;
-    while (r.cluster < kMaxCluster && r.cluster * 2 * T <= sms && r.cluster * 2 <= stages) r.cluster *= 2;
-    const int64_t want = r.cluster > 1 ? (stages + r.cluster - 1) / r.cluster : (stages + 1) / 2;
-    r.warps = 1;
-    while (r.warps < kRingThreads / 32 && r.warps < want) r.warps *= 2;
-    const int per_sm = 32 / r.warps;
-    r.depth = kRingStages / 32;
-    r.ctas = int(std::max<int64_t>(1, std::min<int64_t>(T, int64_t(sms) * per_sm / r.cluster))) * r.cluster;
+RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es, bool grad, int depth) {
+    const int64_t groups = V * es / 16, sms = plan_sms(ctx);
+    RowPlan r{0, 1, 0};
+    if (groups <= 32 * kShortGroups) {
+        for (r.lane_groups = 1; 32 * r.lane_groups < groups;) r.lane_groups *= 2;
+        return r;
+    }
+    // Of the logits' stages (one more of each CTA's where rows start at different offsets) two rows have to be in a ring together, or as many
+    // CTAs take a row as there are SMs for, if rows are few
+    const int64_t stages = (groups + kStageGroups - 1) / kStageGroups;
+    auto per_cta = [&] { return (stages + r.cluster - 1) / r.cluster; };
+    while (r.cluster < kMaxCluster && ((grad && 2 * per_cta() > depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
+    const int64_t n = per_cta();
+    r.lag = !grad ? kMaxLag : 2 * n > depth ? 0 : int(std::max<int64_t>(1, std::min<int64_t>(kMaxLag, depth / n - 2)));
     return r;
 }
 
-// Scratch of k_class_rows and k_class_prep: sums of the CTAs, the order of the rows
+// Scratch of the row kernels: sums of the CTAs, the order of the rows or parts of the sum of weights
 struct RowScratch {
     size_t sums, prep, order;
     size_t bytes() const { return sums + prep + order; }
 };
-RowScratch row_scratch(const RowPlan& plan, int64_t T) {
-    return {up256(size_t(plan.ctas / plan.cluster) * 3 * sizeof(double)), up256(sizeof(ClassPrep)), up256(size_t(T) * sizeof(int))};
+RowScratch row_scratch(const lr_ctx* ctx, int64_t T) {
+    return {up256(size_t(ctx->sm_count) * 8 * 3 * sizeof(double)), up256(sizeof(ClassPrep)), up256(size_t(T) * sizeof(int) + 8)};
 }
 
-template <class E, int MODE>
-int launch_rows(lr_ctx* ctx, ClassParams& p, const RowPlan& plan, const RowScratch& at, const Scratch& scratch, bool grad, cudaStream_t st) {
-    p.cluster = plan.cluster;
-    p.depth = plan.depth;
-    p.cta_sum = reinterpret_cast<double*>(scratch.data);
-    p.words = scratch.words;
-    p.timeout = ctx->d_status;
-    // with a row for every CTA the rows are looked at on the way
-    const bool prep = p.T > plan.ctas / plan.cluster && (MODE != kClassDistill || p.weights);
+// Clusters of such a launch that are resident together (all CTAs have to be: rows are dealt out beforehand)
+template <class Tag>
+cudaError_t resident_clusters(const void* kern, const cudaLaunchConfig_t& cfg, int cluster, int* out) {
+    struct Known {
+        int device, cluster;
+        size_t smem;
+        int clusters;
+    };
+    static std::vector<Known> known;
+    static std::mutex mu;
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const std::lock_guard<std::mutex> hold(mu);
+    for (const Known& k : known)
+        if (k.device == device && k.cluster == cluster && k.smem == cfg.dynamicSmemBytes) {
+            *out = k.clusters;
+            return cudaSuccess;
+        }
+    e = cudaOccupancyMaxActiveClusters(out, kern, &cfg);
+    if (e != cudaSuccess) return e;
+    if (*out < 1) return cudaErrorNotSupported;
+    try {
+        known.push_back(Known{device, cluster, cfg.dynamicSmemBytes, *out});
+    } catch (const std::bad_alloc&) {               // asked again the next time
+    }
+    return cudaSuccess;
+}
+
+template <class E, int MODE, bool GRAD>
+int launch_ring(lr_ctx* ctx, ClassParams& p, const RowScratch& at, const Scratch& scratch, cudaStream_t st) {
+    using Tag = ClassRowsTag<E, MODE, GRAD>;
+    const auto kern = k_class_ring<E, MODE, GRAD>;
+    const size_t smem = size_t(p.depth) * kStageBytes + (MODE == kClassDistill ? kNumberWarps * class_top_bytes(p.K) : 0);
+    LR_CK(ctx, ensure_dynamic_smem<Tag>(reinterpret_cast<const void*>(kern), int(smem)));
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(kRingThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    cfg.attrs = attr;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(p.cluster);
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    cfg.gridDim = dim3(unsigned(ctx->sm_count / p.cluster * p.cluster));
+    LR_CK(ctx, resident_clusters<Tag>(reinterpret_cast<const void*>(kern), cfg, p.cluster, &clusters));
+    clusters = int(std::min<int64_t>(p.T, std::max<int64_t>(1, int64_t(clusters) * plan_sms(ctx) / ctx->sm_count)));
+    cfg.gridDim = dim3(unsigned(clusters * p.cluster));
+    // with a row for every cluster, or where all rows count, the rows are looked at on the way
+    const bool prep = p.T > clusters && (MODE != kClassDistill || p.weights);
     if (prep) {
         ClassPrep* out = reinterpret_cast<ClassPrep*>(scratch.data + at.sums);
         int* order = reinterpret_cast<int*>(scratch.data + at.sums + at.prep);
@@ -89,35 +139,62 @@ int launch_rows(lr_ctx* ctx, ClassParams& p, const RowPlan& plan, const RowScrat
         if (r != LR_OK) return r;
         p.prep = out;
         p.order = order;
+        if (ctx->overlap) {
+            attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr[1].val.programmaticStreamSerializationAllowed = 1;
+            cfg.numAttrs = 2;
+        }
     }
-    const size_t smem = size_t(plan.warps) * plan.depth * (kStageBytes + 8) + (MODE == kClassDistill ? class_top_bytes(p.K, plan.warps) : 0);
-    auto go = [&](auto kern, auto tag) -> int {
-        LR_CK(ctx, ensure_dynamic_smem<decltype(tag)>(reinterpret_cast<const void*>(kern), int(smem)));
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(plan.ctas);
-        cfg.blockDim = dim3(plan.warps * 32);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = st;
-        cudaLaunchAttribute attr[2];
-        if (plan.cluster > 1) {
-            attr[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
-            attr[cfg.numAttrs].val.clusterDim.x = unsigned(plan.cluster);
-            attr[cfg.numAttrs].val.clusterDim.y = 1;
-            attr[cfg.numAttrs++].val.clusterDim.z = 1;
-        }
-        if (prep && ctx->overlap) {
-            attr[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-            attr[cfg.numAttrs++].val.programmaticStreamSerializationAllowed = 1;
-        }
-        cfg.attrs = attr;
-        LR_CK(ctx, cudaLaunchKernelEx(&cfg, kern, p));
+    LR_CK(ctx, cudaLaunchKernelEx(&cfg, kern, p));
+    ctx->launches += 1;
+    return LR_OK;
+}
+
+template <class E, int MODE, bool GRAD>
+int launch_short(lr_ctx* ctx, ClassParams& p, int lane_groups, const RowScratch& at, const Scratch& scratch, cudaStream_t st) {
+    bool dependent = false;
+    if (MODE != kClassLogp && p.norm == 0.0 && p.T > kNormInline) {
+        double* part = reinterpret_cast<double*>(scratch.data + at.sums + at.prep);
+        p.norm_part = part;
+        p.norm_parts = int((p.T + kNormRows - 1) / kNormRows);
+        const int r = launched(ctx, [&] { k_class_norm<MODE><<<p.norm_parts, kNormThreads, 0, st>>>(p, part); });
+        if (r != LR_OK) return r;
+        dependent = ctx->overlap;
+    }
+    const size_t smem = MODE == kClassDistill ? kShortWarps * class_top_bytes(p.K) : 0;
+    const dim3 grid(even_grid(ctx, p.T, kShortWarps, 8));
+    auto go = [&](auto groups) -> int {
+        constexpr int J = decltype(groups)::value;
+        using Tag = ClassShortTag<E, MODE, GRAD, J>;
+        const auto kern = k_class_short<E, MODE, GRAD, J>;
+        LR_CK(ctx, ensure_dynamic_smem<Tag>(reinterpret_cast<const void*>(kern), int(smem)));
+        LR_CK(ctx, launch_kernel(kern, grid, dim3(kShortWarps * 32), smem, st, dependent, p));
         ctx->launches += 1;
         return LR_OK;
     };
-    if constexpr (MODE != kClassLogp) {
-        if (grad) return go(k_class_rows<E, MODE, true>, ClassRowsTag<E, MODE, true>{});
+    switch (lane_groups) {
+        case 1: return go(std::integral_constant<int, 1>{});
+        case 2: return go(std::integral_constant<int, 2>{});
+        case 4: return go(std::integral_constant<int, 4>{});
+        case 8: return go(std::integral_constant<int, 8>{});
+        default: return go(std::integral_constant<int, kShortGroups>{});
     }
-    return go(k_class_rows<E, MODE, false>, ClassRowsTag<E, MODE, false>{});
+}
+
+template <class E, int MODE, bool GRAD>
+int launch_rows(lr_ctx* ctx, ClassParams& p, const RowScratch& at, const Scratch& scratch, cudaStream_t st) {
+    p.cta_sum = reinterpret_cast<double*>(scratch.data);
+    p.words = scratch.words;
+    p.timeout = ctx->d_status;
+    constexpr size_t kSmem = 224 << 10;             // of an SM, for ring and teacher's classes
+    p.depth = kRingDepth;
+    if (MODE == kClassDistill)
+        while (p.depth > 1 && size_t(p.depth) * kStageBytes + kNumberWarps * class_top_bytes(p.K) > kSmem) --p.depth;
+    const RowPlan plan = plan_rows(ctx, p.T, p.V, sizeof(E), GRAD, p.depth);
+    p.cluster = plan.cluster;
+    p.lag = plan.lag;
+    if (plan.lane_groups > 0) return launch_short<E, MODE, GRAD>(ctx, p, plan.lane_groups, at, scratch, st);
+    return launch_ring<E, MODE, GRAD>(ctx, p, at, scratch, st);
 }
 
 template <class E>
@@ -140,9 +217,8 @@ ClassParams row_params(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, in
 template <class E>
 int launch_grad(lr_ctx* ctx, ClassGradParams& p, bool dependent, cudaStream_t st) {
     const int64_t groups = int64_t(p.V) * int64_t(sizeof(E)) / 16 + 1;
-    p.slice_groups = kClassGradThreads * 8;
-    p.slices = int((groups + p.slice_groups - 1) / p.slice_groups);
-    const int threads = int(std::max<int64_t>(32, std::min<int64_t>(kClassGradThreads, (groups + 31) / 32 * 32)));
+    const int threads = int(std::max<int64_t>(32, std::min<int64_t>(kClassGradThreads, (groups + 32 * kClassGradGroups - 1) / (32 * kClassGradGroups) * 32)));
+    p.slices = int((groups + threads * kClassGradGroups - 1) / (threads * kClassGradGroups));
     LR_CK(ctx, launch_kernel(k_class_grad<E>, dim3(grid_for(ctx, p.T * p.slices, 1, 2048 / threads)), dim3(threads), 0, st, dependent && ctx->overlap, p));
     ctx->launches += 1;
     return LR_OK;
@@ -165,12 +241,11 @@ int logp_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
     p.logp = d_logp;
     p.lse = d_lse;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const RowPlan plan = plan_rows(ctx, T, V, sizeof(E));
-    const RowScratch at = row_scratch(plan, T);
+    const RowScratch at = row_scratch(ctx, T);
     Scratch scratch{};
     const int rs = gate_scratch(ctx, at.bytes(), st, &scratch);
     if (rs != LR_OK) return rs;
-    return launch_rows<E, kClassLogp>(ctx, p, plan, at, scratch, false, st);
+    return launch_rows<E, kClassLogp, false>(ctx, p, at, scratch, st);
 }
 
 template <class E>
@@ -244,12 +319,11 @@ int policy_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V
     p.norm = opt->norm;
     p.factor = opt->factor;
     p.out = d_stats;
-    const RowPlan plan = plan_rows(ctx, T, V, sizeof(E));
-    const RowScratch at = row_scratch(plan, T);
+    const RowScratch at = row_scratch(ctx, T);
     Scratch scratch{};
     const int rs = gate_scratch(ctx, at.bytes(), st, &scratch);
     if (rs != LR_OK) return rs;
-    return launch_rows<E, kClassPolicy>(ctx, p, plan, at, scratch, d_dlogits != nullptr, st);
+    return d_dlogits ? launch_rows<E, kClassPolicy, true>(ctx, p, at, scratch, st) : launch_rows<E, kClassPolicy, false>(ctx, p, at, scratch, st);
 }
 
 template <class E>
@@ -288,12 +362,11 @@ int distill_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t 
     p.factor = opt->factor;
     p.out = d_loss;
     if (p.norm == 0.0 && !d_weights) p.norm = double(T);
-    const RowPlan plan = plan_rows(ctx, T, V, sizeof(E));
-    const RowScratch at = row_scratch(plan, T);
+    const RowScratch at = row_scratch(ctx, T);
     Scratch scratch{};
     const int rs = gate_scratch(ctx, at.bytes(), st, &scratch);
     if (rs != LR_OK) return rs;
-    return launch_rows<E, kClassDistill>(ctx, p, plan, at, scratch, d_dlogits != nullptr, st);
+    return d_dlogits ? launch_rows<E, kClassDistill, true>(ctx, p, at, scratch, st) : launch_rows<E, kClassDistill, false>(ctx, p, at, scratch, st);
 }
 
 template <class E>
@@ -322,8 +395,7 @@ int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
         if (d_dlogits && T > 0) LR_CK(ctx, cudaMemset2DAsync(d_dlogits, size_t(ld_d) * sizeof(E), 0, size_t(V) * sizeof(E), size_t(T), st));
         return LR_OK;
     }
-    const RowPlan plan = plan_rows(ctx, std::max<int64_t>(T, 1), V, sizeof(E));
-    const RowScratch at = row_scratch(plan, T);
+    const RowScratch at = row_scratch(ctx, T);
     const size_t rows = at.bytes(), stat = rows + up256(size_t(T) * sizeof(float2)), lp = up256(size_t(T) * 8), coef = up256(size_t(T) * 4),
                  loss = up256(size_t(pairs) * 8);
     Scratch scratch{};
@@ -338,7 +410,7 @@ int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
         p.offsets = d_offsets;
         p.wide_offsets = offset_bytes == 8;
         p.offset_count = 2 * pairs;
-        const int r = launch_rows<E, kClassLogp>(ctx, p, plan, at, scratch, false, st);
+        const int r = launch_rows<E, kClassLogp, false>(ctx, p, at, scratch, st);
         if (r != LR_OK) return r;
     }
     q.ids = d_targets;
