@@ -63,8 +63,8 @@ struct ClassParams {
     // rows and their CTAs
     const int* order;            // the rows that count, then the others (k_class_prep); NULL: all rows, looked at one by one
     const struct ClassPrep* prep;
-    int cluster;                 // long rows: CTAs per row (a power of two), stages in a ring, rows between the passes (see k_class_ring)
-    int depth, lag;
+    int cluster;                 // long rows: CTAs per row (a power of two), stages in a ring
+    int depth;
     const double* norm_part;     // short rows: the sum of the weights in parts (k_class_norm), or none
     int norm_parts;
     double* cta_sum;             // [CTAs][3]
@@ -173,7 +173,7 @@ struct ClassRow {
         x = static_cast<const E*>(base) + t * ld;
         dx = dbase ? static_cast<E*>(dbase) + t * ld_d : nullptr;
         const int off = int(reinterpret_cast<uintptr_t>(x) & 15) / int(sizeof(E));
-        head = min((N - off) % N, V);
+        head = min((N - off) & (N - 1), V);
         groups = (V - head) / N;
         edges = V - groups * N;
         wide_store = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(dx)) & 15) == 0;
@@ -620,26 +620,29 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 
 // ---- long rows -----------------------------------------------------------------------------------------
 // A CTA per row, or a cluster of C.  Its warps have different work, and hand rows to each other through mbarriers:
-//   one warp copies a row's 16-byte groups, in stages of 32 KB, into a ring of shared memory, as far ahead as the ring allows, over the ends of
-//     rows too;
-//   sixteen warps go through the stages: first pass (running maximum and sum) of row k, then second pass (the gradient) of row k - lag, so
-//     that they do not wait for a row's numbers;
-//   kNumberWarps warps take turns at the rows: they fetch what a row has beside its logits, join the sums of the sixteen warps (and of the
-//     cluster's CTAs, by 16-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
-// The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that (lag + 1) rows fit, lag >= 1.
-// For the longest rows lag is 0, and stages that the ring could not hold are copied once more (`dropped`).  Stages are given back in the order
-// of the copies.
-constexpr int kPassWarps = 16;
+//   two teams of eight warps take turns at the rows: first pass (running maximum and sum), then, when the row's numbers are known, second pass
+//     (the gradient).  While one team waits, or reduces, the other one works;
+//   a warp per team copies its rows' 16-byte groups, in stages of 16 KB, into the team's ring of shared memory, as far ahead as the ring
+//     allows (a ring of its own, because who skips the other team's stages cannot tell an mbarrier's phases apart);
+//   kNumberWarps warps take turns at the rows: they fetch what a row has beside its logits, join the sums of the team's warps (and of the
+//     cluster's CTAs, by 8-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
+// The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that a row fits.  Of the longest
+// rows, stages that the ring could not hold are copied once more (`dropped`).  Stages are given back in the order of the copies.
+constexpr int kTeams = 2;
+constexpr int kTeamWarps = 8;
+constexpr int kPassWarps = kTeams * kTeamWarps;
 constexpr int kNumberWarps = 4;
-constexpr int kRingThreads = 32 * (kPassWarps + 1 + kNumberWarps);
-constexpr int kLaneGroups = 4;                      // of a stage
+constexpr int kRingThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
+#ifndef RJ
+#define RJ 4
+#endif
+constexpr int kLaneGroups = RJ;                     // of a stage
 constexpr int kWarpGroups = 32 * kLaneGroups;
-constexpr int kStageGroups = kPassWarps * kWarpGroups;
+constexpr int kStageGroups = kTeamWarps * kWarpGroups;
 constexpr int kStageBytes = kStageGroups * 16;
-constexpr int kRingDepth = 6;
+constexpr int kRingDepth = 7 * 4 / RJ;               // of a team's ring, at most
 constexpr int kMaxCluster = 8;
-constexpr int kRows = 4;                            // rows under way between the warps; a multiple of kNumberWarps, above the largest lag
-constexpr int kMaxLag = kRows - 1;
+constexpr int kRows = 4;                            // rows under way between the warps; a multiple of kNumberWarps and kTeams
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -657,14 +660,14 @@ __device__ __forceinline__ void send_f32x2(const float2* local, const uint64_t* 
 }
 
 struct alignas(16) RingShared {
-    uint64_t full[kRingDepth], free[kRingDepth];
-    // of row k, at k mod kRows: the sixteen warps' sums are there; the row's numbers are there; its gradient is written
+    uint64_t full[kTeams][kRingDepth], free[kTeams][kRingDepth];
+    // of row k, at k mod kRows: the team's sums are there; the row's numbers are there; its gradient is written
     uint64_t summed[kRows], ready[kRows], written[kRows];
     // the cluster's sums, twice as many rows: a CTA that is ahead sends row k + kRows before this one has looked at row k, but not row
     // k + 2 kRows, for which it needs this CTA's row k + kRows, which the warp that looks at row k sends later
     uint64_t joined[2 * kRows];
     float2 cta_sum[2 * kRows][kMaxCluster];
-    float2 warp_sum[kRows][kPassWarps];             // largest logit, sum
+    float2 warp_sum[kRows][kTeamWarps];             // largest logit, sum
     float4 row[kRows];                              // factor, m, 1 where the row counts
     int abort_word;
 };
@@ -675,19 +678,19 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
     constexpr int N = G::N, J = kLaneGroups;
     __shared__ RingShared sh;
     extern __shared__ __align__(128) unsigned char class_smem[];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, depth = p.depth, lag = p.lag;
-    const int C = p.cluster, rank = C > 1 ? int(cluster_rank()) : 0, q = blockIdx.x / C, Q = gridDim.x / C;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, depth = p.depth;
+    const int C = p.cluster, shift = __ffs(C) - 1, rank = C > 1 ? int(cluster_rank()) : 0, q = blockIdx.x / C, Q = gridDim.x / C;
     volatile int* abort_flag = &sh.abort_word;
     if (tid == 0) {
         sh.abort_word = 0;
-        for (int i = 0; i < kRingDepth; ++i) {
-            mbar_init(sh.full + i, 1);
-            mbar_init(sh.free + i, kPassWarps);
+        for (int i = 0; i < kTeams * kRingDepth; ++i) {
+            mbar_init(&sh.full[0][0] + i, 1);
+            mbar_init(&sh.free[0][0] + i, kTeamWarps);
         }
         for (int i = 0; i < kRows; ++i) {
-            mbar_init(sh.summed + i, kPassWarps);
+            mbar_init(sh.summed + i, kTeamWarps);
             mbar_init(sh.ready + i, 1);
-            mbar_init(sh.written + i, kPassWarps);
+            mbar_init(sh.written + i, kTeamWarps);
         }
         for (int i = 0; i < 2 * kRows; ++i) mbar_init(sh.joined + i, 1);
         fence_mbar_init();
@@ -703,28 +706,31 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
     };
     auto stages_of = [&](int groups) {              // of this CTA: every C-th
         const int all = (groups + kStageGroups - 1) / kStageGroups;
-        return all > rank ? (all - rank + C - 1) / C : 0;
+        return all > rank ? (all - rank + C - 1) >> shift : 0;
     };
-    if (warp == kPassWarps) {
+    if (warp >= kPassWarps && warp < kPassWarps + kTeams) {
         if (lane == 0) {
+            const int team = warp - kPassWarps;
+            uint64_t *full = sh.full[team], *free = sh.free[team];
+            unsigned char* ring = class_smem + team * depth * kStageBytes;
             const uint64_t once = l2_policy_evict_first();
             int slot = 0, parity = 0, copies = 0;
             bool ok = true;
-            int t = row_of(0);
-            for (int k = 0; k < mine && ok; ++k) {
+            int t = row_of(team);
+            for (int k = team; k < mine && ok; k += kTeams) {
                 const ClassRow<E> row(p.x, p.ld, nullptr, 0, t, p.V);
-                t = row_of(k + 1);
+                t = row_of(k + kTeams);
                 const int stages = stages_of(row.groups), again = GRAD ? max(0, stages - depth) : 0;
                 for (int i = 0; i < stages + again; ++i) {
                     const int first = ((i < stages ? i : i - stages) * C + rank) * kStageGroups;
                     const uint32_t bytes = min(kStageGroups, row.groups - first) * 16;
-                    if (copies >= depth && !mbar_wait_bounded(sh.free + slot, parity ^ 1, abort_flag)) {
+                    if (copies >= depth && !mbar_wait_bounded(free + slot, parity ^ 1, abort_flag)) {
                         ok = false;
                         break;
                     }
                     fence_proxy_async_smem();
-                    mbar_arrive_expect_tx(sh.full + slot, bytes);
-                    bulk_copy_g2s(class_smem + slot * kStageBytes, row.x + row.head + static_cast<long long>(first) * N, bytes, sh.full + slot, once);
+                    mbar_arrive_expect_tx(full + slot, bytes);
+                    bulk_copy_g2s(ring + slot * kStageBytes, row.x + row.head + static_cast<long long>(first) * N, bytes, full + slot, once);
                     if (copies < depth) ++copies;
                     if (++slot == depth) {
                         slot = 0;
@@ -738,91 +744,106 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
                     slot = depth;
                     parity ^= 1;
                 }
-                mbar_wait_drain(sh.full + --slot, parity);
+                mbar_wait_drain(full + --slot, parity);
             }
         }
     } else if (warp < kPassWarps) {
-        int out_slot = 0, wait_slot = 0, wait_parity = 0;
+        const int team = warp / kTeamWarps, in_team = warp % kTeamWarps;
+        uint64_t *full = sh.full[team], *free = sh.free[team];
+        const unsigned char* ring = class_smem + team * depth * kStageBytes + (in_team * kWarpGroups + lane) * 16;
+        int slot = 0, parity = 0;                   // of the copy that comes next
         bool ok = true;
-        auto wait = [&](uint64_t* bar, int parity) {
-            if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag))) ok = false;
+        auto wait = [&](uint64_t* bar, int parity_now) {
+            if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, parity_now, abort_flag))) ok = false;
+        };
+        auto next_slot = [&]() {
+            if (++slot == depth) {
+                slot = 0;
+                parity ^= 1;
+            }
         };
         auto read_stage = [&](int at, uint4 (&raw)[J]) {
-            const unsigned char* from = class_smem + at * kStageBytes + (warp * kWarpGroups + lane) * 16;
 #pragma unroll
-            for (int j = 0; j < J; ++j) raw[j] = *reinterpret_cast<const uint4*>(from + j * 512);
+            for (int j = 0; j < J; ++j) raw[j] = *reinterpret_cast<const uint4*>(ring + at * kStageBytes + j * 512);
         };
-        auto wait_copy = [&]() {
-            wait(sh.full + wait_slot, wait_parity);
-            const int at = wait_slot;
-            if (++wait_slot == depth) {
-                wait_slot = 0;
-                wait_parity ^= 1;
-            }
-            return at;
-        };
-        auto give_back = [&]() {                    // what is in registers now may be overwritten
+        auto give_back = [&](int at) {              // what is in registers now may be overwritten
             __syncwarp();
-            if (lane == 0) mbar_arrive(sh.free + out_slot);
-            if (++out_slot == depth) out_slot = 0;
+            if (lane == 0 && ok) mbar_arrive(free + at);           // (where a wait ran out the copy may still be on its way)
         };
-        int t_first = row_of(0), t_second = t_first;
-        for (int step = 0; step < mine + lag && ok; ++step) {
-            if (step < mine) {
-                const ClassRow<E> row(p.x, p.ld, nullptr, 0, t_first, p.V);
-                t_first = row_of(step + 1);
-                const int stages = stages_of(row.groups), dropped = GRAD ? max(0, stages - depth) : stages;
-                ClassSum sum;
-                for (int i = 0; i < stages; ++i) {
-                    const int left = row.groups - (i * C + rank) * kStageGroups - warp * kWarpGroups;
-                    uint4 raw[J];
-                    read_stage(wait_copy(), raw);
-                    if (i < dropped) give_back();
-                    if (left >= kWarpGroups) {
-                        sum.add_groups<E, J>(raw, p.c);
-                    } else if (left > 0) {
+        int t_next = row_of(team);
+        for (int k = team; k < mine && ok; k += kTeams) {
+            const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t_next, p.V);
+            t_next = row_of(k + kTeams);
+            const int stages = stages_of(row.groups), dropped = GRAD ? max(0, stages - depth) : stages;
+            const int at = k % kRows;
+            ClassSum sum;
+            int held = slot;                        // the first stage that is kept
+            for (int i = 0; i < stages; ++i) {
+                const int left = row.groups - (i * C + rank) * kStageGroups - in_team * kWarpGroups;
+                wait(full + slot, parity);
+                uint4 raw[J];
+                read_stage(slot, raw);
+                if (i < dropped) give_back(slot);
+                next_slot();
+                if (i + 1 == dropped) held = slot;
+                if (left >= kWarpGroups) {
+                    sum.add_groups<E, J>(raw, p.c);
+                } else if (left > 0) {
 #pragma unroll
-                        for (int j = 0; j < J; ++j) {
-                            const uint4 one[1] = {raw[j]};
-                            if (32 * j + lane < left) sum.add_groups<E, 1>(one, p.c);
-                        }
+                    for (int j = 0; j < J; ++j) {
+                        const uint4 one[1] = {raw[j]};
+                        if (32 * j + lane < left) sum.add_groups<E, 1>(one, p.c);
                     }
                 }
-                sum.over_warp(p.c);
-                if (lane == 0) {
-                    sh.warp_sum[step % kRows][warp] = make_float2(sum.top, sum.s);
-                    mbar_arrive(sh.summed + step % kRows);
-                }
             }
-            const int k = step - lag;
-            if (k < 0 || !ok) continue;
-            wait(sh.ready + k % kRows, (k / kRows) & 1);
-            if (!GRAD || !ok) continue;
-            const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t_second, p.V);
-            t_second = row_of(k + 1);
-            const int stages = stages_of(row.groups), dropped = max(0, stages - depth);
-            const float4 numbers = sh.row[k % kRows];
+            sum.over_warp(p.c);
+            if (!GRAD && k >= kRows) wait(sh.ready + at, (k / kRows - 1) & 1);      // the sums of row k - kRows have been read
+            if (lane == 0) {
+                sh.warp_sum[at][in_team] = make_float2(sum.top, sum.s);
+                mbar_arrive(sh.summed + at);
+            }
+            if (!GRAD) continue;
+            wait(sh.ready + at, (k / kRows) & 1);
+            if (!ok) break;
+            const float4 numbers = sh.row[at];
             const bool counts = numbers.z != 0.0f;
             const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(-numbers.y, -numbers.y), factor2 = f32x2_pack(numbers.x, numbers.x);
-            auto second = [&](int i, int at) {
-                const int first = (i * C + rank) * kStageGroups + warp * kWarpGroups, left = row.groups - first;
+            auto second = [&](int i, int from) {
+                const int first = (i * C + rank) * kStageGroups + in_team * kWarpGroups, left = row.groups - first;
                 uint4 raw[J];
-                read_stage(at, raw);
-                give_back();
+                read_stage(from, raw);
+                give_back(from);
+                auto group = [&](int j) {
+                    uint64_t v[G::P];
 #pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    if (32 * j + lane < left) {
-                        uint64_t v[G::P];
+                    for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(G::power(raw[j], e, c2, m2), factor2);
+                    row.store(first + lane + 32 * j, v);
+                };
+                if (!counts) {
+                    const uint64_t zero[G::P] = {};
 #pragma unroll
-                        for (int e = 0; e < G::P; ++e) v[e] = counts ? f32x2_mul(G::power(raw[j], e, c2, m2), factor2) : 0;
-                        row.store(first + lane + 32 * j, v);
-                    }
+                    for (int j = 0; j < J; ++j)
+                        if (32 * j + lane < left) row.store(first + lane + 32 * j, zero);
+                } else if (left >= kWarpGroups) {
+#pragma unroll
+                    for (int j = 0; j < J; ++j) group(j);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        if (32 * j + lane < left) group(j);
                 }
             };
-            for (int i = dropped; i < stages; ++i) second(i, out_slot);
-            for (int i = 0; i < dropped; ++i) second(i, wait_copy());
+            for (int i = dropped; i < stages; ++i) {
+                second(i, held);
+                if (++held == depth) held = 0;
+            }
+            for (int i = 0; i < dropped; ++i) {
+                wait(full + slot, parity);
+                second(i, slot);
+                next_slot();
+            }
             __syncwarp();
-            if (lane == 0) mbar_arrive(sh.written + k % kRows);
+            if (lane == 0) mbar_arrive(sh.written + at);
         }
         // gradients of rows that do not count
         if (GRAD && p.order) {
@@ -834,10 +855,10 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
             }
         }
     } else {
-        const int h = warp - kPassWarps - 1;
+        const int h = warp - kPassWarps - kTeams;
         ClassTop top{};
         if (MODE == kClassDistill) {
-            top = class_top_at(class_smem + depth * kStageBytes + h * class_top_bytes(p.K), p.K);
+            top = class_top_at(class_smem + kTeams * depth * kStageBytes + h * class_top_bytes(p.K), p.K);
             class_clear_marks(top);
         }
         double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
@@ -868,7 +889,7 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
             const int at = k % kRows, parity = (k / kRows) & 1;
             if (!wait(sh.summed + at, parity)) break;
             ClassSum sum;
-            if (lane < kPassWarps) sum.set(sh.warp_sum[at][lane].x, sh.warp_sum[at][lane].y, p.c);
+            if (lane < kTeamWarps) sum.set(sh.warp_sum[at][lane].x, sh.warp_sum[at][lane].y, p.c);
             if (edges) sum.add(edge, p.c);
             sum.over_warp(p.c);
             if (C > 1) {

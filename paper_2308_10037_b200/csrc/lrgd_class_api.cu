@@ -51,22 +51,19 @@ constexpr int kNormInline = 512;                    // rows whose weights every 
 // How rows are worked on: a warp each (groups per lane: 1, 2, 4, 8 or 16), or by CTAs with rings, `cluster` to a row.
 struct RowPlan {
     int lane_groups;             // 0: rings
-    int cluster, lag;            // (see k_class_ring)
+    int cluster;
 };
 RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es, bool grad, int depth) {
     const int64_t groups = V * es / 16, sms = plan_sms(ctx);
-    RowPlan r{0, 1, 0};
+    RowPlan r{0, 1};
     if (groups <= 32 * kShortGroups) {
         for (r.lane_groups = 1; 32 * r.lane_groups < groups;) r.lane_groups *= 2;
         return r;
     }
-    // Of the logits' stages (one more of each CTA's where rows start at different offsets) two rows have to be in a ring together, or as many
-    // CTAs take a row as there are SMs for, if rows are few
+    // A row has to fit into a team's ring, or as many CTAs take a row as there are SMs for, if rows are few
     const int64_t stages = (groups + kStageGroups - 1) / kStageGroups;
     auto per_cta = [&] { return (stages + r.cluster - 1) / r.cluster; };
-    while (r.cluster < kMaxCluster && ((grad && 2 * per_cta() > depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
-    const int64_t n = per_cta();
-    r.lag = !grad ? kMaxLag : 2 * n > depth ? 0 : int(std::max<int64_t>(1, std::min<int64_t>(kMaxLag, depth / n - 2)));
+    while (r.cluster < kMaxCluster && ((grad && per_cta() > depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
     return r;
 }
 
@@ -112,7 +109,7 @@ template <class E, int MODE, bool GRAD>
 int launch_ring(lr_ctx* ctx, ClassParams& p, const RowScratch& at, const Scratch& scratch, cudaStream_t st) {
     using Tag = ClassRowsTag<E, MODE, GRAD>;
     const auto kern = k_class_ring<E, MODE, GRAD>;
-    const size_t smem = size_t(p.depth) * kStageBytes + (MODE == kClassDistill ? kNumberWarps * class_top_bytes(p.K) : 0);
+    const size_t smem = size_t(kTeams) * p.depth * kStageBytes + (MODE == kClassDistill ? kNumberWarps * class_top_bytes(p.K) : 0);
     LR_CK(ctx, ensure_dynamic_smem<Tag>(reinterpret_cast<const void*>(kern), int(smem)));
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(kRingThreads);
@@ -189,10 +186,9 @@ int launch_rows(lr_ctx* ctx, ClassParams& p, const RowScratch& at, const Scratch
     constexpr size_t kSmem = 224 << 10;             // of an SM, for ring and teacher's classes
     p.depth = kRingDepth;
     if (MODE == kClassDistill)
-        while (p.depth > 1 && size_t(p.depth) * kStageBytes + kNumberWarps * class_top_bytes(p.K) > kSmem) --p.depth;
+        while (p.depth > 1 && size_t(kTeams) * p.depth * kStageBytes + kNumberWarps * class_top_bytes(p.K) > kSmem) --p.depth;
     const RowPlan plan = plan_rows(ctx, p.T, p.V, sizeof(E), GRAD, p.depth);
     p.cluster = plan.cluster;
-    p.lag = plan.lag;
     if (plan.lane_groups > 0) return launch_short<E, MODE, GRAD>(ctx, p, plan.lane_groups, at, scratch, st);
     return launch_ring<E, MODE, GRAD>(ctx, p, at, scratch, st);
 }
