@@ -282,12 +282,16 @@ __device__ __forceinline__ double warp_sum64(double v) {
     return v;
 }
 
-// log2 of the sum.  exp2_fast drops the bits of its argument below 2^-23 or so: terms below 1/2 come out 4.9e-8 too small in the mean
-// (measured over 4 M random arguments; 2.2e-8 between 1/2 and 1, the largest term is exact).  One row's lp does not show that, the sum over a
-// long sequence does; in the gradient it cancels, whose numerator has the same terms.
+// m + log2 of the sum.  The sum is 2^e f with 1 <= f < 2, so that the fp32 logarithm is one of a number below 1 and off by 6e-8 at most.
+// exp2_fast drops the bits of its argument below 2^-23 or so: terms below 1/2 come out 4.9e-8 too small in the mean (measured over 4 M
+// random arguments; 2.2e-8 between 1/2 and 1, the largest term is exact).  One row's lp does not show that, the sum over a long sequence does;
+// in the gradient it cancels, whose numerator has the same terms.
 __device__ __forceinline__ double class_lse2(float m, float s) {
-    const double sum = s;
-    return static_cast<double>(m) + log2(sum + 4.9e-8 * (sum - 1.0));
+    if (!(s > 0.0f && s < INFINITY)) return static_cast<double>(m) + log2f(s);
+    const uint32_t bits = __float_as_uint(s);       // (at least 1 where it is positive: the largest term)
+    const int e = static_cast<int>(bits >> 23) - 127;
+    const float f = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+    return (static_cast<double>(m) + e) + (static_cast<double>(log2f(f)) + 7.07e-8 * (1.0 - __fdividef(1.0f, s)));
 }
 
 // ---- which rows count ----------------------------------------------------------------------------------
@@ -528,7 +532,7 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, long
     if (MODE == kClassDistill) {
         // with the teacher's own normalisation log2 q is smaller by log2(all)
         const double all = in.top.all, one = p.teacher_lse || all == 0.0 ? 1.0 : 1.0 / all, mass = all * one;
-        const double kl = all == 0.0 ? 0.0 : kLn2 * (in.top.cross * one + mass * (lse2 + log2(one)));
+        const double kl = all == 0.0 ? 0.0 : kLn2 * (in.top.cross * one + mass * (lse2 + log2f(static_cast<float>(one))));
         if (p.row_kl && write) p.row_kl[t] = static_cast<float>(kl);
         sums[0] += in.w * kl;
         const double gain = in.w * inv * p.factor * p.scale;
@@ -547,10 +551,11 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, long
             p.coef[t] = 0.0f;
         }
     } else {
-        // exp(lp - old) - 1, exp(ref - lp) - 1 and exp(lp) - 1: one lane each
+        // exp(lp - old) - 1, exp(ref - lp) - 1 and exp(lp) - 1: one lane each.  The differences are fp64, their exponentials fp32 (one unit in
+        // the last place).
         const double d = in.ref_logp - lp;
-        const double e = expm1(lane == 0 ? lp - in.old_logp : lane == 1 ? d : lp);
-        const double ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0) + 1.0 : 1.0, away = __shfl_sync(0xffffffffu, e, 1),
+        const float e = expm1f(static_cast<float>(lane == 0 ? lp - in.old_logp : lane == 1 ? d : lp));
+        const double ratio = p.old_logp ? static_cast<double>(__shfl_sync(0xffffffffu, e, 0)) + 1.0 : 1.0, away = __shfl_sync(0xffffffffu, e, 1),
                      rest = __shfl_sync(0xffffffffu, e, 2);
         const double a = in.adv, held = fmin(fmax(ratio, p.ratio_low), p.ratio_high);
         const bool clipped = ratio * a > held * a;
@@ -624,6 +629,7 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 //     (the gradient).  While one team waits, or reduces, the other one works;
 //   a warp per team copies its rows' 16-byte groups, in stages of 16 KB, into the team's ring of shared memory, as far ahead as the ring
 //     allows (a ring of its own, because who skips the other team's stages cannot tell an mbarrier's phases apart);
+//   one warp writes zeros into the gradients of the rows that do not count, beside the others' work;
 //   kNumberWarps warps take turns at the rows: they fetch what a row has beside its logits, join the sums of the team's warps (and of the
 //     cluster's CTAs, by 8-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
 // The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that a row fits.  Of the longest
@@ -632,7 +638,7 @@ constexpr int kTeams = 2;
 constexpr int kTeamWarps = 8;
 constexpr int kPassWarps = kTeams * kTeamWarps;
 constexpr int kNumberWarps = 4;
-constexpr int kRingThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
+constexpr int kRingThreads = 32 * (kPassWarps + kTeams + kNumberWarps + 1);
 #ifndef RJ
 #define RJ 4
 #endif
@@ -702,7 +708,10 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
     const int mine = live > q ? (live - q + Q - 1) / Q : 0;
     auto row_of = [&](int k) -> int {
         const long long at = q + static_cast<long long>(k) * Q;
-        return k < mine ? (p.order ? __ldg(p.order + at) : static_cast<int>(at)) : 0;
+        if (k >= mine || !p.order) return static_cast<int>(at);
+        int t;                                      // (volatile: fetched here, well before it is needed)
+        asm volatile("ld.global.b32 %0, [%1];" : "=r"(t) : "l"(p.order + at));
+        return t;
     };
     auto stages_of = [&](int groups) {              // of this CTA: every C-th
         const int all = (groups + kStageGroups - 1) / kStageGroups;
@@ -845,13 +854,13 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.written + at);
         }
-        // gradients of rows that do not count
+    } else if (warp == kPassWarps + kTeams + kNumberWarps) {
         if (GRAD && p.order) {
             for (long long k = live + q; k < p.T; k += Q) {
                 const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, __ldg(p.order + k), p.V);
                 const uint64_t zero[G::P] = {};
-                for (int g = rank * (32 * kPassWarps) + tid; g < row.groups; g += C * (32 * kPassWarps)) row.store(g, zero);
-                if (rank == 0 && tid < row.edges) store_from_float(row.dx + row.edge(tid), 0.0f);
+                for (int g = rank * 32 + lane; g < row.groups; g += C * 32) row.store(g, zero);
+                if (rank == 0 && lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
             }
         }
     } else {
