@@ -50,7 +50,7 @@ struct ClassParams {
     const float* adv;
     const float* old_logp;
     const float* ref_logp;
-    double ratio_low, ratio_high, kl_coef;
+    float ratio_low, ratio_high, kl_coef;
     // distillation
     const void* teacher;
     int teacher_half;            // bfloat16
@@ -437,7 +437,7 @@ __device__ __forceinline__ bool class_mark(const ClassTop& top, int id) {
 
 // What the entries add up to
 struct ClassTopSum {
-    double all, cross;           // sum of q, sum of q * (c * v - base - c * x)
+    float all, cross;            // sum of q, sum of q * (c * v - base - c * x)
     bool twice;                  // some class is named twice
 };
 // Reads a row's classes; the bitmap is empty before and after.  Eight entries of a lane are on their way together.
@@ -445,8 +445,9 @@ template <class E>
 __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long long t, const E* row, const ClassTop& top) {
     constexpr int U = 8;
     const int lane = threadIdx.x & 31;
-    ClassTopSum r{0.0, 0.0, false};
+    ClassTopSum r{0.0f, 0.0f, false};
     float largest = -INFINITY;
+    const double lse2 = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) * (static_cast<double>(p.c) / p.scale) : 0.0;
     for (int j0 = 0; j0 < p.K; j0 += 32 * U) {
         ClassEntry e[U];
         int id[U];
@@ -458,8 +459,10 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
             id[i] = j0 + 32 * i + lane < p.K ? class_entry_id(p, e[i]) : -1;
             x[i] = id[i] >= 0 ? load_local(row + id[i]) : 0.0f;
         }
+        uint32_t taken = 0;                         // bit i: the place of entry i in the bitmap was taken, by the same class or another one
 #pragma unroll
         for (int i = 0; i < U; ++i) {
+            if (id[i] >= 0 && class_mark(top, id[i])) taken |= 1u << i;
             const int j = j0 + 32 * i + lane;
             if (j < p.K) {
                 top.id[j] = id[i];
@@ -469,30 +472,30 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
             if (id[i] >= 0) largest = fmaxf(largest, e[i].v);
         }
         __syncwarp();
-#pragma unroll
-        for (int i = 0; i < U; ++i) {               // a place of the bitmap that was taken: is it the same class?
-            if (j0 + 32 * i >= p.K) break;
-            uint32_t taken = __ballot_sync(0xffffffffu, id[i] >= 0 && class_mark(top, id[i]));
-            for (; taken && !r.twice; taken &= taken - 1) {
-                const int from = __ffs(taken) - 1, which = __shfl_sync(0xffffffffu, id[i], from);
-                int same = 0;
-                for (int j = lane; j < min(p.K, j0 + 32 * U); j += 32) same += top.id[j] == which;
-                r.twice = __reduce_add_sync(0xffffffffu, same) > 1;
-            }
+        for (uint32_t lanes = __ballot_sync(0xffffffffu, taken != 0); lanes && !r.twice; lanes = __ballot_sync(0xffffffffu, taken != 0)) {
+            const int from = __ffs(lanes) - 1, i = __ffs(__shfl_sync(0xffffffffu, taken, from)) - 1, which = top.id[j0 + 32 * i + from];
+            if (lane == from) taken &= taken - 1;
+            int same = 0;
+            for (int j = lane; j < min(p.K, j0 + 32 * U); j += 32) same += top.id[j] == which;
+            r.twice = __reduce_add_sync(0xffffffffu, same) > 1;
         }
     }
     largest = warp_max(largest);
-    const double base = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) * (static_cast<double>(p.c) / p.scale)
-                                      : (largest == -INFINITY ? 0.0 : static_cast<double>(largest) * p.c);
+    // 2^(c v - base): base is the largest c v rounded, or the teacher's own, in two parts
+    const float high = p.teacher_lse ? static_cast<float>(lse2) : largest == -INFINITY ? 0.0f : __fmul_rn(largest, p.c),
+                low = p.teacher_lse ? static_cast<float>(lse2 - static_cast<double>(high)) : 0.0f;
     for (int j = lane; j < p.K; j += 32) {
-        const double a = static_cast<double>(top.q[j]) * p.c - base;
-        const float e = top.id[j] >= 0 ? exp2f(static_cast<float>(a)) : 0.0f;
+        const float a = fmaf(top.q[j], p.c, -high) - low;
+        const float e = top.id[j] >= 0 ? exp2f(a) : 0.0f;
         r.all += e;
-        if (e != 0.0f) r.cross += e * (a - static_cast<double>(top.x[j]) * p.c);
+        if (e != 0.0f) r.cross += e * fmaf(-p.c, top.x[j], a);
         top.q[j] = e;
     }
-    r.all = warp_sum64(r.all);
-    r.cross = warp_sum64(r.cross);
+#pragma unroll
+    for (int d = 16; d >= 1; d >>= 1) {
+        r.all += __shfl_xor_sync(0xffffffffu, r.all, d);
+        r.cross += __shfl_xor_sync(0xffffffffu, r.cross, d);
+    }
     class_clear_marks(top);
     return r;
 }
@@ -522,56 +525,72 @@ __device__ __forceinline__ void class_inputs(const ClassParams& p, long long t, 
         in.ref_logp = p.ref_logp ? __ldg(p.ref_logp + t) : 0.0f;
     }
 }
+// ... and what of it is written down afterwards
+struct ClassTerms {
+    double lp, lse2;
+    float first, kl, clipped;    // the row's loss: its parts (distillation: kl alone)
+};
 template <int MODE>
-__device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, long long t, const ClassInputs& in, const ClassSum& sum, double inv, bool write,
-                                                      double (&sums)[3]) {
+__device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, const ClassInputs& in, const ClassSum& sum, double inv, ClassTerms& terms) {
     const int lane = threadIdx.x & 31;
     const double lse2 = class_lse2(sum.m, sum.s);
     ClassNumbers r{};
-    write = write && lane == 0;
+    terms = ClassTerms{0.0, lse2, 0.0f, 0.0f, 0.0f};
+    const float gain = static_cast<float>(in.w * inv * p.factor * p.scale);
     if (MODE == kClassDistill) {
         // with the teacher's own normalisation log2 q is smaller by log2(all)
-        const double all = in.top.all, one = p.teacher_lse || all == 0.0 ? 1.0 : 1.0 / all, mass = all * one;
-        const double kl = all == 0.0 ? 0.0 : kLn2 * (in.top.cross * one + mass * (lse2 + log2f(static_cast<float>(one))));
-        if (p.row_kl && write) p.row_kl[t] = static_cast<float>(kl);
-        sums[0] += in.w * kl;
-        const double gain = in.w * inv * p.factor * p.scale;
-        r.factor = static_cast<float>(mass == 0.0 ? 0.0 : gain * mass / sum.s);
-        r.at = static_cast<float>(gain * one);
+        const float all = in.top.all, one = p.teacher_lse || all == 0.0f ? 1.0f : 1.0f / all, mass = p.teacher_lse || all == 0.0f ? all : 1.0f;
+        terms.kl = all == 0.0f ? 0.0f : static_cast<float>(kLn2 * (in.top.cross * one + mass * (lse2 + log2f(one))));
+        r.factor = mass == 0.0f ? 0.0f : gain * mass / sum.s;
+        r.at = gain * one;
         return r;
     }
-    double lp = kLn2 * (static_cast<double>(in.xy) * p.c - lse2);
-    if (lp > 0.0) lp = 0.0;                         // rounding
-    if (p.logp && write) p.logp[t] = static_cast<float>(lp);
+    terms.lp = kLn2 * (static_cast<double>(in.xy) * p.c - lse2);
+    if (terms.lp > 0.0) terms.lp = 0.0;             // rounding
+    if (MODE == kClassPolicy) {
+        // exp(lp - old) - 1, exp(ref - lp) - 1 and exp(lp) - 1: one lane each.  The differences are fp64, their exponentials fp32 (one unit in
+        // the last place).
+        const float d = static_cast<float>(lane == 0 ? terms.lp - in.old_logp : lane == 1 ? in.ref_logp - terms.lp : terms.lp);
+        const float e = expm1f(d);
+        const float ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0) + 1.0f : 1.0f, away = __shfl_sync(0xffffffffu, e, 1),
+                    rest = __shfl_sync(0xffffffffu, e, 2);
+        const float a = in.adv, held = fminf(fmaxf(ratio, p.ratio_low), p.ratio_high);
+        const bool clipped = ratio * a > held * a;
+        float g = clipped ? 0.0f : -ratio * a;
+        if (p.ref_logp) {
+            terms.kl = away - __shfl_sync(0xffffffffu, d, 1);
+            g -= p.kl_coef * away;
+        }
+        terms.first = -(clipped ? held : ratio) * a;
+        terms.clipped = clipped ? 1.0f : 0.0f;
+        g *= gain;
+        r.factor = -g / sum.s;
+        r.at = -g * rest;
+    }
+    return r;
+}
+template <int MODE>
+__device__ __forceinline__ void class_account(const ClassParams& p, long long t, const ClassInputs& in, const ClassSum& sum, const ClassTerms& terms,
+                                              bool write, double (&sums)[3]) {
+    write = write && (threadIdx.x & 31) == 0;
+    if (MODE == kClassDistill) {
+        if (p.row_kl && write) p.row_kl[t] = terms.kl;
+        sums[0] += static_cast<double>(in.w) * terms.kl;
+        return;
+    }
+    if (p.logp && write) p.logp[t] = static_cast<float>(terms.lp);
     if (MODE == kClassLogp) {
-        if (p.lse && write) p.lse[t] = static_cast<float>(kLn2 * lse2);
+        if (p.lse && write) p.lse[t] = static_cast<float>(kLn2 * terms.lse2);
         if (p.stat && write) {
             p.stat[t] = make_float2(sum.m, sum.s);
-            p.logp64[t] = lp;
+            p.logp64[t] = terms.lp;
             p.coef[t] = 0.0f;
         }
     } else {
-        // exp(lp - old) - 1, exp(ref - lp) - 1 and exp(lp) - 1: one lane each.  The differences are fp64, their exponentials fp32 (one unit in
-        // the last place).
-        const double d = in.ref_logp - lp;
-        const float e = expm1f(static_cast<float>(lane == 0 ? lp - in.old_logp : lane == 1 ? d : lp));
-        const double ratio = p.old_logp ? static_cast<double>(__shfl_sync(0xffffffffu, e, 0)) + 1.0 : 1.0, away = __shfl_sync(0xffffffffu, e, 1),
-                     rest = __shfl_sync(0xffffffffu, e, 2);
-        const double a = in.adv, held = fmin(fmax(ratio, p.ratio_low), p.ratio_high);
-        const bool clipped = ratio * a > held * a;
-        double g = clipped ? 0.0 : -ratio * a, kl = 0.0;
-        if (p.ref_logp) {
-            kl = away - d;
-            g -= p.kl_coef * away;
-        }
-        sums[0] -= in.w * (clipped ? held : ratio) * a;
-        sums[1] += in.w * kl;
-        sums[2] += clipped ? in.w : 0.0;
-        g *= in.w * inv * p.factor * p.scale;
-        r.factor = static_cast<float>(-g / sum.s);
-        r.at = static_cast<float>(-g * rest);
+        sums[0] += static_cast<double>(in.w) * terms.first;
+        sums[1] += static_cast<double>(in.w) * terms.kl;
+        sums[2] += terms.clipped != 0.0f ? in.w : 0.0f;
     }
-    return r;
 }
 // What the gradient is at entry j of the teacher's classes
 __device__ __forceinline__ float class_top_value(const ClassParams& p, const ClassTop& top, int j, bool twice, float m, const ClassNumbers& r) {
@@ -614,7 +633,7 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
     }
     if (lane == 0) {
         if (MODE == kClassPolicy) {
-            p.out[0] = static_cast<float>(p.factor * (sums[0] + p.kl_coef * sums[1]));
+            p.out[0] = static_cast<float>(p.factor * (sums[0] + static_cast<double>(p.kl_coef) * sums[1]));
             for (int i = 0; i < 3; ++i) p.out[1 + i] = static_cast<float>(sums[i]);
         } else {
             p.out[0] = static_cast<float>(p.factor * sums[0]);
@@ -629,16 +648,17 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 //     (the gradient).  While one team waits, or reduces, the other one works;
 //   a warp per team copies its rows' 16-byte groups, in stages of 16 KB, into the team's ring of shared memory, as far ahead as the ring
 //     allows (a ring of its own, because who skips the other team's stages cannot tell an mbarrier's phases apart);
-//   one warp writes zeros into the gradients of the rows that do not count, beside the others' work;
 //   kNumberWarps warps take turns at the rows: they fetch what a row has beside its logits, join the sums of the team's warps (and of the
 //     cluster's CTAs, by 8-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
+//     Between them they write zeros into the gradients of rows that do not count, as many at every row (all at once they fill the queues
+//     of the memory system that the others wait in).
 // The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that a row fits.  Of the longest
 // rows, stages that the ring could not hold are copied once more (`dropped`).  Stages are given back in the order of the copies.
 constexpr int kTeams = 2;
 constexpr int kTeamWarps = 8;
 constexpr int kPassWarps = kTeams * kTeamWarps;
 constexpr int kNumberWarps = 4;
-constexpr int kRingThreads = 32 * (kPassWarps + kTeams + kNumberWarps + 1);
+constexpr int kRingThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
 #ifndef RJ
 #define RJ 4
 #endif
@@ -854,15 +874,6 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
             __syncwarp();
             if (lane == 0) mbar_arrive(sh.written + at);
         }
-    } else if (warp == kPassWarps + kTeams + kNumberWarps) {
-        if (GRAD && p.order) {
-            for (long long k = live + q; k < p.T; k += Q) {
-                const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, __ldg(p.order + k), p.V);
-                const uint64_t zero[G::P] = {};
-                for (int g = rank * 32 + lane; g < row.groups; g += C * 32) row.store(g, zero);
-                if (rank == 0 && lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
-            }
-        }
     } else {
         const int h = warp - kPassWarps - kTeams;
         ClassTop top{};
@@ -886,6 +897,24 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
             if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag))) ok = false;
             return ok;
         };
+        // this cluster's rows that do not count, in pieces of kZeroGroups groups; row k's turn is piece pieces * k / mine and on
+        constexpr int kZeroGroups = 512;
+        const int dead = p.order ? max(0, (int(p.T) - live - q + Q - 1) / Q) : 0, per_row = (p.V / N + kZeroGroups * C) / (kZeroGroups * C);
+        auto zero_pieces = [&](long long first, long long last) {
+            const uint64_t zero[G::P] = {};
+            for (; first < last; ++first) {
+                const int i = static_cast<int>(first / per_row), piece = static_cast<int>(first - static_cast<long long>(i) * per_row);
+                const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, __ldg(p.order + live + q + static_cast<long long>(i) * Q), p.V);
+                const int start = (piece * C + rank) * kZeroGroups, end = min(start + kZeroGroups, row.groups);
+                for (int g = start + lane; g < end; g += 32) row.store(g, zero);
+                if (piece == 0 && rank == 0 && lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
+            }
+        };
+        const long long pieces = static_cast<long long>(dead) * per_row;
+        auto zeros = [&](int k) {
+            if (dead > 0) zero_pieces(pieces * k / mine, pieces * (k + 1) / mine);
+        };
+        if (GRAD && mine == 0) zero_pieces(pieces * h / kNumberWarps, pieces * (h + 1) / kNumberWarps);
         for (int k = h; k < mine; k += kNumberWarps) {
             const long long t = row_of(k);
             const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
@@ -913,13 +942,16 @@ __global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_con
             }
             sum.settle();
             ClassNumbers now{};
-            if (counts) now = class_numbers<MODE>(p, t, in, sum, inv, rank == 0, sums);
-            else if (rank == 0 && lane == 0) class_dead_row<MODE>(p, t);
+            ClassTerms terms;
+            if (counts) now = class_numbers<MODE>(p, in, sum, inv, terms);
             if (lane == 0) {
                 if (GRAD) sh.row[at] = make_float4(now.factor, sum.m, counts ? 1.0f : 0.0f, 0.0f);
                 mbar_arrive(sh.ready + at);
             }
+            if (counts) class_account<MODE>(p, t, in, sum, terms, rank == 0, sums);
+            else if (rank == 0 && lane == 0) class_dead_row<MODE>(p, t);
             if (!GRAD) continue;
+            zeros(k);
             if (edges) store_from_float(row.dx + row.edge(lane), counts ? exp2_fast(fmaf(edge, p.c, -sum.m)) * now.factor : 0.0f);
             // the values at the targets replace what the passes have written, in this CTA's stages
             if (!wait(sh.written + at, parity)) break;
@@ -961,24 +993,29 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
         class_clear_marks(top);
     }
     grid_dependency_wait();
-    long long from = 0, to = p.T;
-    if (MODE == kClassLogp && p.offsets) {
-        from = load_any_id(p.offsets, p.wide_offsets, 0);
-        to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
-    }
     double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
-    if (MODE != kClassLogp) {
-        double n = p.norm;
-        if (n == 0.0 && p.norm_parts > 0)
-            for (int i = 0; i < p.norm_parts; ++i) n += __ldcg(p.norm_part + i);
-        else if (n == 0.0) n = class_norm_warp<MODE>(p);
-        inv = n == 0.0 ? 0.0 : 1.0 / n;
-    }
-    for (long long t = static_cast<long long>(blockIdx.x) * kShortWarps + warp; t < p.T; t += static_cast<long long>(gridDim.x) * kShortWarps) {
+    const long long first = static_cast<long long>(blockIdx.x) * kShortWarps + warp;
+    for (long long t = first; t < p.T; t += static_cast<long long>(gridDim.x) * kShortWarps) {
         const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
         ClassInputs in{};
         bool counts = class_counts(p, t, MODE, &in.target, &in.w);
-        if (MODE == kClassLogp) counts = counts && t >= from && t < to;
+        if (MODE == kClassLogp && p.offsets)
+            counts = counts && t >= load_any_id(p.offsets, p.wide_offsets, 0) && t < load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+        uint4 raw[J];
+        float edge = 0.0f;
+        if (counts) {
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+                if (32 * j + lane < row.groups) raw[j] = row.load(32 * j + lane);
+            if (lane < row.edges) edge = load_local(row.x + row.edge(lane));
+        }
+        if (MODE != kClassLogp && t == first) {     // (beside the first row's loads)
+            double n = p.norm;
+            if (n == 0.0 && p.norm_parts > 0)
+                for (int i = 0; i < p.norm_parts; ++i) n += __ldcg(p.norm_part + i);
+            else if (n == 0.0) n = class_norm_warp<MODE>(p);
+            inv = n == 0.0 ? 0.0 : 1.0 / n;
+        }
         if (!counts) {
             if (GRAD) {
                 const uint64_t zero[G::P] = {};
@@ -988,12 +1025,6 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
             if (lane == 0) class_dead_row<MODE>(p, t);
             continue;
         }
-        uint4 raw[J];
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (32 * j + lane < row.groups) raw[j] = row.load(32 * j + lane);
-        float edge = 0.0f;
-        if (lane < row.edges) edge = load_local(row.x + row.edge(lane));
         class_inputs<MODE>(p, t, row.x, top, in);
         ClassSum sum;
         if (row.groups >= 32 * J) {
@@ -1008,7 +1039,9 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
         if (lane < row.edges) sum.add(edge, p.c);
         sum.over_warp(p.c);
         sum.settle();
-        const ClassNumbers now = class_numbers<MODE>(p, t, in, sum, inv, true, sums);
+        ClassTerms terms;
+        const ClassNumbers now = class_numbers<MODE>(p, in, sum, inv, terms);
+        class_account<MODE>(p, t, in, sum, terms, true, sums);
         if (!GRAD) continue;
         const float m = -sum.m;
         const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), factor2 = f32x2_pack(now.factor, now.factor);

@@ -60,10 +60,11 @@ RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es, bool grad
         for (r.lane_groups = 1; 32 * r.lane_groups < groups;) r.lane_groups *= 2;
         return r;
     }
-    // A row has to fit into a team's ring, or as many CTAs take a row as there are SMs for, if rows are few
+    // Four fifths of a row have to fit into a team's ring (the rest is copied twice, and found in L2 the second time), or as many CTAs take a
+    // row as there are SMs for, if rows are few
     const int64_t stages = (groups + kStageGroups - 1) / kStageGroups;
     auto per_cta = [&] { return (stages + r.cluster - 1) / r.cluster; };
-    while (r.cluster < kMaxCluster && ((grad && per_cta() > depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
+    while (r.cluster < kMaxCluster && ((grad && 4 * per_cta() > 5 * depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
     return r;
 }
 
@@ -309,8 +310,8 @@ int policy_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V
     p.adv = d_advantages;
     p.old_logp = d_old_logp;
     p.ref_logp = d_ref_logp;
-    p.ratio_low = 1.0 - double(opt->clip_low);
-    p.ratio_high = 1.0 + double(opt->clip_high);
+    p.ratio_low = float(1.0 - double(opt->clip_low));
+    p.ratio_high = float(1.0 + double(opt->clip_high));
     p.kl_coef = opt->kl_coef;
     p.norm = opt->norm;
     p.factor = opt->factor;
