@@ -387,21 +387,27 @@ struct ClassTop {
     int* id;                     // [K], -1: absent
     float* q;                    // [K]
     float* x;                    // [K] the student's logits
-    uint32_t* marks;             // [kMarkBits / 32] a bitmap of classes
+    uint32_t* marks;             // a bitmap of classes, 2^bits
+    int bits;
 };
-constexpr int kMarkBits = 1 << 14;
-__host__ __device__ inline size_t class_top_bytes(int K) { return (size_t(K) * 12 + kMarkBits / 8 + 15) / 16 * 16; }
+__host__ __device__ inline int class_mark_bits(int K) {             // at least 32 places for a class: 64 of them find one or so taken
+    int bits = 10;
+    while (bits < 15 && (1 << bits) < 32 * K) ++bits;
+    return bits;
+}
+__host__ __device__ inline size_t class_top_bytes(int K) { return ((size_t(1) << class_mark_bits(K)) / 8 + size_t(K) * 12 + 15) / 16 * 16; }
 __device__ __forceinline__ ClassTop class_top_at(unsigned char* at, int K) {
     ClassTop top;
     top.marks = reinterpret_cast<uint32_t*>(at);
-    at += kMarkBits / 8;
+    top.bits = class_mark_bits(K);
+    at += (1 << top.bits) / 8;
     top.id = reinterpret_cast<int*>(at);
     top.q = reinterpret_cast<float*>(at + 4 * K);
     top.x = reinterpret_cast<float*>(at + 8 * K);
     return top;
 }
 __device__ __forceinline__ void class_clear_marks(const ClassTop& top) {
-    for (int i = threadIdx.x & 31; i < kMarkBits / 128; i += 32) reinterpret_cast<uint4*>(top.marks)[i] = make_uint4(0, 0, 0, 0);
+    for (int i = threadIdx.x & 31; i < (1 << top.bits) / 128; i += 32) reinterpret_cast<uint4*>(top.marks)[i] = make_uint4(0, 0, 0, 0);
     __syncwarp();
 }
 struct ClassEntry {
@@ -430,7 +436,7 @@ __device__ __forceinline__ int class_entry_id(const ClassParams& p, const ClassE
 __device__ __forceinline__ bool class_mark(const ClassTop& top, int id) {
     uint32_t h = static_cast<uint32_t>(id) * 2654435761u;
     h ^= h >> 15;
-    h = h * 2246822519u >> 18;                      // kMarkBits places
+    h = h * 2246822519u >> (32 - top.bits);
     const uint32_t bit = 1u << (h & 31);
     return (atomicOr(top.marks + (h >> 5), bit) & bit) != 0;
 }
@@ -644,31 +650,49 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 
 // ---- long rows -----------------------------------------------------------------------------------------
 // A CTA per row, or a cluster of C.  Its warps have different work, and hand rows to each other through mbarriers:
-//   two teams of eight warps take turns at the rows: first pass (running maximum and sum), then, when the row's numbers are known, second pass
-//     (the gradient).  While one team waits, or reduces, the other one works;
-//   a warp per team copies its rows' 16-byte groups, in stages of 16 KB, into the team's ring of shared memory, as far ahead as the ring
-//     allows (a ring of its own, because who skips the other team's stages cannot tell an mbarrier's phases apart);
+//   two or four teams of warps take turns at the rows: first pass (running maximum and sum), then, when the row's numbers are known, second pass
+//     (the gradient).  While one team waits, or reduces, the others work;
+//   a warp per team copies its rows' 16-byte groups, in stages of 8 to 32 KB, into the team's ring of shared memory, as far ahead as the ring
+//     allows (a ring of its own, because who skips another team's stages cannot tell an mbarrier's phases apart);
 //   kNumberWarps warps take turns at the rows: they fetch what a row has beside its logits, join the sums of the team's warps (and of the
 //     cluster's CTAs, by 8-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
 //     Between them they write zeros into the gradients of rows that do not count, as many at every row (all at once they fill the queues
 //     of the memory system that the others wait in).
 // The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that a row fits.  Of the longest
 // rows, stages that the ring could not hold are copied once more (`dropped`).  Stages are given back in the order of the copies.
-constexpr int kTeams = 2;
-constexpr int kTeamWarps = 8;
-constexpr int kPassWarps = kTeams * kTeamWarps;
-constexpr int kNumberWarps = 4;
-constexpr int kRingThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
-#ifndef RJ
-#define RJ 4
-#endif
-constexpr int kLaneGroups = RJ;                     // of a stage
-constexpr int kWarpGroups = 32 * kLaneGroups;
-constexpr int kStageGroups = kTeamWarps * kWarpGroups;
-constexpr int kStageBytes = kStageGroups * 16;
-constexpr int kRingDepth = 7 * 4 / RJ;               // of a team's ring, at most
+// Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 292 us
+// instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 646 us, two teams
+// 690).  Distillation: the teacher's classes take the room of a stage and every row more of the number warps' time, so there are two teams
+// (4096 x 128000, 64 classes: 395 us, four teams with eight number warps 419).
 constexpr int kMaxCluster = 8;
-constexpr int kRows = 4;                            // rows under way between the warps; a multiple of kNumberWarps and kTeams
+
+template <int MODE>
+struct Ring {
+    static constexpr int kTeams = MODE == kClassPolicy ? 4 : 2;
+    static constexpr int kTeamWarps = 16 / kTeams;
+    static constexpr int kPassWarps = 16;
+    static constexpr int kNumberWarps = 4;
+    static constexpr int kThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
+    static constexpr int kLaneGroups = MODE == kClassLogp ? 8 : 4;              // of a stage
+    static constexpr int kWarpGroups = 32 * kLaneGroups;
+    static constexpr int kStageGroups = kTeamWarps * kWarpGroups;
+    static constexpr int kStageBytes = kStageGroups * 16;
+    static constexpr int kDepth = (224 << 10) / (kTeams * kStageBytes);         // stages of a team's ring, at most
+    static constexpr int kRows = 4;                 // rows under way between the warps; a multiple of kNumberWarps and kTeams
+
+    struct alignas(16) Shared {
+        uint64_t full[kTeams][kDepth], free[kTeams][kDepth];
+        // of row k, at k mod kRows: the team's sums are there; the row's numbers are there; its gradient is written
+        uint64_t summed[kRows], ready[kRows], written[kRows];
+        // the cluster's sums, twice as many rows: a CTA that is ahead sends row k + kRows before this one has looked at row k, but not row
+        // k + 2 kRows, for which it needs this CTA's row k + kRows, which the warp that looks at row k sends later
+        uint64_t joined[2 * kRows];
+        float2 cta_sum[2 * kRows][kMaxCluster];
+        float2 warp_sum[kRows][kTeamWarps];         // largest logit, sum
+        float4 row[kRows];                          // factor, m, 1 where the row counts
+        int abort_word;
+    };
+};
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -685,31 +709,21 @@ __device__ __forceinline__ void send_f32x2(const float2* local, const uint64_t* 
                  : "memory");
 }
 
-struct alignas(16) RingShared {
-    uint64_t full[kTeams][kRingDepth], free[kTeams][kRingDepth];
-    // of row k, at k mod kRows: the team's sums are there; the row's numbers are there; its gradient is written
-    uint64_t summed[kRows], ready[kRows], written[kRows];
-    // the cluster's sums, twice as many rows: a CTA that is ahead sends row k + kRows before this one has looked at row k, but not row
-    // k + 2 kRows, for which it needs this CTA's row k + kRows, which the warp that looks at row k sends later
-    uint64_t joined[2 * kRows];
-    float2 cta_sum[2 * kRows][kMaxCluster];
-    float2 warp_sum[kRows][kTeamWarps];             // largest logit, sum
-    float4 row[kRows];                              // factor, m, 1 where the row counts
-    int abort_word;
-};
-
 template <class E, int MODE, bool GRAD>
-__global__ void __launch_bounds__(kRingThreads, 1) k_class_ring(const __grid_constant__ ClassParams p) {
+__global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __grid_constant__ ClassParams p) {
     using G = ClassGroup<E>;
-    constexpr int N = G::N, J = kLaneGroups;
-    __shared__ RingShared sh;
+    using R = Ring<MODE>;
+    constexpr int N = G::N, J = R::kLaneGroups, kTeams = R::kTeams, kTeamWarps = R::kTeamWarps, kPassWarps = R::kPassWarps,
+                  kNumberWarps = R::kNumberWarps, kRows = R::kRows, kWarpGroups = R::kWarpGroups, kStageGroups = R::kStageGroups,
+                  kStageBytes = R::kStageBytes;
+    __shared__ typename R::Shared sh;
     extern __shared__ __align__(128) unsigned char class_smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, depth = p.depth;
     const int C = p.cluster, shift = __ffs(C) - 1, rank = C > 1 ? int(cluster_rank()) : 0, q = blockIdx.x / C, Q = gridDim.x / C;
     volatile int* abort_flag = &sh.abort_word;
     if (tid == 0) {
         sh.abort_word = 0;
-        for (int i = 0; i < kTeams * kRingDepth; ++i) {
+        for (int i = 0; i < kTeams * R::kDepth; ++i) {
             mbar_init(&sh.full[0][0] + i, 1);
             mbar_init(&sh.free[0][0] + i, kTeamWarps);
         }

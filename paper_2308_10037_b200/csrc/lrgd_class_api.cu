@@ -53,6 +53,7 @@ struct RowPlan {
     int lane_groups;             // 0: rings
     int cluster;
 };
+template <int MODE>
 RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es, bool grad, int depth) {
     const int64_t groups = V * es / 16, sms = plan_sms(ctx);
     RowPlan r{0, 1};
@@ -60,11 +61,11 @@ RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es, bool grad
         for (r.lane_groups = 1; 32 * r.lane_groups < groups;) r.lane_groups *= 2;
         return r;
     }
-    // Four fifths of a row have to fit into a team's ring (the rest is copied twice, and found in L2 the second time), or as many CTAs take a
+    // Three quarters of a row have to fit into a team's ring (the rest is copied twice, and found in L2 the second time), or as many CTAs take a
     // row as there are SMs for, if rows are few
-    const int64_t stages = (groups + kStageGroups - 1) / kStageGroups;
+    const int64_t stages = (groups + Ring<MODE>::kStageGroups - 1) / Ring<MODE>::kStageGroups;
     auto per_cta = [&] { return (stages + r.cluster - 1) / r.cluster; };
-    while (r.cluster < kMaxCluster && ((grad && 4 * per_cta() > 5 * depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
+    while (r.cluster < kMaxCluster && ((grad && 3 * per_cta() > 4 * depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
     return r;
 }
 
@@ -109,11 +110,12 @@ cudaError_t resident_clusters(const void* kern, const cudaLaunchConfig_t& cfg, i
 template <class E, int MODE, bool GRAD>
 int launch_ring(lr_ctx* ctx, ClassParams& p, const RowScratch& at, const Scratch& scratch, cudaStream_t st) {
     using Tag = ClassRowsTag<E, MODE, GRAD>;
+    using R = Ring<MODE>;
     const auto kern = k_class_ring<E, MODE, GRAD>;
-    const size_t smem = size_t(kTeams) * p.depth * kStageBytes + (MODE == kClassDistill ? kNumberWarps * class_top_bytes(p.K) : 0);
+    const size_t smem = size_t(R::kTeams) * p.depth * R::kStageBytes + (MODE == kClassDistill ? R::kNumberWarps * class_top_bytes(p.K) : 0);
     LR_CK(ctx, ensure_dynamic_smem<Tag>(reinterpret_cast<const void*>(kern), int(smem)));
     cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(kRingThreads);
+    cfg.blockDim = dim3(R::kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -185,10 +187,11 @@ int launch_rows(lr_ctx* ctx, ClassParams& p, const RowScratch& at, const Scratch
     p.words = scratch.words;
     p.timeout = ctx->d_status;
     constexpr size_t kSmem = 224 << 10;             // of an SM, for ring and teacher's classes
-    p.depth = kRingDepth;
+    using R = Ring<MODE>;
+    p.depth = R::kDepth;
     if (MODE == kClassDistill)
-        while (p.depth > 1 && size_t(kTeams) * p.depth * kStageBytes + kNumberWarps * class_top_bytes(p.K) > kSmem) --p.depth;
-    const RowPlan plan = plan_rows(ctx, p.T, p.V, sizeof(E), GRAD, p.depth);
+        while (p.depth > 1 && size_t(R::kTeams) * p.depth * R::kStageBytes + R::kNumberWarps * class_top_bytes(p.K) > kSmem) --p.depth;
+    const RowPlan plan = plan_rows<MODE>(ctx, p.T, p.V, sizeof(E), GRAD, p.depth);
     p.cluster = plan.cluster;
     if (plan.lane_groups > 0) return launch_short<E, MODE, GRAD>(ctx, p, plan.lane_groups, at, scratch, st);
     return launch_ring<E, MODE, GRAD>(ctx, p, at, scratch, st);
