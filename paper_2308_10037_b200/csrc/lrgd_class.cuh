@@ -6,10 +6,11 @@
 //                     sequences;  -(1 - smoothing) log sigmoid(h) - smoothing log sigmoid(-h)
 //   distillation      q_k over K of the classes from a teacher's logits;  sum_k q_k (log q_k - lp_k)
 //
-// Everything needs a row's largest logit and the sum of its exponentials, and the gradients read the row again.  Exponentials are powers of
-// two: with c = scale * log2(e) rounded to fp32 once, every term is 2^(fma(x, c, -m)), m = fl(c * largest x); lse = ln 2 * (m + log2 s)
-// with the same m, so that the rounding of m cancels.  The gradient forms the same terms again and multiplies them by -g / s: the
-// probabilities of a row add up to one.  Row sums are fp32 in trees of a thread's own terms, the few numbers of a row fp64.
+// Everything needs a row's largest logit `top` and the sum s of its exponentials, and the gradients read the row again.  Exponentials are
+// powers of two: with c = scale * log2(e) rounded to fp32 once, every term is 2^((x - top) * c), and lse = scale * top + log s.  (The difference
+// comes first, so that rows far from zero keep their bits, and rows of the type's lowest value their sum: x * c would overflow there.)  The
+// gradient forms the same terms again and multiplies them by -g / s: the probabilities of a row add up to one.  Row sums are fp32 in trees of a
+// thread's own terms, the few numbers of a row fp64.
 #pragma once
 #include <cmath>
 
@@ -39,7 +40,7 @@ struct ClassParams {
     // log-probabilities
     float* logp;
     float* lse;
-    // what the preference loss keeps of a row: m and s, lp in fp64; rows outside [offsets[0], offsets[count]) do not count
+    // what the preference loss keeps of a row: its largest logit and its sum, lp in fp64; rows outside [offsets[0], offsets[count]) do not count
     float2* stat;
     double* logp64;
     float* coef;                 // set to 0
@@ -67,6 +68,7 @@ struct ClassParams {
     int depth;
     const double* norm_part;     // short rows: the sum of the weights in parts (k_class_norm), or none
     int norm_parts;
+    long long norm_rows;         // of a part
     double* cta_sum;             // [CTAs][3]
     int* timeout;                // status word of waits
     unsigned int* words;         // [0] CTAs that are done
@@ -93,10 +95,11 @@ __device__ __forceinline__ uint64_t f32x2_mul(uint64_t a, uint64_t b) {
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-// 2^(x * c - m) of both halves
-__device__ __forceinline__ uint64_t exp2_pair(uint64_t x, uint64_t c, uint64_t minus_m) {
+// 2^((x - top) * c), and of both halves
+__device__ __forceinline__ float class_power(float x, float top, float c) { return exp2_fast((x - top) * c); }
+__device__ __forceinline__ uint64_t class_powers(uint64_t x, uint64_t minus_top, uint64_t c) {
     float lo, hi;
-    f32x2_unpack(f32x2_fma(x, c, minus_m), lo, hi);
+    f32x2_unpack(f32x2_mul(f32x2_add(x, minus_top), c), lo, hi);
     return f32x2_pack(exp2_fast(lo), exp2_fast(hi));
 }
 
@@ -111,8 +114,6 @@ struct ClassGroup {
         if constexpr (sizeof(E) == 4) return f32x2_pack(__uint_as_float(word(w, 2 * i)), __uint_as_float(word(w, 2 * i + 1)));
         else return f32x2_pack(__uint_as_float(word(w, i) << 16), __uint_as_float(word(w, i) & 0xffff0000u));
     }
-    // 2^(x * c - m) of pair i
-    static __device__ __forceinline__ uint64_t power(const uint4& w, int i, uint64_t c, uint64_t minus_m) { return exp2_pair(pair(w, i), c, minus_m); }
     static __device__ __forceinline__ uint4 narrow(const uint64_t (&v)[P]) {
         uint32_t u[4];
 #pragma unroll
@@ -157,10 +158,6 @@ struct ClassGroup {
     }
 };
 
-__device__ __forceinline__ void store_group(void* at, const uint4& v) {
-    *reinterpret_cast<uint4*>(at) = v;
-}
-
 // A row as `head` elements, `groups` groups of 16 bytes that start on 16 bytes, and a tail
 template <class E>
 struct ClassRow {
@@ -185,7 +182,7 @@ struct ClassRow {
         constexpr int N = ClassGroup<E>::N;
         E* at = dx + head + g * N;
         if (wide_store) {
-            store_group(at, ClassGroup<E>::narrow(v));
+            *reinterpret_cast<uint4*>(at) = ClassGroup<E>::narrow(v);
         } else {
 #pragma unroll
             for (int i = 0; i < N / 2; ++i) {
@@ -198,21 +195,19 @@ struct ClassRow {
     }
 };
 
-// The running maximum and sum of a part of a row: s = sum of 2^(fma(x, c, -m)), m = fl(c * largest), m = -inf before the first finite x
+// The running maximum and sum of a part of a row: s = sum of 2^((x - top) * c), top = -inf before the first finite x
 struct ClassSum {
-    float top = -INFINITY, m = -INFINITY, s = 0.0f;
+    float top = -INFINITY, s = 0.0f;
     // room for terms up to t; false where nothing finite has come yet
     __device__ __forceinline__ bool raise(float t, float c) {
         if (t > top) {
-            const float next = __fmul_rn(t, c);     // (rounded before anything is taken from it, here and wherever m is formed)
-            s *= exp2_fast(m - next);
+            s *= class_power(top, t, c);
             top = t;
-            m = next;
         }
         return top != -INFINITY;
     }
     __device__ __forceinline__ void add(float v, float c) {
-        if (raise(v, c)) s += exp2_fast(fmaf(v, c, -m));
+        if (raise(v, c)) s += class_power(v, top, c);
         else if (v != v) s = v;
     }
     template <class E, int J>
@@ -229,12 +224,12 @@ struct ClassSum {
                 }
             return;
         }
-        const uint64_t c2 = f32x2_pack(c, c), m2 = f32x2_pack(-m, -m);
+        const uint64_t c2 = f32x2_pack(c, c), top2 = f32x2_pack(-top, -top);
         uint64_t part[2] = {0, 0};
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int i = 0; i < G::P; ++i) part[i & 1] = f32x2_add(part[i & 1], G::power(raw[j], i, c2, m2));
+            for (int i = 0; i < G::P; ++i) part[i & 1] = f32x2_add(part[i & 1], class_powers(G::pair(raw[j], i), top2, c2));
         float lo, hi;
         f32x2_unpack(f32x2_add(part[0], part[1]), lo, hi);
         s += lo + hi;
@@ -242,21 +237,15 @@ struct ClassSum {
     // the sum over the lanes of a warp, the same bits in all of them
     __device__ __forceinline__ void over_warp(float c) {
         const uint32_t key = __reduce_max_sync(0xffffffffu, order_key(top));
-        top = __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
-        const float next = __fmul_rn(top, c);
-        s = s == 0.0f ? 0.0f : s * exp2_fast(m - next);             // (a NaN stays one)
-        m = next;
+        const float most = __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
+        s = s == 0.0f ? 0.0f : s * class_power(top, most, c);       // (a NaN stays one)
+        top = most;
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
     }
-    __device__ __forceinline__ void set(float top2, float s2, float c) {
-        top = top2;
-        m = __fmul_rn(top2, c);
-        s = s2;
-    }
-    // where no logit is finite s is 0 (or NaN), and m is not used
+    // where no logit is finite s is 0 (or NaN): lse is -inf, a probability NaN
     __device__ __forceinline__ void settle() {
-        if (top == -INFINITY) m = 0.0f;
+        if (top == -INFINITY) top = 0.0f;
     }
 };
 
@@ -282,16 +271,16 @@ __device__ __forceinline__ double warp_sum64(double v) {
     return v;
 }
 
-// m + log2 of the sum.  The sum is 2^e f with 1 <= f < 2, so that the fp32 logarithm is one of a number below 1 and off by 6e-8 at most.
+// log of the sum.  It is 2^e f with 1 <= f < 2, so that the fp32 logarithm is one of a number below 1 and off by 6e-8 at most.
 // exp2_fast drops the bits of its argument below 2^-23 or so: terms below 1/2 come out 4.9e-8 too small in the mean (measured over 4 M
 // random arguments; 2.2e-8 between 1/2 and 1, the largest term is exact).  One row's lp does not show that, the sum over a long sequence does;
 // in the gradient it cancels, whose numerator has the same terms.
-__device__ __forceinline__ double class_lse2(float m, float s) {
-    if (!(s > 0.0f && s < INFINITY)) return static_cast<double>(m) + log2f(s);
+__device__ __forceinline__ double class_log(float s) {
+    if (!(s > 0.0f && s < INFINITY)) return logf(s);
     const uint32_t bits = __float_as_uint(s);       // (at least 1 where it is positive: the largest term)
     const int e = static_cast<int>(bits >> 23) - 127;
     const float f = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
-    return (static_cast<double>(m) + e) + (static_cast<double>(log2f(f)) + 7.07e-8 * (1.0 - __fdividef(1.0f, s)));
+    return kLn2 * (e + static_cast<double>(log2f(f))) + 4.9e-8 * (1.0 - __fdividef(1.0f, s));
 }
 
 // ---- which rows count ----------------------------------------------------------------------------------
@@ -323,6 +312,7 @@ template <int MODE>
 __global__ void __launch_bounds__(kPrepThreads) k_class_prep(const __grid_constant__ ClassParams p, int* order, ClassPrep* prep) {
     __shared__ double warp_norm[kPrepThreads / 32];
     __shared__ int warp_live[kPrepThreads / 32];
+    static_assert(kPrepThreads == 32 * 32, "a lane for every warp");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_dependency_release();
     long long from = 0, to = p.T;
@@ -354,12 +344,9 @@ __global__ void __launch_bounds__(kPrepThreads) k_class_prep(const __grid_consta
         __syncthreads();                            // the last turn's counts have been read
         if (lane == 0) warp_live[warp] = mine;
         __syncthreads();
-        int at = before, all = 0;
-        for (int w = 0; w < kPrepThreads / 32; ++w) {
-            const int n = warp_live[w];
-            if (w < warp) at += n;
-            all += n;
-        }
+        const int of_lane = warp_live[lane];
+        const int all = __reduce_add_sync(0xffffffffu, of_lane);
+        int at = before + __reduce_add_sync(0xffffffffu, lane < warp ? of_lane : 0);
         before += all;
 #pragma unroll
         for (int j = 0; j < kPrepItems; ++j) {
@@ -373,16 +360,17 @@ __global__ void __launch_bounds__(kPrepThreads) k_class_prep(const __grid_consta
     norm = warp_sum64(norm);
     if (lane == 0) warp_norm[warp] = norm;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        norm = 0.0;
-        for (int w = 0; w < kPrepThreads / 32; ++w) norm += warp_norm[w];
-        prep->norm = norm;
-        prep->live = before;
+    if (warp == 0) {
+        norm = warp_sum64(warp_norm[lane]);
+        if (lane == 0) {
+            prep->norm = norm;
+            prep->live = before;
+        }
     }
 }
 
 // ---- a teacher's classes -------------------------------------------------------------------------------
-// One warp has them: entry j belongs to lane j mod 32.  q is 2^(c * v - base), times `part` it is the weight.
+// One warp has them: entry j belongs to lane j mod 32.  q is 2^((v - base) * c), times a factor it is the weight.
 struct ClassTop {
     int* id;                     // [K], -1: absent
     float* q;                    // [K]
@@ -441,9 +429,11 @@ __device__ __forceinline__ bool class_mark(const ClassTop& top, int id) {
     return (atomicOr(top.marks + (h >> 5), bit) & bit) != 0;
 }
 
-// What the entries add up to
+// What the entries add up to.  The student's logits may be as far apart as fp32 allows (masked by the lowest value): their sum is kept small.
+constexpr float kFar = 4096.0f;
 struct ClassTopSum {
-    float all, cross;            // sum of q, sum of q * (c * v - base - c * x)
+    float all, own, his;         // sum of q, of q * (v - base) * c, of q * (x - near) / kFar
+    float near;                  // the largest of their x
     bool twice;                  // some class is named twice
 };
 // Reads a row's classes; the bitmap is empty before and after.  Eight entries of a lane are on their way together.
@@ -451,9 +441,9 @@ template <class E>
 __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long long t, const E* row, const ClassTop& top) {
     constexpr int U = 8;
     const int lane = threadIdx.x & 31;
-    ClassTopSum r{0.0f, 0.0f, false};
+    ClassTopSum r{0.0f, 0.0f, 0.0f, -INFINITY, false};
     float largest = -INFINITY;
-    const double lse2 = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) * (static_cast<double>(p.c) / p.scale) : 0.0;
+    const double own = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) / p.scale : 0.0;
     for (int j0 = 0; j0 < p.K; j0 += 32 * U) {
         ClassEntry e[U];
         int id[U];
@@ -475,7 +465,10 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
                 top.q[j] = e[i].v;
                 top.x[j] = x[i];
             }
-            if (id[i] >= 0) largest = fmaxf(largest, e[i].v);
+            if (id[i] >= 0) {
+                largest = fmaxf(largest, e[i].v);
+                r.near = fmaxf(r.near, x[i]);
+            }
         }
         __syncwarp();
         for (uint32_t lanes = __ballot_sync(0xffffffffu, taken != 0); lanes && !r.twice; lanes = __ballot_sync(0xffffffffu, taken != 0)) {
@@ -487,20 +480,26 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
         }
     }
     largest = warp_max(largest);
-    // 2^(c v - base): base is the largest c v rounded, or the teacher's own, in two parts
-    const float high = p.teacher_lse ? static_cast<float>(lse2) : largest == -INFINITY ? 0.0f : __fmul_rn(largest, p.c),
-                low = p.teacher_lse ? static_cast<float>(lse2 - static_cast<double>(high)) : 0.0f;
+    r.near = warp_max(r.near);
+    if (r.near == -INFINITY) r.near = 0.0f;
+    // base is the largest v, or the teacher's own lse / scale in two parts
+    const float high = p.teacher_lse ? static_cast<float>(own) : largest == -INFINITY ? 0.0f : largest,
+                low = p.teacher_lse ? static_cast<float>((own - static_cast<double>(high)) * p.c) : 0.0f;
     for (int j = lane; j < p.K; j += 32) {
-        const float a = fmaf(top.q[j], p.c, -high) - low;
+        const float a = (top.q[j] - high) * p.c - low;
         const float e = top.id[j] >= 0 ? exp2f(a) : 0.0f;
         r.all += e;
-        if (e != 0.0f) r.cross += e * fmaf(-p.c, top.x[j], a);
+        if (e != 0.0f) {
+            r.own += e * a;
+            r.his += e * ((top.x[j] - r.near) * (1.0f / kFar));
+        }
         top.q[j] = e;
     }
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) {
         r.all += __shfl_xor_sync(0xffffffffu, r.all, d);
-        r.cross += __shfl_xor_sync(0xffffffffu, r.cross, d);
+        r.own += __shfl_xor_sync(0xffffffffu, r.own, d);
+        r.his += __shfl_xor_sync(0xffffffffu, r.his, d);
     }
     class_clear_marks(top);
     return r;
@@ -533,40 +532,41 @@ __device__ __forceinline__ void class_inputs(const ClassParams& p, long long t, 
 }
 // ... and what of it is written down afterwards
 struct ClassTerms {
-    double lp, lse2;
+    double lp, lse;
     float first, kl, clipped;    // the row's loss: its parts (distillation: kl alone)
 };
 template <int MODE>
 __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, const ClassInputs& in, const ClassSum& sum, double inv, ClassTerms& terms) {
     const int lane = threadIdx.x & 31;
-    const double lse2 = class_lse2(sum.m, sum.s);
+    const double log_s = class_log(sum.s);
     ClassNumbers r{};
-    terms = ClassTerms{0.0, lse2, 0.0f, 0.0f, 0.0f};
+    terms = ClassTerms{0.0, static_cast<double>(sum.top) * p.scale + log_s, 0.0f, 0.0f, 0.0f};
     const float gain = static_cast<float>(in.w * inv * p.factor * p.scale);
     if (MODE == kClassDistill) {
-        // with the teacher's own normalisation log2 q is smaller by log2(all)
+        // with the teacher's own normalisation log q is smaller by log(all)
         const float all = in.top.all, one = p.teacher_lse || all == 0.0f ? 1.0f : 1.0f / all, mass = p.teacher_lse || all == 0.0f ? all : 1.0f;
-        terms.kl = all == 0.0f ? 0.0f : static_cast<float>(kLn2 * (in.top.cross * one + mass * (lse2 + log2f(one))));
+        const double ahead = (static_cast<double>(sum.top) - in.top.near) * p.scale;
+        terms.kl = all == 0.0f ? 0.0f
+                               : static_cast<float>((kLn2 * in.top.own - static_cast<double>(in.top.his) * kFar * p.scale) * one +
+                                                    mass * (ahead + log_s + logf(one)));
         r.factor = mass == 0.0f ? 0.0f : gain * mass / sum.s;
         r.at = gain * one;
         return r;
     }
-    terms.lp = kLn2 * (static_cast<double>(in.xy) * p.c - lse2);
+    terms.lp = (static_cast<double>(in.xy) - sum.top) * p.scale - log_s;
     if (terms.lp > 0.0) terms.lp = 0.0;             // rounding
     if (MODE == kClassPolicy) {
         // exp(lp - old) - 1, exp(ref - lp) - 1 and exp(lp) - 1: one lane each.  The differences are fp64, their exponentials fp32 (one unit in
         // the last place).
         const float d = static_cast<float>(lane == 0 ? terms.lp - in.old_logp : lane == 1 ? in.ref_logp - terms.lp : terms.lp);
         const float e = expm1f(d);
-        const float ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0) + 1.0f : 1.0f, away = __shfl_sync(0xffffffffu, e, 1),
-                    rest = __shfl_sync(0xffffffffu, e, 2);
+        float ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0) + 1.0f : 1.0f;
+        if (ratio > 3.4e38f) ratio = 3.4e38f;       // (no infinity: an advantage of 0 has no loss whatever the ratio)
+        const float away = __shfl_sync(0xffffffffu, e, 1), rest = __shfl_sync(0xffffffffu, e, 2);
         const float a = in.adv, held = fminf(fmaxf(ratio, p.ratio_low), p.ratio_high);
         const bool clipped = ratio * a > held * a;
         float g = clipped ? 0.0f : -ratio * a;
-        if (p.ref_logp) {
-            terms.kl = away - __shfl_sync(0xffffffffu, d, 1);
-            g -= p.kl_coef * away;
-        }
+        if (p.ref_logp) g -= p.kl_coef * away;
         terms.first = -(clipped ? held : ratio) * a;
         terms.clipped = clipped ? 1.0f : 0.0f;
         g *= gain;
@@ -586,20 +586,23 @@ __device__ __forceinline__ void class_account(const ClassParams& p, long long t,
     }
     if (p.logp && write) p.logp[t] = static_cast<float>(terms.lp);
     if (MODE == kClassLogp) {
-        if (p.lse && write) p.lse[t] = static_cast<float>(kLn2 * terms.lse2);
+        if (p.lse && write) p.lse[t] = static_cast<float>(terms.lse);
         if (p.stat && write) {
-            p.stat[t] = make_float2(sum.m, sum.s);
+            p.stat[t] = make_float2(sum.top, sum.s);
             p.logp64[t] = terms.lp;
             p.coef[t] = 0.0f;
         }
     } else {
         sums[0] += static_cast<double>(in.w) * terms.first;
-        sums[1] += static_cast<double>(in.w) * terms.kl;
+        if (p.ref_logp) {                           // (a difference of nearly equal numbers where the policies are near each other: fp64)
+            const double d = in.ref_logp - terms.lp;
+            sums[1] += in.w * (d == INFINITY ? d : expm1(d) - d);
+        }
         sums[2] += terms.clipped != 0.0f ? in.w : 0.0f;
     }
 }
 // What the gradient is at entry j of the teacher's classes
-__device__ __forceinline__ float class_top_value(const ClassParams& p, const ClassTop& top, int j, bool twice, float m, const ClassNumbers& r) {
+__device__ __forceinline__ float class_top_value(const ClassParams& p, const ClassTop& top, int j, bool twice, float largest, const ClassNumbers& r) {
     const int id = top.id[j];
     float q = top.q[j];
     if (twice) {                                    // a class that the teacher names twice has both weights
@@ -607,7 +610,7 @@ __device__ __forceinline__ float class_top_value(const ClassParams& p, const Cla
         for (int i = 0; i < p.K; ++i)
             if (top.id[i] == id) q += top.q[i];
     }
-    return fmaf(exp2_fast(fmaf(top.x[j], p.c, -m)), r.factor, -r.at * q);
+    return fmaf(class_power(top.x[j], largest, p.c), r.factor, -r.at * q);
 }
 // Sum of the weights of all rows that count, by one warp
 template <int MODE>
@@ -671,7 +674,7 @@ struct Ring {
     static constexpr int kTeams = MODE == kClassPolicy ? 4 : 2;
     static constexpr int kTeamWarps = 16 / kTeams;
     static constexpr int kPassWarps = 16;
-    static constexpr int kNumberWarps = 4;
+    static constexpr int kNumberWarps = 4;          // (eight are no faster: policy 647 us, distillation 402)
     static constexpr int kThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
     static constexpr int kLaneGroups = MODE == kClassLogp ? 8 : 4;              // of a stage
     static constexpr int kWarpGroups = 32 * kLaneGroups;
@@ -689,11 +692,16 @@ struct Ring {
         uint64_t joined[2 * kRows];
         float2 cta_sum[2 * kRows][kMaxCluster];
         float2 warp_sum[kRows][kTeamWarps];         // largest logit, sum
-        float4 row[kRows];                          // factor, m, 1 where the row counts
+        float4 row[kRows];                          // factor, top, 1 where the row counts
         int abort_word;
     };
 };
 
+__device__ __forceinline__ uint64_t l2_policy_evict_normal() {
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(pol));
+    return pol;
+}
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -756,7 +764,8 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             const int team = warp - kPassWarps;
             uint64_t *full = sh.full[team], *free = sh.free[team];
             unsigned char* ring = class_smem + team * depth * kStageBytes;
-            const uint64_t once = l2_policy_evict_first();
+            // (rows that a later pass reads again may stay in L2)
+            const uint64_t once = MODE == kClassLogp && p.stat ? l2_policy_evict_normal() : l2_policy_evict_first();
             int slot = 0, parity = 0, copies = 0;
             bool ok = true;
             int t = row_of(team);
@@ -850,7 +859,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (!ok) break;
             const float4 numbers = sh.row[at];
             const bool counts = numbers.z != 0.0f;
-            const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(-numbers.y, -numbers.y), factor2 = f32x2_pack(numbers.x, numbers.x);
+            const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-numbers.y, -numbers.y), factor2 = f32x2_pack(numbers.x, numbers.x);
             auto second = [&](int i, int from) {
                 const int first = (i * C + rank) * kStageGroups + in_team * kWarpGroups, left = row.groups - first;
                 uint4 raw[J];
@@ -859,7 +868,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                 auto group = [&](int j) {
                     uint64_t v[G::P];
 #pragma unroll
-                    for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(G::power(raw[j], e, c2, m2), factor2);
+                    for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(class_powers(G::pair(raw[j], e), top2, c2), factor2);
                     row.store(first + lane + 32 * j, v);
                 };
                 if (!counts) {
@@ -941,7 +950,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             const int at = k % kRows, parity = (k / kRows) & 1;
             if (!wait(sh.summed + at, parity)) break;
             ClassSum sum;
-            if (lane < kTeamWarps) sum.set(sh.warp_sum[at][lane].x, sh.warp_sum[at][lane].y, p.c);
+            if (lane < kTeamWarps) sum = ClassSum{sh.warp_sum[at][lane].x, sh.warp_sum[at][lane].y};
             if (edges) sum.add(edge, p.c);
             sum.over_warp(p.c);
             if (C > 1) {
@@ -951,7 +960,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                 if (lane < C) send_f32x2(&sh.cta_sum[at2][rank], sh.joined + at2, lane, sum.top, sum.s);
                 if (!wait(sh.joined + at2, (k / (2 * kRows)) & 1)) break;
                 sum = ClassSum{};
-                if (lane < C) sum.set(sh.cta_sum[at2][lane].x, sh.cta_sum[at2][lane].y, p.c);
+                if (lane < C) sum = ClassSum{sh.cta_sum[at2][lane].x, sh.cta_sum[at2][lane].y};
                 sum.over_warp(p.c);
             }
             sum.settle();
@@ -959,14 +968,14 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             ClassTerms terms;
             if (counts) now = class_numbers<MODE>(p, in, sum, inv, terms);
             if (lane == 0) {
-                if (GRAD) sh.row[at] = make_float4(now.factor, sum.m, counts ? 1.0f : 0.0f, 0.0f);
+                if (GRAD) sh.row[at] = make_float4(now.factor, sum.top, counts ? 1.0f : 0.0f, 0.0f);
                 mbar_arrive(sh.ready + at);
             }
             if (counts) class_account<MODE>(p, t, in, sum, terms, rank == 0, sums);
             else if (rank == 0 && lane == 0) class_dead_row<MODE>(p, t);
             if (!GRAD) continue;
             zeros(k);
-            if (edges) store_from_float(row.dx + row.edge(lane), counts ? exp2_fast(fmaf(edge, p.c, -sum.m)) * now.factor : 0.0f);
+            if (edges) store_from_float(row.dx + row.edge(lane), counts ? class_power(edge, sum.top, p.c) * now.factor : 0.0f);
             // the values at the targets replace what the passes have written, in this CTA's stages
             if (!wait(sh.written + at, parity)) break;
             if (!counts) continue;
@@ -980,7 +989,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             } else {
                 __syncwarp();
                 for (int j = lane; j < p.K; j += 32)
-                    if (top.id[j] >= 0 && here(top.id[j])) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, in.top.twice, sum.m, now));
+                    if (top.id[j] >= 0 && here(top.id[j])) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, in.top.twice, sum.top, now));
                 __syncwarp();
             }
         }
@@ -1023,11 +1032,15 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
                 if (32 * j + lane < row.groups) raw[j] = row.load(32 * j + lane);
             if (lane < row.edges) edge = load_local(row.x + row.edge(lane));
         }
+        if (counts) class_inputs<MODE>(p, t, row.x, top, in);
         if (MODE != kClassLogp && t == first) {     // (beside the first row's loads)
             double n = p.norm;
-            if (n == 0.0 && p.norm_parts > 0)
-                for (int i = 0; i < p.norm_parts; ++i) n += __ldcg(p.norm_part + i);
-            else if (n == 0.0) n = class_norm_warp<MODE>(p);
+            if (n == 0.0 && p.norm_parts > 0) {
+                for (int i = lane; i < p.norm_parts; i += 32) n += __ldcg(p.norm_part + i);
+                n = warp_sum64(n);
+            } else if (n == 0.0) {
+                n = class_norm_warp<MODE>(p);
+            }
             inv = n == 0.0 ? 0.0 : 1.0 / n;
         }
         if (!counts) {
@@ -1039,7 +1052,6 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
             if (lane == 0) class_dead_row<MODE>(p, t);
             continue;
         }
-        class_inputs<MODE>(p, t, row.x, top, in);
         ClassSum sum;
         if (row.groups >= 32 * J) {
             sum.add_groups<E, J>(raw, p.c);
@@ -1057,24 +1069,23 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
         const ClassNumbers now = class_numbers<MODE>(p, in, sum, inv, terms);
         class_account<MODE>(p, t, in, sum, terms, true, sums);
         if (!GRAD) continue;
-        const float m = -sum.m;
-        const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), factor2 = f32x2_pack(now.factor, now.factor);
+        const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-sum.top, -sum.top), factor2 = f32x2_pack(now.factor, now.factor);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             if (32 * j + lane < row.groups) {
                 uint64_t v[G::P];
 #pragma unroll
-                for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(G::power(raw[j], e, c2, m2), factor2);
+                for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(class_powers(G::pair(raw[j], e), top2, c2), factor2);
                 row.store(32 * j + lane, v);
             }
         }
-        if (lane < row.edges) store_from_float(row.dx + row.edge(lane), exp2_fast(fmaf(edge, p.c, m)) * now.factor);
+        if (lane < row.edges) store_from_float(row.dx + row.edge(lane), class_power(edge, sum.top, p.c) * now.factor);
         __syncwarp();                               // the targets' values replace what was just written
         if (MODE == kClassPolicy) {
             if (lane == 0) store_from_float(row.dx + in.target, now.at);
         } else {
             for (int j = lane; j < p.K; j += 32)
-                if (top.id[j] >= 0) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, in.top.twice, sum.m, now));
+                if (top.id[j] >= 0) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, in.top.twice, sum.top, now));
             __syncwarp();
         }
     }
@@ -1090,15 +1101,14 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
     class_finish<MODE>(p, blockIdx.x, gridDim.x, inv, sums);
 }
 
-// norm_part[b] = sum of the weights of the rows that count among rows b * kNormRows ...
+// norm_part[b] = sum of the weights of the rows that count among rows b * norm_rows ...
 constexpr int kNormThreads = 256;
-constexpr int kNormRows = 4096;
 
 template <int MODE>
 __global__ void __launch_bounds__(kNormThreads) k_class_norm(const __grid_constant__ ClassParams p, double* part) {
     __shared__ double warp_part[kNormThreads / 32];
     grid_dependency_release();
-    const long long first = static_cast<long long>(blockIdx.x) * kNormRows, last = min(first + kNormRows, p.T);
+    const long long first = blockIdx.x * p.norm_rows, last = min(first + p.norm_rows, p.T);
     double sum = 0.0;
     for (long long t = first + threadIdx.x; t < last; t += kNormThreads) {
         long long target;
@@ -1116,7 +1126,7 @@ __global__ void __launch_bounds__(kNormThreads) k_class_norm(const __grid_consta
 }
 
 // ---- gradient of log-probabilities ---------------------------------------------------------------------
-// Rows whose statistics are known: from the caller (lse, fp32) or from an earlier pass (m and s).  One read, one write.
+// Rows whose statistics are known: from the caller (lse, fp32) or from an earlier pass (top and s).  One read, one write.
 struct ClassGradParams {
     const void* x;
     long long ld;
@@ -1138,10 +1148,7 @@ struct ClassGradParams {
 };
 
 constexpr int kClassGradThreads = 256;
-#ifndef GU
-#define GU 4
-#endif
-constexpr int kClassGradGroups = GU;                // per thread, all on their way before the first is worked on
+constexpr int kClassGradGroups = 4;                 // per thread, all on their way before the first is worked on
 
 template <class E>
 __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_constant__ ClassGradParams p) {
@@ -1193,24 +1200,24 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (first + u * threads < row.groups) raw[u] = row.load(first + u * threads);
-        float m, k;
+        float base, k;
         if (p.stat) {
-            m = -now.stat.x;
+            base = now.stat.x;
             k = -gt / now.stat.y;
-        } else {                                    // lse in the units of c, the part below fp32 put into the factor
-            const double l2 = static_cast<double>(now.stat.x) * (static_cast<double>(p.c) / p.scale);
-            m = -static_cast<float>(l2);
-            k = -gt * exp2_fast(static_cast<float>(-static_cast<double>(m) - l2));
+        } else {                                    // lse / scale in place of the largest logit, the part below fp32 put into the factor
+            const double own = static_cast<double>(now.stat.x) / p.scale;
+            base = static_cast<float>(own);
+            k = -gt * exp2_fast(static_cast<float>((static_cast<double>(base) - own) * p.c));
         }
         const int where = static_cast<int>(now.target) - row.head;
-        const uint64_t c2 = f32x2_pack(p.c, p.c), m2 = f32x2_pack(m, m), k2 = f32x2_pack(k, k);
+        const uint64_t c2 = f32x2_pack(p.c, p.c), base2 = f32x2_pack(-base, -base), k2 = f32x2_pack(k, k);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int g = first + u * threads;
             if (g >= row.groups) break;
             uint64_t v[G::P];
 #pragma unroll
-            for (int j = 0; j < G::P; ++j) v[j] = f32x2_mul(exp2_pair(G::pair(raw[u], j), c2, m2), k2);
+            for (int j = 0; j < G::P; ++j) v[j] = f32x2_mul(class_powers(G::pair(raw[u], j), base2, c2), k2);
             if (where >= g * N && where < g * N + N) {
 #pragma unroll
                 for (int j = 0; j < G::P; ++j) {
@@ -1222,7 +1229,7 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
         }
         if (edges) {
             const int at = row.edge(tid);
-            const float v = exp2_fast(fmaf(load_local(row.x + at), p.c, m)) * k;
+            const float v = class_power(load_local(row.x + at), base, p.c) * k;
             store_from_float(row.dx + at, at == now.target ? v + gt : v);
         }
     }
@@ -1260,6 +1267,7 @@ __global__ void __launch_bounds__(kPairThreads) k_class_pair(const __grid_consta
     __shared__ double total[3];
     __shared__ bool last_cta;
     const int tid = threadIdx.x, warp = tid >> 5, side = tid >= kPairThreads / 2, lane = tid & (kPairThreads / 2 - 1);
+    grid_dependency_release();
     grid_dependency_wait();
     double sum = 0.0;                               // of the weights, the same in every CTA
     if (p.norm == 0.0 && p.weights)
@@ -1277,6 +1285,8 @@ __global__ void __launch_bounds__(kPairThreads) k_class_pair(const __grid_consta
     for (long long pair = blockIdx.x; pair < p.P; pair += gridDim.x) {
         __syncthreads();
         const long long seq = pair + (side ? p.P : 0);
+        const float w = p.weights ? __ldg(p.weights + pair) : 1.0f;
+        const double ref = p.ref ? static_cast<double>(__ldg(p.ref + pair)) - static_cast<double>(__ldg(p.ref + p.P + pair)) : 0.0;
         long long a = load_any_id(p.offsets, p.wide_offsets, seq), z = load_any_id(p.offsets, p.wide_offsets, seq + 1);
         if (a < 0 || z < a || z > p.T) {            // no sequence: nothing is read
             if (lane == 0) atomicExch(p.status, -4);
@@ -1296,35 +1306,34 @@ __global__ void __launch_bounds__(kPairThreads) k_class_pair(const __grid_consta
             warp_part[warp][1] = count;
         }
         __syncthreads();
-        double s[2], size[2];
+        double s[2], rows[2];
         for (int j = 0; j < 2; ++j) {
             s[j] = 0.0;
-            size[j] = 0.0;
+            rows[j] = 0.0;
             for (int i = 0; i < kPairThreads / 64; ++i) {
                 s[j] += warp_part[j * (kPairThreads / 64) + i][0];
-                size[j] += warp_part[j * (kPairThreads / 64) + i][1];
+                rows[j] += warp_part[j * (kPairThreads / 64) + i][1];
             }
-            if (!p.average || size[j] == 0.0) size[j] = 1.0;
-            s[j] /= size[j];
+            if (!p.average || rows[j] == 0.0) rows[j] = 1.0;
+            s[j] /= rows[j];
         }
         if (tid == 0) {
-            const double d = (s[0] - (p.ref ? static_cast<double>(__ldg(p.ref + pair)) : 0.0)) -
-                             (s[1] - (p.ref ? static_cast<double>(__ldg(p.ref + p.P + pair)) : 0.0));
-            const double h = p.beta * d - p.margin, w = p.weights ? static_cast<double>(__ldg(p.weights + pair)) : 1.0;
-            // log sigmoid(h) = -softplus(-h), log sigmoid(-h) = -softplus(h)
-            const double soft = log1p(exp(-fabs(h))), plus = fmax(h, 0.0) + soft, minus = fmax(-h, 0.0) + soft;
-            const double right = 1.0 / (1.0 + exp(-h)), wrong = 1.0 / (1.0 + exp(h));
+            const double h = p.beta * (s[0] - s[1] - ref) - p.margin;
+            // log sigmoid(h) = -softplus(-h), log sigmoid(-h) = -softplus(h); t = exp(-|h|) and what follows from it in fp32 (see logistic_terms)
+            const float size = fabsf(static_cast<float>(h)), t = expf(-size) * (1.0f - static_cast<float>(fabs(h) - size)), one = 1.0f / (1.0f + t);
+            const double soft = log1pf(t), plus = fmax(h, 0.0) + soft, minus = fmax(-h, 0.0) + soft;
+            const float right = h >= 0.0 ? one : t * one, wrong = h >= 0.0 ? t * one : one;
             const double loss = (1.0 - p.smoothing) * minus + p.smoothing * plus;
-            p.pair_loss[pair] = w == 0.0 ? 0.0 : w * loss;
+            p.pair_loss[pair] = w == 0.0f ? 0.0 : w * loss;
             p.h[pair] = static_cast<float>(h);
             if (p.seq_logp) {
                 p.seq_logp[pair] = static_cast<float>(s[0]);
                 p.seq_logp[p.P + pair] = static_cast<float>(s[1]);
             }
-            total[0] = w == 0.0 ? 0.0 : w * inv * p.factor * p.beta * (p.smoothing * right - (1.0 - p.smoothing) * wrong);
+            total[0] = w == 0.0f ? 0.0 : w * inv * p.factor * p.beta * (p.smoothing * right - (1.0 - p.smoothing) * wrong);
         }
         __syncthreads();
-        const float g = static_cast<float>((side ? -total[0] : total[0]) / size[side]);
+        const float g = static_cast<float>((side ? -total[0] : total[0]) / rows[side]);
         for (long long t = a + lane; t < z; t += kPairThreads / 2) p.coef[t] = g;
     }
     if (tid == 0) {

@@ -24,10 +24,12 @@ constexpr int64_t kMaxPairs = int64_t(1) << 24;
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
+float class_c(float scale) { return float(double(scale) * 1.4426950408889634074); }        // scale * log2(e)
+
 int check_rows(int64_t T, int32_t V, int64_t ld, int32_t id_bytes, float scale) {
     if (T < 0 || T > kMaxRows || V < 1 || V > kMaxClasses || ld < V || ld > kMaxPitch) return LR_ERR_SHAPE;
     if (id_bytes != 4 && id_bytes != 8) return LR_ERR_VALUE;
-    if (!std::isfinite(scale) || !(scale > 0.0f)) return LR_ERR_VALUE;
+    if (!(scale > 0.0f) || !std::isfinite(class_c(scale))) return LR_ERR_VALUE;
     return LR_OK;
 }
 bool norm_ok(float norm, float factor) { return std::isfinite(norm) && norm >= 0.0f && std::isfinite(factor); }
@@ -37,11 +39,12 @@ template <class E>
 bool apart(const E* x, int64_t ld, const E* dx, int64_t ld_d, int64_t T, int64_t V) {
     if (T == 0) return true;
     if (x == dx) return ld == ld_d || T == 1;
-    const intptr_t a = reinterpret_cast<intptr_t>(x), b = reinterpret_cast<intptr_t>(dx), es = sizeof(E);
-    const intptr_t a_end = a + ((T - 1) * ld + V) * es, b_end = b + ((T - 1) * ld_d + V) * es;
+    using Wide = __int128;                          // (a leading dimension may be anything up to 2^40)
+    const Wide a = Wide(reinterpret_cast<uintptr_t>(x)), b = Wide(reinterpret_cast<uintptr_t>(dx)), es = sizeof(E);
+    const Wide a_end = a + (Wide(T - 1) * ld + V) * es, b_end = b + (Wide(T - 1) * ld_d + V) * es;
     if (a_end <= b || b_end <= a) return true;
     if (ld != ld_d) return false;
-    const intptr_t pitch = ld * es, off = ((b - a) % pitch + pitch) % pitch;                // columns of one wider matrix
+    const Wide pitch = Wide(ld) * es, off = ((b - a) % pitch + pitch) % pitch;             // columns of one wider matrix
     return off >= V * es && off + V * es <= pitch;
 }
 
@@ -156,7 +159,8 @@ int launch_short(lr_ctx* ctx, ClassParams& p, int lane_groups, const RowScratch&
     if (MODE != kClassLogp && p.norm == 0.0 && p.T > kNormInline) {
         double* part = reinterpret_cast<double*>(scratch.data + at.sums + at.prep);
         p.norm_part = part;
-        p.norm_parts = int((p.T + kNormRows - 1) / kNormRows);
+        p.norm_rows = std::max<int64_t>(4096, (p.T + 1023) / 1024);
+        p.norm_parts = int((p.T + p.norm_rows - 1) / p.norm_rows);
         const int r = launched(ctx, [&] { k_class_norm<MODE><<<p.norm_parts, kNormThreads, 0, st>>>(p, part); });
         if (r != LR_OK) return r;
         dependent = ctx->overlap;
@@ -209,7 +213,7 @@ ClassParams row_params(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, in
     p.wide_ids = id_bytes == 8;
     p.ignore = ignore;
     p.scale = scale;
-    p.c = float(double(scale) * 1.4426950408889634074);
+    p.c = class_c(scale);
     p.status = ctx->d_status + 1;
     return p;
 }
@@ -273,7 +277,7 @@ int logp_grad_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_
     p.wide_ids = id_bytes == 8;
     p.ignore = ignore_id;
     p.scale = scale;
-    p.c = float(double(scale) * 1.4426950408889634074);
+    p.c = class_c(scale);
     p.lse = d_lse;
     p.g = d_dlogp;
     p.dx = d_dlogits;
@@ -449,7 +453,7 @@ int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
     d.wide_ids = id_bytes == 8;
     d.ignore = opt->ignore_id;
     d.scale = opt->scale;
-    d.c = float(double(opt->scale) * 1.4426950408889634074);
+    d.c = class_c(opt->scale);
     d.stat = reinterpret_cast<const float2*>(scratch.data + rows);
     d.g = q.coef;
     d.dx = d_dlogits;

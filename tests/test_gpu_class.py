@@ -2,11 +2,11 @@
 and from differences.
 
 Tolerances, with u = 2^-24 (fp32 rounding), R the largest distance of a row's scaled logits from their maximum, derived from the operations:
-  a term of a row    2^a with a = fma(x, c, -m): a is off by u |a| from its rounding and by as much from that of c, |a| <= R / ln 2; the power
-                     itself is good to 2^-22: (2R + 4) u relative
+  a term of a row    2^a with a = (x - top) * c: the difference, c and the product are rounded, each is u |a| in a, |a| <= R / ln 2; the power
+                     itself is good to 2^-22: (3R + 4) u relative
   a row's sum        a thread's chain of at most 32 + V / (32 * 64) terms, then trees and the other warps: at most 100 additions here:
-                     (2R + 104) u relative; lse and lp, the rest of which is fp64, are off by that and by R u from c: (3R + 110) u =: L
-  p                  its term and the sum: (4R + 115) u relative =: 4R + 115 <= P / u
+                     (3R + 104) u relative; lse and lp, the rest of which is fp64 but for a logarithm good to 2u, are off by that: (3R + 110) u =: L
+  p                  its term and the sum: (6R + 115) u relative =: P
   a row's factor g   policy: |r A| L + kl_coef e^(ref-lp) L;  preference: |dloss/dh| <= beta, curvature <= 1/4, both over a sum of n rows
   a gradient         (p + [target]) times the error of g, |g| (P p + [target] L), three roundings of products, and half a step of its type
 """
@@ -51,7 +51,7 @@ def spread_of(x, scale):
 
 def errs(x, scale):
     R = spread_of(x, scale)
-    return (3 * R + 110) * U, (4 * R + 115) * U
+    return (3 * R + 110) * U, (6 * R + 115) * U
 
 
 def close(got, want, bound):
@@ -146,12 +146,62 @@ def test_logp_far_from_zero_and_masked(ctx):
         want = log_softmax(xx.double(), 1.0).gather(1, y[:, None])[:, 0]
         got, lse = ctx.logp(xx, y)
         assert bool(got[2:5].isnan().all()) and bool(want[2:5].isnan().all())
-        assert -110 * U <= float(got[1]) <= 0.0     # R = 0: the one term is 2 to the rounding of m, not 1; never above 0
+        assert float(got[1]) == 0.0                 # the one term is 1
         close(got[[0, 1]], want[[0, 1]], 1e-5)
         close(got[5:], want[5:], 4 * U * want[5:].abs())
         d = ctx.logp_grad(xx, y, lse, torch.ones(6, device="cuda"))
         assert bool((d[0, ::2] == 0).all()) and float(d[1].abs().max()) <= 115 * U + HALF[dt] and bool(d[3].isnan().all())
         assert float(d[5, 0]) == 1.0
+
+
+@pytest.mark.parametrize("V", [40, 3000, 50021])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_rows_far_out(ctx, dt, V):
+    """Rows at the type's lowest or highest value, at the values that programs mask with, and far from zero with differences of their own."""
+    lowest = torch.finfo(DT[dt]).min
+    rows = [torch.full((V,), v) for v in (lowest, -lowest, -1e9, -1e30, -1e4, 0.0, -65504.0)]
+    rows += [torch.full((V,), lowest), torch.full((V,), -1e9), torch.full((V,), lowest)]
+    rows[7][3] = 2.0                                # all but one masked
+    rows[8][5:9] = torch.tensor([1.0, 2.0, 3.0, 4.0])
+    rows[9][::2] = -1e30                            # one mask above another
+    x = torch.stack(rows).to(DT[dt]).cuda()
+    T = len(rows)
+    y = torch.full((T,), 7, device="cuda")
+    y[7], y[9] = 3, 4
+    want = log_softmax(x.double(), 1.0).gather(1, y[:, None])[:, 0]
+    lp, lse = ctx.logp(x, y)
+    close(lp, want, 110 * U + 2 * U * want.abs())
+    close(lse, torch.logsumexp(x.double(), 1), 110 * U + 2 * U * torch.logsumexp(x.double(), 1).abs())
+    adv, one = torch.linspace(-1, 1, T, device="cuda"), torch.ones(T, device="cuda")
+    stats, _, d = ctx.policy_loss(x, y, adv)
+    ref = policy_reference(x, y, adv, None, None, one, 1.0, 0.2, 0.2, 0.0, None, 1.0)
+    p = torch.softmax(x.double(), 1)
+    close(d, ref[2], adv.double().abs()[:, None] / T * (p + onehot(y, V)) * 230 * U + 1.01 * HALF[dt] * ref[2].abs() + 1e-38)
+    ids = torch.stack([torch.arange(3, 9, device="cuda")] * T)
+    t = rnd(T, 6)
+    loss, kl, dd = ctx.distill_loss(x, ids, t)
+    want = distill_reference(x, ids, t, None, one, 1.0, None, 1.0)
+    close(kl, want[1], 300 * U + 8 * U * (want[1].abs() + want[5]))
+    q = torch.zeros(T, V, dtype=torch.float64, device="cuda").scatter_add_(1, ids, want[3])
+    close(dd, want[2], (p * 230 * U + q * 14 * U) / T + 1.01 * HALF[dt] * want[2].abs() + 1e-38)
+
+
+def test_policy_loss_of_unlikely_rows(ctx):
+    """Ratios beyond fp32, targets without probability, an advantage of zero."""
+    x = rnd(6, 50, seed=1)
+    x[0, 3] = x[1, 3] = -math.inf
+    y = torch.full((6,), 3, device="cuda")
+    adv = torch.tensor([1.0, -1.0, 0.0, 1.0, 0.0, -2.0], device="cuda")
+    lp = ctx.logp(x, y)[0]
+    old = torch.stack([torch.tensor(-3.0), torch.tensor(-3.0), torch.tensor(-200.0), torch.tensor(-200.0), torch.tensor(200.0), torch.tensor(150.0)]).cuda()
+    stats, got, d = ctx.policy_loss(x, y, adv, old)
+    assert torch.equal(got, lp) and float(got[0]) == -math.inf
+    assert bool(torch.isfinite(d).all()) and bool(torch.isfinite(stats).all())
+    assert bool((d[2] == 0).all()) and bool((d[3] == 0).all()) and bool((d[4] == 0).all())      # no advantage; held by the clip; no advantage
+    # -min(r A, r' A) with r' = r held in [0.8, 1.2]: row 3 (r huge) -1.2; rows 1 and 5 (r = 0, A = -1 and -2: r A = 0 > r' A) 0.8 and 1.6; these
+    # three are held; row 0 (r = 0, A = 1) and the rows without an advantage 0
+    assert abs(float(stats[1]) - (-1.2 + 0.8 + 1.6) / 6) < 1e-6
+    assert abs(float(stats[3]) - 3 / 6) < 1e-6
 
 
 def test_targets_outside_the_classes(ctx):
