@@ -11,5 +11,6 @@ __all__ = ["datagen", "api", *_FROM_API]
 def __getattr__(name):
     if name in _FROM_API:
         from . import api
-        return getattr(api, name)
+        globals()[name] = value = getattr(api, name)    # (found without this function the next time)
+        return value
     raise AttributeError(name)

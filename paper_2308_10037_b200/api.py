@@ -541,9 +541,15 @@ class Context:
 
     def _per_row(self, t, T, name):
         """Address of an optional float32 [T]."""
-        if t is not None and (not isinstance(t, torch.Tensor) or t.shape != (T,)):
-            raise ValueError(f"{name}: expected a float32 CUDA tensor of shape {(T,)}")
-        return self._p(t, torch.float32, name)
+        if t is None:
+            return None
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype is torch.float32 and t.is_contiguous()):
+            raise TypeError(f"{name}: expected a contiguous CUDA tensor of dtype torch.float32")
+        if t.shape != (T,):
+            raise ValueError(f"{name}: shape {tuple(t.shape)}, the call needs {(T,)}")
+        if t.device.index != self.device:
+            raise ValueError(f"{name}: lives on cuda:{t.device.index}, the call runs on cuda:{self.device}")
+        return t.data_ptr()
 
     def _dlogits(self, logits, out):
         """(gradient, its address, its leading dimension): ``out``, or a new one whose rows start as far from a 16-byte boundary as those
@@ -553,8 +559,10 @@ class Context:
             per = 16 // logits.element_size()
             pitch = V + (logits.stride(0) - V) % per if T > 1 else V
             first = logits.data_ptr() % 16 // logits.element_size()
-            out = torch.empty_strided((T * pitch + first,), (1,), dtype=logits.dtype, device=logits.device)[first:].as_strided((T, V), (pitch, 1)) \
-                if pitch != V or first else _new(T, V, logits.dtype, logits.device)
+            if pitch == V and first == 0:
+                out = _new(T, V, logits.dtype, logits.device)
+            else:
+                out = torch.empty_strided((T * pitch + first,), (1,), dtype=logits.dtype, device=logits.device)[first:].as_strided((T, V), (pitch, 1))
             return out, out.data_ptr(), pitch
         return (out, *self._rows(out, (logits.dtype,), "out", (T, V))[0:4:3])
 
@@ -609,11 +617,12 @@ class Context:
         opt = self._loss_opt(LrPolicyOpt, int(ignore_id), float(scale), float(clip_low), float(clip_high), float(kl_coef), self._norm(norm), float(factor))
         if advantages is None:
             raise ValueError("advantages: expected a float32 CUDA tensor")
-        rows = [self._per_row(t, T, n) for t, n in ((advantages, "advantages"), (old_logp, "old_logp"), (ref_logp, "ref_logp"), (weights, "weights"))]
+        pa, pq = self._per_row(advantages, T, "advantages"), self._per_row(old_logp, T, "old_logp")
+        pr, pw = self._per_row(ref_logp, T, "ref_logp"), self._per_row(weights, T, "weights")
         buf = torch.empty_strided((4 + T,), (1,), dtype=torch.float32, device=logits.device)
         out, po, ldo = self._dlogits(logits, out) if grad else (None, None, V)
         at = buf.data_ptr()
-        rc = getattr(lib(), "lr_policy_loss" + sfx)(self._h, pl, ld, T, V, pt, ib, ctypes.byref(opt), *rows, at, at + 16, po, ldo, self._stream())
+        rc = getattr(lib(), "lr_policy_loss" + sfx)(self._h, pl, ld, T, V, pt, ib, ctypes.byref(opt), pa, pq, pr, pw, at, at + 16, po, ldo, self._stream())
         if rc:
             self._check(rc, "lr_policy_loss" + sfx)
         return buf[:4], buf[4:], out
