@@ -62,7 +62,8 @@ struct ClassParams {
     double norm;                 // 0: the sum of the weights of the rows that count
     double factor;
     // rows and their CTAs
-    const int* order;            // the rows that count, then the others (k_class_prep); NULL: all rows, looked at one by one
+    int listed;                  // long rows: every CTA lists its rows for itself (see class_list)
+    const int* order;            // the rows that count, then the others (k_class_prep).  Neither: all rows, looked at one by one
     const struct ClassPrep* prep;
     int cluster;                 // long rows: CTAs per row (a power of two), stages in a ring
     int depth;
@@ -669,6 +670,15 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 // (4096 x 128000, 64 classes: 395 us, four teams with eight number warps 419).
 constexpr int kMaxCluster = 8;
 
+// Up to this many rows the CTAs look all of them over themselves, which takes as long as a launch of k_class_prep less (T = 300: 2 us).
+constexpr int kListedRows = 4096;
+constexpr int kListedMine = 256;                    // ... if no cluster has more of them
+struct ClassList {
+    double norm[32], total;
+    int count[32], all;
+    unsigned short live[kListedMine], dead[kListedMine];
+};
+
 template <int MODE>
 struct Ring {
     static constexpr int kTeams = MODE == kClassPolicy ? 4 : 2;
@@ -693,9 +703,67 @@ struct Ring {
         float2 cta_sum[2 * kRows][kMaxCluster];
         float2 warp_sum[kRows][kTeamWarps];         // largest logit, sum
         float4 row[kRows];                          // factor, top, 1 where the row counts
+        ClassList list;
         int abort_word;
     };
 };
+
+// A CTA lists its rows (see kListedRows): its cluster's are every Q-th of those that count, and every Q-th of the others.
+template <int MODE>
+__device__ __forceinline__ void class_list(const ClassParams& p, ClassList& list, int q, int Q, bool write) {
+    constexpr int kWarps = Ring<MODE>::kThreads / 32, kTurns = (kListedRows + 32 * kWarps - 1) / (32 * kWarps);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, turns = (int(p.T) + 32 * kWarps - 1) / (32 * kWarps);
+    long long from = 0, to = p.T;
+    if (MODE == kClassLogp && p.offsets) {
+        from = load_any_id(p.offsets, p.wide_offsets, 0);
+        to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+    }
+    unsigned int mask[kTurns];
+    double norm = 0.0;
+    int count = 0;
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+        const int t = (warp * turns + j) * 32 + lane;
+        bool live = false;
+        if (j < turns && t < p.T) {
+            long long target;
+            float w;
+            live = class_counts(p, t, MODE, &target, &w);
+            if (MODE == kClassLogp) live = live && t >= from && t < to;
+            if (live) norm += w;
+        }
+        mask[j] = __ballot_sync(0xffffffffu, live);
+        count += __popc(mask[j]);
+    }
+    norm = warp_sum64(norm);
+    if (lane == 0) {
+        list.count[warp] = count;
+        list.norm[warp] = norm;
+    }
+    __syncthreads();
+    const int of_lane = lane < kWarps ? list.count[lane] : 0;
+    int at = __reduce_add_sync(0xffffffffu, lane < warp ? of_lane : 0);
+#pragma unroll
+    for (int j = 0; j < kTurns; ++j) {
+        const int t = (warp * turns + j) * 32 + lane, ahead = at + __popc(mask[j] & ((1u << lane) - 1));
+        at += __popc(mask[j]);
+        if (j >= turns || t >= p.T) continue;
+        const bool live = mask[j] >> lane & 1;
+        const int i = live ? ahead : t - ahead;
+        if (i % Q != q) continue;
+        (live ? list.live : list.dead)[i / Q] = static_cast<unsigned short>(t);
+        if (!live && write) class_dead_row<MODE>(p, t);
+    }
+    if (warp == 0) {
+        const int all = __reduce_add_sync(0xffffffffu, of_lane);
+        norm = warp_sum64(lane < kWarps ? list.norm[lane] : 0.0);
+        if (lane == 0) {
+            list.all = all;
+            list.total = norm;
+        }
+    }
+    __syncthreads();
+}
 
 __device__ __forceinline__ uint64_t l2_policy_evict_normal() {
     uint64_t pol;
@@ -746,11 +814,14 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
     __syncthreads();
     if (C > 1) cluster_barrier();                   // who writes into another CTA's shared memory has to find it started
     grid_dependency_wait();
-    const int live = p.order ? p.prep->live : int(p.T);
+    const bool known = p.order || p.listed;         // which rows count
+    if (p.listed) class_list<MODE>(p, sh.list, q, Q, rank == 0);
+    const int live = p.listed ? sh.list.all : p.order ? p.prep->live : int(p.T);
     const int mine = live > q ? (live - q + Q - 1) / Q : 0;
     auto row_of = [&](int k) -> int {
         const long long at = q + static_cast<long long>(k) * Q;
-        if (k >= mine || !p.order) return static_cast<int>(at);
+        if (k >= mine || !known) return static_cast<int>(at);
+        if (p.listed) return sh.list.live[k];
         int t;                                      // (volatile: fetched here, well before it is needed)
         asm volatile("ld.global.b32 %0, [%1];" : "=r"(t) : "l"(p.order + at));
         return t;
@@ -907,11 +978,11 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
         double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
         if (MODE != kClassLogp) {
             double n = p.norm;
-            if (n == 0.0) n = p.order ? p.prep->norm : class_norm_warp<MODE>(p);
+            if (n == 0.0) n = p.listed ? sh.list.total : p.order ? p.prep->norm : class_norm_warp<MODE>(p);
             inv = n == 0.0 ? 0.0 : 1.0 / n;
         }
         long long from = 0, to = p.T;
-        if (MODE == kClassLogp && !p.order && p.offsets) {
+        if (MODE == kClassLogp && !known && p.offsets) {
             from = load_any_id(p.offsets, p.wide_offsets, 0);
             to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
         }
@@ -922,12 +993,12 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
         };
         // this cluster's rows that do not count, in pieces of kZeroGroups groups; row k's turn is piece pieces * k / mine and on
         constexpr int kZeroGroups = 512;
-        const int dead = p.order ? max(0, (int(p.T) - live - q + Q - 1) / Q) : 0, per_row = (p.V / N + kZeroGroups * C) / (kZeroGroups * C);
+        const int dead = known ? max(0, (int(p.T) - live - q + Q - 1) / Q) : 0, per_row = (p.V / N + kZeroGroups * C) / (kZeroGroups * C);
         auto zero_pieces = [&](long long first, long long last) {
             const uint64_t zero[G::P] = {};
             for (; first < last; ++first) {
                 const int i = static_cast<int>(first / per_row), piece = static_cast<int>(first - static_cast<long long>(i) * per_row);
-                const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, __ldg(p.order + live + q + static_cast<long long>(i) * Q), p.V);
+                const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, p.listed ? sh.list.dead[i] : __ldg(p.order + live + q + static_cast<long long>(i) * Q), p.V);
                 const int start = (piece * C + rank) * kZeroGroups, end = min(start + kZeroGroups, row.groups);
                 for (int g = start + lane; g < end; g += 32) row.store(g, zero);
                 if (piece == 0 && rank == 0 && lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);

@@ -133,9 +133,11 @@ int launch_ring(lr_ctx* ctx, ClassParams& p, const RowScratch& at, const Scratch
     LR_CK(ctx, resident_clusters<Tag>(reinterpret_cast<const void*>(kern), cfg, p.cluster, &clusters));
     clusters = int(std::min<int64_t>(p.T, std::max<int64_t>(1, int64_t(clusters) * plan_sms(ctx) / ctx->sm_count)));
     cfg.gridDim = dim3(unsigned(clusters * p.cluster));
-    // with a row for every cluster, or where all rows count, the rows are looked at on the way
-    const bool prep = p.T > clusters && (MODE != kClassDistill || p.weights);
-    if (prep) {
+    // With a row for every cluster, or where all rows count, the rows are looked at on the way; a few thousand are looked over by every CTA
+    // (policy loss, 1000 x 32000 bfloat16: PREPFIG us, 40 with a launch for it), more by a kernel before this one.
+    const bool pick = p.T > clusters && (MODE != kClassDistill || p.weights);
+    p.listed = pick && p.T <= kListedRows && p.T <= int64_t(clusters) * kListedMine;
+    if (pick && !p.listed) {
         ClassPrep* out = reinterpret_cast<ClassPrep*>(scratch.data + at.sums);
         int* order = reinterpret_cast<int*>(scratch.data + at.sums + at.prep);
         const int r = launched(ctx, [&] { k_class_prep<MODE><<<1, kPrepThreads, 0, st>>>(p, order, out); });
