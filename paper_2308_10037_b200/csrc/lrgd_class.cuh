@@ -179,9 +179,9 @@ struct ClassRow {
     // element e of those outside the groups
     __device__ __forceinline__ int edge(int e) const { return e < head ? e : e + groups * ClassGroup<E>::N; }
     __device__ __forceinline__ uint4 load(int g) const { return *reinterpret_cast<const uint4*>(x + head + g * ClassGroup<E>::N); }
-    __device__ __forceinline__ void store(int g, const uint64_t (&v)[ClassGroup<E>::P]) const {
+    __device__ __forceinline__ void store(int g, const uint64_t (&v)[ClassGroup<E>::P]) const { store_at(dx + head + g * ClassGroup<E>::N, v); }
+    __device__ __forceinline__ void store_at(E* at, const uint64_t (&v)[ClassGroup<E>::P]) const {
         constexpr int N = ClassGroup<E>::N;
-        E* at = dx + head + g * N;
         if (wide_store) {
             *reinterpret_cast<uint4*>(at) = ClassGroup<E>::narrow(v);
         } else {
@@ -936,17 +936,18 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                 uint4 raw[J];
                 read_stage(from, raw);
                 give_back(from);
+                E* out = row.dx + row.head + (first + lane) * N;
                 auto group = [&](int j) {
                     uint64_t v[G::P];
 #pragma unroll
                     for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(class_powers(G::pair(raw[j], e), top2, c2), factor2);
-                    row.store(first + lane + 32 * j, v);
+                    row.store_at(out + 32 * N * j, v);
                 };
                 if (!counts) {
                     const uint64_t zero[G::P] = {};
 #pragma unroll
                     for (int j = 0; j < J; ++j)
-                        if (32 * j + lane < left) row.store(first + lane + 32 * j, zero);
+                        if (32 * j + lane < left) row.store_at(out + 32 * N * j, zero);
                 } else if (left >= kWarpGroups) {
 #pragma unroll
                     for (int j = 0; j < J; ++j) group(j);
@@ -1227,29 +1228,38 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
     constexpr int N = G::N, U = kClassGradGroups;
     const int tid = threadIdx.x, threads = blockDim.x;
     grid_dependency_wait();
-    const long long items = p.T * p.slices;
     struct Numbers {             // of a row
         long long target;
         float g;
         float2 stat;
     };
-    auto row_of = [&](long long item) { return (p.backwards ? items - 1 - item : item) / p.slices; };
-    auto fetch = [&](long long item) {
+    // slice `slice` of row t, and what comes gridDim.x pieces later
+    auto row_of = [&](long long t) { return p.backwards ? p.T - 1 - t : t; };
+    auto fetch = [&](long long t) {
         Numbers n{};
-        if (item < items) {
-            const long long t = row_of(item);
+        if (t < p.T) {
+            t = row_of(t);
             n.target = load_any_id(p.ids, p.wide_ids, t);
             n.g = p.g[t];
             n.stat = p.stat ? p.stat[t] : make_float2(p.lse[t], 0.0f);
         }
         return n;
     };
-    Numbers next = fetch(blockIdx.x);
-    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+    const int rows = gridDim.x / p.slices, rest = gridDim.x % p.slices;
+    long long next_t = blockIdx.x / p.slices;
+    int next_slice = blockIdx.x % p.slices;
+    Numbers next = fetch(next_t);
+    while (next_t < p.T) {
         const Numbers now = next;
-        next = fetch(item + gridDim.x);
-        const long long t = row_of(item);
-        const int slice = static_cast<int>((p.backwards ? items - 1 - item : item) - t * p.slices);
+        const long long t = row_of(next_t);
+        const int slice = next_slice;
+        next_t += rows;
+        next_slice += rest;
+        if (next_slice >= p.slices) {
+            next_slice -= p.slices;
+            ++next_t;
+        }
+        next = fetch(next_t);
         const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
         const float gt = now.g * p.scale;
         bool live = now.target != p.ignore && gt != 0.0f;
@@ -1267,10 +1277,12 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
             if (edges) store_from_float(row.dx + row.edge(tid), 0.0f);
             continue;
         }
+        const E* in = row.x + row.head + first * N;
+        E* out = row.dx + row.head + first * N;
         uint4 raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (first + u * threads < row.groups) raw[u] = row.load(first + u * threads);
+            if (first + u * threads < row.groups) raw[u] = *reinterpret_cast<const uint4*>(in + u * threads * N);
         float base, k;
         if (p.stat) {
             base = now.stat.x;
@@ -1296,7 +1308,7 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
                     v[j] = f32x2_add(v[j], f32x2_pack(at == 0 ? gt : 0.0f, at == 1 ? gt : 0.0f));
                 }
             }
-            row.store(g, v);
+            row.store_at(out + u * threads * N, v);
         }
         if (edges) {
             const int at = row.edge(tid);
