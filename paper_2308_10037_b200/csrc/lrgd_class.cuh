@@ -656,7 +656,7 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 // A CTA per row, or a cluster of C.  Its warps have different work, and hand rows to each other through mbarriers:
 //   two or four teams of warps take turns at the rows: first pass (running maximum and sum), then, when the row's numbers are known, second pass
 //     (the gradient).  While one team waits, or reduces, the others work;
-//   a warp per team copies its rows' 16-byte groups, in stages of 8 to 32 KB, into the team's ring of shared memory, as far ahead as the ring
+//   a warp per team copies its rows' 16-byte groups, in stages of 8, 18 or 32 KB, into the team's ring of shared memory, as far ahead as the ring
 //     allows (a ring of its own, because who skips another team's stages cannot tell an mbarrier's phases apart);
 //   kNumberWarps warps take turns at the rows: they fetch what a row has beside its logits, join the sums of the team's warps (and of the
 //     cluster's CTAs, by 8-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
@@ -664,10 +664,11 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 //     of the memory system that the others wait in).
 // The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that a row fits.  Of the longest
 // rows, stages that the ring could not hold are copied once more (`dropped`).  Stages are given back in the order of the copies.
-// Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 292 us
-// instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 646 us, two teams
-// 690).  Distillation: the teacher's classes take the room of a stage and every row more of the number warps' time, so there are two teams
-// (4096 x 128000, 64 classes: 395 us, four teams with eight number warps 419).
+// Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 290 us
+// instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 650 us; two teams
+// 690, three 715, five of three warps 839).  Distillation: the teacher's classes take the room of a stage, and every row more of the number
+// warps' time, so there are two teams (4096 x 128000, 64 classes: nine warps a team 375 us, eight 392; three teams 495, four teams with eight
+// number warps 419).
 constexpr int kMaxCluster = 8;
 
 // Up to this many rows the CTAs look all of them over themselves, which takes as long as a launch of k_class_prep less (T = 300: 2 us).
@@ -682,8 +683,8 @@ struct ClassList {
 template <int MODE>
 struct Ring {
     static constexpr int kTeams = MODE == kClassPolicy ? 4 : 2;
-    static constexpr int kTeamWarps = 16 / kTeams;
-    static constexpr int kPassWarps = 16;
+    static constexpr int kTeamWarps = MODE == kClassPolicy ? 4 : MODE == kClassDistill ? 9 : 8;
+    static constexpr int kPassWarps = kTeams * kTeamWarps;
     static constexpr int kNumberWarps = 4;          // (eight are no faster: policy 647 us, distillation 402)
     static constexpr int kThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
     static constexpr int kLaneGroups = MODE == kClassLogp ? 8 : 4;              // of a stage

@@ -1,12 +1,12 @@
 """The hand-over of rows inside ``k_class_ring`` (csrc/lrgd_class.cuh), replayed on the CPU under random schedules: the copying warps, the
-two teams, and the warps that work out a row's numbers, in clusters of CTAs.  An mbarrier's wait knows a phase only by its parity, so every
+teams, and the warps that work out a row's numbers, in clusters of CTAs.  An mbarrier's wait knows a phase only by its parity, so every
 wait that returns has to return for the phase that is meant, no place may be overwritten while somebody still reads it, and all have to
 come to their end."""
 import random
 
 import pytest
 
-TEAMS, TEAM_WARPS, NUMBERS, ROWS = 2, 3, 4, 4       # (three warps a team instead of eight: fewer steps, the same protocol)
+TEAM_WARPS, NUMBERS, ROWS = 3, 4, 4                 # (three warps a team instead of up to nine: fewer steps, the same protocol)
 
 
 class Barrier:
@@ -35,19 +35,19 @@ def wait(bar, parity, phase):
 
 
 class Cta:
-    def __init__(self, depth):
-        self.full = [[Barrier(1) for _ in range(depth)] for _ in range(TEAMS)]
-        self.free = [[Barrier(TEAM_WARPS) for _ in range(depth)] for _ in range(TEAMS)]
-        self.ring = [[None] * depth for _ in range(TEAMS)]
+    def __init__(self, teams, depth):
+        self.full = [[Barrier(1) for _ in range(depth)] for _ in range(teams)]
+        self.free = [[Barrier(TEAM_WARPS) for _ in range(depth)] for _ in range(teams)]
+        self.ring = [[None] * depth for _ in range(teams)]
         self.summed, self.ready, self.written = ([Barrier(n) for _ in range(ROWS)] for n in (TEAM_WARPS, 1, TEAM_WARPS))
         self.joined = [Barrier(1) for _ in range(2 * ROWS)]
         self.sums, self.row, self.cta_sum = [{} for _ in range(ROWS)], [None] * ROWS, [{} for _ in range(2 * ROWS)]
         self.inflight, self.done = [], {}
 
 
-def copier(c, team, mine, stages, depth, grad):
+def copier(c, teams, team, mine, stages, depth, grad):
     copies = 0
-    for k in range(team, mine, TEAMS):
+    for k in range(team, mine, teams):
         n = stages(k)
         for i in [*range(n), *range(max(0, n - depth) if grad else 0)]:
             slot, lap = copies % depth, copies // depth
@@ -59,9 +59,9 @@ def copier(c, team, mine, stages, depth, grad):
             yield
 
 
-def passes(c, team, warp, mine, stages, depth, grad):
+def passes(c, teams, team, warp, mine, stages, depth, grad):
     used = 0
-    for k in range(team, mine, TEAMS):
+    for k in range(team, mine, teams):
         n, at, lap = stages(k), k % ROWS, k // ROWS
         dropped = max(0, n - depth) if grad else n
         for i in range(n):
@@ -123,19 +123,20 @@ def numbers(ctas, rank, h, mine, grad):
         c.done[k] = c.done.get(k, 0) + 1
 
 
+@pytest.mark.parametrize("teams", [2, 4])
 @pytest.mark.parametrize("grad", [False, True])
 @pytest.mark.parametrize("C,depth,stages", [(1, 3, 1), (1, 3, 3), (1, 4, 2), (1, 3, 5), (1, 2, 7), (2, 3, 2), (4, 3, 1), (2, 3, 4), (4, 5, 3), (1, 3, 0),
                                             (2, 3, "ragged"), (1, 4, "ragged")])
-def test_rows_are_handed_over(grad, C, depth, stages):
-    for seed in range(8):
+def test_rows_are_handed_over(teams, grad, C, depth, stages):
+    for seed in range(6):
         rng = random.Random(seed)
         mine = rng.choice([1, 2, 3, 9, 26])
-        ctas = [Cta(depth) for _ in range(C)]
+        ctas = [Cta(teams, depth) for _ in range(C)]
         agents = []
         for r, c in enumerate(ctas):
             count = (lambda k, r=r: (k * 7 + r) % 6) if stages == "ragged" else (lambda k: stages)
-            agents += [copier(c, t, mine, count, depth, grad) for t in range(TEAMS)]
-            agents += [passes(c, t, w, mine, count, depth, grad) for t in range(TEAMS) for w in range(TEAM_WARPS)]
+            agents += [copier(c, teams, t, mine, count, depth, grad) for t in range(teams)]
+            agents += [passes(c, teams, t, w, mine, count, depth, grad) for t in range(teams) for w in range(TEAM_WARPS)]
             agents += [numbers(ctas, r, h, mine, grad) for h in range(NUMBERS)]
         weight = [rng.choice([1, 1, 1, 10, 50]) for _ in agents]      # some are much faster than others
         alive, waiting = list(range(len(agents))), set()
