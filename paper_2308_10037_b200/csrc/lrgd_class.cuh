@@ -836,8 +836,8 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             const int team = warp - kPassWarps;
             uint64_t *full = sh.full[team], *free = sh.free[team];
             unsigned char* ring = class_smem + team * depth * kStageBytes;
-            // (rows that a later pass reads again may stay in L2)
-            const uint64_t once = MODE == kClassLogp && p.stat ? l2_policy_evict_normal() : l2_policy_evict_first();
+            // what is read again, by a later pass or because the ring cannot hold it, may stay in L2
+            const uint64_t again_policy = l2_policy_evict_normal(), once = MODE == kClassLogp && p.stat ? again_policy : l2_policy_evict_first();
             int slot = 0, parity = 0, copies = 0;
             bool ok = true;
             int t = row_of(team);
@@ -854,7 +854,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                     }
                     fence_proxy_async_smem();
                     mbar_arrive_expect_tx(full + slot, bytes);
-                    bulk_copy_g2s(ring + slot * kStageBytes, row.x + row.head + static_cast<long long>(first) * N, bytes, full + slot, once);
+                    bulk_copy_g2s(ring + slot * kStageBytes, row.x + row.head + static_cast<long long>(first) * N, bytes, full + slot, i < again ? again_policy : once);
                     if (copies < depth) ++copies;
                     if (++slot == depth) {
                         slot = 0;
