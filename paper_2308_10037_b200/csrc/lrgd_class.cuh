@@ -110,6 +110,10 @@ struct ClassGroup {
     static constexpr int N = 16 / int(sizeof(E));
     static constexpr int P = N / 2;
     static __device__ __forceinline__ uint32_t word(const uint4& w, int i) { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
+    static __device__ __forceinline__ uint4 nothing() {         // all -inf
+        constexpr uint32_t w = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;
+        return make_uint4(w, w, w, w);
+    }
     // elements 2 i and 2 i + 1
     static __device__ __forceinline__ uint64_t pair(const uint4& w, int i) {
         if constexpr (sizeof(E) == 4) return f32x2_pack(__uint_as_float(word(w, 2 * i)), __uint_as_float(word(w, 2 * i + 1)));
@@ -437,10 +441,9 @@ struct ClassTopSum {
     float near;                  // the largest of their x
     bool twice;                  // some class is named twice
 };
-// Reads a row's classes; the bitmap is empty before and after.  Eight entries of a lane are on their way together.
-template <class E>
+// Reads a row's classes; the bitmap is empty before and after.  U entries of a lane are on their way together.
+template <int U, class E>
 __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long long t, const E* row, const ClassTop& top) {
-    constexpr int U = 8;
     const int lane = threadIdx.x & 31;
     ClassTopSum r{0.0f, 0.0f, 0.0f, -INFINITY, false};
     float largest = -INFINITY;
@@ -518,10 +521,10 @@ struct ClassInputs {
     float w, xy, adv, old_logp, ref_logp;
     ClassTopSum top;
 };
-template <int MODE, class E>
+template <int MODE, int U = 8, class E>
 __device__ __forceinline__ void class_inputs(const ClassParams& p, long long t, const E* row, const ClassTop& top, ClassInputs& in) {
     if (MODE == kClassDistill) {
-        in.top = class_top_read(p, t, row, top);
+        in.top = class_top_read<U>(p, t, row, top);
         return;
     }
     in.xy = load_local(row + in.target);
@@ -531,10 +534,21 @@ __device__ __forceinline__ void class_inputs(const ClassParams& p, long long t, 
         in.ref_logp = p.ref_logp ? __ldg(p.ref_logp + t) : 0.0f;
     }
 }
+// exp(d) - 1 - d.  Near 0, where that is the difference of nearly equal numbers, by its series: d^2/2 (1 + d/3 (1 + d/4 (...))), cut off where a
+// term of |d| = 1/4 is below 2e-8 of the sum.
+__device__ __forceinline__ float class_kl(float d) {
+    if (fabsf(d) < 0.25f) {
+        float r = 1.0f;
+#pragma unroll
+        for (int i = 8; i >= 3; --i) r = fmaf(d * (1.0f / i), r, 1.0f);
+        return 0.5f * d * d * r;
+    }
+    return d == INFINITY ? d : expm1f(d) - d;
+}
 // ... and what of it is written down afterwards
 struct ClassTerms {
     double lp, lse;
-    float first, kl, clipped;    // the row's loss: its parts (distillation: kl alone)
+    float first, kl, clipped;    // the row's loss: its parts (policy: the first and whether it is clipped; distillation: kl)
 };
 template <int MODE>
 __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, const ClassInputs& in, const ClassSum& sum, double inv, ClassTerms& terms) {
@@ -595,10 +609,7 @@ __device__ __forceinline__ void class_account(const ClassParams& p, long long t,
         }
     } else {
         sums[0] += static_cast<double>(in.w) * terms.first;
-        if (p.ref_logp) {                           // (a difference of nearly equal numbers where the policies are near each other: fp64)
-            const double d = in.ref_logp - terms.lp;
-            sums[1] += in.w * (d == INFINITY ? d : expm1(d) - d);
-        }
+        if (p.ref_logp) sums[1] += static_cast<double>(in.w) * class_kl(static_cast<float>(in.ref_logp - terms.lp));
         sums[2] += terms.clipped != 0.0f ? in.w : 0.0f;
     }
 }
@@ -910,15 +921,13 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                 if (i < dropped) give_back(slot);
                 next_slot();
                 if (i + 1 == dropped) held = slot;
-                if (left >= kWarpGroups) {
-                    sum.add_groups<E, J>(raw, p.c);
-                } else if (left > 0) {
+                if (left <= 0) continue;
+                if (left < kWarpGroups) {
 #pragma unroll
-                    for (int j = 0; j < J; ++j) {
-                        const uint4 one[1] = {raw[j]};
-                        if (32 * j + lane < left) sum.add_groups<E, 1>(one, p.c);
-                    }
+                    for (int j = 0; j < J; ++j)
+                        if (32 * j + lane >= left) raw[j] = G::nothing();
                 }
+                sum.add_groups<E, J>(raw, p.c);
             }
             sum.over_warp(p.c);
             if (!GRAD && k >= kRows) wait(sh.ready + at, (k / kRows - 1) & 1);      // the sums of row k - kRows have been read
@@ -1074,12 +1083,17 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
 }
 
 // ---- short rows ----------------------------------------------------------------------------------------
-// A warp per row, the row in its registers between the passes: no barrier, no shared memory but for a teacher's classes.
+// A warp per row, the row in its registers between the passes: no barrier, no shared memory but for a teacher's classes.  Up to four groups a
+// lane the next row's logits are on their way meanwhile, and always its target.  Bound by the chain of a row's numbers, a few hundred
+// instructions of a warp: SHORTFIG
 constexpr int kShortWarps = 8;
+__host__ __device__ constexpr int short_ctas(int mode, int J) { return J <= 2 && mode != kClassDistill ? 4 : J <= 8 ? 3 : 2; }       // per SM, in registers
 
 template <class E, int MODE, bool GRAD, int J>
-__global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_constant__ ClassParams p) {
+__global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class_short(const __grid_constant__ ClassParams p) {
     using G = ClassGroup<E>;
+    constexpr bool kAhead = J <= 4 && MODE != kClassDistill;
+    constexpr int B = J < 4 ? J : 4;                // groups that are worked on together
     __shared__ double cta_part[kShortWarps][3];
     extern __shared__ __align__(128) unsigned char class_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -1089,78 +1103,98 @@ __global__ void __launch_bounds__(kShortWarps * 32) k_class_short(const __grid_c
         class_clear_marks(top);
     }
     grid_dependency_wait();
-    double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
-    const long long first = static_cast<long long>(blockIdx.x) * kShortWarps + warp;
-    for (long long t = first; t < p.T; t += static_cast<long long>(gridDim.x) * kShortWarps) {
-        const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
-        ClassInputs in{};
-        bool counts = class_counts(p, t, MODE, &in.target, &in.w);
-        if (MODE == kClassLogp && p.offsets)
-            counts = counts && t >= load_any_id(p.offsets, p.wide_offsets, 0) && t < load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+    struct Row {
+        ClassInputs in;
         uint4 raw[J];
-        float edge = 0.0f;
-        if (counts) {
+        float edge;
+        bool counts;
+    };
+    auto look = [&](long long t, Row& r) {          // its target and weight
+        r.counts = false;
+        if (t >= p.T) return;
+        r.counts = class_counts(p, t, MODE, &r.in.target, &r.in.w);
+        if (MODE == kClassLogp && p.offsets)
+            r.counts = r.counts && t >= load_any_id(p.offsets, p.wide_offsets, 0) && t < load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+    };
+    auto load = [&](long long t, Row& r) {          // its logits and what goes with them
+        if (!r.counts) return;
+        const ClassRow<E> row(p.x, p.ld, nullptr, 0, t, p.V);
 #pragma unroll
-            for (int j = 0; j < J; ++j)
-                if (32 * j + lane < row.groups) raw[j] = row.load(32 * j + lane);
-            if (lane < row.edges) edge = load_local(row.x + row.edge(lane));
+        for (int j = 0; j < J; ++j) r.raw[j] = 32 * j + lane < row.groups ? row.load(32 * j + lane) : G::nothing();
+        r.edge = lane < row.edges ? load_local(row.x + row.edge(lane)) : 0.0f;
+        if (MODE != kClassDistill) class_inputs<MODE>(p, t, row.x, top, r.in);
+    };
+    double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
+    const long long step = static_cast<long long>(gridDim.x) * kShortWarps;
+    long long t = static_cast<long long>(blockIdx.x) * kShortWarps + warp;
+    Row now{}, next{};
+    look(t, now);
+    load(t, now);
+    look(t + step, next);
+    if (MODE != kClassLogp) {                       // (beside the first row's loads)
+        double n = p.norm;
+        if (n == 0.0 && p.norm_parts > 0) {
+            for (int i = lane; i < p.norm_parts; i += 32) n += __ldcg(p.norm_part + i);
+            n = warp_sum64(n);
+        } else if (n == 0.0) {
+            n = class_norm_warp<MODE>(p);
         }
-        if (counts) class_inputs<MODE>(p, t, row.x, top, in);
-        if (MODE != kClassLogp && t == first) {     // (beside the first row's loads)
-            double n = p.norm;
-            if (n == 0.0 && p.norm_parts > 0) {
-                for (int i = lane; i < p.norm_parts; i += 32) n += __ldcg(p.norm_part + i);
-                n = warp_sum64(n);
-            } else if (n == 0.0) {
-                n = class_norm_warp<MODE>(p);
+        inv = n == 0.0 ? 0.0 : 1.0 / n;
+    }
+    for (; t < p.T; t += step) {
+        Row after{};
+        if (kAhead) {
+            load(t + step, next);
+            look(t + 2 * step, after);
+        }
+        const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
+        if (now.counts) {
+            if (MODE == kClassDistill) class_inputs<MODE, 2>(p, t, row.x, top, now.in);
+            ClassSum sum;
+#pragma unroll
+            for (int b = 0; b < J / B; ++b)
+                if (32 * B * b < row.groups) sum.add_groups<E, B>(reinterpret_cast<const uint4(&)[B]>(now.raw[B * b]), p.c);
+            if (lane < row.edges) sum.add(now.edge, p.c);
+            sum.over_warp(p.c);
+            sum.settle();
+            ClassTerms terms;
+            const ClassNumbers numbers = class_numbers<MODE>(p, now.in, sum, inv, terms);
+            class_account<MODE>(p, t, now.in, sum, terms, true, sums);
+            if (GRAD) {
+                const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-sum.top, -sum.top), factor2 = f32x2_pack(numbers.factor, numbers.factor);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    if (32 * j + lane < row.groups) {
+                        uint64_t v[G::P];
+#pragma unroll
+                        for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(class_powers(G::pair(now.raw[j], e), top2, c2), factor2);
+                        row.store(32 * j + lane, v);
+                    }
+                }
+                if (lane < row.edges) store_from_float(row.dx + row.edge(lane), class_power(now.edge, sum.top, p.c) * numbers.factor);
+                __syncwarp();                       // the targets' values replace what was just written
+                if (MODE == kClassPolicy) {
+                    if (lane == 0) store_from_float(row.dx + now.in.target, numbers.at);
+                } else {
+                    for (int j = lane; j < p.K; j += 32)
+                        if (top.id[j] >= 0) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, now.in.top.twice, sum.top, numbers));
+                    __syncwarp();
+                }
             }
-            inv = n == 0.0 ? 0.0 : 1.0 / n;
-        }
-        if (!counts) {
+        } else {
             if (GRAD) {
                 const uint64_t zero[G::P] = {};
                 for (int g = lane; g < row.groups; g += 32) row.store(g, zero);
                 if (lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
             }
             if (lane == 0) class_dead_row<MODE>(p, t);
-            continue;
         }
-        ClassSum sum;
-        if (row.groups >= 32 * J) {
-            sum.add_groups<E, J>(raw, p.c);
-        } else {
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const uint4 one[1] = {raw[j]};
-                if (32 * j + lane < row.groups) sum.add_groups<E, 1>(one, p.c);
-            }
+        if (!kAhead) {
+            load(t + step, next);
+            look(t + 2 * step, after);
         }
-        if (lane < row.edges) sum.add(edge, p.c);
-        sum.over_warp(p.c);
-        sum.settle();
-        ClassTerms terms;
-        const ClassNumbers now = class_numbers<MODE>(p, in, sum, inv, terms);
-        class_account<MODE>(p, t, in, sum, terms, true, sums);
-        if (!GRAD) continue;
-        const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-sum.top, -sum.top), factor2 = f32x2_pack(now.factor, now.factor);
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            if (32 * j + lane < row.groups) {
-                uint64_t v[G::P];
-#pragma unroll
-                for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(class_powers(G::pair(raw[j], e), top2, c2), factor2);
-                row.store(32 * j + lane, v);
-            }
-        }
-        if (lane < row.edges) store_from_float(row.dx + row.edge(lane), class_power(edge, sum.top, p.c) * now.factor);
-        __syncwarp();                               // the targets' values replace what was just written
-        if (MODE == kClassPolicy) {
-            if (lane == 0) store_from_float(row.dx + in.target, now.at);
-        } else {
-            for (int j = lane; j < p.K; j += 32)
-                if (top.id[j] >= 0) store_from_float(row.dx + top.id[j], class_top_value(p, top, j, in.top.twice, sum.top, now));
-            __syncwarp();
-        }
+        now = next;
+        next = after;
     }
     if (MODE == kClassLogp) return;
     if (lane == 0)

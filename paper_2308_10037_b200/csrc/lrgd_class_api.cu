@@ -168,9 +168,9 @@ int launch_short(lr_ctx* ctx, ClassParams& p, int lane_groups, const RowScratch&
         dependent = ctx->overlap;
     }
     const size_t smem = MODE == kClassDistill ? kShortWarps * class_top_bytes(p.K) : 0;
-    const dim3 grid(even_grid(ctx, p.T, kShortWarps, 8));
     auto go = [&](auto groups) -> int {
         constexpr int J = decltype(groups)::value;
+        const dim3 grid(grid_for(ctx, p.T, kShortWarps, short_ctas(MODE, J)));
         using Tag = ClassShortTag<E, MODE, GRAD, J>;
         const auto kern = k_class_short<E, MODE, GRAD, J>;
         LR_CK(ctx, ensure_dynamic_smem<Tag>(reinterpret_cast<const void*>(kern), int(smem)));
