@@ -551,18 +551,19 @@ int lr_ckpt8_grad_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float
  * Losses over a vocabulary's classes.  (No counterpart in the paper: its model has two classes.  These are the log-likelihood of a
  * many-class logistic model and what is learned through it from preferences -- the logistic loss again --, from rewards and from a
  * teacher.)  A row holds the logits of V classes; with l = scale * row, lse = log sum_v exp(l_v), p = exp(l - lse) and a target y its
- * log-probability is lp = l_y - lse.  scale (finite, > 0) is the inverse of a temperature.
+ * log-probability is lp = l_y - lse.  scale (> 0, below 2.3e38) is the inverse of a temperature.
  * Logits are fp32 or bfloat16 (the *_bf16 calls), row-major with a leading dimension, of any alignment to the element size; gradients have
  * their type, are formed in fp32 and rounded once.  They are fastest where rows of the gradient start at the same offset from a 16-byte
  * boundary as those of the logits.  d_dlogits may be the logits themselves (the same address and ld: the gradient replaces them); any other
  * overlap is LR_ERR_VALUE.  All T rows of a gradient are written.
- * Targets and classes are int32 or int64 (id_bytes 4, 8).  A row whose target is ignore_id does not count: its logits are not read (they may
- * hold anything), its log-probability and its gradient are 0.  A target outside [0, V) that is not ignore_id is treated the same way and sets
- * the device status word to LR_ERR_VALUE (lr_last_device_status).  The same goes for a row whose weight is 0.
- * A row of logits may hold -inf (a class that is masked); a NaN, a +inf or nothing but -inf makes what the row enters NaN.
+ * Targets and classes are int32 or int64 (id_bytes 4, 8).  A row whose target is ignore_id does not count: whatever its logits hold is
+ * left out, its log-probability and its gradient are 0.  A target outside [0, V) that is not ignore_id is treated the same way and sets
+ * the device status word to LR_ERR_VALUE (lr_last_device_status).  Nor does a row count whose weight is 0.
+ * A row of logits may hold -inf (a class that is masked) and be anywhere in the type's range (a row of the lowest value is uniform); a NaN, a
+ * +inf or nothing but -inf makes what the row enters NaN.
  * A loss is factor * sum of weight * (row's or pair's loss) / norm; norm = 0 stands for the sum of the weights that count (their number without
  * weights), and where that is 0 the loss and the gradient are 0.  factor carries a gradient from further up, or a share of a larger batch.
- * Sums of a row are fp32, what is left of it and sums over rows fp64; results are bit-reproducible.
+ * Sums of a row are fp32, its logarithm and sums over rows fp64; results are bit-reproducible (on GPUs with the same number of SMs).
  * T is at most 2^31 - 1 and may be 0, V at most 2^24.  Scratch, streams, threads and graphs as in the section above.
  * Errors: LR_ERR_NULL, LR_ERR_SHAPE (a size, ld or K out of range), LR_ERR_ALIGNMENT, LR_ERR_VALUE (an option out of range or not
  * finite, an id width, an overlap), LR_ERR_NOMEM.

@@ -290,7 +290,7 @@ __device__ __forceinline__ double class_log(float s) {
 
 // ---- which rows count ----------------------------------------------------------------------------------
 // One CTA writes the numbers of the rows that count into `order`, in their order, those of the others behind them, and sums the weights.
-// Rows that do not count get their zeros here (all but their gradient).  T = 8192: 3 us, beside the start of k_class_ring.
+// Rows that do not count get their zeros here (all but their gradient).  Bound by latency, 8192 rows at a turn: about 4 us.
 constexpr int kPrepThreads = 1024;
 constexpr int kPrepItems = 8;
 
@@ -673,8 +673,12 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 //     cluster's CTAs, by 8-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
 //     Between them they write zeros into the gradients of rows that do not count, as many at every row (all at once they fill the queues
 //     of the memory system that the others wait in).
-// The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that a row fits.  Of the longest
-// rows, stages that the ring could not hold are copied once more (`dropped`).  Stages are given back in the order of the copies.
+// The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that three quarters of a row fit.
+// Stages that the ring could not hold are copied once more (`dropped`), from L2.  Stages are given back in the order of the copies.
+// Bound by HBM for log-probabilities (6.6 TB/s); with a gradient by HBM and by the waits between the passes: 52 % of the issue slots and 56 % of
+// the unit for powers are busy (a quarter of the powers on the FMA pipe instead was no faster), 132 of 148 SMs where a row takes four CTAs.
+// 8192 x 128000 bfloat16, three quarters counting, policy loss 658 us (5.6 TB/s; 693 under the power cap of a long run); 4096 x 128000, 64
+// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 326 us (4.8: bound by the number warps).
 // Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 290 us
 // instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 650 us; two teams
 // 690, three 715, five of three warps 839).  Distillation: the teacher's classes take the room of a stage, and every row more of the number
@@ -1084,8 +1088,9 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
 
 // ---- short rows ----------------------------------------------------------------------------------------
 // A warp per row, the row in its registers between the passes: no barrier, no shared memory but for a teacher's classes.  Up to four groups a
-// lane the next row's logits are on their way meanwhile, and always its target.  Bound by the chain of a row's numbers, a few hundred
-// instructions of a warp: SHORTFIG
+// lane the next row's logits are on their way meanwhile, and always its target.  Bound by instructions: about 600 a row beside 8 a logit and lane
+// (its numbers, set up and stored by a whole warp).  32768 rows of 1000 bfloat16: policy loss 53 us, distillation of 16 classes 56; of 2000,
+// log-probabilities 32 (4.1 TB/s); of 4000, policy loss 126 (4.0 TB/s).
 constexpr int kShortWarps = 8;
 __host__ __device__ constexpr int short_ctas(int mode, int J) { return J <= 2 && mode != kClassDistill ? 4 : J <= 8 ? 3 : 2; }       // per SM, in registers
 
@@ -1233,7 +1238,9 @@ __global__ void __launch_bounds__(kNormThreads) k_class_norm(const __grid_consta
 }
 
 // ---- gradient of log-probabilities ---------------------------------------------------------------------
-// Rows whose statistics are known: from the caller (lse, fp32) or from an earlier pass (top and s).  One read, one write.
+// Rows whose statistics are known: from the caller (lse, fp32) or from an earlier pass (top and s).  One read, one write: bound by HBM.  A CTA
+// takes 16 KB of a row at a time, all loads on their way before the first power (with two groups a thread 444 us instead of 349), and steps
+// through the pieces without a division (336).  8192 x 65536 bfloat16 335 us, 6.4 TB/s; under the power cap of a long run 362.
 struct ClassGradParams {
     const void* x;
     long long ld;
@@ -1379,7 +1386,7 @@ struct ClassPairParams {
 
 constexpr int kPairThreads = 256;
 
-// One CTA per pair, the two sequences by half of it each; the last CTA adds the pairs up.
+// One CTA per pair, the two sequences by half of it each; the last CTA adds the pairs up.  Bound by latency: 4 us for a pair of 150 tokens.
 __global__ void __launch_bounds__(kPairThreads) k_class_pair(const __grid_constant__ ClassPairParams p) {
     __shared__ double warp_part[kPairThreads / 32][2];
     __shared__ double total[3];
