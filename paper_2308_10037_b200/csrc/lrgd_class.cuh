@@ -200,6 +200,10 @@ struct ClassRow {
     }
 };
 
+__device__ __forceinline__ float warp_largest(float v) {
+    const uint32_t key = __reduce_max_sync(0xffffffffu, order_key(v));
+    return __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
+}
 // The running maximum and sum of a part of a row: s = sum of 2^((x - top) * c), top = -inf before the first finite x
 struct ClassSum {
     float top = -INFINITY, s = 0.0f;
@@ -241,8 +245,7 @@ struct ClassSum {
     }
     // the sum over the lanes of a warp, the same bits in all of them
     __device__ __forceinline__ void over_warp(float c) {
-        const uint32_t key = __reduce_max_sync(0xffffffffu, order_key(top));
-        const float most = __uint_as_float(key ^ ((key >> 31) ? 0x80000000u : 0xffffffffu));
+        const float most = warp_largest(top);
         s = s == 0.0f ? 0.0f : s * class_power(top, most, c);       // (a NaN stays one)
         top = most;
 #pragma unroll
@@ -550,9 +553,10 @@ struct ClassTerms {
     double lp, lse;
     float first, kl, clipped;    // the row's loss: its parts (policy: the first and whether it is clipped; distillation: kl)
 };
-template <int MODE>
+// (by W lanes, each with the same arguments)
+template <int MODE, int W = 32>
 __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, const ClassInputs& in, const ClassSum& sum, double inv, ClassTerms& terms) {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & (W - 1);
     const double log_s = class_log(sum.s);
     ClassNumbers r{};
     terms = ClassTerms{0.0, static_cast<double>(sum.top) * p.scale + log_s, 0.0f, 0.0f, 0.0f};
@@ -575,9 +579,9 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
         // the last place).
         const float d = static_cast<float>(lane == 0 ? terms.lp - in.old_logp : lane == 1 ? in.ref_logp - terms.lp : terms.lp);
         const float e = expm1f(d);
-        float ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0) + 1.0f : 1.0f;
+        float ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0, W) + 1.0f : 1.0f;
         if (ratio > 3.4e38f) ratio = 3.4e38f;       // (no infinity: an advantage of 0 has no loss whatever the ratio)
-        const float away = __shfl_sync(0xffffffffu, e, 1), rest = __shfl_sync(0xffffffffu, e, 2);
+        const float away = __shfl_sync(0xffffffffu, e, 1, W), rest = __shfl_sync(0xffffffffu, e, 2, W);
         const float a = in.adv, held = fminf(fmaxf(ratio, p.ratio_low), p.ratio_high);
         const bool clipped = ratio * a > held * a;
         float g = clipped ? 0.0f : -ratio * a;
@@ -590,10 +594,10 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
     }
     return r;
 }
+// (`write` in one lane)
 template <int MODE>
 __device__ __forceinline__ void class_account(const ClassParams& p, long long t, const ClassInputs& in, const ClassSum& sum, const ClassTerms& terms,
                                               bool write, double (&sums)[3]) {
-    write = write && (threadIdx.x & 31) == 0;
     if (MODE == kClassDistill) {
         if (p.row_kl && write) p.row_kl[t] = terms.kl;
         sums[0] += static_cast<double>(in.w) * terms.kl;
@@ -624,16 +628,25 @@ __device__ __forceinline__ float class_top_value(const ClassParams& p, const Cla
     }
     return fmaf(class_power(top.x[j], largest, p.c), r.factor, -r.at * q);
 }
-// Sum of the weights of all rows that count, by one warp
+// Thread `me` of `many`: its part of the sum of the weights of the rows first ... last - 1 that count, four rows' loads at a time
 template <int MODE>
-__device__ __forceinline__ double class_norm_warp(const ClassParams& p) {
+__device__ __forceinline__ double class_norm_part(const ClassParams& p, long long first, long long last, int me, int many) {
+    constexpr int U = 4;
     double n = 0.0;
-    for (long long t = threadIdx.x & 31; t < p.T; t += 32) {
-        long long target;
-        float w;
-        if (class_counts(p, t, MODE, &target, &w)) n += w;
+    for (long long t = first + me; t < last; t += U * many) {
+        long long id[U];
+        float w[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long at = t + u * many;
+            w[u] = at >= last ? 0.0f : p.weights ? __ldg(p.weights + at) : 1.0f;
+            id[u] = at < last && MODE != kClassDistill ? load_any_id(p.ids, p.wide_ids, at) : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (w[u] != 0.0f && (MODE == kClassDistill || (id[u] != p.ignore && id[u] >= 0 && id[u] < p.V))) n += w[u];
     }
-    return warp_sum64(n);
+    return n;
 }
 // The warp that is done last adds the sums of all `ctas` warps that call this up, in a fixed order
 template <int MODE>
@@ -993,7 +1006,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
         double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
         if (MODE != kClassLogp) {
             double n = p.norm;
-            if (n == 0.0) n = p.listed ? sh.list.total : p.order ? p.prep->norm : class_norm_warp<MODE>(p);
+            if (n == 0.0) n = p.listed ? sh.list.total : p.order ? p.prep->norm : warp_sum64(class_norm_part<MODE>(p, 0, p.T, lane, 32));
             inv = n == 0.0 ? 0.0 : 1.0 / n;
         }
         long long from = 0, to = p.T;
@@ -1057,7 +1070,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                 if (GRAD) sh.row[at] = make_float4(now.factor, sum.top, counts ? 1.0f : 0.0f, 0.0f);
                 mbar_arrive(sh.ready + at);
             }
-            if (counts) class_account<MODE>(p, t, in, sum, terms, rank == 0, sums);
+            if (counts) class_account<MODE>(p, t, in, sum, terms, rank == 0 && lane == 0, sums);
             else if (rank == 0 && lane == 0) class_dead_row<MODE>(p, t);
             if (!GRAD) continue;
             zeros(k);
@@ -1089,17 +1102,51 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
 // ---- short rows ----------------------------------------------------------------------------------------
 // A warp per row, the row in its registers between the passes: no barrier, no shared memory but for a teacher's classes.  Up to four groups a
 // lane the next row's logits are on their way meanwhile, and always its target.  Bound by instructions: about 600 a row beside 8 a logit and lane
-// (its numbers, set up and stored by a whole warp).  32768 rows of 1000 bfloat16: policy loss 53 us, distillation of 16 classes 56; of 2000,
-// log-probabilities 32 (4.1 TB/s); of 4000, policy loss 126 (4.0 TB/s).
+// (its numbers, set up and stored by a whole warp), which k_class_bundle shares among rows of up to 1024 logits where there are many.  32768 rows
+// of 1000 bfloat16: distillation of 16 classes 55 us; of 2000, log-probabilities 32 (4.1 TB/s); of 4000, policy loss 121 (4.1 TB/s).
 constexpr int kShortWarps = 8;
 __host__ __device__ constexpr int short_ctas(int mode, int J) { return J <= 2 && mode != kClassDistill ? 4 : J <= 8 ? 3 : 2; }       // per SM, in registers
+
+// (by all threads of a CTA)
+template <int MODE>
+__device__ __forceinline__ double short_inverse_norm(const ClassParams& p) {
+    if (MODE == kClassLogp) return 0.0;
+    __shared__ double warp_part[kShortWarps];
+    double n = p.norm;
+    if (n == 0.0 && p.norm_parts > 0) {
+        for (int i = threadIdx.x & 31; i < p.norm_parts; i += 32) n += __ldcg(p.norm_part + i);
+        n = warp_sum64(n);
+    } else if (n == 0.0) {
+        n = warp_sum64(class_norm_part<MODE>(p, 0, p.T, threadIdx.x, kShortWarps * 32));
+        if ((threadIdx.x & 31) == 0) warp_part[threadIdx.x >> 5] = n;
+        __syncthreads();
+        n = 0.0;
+        for (int w = 0; w < kShortWarps; ++w) n += warp_part[w];
+    }
+    return n == 0.0 ? 0.0 : 1.0 / n;
+}
+// Every warp's sums, the same in all of its lanes, to the outputs
+template <int MODE>
+__device__ __forceinline__ void short_finish(const ClassParams& p, double inv, double (&sums)[3]) {
+    __shared__ double cta_part[kShortWarps][3];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (MODE == kClassLogp) return;
+    if (lane == 0)
+        for (int i = 0; i < 3; ++i) cta_part[warp][i] = sums[i];
+    __syncthreads();
+    if (warp != 0) return;
+    for (int i = 0; i < 3; ++i) {
+        sums[i] = 0.0;
+        for (int w = 0; w < kShortWarps; ++w) sums[i] += cta_part[w][i];
+    }
+    class_finish<MODE>(p, blockIdx.x, gridDim.x, inv, sums);
+}
 
 template <class E, int MODE, bool GRAD, int J>
 __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class_short(const __grid_constant__ ClassParams p) {
     using G = ClassGroup<E>;
     constexpr bool kAhead = J <= 4 && MODE != kClassDistill;
     constexpr int B = J < 4 ? J : 4;                // groups that are worked on together
-    __shared__ double cta_part[kShortWarps][3];
     extern __shared__ __align__(128) unsigned char class_smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     ClassTop top{};
@@ -1129,23 +1176,14 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
         r.edge = lane < row.edges ? load_local(row.x + row.edge(lane)) : 0.0f;
         if (MODE != kClassDistill) class_inputs<MODE>(p, t, row.x, top, r.in);
     };
-    double sums[3] = {0.0, 0.0, 0.0}, inv = 0.0;
+    double sums[3] = {0.0, 0.0, 0.0};
     const long long step = static_cast<long long>(gridDim.x) * kShortWarps;
     long long t = static_cast<long long>(blockIdx.x) * kShortWarps + warp;
     Row now{}, next{};
     look(t, now);
     load(t, now);
     look(t + step, next);
-    if (MODE != kClassLogp) {                       // (beside the first row's loads)
-        double n = p.norm;
-        if (n == 0.0 && p.norm_parts > 0) {
-            for (int i = lane; i < p.norm_parts; i += 32) n += __ldcg(p.norm_part + i);
-            n = warp_sum64(n);
-        } else if (n == 0.0) {
-            n = class_norm_warp<MODE>(p);
-        }
-        inv = n == 0.0 ? 0.0 : 1.0 / n;
-    }
+    const double inv = short_inverse_norm<MODE>(p); // (beside the first row's loads)
     for (; t < p.T; t += step) {
         Row after{};
         if (kAhead) {
@@ -1164,7 +1202,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
             sum.settle();
             ClassTerms terms;
             const ClassNumbers numbers = class_numbers<MODE>(p, now.in, sum, inv, terms);
-            class_account<MODE>(p, t, now.in, sum, terms, true, sums);
+            class_account<MODE>(p, t, now.in, sum, terms, lane == 0, sums);
             if (GRAD) {
                 const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-sum.top, -sum.top), factor2 = f32x2_pack(numbers.factor, numbers.factor);
 #pragma unroll
@@ -1201,16 +1239,131 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
         now = next;
         next = after;
     }
-    if (MODE == kClassLogp) return;
-    if (lane == 0)
-        for (int i = 0; i < 3; ++i) cta_part[warp][i] = sums[i];
-    __syncthreads();
-    if (warp != 0) return;
-    for (int i = 0; i < 3; ++i) {
-        sums[i] = 0.0;
-        for (int w = 0; w < kShortWarps; ++w) sums[i] += cta_part[w][i];
+    short_finish<MODE>(p, inv, sums);
+}
+
+// R rows per warp and turn: their numbers are worked out at the same time, by 32 / R lanes each, which the sums reach by exchanging halves; a row's
+// terms stay in registers for the gradient, 64 a lane at most.  Bound by instructions and by the two loads in turn of a row's target and logits:
+// 32768 rows of 1000 bfloat16, policy loss 40 us (a warp per row: 53); of 200, 22 (33); of 256, log-probabilities 9.2 (15.4).  With rows for one
+// CTA per SM or less a warp per row is faster (500 bfloat16, policy loss: 64 rows 7.1 us instead of 8.9, 600 rows 8.2 instead of 9.1, 2000 rows
+// 11.5 instead of 11.2, 4000 rows 14.1 instead of 11.7).  Three CTAs per SM spill with a gradient (32768 x 1000: 55 us).
+template <class E>
+__host__ __device__ constexpr int bundle_rows(int J) {
+    return J * ClassGroup<E>::N <= 16 ? 4 : 64 / (J * ClassGroup<E>::N);
+}
+__host__ __device__ constexpr int bundle_ctas(bool grad) { return grad ? 2 : 3; }          // per SM, in registers
+
+template <class E, int MODE, bool GRAD, int J>
+__global__ void __launch_bounds__(kShortWarps * 32, bundle_ctas(GRAD)) k_class_bundle(const __grid_constant__ ClassParams p) {
+    using G = ClassGroup<E>;
+    constexpr int R = bundle_rows<E>(J), W = 32 / R;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane / W;
+    const bool writes = (lane & (W - 1)) == 0;      // lanes part * W ... belong to row `first + part`
+    grid_dependency_wait();
+    struct Look {
+        long long target;
+        float w;
+        bool counts;
+    };
+    auto look = [&](long long t) {
+        Look l{0, 0.0f, false};
+        if (t >= p.T) return l;
+        l.counts = class_counts(p, t, MODE, &l.target, &l.w);
+        if (MODE == kClassLogp && p.offsets)
+            l.counts = l.counts && t >= load_any_id(p.offsets, p.wide_offsets, 0) && t < load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+        return l;
+    };
+    double sums[3] = {0.0, 0.0, 0.0};
+    const long long step = static_cast<long long>(gridDim.x) * kShortWarps * R;
+    long long first = (static_cast<long long>(blockIdx.x) * kShortWarps + warp) * R;
+    Look now = look(first + part);
+    const double inv = short_inverse_norm<MODE>(p);
+    for (; first < p.T; first += step) {
+        const long long t = first + part;
+        const unsigned live = __ballot_sync(0xffffffffu, now.counts);
+        uint4 raw[R][J];
+        float edge[R], top[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool counts = live >> (r * W) & 1;
+            const ClassRow<E> row(p.x, p.ld, nullptr, 0, first + r, p.V);
+#pragma unroll
+            for (int j = 0; j < J; ++j) raw[r][j] = counts && 32 * j + lane < row.groups ? row.load(32 * j + lane) : G::nothing();
+            edge[r] = counts && lane < row.edges ? load_local(row.x + row.edge(lane)) : -INFINITY;
+        }
+        ClassInputs in{};
+        in.target = now.target;
+        in.w = now.w;
+        if (now.counts) class_inputs<MODE>(p, t, static_cast<const E*>(p.x) + t * p.ld, ClassTop{}, in);
+        const Look next = look(t + step);
+        uint64_t term[R][J][G::P];
+        float s[R];
+        const uint64_t c2 = f32x2_pack(p.c, p.c);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {               // -inf and no term: rows that do not count
+            top[r] = warp_largest(fmaxf(G::template largest<J>(raw[r]), edge[r]));
+            if (top[r] == -INFINITY) top[r] = 0.0f;
+            const uint64_t top2 = f32x2_pack(-top[r], -top[r]);
+            uint64_t two[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < J; ++j)
+#pragma unroll
+                for (int i = 0; i < G::P; ++i) {
+                    term[r][j][i] = class_powers(G::pair(raw[r][j], i), top2, c2);
+                    two[i & 1] = f32x2_add(two[i & 1], term[r][j][i]);
+                }
+            edge[r] = class_power(edge[r], top[r], p.c);
+            float lo, hi;
+            f32x2_unpack(f32x2_add(two[0], two[1]), lo, hi);
+            s[r] = lo + hi + edge[r];
+        }
+        ClassSum sum;
+        sum.top = top[0];
+#pragma unroll
+        for (int r = 1; r < R; ++r) sum.top = part == r ? top[r] : sum.top;
+#pragma unroll
+        for (int d = R / 2; d >= 1; d >>= 1)
+#pragma unroll
+            for (int r = 0; r < d; ++r) {           // the upper half of the lanes takes the upper half of the rows
+                const bool up = part & d;
+                const float give = up ? s[r] : s[r + d];
+                s[r] = (up ? s[r + d] : s[r]) + __shfl_xor_sync(0xffffffffu, give, d * W);
+            }
+        sum.s = s[0];
+#pragma unroll
+        for (int d = W / 2; d >= 1; d >>= 1) sum.s += __shfl_xor_sync(0xffffffffu, sum.s, d);
+        ClassTerms terms;
+        const ClassNumbers numbers = class_numbers<MODE, W>(p, in, sum, inv, terms);
+        if (now.counts) class_account<MODE>(p, t, in, sum, terms, writes, sums);
+        else if (writes && t < p.T) class_dead_row<MODE>(p, t);
+        if (GRAD) {
+            const float own = now.counts ? numbers.factor : 0.0f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (first + r >= p.T) break;
+                const float factor = __shfl_sync(0xffffffffu, own, r * W);
+                const uint64_t factor2 = f32x2_pack(factor, factor);
+                const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, first + r, p.V);
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    if (32 * j + lane < row.groups) {
+                        uint64_t v[G::P];
+#pragma unroll
+                        for (int i = 0; i < G::P; ++i) v[i] = f32x2_mul(term[r][j][i], factor2);
+                        row.store(32 * j + lane, v);
+                    }
+                }
+                if (lane < row.edges) store_from_float(row.dx + row.edge(lane), edge[r] * factor);
+            }
+            __syncwarp();                           // the targets' values replace what was just written
+            if (now.counts && writes) store_from_float(static_cast<E*>(p.dx) + t * p.ld_d + in.target, numbers.at);
+        }
+        now = next;
     }
-    class_finish<MODE>(p, blockIdx.x, gridDim.x, inv, sums);
+#pragma unroll
+    for (int d = W; d < 32; d *= 2)
+        for (int i = 0; i < 3; ++i) sums[i] += __shfl_xor_sync(0xffffffffu, sums[i], d);
+    short_finish<MODE>(p, inv, sums);
 }
 
 // norm_part[b] = sum of the weights of the rows that count among rows b * norm_rows ...
@@ -1221,12 +1374,7 @@ __global__ void __launch_bounds__(kNormThreads) k_class_norm(const __grid_consta
     __shared__ double warp_part[kNormThreads / 32];
     grid_dependency_release();
     const long long first = blockIdx.x * p.norm_rows, last = min(first + p.norm_rows, p.T);
-    double sum = 0.0;
-    for (long long t = first + threadIdx.x; t < last; t += kNormThreads) {
-        long long target;
-        float w;
-        if (class_counts(p, t, MODE, &target, &w)) sum += w;
-    }
+    double sum = class_norm_part<MODE>(p, first, last, threadIdx.x, kNormThreads);
     sum = warp_sum64(sum);
     if ((threadIdx.x & 31) == 0) warp_part[threadIdx.x >> 5] = sum;
     __syncthreads();

@@ -49,7 +49,9 @@ bool apart(const E* x, int64_t ld, const E* dx, int64_t ld_d, int64_t T, int64_t
 }
 
 constexpr int kShortGroups = 16;                    // 16-byte groups per lane of the short rows, at most
-constexpr int kNormInline = 512;                    // rows whose weights every warp adds up for itself
+// Short rows: up to this many, every CTA adds up the weights for itself, beyond, a kernel before this one does (policy loss, 1000 x 200: 8.3 and
+// 8.9 us; 4000 x 200: 11.1 and 10.2)
+constexpr int kNormInline = 1024;
 
 // How rows are worked on: a warp each (groups per lane: 1, 2, 4, 8 or 16), or by CTAs with rings, `cluster` to a row.
 struct RowPlan {
@@ -161,7 +163,7 @@ int launch_short(lr_ctx* ctx, ClassParams& p, int lane_groups, const RowScratch&
     if (MODE != kClassLogp && p.norm == 0.0 && p.T > kNormInline) {
         double* part = reinterpret_cast<double*>(scratch.data + at.sums + at.prep);
         p.norm_part = part;
-        p.norm_rows = std::max<int64_t>(4096, (p.T + 1023) / 1024);
+        p.norm_rows = std::max<int64_t>(1024, (p.T + 1023) / 1024);
         p.norm_parts = int((p.T + p.norm_rows - 1) / p.norm_rows);
         const int r = launched(ctx, [&] { k_class_norm<MODE><<<p.norm_parts, kNormThreads, 0, st>>>(p, part); });
         if (r != LR_OK) return r;
@@ -170,6 +172,14 @@ int launch_short(lr_ctx* ctx, ClassParams& p, int lane_groups, const RowScratch&
     const size_t smem = MODE == kClassDistill ? kShortWarps * class_top_bytes(p.K) : 0;
     auto go = [&](auto groups) -> int {
         constexpr int J = decltype(groups)::value;
+        if constexpr (MODE != kClassDistill && J * ClassGroup<E>::N <= 32) {
+            if (p.T > int64_t(plan_sms(ctx)) * kShortWarps) {       // (both ways: see k_class_bundle)
+                const dim3 grid(grid_for(ctx, p.T, kShortWarps * bundle_rows<E>(J), bundle_ctas(GRAD)));
+                LR_CK(ctx, launch_kernel(k_class_bundle<E, MODE, GRAD, J>, grid, dim3(kShortWarps * 32), 0, st, dependent, p));
+                ctx->launches += 1;
+                return LR_OK;
+            }
+        }
         const dim3 grid(grid_for(ctx, p.T, kShortWarps, short_ctas(MODE, J)));
         using Tag = ClassShortTag<E, MODE, GRAD, J>;
         const auto kern = k_class_short<E, MODE, GRAD, J>;
