@@ -406,6 +406,14 @@ __device__ __forceinline__ void class_clear_marks(const ClassTop& top) {
     for (int i = threadIdx.x & 31; i < (1 << top.bits) / 128; i += 32) reinterpret_cast<uint4*>(top.marks)[i] = make_uint4(0, 0, 0, 0);
     __syncwarp();
 }
+// Asks for a row's classes and the teacher's logits to be in L2 (2048 x 100000 fp32, 128 classes: 307 -> 297 us)
+__device__ __forceinline__ void class_top_ahead(const ClassParams& p, long long t) {
+    const int id_bytes = p.K * (p.wide_ids ? 8 : 4), v_bytes = p.K * (p.teacher_half ? 2 : 4);
+    const char* ids = static_cast<const char*>(p.ids) + t * id_bytes;
+    const char* v = static_cast<const char*>(p.teacher) + t * v_bytes;
+    for (int b = 128 * (threadIdx.x & 31); b < id_bytes; b += 128 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(ids + b));
+    for (int b = 128 * (threadIdx.x & 31); b < v_bytes; b += 128 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(v + b));
+}
 struct ClassEntry {
     long long id;
     float v;
@@ -686,12 +694,12 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 //     cluster's CTAs, by 8-byte messages), work out the row's numbers in fp64, and put the values at the targets over the gradient.
 //     Between them they write zeros into the gradients of rows that do not count, as many at every row (all at once they fill the queues
 //     of the memory system that the others wait in).
-// The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that three quarters of a row fit.
+// The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that two thirds of a row fit.
 // Stages that the ring could not hold are copied once more (`dropped`), from L2.  Stages are given back in the order of the copies.
 // Bound by HBM for log-probabilities (6.6 TB/s); with a gradient by HBM and by the waits between the passes: 52 % of the issue slots and 56 % of
 // the unit for powers are busy (a quarter of the powers on the FMA pipe instead was no faster), 132 of 148 SMs where a row takes four CTAs.
-// 8192 x 128000 bfloat16, three quarters counting, policy loss 658 us (5.6 TB/s; 693 under the power cap of a long run); 4096 x 128000, 64
-// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 326 us (4.8: bound by the number warps).
+// 8192 x 128000 bfloat16, three quarters counting, policy loss 661 us (5.6 TB/s; 693 under the power cap of a long run); 4096 x 128000, 64
+// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 320 us (4.9: bound by the number warps).
 // Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 290 us
 // instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 650 us; two teams
 // 690, three 715, five of three warps 839).  Distillation: the teacher's classes take the room of a stage, and every row more of the number
@@ -1045,6 +1053,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (MODE == kClassLogp) counts = counts && t >= from && t < to;
             const bool edges = rank == 0 && lane < row.edges;
             const float edge = counts && edges ? load_local(row.x + row.edge(lane)) : 0.0f;
+            if (MODE == kClassDistill && k + kNumberWarps < mine) class_top_ahead(p, row_of(k + kNumberWarps));
             if (counts) class_inputs<MODE>(p, t, row.x, top, in);
             const int at = k % kRows, parity = (k / kRows) & 1;
             if (!wait(sh.summed + at, parity)) break;
