@@ -414,6 +414,17 @@ __device__ __forceinline__ void class_top_ahead(const ClassParams& p, long long 
     for (int b = 128 * (threadIdx.x & 31); b < id_bytes; b += 128 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(ids + b));
     for (int b = 128 * (threadIdx.x & 31); b < v_bytes; b += 128 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(v + b));
 }
+// ... and the logits at them, by the CTAs of a cluster together, each of which will read them all (2048 x 100000 fp32, 256 classes: 332 -> 309
+// us; 4096 x 128000 bfloat16, 128 classes: 364 -> 359; a CTA alone would ask for what it reads next: no faster)
+template <class E>
+__device__ __forceinline__ void class_top_logits_ahead(const ClassParams& p, long long t, int rank) {
+    const E* row = static_cast<const E*>(p.x) + t * p.ld;
+#pragma unroll 2
+    for (int j = 32 * rank + (threadIdx.x & 31); j < p.K; j += 32 * p.cluster) {
+        const long long id = load_any_id(p.ids, p.wide_ids, t * p.K + j);
+        if (id >= 0 && id < p.V) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + id));
+    }
+}
 struct ClassEntry {
     long long id;
     float v;
@@ -699,7 +710,7 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 // Bound by HBM for log-probabilities (6.6 TB/s); with a gradient by HBM and by the waits between the passes: 52 % of the issue slots and 56 % of
 // the unit for powers are busy (a quarter of the powers on the FMA pipe instead was no faster), 132 of 148 SMs where a row takes four CTAs.
 // 8192 x 128000 bfloat16, three quarters counting, policy loss 661 us (5.6 TB/s; 693 under the power cap of a long run); 4096 x 128000, 64
-// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 320 us (4.9: bound by the number warps).
+// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 301 us (5.2: bound by the number warps).
 // Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 290 us
 // instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 650 us; two teams
 // 690, three 715, five of three warps 839).  Distillation: the teacher's classes take the room of a stage, and every row more of the number
@@ -1081,6 +1092,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             }
             if (counts) class_account<MODE>(p, t, in, sum, terms, rank == 0 && lane == 0, sums);
             else if (rank == 0 && lane == 0) class_dead_row<MODE>(p, t);
+            if (MODE == kClassDistill && C > 1 && k + kNumberWarps < mine) class_top_logits_ahead<E>(p, row_of(k + kNumberWarps), rank);
             if (!GRAD) continue;
             zeros(k);
             if (edges) store_from_float(row.dx + row.edge(lane), counts ? class_power(edge, sum.top, p.c) * now.factor : 0.0f);
