@@ -709,8 +709,8 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 // Stages that the ring could not hold are copied once more (`dropped`), from L2.  Stages are given back in the order of the copies.
 // Bound by HBM for log-probabilities (6.6 TB/s); with a gradient by HBM and by the waits between the passes: 52 % of the issue slots and 56 % of
 // the unit for powers are busy (a quarter of the powers on the FMA pipe instead was no faster), 132 of 148 SMs where a row takes four CTAs.
-// 8192 x 128000 bfloat16, three quarters counting, policy loss 661 us (5.6 TB/s; 693 under the power cap of a long run); 4096 x 128000, 64
-// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 301 us (5.2: bound by the number warps).
+// 8192 x 128000 bfloat16, three quarters counting, policy loss 661 us (5.6 TB/s; 693 to 707 under the power cap of a long run); 4096 x 128000, 64
+// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 299 us (5.2: bound by the number warps).
 // Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 290 us
 // instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 650 us; two teams
 // 690, three 715, five of three warps 839).  Distillation: the teacher's classes take the room of a stage, and every row more of the number
