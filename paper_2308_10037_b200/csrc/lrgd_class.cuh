@@ -441,8 +441,9 @@ __device__ __forceinline__ ClassEntry class_entry(const ClassParams& p, long lon
 }
 // id in [0, V), or -1 where the entry is absent
 __device__ __forceinline__ int class_entry_id(const ClassParams& p, const ClassEntry& e) {
+    if (e.id == p.ignore) return -1;                // (a class of the vocabulary or not)
     if (e.id < 0 || e.id >= p.V) {
-        if (e.id != p.ignore) atomicExch(p.status, -4);
+        atomicExch(p.status, -4);                   // LR_ERR_VALUE
         return -1;
     }
     return e.v == -INFINITY ? -1 : static_cast<int>(e.id);
