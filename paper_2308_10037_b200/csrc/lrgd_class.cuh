@@ -1615,10 +1615,12 @@ __global__ void __launch_bounds__(kPairThreads) k_class_pair(const __grid_consta
         if (tid == 0) {
             const double h = p.beta * (s[0] - s[1] - ref) - p.margin;
             // log sigmoid(h) = -softplus(-h), log sigmoid(-h) = -softplus(h); t = exp(-|h|) and what follows from it in fp32 (see logistic_terms)
-            const float size = fabsf(static_cast<float>(h)), t = expf(-size) * (1.0f - static_cast<float>(fabs(h) - size)), one = 1.0f / (1.0f + t);
+            // An h that is infinite (a sequence without probability) or past fp32 has t = 0; a term without weight is left out, infinite or not.
+            const float size = fabsf(static_cast<float>(h)), t = size > 104.0f ? 0.0f : expf(-size) * (1.0f - static_cast<float>(fabs(h) - size)),
+                        one = 1.0f / (1.0f + t);
             const double soft = log1pf(t), plus = fmax(h, 0.0) + soft, minus = fmax(-h, 0.0) + soft;
             const float right = h >= 0.0 ? one : t * one, wrong = h >= 0.0 ? t * one : one;
-            const double loss = (1.0 - p.smoothing) * minus + p.smoothing * plus;
+            const double loss = (p.smoothing < 1.0 ? (1.0 - p.smoothing) * minus : 0.0) + (p.smoothing > 0.0 ? p.smoothing * plus : 0.0);
             p.pair_loss[pair] = w == 0.0f ? 0.0 : w * loss;
             p.h[pair] = static_cast<float>(h);
             if (p.seq_logp) {

@@ -47,3 +47,92 @@ def test_a_class_of_the_vocabulary_that_is_ignored(ctx, dt, T, V):
             other = ctx.distill_loss(x, gone, t, tlse, scale=scale)
             assert all(torch.equal(a, b) for a, b in zip(other, (got, gr, d)))
     assert ctx.device_status() == 0
+
+
+# ---- an infinite log-probability -------------------------------------------------------------------------
+
+def pref_by_hand(x, y, o, ref, w, beta, margin, smoothing, average=False, scale=1.0):
+    """(loss, margins, seq_logp, dlogits, each row's coefficient) in float64 from the definition: a term of a loss whose factor is 0 is left out; a
+    sequence whose own offsets fall or leave the rows is empty; a row that several sequences hold counts in each."""
+    T, P = len(y), len(o) // 2
+    lp = log_softmax(x.double(), scale).gather(1, y.clamp(0, x.shape[1] - 1)[:, None])[:, 0]
+    live = (y >= 0) & (y < x.shape[1])
+    lp = torch.where(live, lp, 0.0)
+    rows = [range(a, z) if 0 <= a <= z <= T else range(0) for a, z in zip(o, o[1:])]
+    n = [max(1, int(live[r.start:r.stop].sum())) if average else 1 for r in rows]
+    s = [lp[r.start:r.stop].sum() / m if len(r) else torch.zeros((), dtype=torch.float64, device="cuda") for r, m in zip(rows, n)]
+    s = torch.stack(s)
+    d = s - (ref.double() if ref is not None else 0.0)
+    h = beta * (d[:P] - d[P:]) - margin
+    wl = torch.ones(P, dtype=torch.float64, device="cuda") if w is None else w.double()
+    inv = 1.0 / float(wl.sum()) if float(wl.sum()) else 0.0
+    loss, coef = 0.0, torch.zeros(T, dtype=torch.float64, device="cuda")
+    for i in range(P):
+        if float(wl[i]) == 0.0:
+            continue
+        hi, each = float(h[i]), 0.0
+        soft = math.nan if hi != hi else math.log1p(math.exp(-abs(hi)))
+        if smoothing < 1:
+            each += (1 - smoothing) * (max(-hi, 0.0) + soft)
+        if smoothing > 0:
+            each += smoothing * (max(hi, 0.0) + soft)
+        right = math.nan if hi != hi else 1 / (1 + math.exp(-hi)) if hi > -700 else 0.0
+        wrong = math.nan if hi != hi else 1 / (1 + math.exp(hi)) if hi < 700 else 0.0
+        loss += float(wl[i]) * each * inv
+        g = float(wl[i]) * inv * beta * (smoothing * right - (1 - smoothing) * wrong)
+        for j, sign in ((i, 1.0), (i + P, -1.0)):
+            coef[rows[j].start:rows[j].stop] += sign * g / n[j]
+    coef = torch.where(live, coef, 0.0)
+    p = torch.softmax(x.double() * scale, 1)
+    dx = torch.where((coef != 0)[:, None], scale * coef[:, None] * (onehot(y, x.shape[1]) - p), 0.0)
+    return torch.tensor([loss], dtype=torch.float64, device="cuda"), h, s, dx, coef
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [60, 5000, 50021])
+def test_a_sequence_without_probability(ctx, dt, V):
+    """A target on a masked class: the pair's margin is infinite.  A rejected answer that cannot be is rejected for good (loss 0, no gradient); a
+    preferred one has an infinite loss and the largest gradient."""
+    o = [0, 4, 7, 12, 15, 20, 22]
+    T = o[-1]
+    x, y = logits(T, V, dt), targets(T, V, drop=0.1)
+    y[[5, 13, 16]] = 3
+    ref = rnd(6, seed=4)
+    for mask_at, smoothing, w in [((13,), 0.0, None), ((13,), 0.2, None), ((5,), 0.0, None), ((5,), 0.1, None), ((5,), 1.0, None), ((16,), 0.0, None),
+                                  ((5, 13), 0.0, None), ((5,), 0.0, torch.tensor([1.0, 0.0, 2.0], device="cuda"))]:
+        xx = x.clone()
+        for at in mask_at:
+            xx[at, 3] = -math.inf
+        loss, h, s, want, coef = pref_by_hand(xx, y, o, ref, w, 0.3, 0.1, smoothing)
+        got, gh, gs, d = ctx.pref_loss(xx, y, torch.tensor(o, device="cuda"), ref, w, beta=0.3, margin=0.1, smoothing=smoothing)
+        L, P = errs(xx, 1.0)
+        fine = s.isfinite()
+        assert torch.equal(gs[~fine].double(), s[~fine]) and torch.equal(gh[~h.isfinite()].double(), h[~h.isfinite()])
+        close(gs[fine], s[fine], 6 * L + 2 * U * s[fine].abs())
+        if math.isfinite(float(loss)):
+            close(got, loss, 0.3 * 12 * L + 4 * U * loss.abs())
+        else:
+            assert float(got) == float(loss)
+        p = torch.softmax(xx.double(), 1)
+        c = coef.abs()[:, None]
+        close(d, want, c * ((p + onehot(y, V)) * (0.3 * 12 * L + 6 * U) + P * p + (L + 8 * U) * onehot(y, V)) + 1.01 * HALF[dt] * want.abs() + 1e-38)
+
+
+def test_margins_beyond_fp32(ctx):
+    """h past fp32's largest number, by a reference and by classes at the type's lowest value."""
+    x, y = rnd(40, 50) * 2, targets(40, 50)
+    o = [0, 20, 40]
+    for r, beta in (([3e38, -3e38], 2.0), ([-3e38, 3e38], 2.0), ([math.inf, 0.0], 0.5), ([0.0, math.inf], 0.5), ([200.0, 0.0], 1.0), ([0.0, 200.0], 1.0)):
+        ref = torch.tensor(r, device="cuda")
+        loss, h, s, want, coef = pref_by_hand(x, y, o, ref, None, beta, 0.0, 0.0)
+        got, gh, gs, d = ctx.pref_loss(x, y, torch.tensor(o, device="cuda"), ref, beta=beta)
+        close(gh, h.float(), 1e-6 * h.abs().nan_to_num(0.0, posinf=0.0) + 1e-4)
+        close(got, loss.float(), 1e-5 * loss.abs().nan_to_num(0.0, posinf=0.0) + 1e-38)
+        close(d, want, 1e-4 * want.abs() + 1e-6 * coef.abs()[:, None] + 1e-38)
+    low = torch.finfo(torch.float32).min
+    x[25, 3], y[25] = low, 3
+    x[30, 3], y[30] = low, 3
+    got, gh, gs, d = ctx.pref_loss(x, y, torch.tensor(o, device="cuda"), beta=2.0)
+    assert float(gh) == math.inf and float(got) == 0.0 and bool((d == 0).all())
+    got, gh, gs, d = ctx.pref_loss(x, y, torch.tensor([0, 0, 40], device="cuda"), beta=-2.0)
+    assert float(gh) == -math.inf and float(got) == math.inf and bool(torch.isfinite(d).all()) and bool((d != 0).any())
