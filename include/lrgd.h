@@ -592,6 +592,8 @@ int lr_logp_grad_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t
  * d_stats [4] = loss, and of the rows that count the weighted means (divided by norm) of -min(r A, r' A), of kl and of [r A > r' A]
  * (rows that the clip holds: no gradient from the first term).  d_logp NULL or [T] = lp.  d_dlogits NULL: no gradient.
  * d_weights NULL or [T] (a mask, or 1 / length).  clip_low, clip_high >= 0 (infinity: no clip), kl_coef finite.
+ * With kl_coef = 0 the divergence is only watched: whatever it is, even infinite, enters d_stats[2] alone.  What a row's gradient is multiplied by
+ * is held within 1.69e38 where r A or exp(ref - lp) is past fp32.
  */
 typedef struct lr_policy_opt {
     int64_t ignore_id;

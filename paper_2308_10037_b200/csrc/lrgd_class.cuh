@@ -568,6 +568,9 @@ __device__ __forceinline__ float class_kl(float d) {
     }
     return d == INFINITY ? d : expm1f(d) - d;
 }
+// Half of fp32's range at most (a NaN stays one): a difference of two such numbers is finite, and a row's factor times a power that is 0 is 0 also
+// where the formula is past fp32.
+__device__ __forceinline__ float class_held(float v) { return v > 1.69e38f ? 1.69e38f : v < -1.69e38f ? -1.69e38f : v; }
 // ... and what of it is written down afterwards
 struct ClassTerms {
     double lp, lse;
@@ -580,7 +583,7 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
     const double log_s = class_log(sum.s);
     ClassNumbers r{};
     terms = ClassTerms{0.0, static_cast<double>(sum.top) * p.scale + log_s, 0.0f, 0.0f, 0.0f};
-    const float gain = static_cast<float>(in.w * inv * p.factor * p.scale);
+    const float gain = class_held(static_cast<float>(in.w * inv * p.factor * p.scale));
     if (MODE == kClassDistill) {
         // with the teacher's own normalisation log q is smaller by log(all)
         const float all = in.top.all, one = p.teacher_lse || all == 0.0f ? 1.0f : 1.0f / all, mass = p.teacher_lse || all == 0.0f ? all : 1.0f;
@@ -604,11 +607,11 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
         const float away = __shfl_sync(0xffffffffu, e, 1, W), rest = __shfl_sync(0xffffffffu, e, 2, W);
         const float a = in.adv, held = fminf(fmaxf(ratio, p.ratio_low), p.ratio_high);
         const bool clipped = ratio * a > held * a;
-        float g = clipped ? 0.0f : -ratio * a;
-        if (p.ref_logp) g -= p.kl_coef * away;
+        float g = clipped ? 0.0f : class_held(-ratio * a);
+        if (p.ref_logp && p.kl_coef != 0.0f) g -= class_held(p.kl_coef * away);
         terms.first = -(clipped ? held : ratio) * a;
         terms.clipped = clipped ? 1.0f : 0.0f;
-        g *= gain;
+        g = class_held(g * gain);
         r.factor = -g / sum.s;
         r.at = -g * rest;
     }
@@ -687,7 +690,8 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
     }
     if (lane == 0) {
         if (MODE == kClassPolicy) {
-            p.out[0] = static_cast<float>(p.factor * (sums[0] + static_cast<double>(p.kl_coef) * sums[1]));
+            const double kl = p.kl_coef != 0.0f ? static_cast<double>(p.kl_coef) * sums[1] : 0.0;       // (0 * inf where it is only watched)
+            p.out[0] = static_cast<float>(p.factor * (sums[0] + kl));
             for (int i = 0; i < 3; ++i) p.out[1 + i] = static_cast<float>(sums[i]);
         } else {
             p.out[0] = static_cast<float>(p.factor * sums[0]);

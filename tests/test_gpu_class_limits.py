@@ -136,3 +136,35 @@ def test_margins_beyond_fp32(ctx):
     assert float(gh) == math.inf and float(got) == 0.0 and bool((d == 0).all())
     got, gh, gs, d = ctx.pref_loss(x, y, torch.tensor([0, 0, 40], device="cuda"), beta=-2.0)
     assert float(gh) == -math.inf and float(got) == math.inf and bool(torch.isfinite(d).all()) and bool((d != 0).any())
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(6, 50), (1200, 50), (6, 5000), (160, 5000), (6, 50021)])
+def test_a_reference_that_is_far_off(ctx, dt, T, V):
+    """exp(ref - lp) past fp32, and a target without probability under a reference that has one."""
+    x, y, adv = logits(T, V, dt), torch.full((T,), 3, device="cuda"), rnd(T, seed=1)
+    x[0, 3] = -math.inf                             # no probability
+    x[1, 3] = -300.0                                # hardly one
+    x[2, :2] = -math.inf                            # masked classes beside the target
+    x[1, 5:9] = -math.inf
+    ref = torch.full((T,), -2.0, device="cuda")
+    ref[2] = 200.0
+    ref[3] = -math.inf                              # the reference has none: a loss, but no gradient of its own
+    ref[4:] = ctx.logp(x, y)[0][4:] + 0.2
+    plain = ctx.policy_loss(x, y, adv)
+    stats, lp, d = ctx.policy_loss(x, y, adv, None, ref)            # watched only
+    assert torch.equal(stats[:2], plain[0][:2]) and torch.equal(d, plain[2]) and float(stats[2]) == math.inf
+    assert bool(torch.isfinite(d).all())
+    stats, lp, d = ctx.policy_loss(x, y, adv, None, ref, kl_coef=0.1, norm=1.0)
+    assert float(stats[0]) == math.inf and float(stats[2]) == math.inf and torch.equal(stats[1:2], ctx.policy_loss(x, y, adv, norm=1.0)[0][1:2])
+    assert bool(torch.isfinite(d).all())
+    assert bool((d[0] >= 0).sum() >= V - 1) and float(d[0, 3]) < -1e37 and bool((d[1, 5:9] == 0).all()) and bool((d[2, :2] == 0).all())
+    # what is finite is as before: without rows 0 to 3
+    rest = ctx.policy_loss(x[4:], y[4:], adv[4:], None, ref[4:], kl_coef=0.1, norm=1.0)
+    L, P = errs(x[4:], 1.0)
+    size = (adv[4:].double().abs() + 0.1 * math.exp(0.2) + 0.1)[:, None] * (torch.softmax(x[4:].double(), 1) + onehot(y[4:], V))
+    close(d[4:], rest[2], 2 * (L + P) * size + 2.0 ** -7 * (dt == "bf16") * rest[2].double().abs() + 1e-38)
+    # beyond fp32 whatever the norm, with advantages above 1, both signs and a large factor
+    old = torch.full((T,), -400.0, device="cuda")
+    d = ctx.policy_loss(x, y, torch.full((T,), -3.0, device="cuda"), old, ref, kl_coef=7.0, norm=1e-3, factor=100.0)[2]
+    assert bool(torch.isfinite(d).all()) and bool((d[1, 5:9] == 0).all())
