@@ -618,7 +618,8 @@ int lr_policy_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64
  *   h_i = beta * ((S_i - R_i) - (S_(i+pairs) - R_(i+pairs))) - margin
  *   pair's loss = -(1 - smoothing) * log sigmoid(h_i) - smoothing * log sigmoid(-h_i),   0 <= smoothing <= 1
  * d_loss [1], d_margins [pairs] = h, d_seq_logp NULL or [2 * pairs] = S.  Weights (NULL or [pairs]) and norm are those of pairs.  Rows
- * outside all sequences do not count.  A sequence whose offsets fall or leave [0, T] is taken as empty and sets the status word.
+ * outside all sequences do not count.  A sequence whose own offsets fall or leave [0, T] is taken as empty and sets the status word; rows that
+ * falling offsets put into several of the others count in each (bit-reproducibly up to two), and their gradients add up.
  * A target without probability (a masked class) makes S -inf and h infinite: log sigmoid and its derivative are then their limits (a pair whose
  * rejected sequence cannot be has loss and gradient 0, one whose preferred sequence cannot be an infinite loss), and the term whose factor
  * is 0 is left out.  Where that is so of both sequences, h and what it enters are NaN.

@@ -40,13 +40,13 @@ struct ClassParams {
     // log-probabilities
     float* logp;
     float* lse;
-    // what the preference loss keeps of a row: its largest logit and its sum, lp in fp64; rows outside [offsets[0], offsets[count]) do not count
+    // what the preference loss keeps of a row: its largest logit and its sum, lp in fp64; rows before and behind all sequences do not count
     float2* stat;
     double* logp64;
     float* coef;                 // set to 0
     const void* offsets;
     int wide_offsets;
-    long long offset_count;
+    long long sequences;
     // policy
     const float* adv;
     const float* old_logp;
@@ -273,6 +273,26 @@ __device__ __forceinline__ bool class_counts(const ClassParams& p, long long t, 
     return live;
 }
 
+// The rows that sequences hold: those from the first to the last that a sequence names whose own offsets neither fall nor leave the rows, by a warp.
+// With more than kSpanSequences all rows are taken (the coefficient of a row that no sequence names is 0 all the same).
+constexpr int kSpanSequences = 256;
+struct ClassSpan {
+    int from, to;
+    __device__ __forceinline__ bool has(long long t) const { return t >= from && t < to; }
+};
+__device__ __forceinline__ ClassSpan class_span(const ClassParams& p) {
+    if (!p.offsets || p.sequences > kSpanSequences) return {0, static_cast<int>(p.T)};
+    int from = static_cast<int>(p.T), to = 0;
+    for (int i = threadIdx.x & 31; i < p.sequences; i += 32) {
+        const long long a = load_any_id(p.offsets, p.wide_offsets, i), z = load_any_id(p.offsets, p.wide_offsets, i + 1);
+        if (a >= 0 && a < z && z <= p.T) {
+            from = min(from, static_cast<int>(a));
+            to = max(to, static_cast<int>(z));
+        }
+    }
+    return {__reduce_min_sync(0xffffffffu, from), __reduce_max_sync(0xffffffffu, to)};
+}
+
 __device__ __forceinline__ double warp_sum64(double v) {
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
@@ -323,11 +343,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_class_prep(const __grid_consta
     static_assert(kPrepThreads == 32 * 32, "a lane for every warp");
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     grid_dependency_release();
-    long long from = 0, to = p.T;
-    if (MODE == kClassLogp && p.offsets) {
-        from = load_any_id(p.offsets, p.wide_offsets, 0);
-        to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
-    }
+    const ClassSpan span = MODE == kClassLogp ? class_span(p) : ClassSpan{};
     double norm = 0.0;
     int before = 0;                                 // rows that count so far
     for (long long base = 0; base < p.T; base += kPrepThreads * kPrepItems) {
@@ -342,7 +358,7 @@ __global__ void __launch_bounds__(kPrepThreads) k_class_prep(const __grid_consta
                 long long target;
                 float w;
                 live = class_counts(p, t, MODE, &target, &w);
-                if (MODE == kClassLogp) live = live && t >= from && t < to;
+                if (MODE == kClassLogp) live = live && span.has(t);
                 if (live) norm += w;
                 else class_dead_row<MODE>(p, t);
             }
@@ -766,11 +782,7 @@ template <int MODE>
 __device__ __forceinline__ void class_list(const ClassParams& p, ClassList& list, int q, int Q, bool write) {
     constexpr int kWarps = Ring<MODE>::kThreads / 32, kTurns = (kListedRows + 32 * kWarps - 1) / (32 * kWarps);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, turns = (int(p.T) + 32 * kWarps - 1) / (32 * kWarps);
-    long long from = 0, to = p.T;
-    if (MODE == kClassLogp && p.offsets) {
-        from = load_any_id(p.offsets, p.wide_offsets, 0);
-        to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
-    }
+    const ClassSpan span = MODE == kClassLogp ? class_span(p) : ClassSpan{};
     unsigned int mask[kTurns];
     double norm = 0.0;
     int count = 0;
@@ -782,7 +794,7 @@ __device__ __forceinline__ void class_list(const ClassParams& p, ClassList& list
             long long target;
             float w;
             live = class_counts(p, t, MODE, &target, &w);
-            if (MODE == kClassLogp) live = live && t >= from && t < to;
+            if (MODE == kClassLogp) live = live && span.has(t);
             if (live) norm += w;
         }
         mask[j] = __ballot_sync(0xffffffffu, live);
@@ -1033,11 +1045,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (n == 0.0) n = p.listed ? sh.list.total : p.order ? p.prep->norm : warp_sum64(class_norm_part<MODE>(p, 0, p.T, lane, 32));
             inv = n == 0.0 ? 0.0 : 1.0 / n;
         }
-        long long from = 0, to = p.T;
-        if (MODE == kClassLogp && !known && p.offsets) {
-            from = load_any_id(p.offsets, p.wide_offsets, 0);
-            to = load_any_id(p.offsets, p.wide_offsets, p.offset_count);
-        }
+        const ClassSpan span = MODE == kClassLogp && !known ? class_span(p) : ClassSpan{0, static_cast<int>(p.T)};
         bool ok = true;
         auto wait = [&](uint64_t* bar, int parity) {
             if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag))) ok = false;
@@ -1066,7 +1074,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
             ClassInputs in{};
             bool counts = class_counts(p, t, MODE, &in.target, &in.w);
-            if (MODE == kClassLogp) counts = counts && t >= from && t < to;
+            if (MODE == kClassLogp) counts = counts && span.has(t);
             const bool edges = rank == 0 && lane < row.edges;
             const float edge = counts && edges ? load_local(row.x + row.edge(lane)) : 0.0f;
             if (MODE == kClassDistill && k + kNumberWarps < mine) class_top_ahead(p, row_of(k + kNumberWarps));
@@ -1181,6 +1189,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
         class_clear_marks(top);
     }
     grid_dependency_wait();
+    const ClassSpan span = MODE == kClassLogp ? class_span(p) : ClassSpan{};
     struct Row {
         ClassInputs in;
         uint4 raw[J];
@@ -1191,8 +1200,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
         r.counts = false;
         if (t >= p.T) return;
         r.counts = class_counts(p, t, MODE, &r.in.target, &r.in.w);
-        if (MODE == kClassLogp && p.offsets)
-            r.counts = r.counts && t >= load_any_id(p.offsets, p.wide_offsets, 0) && t < load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+        if (MODE == kClassLogp) r.counts = r.counts && span.has(t);
     };
     auto load = [&](long long t, Row& r) {          // its logits and what goes with them
         if (!r.counts) return;
@@ -1286,6 +1294,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, bundle_ctas(GRAD)) k_class_b
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane / W;
     const bool writes = (lane & (W - 1)) == 0;      // lanes part * W ... belong to row `first + part`
     grid_dependency_wait();
+    const ClassSpan span = MODE == kClassLogp ? class_span(p) : ClassSpan{};
     struct Look {
         long long target;
         float w;
@@ -1295,8 +1304,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, bundle_ctas(GRAD)) k_class_b
         Look l{0, 0.0f, false};
         if (t >= p.T) return l;
         l.counts = class_counts(p, t, MODE, &l.target, &l.w);
-        if (MODE == kClassLogp && p.offsets)
-            l.counts = l.counts && t >= load_any_id(p.offsets, p.wide_offsets, 0) && t < load_any_id(p.offsets, p.wide_offsets, p.offset_count);
+        if (MODE == kClassLogp) l.counts = l.counts && span.has(t);
         return l;
     };
     double sums[3] = {0.0, 0.0, 0.0};
@@ -1635,7 +1643,8 @@ __global__ void __launch_bounds__(kPairThreads) k_class_pair(const __grid_consta
         }
         __syncthreads();
         const float g = static_cast<float>((side ? -total[0] : total[0]) / rows[side]);
-        for (long long t = a + lane; t < z; t += kPairThreads / 2) p.coef[t] = g;
+        // (added to 0: falling offsets may put a row into several sequences)
+        for (long long t = a + lane; t < z; t += kPairThreads / 2) atomicAdd(p.coef + t, g);
     }
     if (tid == 0) {
         __threadfence();

@@ -426,7 +426,7 @@ int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
         p.coef = reinterpret_cast<float*>(scratch.data + stat + lp);
         p.offsets = d_offsets;
         p.wide_offsets = offset_bytes == 8;
-        p.offset_count = 2 * pairs;
+        p.sequences = 2 * pairs;
         const int r = launch_rows<E, kClassLogp, false>(ctx, p, at, scratch, st);
         if (r != LR_OK) return r;
     }

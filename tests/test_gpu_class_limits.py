@@ -168,3 +168,61 @@ def test_a_reference_that_is_far_off(ctx, dt, T, V):
     old = torch.full((T,), -400.0, device="cuda")
     d = ctx.policy_loss(x, y, torch.full((T,), -3.0, device="cuda"), old, ref, kl_coef=7.0, norm=1e-3, factor=100.0)[2]
     assert bool(torch.isfinite(d).all()) and bool((d[1, 5:9] == 0).all())
+
+
+# ---- offsets ---------------------------------------------------------------------------------------------
+
+def check_offsets(ctx, T, V, dt, o, average=False):
+    x, y = logits(T, V, dt), targets(T, V, drop=0.2)
+    junk = logits(T, V, dt, seed=7, spread=30.0)
+    ctx.pref_loss(junk, targets(T, V), torch.tensor([0, T // 2, T], device="cuda"))          # other values where the call works
+    bad = any(not 0 <= a <= z <= T for a, z in zip(o, o[1:]))
+    inside = torch.zeros(T, dtype=torch.bool, device="cuda")
+    for a, z in zip(o, o[1:]):
+        if 0 <= a <= z <= T:
+            inside[a:z] = True
+    x[~inside] = math.nan                           # rows outside all sequences do not count
+    clean = torch.where(inside[:, None], x.float(), 0.0).to(x.dtype)
+    loss, h, s, want, coef = pref_by_hand(clean, torch.where(inside, y, -100), o, None, None, 0.05, 0.0, 0.1, average)
+    got, gh, gs, d = ctx.pref_loss(x, y, torch.tensor(o, device="cuda"), beta=0.05, smoothing=0.1, average=average)
+    assert ctx.device_status() == (api.LR_ERR_VALUE if bad else 0)
+    L, P = errs(clean, 1.0)
+    most = max([z - a for a, z in zip(o, o[1:]) if 0 <= a <= z <= T], default=0)
+    s_err = L * (1 if average else most)
+    close(gs, s, s_err + 2 * U * s.abs())
+    close(gh, h, 0.1 * s_err + 4 * U * h.abs())
+    close(got, loss, 0.1 * s_err + 4 * U * loss.abs())
+    p = torch.softmax(clean.double(), 1)
+    c = coef.abs()[:, None]
+    # the coefficient of a row of two sequences is a difference: its parts are at most beta / P
+    part = (0.05 / (len(o) // 2)) * inside.double()[:, None]
+    close(d, want, part * (p + onehot(y, V)) * (0.1 * s_err + 12 * U) + c * (P * p + (L + 8 * U) * onehot(y, V)) + 1.01 * HALF[dt] * want.abs() + 1e-38)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", WAYS)
+@pytest.mark.parametrize("average", [False, True])
+def test_a_sequence_counts_by_its_own_offsets(ctx, dt, T, V, average):
+    """Only a sequence whose own offsets fall or leave the rows is empty."""
+    a, b, c = T // 5, T // 2, T - T // 4
+    for o in ([0, c, b], [b, 0, T], [0, b, T + 1], [-1, b, T], [0, c, 0], [a, b, c], [0, b, c, a, a], [c, a, b, T, b], [T, 0, 0, b, b]):
+        check_offsets(ctx, T, V, dt, o, average)
+
+
+@pytest.mark.parametrize("T,V", [(1300, 60), (900, 4200), (5000, 4200)])
+def test_many_sequences_with_rows_outside(ctx, T, V):
+    """More sequences than a warp looks through for the rows between the first and the last."""
+    n = 2 * 140
+    edges = torch.linspace(T // 6, T - T // 6, n + 1).long().tolist()
+    check_offsets(ctx, T, V, "f32", edges)
+    fall = list(edges)
+    fall[n], fall[3] = edges[n - 3], T + 5          # the last falls, two others leave the rows
+    check_offsets(ctx, T, V, "f32", fall)
+
+
+@pytest.mark.parametrize("T,V", WAYS)
+def test_rows_of_two_sequences(ctx, T, V):
+    """Where falling offsets make sequences overlap, a row counts in each of them."""
+    a, b, c = T // 5, T // 2, T - T // 4
+    for o in ([0, c, a, b, T], [0, T, 0, T, T], [a, T, 0, c, c]):
+        check_offsets(ctx, T, V, "f32", o)
