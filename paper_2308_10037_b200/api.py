@@ -576,8 +576,8 @@ class Context:
         """The C side's 0 is the sum of the weights that count."""
         if norm is None:
             return 0.0
-        if not float(norm) > 0.0:
-            raise ValueError("norm: expected a positive number, or None for the sum of the weights that count")
+        if not ctypes.c_float(float(norm)).value > 0.0:        # (as the library gets it)
+            raise ValueError("norm: expected a positive number of float32, or None for the sum of the weights that count")
         return float(norm)
 
     def logp(self, logits, targets, scale=1.0, ignore_id=-100):
