@@ -11,6 +11,5 @@ __all__ = ["datagen", "api", *_FROM_API]
 def __getattr__(name):
     if name in _FROM_API:
         from . import api
-        globals()[name] = value = getattr(api, name)    # (found without this function the next time)
-        return value
+        return getattr(api, name)
     raise AttributeError(name)
