@@ -649,7 +649,7 @@ int lr_pref_loss_bf16(lr_ctx* ctx, const uint16_t* d_logits, int64_t ld, int64_t
  *   row's loss = sum_k q_k (log q_k - lp_k),  lp over all V classes of the student;   gradient scale * ((sum_k q_k) p_v - q_v)
  * d_loss [1], d_row_kl NULL or [T] = the rows' losses.  Weights NULL or [T]; all rows of a weight other than 0 count in norm.  A class equal
  * to ignore_id, or whose teacher logit is -inf, is absent; one outside [0, V) is absent and sets the status word.  A row of which
- * all are absent has loss and gradient 0.  A class that is named twice has both weights.  K <= 1024.
+ * all are absent has loss and gradient 0, whatever its logits hold.  A class that is named twice has both weights.  K <= 1024.
  */
 typedef struct lr_distill_opt {
     int64_t ignore_id;

@@ -560,6 +560,9 @@ struct ClassInputs {
     float w, xy, adv, old_logp, ref_logp;
     ClassTopSum top;
 };
+// A row without a teacher has no gradient, whatever its logits hold (a NaN times 0 would be one)
+template <int MODE>
+__device__ __forceinline__ bool class_learns(const ClassInputs& in) { return MODE != kClassDistill || in.top.all != 0.0f; }
 template <int MODE, int U = 8, class E>
 __device__ __forceinline__ void class_inputs(const ClassParams& p, long long t, const E* row, const ClassTop& top, ClassInputs& in) {
     if (MODE == kClassDistill) {
@@ -771,7 +774,7 @@ struct Ring {
         uint64_t joined[2 * kRows];
         float2 cta_sum[2 * kRows][kMaxCluster];
         float2 warp_sum[kRows][kTeamWarps];         // largest logit, sum
-        float4 row[kRows];                          // factor, top, 1 where the row counts
+        float4 row[kRows];                          // factor, top, 1 where the row has a gradient
         ClassList list;
         int abort_word;
     };
@@ -992,7 +995,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             wait(sh.ready + at, (k / kRows) & 1);
             if (!ok) break;
             const float4 numbers = sh.row[at];
-            const bool counts = numbers.z != 0.0f;
+            const bool learns = numbers.z != 0.0f;
             const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-numbers.y, -numbers.y), factor2 = f32x2_pack(numbers.x, numbers.x);
             auto second = [&](int i, int from) {
                 const int first = (i * C + rank) * kStageGroups + in_team * kWarpGroups, left = row.groups - first;
@@ -1006,7 +1009,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                     for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(class_powers(G::pair(raw[j], e), top2, c2), factor2);
                     row.store_at(out + 32 * N * j, v);
                 };
-                if (!counts) {
+                if (!learns) {
                     const uint64_t zero[G::P] = {};
 #pragma unroll
                     for (int j = 0; j < J; ++j)
@@ -1099,8 +1102,9 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             ClassNumbers now{};
             ClassTerms terms;
             if (counts) now = class_numbers<MODE>(p, in, sum, inv, terms);
+            const bool learns = counts && class_learns<MODE>(in);
             if (lane == 0) {
-                if (GRAD) sh.row[at] = make_float4(now.factor, sum.top, counts ? 1.0f : 0.0f, 0.0f);
+                if (GRAD) sh.row[at] = make_float4(now.factor, sum.top, learns ? 1.0f : 0.0f, 0.0f);
                 mbar_arrive(sh.ready + at);
             }
             if (counts) class_account<MODE>(p, t, in, sum, terms, rank == 0 && lane == 0, sums);
@@ -1108,10 +1112,10 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (MODE == kClassDistill && C > 1 && k + kNumberWarps < mine) class_top_logits_ahead<E>(p, row_of(k + kNumberWarps), rank);
             if (!GRAD) continue;
             zeros(k);
-            if (edges) store_from_float(row.dx + row.edge(lane), counts ? class_power(edge, sum.top, p.c) * now.factor : 0.0f);
+            if (edges) store_from_float(row.dx + row.edge(lane), learns ? class_power(edge, sum.top, p.c) * now.factor : 0.0f);
             // the values at the targets replace what the passes have written, in this CTA's stages
             if (!wait(sh.written + at, parity)) break;
-            if (!counts) continue;
+            if (!learns) continue;
             auto here = [&](int column) {
                 const int g = (column - row.head) / N;
                 return column < row.head || g >= row.groups ? rank == 0 : (g / kStageGroups & (C - 1)) == rank;
@@ -1225,6 +1229,11 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
             look(t + 2 * step, after);
         }
         const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
+        auto zeros = [&] {
+            const uint64_t zero[G::P] = {};
+            for (int g = lane; g < row.groups; g += 32) row.store(g, zero);
+            if (lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
+        };
         if (now.counts) {
             if (MODE == kClassDistill) class_inputs<MODE, 2>(p, t, row.x, top, now.in);
             ClassSum sum;
@@ -1237,7 +1246,9 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
             ClassTerms terms;
             const ClassNumbers numbers = class_numbers<MODE>(p, now.in, sum, inv, terms);
             class_account<MODE>(p, t, now.in, sum, terms, lane == 0, sums);
-            if (GRAD) {
+            if (GRAD && !class_learns<MODE>(now.in)) {
+                zeros();
+            } else if (GRAD) {
                 const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-sum.top, -sum.top), factor2 = f32x2_pack(numbers.factor, numbers.factor);
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
@@ -1259,11 +1270,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
                 }
             }
         } else {
-            if (GRAD) {
-                const uint64_t zero[G::P] = {};
-                for (int g = lane; g < row.groups; g += 32) row.store(g, zero);
-                if (lane < row.edges) store_from_float(row.dx + row.edge(lane), 0.0f);
-            }
+            if (GRAD) zeros();
             if (lane == 0) class_dead_row<MODE>(p, t);
         }
         if (!kAhead) {

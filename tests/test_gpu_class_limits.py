@@ -49,6 +49,29 @@ def test_a_class_of_the_vocabulary_that_is_ignored(ctx, dt, T, V):
     assert ctx.device_status() == 0
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", WAYS)
+def test_rows_without_a_teacher(ctx, dt, T, V):
+    """A row of which all classes are absent has loss and gradient 0, whatever its logits hold; its neighbours do not see it."""
+    K = 5
+    x, t = logits(T, V, dt), rnd(T, K, seed=2)
+    ids = torch.randint(0, V, (T, K), generator=gen(3), device="cuda")
+    none = torch.zeros(T, dtype=torch.bool, device="cuda")
+    none[::3] = True
+    ids[none] = -1
+    ids[0], t[0] = 1, -math.inf                     # the other way to be absent
+    want = ctx.distill_loss(x, ids, t)
+    for junk in (math.nan, math.inf, -math.inf):
+        xx = x.clone()
+        xx[none] = junk
+        if T > 3:
+            xx[3] = x[3]
+            xx[3, V // 2] = junk
+        got = ctx.distill_loss(xx, ids, t)
+        assert bool((got[2][none] == 0).all()) and bool((got[1][none] == 0).all())
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 # ---- an infinite log-probability -------------------------------------------------------------------------
 
 def pref_by_hand(x, y, o, ref, w, beta, margin, smoothing, average=False, scale=1.0):
