@@ -85,6 +85,17 @@ __device__ __forceinline__ float exp2_fast(float v) {               // 2^v, rela
     return r;
 }
 
+// A log-sum-exp in units of the logits, lse / scale, as high + low / c: high is the nearest finite fp32 (lse / scale may be past them where scale is
+// tiny), low what that leaves of the exponent.
+struct ClassBase {
+    float high, low;
+};
+__device__ __forceinline__ ClassBase class_base(float lse, float scale) {
+    const double own = static_cast<double>(lse) / scale;
+    const float near = static_cast<float>(own), high = near > 3.4028234e38f ? 3.4028234e38f : near < -3.4028234e38f ? -3.4028234e38f : near;
+    return {high, static_cast<float>((own - static_cast<double>(high)) * scale * 1.4426950408889634)};
+}
+
 // Two fp32 values in one 64-bit register (see f32x2_fma)
 __device__ __forceinline__ uint64_t f32x2_add(uint64_t a, uint64_t b) {
     uint64_t d;
@@ -486,7 +497,7 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
     const int lane = threadIdx.x & 31;
     ClassTopSum r{0.0f, 0.0f, 0.0f, -INFINITY, false};
     float largest = -INFINITY;
-    const double own = p.teacher_lse ? static_cast<double>(__ldg(p.teacher_lse + t)) / p.scale : 0.0;
+    const ClassBase own = p.teacher_lse ? class_base(__ldg(p.teacher_lse + t), p.scale) : ClassBase{};
     for (int j0 = 0; j0 < p.K; j0 += 32 * U) {
         ClassEntry e[U];
         int id[U];
@@ -526,8 +537,7 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
     r.near = warp_max(r.near);
     if (r.near == -INFINITY) r.near = 0.0f;
     // base is the largest v, or the teacher's own lse / scale in two parts
-    const float high = p.teacher_lse ? static_cast<float>(own) : largest == -INFINITY ? 0.0f : largest,
-                low = p.teacher_lse ? static_cast<float>((own - static_cast<double>(high)) * p.c) : 0.0f;
+    const float high = p.teacher_lse ? own.high : largest == -INFINITY ? 0.0f : largest, low = own.low;
     for (int j = lane; j < p.K; j += 32) {
         const float a = (top.q[j] - high) * p.c - low;
         const float e = top.id[j] >= 0 ? exp2f(a) : 0.0f;
@@ -1519,9 +1529,9 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
             base = now.stat.x;
             k = -gt / now.stat.y;
         } else {                                    // lse / scale in place of the largest logit, the part below fp32 put into the factor
-            const double own = static_cast<double>(now.stat.x) / p.scale;
-            base = static_cast<float>(own);
-            k = -gt * exp2_fast(static_cast<float>((static_cast<double>(base) - own) * p.c));
+            const ClassBase own = class_base(now.stat.x, p.scale);
+            base = own.high;
+            k = -gt * exp2_fast(-own.low);
         }
         const int where = static_cast<int>(now.target) - row.head;
         const uint64_t c2 = f32x2_pack(p.c, p.c), base2 = f32x2_pack(-base, -base), k2 = f32x2_pack(k, k);

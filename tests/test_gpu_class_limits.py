@@ -249,3 +249,30 @@ def test_rows_of_two_sequences(ctx, T, V):
     a, b, c = T // 5, T // 2, T - T // 4
     for o in ([0, c, a, b, T], [0, T, 0, T, T], [a, T, 0, c, c]):
         check_offsets(ctx, T, V, "f32", o)
+
+
+# ---- numbers that fp32 does not hold ---------------------------------------------------------------------
+
+@pytest.mark.parametrize("scale", [1e-38, 3e-39, 1e-41])
+@pytest.mark.parametrize("V", [50, 5000, 200003])
+def test_scales_that_make_every_class_alike(ctx, scale, V):
+    """lse / scale is past fp32's largest number: the gradient is that of equal classes all the same, and so is a teacher's q."""
+    T, K = 3, 4
+    x, y = logits(T, V, "f32"), targets(T, V)
+    got, lse = ctx.logp(x, y, scale=scale)
+    close(got, torch.full((T,), -math.log(V), device="cuda"), 110 * U + U * math.log(V))
+    g = rnd(T, seed=1) * 1e37
+    s = float(torch.tensor(scale, dtype=torch.float32))
+    gt = (g.double() * s)[:, None]
+    p = torch.exp(x.double() * s - lse.double()[:, None])
+    want = gt * (onehot(y, V) - p)
+    d = ctx.logp_grad(x, y, lse, g, scale=scale)
+    # the exponent is at most log2(V) < 18, and rounded like every term's (3 * 18 u); (x - 2^128) c is off by 2^128 times half a step of c, which below
+    # fp32's normal numbers is 2^-150: 2^-22 = 4 u
+    close(d, want, gt.abs() * ((54 + 4 + 115) * U * p + 8 * U * onehot(y, V)) + 2e-38 + U * want.abs())
+    t = rnd(T, K, seed=2)
+    ids = torch.stack([torch.arange(K, device="cuda")] * T)
+    tlse = torch.full((T,), 9.0, device="cuda")
+    kl = ctx.distill_loss(x, ids, t, tlse, scale=scale)[1]
+    q = torch.exp(t.double() * s - 9.0)
+    close(kl, (q * (math.log(V) - 9.0)).sum(1), float(q.sum(1).max()) * (110 + 60) * U * (9.0 + math.log(V)))
