@@ -1099,6 +1099,10 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (edges) sum.add(edge, p.c);
             sum.over_warp(p.c);
             if (C > 1) {
+                // The gradient may replace the logits, and a CTA that has all sums writes over the target's: what this one reads of the row has to be
+                // here before its sum goes out.  Edges are in the sum and a teacher's classes in shared memory; the target's logit is
+                // made part of what is sent (where it is no number, neither is the sum).
+                if (MODE == kClassPolicy && in.xy != in.xy) sum.s = in.xy;
                 const int at2 = k % (2 * kRows);
                 if (lane == 0) mbar_arrive_expect_tx(sh.joined + at2, 8 * C);
                 __syncwarp();

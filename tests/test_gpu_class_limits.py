@@ -276,3 +276,28 @@ def test_scales_that_make_every_class_alike(ctx, scale, V):
     kl = ctx.distill_loss(x, ids, t, tlse, scale=scale)[1]
     q = torch.exp(t.double() * s - 9.0)
     close(kl, (q * (math.log(V) - 9.0)).sum(1), float(q.sum(1).max()) * (110 + 60) * U * (9.0 + math.log(V)))
+
+
+# ---- the gradient in place of the logits -----------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(3, 50021), (20, 131072), (60, 40000), (300, 128000)])
+def test_rows_of_a_cluster_in_place(ctx, dt, T, V):
+    """CTAs that share a row read each other's part of it only as long as it holds logits: the same bits in place and beside, targets at
+    the ends of the row, in its middle and in its unaligned edges."""
+    x = strided(logits(T, V, dt), 3, 1)
+    y = targets(T, V, drop=0.1)
+    y[::4], y[1::4] = 0, V - 1
+    adv, old = rnd(T, seed=1), ctx.logp(x, y)[0] + 0.1
+    ids = torch.randint(0, V, (T, 40), generator=gen(5), device="cuda")
+    ids[:, 0], ids[:, 1] = 0, V - 1
+    t = rnd(T, 40, seed=6)
+    stats, lp, d = ctx.policy_loss(x, y, adv, old, clip_low=1.0, clip_high=9.0)
+    loss, kl, dd = ctx.distill_loss(x, ids, t)
+    for _ in range(10):
+        mine = strided(x, 3, 1)
+        got = ctx.policy_loss(mine, y, adv, old, clip_low=1.0, clip_high=9.0, out=mine)
+        assert torch.equal(got[0], stats) and torch.equal(got[1], lp) and torch.equal(mine, d)
+        mine = strided(x, 3, 1)
+        got = ctx.distill_loss(mine, ids, t, out=mine)
+        assert torch.equal(got[0], loss) and torch.equal(got[1], kl) and torch.equal(mine, dd)
