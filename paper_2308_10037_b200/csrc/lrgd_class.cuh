@@ -32,6 +32,7 @@ struct ClassParams {
     int wide_ids;
     long long ignore;
     float c;                     // scale * log2(e)
+    double c64;
     float scale;
     const float* weights;        // nullable [T]
     void* dx;
@@ -90,10 +91,10 @@ __device__ __forceinline__ float exp2_fast(float v) {               // 2^v, rela
 struct ClassBase {
     float high, low;
 };
-__device__ __forceinline__ ClassBase class_base(float lse, float scale) {
+__device__ __forceinline__ ClassBase class_base(float lse, float scale, double c64) {
     const double own = static_cast<double>(lse) / scale;
-    const float near = static_cast<float>(own), high = near > 3.4028234e38f ? 3.4028234e38f : near < -3.4028234e38f ? -3.4028234e38f : near;
-    return {high, static_cast<float>((own - static_cast<double>(high)) * scale * 1.4426950408889634)};
+    const float high = fminf(fmaxf(static_cast<float>(own), -3.4028234e38f), 3.4028234e38f);       // (a NaN is in low)
+    return {high, static_cast<float>((own - static_cast<double>(high)) * c64)};
 }
 
 // Two fp32 values in one 64-bit register (see f32x2_fma)
@@ -284,24 +285,45 @@ __device__ __forceinline__ bool class_counts(const ClassParams& p, long long t, 
     return live;
 }
 
-// The rows that sequences hold: those from the first to the last that a sequence names whose own offsets neither fall nor leave the rows, by a warp.
-// With more than kSpanSequences all rows are taken (the coefficient of a row that no sequence names is 0 all the same).
+// The rows that sequences hold: those from the first to the last that a sequence names whose own offsets neither fall nor leave the rows.  With more
+// than kSpanSequences all rows are taken (the coefficient of a row that no sequence names is 0 all the same).
 constexpr int kSpanSequences = 256;
 struct ClassSpan {
     int from, to;
     __device__ __forceinline__ bool has(long long t) const { return t >= from && t < to; }
-};
-__device__ __forceinline__ ClassSpan class_span(const ClassParams& p) {
-    if (!p.offsets || p.sequences > kSpanSequences) return {0, static_cast<int>(p.T)};
-    int from = static_cast<int>(p.T), to = 0;
-    for (int i = threadIdx.x & 31; i < p.sequences; i += 32) {
+    __device__ __forceinline__ void join(const ClassParams& p, int i) {         // sequence i
         const long long a = load_any_id(p.offsets, p.wide_offsets, i), z = load_any_id(p.offsets, p.wide_offsets, i + 1);
         if (a >= 0 && a < z && z <= p.T) {
             from = min(from, static_cast<int>(a));
             to = max(to, static_cast<int>(z));
         }
     }
-    return {__reduce_min_sync(0xffffffffu, from), __reduce_max_sync(0xffffffffu, to)};
+    __device__ __forceinline__ void over_warp() {
+        from = __reduce_min_sync(0xffffffffu, from);
+        to = __reduce_max_sync(0xffffffffu, to);
+    }
+};
+// (by one warp)
+__device__ __forceinline__ ClassSpan class_warp_span(const ClassParams& p) {
+    if (!p.offsets || p.sequences > kSpanSequences) return {0, static_cast<int>(p.T)};
+    ClassSpan span{static_cast<int>(p.T), 0};
+    for (int i = threadIdx.x & 31; i < p.sequences; i += 32) span.join(p, i);
+    span.over_warp();
+    return span;
+}
+// (by all threads of a CTA, a sequence each: 100 pairs in front of 6101 rows by a warp alone take 4 us more)
+__device__ __forceinline__ ClassSpan class_span(const ClassParams& p) {
+    if (!p.offsets || p.sequences > kSpanSequences) return {0, static_cast<int>(p.T)};
+    constexpr int kWarps = kSpanSequences / 32;
+    __shared__ ClassSpan part[kWarps];
+    ClassSpan span{static_cast<int>(p.T), 0};
+    if (threadIdx.x < p.sequences) span.join(p, threadIdx.x);
+    span.over_warp();
+    if (threadIdx.x < kSpanSequences && (threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = span;
+    __syncthreads();
+    span = part[threadIdx.x & (kWarps - 1)];
+    span.over_warp();
+    return span;
 }
 
 __device__ __forceinline__ double warp_sum64(double v) {
@@ -497,7 +519,7 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
     const int lane = threadIdx.x & 31;
     ClassTopSum r{0.0f, 0.0f, 0.0f, -INFINITY, false};
     float largest = -INFINITY;
-    const ClassBase own = p.teacher_lse ? class_base(__ldg(p.teacher_lse + t), p.scale) : ClassBase{};
+    const float own = p.teacher_lse ? __ldg(p.teacher_lse + t) : 0.0f;
     for (int j0 = 0; j0 < p.K; j0 += 32 * U) {
         ClassEntry e[U];
         int id[U];
@@ -537,7 +559,12 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
     r.near = warp_max(r.near);
     if (r.near == -INFINITY) r.near = 0.0f;
     // base is the largest v, or the teacher's own lse / scale in two parts
-    const float high = p.teacher_lse ? own.high : largest == -INFINITY ? 0.0f : largest, low = own.low;
+    float high = largest == -INFINITY ? 0.0f : largest, low = 0.0f;
+    if (p.teacher_lse) {
+        const ClassBase base = class_base(own, p.scale, p.c64);
+        high = base.high;
+        low = base.low;
+    }
     for (int j = lane; j < p.K; j += 32) {
         const float a = (top.q[j] - high) * p.c - low;
         const float e = top.id[j] >= 0 ? exp2f(a) : 0.0f;
@@ -570,9 +597,6 @@ struct ClassInputs {
     float w, xy, adv, old_logp, ref_logp;
     ClassTopSum top;
 };
-// A row without a teacher has no gradient, whatever its logits hold (a NaN times 0 would be one)
-template <int MODE>
-__device__ __forceinline__ bool class_learns(const ClassInputs& in) { return MODE != kClassDistill || in.top.all != 0.0f; }
 template <int MODE, int U = 8, class E>
 __device__ __forceinline__ void class_inputs(const ClassParams& p, long long t, const E* row, const ClassTop& top, ClassInputs& in) {
     if (MODE == kClassDistill) {
@@ -599,7 +623,11 @@ __device__ __forceinline__ float class_kl(float d) {
 }
 // Half of fp32's range at most (a NaN stays one): a difference of two such numbers is finite, and a row's factor times a power that is 0 is 0 also
 // where the formula is past fp32.
-__device__ __forceinline__ float class_held(float v) { return v > 1.69e38f ? 1.69e38f : v < -1.69e38f ? -1.69e38f : v; }
+__device__ __forceinline__ float class_held(float v) {
+    asm("min.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(1.69e38f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(v) : "f"(-1.69e38f));
+    return v;
+}
 // ... and what of it is written down afterwards
 struct ClassTerms {
     double lp, lse;
@@ -612,7 +640,7 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
     const double log_s = class_log(sum.s);
     ClassNumbers r{};
     terms = ClassTerms{0.0, static_cast<double>(sum.top) * p.scale + log_s, 0.0f, 0.0f, 0.0f};
-    const float gain = class_held(static_cast<float>(in.w * inv * p.factor * p.scale));
+    const float gain = static_cast<float>(in.w * inv * p.factor * p.scale);
     if (MODE == kClassDistill) {
         // with the teacher's own normalisation log q is smaller by log(all)
         const float all = in.top.all, one = p.teacher_lse || all == 0.0f ? 1.0f : 1.0f / all, mass = p.teacher_lse || all == 0.0f ? all : 1.0f;
@@ -784,7 +812,7 @@ struct Ring {
         uint64_t joined[2 * kRows];
         float2 cta_sum[2 * kRows][kMaxCluster];
         float2 warp_sum[kRows][kTeamWarps];         // largest logit, sum
-        float4 row[kRows];                          // factor, top, 1 where the row has a gradient
+        float2 row[kRows];                          // factor, top
         ClassList list;
         int abort_word;
     };
@@ -1004,8 +1032,8 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (!GRAD) continue;
             wait(sh.ready + at, (k / kRows) & 1);
             if (!ok) break;
-            const float4 numbers = sh.row[at];
-            const bool learns = numbers.z != 0.0f;
+            const float2 numbers = sh.row[at];
+            const bool zero_row = numbers.x == 0.0f;       // it does not count, or has no teacher: whatever its logits hold
             const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-numbers.y, -numbers.y), factor2 = f32x2_pack(numbers.x, numbers.x);
             auto second = [&](int i, int from) {
                 const int first = (i * C + rank) * kStageGroups + in_team * kWarpGroups, left = row.groups - first;
@@ -1019,7 +1047,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                     for (int e = 0; e < G::P; ++e) v[e] = f32x2_mul(class_powers(G::pair(raw[j], e), top2, c2), factor2);
                     row.store_at(out + 32 * N * j, v);
                 };
-                if (!learns) {
+                if (zero_row) {
                     const uint64_t zero[G::P] = {};
 #pragma unroll
                     for (int j = 0; j < J; ++j)
@@ -1058,7 +1086,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (n == 0.0) n = p.listed ? sh.list.total : p.order ? p.prep->norm : warp_sum64(class_norm_part<MODE>(p, 0, p.T, lane, 32));
             inv = n == 0.0 ? 0.0 : 1.0 / n;
         }
-        const ClassSpan span = MODE == kClassLogp && !known ? class_span(p) : ClassSpan{0, static_cast<int>(p.T)};
+        const ClassSpan span = MODE == kClassLogp && !known ? class_warp_span(p) : ClassSpan{};
         bool ok = true;
         auto wait = [&](uint64_t* bar, int parity) {
             if (!__all_sync(0xffffffffu, mbar_wait_bounded(bar, parity, abort_flag))) ok = false;
@@ -1087,7 +1115,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             const ClassRow<E> row(p.x, p.ld, p.dx, p.ld_d, t, p.V);
             ClassInputs in{};
             bool counts = class_counts(p, t, MODE, &in.target, &in.w);
-            if (MODE == kClassLogp) counts = counts && span.has(t);
+            if (MODE == kClassLogp && !known) counts = counts && span.has(t);
             const bool edges = rank == 0 && lane < row.edges;
             const float edge = counts && edges ? load_local(row.x + row.edge(lane)) : 0.0f;
             if (MODE == kClassDistill && k + kNumberWarps < mine) class_top_ahead(p, row_of(k + kNumberWarps));
@@ -1116,9 +1144,8 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             ClassNumbers now{};
             ClassTerms terms;
             if (counts) now = class_numbers<MODE>(p, in, sum, inv, terms);
-            const bool learns = counts && class_learns<MODE>(in);
             if (lane == 0) {
-                if (GRAD) sh.row[at] = make_float4(now.factor, sum.top, learns ? 1.0f : 0.0f, 0.0f);
+                if (GRAD) sh.row[at] = make_float2(now.factor, sum.top);
                 mbar_arrive(sh.ready + at);
             }
             if (counts) class_account<MODE>(p, t, in, sum, terms, rank == 0 && lane == 0, sums);
@@ -1126,10 +1153,10 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (MODE == kClassDistill && C > 1 && k + kNumberWarps < mine) class_top_logits_ahead<E>(p, row_of(k + kNumberWarps), rank);
             if (!GRAD) continue;
             zeros(k);
-            if (edges) store_from_float(row.dx + row.edge(lane), learns ? class_power(edge, sum.top, p.c) * now.factor : 0.0f);
+            if (edges) store_from_float(row.dx + row.edge(lane), now.factor != 0.0f ? class_power(edge, sum.top, p.c) * now.factor : 0.0f);
             // the values at the targets replace what the passes have written, in this CTA's stages
             if (!wait(sh.written + at, parity)) break;
-            if (!learns) continue;
+            if (!counts) continue;
             auto here = [&](int column) {
                 const int g = (column - row.head) / N;
                 return column < row.head || g >= row.groups ? rank == 0 : (g / kStageGroups & (C - 1)) == rank;
@@ -1207,7 +1234,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
         class_clear_marks(top);
     }
     grid_dependency_wait();
-    const ClassSpan span = MODE == kClassLogp ? class_span(p) : ClassSpan{};
+    const ClassSpan span = MODE == kClassLogp ? class_warp_span(p) : ClassSpan{};
     struct Row {
         ClassInputs in;
         uint4 raw[J];
@@ -1260,8 +1287,8 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
             ClassTerms terms;
             const ClassNumbers numbers = class_numbers<MODE>(p, now.in, sum, inv, terms);
             class_account<MODE>(p, t, now.in, sum, terms, lane == 0, sums);
-            if (GRAD && !class_learns<MODE>(now.in)) {
-                zeros();
+            if (GRAD && MODE == kClassDistill && numbers.factor == 0.0f) {
+                zeros();                            // without a teacher, whatever the logits hold
             } else if (GRAD) {
                 const uint64_t c2 = f32x2_pack(p.c, p.c), top2 = f32x2_pack(-sum.top, -sum.top), factor2 = f32x2_pack(numbers.factor, numbers.factor);
 #pragma unroll
@@ -1274,6 +1301,8 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
                     }
                 }
                 if (lane < row.edges) store_from_float(row.dx + row.edge(lane), class_power(now.edge, sum.top, p.c) * numbers.factor);
+            }
+            if (GRAD) {
                 __syncwarp();                       // the targets' values replace what was just written
                 if (MODE == kClassPolicy) {
                     if (lane == 0) store_from_float(row.dx + now.in.target, numbers.at);
@@ -1315,7 +1344,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, bundle_ctas(GRAD)) k_class_b
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, part = lane / W;
     const bool writes = (lane & (W - 1)) == 0;      // lanes part * W ... belong to row `first + part`
     grid_dependency_wait();
-    const ClassSpan span = MODE == kClassLogp ? class_span(p) : ClassSpan{};
+    const ClassSpan span = MODE == kClassLogp ? class_warp_span(p) : ClassSpan{};
     struct Look {
         long long target;
         float w;
@@ -1453,6 +1482,7 @@ struct ClassGradParams {
     int wide_ids;
     long long ignore;
     float c;
+    double c64;
     float scale;
     const float* lse;
     const float2* stat;
@@ -1533,7 +1563,7 @@ __global__ void __launch_bounds__(kClassGradThreads) k_class_grad(const __grid_c
             base = now.stat.x;
             k = -gt / now.stat.y;
         } else {                                    // lse / scale in place of the largest logit, the part below fp32 put into the factor
-            const ClassBase own = class_base(now.stat.x, p.scale);
+            const ClassBase own = class_base(now.stat.x, p.scale, p.c64);
             base = own.high;
             k = -gt * exp2_fast(-own.low);
         }

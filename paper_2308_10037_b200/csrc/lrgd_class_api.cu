@@ -24,7 +24,8 @@ constexpr int64_t kMaxPairs = int64_t(1) << 24;
 
 size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
-float class_c(float scale) { return float(double(scale) * 1.4426950408889634074); }        // scale * log2(e)
+double class_c64(float scale) { return double(scale) * 1.4426950408889634074; }            // scale * log2(e)
+float class_c(float scale) { return float(class_c64(scale)); }
 
 int check_rows(int64_t T, int32_t V, int64_t ld, int32_t id_bytes, float scale) {
     if (T < 0 || T > kMaxRows || V < 1 || V > kMaxClasses || ld < V || ld > kMaxPitch) return LR_ERR_SHAPE;
@@ -227,6 +228,7 @@ ClassParams row_params(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, in
     p.ignore = ignore;
     p.scale = scale;
     p.c = class_c(scale);
+    p.c64 = class_c64(scale);
     p.status = ctx->d_status + 1;
     return p;
 }
@@ -291,6 +293,7 @@ int logp_grad_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_
     p.ignore = ignore_id;
     p.scale = scale;
     p.c = class_c(scale);
+    p.c64 = class_c64(scale);
     p.lse = d_lse;
     p.g = d_dlogp;
     p.dx = d_dlogits;
@@ -467,6 +470,7 @@ int pref_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V, 
     d.ignore = opt->ignore_id;
     d.scale = opt->scale;
     d.c = class_c(opt->scale);
+    d.c64 = class_c64(opt->scale);
     d.stat = reinterpret_cast<const float2*>(scratch.data + rows);
     d.g = q.coef;
     d.dx = d_dlogits;
