@@ -301,3 +301,37 @@ def test_rows_of_a_cluster_in_place(ctx, dt, T, V):
         mine = strided(x, 3, 1)
         got = ctx.distill_loss(mine, ids, t, out=mine)
         assert torch.equal(got[0], loss) and torch.equal(got[1], kl) and torch.equal(mine, dd)
+
+
+# ---- errors that add up ----------------------------------------------------------------------------------
+
+def nearly_exact_scale():
+    """A scale near 1 whose product with log2(e) fp32 holds to 1e-10: the exponents are then off by their own rounding alone."""
+    s = torch.arange(-2 ** 14, 2 ** 14, dtype=torch.float64) * 2.0 ** -23 + 1.0
+    c = s * math.log2(math.e)
+    off = (c.float().double() / c - 1).abs()
+    assert float(off.min()) < 1e-10
+    return float(s[off.argmin()])
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [500, 4096, 9001])
+def test_errors_of_a_long_sequence_cancel(ctx, dt, V):
+    """The mean signed error of lp over many rows, of terms of every size and of equal ones: an error that all rows share would add up over a
+    sequence.  lp is rounded to half a step of 2^-20 (3e-7 in the mean square), its sum and logarithm less: 4 / sqrt(8192) of it is 1.3e-8; the
+    powers' mean error is 3e-9, and 3e-8 in the few terms above 1/2; the scale's 1e-9.  3e-8 in all; an uncorrected power gives 5e-8."""
+    T, scale = 8192, nearly_exact_scale()
+    y = torch.randint(0, V, (T,), generator=gen(1), device="cuda")
+    kinds = {"random": 2.5 * rnd(T, V, seed=2), "near one another": 0.3 * rnd(T, V, seed=5), "of one value": rnd(T, 1, seed=3).expand(T, V).contiguous()}
+    kinds["ties beside masked classes"] = kinds["of one value"].clone()
+    count = torch.randint(2, V + 1, (T, 1), generator=gen(4), device="cuda")
+    kinds["ties beside masked classes"][torch.arange(V, device="cuda") >= count] = -math.inf
+    for name, x in kinds.items():
+        x = x.to(DT[dt])
+        at = y if name in ("random", "near one another") else y % 2
+        want = torch.cat([torch.log_softmax(p.double() * scale, 1) for p in x.split(1024)])[torch.arange(T, device="cuda"), at]
+        off = float((ctx.logp(x, at, scale=scale)[0].double() - want).mean())
+        if name == "of one value":                  # (one number for all rows: its own rounding)
+            assert abs(off) <= 0.5 * 2.0 ** -20 + 1e-7
+        else:
+            assert abs(off) <= 3e-8, (name, off)
