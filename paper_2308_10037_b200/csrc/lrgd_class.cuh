@@ -23,6 +23,11 @@ constexpr double kLn2 = 0.693147180559945309417232121458;
 
 enum ClassMode { kClassLogp = 0, kClassPolicy = 1, kClassDistill = 2 };
 
+struct ClassScale {              // scale * log2(e)
+    float c;                     // to the nearest
+    float down, rest;            // in two parts; rest is above 0, so that -inf stays -inf in the product with each
+};
+
 struct ClassParams {
     const void* x;
     long long ld;
@@ -31,7 +36,8 @@ struct ClassParams {
     const void* ids;             // targets [T]; distillation: the teacher's classes [T][K]
     int wide_ids;
     long long ignore;
-    float c;                     // scale * log2(e)
+    ClassScale cs;               // scale * log2(e) ...
+    float c;                     // ... to the nearest
     double c64;
     float scale;
     const float* weights;        // nullable [T]
@@ -114,16 +120,35 @@ __device__ __forceinline__ uint64_t f32x2_mul(uint64_t a, uint64_t b) {
 // and rows of one value are exact.  A row's many terms are raised alike (those above 1/2 are few, and come out 3e-8 too large).
 constexpr float kPowerLift = 7e-8f, kPowerLiftHigh = 3e-8f, kPowerLiftRaise = 4e-8f;
 __device__ __forceinline__ float class_power(float x, float top, float c) { return exp2_fast(fmaf(x - top, c, kPowerLift)); }
-// What carries a sum of terms up to `top` to the larger maximum `most`: often above 1/2, and several of them one after the other, so both kinds are told
-// apart (rows of 32003 logits with a spread of 0.3: the mean error of lp 1.8e-8 at most, 8e-8 with 7e-8 for all).  Within a thread the running maximum
-// takes a number between the two (policy loss 8192 x 128000: 661 us; told apart there too: 679).
-__device__ __forceinline__ float class_carry(float top, float most, float c) {
-    return exp2_fast(fmaf(top - most, c, (top - most) * c > -1.0f ? kPowerLiftHigh : kPowerLift));
-}
 __device__ __forceinline__ uint64_t class_powers(uint64_t x, uint64_t minus_top, uint64_t c) {
     float lo, hi;
     f32x2_unpack(f32x2_fma(f32x2_add(x, minus_top), c, f32x2_pack(kPowerLift, kPowerLift)), lo, hi);
     return f32x2_pack(exp2_fast(lo), exp2_fast(hi));
+}
+// The exponent of a difference d.  WHOLE: with what fp32 leaves of scale * log2(e), 1.3e-8 of it at a scale of 1, which is the same for all rows: 5e-8 in
+// lp where the largest logit is 10 above most.  An instruction more per two logits, so only for log-probabilities that are added up: they wait
+// for HBM anyway (the policy loss does not: 8192 x 128000 676 us instead of 661).
+template <bool WHOLE>
+__device__ __forceinline__ float class_exponent(float d, ClassScale c, float lift) {
+    return WHOLE ? fmaf(d, c.down, fmaf(d, c.rest, lift)) : fmaf(d, c.c, lift);
+}
+template <bool WHOLE>
+__device__ __forceinline__ uint64_t class_powers(uint64_t x, uint64_t minus_top, ClassScale c) {
+    if constexpr (!WHOLE) {
+        return class_powers(x, minus_top, f32x2_pack(c.c, c.c));
+    } else {
+        float lo, hi;
+        const uint64_t d = f32x2_add(x, minus_top);
+        f32x2_unpack(f32x2_fma(d, f32x2_pack(c.down, c.down), f32x2_fma(d, f32x2_pack(c.rest, c.rest), f32x2_pack(kPowerLift, kPowerLift))), lo, hi);
+        return f32x2_pack(exp2_fast(lo), exp2_fast(hi));
+    }
+}
+// What carries a sum of terms up to `top` to the larger maximum `most`: often above 1/2, and several of them one after the other, so both kinds are told
+// apart (rows of 32003 logits with a spread of 0.3: the mean error of lp 2e-8 at most, 8e-8 with 7e-8 for all).  Within a thread the running maximum
+// takes a number between the two (policy loss 8192 x 128000: 661 us; told apart there too: 679).
+template <bool WHOLE>
+__device__ __forceinline__ float class_carry(float top, float most, ClassScale c) {
+    return exp2_fast(class_exponent<WHOLE>(top - most, c, (top - most) * c.c > -1.0f ? kPowerLiftHigh : kPowerLift));
 }
 
 // 16 bytes of a row
@@ -230,21 +255,23 @@ __device__ __forceinline__ float warp_largest(float v) {
 struct ClassSum {
     float top = -INFINITY, s = 0.0f;
     // room for terms up to t; false where nothing finite has come yet
-    __device__ __forceinline__ bool raise(float t, float c) {
+    template <bool WHOLE>
+    __device__ __forceinline__ bool raise(float t, ClassScale c) {
         if (t > top) {
-            s *= exp2_fast(fmaf(top - t, c, kPowerLiftRaise));
+            s *= exp2_fast(class_exponent<WHOLE>(top - t, c, kPowerLiftRaise));
             top = t;
         }
         return top != -INFINITY;
     }
-    __device__ __forceinline__ void add(float v, float c) {
-        if (raise(v, c)) s += class_power(v, top, c);
+    template <bool WHOLE>
+    __device__ __forceinline__ void add(float v, ClassScale c) {
+        if (raise<WHOLE>(v, c)) s += exp2_fast(class_exponent<WHOLE>(v - top, c, kPowerLift));
         else if (v != v) s = v;
     }
-    template <class E, int J>
-    __device__ __forceinline__ void add_groups(const uint4 (&raw)[J], float c) {
+    template <class E, int J, bool WHOLE>
+    __device__ __forceinline__ void add_groups(const uint4 (&raw)[J], ClassScale c) {
         using G = ClassGroup<E>;
-        if (!raise(G::template largest<J>(raw), c)) {               // a NaN has to be seen all the same
+        if (!raise<WHOLE>(G::template largest<J>(raw), c)) {               // a NaN has to be seen all the same
 #pragma unroll
             for (int j = 0; j < J; ++j)
 #pragma unroll
@@ -255,20 +282,21 @@ struct ClassSum {
                 }
             return;
         }
-        const uint64_t c2 = f32x2_pack(c, c), top2 = f32x2_pack(-top, -top);
+        const uint64_t top2 = f32x2_pack(-top, -top);
         uint64_t part[2] = {0, 0};
 #pragma unroll
         for (int j = 0; j < J; ++j)
 #pragma unroll
-            for (int i = 0; i < G::P; ++i) part[i & 1] = f32x2_add(part[i & 1], class_powers(G::pair(raw[j], i), top2, c2));
+            for (int i = 0; i < G::P; ++i) part[i & 1] = f32x2_add(part[i & 1], class_powers<WHOLE>(G::pair(raw[j], i), top2, c));
         float lo, hi;
         f32x2_unpack(f32x2_add(part[0], part[1]), lo, hi);
         s += lo + hi;
     }
     // the sum over the lanes of a warp, the same bits in all of them
-    __device__ __forceinline__ void over_warp(float c) {
+    template <bool WHOLE>
+    __device__ __forceinline__ void over_warp(ClassScale c) {
         const float most = warp_largest(top);
-        s = s == 0.0f ? 0.0f : s * class_carry(top, most, c);       // (a NaN stays one)
+        s = s == 0.0f ? 0.0f : s * class_carry<WHOLE>(top, most, c);       // (a NaN stays one)
         top = most;
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
@@ -905,6 +933,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
     constexpr int N = G::N, J = R::kLaneGroups, kTeams = R::kTeams, kTeamWarps = R::kTeamWarps, kPassWarps = R::kPassWarps,
                   kNumberWarps = R::kNumberWarps, kRows = R::kRows, kWarpGroups = R::kWarpGroups, kStageGroups = R::kStageGroups,
                   kStageBytes = R::kStageBytes;
+    constexpr bool kWhole = MODE == kClassLogp;
     __shared__ typename R::Shared sh;
     extern __shared__ __align__(128) unsigned char class_smem[];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, depth = p.depth;
@@ -1028,9 +1057,9 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                     for (int j = 0; j < J; ++j)
                         if (32 * j + lane >= left) raw[j] = G::nothing();
                 }
-                sum.add_groups<E, J>(raw, p.c);
+                sum.add_groups<E, J, kWhole>(raw, p.cs);
             }
-            sum.over_warp(p.c);
+            sum.over_warp<kWhole>(p.cs);
             if (!GRAD && k >= kRows) wait(sh.ready + at, (k / kRows - 1) & 1);      // the sums of row k - kRows have been read
             if (lane == 0) {
                 sh.warp_sum[at][in_team] = make_float2(sum.top, sum.s);
@@ -1131,8 +1160,8 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
             if (!wait(sh.summed + at, parity)) break;
             ClassSum sum;
             if (lane < kTeamWarps) sum = ClassSum{sh.warp_sum[at][lane].x, sh.warp_sum[at][lane].y};
-            if (edges) sum.add(edge, p.c);
-            sum.over_warp(p.c);
+            if (edges) sum.add<kWhole>(edge, p.cs);
+            sum.over_warp<kWhole>(p.cs);
             if (C > 1) {
                 // The gradient may replace the logits, and a CTA that has all sums writes over the target's: what this one reads of the row has to be
                 // here before its sum goes out.  Edges are in the sum and a teacher's classes in shared memory; the target's logit is
@@ -1145,7 +1174,7 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
                 if (!wait(sh.joined + at2, (k / (2 * kRows)) & 1)) break;
                 sum = ClassSum{};
                 if (lane < C) sum = ClassSum{sh.cta_sum[at2][lane].x, sh.cta_sum[at2][lane].y};
-                sum.over_warp(p.c);
+                sum.over_warp<kWhole>(p.cs);
             }
             sum.settle();
             ClassNumbers now{};
@@ -1287,9 +1316,9 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
             ClassSum sum;
 #pragma unroll
             for (int b = 0; b < J / B; ++b)
-                if (32 * B * b < row.groups) sum.add_groups<E, B>(reinterpret_cast<const uint4(&)[B]>(now.raw[B * b]), p.c);
-            if (lane < row.edges) sum.add(now.edge, p.c);
-            sum.over_warp(p.c);
+                if (32 * B * b < row.groups) sum.add_groups<E, B, false>(reinterpret_cast<const uint4(&)[B]>(now.raw[B * b]), p.cs);
+            if (lane < row.edges) sum.add<false>(now.edge, p.cs);
+            sum.over_warp<false>(p.cs);
             sum.settle();
             ClassTerms terms;
             const ClassNumbers numbers = class_numbers<MODE>(p, now.in, sum, inv, terms);

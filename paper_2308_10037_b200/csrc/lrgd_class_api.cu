@@ -3,6 +3,7 @@
 #include "../../include/lrgd.h"
 
 #include <cmath>
+#include <limits>
 #include <type_traits>
 
 #include "lrgd_class.cuh"
@@ -26,6 +27,14 @@ size_t up256(size_t b) { return (b + 255) / 256 * 256; }
 
 double class_c64(float scale) { return double(scale) * 1.4426950408889634074; }            // scale * log2(e)
 float class_c(float scale) { return float(class_c64(scale)); }
+ClassScale class_scale(float scale) {
+    const double c64 = class_c64(scale);
+    ClassScale s{};
+    s.c = s.down = float(c64);
+    if (double(s.down) > c64) s.down = std::nextafter(s.down, 0.0f);
+    s.rest = std::max(float(c64 - double(s.down)), std::numeric_limits<float>::denorm_min());
+    return s;
+}
 
 int check_rows(int64_t T, int32_t V, int64_t ld, int32_t id_bytes, float scale) {
     if (T < 0 || T > kMaxRows || V < 1 || V > kMaxClasses || ld < V || ld > kMaxPitch) return LR_ERR_SHAPE;
@@ -229,6 +238,7 @@ ClassParams row_params(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, in
     p.scale = scale;
     p.c = class_c(scale);
     p.c64 = class_c64(scale);
+    p.cs = class_scale(scale);
     p.status = ctx->d_status + 1;
     return p;
 }

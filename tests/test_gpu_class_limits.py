@@ -315,12 +315,14 @@ def nearly_exact_scale():
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("V", [500, 4096, 9001])
-def test_errors_of_a_long_sequence_cancel(ctx, dt, V):
+@pytest.mark.parametrize("V,scale", [(500, None), (4096, None), (9001, None), (9001, 1.0), (9001, 0.7), (32003, 1.25)])
+def test_errors_of_a_long_sequence_cancel(ctx, dt, V, scale):
     """The mean signed error of lp over many rows, of terms of every size and of equal ones: an error that all rows share would add up over a
     sequence.  lp is rounded to half a step of 2^-20 (3e-7 in the mean square), its sum and logarithm less: 4 / sqrt(8192) of it is 1.3e-8; the
-    powers' mean error is 3e-9, and 3e-8 in the few terms above 1/2; the scale's 1e-9.  3e-8 in all; an uncorrected power gives 5e-8."""
-    T, scale = 8192, nearly_exact_scale()
+    powers' mean error is 3e-9, and 3e-8 in the few terms above 1/2; the scale's 1e-9 (long rows: any scale's, short ones: of one that is nearly
+    exact).  3e-8 in all; an uncorrected power gives 5e-8."""
+    scale = float(torch.tensor(scale or nearly_exact_scale(), dtype=torch.float32))
+    T = 8192
     y = torch.randint(0, V, (T,), generator=gen(1), device="cuda")
     kinds = {"random": 2.5 * rnd(T, V, seed=2), "near one another": 0.3 * rnd(T, V, seed=5), "of one value": rnd(T, 1, seed=3).expand(T, V).contiguous()}
     kinds["ties beside masked classes"] = kinds["of one value"].clone()
@@ -329,7 +331,7 @@ def test_errors_of_a_long_sequence_cancel(ctx, dt, V):
     for name, x in kinds.items():
         x = x.to(DT[dt])
         at = y if name in ("random", "near one another") else y % 2
-        want = torch.cat([torch.log_softmax(p.double() * scale, 1) for p in x.split(1024)])[torch.arange(T, device="cuda"), at]
+        want = torch.cat([torch.log_softmax(p.double() * scale, 1).gather(1, i[:, None])[:, 0] for p, i in zip(x.split(512), at.split(512))])
         off = float((ctx.logp(x, at, scale=scale)[0].double() - want).mean())
         if name == "of one value":                  # (one number for all rows: its own rounding)
             assert abs(off) <= 0.5 * 2.0 ** -20 + 1e-7
