@@ -541,10 +541,9 @@ __device__ __forceinline__ bool class_mark(const ClassTop& top, int id) {
     return (atomicOr(top.marks + (h >> 5), bit) & bit) != 0;
 }
 
-// What the entries add up to.  The student's logits may be as far apart as fp32 allows (masked by the lowest value): their sum is kept small.
-constexpr float kFar = 4096.0f;
+// What the entries add up to, in fp64: the divergence is a difference of sums of its size and larger.
 struct ClassTopSum {
-    float all, own, his;         // sum of q, of q * (v - base) * c, of q * (x - near) / kFar
+    double all, mixed;           // sum of q, of q * (scale * (v - base) - scale * (x - near))
     float near;                  // the largest of their x
     bool twice;                  // some class is named twice
 };
@@ -552,7 +551,7 @@ struct ClassTopSum {
 template <int U, class E>
 __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long long t, const E* row, const ClassTop& top) {
     const int lane = threadIdx.x & 31;
-    ClassTopSum r{0.0f, 0.0f, 0.0f, -INFINITY, false};
+    ClassTopSum r{0.0, 0.0, -INFINITY, false};
     float largest = -INFINITY;
     const float own = p.teacher_lse ? __ldg(p.teacher_lse + t) : 0.0f;
     for (int j0 = 0; j0 < p.K; j0 += 32 * U) {
@@ -593,28 +592,25 @@ __device__ __forceinline__ ClassTopSum class_top_read(const ClassParams& p, long
     largest = warp_max(largest);
     r.near = warp_max(r.near);
     if (r.near == -INFINITY) r.near = 0.0f;
-    // base is the largest v, or the teacher's own lse / scale in two parts
-    float high = largest == -INFINITY ? 0.0f : largest, low = 0.0f;
-    if (p.teacher_lse) {
-        const ClassBase base = class_base(own, p.scale, p.c64);
-        high = base.high;
-        low = base.low;
-    }
+    // base is the largest v, or the teacher's own lse / scale.  The exponent is fp64, its power fp32 (exp2f is good to 2 units of the last place)
+    // with what the fp32 exponent leaves.
+    const double base = p.teacher_lse ? static_cast<double>(own) / p.scale : largest == -INFINITY ? 0.0 : static_cast<double>(largest);
     for (int j = lane; j < p.K; j += 32) {
-        const float a = (top.q[j] - high) * p.c - low;
-        const float e = top.id[j] >= 0 ? exp2f(a) : 0.0f;
-        r.all += e;
-        if (e != 0.0f) {
-            r.own += e * a;
-            r.his += e * ((top.x[j] - r.near) * (1.0f / kFar));
+        const double a = (static_cast<double>(top.q[j]) - base) * p.c64;
+        const float near = static_cast<float>(a + kPowerLift), power = exp2f(near);         // (the lift as in class_power)
+        float e = 0.0f;
+        if (top.id[j] >= 0 && power != 0.0f) {
+            e = fmaf(power, static_cast<float>(a + kPowerLift - near) * static_cast<float>(kLn2), power);
+            r.all += e;
+            r.mixed += e * (kLn2 * a - static_cast<double>(top.x[j] - r.near) * p.scale);
         }
         top.q[j] = e;
     }
 #pragma unroll
     for (int d = 16; d >= 1; d >>= 1) {
-        r.all += __shfl_xor_sync(0xffffffffu, r.all, d);
-        r.own += __shfl_xor_sync(0xffffffffu, r.own, d);
-        r.his += __shfl_xor_sync(0xffffffffu, r.his, d);
+        const double all = __shfl_xor_sync(0xffffffffu, r.all, d), mixed = __shfl_xor_sync(0xffffffffu, r.mixed, d);
+        r.all += all;
+        r.mixed += mixed;
     }
     class_clear_marks(top);
     return r;
@@ -678,11 +674,16 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
     const float gain = static_cast<float>(in.w * inv * p.factor * p.scale);
     if (MODE == kClassDistill) {
         // with the teacher's own normalisation log q is smaller by log(all)
-        const float all = in.top.all, one = p.teacher_lse || all == 0.0f ? 1.0f : 1.0f / all, mass = p.teacher_lse || all == 0.0f ? all : 1.0f;
-        const double ahead = (static_cast<double>(sum.top) - in.top.near) * p.scale;
-        terms.kl = all == 0.0f ? 0.0f
-                               : static_cast<float>((kLn2 * in.top.own - static_cast<double>(in.top.his) * kFar * p.scale) * one +
-                                                    mass * (ahead + log_s + logf(one)));
+        const float all = static_cast<float>(in.top.all), one = p.teacher_lse || all == 0.0f ? 1.0f : 1.0f / all, mass = p.teacher_lse || all == 0.0f ? all : 1.0f;
+        const double ahead = (static_cast<double>(sum.top) - in.top.near) * p.scale + log_s;
+        if (all == 0.0f) {
+            terms.kl = 0.0f;
+        } else if (p.teacher_lse) {
+            terms.kl = static_cast<float>(in.top.mixed + in.top.all * ahead);
+        } else {                                    // (1 / all to fp64: a step of Newton's)
+            const double whole = one * (2.0 - in.top.all * one);
+            terms.kl = static_cast<float>(in.top.mixed * whole + ahead - logf(all));
+        }
         r.factor = mass == 0.0f ? 0.0f : gain * mass / sum.s;
         r.at = gain * one;
         return r;

@@ -337,3 +337,25 @@ def test_errors_of_a_long_sequence_cancel(ctx, dt, V, scale):
             assert abs(off) <= 0.5 * 2.0 ** -20 + 1e-7
         else:
             assert abs(off) <= 3e-8, (name, off)
+
+
+@pytest.mark.parametrize("part", [False, True])
+@pytest.mark.parametrize("V,K", [(900, 200), (40000, 200), (40000, 1024)])
+def test_the_divergence_has_the_bits_of_its_terms(ctx, V, K, part):
+    """Errors of the rows' divergences over 400 rows, student and teacher far apart, in the mean square and relative to the sum of the magnitudes m
+    (10 or more times the mass).  An entry's power is off by 1u in the mean square, which the few entries that matter average to 0.5u; the student's
+    log-sum-exp by a logarithm good to 1u and by scale * log2(e) in fp32, u / 2 of a distance of up to 15: 0.8u of m in all; the result's own
+    rounding is less than 0.3u of m.  Together 1u; 1.2u is asked for.  A teacher's exponent held in fp32 alone, 5 to 20 in size, is off by u / 2
+    of itself from scale * log2(e) alone, for all entries alike: 2u of m and more where nothing divides it away."""
+    T, scale = 400, 0.9
+    x, t = 2.5 * rnd(T, V, seed=1), -20 * torch.rand(T, K, generator=gen(2), device="cuda") + 40 * rnd(T, 1, seed=3)
+    ids = torch.stack([torch.randperm(V, generator=gen(10 + i), device="cuda")[:K] for i in range(T)])
+    s = float(torch.tensor(scale, dtype=torch.float32))
+    z = t.double() * s
+    tlse = (torch.logsumexp(z, 1) + 0.3).float() if part else None
+    logq = z - (tlse.double()[:, None] if part else torch.logsumexp(z, 1, keepdim=True))
+    lp = torch.log_softmax(x.double() * s, 1).gather(1, ids)
+    want = (logq.exp() * (logq - lp)).sum(1)
+    m = (logq.exp() * (logq.abs() + lp.abs())).sum(1)
+    off = (ctx.distill_loss(x, ids, t, tlse, scale=scale, grad=False)[1].double() - want) / m
+    assert float(off.square().mean().sqrt()) <= 1.2 * U
