@@ -59,6 +59,7 @@ struct ClassParams {
     const float* old_logp;
     const float* ref_logp;
     float ratio_low, ratio_high, kl_coef;
+    double log_low, log_high;    // of 1 - clip_low (-inf where that is not above 0) and 1 + clip_high
     // distillation
     const void* teacher;
     int teacher_half;            // bfloat16
@@ -698,8 +699,11 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
         float ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0, W) + 1.0f : 1.0f;
         if (ratio > 3.4e38f) ratio = 3.4e38f;       // (no infinity: an advantage of 0 has no loss whatever the ratio)
         const float away = __shfl_sync(0xffffffffu, e, 1, W), rest = __shfl_sync(0xffffffffu, e, 2, W);
-        const float a = in.adv, held = fminf(fmaxf(ratio, p.ratio_low), p.ratio_high);
-        const bool clipped = ratio * a > held * a;
+        // r A > r' A: the ratio is past the border on the side that A pulls to.  Decided on its fp64 logarithm, because a row gains or loses all of
+        // its gradient there.
+        const float a = in.adv, held = a > 0.0f ? p.ratio_high : p.ratio_low;
+        const double log_ratio = p.old_logp ? terms.lp - in.old_logp : 0.0;
+        const bool clipped = a > 0.0f ? log_ratio > p.log_high : a < 0.0f && log_ratio < p.log_low;
         float g = clipped ? 0.0f : class_held(-ratio * a);
         if (p.ref_logp && p.kl_coef != 0.0f) g -= class_held(p.kl_coef * away);
         terms.first = -(clipped ? held : ratio) * a;

@@ -345,6 +345,8 @@ int policy_impl(lr_ctx* ctx, const E* d_logits, int64_t ld, int64_t T, int32_t V
     p.ref_logp = d_ref_logp;
     p.ratio_low = float(1.0 - double(opt->clip_low));
     p.ratio_high = float(1.0 + double(opt->clip_high));
+    p.log_low = opt->clip_low < 1.0f ? std::log1p(-double(opt->clip_low)) : -INFINITY;
+    p.log_high = std::log1p(double(opt->clip_high));
     p.kl_coef = opt->kl_coef;
     p.norm = opt->norm;
     p.factor = opt->factor;

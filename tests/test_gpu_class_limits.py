@@ -359,3 +359,29 @@ def test_the_divergence_has_the_bits_of_its_terms(ctx, V, K, part):
     m = (logq.exp() * (logq.abs() + lp.abs())).sum(1)
     off = (ctx.distill_loss(x, ids, t, tlse, scale=scale, grad=False)[1].double() - want) / m
     assert float(off.square().mean().sqrt()) <= 1.2 * U
+
+
+# ---- the clip's borders ----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(1, 3), (1200, 20), (2, 9000)])
+def test_rows_next_to_the_borders_of_the_clip(ctx, dt, T, V):
+    """Rows whose one class has log-probability 0, so that the ratio is exp(-old) to all bits: older scores one fp32 step after the other across
+    the logarithms of both borders, which are far closer to each other than fp32 ratios are."""
+    x = torch.full((T, V), -math.inf, device="cuda").to(DT[dt])
+    x[:, V // 2] = 1.0
+    y = torch.full((T,), V // 2, device="cuda")
+    clip_low, clip_high = 0.2, 0.25
+    low, high = (float(torch.tensor(c, dtype=torch.float32)) for c in (clip_low, clip_high))
+    for border, sign in ((math.log1p(high), 1.0), (math.log1p(-low), -1.0)):
+        old = torch.tensor(-border, dtype=torch.float32)
+        steps = [old]
+        for _ in range(5):
+            steps = [torch.nextafter(steps[0], torch.tensor(-10.0))] + steps + [torch.nextafter(steps[-1], torch.tensor(10.0))]
+        for o in steps:
+            stats = ctx.policy_loss(x, y, torch.full((T,), sign, device="cuda"), torch.full((T,), float(o), device="cuda"), clip_low=clip_low,
+                                    clip_high=clip_high)[0]
+            past = -float(o) > border if sign > 0 else -float(o) < border
+            assert float(stats[3]) == float(past), (float(o), border)
+            assert float(ctx.policy_loss(x, y, torch.full((T,), -sign, device="cuda"), torch.full((T,), float(o), device="cuda"), clip_low=clip_low,
+                                         clip_high=clip_high)[0][3]) == 0.0
