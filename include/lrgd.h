@@ -560,7 +560,7 @@ int lr_ckpt8_grad_bf16(lr_ctx* ctx, const int8_t* d_q, int64_t ld_q, const float
  * left out, its log-probability and its gradient are 0.  A target outside [0, V) that is not ignore_id is treated the same way and sets
  * the device status word to LR_ERR_VALUE (lr_last_device_status).  Nor does a row count whose weight is 0.
  * A row of logits may hold -inf (a class that is masked) and be anywhere in the type's range (a row of the lowest value is uniform); a NaN, a
- * +inf or nothing but -inf makes what the row enters NaN.
+ * +inf or nothing but -inf makes what the row enters NaN (but for the lse of the last, which is -inf).
  * A loss is factor * sum of weight * (row's or pair's loss) / norm; norm = 0 stands for the sum of the weights that count (their number without
  * weights), and where that is 0 the loss and the gradient are 0.  factor carries a gradient from further up, or a share of a larger batch.
  * Sums of a row are fp32, its logarithm and sums over rows fp64; results are bit-reproducible (on GPUs with the same number of SMs).

@@ -491,7 +491,8 @@ __device__ __forceinline__ void class_clear_marks(const ClassTop& top) {
     for (int i = threadIdx.x & 31; i < (1 << top.bits) / 128; i += 32) reinterpret_cast<uint4*>(top.marks)[i] = make_uint4(0, 0, 0, 0);
     __syncwarp();
 }
-// Asks for a row's classes and the teacher's logits to be in L2 (2048 x 100000 fp32, 128 classes: 307 -> 297 us)
+// Asks for a row's classes and the teacher's logits to be in L2 (4096 x 128000 bfloat16, 256 classes: 418 us without, 414 with; up to 128 classes the
+// same)
 __device__ __forceinline__ void class_top_ahead(const ClassParams& p, long long t) {
     const int id_bytes = p.K * (p.wide_ids ? 8 : 4), v_bytes = p.K * (p.teacher_half ? 2 : 4);
     const char* ids = static_cast<const char*>(p.ids) + t * id_bytes;
@@ -499,8 +500,9 @@ __device__ __forceinline__ void class_top_ahead(const ClassParams& p, long long 
     for (int b = 128 * (threadIdx.x & 31); b < id_bytes; b += 128 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(ids + b));
     for (int b = 128 * (threadIdx.x & 31); b < v_bytes; b += 128 * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(v + b));
 }
-// ... and the logits at them, by the CTAs of a cluster together, each of which will read them all (2048 x 100000 fp32, 256 classes: 332 -> 309
-// us; 4096 x 128000 bfloat16, 128 classes: 364 -> 359; a CTA alone would ask for what it reads next: no faster)
+// ... and the logits at them, by the CTAs of a cluster together, each of which will read them all (2048 x 100000 fp32, 256 classes: 331 us without, 302
+// with; 128 classes 302 and 290; 4096 x 128000 bfloat16, 256 classes 424 and 414, 64 classes 372 and 374; a CTA alone would ask for what it reads
+// next)
 template <class E>
 __device__ __forceinline__ void class_top_logits_ahead(const ClassParams& p, long long t, int rank) {
     const E* row = static_cast<const E*>(p.x) + t * p.ld;
@@ -693,7 +695,7 @@ __device__ __forceinline__ ClassNumbers class_numbers(const ClassParams& p, cons
     if (terms.lp > 0.0) terms.lp = 0.0;             // rounding
     if (MODE == kClassPolicy) {
         // exp(lp - old) - 1, exp(ref - lp) - 1 and exp(lp) - 1: one lane each.  The differences are fp64, their exponentials fp32 (one unit in
-        // the last place).
+        // the last place), which is what outputs in fp32 show.
         const float d = static_cast<float>(lane == 0 ? terms.lp - in.old_logp : lane == 1 ? in.ref_logp - terms.lp : terms.lp);
         const float e = expm1f(d);
         float ratio = p.old_logp ? __shfl_sync(0xffffffffu, e, 0, W) + 1.0f : 1.0f;
@@ -809,15 +811,14 @@ __device__ __forceinline__ void class_finish(const ClassParams& p, int me, int c
 //     of the memory system that the others wait in).
 // The logits stay in the ring between the passes, so they are read once: the host takes clusters so large that two thirds of a row fit.
 // Stages that the ring could not hold are copied once more (`dropped`), from L2.  Stages are given back in the order of the copies.
-// Bound by HBM for log-probabilities (6.6 TB/s); with a gradient by HBM and by the waits between the passes: 52 % of the issue slots and 56 % of
-// the unit for powers are busy (a quarter of the powers on the FMA pipe instead was no faster), 132 of 148 SMs where a row takes four CTAs.
-// 8192 x 128000 bfloat16, three quarters counting, policy loss 661 us (5.6 TB/s; 693 to 707 under the power cap of a long run); 4096 x 128000, 64
-// classes of a teacher 372 us (5.6); 2048 x 100000 fp32, 256 classes 299 us (5.2: bound by the number warps).
-// Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist (6000 x 100000 fp32 290 us
-// instead of 303 with stages of 16 KB).  The policy loss: four teams hide one another's waits better (8192 x 128000 bfloat16 650 us; two teams
-// 690, three 715, five of three warps 839).  Distillation: the teacher's classes take the room of a stage, and every row more of the number
-// warps' time, so there are two teams (4096 x 128000, 64 classes: nine warps a team 375 us, eight 392; three teams 495, four teams with eight
-// number warps 419).
+// Bound by HBM for log-probabilities (6000 x 100000 fp32, 80 % counting, 290 us: 6.6 TB/s); with a gradient by HBM and by the waits between the passes:
+// 52 % of the issue slots and 56 % of the unit for powers are busy, 132 of 148 SMs work where a row takes four CTAs.  8192 x 128000 bfloat16, three
+// quarters counting, policy loss 664 us (5.5 TB/s; 714 under the power cap of a long run); 4096 x 128000, 64 classes of a teacher 375 us (5.6);
+// 2048 x 100000 fp32, 256 classes 302 us (5.2: bound by the number warps).
+// Who shares the work, by what is asked for.  Log-probabilities alone: large stages, the second pass does not exist.  The policy loss: four teams, which
+// hide one another's waits better than two (in the kernel's first form 650 us instead of 690; three 715, five of three warps 839).
+// Distillation: the teacher's classes take the room of a stage, and every row more of the number warps' time, so there are two teams, of
+// nine warps (375 us; of eight 380).
 constexpr int kMaxCluster = 8;
 
 // Up to this many rows the CTAs look all of them over themselves, which takes as long as a launch of k_class_prep less (T = 300: 2 us).
@@ -834,7 +835,7 @@ struct Ring {
     static constexpr int kTeams = MODE == kClassPolicy ? 4 : 2;
     static constexpr int kTeamWarps = MODE == kClassPolicy ? 4 : MODE == kClassDistill ? 9 : 8;
     static constexpr int kPassWarps = kTeams * kTeamWarps;
-    static constexpr int kNumberWarps = 4;          // (eight are no faster: policy 647 us, distillation 402)
+    static constexpr int kNumberWarps = 4;          // (eight: policy 672 us instead of 664, distillation 403 instead of 375, of 256 classes 326 instead of 303)
     static constexpr int kThreads = 32 * (kPassWarps + kTeams + kNumberWarps);
     static constexpr int kLaneGroups = MODE == kClassLogp ? 8 : 4;              // of a stage
     static constexpr int kWarpGroups = 32 * kLaneGroups;
@@ -1221,9 +1222,10 @@ __global__ void __launch_bounds__(Ring<MODE>::kThreads, 1) k_class_ring(const __
 
 // ---- short rows ----------------------------------------------------------------------------------------
 // A warp per row, the row in its registers between the passes: no barrier, no shared memory but for a teacher's classes.  Up to four groups a
-// lane the next row's logits are on their way meanwhile, and always its target.  Bound by instructions: about 600 a row beside 8 a logit and lane
-// (its numbers, set up and stored by a whole warp), which k_class_bundle shares among rows of up to 1024 logits where there are many.  32768 rows
-// of 1000 bfloat16: distillation of 16 classes 55 us; of 2000, log-probabilities 32 (4.1 TB/s); of 4000, policy loss 121 (4.1 TB/s).
+// lane the next row's logits are on their way meanwhile, and always its target.  A row takes about 600 instructions beside 8 a logit and lane
+// (its numbers, set up and stored by a whole warp), which k_class_bundle shares among rows of up to 1024 logits where there are many; they
+// depend on one another, and 16 to 32 warps an SM do not hide that.  32768 rows of 1000 bfloat16: distillation of 16 classes 54 us (its bytes
+// take 21); of 2000, log-probabilities 34 (20); of 4000, policy loss 121 (80).
 constexpr int kShortWarps = 8;
 __host__ __device__ constexpr int short_ctas(int mode, int J) { return J <= 2 && mode != kClassDistill ? 4 : J <= 8 ? 3 : 2; }       // per SM, in registers
 
@@ -1368,8 +1370,9 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
 }
 
 // R rows per warp and turn: their numbers are worked out at the same time, by 32 / R lanes each, which the sums reach by exchanging halves; a row's
-// terms stay in registers for the gradient, 64 a lane at most.  Bound by instructions and by the two loads in turn of a row's target and logits:
-// 32768 rows of 1000 bfloat16, policy loss 40 us (a warp per row: 53); of 200, 22 (33); of 256, log-probabilities 9.2 (15.4).  With rows for one
+// terms stay in registers for the gradient, 64 a lane at most.  Bound by waiting: a turn loads its rows' logits after their targets, nothing of the
+// next turn but its targets is on the way, 16 warps an SM have no other work, and no unit is full (powers 32 %, ALU 37 %).  32768 rows of 1000
+// bfloat16, policy loss 41 us (a warp per row: 53; its bytes take 20); of 200, 21 (33; 4); of 256, log-probabilities 9.8 (15.4; 2.6).  With rows for one
 // CTA per SM or less a warp per row is faster (500 bfloat16, policy loss: 64 rows 7.1 us instead of 8.9, 600 rows 8.2 instead of 9.1, 2000 rows
 // 11.5 instead of 11.2, 4000 rows 14.1 instead of 11.7).  Three CTAs per SM spill with a gradient (32768 x 1000: 55 us).
 template <class E>
@@ -1513,7 +1516,7 @@ __global__ void __launch_bounds__(kNormThreads) k_class_norm(const __grid_consta
 // ---- gradient of log-probabilities ---------------------------------------------------------------------
 // Rows whose statistics are known: from the caller (lse, fp32) or from an earlier pass (top and s).  One read, one write: bound by HBM.  A CTA
 // takes 16 KB of a row at a time, all loads on their way before the first power (with two groups a thread 444 us instead of 349), and steps
-// through the pieces without a division (336).  8192 x 65536 bfloat16 335 us, 6.4 TB/s; under the power cap of a long run 362.
+// through the pieces without a division.  8192 x 65536 bfloat16 337 us, 6.4 TB/s; under the power cap of a long run 373.
 struct ClassGradParams {
     const void* x;
     long long ld;

@@ -76,9 +76,9 @@ RowPlan plan_rows(const lr_ctx* ctx, int64_t T, int64_t V, int64_t es, bool grad
         for (r.lane_groups = 1; 32 * r.lane_groups < groups;) r.lane_groups *= 2;
         return r;
     }
-    // Two thirds of a row have to fit into a team's ring (the rest is copied twice, and found in L2 the second time; 2000 x 160000 bfloat16,
-    // distillation: 241 us, 297 with three quarters, which takes eight CTAs instead of four; 2048 x 100000 fp32: 276, 302 with a half), or as
-    // many CTAs take a row as there are SMs for, if rows are few
+    // Two thirds of a row have to fit into a team's ring (the rest is copied twice, and found in L2 the second time), or as many CTAs take a row
+    // as there are SMs for, if rows are few.  Distillation, 2000 x 160000 bfloat16, 64 classes: 246 to 258 us, 303 with three quarters, which
+    // takes eight CTAs instead of four; 4096 x 128000, 256 classes: 415, 607; 2048 x 100000 fp32, 128 classes: 290, 314 with a half.
     const int64_t stages = (groups + Ring<MODE>::kStageGroups - 1) / Ring<MODE>::kStageGroups;
     auto per_cta = [&] { return (stages + r.cluster - 1) / r.cluster; };
     while (r.cluster < kMaxCluster && ((grad && 2 * per_cta() > 3 * depth) || (r.cluster * 2 * T <= sms && r.cluster < stages))) r.cluster *= 2;
