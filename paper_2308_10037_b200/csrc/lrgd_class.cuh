@@ -1371,7 +1371,7 @@ __global__ void __launch_bounds__(kShortWarps * 32, short_ctas(MODE, J)) k_class
 
 // R rows per warp and turn: their numbers are worked out at the same time, by 32 / R lanes each, which the sums reach by exchanging halves; a row's
 // terms stay in registers for the gradient, 64 a lane at most.  Bound by waiting: a turn loads its rows' logits after their targets, nothing of the
-// next turn but its targets is on the way, 16 warps an SM have no other work, and no unit is full (powers 32 %, ALU 37 %).  32768 rows of 1000
+// next turn but its targets is on the way, 16 warps an SM have no other work, and no unit is full (powers 31 %, ALU 37 %).  32768 rows of 1000
 // bfloat16, policy loss 41 us (a warp per row: 53; its bytes take 20); of 200, 21 (33; 4); of 256, log-probabilities 9.8 (15.4; 2.6).  With rows for one
 // CTA per SM or less a warp per row is faster (500 bfloat16, policy loss: 64 rows 7.1 us instead of 8.9, 600 rows 8.2 instead of 9.1, 2000 rows
 // 11.5 instead of 11.2, 4000 rows 14.1 instead of 11.7).  Three CTAs per SM spill with a gradient (32768 x 1000: 55 us).
